@@ -377,6 +377,62 @@ int rib_last_path(void);
 long long rib_kernel_launches(void);
 
 /*
+ * Window attention with a learned bias for relative positions, in place of the rank-r tables:
+ *
+ *     S_ij = (q_i . k_j) / sqrt(d) + bias[h][u],      u = buckets[(y_j - y_i + M - 1) * (2M - 1) + x_j - x_i + M - 1],
+ *
+ * with (y, x) the place of a token inside its window.  `buckets` names a bucket for each of the (2M-1)^2 offsets (key minus
+ * query) and is the same for all heads; several offsets may share a bucket.  A key whose offset has a bucket outside
+ * [0, num_buckets) (-1, say) or a bias of -1e30 or less (minus infinity, the lowest value of a type) is not attended to.  A row that
+ * is left without any key gets out = 0 and lse = -infinity, and no gradient.  Other biases are finite.
+ *   bias     RIB_DTYPE_F32 or RIB_DTYPE_BF16, [heads][num_buckets], the heads' tables bias_head_stride (>= num_buckets) elements
+ *            apart; bias_head_stride = 0: one table [num_buckets] that all heads share.  Aligned to its element type.
+ *   buckets  int32 [2M-1][2M-1], 4-byte aligned.
+ * H and W need not be multiples of the window (rib_window_attn_fwd_padded says what happens then); with `masked` not 0 they have to
+ * be, and the wrapped parts of shifted windows do not attend to each other (rib_window_attn_fwd_masked).  Everything else is as
+ * for rib_window_attn_fwd.
+ *
+ * The backward pass recomputes the probabilities from lse.  dbias has bias's type and layout; it is the sum of dS over all windows
+ * and pairs of tokens whose offset has the bucket, and over the heads where they share a table.  Buckets that no offset
+ * names get 0.  Elements between the heads' tables are left as they are.
+ */
+enum { RIB_DTYPE_F32 = 0, RIB_DTYPE_BF16 = 1 };
+int rib_window_attn_fwd_bucketed(const void* q, const void* k, const void* v, const void* bias, int bias_dtype, long long bias_head_stride,
+                                 const int* buckets, int num_buckets,
+                                 int B, int H, int W, int heads, int d, int window, int shift, int masked,
+                                 void* out, float* lse, void* stream);
+size_t rib_window_attn_bwd_bucketed_workspace(long long bias_head_stride, int num_buckets, int B, int H, int W, int heads, int d, int window);
+int rib_window_attn_bwd_bucketed(const void* q, const void* k, const void* v, const void* bias, int bias_dtype, long long bias_head_stride,
+                                 const int* buckets, int num_buckets, const void* out, const float* lse, const void* dout,
+                                 int B, int H, int W, int heads, int d, int window, int shift, int masked,
+                                 void* dq, void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Activation checkpoints in 8 bits.  A row of d <= 64 bf16 channels (one token of one head) becomes d int8 codes and one fp32 scale,
+ *     scale = max|x| * (1/127),   code = round(x / scale)   (half to even),   restored x = bf16(code * scale).
+ * A row of zeros has scale 0.  A row that holds an infinity or a NaN has scale NaN and is restored as NaNs.  `rows` may be 0.
+ *   x bf16 [rows][d], codes int8 [rows][d], scales fp32 [rows]; all 16-byte aligned.
+ */
+int rib_checkpoint_store(const void* x, long long rows, int d, void* codes, float* scales, void* stream);
+int rib_checkpoint_restore(const void* codes, const float* scales, long long rows, int d, void* x, void* stream);
+
+/*
+ * The backward passes of a layer whose q, k, v and out (in this order in `saved`) are kept as checkpoints of
+ * B * H * W * heads rows each, in the layout of the tensors.  lse is the one of the forward pass; everything else is as for
+ * rib_window_attn_bwd_padded / _masked (pos_head_stride, masked) and rib_window_attn_bwd_bucketed.
+ */
+typedef struct rib_checkpoint { const void* codes; const float* scales; } rib_checkpoint;
+size_t rib_window_attn_bwd_checkpointed_workspace(long long pos_head_stride, int B, int H, int W, int heads, int d, int r, int window);
+int rib_window_attn_bwd_checkpointed(const rib_checkpoint* saved, const void* pq, const void* pk, long long pos_head_stride, const float* lse,
+                                     const void* dout, int B, int H, int W, int heads, int d, int r, int window, int shift, int masked,
+                                     void* dq, void* dk, void* dv, float* dpq, float* dpk, void* workspace, size_t workspace_bytes, void* stream);
+size_t rib_window_attn_bwd_bucketed_checkpointed_workspace(long long bias_head_stride, int num_buckets, int B, int H, int W, int heads, int d, int window);
+int rib_window_attn_bwd_bucketed_checkpointed(const rib_checkpoint* saved, const void* bias, int bias_dtype, long long bias_head_stride,
+                                              const int* buckets, int num_buckets, const float* lse, const void* dout,
+                                              int B, int H, int W, int heads, int d, int window, int shift, int masked,
+                                              void* dq, void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The tcgen05 kernels address their operands through TMA tensor maps, which depend on the base pointer and the
  * shape only; the library keeps 2048 of them (256 sets of 8, least recently asked for out first), more than both
  * passes of 64 layers need, so a call that repeats an earlier call's buffers and shape encodes none.  Writes how many maps were served from that cache (`hits`) and how many had to be encoded
@@ -399,7 +455,9 @@ enum { RIB_KERNEL_FWD_MAIN = 1, RIB_KERNEL_BWD_PREPARE = 2, RIB_KERNEL_BWD_MAIN 
        RIB_KERNEL_ANY_BWD_DKV = 9, RIB_KERNEL_GENERATOR_FWD = 10, RIB_KERNEL_GENERATOR_BWD = 11,
     RIB_KERNEL_CLA_GATE = 12, RIB_KERNEL_CLA_BWD_PW = 13, RIB_KERNEL_CLA_BWD_DW = 14, RIB_KERNEL_CLA_PRODUCT = 15, RIB_KERNEL_CLA_BWD_TC = 16,
     RIB_KERNEL_FWD_FRAME = 17, RIB_KERNEL_WINDOW8_FWD = 18, RIB_KERNEL_WINDOW8_CLEAR = 19, RIB_KERNEL_WINDOW8_BWD = 20,
-    RIB_KERNEL_WINDOW16_FWD = 21, RIB_KERNEL_WINDOW16_CLEAR = 22, RIB_KERNEL_WINDOW16_BWD = 23, RIB_KERNEL_GENERATOR_CLEAR = 24 };
+    RIB_KERNEL_WINDOW16_FWD = 21, RIB_KERNEL_WINDOW16_CLEAR = 22, RIB_KERNEL_WINDOW16_BWD = 23, RIB_KERNEL_GENERATOR_CLEAR = 24,
+    RIB_KERNEL_BIAS_FINISH = 25, RIB_KERNEL_CHECKPOINT_STORE = 26, RIB_KERNEL_CHECKPOINT_RESTORE = 27, RIB_KERNEL_BIAS_FWD = 28,
+    RIB_KERNEL_BIAS_BWD_PREPARE = 29, RIB_KERNEL_BIAS_BWD = 30, RIB_KERNEL_BIAS_BWD_FINISH = 31 };
 int rib_profile_begin(int max_launches);
 int rib_profile_end(int* kernel_ids, float* ms, int capacity);
 

@@ -56,6 +56,10 @@ EXPORTS = (
     "rib_window_attn_fwd_masked", "rib_window_attn_bwd_masked", "rib_window_cycle_bwd", "rib_window_cycle_bwd_workspace",
     "rib_cla_product", "rib_cla_product_bwd", "rib_cla_gate_bwd", "rib_cla_gate_bwd_workspace",
     "rib_wait_probe", "rib_exp_probe", "rib_tensor_map_cache_counts", "rib_window_cycle_fwd",
+    "rib_window_attn_fwd_bucketed", "rib_window_attn_bwd_bucketed", "rib_window_attn_bwd_bucketed_workspace",
+    "rib_checkpoint_store", "rib_checkpoint_restore",
+    "rib_window_attn_bwd_checkpointed", "rib_window_attn_bwd_checkpointed_workspace",
+    "rib_window_attn_bwd_bucketed_checkpointed", "rib_window_attn_bwd_bucketed_checkpointed_workspace",
 )
 KERNEL_NAMES = {1: "rib_fwd_sm100_kernel", 2: "rib_bwd_prepare_kernel", 3: "rib_bwd_sm100_kernel",
                 4: "rib_bwd_finish_kernel", 6: "generic_fwd_kernel",
@@ -63,7 +67,10 @@ KERNEL_NAMES = {1: "rib_fwd_sm100_kernel", 2: "rib_bwd_prepare_kernel", 3: "rib_
                 10: "rib_generator_fwd_kernel", 11: "rib_generator_bwd_kernel", 12: "rib_cla_gate_kernel",
                 13: "rib_cla_bwd_pw_kernel", 14: "rib_cla_bwd_dw_kernel", 15: "rib_cla_product_kernel", 16: "rib_cla_bwd_tc_kernel",
                 17: "rib_fwd_frame_sm100_kernel", 18: "rib_window8_fwd_kernel", 19: "rib_window8_clear_kernel", 20: "rib_window8_bwd_kernel",
-                21: "rib_window16_fwd_kernel", 22: "rib_window16_clear_kernel", 23: "rib_window16_bwd_kernel", 24: "rib_generator_clear_kernel"}
+                21: "rib_window16_fwd_kernel", 22: "rib_window16_clear_kernel", 23: "rib_window16_bwd_kernel", 24: "rib_generator_clear_kernel",
+                25: "rib_bias_finish_kernel", 26: "rib_checkpoint_store_kernel", 27: "rib_checkpoint_restore_kernel", 28: "rib_bias_fwd_kernel",
+                29: "rib_bias_bwd_prepare_kernel", 30: "rib_bias_bwd_kernel", 31: "rib_bias_bwd_finish_kernel"}
+RIB_DTYPE_F32, RIB_DTYPE_BF16 = 0, 1
 RIB_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 
@@ -153,6 +160,25 @@ def library() -> ctypes.CDLL:
         lib.rib_wait_probe.argtypes = [ctypes.c_ulonglong, vp]
         lib.rib_exp_probe.restype = ctypes.c_longlong
         lib.rib_exp_probe.argtypes = [vp, ci, ci, vp]
+        size = ctypes.c_size_t
+        lib.rib_window_attn_fwd_bucketed.restype = ci
+        lib.rib_window_attn_fwd_bucketed.argtypes = [vp] * 4 + [ci, ll, vp, ci] + [ci] * 8 + [vp, fp, vp]
+        lib.rib_window_attn_bwd_bucketed.restype = ci
+        lib.rib_window_attn_bwd_bucketed.argtypes = [vp] * 4 + [ci, ll, vp, ci] + [vp] * 3 + [ci] * 8 + [vp] * 5 + [size, vp]
+        lib.rib_window_attn_bwd_bucketed_workspace.restype = size
+        lib.rib_window_attn_bwd_bucketed_workspace.argtypes = [ll] + [ci] * 7
+        lib.rib_checkpoint_store.restype = ci
+        lib.rib_checkpoint_store.argtypes = [vp, ll, ci, vp, vp, vp]
+        lib.rib_checkpoint_restore.restype = ci
+        lib.rib_checkpoint_restore.argtypes = [vp, vp, ll, ci, vp, vp]
+        lib.rib_window_attn_bwd_checkpointed.restype = ci
+        lib.rib_window_attn_bwd_checkpointed.argtypes = [vp] * 3 + [ll, vp, vp] + [ci] * 9 + [vp] * 6 + [size, vp]
+        lib.rib_window_attn_bwd_checkpointed_workspace.restype = size
+        lib.rib_window_attn_bwd_checkpointed_workspace.argtypes = [ll] + [ci] * 7
+        lib.rib_window_attn_bwd_bucketed_checkpointed.restype = ci
+        lib.rib_window_attn_bwd_bucketed_checkpointed.argtypes = [vp, vp, ci, ll, vp, ci, vp, vp] + [ci] * 8 + [vp] * 5 + [size, vp]
+        lib.rib_window_attn_bwd_bucketed_checkpointed_workspace.restype = size
+        lib.rib_window_attn_bwd_bucketed_checkpointed_workspace.argtypes = [ll] + [ci] * 7
         lib.rib_addresses = {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS}
         _lib = lib
     return _lib
@@ -686,6 +712,158 @@ def rib_window_attn_bwd_noalloc(q, k, v, pq, pk, out, lse, dout, dq, dk, dv, dpq
                                                _ptr(dv), _ptr(dpq), _ptr(dpk), _stream_ptr(stream))
     if rc != RIB_OK:
         raise RibError(rc)
+
+
+def _check_bias(bias, buckets, heads, window, device):
+    """(dtype, elements between the heads' tables, number of buckets) of a bias [heads, buckets] or [buckets] (shared by the heads)."""
+    if bias.dtype not in (torch.float32, torch.bfloat16) or not bias.is_contiguous() or bias.device != device:
+        raise ValueError("bias must be a contiguous float32 or bfloat16 tensor [heads, num_buckets] or [num_buckets] on q's device")
+    if bias.dim() not in (1, 2) or bias.shape[-1] < 1 or (bias.dim() == 2 and bias.shape[0] != heads):
+        raise ValueError(f"bias has shape {tuple(bias.shape)}, expected [{heads}, num_buckets] or [num_buckets]")
+    side = 2 * window - 1
+    if buckets.dtype != torch.int32 or not buckets.is_contiguous() or buckets.device != device or tuple(buckets.shape) != (side, side):
+        raise ValueError(f"buckets must be a contiguous int32 tensor [{side}, {side}] on q's device")
+    count = bias.shape[-1]
+    return RIB_DTYPE_BF16 if bias.dtype == torch.bfloat16 else RIB_DTYPE_F32, count if bias.dim() == 2 else 0, count
+
+
+def rib_window_attn_fwd_bucketed(q, k, v, bias, buckets, window, shift=0, masked=False, stream=None, want_lse=True):
+    """Forward pass with a learned bias for relative positions: bias fp32 or bf16 [heads, num_buckets] (or [num_buckets], shared by
+    the heads), buckets int32 [2 window - 1, 2 window - 1], the bucket of every offset key - query (outside [0, num_buckets): not
+    attended to).  Any H and W; `masked` keeps the wrapped parts of shifted windows apart (H, W multiples of the window).
+    Returns (out, lse)."""
+    _check_image("q", q)
+    B, H, W, heads, d = q.shape
+    _check_image("k", k, q.shape)
+    _check_image("v", v, q.shape)
+    dtype, stride, count = _check_bias(bias, buckets, heads, window, q.device)
+    out = torch.empty_like(q)
+    lse = torch.empty((B, heads, H, W), dtype=torch.float32, device=q.device) if want_lse else None
+    rc = library().rib_window_attn_fwd_bucketed(_ptr(q), _ptr(k), _ptr(v), _ptr(bias), dtype, stride, _ptr(buckets), count, B, H, W, heads, d,
+                                                window, shift, int(masked), _ptr(out), _ptr(lse), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return out, lse
+
+
+def _check_lse(lse, B, heads, H, W, device):
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (B, heads, H, W) or not lse.is_contiguous() or lse.device != device:
+        raise ValueError("lse must be a contiguous fp32 tensor [B,heads,H,W] on q's device")
+
+
+def rib_window_attn_bwd_bucketed_workspace(bias_head_stride, num_buckets, B, H, W, heads, d, window) -> int:
+    return int(library().rib_window_attn_bwd_bucketed_workspace(bias_head_stride, num_buckets, B, H, W, heads, d, window))
+
+
+def rib_window_attn_bwd_bucketed(q, k, v, bias, buckets, out, lse, dout, window, shift=0, masked=False, workspace=None, stream=None):
+    """Backward pass of rib_window_attn_fwd_bucketed.  Returns (dq, dk, dv bf16, dbias of bias's shape and type)."""
+    _check_image("q", q)
+    B, H, W, heads, d = q.shape
+    for name, t in (("k", k), ("v", v), ("out", out), ("dout", dout)):
+        _check_image(name, t, q.shape)
+    dtype, stride, count = _check_bias(bias, buckets, heads, window, q.device)
+    _check_lse(lse, B, heads, H, W, q.device)
+    if workspace is None:
+        need = rib_window_attn_bwd_bucketed_workspace(stride, count, B, H, W, heads, d, window)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    dq, dk, dv, dbias = torch.empty_like(q), torch.empty_like(q), torch.empty_like(q), torch.empty_like(bias)
+    rc = library().rib_window_attn_bwd_bucketed(_ptr(q), _ptr(k), _ptr(v), _ptr(bias), dtype, stride, _ptr(buckets), count, _ptr(out), _ptr(lse),
+                                                _ptr(dout), B, H, W, heads, d, window, shift, int(masked), _ptr(dq), _ptr(dk), _ptr(dv),
+                                                _ptr(dbias), _ptr(workspace), workspace.numel(), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return dq, dk, dv, dbias
+
+
+def rib_checkpoint_store(x, stream=None):
+    """x bf16 [..., d], d <= 64, as (codes int8 of x's shape, scales fp32 of x's shape without its last dimension)."""
+    if x.dtype != torch.bfloat16 or not x.is_cuda or not x.is_contiguous() or x.dim() < 1:
+        raise ValueError("x must be a contiguous CUDA bfloat16 tensor [..., d]")
+    d = x.shape[-1]
+    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    if x.numel() == 0 and 0 < d <= 64:
+        return codes, scales
+    rc = library().rib_checkpoint_store(_ptr(x), scales.numel(), d, _ptr(codes), _ptr(scales), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return codes, scales
+
+
+def _check_checkpoint(name, codes, scales, shape=None):
+    if codes.dtype != torch.int8 or not codes.is_cuda or not codes.is_contiguous() or codes.dim() < 1 or (shape is not None and tuple(codes.shape) != tuple(shape)):
+        raise ValueError(f"the codes of {name} must be a contiguous CUDA int8 tensor " + (f"of shape {tuple(shape)}" if shape is not None else "[..., d]"))
+    if scales.dtype != torch.float32 or not scales.is_contiguous() or scales.device != codes.device or scales.shape != codes.shape[:-1]:
+        raise ValueError(f"the scales of {name} must be a contiguous fp32 tensor of shape {tuple(codes.shape[:-1])} on the codes' device")
+
+
+def rib_checkpoint_restore(codes, scales, stream=None):
+    """What rib_checkpoint_store kept, as bf16."""
+    _check_checkpoint("x", codes, scales)
+    x = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device)
+    if x.numel() == 0 and 0 < codes.shape[-1] <= 64:
+        return x
+    rc = library().rib_checkpoint_restore(_ptr(codes), _ptr(scales), scales.numel(), codes.shape[-1], _ptr(x), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return x
+
+
+def _saved(q, k, v, out, dout):
+    """The C call's array of the checkpoints (codes, scales) of q, k, v and out."""
+    _check_image("dout", dout)
+    for name, pair in (("q", q), ("k", k), ("v", v), ("out", out)):
+        _check_checkpoint(name, *pair, shape=dout.shape)
+    return (ctypes.c_void_p * 8)(*[_ptr(t) for pair in (q, k, v, out) for t in pair])
+
+
+def rib_window_attn_bwd_checkpointed(q, k, v, out, pq, pk, lse, dout, window, shift=0, masked=False, workspace=None, stream=None):
+    """Backward pass of a layer that kept q, k, v and out as checkpoints (codes, scales); pq, pk [n, r] or [heads, n, r].  On a map whose
+    sides are not multiples of the window as rib_window_attn_bwd_padded, with `masked` as rib_window_attn_bwd_masked.
+    Returns (dq, dk, dv bf16, dpq, dpk fp32 of the shape of pq)."""
+    saved = _saved(q, k, v, out, dout)
+    B, H, W, heads, d = dout.shape
+    n = window * window
+    headwise = pq.dim() == 3
+    for name, t in (("pq", pq), ("pk", pk)):
+        if headwise:
+            _check_pos_headwise(name, t, heads, n)
+        else:
+            _check_pos(name, t, n)
+    r = pq.shape[-1]
+    stride = n * r if headwise else 0
+    _check_lse(lse, B, heads, H, W, dout.device)
+    if workspace is None:
+        need = int(library().rib_window_attn_bwd_checkpointed_workspace(stride, B, H, W, heads, d, r, window))
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dout.device)
+    dq, dk, dv = torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(dout)
+    dpq = torch.empty(tuple(pq.shape), dtype=torch.float32, device=dout.device)
+    dpk = torch.empty(tuple(pk.shape), dtype=torch.float32, device=dout.device)
+    rc = library().rib_window_attn_bwd_checkpointed(saved, _ptr(pq), _ptr(pk), stride, _ptr(lse), _ptr(dout), B, H, W, heads, d, r, window, shift,
+                                                    int(masked), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dpq), _ptr(dpk), _ptr(workspace),
+                                                    workspace.numel(), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return dq, dk, dv, dpq, dpk
+
+
+def rib_window_attn_bwd_bucketed_checkpointed(q, k, v, out, bias, buckets, lse, dout, window, shift=0, masked=False, workspace=None, stream=None):
+    """Backward pass of rib_window_attn_fwd_bucketed for a layer that kept q, k, v and out as checkpoints (codes, scales).
+    Returns (dq, dk, dv bf16, dbias of bias's shape and type)."""
+    saved = _saved(q, k, v, out, dout)
+    B, H, W, heads, d = dout.shape
+    dtype, stride, count = _check_bias(bias, buckets, heads, window, dout.device)
+    _check_lse(lse, B, heads, H, W, dout.device)
+    if workspace is None:
+        need = int(library().rib_window_attn_bwd_bucketed_checkpointed_workspace(stride, count, B, H, W, heads, d, window))
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dout.device)
+    dq, dk, dv, dbias = torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(bias)
+    rc = library().rib_window_attn_bwd_bucketed_checkpointed(saved, _ptr(bias), dtype, stride, _ptr(buckets), count, _ptr(lse), _ptr(dout), B, H, W,
+                                                             heads, d, window, shift, int(masked), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbias),
+                                                             _ptr(workspace), workspace.numel(), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return dq, dk, dv, dbias
 
 
 def _check_f32(name, t, shape):

@@ -60,9 +60,28 @@ void fill_shape(rib::Problem& p, int B, int H, int W, int heads, int d, int r, i
     p.pairs = B * p.nWy * p.nWx * heads;
 }
 
+// A learned bias by buckets, which takes the place of the rank-r tables (r = 0).
+struct BiasArgs { const void* table; int dtype; long long head_stride; const int* buckets; int num_buckets; };
+
+int check_bias(const BiasArgs& b)
+{
+    if (!b.table || !b.buckets) return RIB_ERR_NULL;
+    if (b.num_buckets <= 0 || b.head_stride < 0 || (b.head_stride && b.head_stride < b.num_buckets)) return RIB_ERR_SHAPE;
+    if (b.dtype != RIB_DTYPE_F32 && b.dtype != RIB_DTYPE_BF16) return RIB_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(b.table) & (b.dtype == RIB_DTYPE_F32 ? 3u : 1u)) return RIB_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(b.buckets) & 3u) return RIB_ERR_ALIGN;
+    return RIB_OK;
+}
+
+void fill_bias(rib::Problem& p, const BiasArgs& b)
+{
+    p.bias = b.table; p.bias_bf16 = b.dtype == RIB_DTYPE_BF16; p.bias_head_stride = b.head_stride;
+    p.buckets = b.buckets; p.num_buckets = b.num_buckets;
+}
+
 int fwd_impl(const void* q, const void* k, const void* v, const void* pq, const void* pk, long long pos_head_stride, const void* gate,
              int B, int H, int W, int heads, int d, int r, int window, int shift, void* out, float* lse, void* stream,
-             bool validate_only = false, bool masked = false);
+             bool validate_only = false, bool masked = false, const BiasArgs* bias = nullptr);
 
 int check_pos_stride(long long stride, int window, int r)
 {
@@ -325,7 +344,7 @@ namespace {
 
 int fwd_impl(const void* q, const void* k, const void* v, const void* pq, const void* pk, long long pos_head_stride, const void* gate,
              int B, int H, int W, int heads, int d, int r, int window, int shift, void* out, float* lse, void* stream, bool validate_only,
-             bool masked)
+             bool masked, const BiasArgs* bias)
 {
     if (!q || !k || !v || !out || (r > 0 && (!pq || !pk))) return RIB_ERR_NULL;
     if (int rc = check_shape(B, H, W, heads, d, r, window, shift, true)) return rc;
@@ -346,17 +365,18 @@ int fwd_impl(const void* q, const void* k, const void* v, const void* pq, const 
     p.pos_head_stride = pos_head_stride;
     p.gate = static_cast<const __nv_bfloat16*>(gate);
     p.masked = masked;
+    if (bias) fill_bias(p, *bias);
     if (int rc = device_status_ptr(&p.status)) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int forced = g_forced_path.load();
-    const bool frame = rib::sm100_frame_supported(p);
-    bool fast = forced != RIB_PATH_GENERIC && (frame || rib::sm100_fwd_supported(p));
+    const bool frame = !bias && rib::sm100_frame_supported(p);
+    bool fast = forced != RIB_PATH_GENERIC && !bias && (frame || rib::sm100_fwd_supported(p));
     p.exact_softmax = forced == RIB_PATH_SM100_EXACT;
     int launches = 1;
     cudaError_t e;
     if (fast) {
         e = frame ? rib::sm100_fwd_frame(p, st) : rib::sm100_fwd(p, st);
-    } else if (forced != RIB_PATH_GENERIC && rib::sm100_repack_fwd_supported(p)) {
+    } else if (forced != RIB_PATH_GENERIC && !bias && rib::sm100_repack_fwd_supported(p)) {
         // rows TMA cannot address (d = 30, r = 18, ...): the tensor-core kernels on zero-padded copies
         e = rib::sm100_fwd_repacked(p, st, &launches);
         fast = e == cudaSuccess;
@@ -436,12 +456,33 @@ size_t rib_window_attn_bwd_padded_workspace(long long pos_head_stride, int B, in
     return need;
 }
 
+}  // extern "C"
+
+namespace {
+
+struct BwdBias : BiasArgs { void* gradient; };
+
+// Scratch of a backward pass with a bias: what the attention kernels need, then the sums of the table's gradient.
+size_t bucketed_attention_bytes(int B, int H, int W, int heads) { return rowdot_bytes(B, H, W, heads); }
+
+size_t bucketed_workspace(long long bias_head_stride, int num_buckets, int B, int H, int W, int heads, int d, int window)
+{
+    if (check_shape(B, H, W, heads, d, 0, window, 0, true) != RIB_OK) return 0;
+    if (num_buckets <= 0 || bias_head_stride < 0 || (bias_head_stride && bias_head_stride < num_buckets)) return 0;
+    return bucketed_attention_bytes(B, H, W, heads) + rib::bias_grad_layout(heads, bias_head_stride ? heads : 1, window, num_buckets, nullptr).bytes;
+}
+
+}  // namespace
+
+extern "C" {
+
 static int bwd_impl(const void* q, const void* k, const void* v, const void* pq, const void* pk,
                     long long pos_head_stride,
                     const void* out, const float* lse, const void* dout,
                     int B, int H, int W, int heads, int d, int r, int window, int shift,
                     void* dq, void* dk, void* dv, float* dpq, float* dpk,
-                    void* workspace, size_t workspace_bytes, void* stream, bool masked, bool validate_only = false)
+                    void* workspace, size_t workspace_bytes, void* stream, bool masked, bool validate_only = false,
+                    const BwdBias* bias = nullptr)
 {
     if (!q || !k || !v || !out || !lse || !dout || !dq || !dk || !dv) return RIB_ERR_NULL;
     if (r > 0 && (!pq || !pk || !dpq || !dpk)) return RIB_ERR_NULL;
@@ -450,7 +491,8 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
     const void* ptrs[] = {q, k, v, pq, pk, out, lse, dout, dq, dk, dv, dpq, dpk};
     for (const void* ptr : ptrs)
         if (!aligned16(ptr)) return RIB_ERR_ALIGN;
-    const size_t need = rib_window_attn_bwd_padded_workspace(pos_head_stride, B, H, W, heads, d, r, window);
+    const size_t need = bias ? bucketed_workspace(bias->head_stride, bias->num_buckets, B, H, W, heads, d, window)
+                             : rib_window_attn_bwd_padded_workspace(pos_head_stride, B, H, W, heads, d, r, window);
     if (!workspace || workspace_bytes < need) return RIB_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return RIB_ERR_ALIGN;
     if (validate_only) return RIB_OK;
@@ -476,6 +518,19 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
     p.masked = masked;
     if (int rc = device_status_ptr(&p.status)) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (bias) {
+        fill_bias(p, *bias);
+        p.dbias = bias->gradient;
+        const rib::BiasGrad g = rib::bias_grad_layout(heads, rib::bias_tables(p), window, bias->num_buckets,
+                                                      static_cast<unsigned char*>(workspace) + bucketed_attention_bytes(B, H, W, heads));
+        cudaError_t e = rib::bias_grad_clear(g, st);
+        if (e == cudaSuccess) e = rib::generic_bwd(p, st, g.offsets);
+        if (e == cudaSuccess) e = rib::bias_grad_finish(p, g, st);
+        if (e != cudaSuccess) return RIB_ERR_CUDA;
+        t_last_path = RIB_PATH_GENERIC;
+        g_kernel_launches += 4;
+        return RIB_OK;
+    }
     const bool allowed = g_forced_path.load() != RIB_PATH_GENERIC;
     bool fast = allowed && rib::sm100_bwd_supported(p);
     int launches = fast ? rib::sm100_bwd_launches(p) : 3;          // any-shape kernels: rowdot, dq, dk/dv
@@ -561,6 +616,169 @@ int rib_window_attn_bwd_masked(const void* q, const void* k, const void* v, cons
     if (H > 0 && W > 0 && window > 0 && (H % window || W % window)) return RIB_ERR_SHAPE;
     return bwd_impl(q, k, v, pq, pk, pos_head_stride, out, lse, dout, B, H, W, heads, d, r, window, shift, dq, dk, dv, dpq, dpk,
                     workspace, workspace_bytes, stream, true);
+}
+
+int rib_window_attn_fwd_bucketed(const void* q, const void* k, const void* v, const void* bias, int bias_dtype, long long bias_head_stride,
+                                 const int* buckets, int num_buckets,
+                                 int B, int H, int W, int heads, int d, int window, int shift, int masked,
+                                 void* out, float* lse, void* stream)
+{
+    if (masked && H > 0 && W > 0 && window > 0 && (H % window || W % window)) return RIB_ERR_SHAPE;
+    const BiasArgs b{bias, bias_dtype, bias_head_stride, buckets, num_buckets};
+    if (int rc = check_bias(b)) return rc;
+    return fwd_impl(q, k, v, nullptr, nullptr, 0, nullptr, B, H, W, heads, d, 0, window, shift, out, lse, stream, false, masked != 0, &b);
+}
+
+size_t rib_window_attn_bwd_bucketed_workspace(long long bias_head_stride, int num_buckets, int B, int H, int W, int heads, int d, int window)
+{
+    return bucketed_workspace(bias_head_stride, num_buckets, B, H, W, heads, d, window);
+}
+
+}  // extern "C"
+
+namespace {
+
+// The bias of a backward call, checked.
+int bwd_bias(const void* bias, int dtype, long long head_stride, const int* buckets, int num_buckets, void* dbias, BwdBias* b)
+{
+    *b = BwdBias{{bias, dtype, head_stride, buckets, num_buckets}, dbias};
+    if (!dbias) return RIB_ERR_NULL;
+    if (int rc = check_bias(*b)) return rc;
+    return reinterpret_cast<uintptr_t>(dbias) & (dtype == RIB_DTYPE_F32 ? 3u : 1u) ? RIB_ERR_ALIGN : RIB_OK;
+}
+
+int check_checkpoint(const void* codes, const float* scales, long long rows, int d)
+{
+    if (!codes || !scales) return RIB_ERR_NULL;
+    if (rows < 0 || d <= 0) return RIB_ERR_SHAPE;
+    if (d > 64 || rows > (1ll << 31)) return RIB_ERR_UNSUPPORTED;
+    if (!aligned16(codes) || !aligned16(scales)) return RIB_ERR_ALIGN;
+    return RIB_OK;
+}
+
+size_t image_bytes(int B, int H, int W, int heads, int d) { return (2 * (size_t)B * H * W * heads * d + 255) & ~(size_t)255; }
+
+// A backward call from checkpoints: the four tensors come back as bf16 at the start of the workspace, what is behind them is the backward
+// pass's own.  Every check is made before the first launch (`validate_only` of the pass sees the addresses).
+struct Restored {
+    rib::CheckpointRows t[4];
+    long long rows;
+    int d;
+    void* rest;
+    size_t rest_bytes;
+};
+
+int plan_restore(const rib_checkpoint* saved, int B, int H, int W, int heads, int d, void* workspace, size_t workspace_bytes, Restored* r)
+{
+    if (!saved) return RIB_ERR_NULL;
+    if (B <= 0 || H <= 0 || W <= 0 || heads <= 0) return RIB_ERR_SHAPE;
+    r->rows = (long long)B * H * W * heads;
+    r->d = d;
+    for (int i = 0; i < 4; ++i)
+        if (int rc = check_checkpoint(saved[i].codes, saved[i].scales, r->rows, d)) return rc;
+    const size_t image = image_bytes(B, H, W, heads, d);
+    if (!workspace || workspace_bytes < 4 * image) return RIB_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return RIB_ERR_ALIGN;
+    unsigned char* at = static_cast<unsigned char*>(workspace);
+    for (int i = 0; i < 4; ++i, at += image)
+        r->t[i] = {static_cast<const int8_t*>(saved[i].codes), saved[i].scales, reinterpret_cast<__nv_bfloat16*>(at)};
+    r->rest = at;
+    r->rest_bytes = workspace_bytes - 4 * image;
+    return RIB_OK;
+}
+
+int restore(const Restored& r, void* stream)
+{
+    if (rib::checkpoint_restore(r.t, 4, r.rows, r.d, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RIB_ERR_CUDA;
+    g_kernel_launches += 1;
+    return RIB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rib_window_attn_bwd_bucketed(const void* q, const void* k, const void* v, const void* bias, int bias_dtype, long long bias_head_stride,
+                                 const int* buckets, int num_buckets, const void* out, const float* lse, const void* dout,
+                                 int B, int H, int W, int heads, int d, int window, int shift, int masked,
+                                 void* dq, void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (masked && H > 0 && W > 0 && window > 0 && (H % window || W % window)) return RIB_ERR_SHAPE;
+    BwdBias b;
+    if (int rc = bwd_bias(bias, bias_dtype, bias_head_stride, buckets, num_buckets, dbias, &b)) return rc;
+    return bwd_impl(q, k, v, nullptr, nullptr, 0, out, lse, dout, B, H, W, heads, d, 0, window, shift, dq, dk, dv, nullptr, nullptr,
+                    workspace, workspace_bytes, stream, masked != 0, false, &b);
+}
+
+int rib_checkpoint_store(const void* x, long long rows, int d, void* codes, float* scales, void* stream)
+{
+    if (!x) return RIB_ERR_NULL;
+    if (int rc = check_checkpoint(codes, scales, rows, d)) return rc;
+    if (!aligned16(x)) return RIB_ERR_ALIGN;
+    if (rows == 0) return RIB_OK;
+    if (rib::checkpoint_store(static_cast<const __nv_bfloat16*>(x), rows, d, static_cast<int8_t*>(codes), scales, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+        return RIB_ERR_CUDA;
+    g_kernel_launches += 1;
+    return RIB_OK;
+}
+
+int rib_checkpoint_restore(const void* codes, const float* scales, long long rows, int d, void* x, void* stream)
+{
+    if (!x) return RIB_ERR_NULL;
+    if (int rc = check_checkpoint(codes, scales, rows, d)) return rc;
+    if (!aligned16(x)) return RIB_ERR_ALIGN;
+    if (rows == 0) return RIB_OK;
+    const rib::CheckpointRows t{static_cast<const int8_t*>(codes), scales, static_cast<__nv_bfloat16*>(x)};
+    if (rib::checkpoint_restore(&t, 1, rows, d, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RIB_ERR_CUDA;
+    g_kernel_launches += 1;
+    return RIB_OK;
+}
+
+size_t rib_window_attn_bwd_checkpointed_workspace(long long pos_head_stride, int B, int H, int W, int heads, int d, int r, int window)
+{
+    const size_t need = rib_window_attn_bwd_padded_workspace(pos_head_stride, B, H, W, heads, d, r, window);
+    return need ? need + 4 * image_bytes(B, H, W, heads, d) : 0;
+}
+
+int rib_window_attn_bwd_checkpointed(const rib_checkpoint* saved, const void* pq, const void* pk, long long pos_head_stride, const float* lse,
+                                     const void* dout, int B, int H, int W, int heads, int d, int r, int window, int shift, int masked,
+                                     void* dq, void* dk, void* dv, float* dpq, float* dpk, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (masked && H > 0 && W > 0 && window > 0 && (H % window || W % window)) return RIB_ERR_SHAPE;
+    Restored s;
+    if (int rc = plan_restore(saved, B, H, W, heads, d, workspace, workspace_bytes, &s)) return rc;
+    auto pass = [&](bool validate_only) {
+        return bwd_impl(s.t[0].x, s.t[1].x, s.t[2].x, pq, pk, pos_head_stride, s.t[3].x, lse, dout, B, H, W, heads, d, r, window, shift, dq, dk, dv,
+                        dpq, dpk, s.rest, s.rest_bytes, stream, masked != 0, validate_only);
+    };
+    if (int rc = pass(true)) return rc;
+    if (int rc = restore(s, stream)) return rc;
+    return pass(false);
+}
+
+size_t rib_window_attn_bwd_bucketed_checkpointed_workspace(long long bias_head_stride, int num_buckets, int B, int H, int W, int heads, int d, int window)
+{
+    const size_t need = bucketed_workspace(bias_head_stride, num_buckets, B, H, W, heads, d, window);
+    return need ? need + 4 * image_bytes(B, H, W, heads, d) : 0;
+}
+
+int rib_window_attn_bwd_bucketed_checkpointed(const rib_checkpoint* saved, const void* bias, int bias_dtype, long long bias_head_stride,
+                                              const int* buckets, int num_buckets, const float* lse, const void* dout,
+                                              int B, int H, int W, int heads, int d, int window, int shift, int masked,
+                                              void* dq, void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (masked && H > 0 && W > 0 && window > 0 && (H % window || W % window)) return RIB_ERR_SHAPE;
+    BwdBias b;
+    if (int rc = bwd_bias(bias, bias_dtype, bias_head_stride, buckets, num_buckets, dbias, &b)) return rc;
+    Restored s;
+    if (int rc = plan_restore(saved, B, H, W, heads, d, workspace, workspace_bytes, &s)) return rc;
+    auto pass = [&](bool validate_only) {
+        return bwd_impl(s.t[0].x, s.t[1].x, s.t[2].x, nullptr, nullptr, 0, s.t[3].x, lse, dout, B, H, W, heads, d, 0, window, shift, dq, dk, dv,
+                        nullptr, nullptr, s.rest, s.rest_bytes, stream, masked != 0, validate_only, &b);
+    };
+    if (int rc = pass(true)) return rc;
+    if (int rc = restore(s, stream)) return rc;
+    return pass(false);
 }
 
 int rib_window_attn_bwd_noalloc(const void* q, const void* k, const void* v, const void* pq, const void* pk,

@@ -41,6 +41,13 @@ struct Problem {
     bool masked;                      // shifted windows: the wrapped parts of a border window do not attend to each other
     int d_true, r_true;               // tcgen05 kernels on zero-padded copies (rib_repack.cu): the widths the scales 1/sqrt(d),
                                       // 1/sqrt(r) are taken from; 0 = d, r themselves
+    // learned bias by buckets in place of the rank-r tables (then r = 0); null: none
+    const void* bias;                 // [heads][num_buckets], bias_head_stride elements apart (0: one table for all heads)
+    int bias_bf16;                    // 1: bf16, 0: fp32
+    long long bias_head_stride;
+    const int* buckets;               // [2M-1][2M-1]: bucket of the offset (key - query); outside [0, num_buckets): not attended to
+    int num_buckets;
+    void* dbias;                      // gradient, layout and type of bias
     int narrow;                       // general tcgen05 backward on such copies: width of the rows of `out` and `dq`, which are the caller's; 0 = d
 };
 
@@ -52,14 +59,43 @@ inline size_t pos_extent(const Problem& p)
     return (size_t)(pos_tables(p) - 1) * (size_t)p.pos_head_stride + (size_t)p.n * p.r;
 }
 
+// Tables of a bias by buckets: one for all heads or one per head.
+inline int bias_tables(const Problem& p) { return p.bias_head_stride ? p.heads : 1; }
+
+// A bias of kBiasMasked or less takes its pair out of the softmax, as minus infinity does: the lowest value of a type, the usual stand-in for
+// minus infinity, means the same, and what is left stays far from overflow when it is scaled by log2(e).
+constexpr float kBiasMasked = -1e30f;
+
+__device__ __forceinline__ float bias_at(const void* bias, int bf16, long long at)
+{
+    const float b = bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(bias)[at]) : static_cast<const float*>(bias)[at];
+    return b <= kBiasMasked ? -INFINITY : b;
+}
+
 // The head width and the rank that the scales of Eq. 6 are taken from.
 inline float scale_width_d(const Problem& p) { return (float)(p.d_true ? p.d_true : p.d); }
 inline float scale_width_r(const Problem& p) { return (float)(p.r_true ? p.r_true : p.r); }
 
 // Launchers; each returns the cudaError_t of its launches.
 cudaError_t generic_fwd(const Problem& p, cudaStream_t stream);
-cudaError_t generic_bwd(const Problem& p, cudaStream_t stream);
+cudaError_t generic_bwd(const Problem& p, cudaStream_t stream, double* offset_sums = nullptr);     // offset_sums: BiasGrad::offsets
 cudaError_t rowdot_prepass(const Problem& p, cudaStream_t stream);
+
+// The gradient of a bias by buckets (rib_bias.cu): its scratch lies at the end of a backward workspace.
+struct BiasGrad {
+    double* offsets;      // [heads][(2M-1)^2] sums of dS by offset
+    double* tables;       // [tables][num_buckets]
+    unsigned* done;       // blocks of the finishing kernel that are through
+    size_t bytes;         // of all three, which start at zero
+};
+BiasGrad bias_grad_layout(int heads, int tables, int M, int num_buckets, void* base);
+cudaError_t bias_grad_clear(const BiasGrad& g, cudaStream_t stream);
+cudaError_t bias_grad_finish(const Problem& p, const BiasGrad& g, cudaStream_t stream);
+
+// Rows of bf16 as whole numbers of 8 bits with a scale each, and back (rib_checkpoint.cu).
+cudaError_t checkpoint_store(const __nv_bfloat16* x, long long rows, int d, int8_t* codes, float* scales, cudaStream_t stream);
+struct CheckpointRows { const int8_t* codes; const float* scales; __nv_bfloat16* x; };
+cudaError_t checkpoint_restore(const CheckpointRows* tensors, int count, long long rows, int d, cudaStream_t stream);
 
 bool sm100_fwd_supported(const Problem& p);
 cudaError_t sm100_fwd(const Problem& p, cudaStream_t stream);

@@ -47,6 +47,21 @@ __device__ inline bool pair_allowed(const Problem& p, const PairCoord& c, int i,
     return window_part(p.M, p.s, ly, lx, i / p.M, i % p.M) == window_part(p.M, p.s, ly, lx, j / p.M, j % p.M);
 }
 
+// Entry of the bucket map for query position i and key position j.
+__device__ inline int bias_offset(const Problem& p, int i, int j)
+{
+    const int yi = i / p.M, yj = j / p.M, side = 2 * p.M - 1;
+    return (yj - yi + p.M - 1) * side + (j - yj * p.M) - (i - yi * p.M) + p.M - 1;
+}
+// Bias of that pair: minus infinity where the key is not attended to.
+__device__ inline float pair_bias(const Problem& p, int h, int i, int j)
+{
+    const int u = __ldg(p.buckets + bias_offset(p, i, j));
+    return (unsigned)u < (unsigned)p.num_buckets ? bias_at(p.bias, p.bias_bf16, (long long)h * p.bias_head_stride + u) : -INFINITY;
+}
+// exp(s - lse).  A row without any key has lse = -inf, and so has every s of it.
+__device__ inline float probability(float s, float lse) { return s == -INFINITY ? 0.f : expf(s - lse); }
+
 // element offset of channel 0 of token i of the pair in a [B][H][W][heads][d] tensor (the token must exist)
 __device__ inline size_t token_offset(const Problem& p, const PairCoord& c, int i)
 {
@@ -136,6 +151,7 @@ __global__ void __launch_bounds__(kThreads) generic_fwd_kernel(const Problem p)
                 s1 = fmaf(a, Kt[(lane + 32) * ldk + col], s1);
             }
             const int qi = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
+            if (p.bias) { s0 += pair_bias(p, c.h, qi, min(j0 + lane, p.n - 1)); s1 += pair_bias(p, c.h, qi, min(j0 + lane + 32, p.n - 1)); }
             if (j0 + lane >= p.n || !token_exists(p, c, j0 + lane) || !pair_allowed(p, c, qi, j0 + lane)) s0 = -INFINITY;
             if (j0 + lane + 32 >= p.n || !token_exists(p, c, j0 + lane + 32) || !pair_allowed(p, c, qi, j0 + lane + 32)) s1 = -INFINITY;
             const float m_new = fmaxf(m[rr], warp_max(fmaxf(s0, s1)));
@@ -165,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) generic_fwd_kernel(const Problem p)
         const int i = row0 + warp * kRowsPerWarp + rr;
         if (i >= p.n || !token_exists(p, c, i)) continue;
         const size_t off = token_offset(p, c, i);
-        const float inv = 1.f / l[rr];
+        const float inv = l[rr] > 0.f ? 1.f / l[rr] : 0.f;          // (0: a bias that leaves the row no key)
         const float g0 = p.gate && lane < p.d ? __bfloat162float(p.gate[off + lane]) : 1.f;            // Eq. 9
         const float g1 = p.gate && lane + 32 < p.d ? __bfloat162float(p.gate[off + lane + 32]) : 1.f;
         if (lane < p.d) p.out_w[off + lane] = __float2bfloat16_rn(o[rr][0] * inv * g0);
@@ -193,7 +209,8 @@ __global__ void rowdot_kernel(const Problem p, size_t items)
 
 // ------------------------------------------------------- backward: dq and dPq (by query row)
 // dQ~_i = sum_j dS_ij [k_j, pk_j]; columns < d give dq (times 1/sqrt d), the rest dPq (1/sqrt r).
-__global__ void __launch_bounds__(kThreads) generic_bwd_dq_kernel(const Problem p)
+// With a bias by buckets dS is also summed by offset, in 64 bits: the order of the adds is then lost in the rounding to the result.
+__global__ void __launch_bounds__(kThreads) generic_bwd_dq_kernel(const Problem p, double* offset_sums)
 {
     extern __shared__ float sm[];
     const int dk = p.d + p.r, ldk = dk | 1, ldv = p.d | 1;
@@ -239,11 +256,18 @@ __global__ void __launch_bounds__(kThreads) generic_bwd_dq_kernel(const Problem 
             }
             // keys beyond the window or, on an extended map, beyond the image have probability 0
             const int qi = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
-            const float p0 = j0 + lane < p.n && token_exists(p, c, j0 + lane) && pair_allowed(p, c, qi, j0 + lane) ? expf(s0 - lse[rr]) : 0.f;
-            const float p1 = j0 + lane + 32 < p.n && token_exists(p, c, j0 + lane + 32) && pair_allowed(p, c, qi, j0 + lane + 32) ? expf(s1 - lse[rr]) : 0.f;
+            if (p.bias) { s0 += pair_bias(p, c.h, qi, min(j0 + lane, p.n - 1)); s1 += pair_bias(p, c.h, qi, min(j0 + lane + 32, p.n - 1)); }
+            const float p0 = j0 + lane < p.n && token_exists(p, c, j0 + lane) && pair_allowed(p, c, qi, j0 + lane) ? probability(s0, lse[rr]) : 0.f;
+            const float p1 = j0 + lane + 32 < p.n && token_exists(p, c, j0 + lane + 32) && pair_allowed(p, c, qi, j0 + lane + 32) ? probability(s1, lse[rr]) : 0.f;
             float* srow = Ss + (warp * kRowsPerWarp + rr) * kTile;
-            srow[lane] = p0 * (g0 - Di[rr]);
-            srow[lane + 32] = p1 * (g1 - Di[rr]);
+            const float ds0 = p0 * (g0 - Di[rr]), ds1 = p1 * (g1 - Di[rr]);
+            srow[lane] = ds0;
+            srow[lane + 32] = ds1;
+            if (p.bias && row0 + warp * kRowsPerWarp + rr < p.n && token_exists(p, c, qi)) {
+                double* sums = offset_sums + (size_t)c.h * (2 * p.M - 1) * (2 * p.M - 1);
+                if (p0 != 0.f) atomicAdd(sums + bias_offset(p, qi, j0 + lane), (double)ds0);
+                if (p1 != 0.f) atomicAdd(sums + bias_offset(p, qi, j0 + lane + 32), (double)ds1);
+            }
         }
         __syncwarp();
         for (int j = 0; j < kTile; ++j) {
@@ -320,8 +344,9 @@ __global__ void __launch_bounds__(kThreads) generic_bwd_dkv_kernel(const Problem
                 g1 = fmaf(a, Gt[(lane + 32) * ldv + col], g1);
             }
             const int kj = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
-            const float p0 = i0 + lane < p.n && pair_allowed(p, c, i0 + lane, kj) ? expf(s0 - Lt[lane]) : 0.f;
-            const float p1 = i0 + lane + 32 < p.n && pair_allowed(p, c, i0 + lane + 32, kj) ? expf(s1 - Lt[lane + 32]) : 0.f;
+            if (p.bias) { s0 += pair_bias(p, c.h, min(i0 + lane, p.n - 1), kj); s1 += pair_bias(p, c.h, min(i0 + lane + 32, p.n - 1), kj); }
+            const float p0 = i0 + lane < p.n && pair_allowed(p, c, i0 + lane, kj) ? probability(s0, Lt[lane]) : 0.f;
+            const float p1 = i0 + lane + 32 < p.n && pair_allowed(p, c, i0 + lane + 32, kj) ? probability(s1, Lt[lane + 32]) : 0.f;
             float* prow = Ps + (warp * kRowsPerWarp + rr) * kTile;
             float* srow = Ss + (warp * kRowsPerWarp + rr) * kTile;
             prow[lane] = p0; prow[lane + 32] = p1;
@@ -386,7 +411,7 @@ cudaError_t rowdot_prepass(const Problem& p, cudaStream_t stream)
     return cudaGetLastError();
 }
 
-cudaError_t generic_bwd(const Problem& p, cudaStream_t stream)
+cudaError_t generic_bwd(const Problem& p, cudaStream_t stream, double* offset_sums)
 {
     const int dk = p.d + p.r;
     const size_t pos_floats = p.r > 0 ? pos_extent(p) : 0;      // rank 0: there are no positional gradients (dpq, dpk may be null)
@@ -404,7 +429,7 @@ cudaError_t generic_bwd(const Problem& p, cudaStream_t stream)
                                            (size_t)kRows * p.d + (size_t)kRows * kTile);
     e = set_smem(generic_bwd_dq_kernel, smem_q);
     if (e != cudaSuccess) return e;
-    { ProfileScope scope(RIB_KERNEL_ANY_BWD_DQ, stream); generic_bwd_dq_kernel<<<grid, kThreads, smem_q, stream>>>(p); }
+    { ProfileScope scope(RIB_KERNEL_ANY_BWD_DQ, stream); generic_bwd_dq_kernel<<<grid, kThreads, smem_q, stream>>>(p, offset_sums); }
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const size_t smem_k = sizeof(float) * ((size_t)kTile * (dk | 1) + (size_t)kTile * (p.d | 1) + 2 * (size_t)kTile +
