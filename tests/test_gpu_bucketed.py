@@ -7,12 +7,9 @@ also round P and dS to bf16 before they are contracted: independent errors of th
 sqrt(n) where the result does, so the two together stay below 1.5 x 2.3e-3 = 3.5e-3 in relative L2.  Bounds: 5e-3 in relative L2 and 1e-2 of the
 largest value, those of the rank-r kernels.  lse is fp32: its error is that of ln of a sum of bf16-rounded terms, at most 2^-8.
 
-What the rounding of `out` to bf16, an input of the backward pass, brings in (`noise`): D_i = sum_c dO_ic out_ic is off by e_i, independent errors of
-at most 2^-8 / sqrt(3) of each term in the mean, so by E = 2^-8 / sqrt(3) x sqrt(sum_ic (dO_ic out_ic)^2) in L2 over the rows.  dS_ij is then off by
-P_ij e_i, and with sum_j P_ij <= 1
-  dbias (a sum over many rows that may cancel: over all offsets it is 0) by at most E in L2,
-  dq_i = sum_j dS_ij k_j / sqrt(d) by at most E max_j |k_j| / sqrt(d),   dk_j = sum_i dS_ij q_i / sqrt(d) by at most E max_i |q_i| / sqrt(d);
-which counts where rows are all but one key each, so that dP - D is small beside D."""
+The gradients are compared with the oracle's for the out and lse that the backward pass was given: D = rowsum(dO o out) of a rounded out is off
+by up to 2^-8 of its terms, which is a property of that input and, where rows are all but one key each or a bucket's sum cancels, larger
+than the gradients themselves."""
 import numpy as np
 import pytest
 import torch
@@ -62,15 +59,8 @@ def close(name, got, ref, rel_l2=5e-3, noise=0.0):
     if ref.size == 0:
         return
     err, norm = np.abs(got - ref).max(), np.linalg.norm(ref)
-    assert err <= 1e-2 * max(1.0, np.abs(ref).max()) + noise, (name, err)
-    assert np.linalg.norm(got - ref) <= rel_l2 * norm + 1e-5 * np.sqrt(ref.size) + noise, (name, np.linalg.norm(got - ref) / norm, noise / norm)
-
-
-def noises(q, k, dout, out):
-    """`noise` of dq, dk, dv and dbias."""
-    q, k, dout, out = (np.asarray(to_f64(t) if torch.is_tensor(t) else t) for t in (q, k, dout, out))
-    e, longest = 2.0 ** -8 / 3 ** 0.5 * np.linalg.norm(dout * out), lambda t: np.linalg.norm(t, axis=-1).max() / t.shape[-1] ** 0.5
-    return e * longest(k), e * longest(q), 0.0, e
+    assert err <= 1e-2 * max(1.0, np.abs(ref).max()), (name, err)
+    assert np.linalg.norm(got - ref) <= rel_l2 * norm + 1e-5 * np.sqrt(ref.size) + noise, (name, np.linalg.norm(got - ref) / norm)
 
 
 def check(inputs, M, s, masked=False, path="auto", fast=None):
@@ -93,8 +83,8 @@ def check(inputs, M, s, masked=False, path="auto", fast=None):
     ref_out, ref_lse = orc.fwd(*f, M, s, masked)
     close("out", out, ref_out)
     close("lse", lse, ref_lse)
-    for name, got, ref, noise in zip(("dq", "dk", "dv", "dbias"), grads, orc.bwd(*f, to_f64(dout), M, s, masked), noises(q, k, dout, ref_out)):
-        close(name, got, ref, noise=noise)
+    for name, got, ref in zip(("dq", "dk", "dv", "dbias"), grads, orc.bwd(*f, to_f64(dout), M, s, masked, out=to_f64(out), lse=to_f64(lse))):
+        close(name, got, ref)
     assert grads[3].dtype == bias.dtype and grads[3].shape == bias.shape
     return out, lse, grads
 
@@ -206,8 +196,7 @@ def test_strides_between_tables_and_untouched_elements():
                                             *[p(x) for x in grads], p(dwide), p(ws), need, s) == 0
     ref = binding.rib_window_attn_fwd_bucketed(*t[:3], bias.cuda(), t[4], M, 8)
     assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1]) and (dwide[:, count:] == 7.0).all()
-    f = [to_f64(x) for x in (q, k, v, bias)]
-    close("dbias", dwide[:, :count], orc.bwd(*f, named.numpy(), to_f64(dout), M, 8)[3], noise=noises(q, k, dout, orc.fwd(*f, named.numpy(), M, 8)[0])[3])
+    close("dbias", dwide[:, :count], orc.bwd(*(to_f64(x) for x in (q, k, v, bias)), named.numpy(), to_f64(dout), M, 8, out=to_f64(out), lse=to_f64(lse))[3])
 
 
 def test_other_streams_graphs_and_repeats():
@@ -241,16 +230,20 @@ def test_other_streams_graphs_and_repeats():
 
 
 def test_a_training_loop_uses_them_together():
-    """Forward, backward and a step of the table, ten times, the gradient of every step held against the oracle's."""
+    """Forward, backward and a step of the table, ten times, the gradient of every step held against the oracle's.
+
+    The steps are large, so that the rows become all but one key each and dP - D small beside dP and D.  Those are fp32 sums of d = 32 products
+    each, off by at most 32 x 2^-24 |dO_i| |v_j|; with weights P_ij that add up to 1 over a row and errors that are independent
+    between rows, dbias is off by up to 2 x 2^-19 max_j |v_j| |dO| in L2 (`noise`)."""
     M, heads, d = 16, 2, 32
     q, k, v, _, target, named = (t.cuda() for t in make(1, 32, 32, heads, d, M, log_map(M), torch.float32, seed=20, bias_scale=1.5))
     want, _ = binding.rib_window_attn_fwd_bucketed(q, k, v, target, named, M, 8)
-    bias = torch.zeros_like(target)
+    bias, longest = torch.zeros_like(target), v.float().norm(dim=-1).max().item()
     for _ in range(10):
         out, lse = binding.rib_window_attn_fwd_bucketed(q, k, v, bias, named, M, 8)
         dout = (out.float() - want.float()).bfloat16()
         grads = binding.rib_window_attn_bwd_bucketed(q, k, v, bias, named, out, lse, dout, M, 8)
         assert all(torch.isfinite(t.float()).all() for t in grads)
-        f = [to_f64(t) for t in (q, k, v, bias)]
-        close("dbias", grads[3], orc.bwd(*f, named.cpu().numpy(), to_f64(dout), M, 8)[3], noise=noises(q, k, dout, to_f64(out))[3])
+        close("dbias", grads[3], orc.bwd(*(to_f64(t) for t in (q, k, v, bias)), named.cpu().numpy(), to_f64(dout), M, 8, out=to_f64(out), lse=to_f64(lse))[3],
+              noise=2.0 ** -18 * longest * dout.float().norm().item())
         bias -= 2.0 * grads[3]
