@@ -370,12 +370,12 @@ int fwd_impl(const void* q, const void* k, const void* v, const void* pq, const 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int forced = g_forced_path.load();
     const bool frame = !bias && rib::sm100_frame_supported(p);
-    bool fast = forced != RIB_PATH_GENERIC && !bias && (frame || rib::sm100_fwd_supported(p));
+    bool fast = forced != RIB_PATH_GENERIC && (bias ? rib::sm100_bias_fwd_supported(p) : frame || rib::sm100_fwd_supported(p));
     p.exact_softmax = forced == RIB_PATH_SM100_EXACT;
     int launches = 1;
     cudaError_t e;
     if (fast) {
-        e = frame ? rib::sm100_fwd_frame(p, st) : rib::sm100_fwd(p, st);
+        e = bias ? rib::sm100_bias_fwd(p, st) : frame ? rib::sm100_fwd_frame(p, st) : rib::sm100_fwd(p, st);
     } else if (forced != RIB_PATH_GENERIC && !bias && rib::sm100_repack_fwd_supported(p)) {
         // rows TMA cannot address (d = 30, r = 18, ...): the tensor-core kernels on zero-padded copies
         e = rib::sm100_fwd_repacked(p, st, &launches);

