@@ -64,14 +64,15 @@ def fwd(q, k, v, bias, buckets, window, shift=0, masked=False):
     return out, lse
 
 
-def bwd(q, k, v, bias, buckets, dout, window, shift=0, masked=False, out=None, lse=None):
-    """dq, dk, dv and dbias; out and lse are computed here unless those of a forward pass on other inputs are given."""
+def bwd(q, k, v, bias, buckets, dout, window, shift=0, masked=False, out=None, lse=None, want_norm=False):
+    """dq, dk, dv and dbias (and the 2-norm of all dS); out and lse are computed here unless those of a forward pass on other inputs are given."""
     q, k, v, bias, dout = (np.asarray(a, dtype=np.float64) for a in (q, k, v, bias, dout))
     if out is None:
         out, lse = fwd(q, k, v, bias, buckets, window, shift, masked)
     out, lse = np.asarray(out, dtype=np.float64), np.asarray(lse, dtype=np.float64)
     B, H, W, heads, d = q.shape
     dq, dk, dv, dbias = np.full(q.shape, np.nan), np.full(q.shape, np.nan), np.full(q.shape, np.nan), np.zeros(bias.shape)
+    squares = 0.0
     for Y, X, y, x, part in _windows(H, W, window, shift, masked):
         for h in range(heads):
             u, add = _bias(_table(bias, h), buckets, window, y, x)
@@ -86,7 +87,8 @@ def bwd(q, k, v, bias, buckets, dout, window, shift=0, masked=False, out=None, l
                 dk[b, Y, X, h] = ds.T @ qw / np.sqrt(d)
                 dv[b, Y, X, h] = p.T @ g
                 np.add.at(_table(dbias, h), u[seen], ds[seen])
-    return dq, dk, dv, dbias
+                squares += (ds * ds).sum()
+    return (dq, dk, dv, dbias, np.sqrt(squares)) if want_norm else (dq, dk, dv, dbias)
 
 
 def store(x):

@@ -463,13 +463,19 @@ namespace {
 struct BwdBias : BiasArgs { void* gradient; };
 
 // Scratch of a backward pass with a bias: what the attention kernels need, then the sums of the table's gradient.
-size_t bucketed_attention_bytes(int B, int H, int W, int heads) { return rowdot_bytes(B, H, W, heads); }
+size_t bucketed_attention_bytes(int B, int H, int W, int heads, int window)
+{
+    rib::Problem p{};
+    fill_shape(p, B, H, W, heads, 8, 0, window, 0);
+    const size_t any = rowdot_bytes(B, H, W, heads), fast = window % 8 == 0 ? rib::sm100_bias_bwd_workspace_bytes(p.pairs, p.n) : 0;
+    return any > fast ? any : fast;
+}
 
 size_t bucketed_workspace(long long bias_head_stride, int num_buckets, int B, int H, int W, int heads, int d, int window)
 {
     if (check_shape(B, H, W, heads, d, 0, window, 0, true) != RIB_OK) return 0;
     if (num_buckets <= 0 || bias_head_stride < 0 || (bias_head_stride && bias_head_stride < num_buckets)) return 0;
-    return bucketed_attention_bytes(B, H, W, heads) + rib::bias_grad_layout(heads, bias_head_stride ? heads : 1, window, num_buckets, nullptr).bytes;
+    return bucketed_attention_bytes(B, H, W, heads, window) + rib::bias_grad_layout(heads, bias_head_stride ? heads : 1, window, num_buckets, nullptr).bytes;
 }
 
 }  // namespace
@@ -522,12 +528,18 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
         fill_bias(p, *bias);
         p.dbias = bias->gradient;
         const rib::BiasGrad g = rib::bias_grad_layout(heads, rib::bias_tables(p), window, bias->num_buckets,
-                                                      static_cast<unsigned char*>(workspace) + bucketed_attention_bytes(B, H, W, heads));
-        cudaError_t e = rib::bias_grad_clear(g, st);
-        if (e == cudaSuccess) e = rib::generic_bwd(p, st, g.offsets);
-        if (e == cudaSuccess) e = rib::bias_grad_finish(p, g, st);
+                                                      static_cast<unsigned char*>(workspace) + bucketed_attention_bytes(B, H, W, heads, window));
+        const bool fast = g_forced_path.load() != RIB_PATH_GENERIC && rib::sm100_bias_bwd_supported(p);
+        cudaError_t e;
+        if (fast) {
+            e = rib::sm100_bias_bwd(p, g, st);
+        } else {
+            e = rib::bias_grad_clear(g, st);
+            if (e == cudaSuccess) e = rib::generic_bwd(p, st, g.offsets);
+            if (e == cudaSuccess) e = rib::bias_grad_finish(p, g, st);
+        }
         if (e != cudaSuccess) return RIB_ERR_CUDA;
-        t_last_path = RIB_PATH_GENERIC;
+        t_last_path = fast ? RIB_PATH_SM100 : RIB_PATH_GENERIC;
         g_kernel_launches += 4;
         return RIB_OK;
     }

@@ -1,0 +1,723 @@
+// Backward window attention with a learned bias by buckets for B200 (sm_100a): the chain rule of the softmax as five tcgen05 contractions
+// per (query tile, key block) with TMEM accumulators and TMA loads, the probabilities recomputed from lse, and the gradient of the bias summed
+// by offset on the way.
+//
+// Shapes and windows: as the forward (rib_bias_fwd_sm100.cu).  Work item = one key block of two patches of one (head, batch item, window); a persistent
+// CTA keeps K_J and V_J in shared memory and dV_J, dK_J in tensor memory, and walks the query tiles I of the window.  The pipeline, its roles and
+// its barriers are those of the rank-r backward kernel (rib_bwd_sm100.cu, rank 16), everything transposed (keys on the TMEM lanes), the unit
+// a half-tile u = 2 I + h of the 64 queries of one patch:
+//     S^T  = K_J Q_u^T,   dP^T = V_J dO_u^T                                                      (M128 N64 K32)
+//     P^T  = exp2(S^T * log2(e) / sqrt(d) + b(key - query) - lse_i * log2(e)),   dS^T = P^T o (dP^T - D_i)     (arithmetic warps)
+//     dV_J += P^T dO_u,   dK_J += dS^T Q_u                                                       (A from TMEM, N = 32)
+// and once per tile  dQ_I = dS K_J  (A = dS in shared memory, N = 32), added (fp32 red) into a workspace [pair][group of 4 columns][token][4].
+//
+// Biases: an arithmetic warp has 4 x 8 keys and 4 x 8 queries of a unit, a thread 4 rows of one key column and 2 neighbouring query columns of 4
+// rows: 7 pairs of the table in shared memory serve its 32 scores (rib_bias_sm100.cuh).
+//
+// Gradient of the bias: the sum of dS over all pairs of tokens at the same offset.  Four warps of their own take the dS tile that dQ reads from
+// shared memory (bf16, as dQ and dK see it), one patch of keys against one of queries each: 64 blocks of 8 x 8 (key row, query row).
+// The blocks with the same difference of rows are summed in fp32 by warp-level MMAs against stacked identities (four blocks at a time, two to
+// each of two differences), which leaves 15 blocks; those are then summed along their diagonals and added to the sums by offset.
+#include "rib_bias_sm100.cuh"
+
+namespace rib {
+namespace {
+
+using namespace sm100;
+
+constexpr int kQStages = 3;           // ring of query-side tiles (Q, dO, lse/D)
+constexpr int kThreads = 896;
+constexpr int kArithmeticThreads = 512;
+
+// shared-memory map (offsets from a 1024-byte aligned base)
+constexpr uint32_t kOffK = 0;                                    // [2] (one slot per item in flight)
+constexpr uint32_t kOffV = kOffK + 2 * kContentBytes;            // [2]
+constexpr uint32_t kOffRing = kOffV + 2 * kContentBytes;
+constexpr uint32_t kLdPatch = 64 * 8, kLdBytes = 2 * kLdPatch;   // per patch 32 query pairs x (-lse2, -lse2', -D, -D')
+constexpr uint32_t kRingQ = 0, kRingDO = kContentBytes, kRingLD = kRingDO + kContentBytes;
+constexpr uint32_t kRingBytes = kRingLD + kLdBytes;              // 17408
+constexpr uint32_t kOffDS = kOffRing + kQStages * kRingBytes;    // dS: [2 tiles][2 halves of 64 queries][128 keys][128 B], SWIZZLE_128B
+constexpr uint32_t kDSHalf = kTile * 128;
+constexpr uint32_t kOffDK = kOffDS + 4 * kDSHalf;                // dK rows of an item on their way out (dV rows leave through V's slot)
+constexpr uint32_t kOffBar = kOffDK + kContentBytes;
+// kSFull, kPReady, kPFree: unit mod 4 (on_unit); kDSFree: per dS tile buffer.  A parity wait cannot tell "two phases ahead" from "not yet", so a
+// barrier's next phase must not be able to complete before every waiter has seen the current one: the next phases of kPReady of the units 2 g,
+// 2 g + 1 belong to tile g + 2, whose dS buffer is released by dQ of tile g and by the four warps that sum the bias gradient.
+enum Bar { kKVFull = 0, kKVEmpty = 2, kQFull = 4, kQEmpty = kQFull + kQStages, kSFull = kQEmpty + kQStages, kPReady = kSFull + 4, kPFree = kPReady + 4,
+           kDSFree = kPFree + 4, kDQFull = kDSFree + 2, kDQFree, kAccFull, kAccFree, kTabDone, kTabReady, kDrain, kNumBars = kDrain + 3 };
+constexpr uint32_t kOffMisc = kOffBar + kNumBars * 8;
+constexpr uint32_t kOffTable = (kOffMisc + 16 + 15) & ~15u;      // [(2M-1)^2] fp32
+constexpr uint32_t smem_bytes(int M) { return kOffTable + 4u * (2 * M - 1) * (2 * M - 1) + 1024; }
+static_assert(smem_bytes(kBiasMaxWindow) <= 232448, "shared memory of one CTA");
+static_assert(kOffRing % 1024 == 0 && kRingBytes % 1024 == 0 && kOffDS % 1024 == 0, "swizzle atoms need aligned tiles");
+
+// tensor-memory columns: S^T of unit u in buffer u mod 3 (64 fp32 columns) and dP^T beside it; a warp writes P^T over its own scores and dS^T over its
+// dP^T: 32 queries in the first 16 of its 32 columns
+constexpr uint32_t kBuffers = 3;
+constexpr uint32_t kStep = 128, kColDP = 64, kColDV = kBuffers * kStep, kColDK = kColDV + kD, kColDQ = kColDK + kD;
+static_assert(kColDQ + kD <= 512, "tensor memory has 512 columns");
+constexpr uint32_t kTmemCols = 512;
+
+constexpr uint32_t kIdescSS = idesc_bf16_f32(kTile, kTile / 2, false);        // both operands K-major
+constexpr uint32_t kIdescT = idesc_bf16_f32(kTile, kD, true);                 // A in TMEM, B MN-major, N = 32
+constexpr uint32_t kIdescQ = idesc_bf16_f32_ab(kTile, kD, true, true);        // A and B MN-major
+
+struct Params {
+    const float2* ld;          // [pairs][n / 2], patches of the window in rows: per query pair (-lse2, -lse2', -D, -D') as two float2; then one patch of no queries
+    float* dq_acc;             // [pairs][32 / 4][n][4] fp32, zeroed by the preparation kernel
+    double* offsets;           // [heads][(2M-1)^2] sums of dS
+    int* status;
+    long long no_queries;      // element of ld where the patch of no queries begins
+    int H, W, heads, M, s, n, nWy, nWx, Hp, Wp;
+    int items;
+    float scale_log2;          // log2(e) / sqrt(d)
+    float inv_sqrt_d;
+    BiasSource source;
+    BiasItems g;
+};
+
+// `sp` counts the patches of the window that hold tokens; beyond the last one the last one stands in
+__device__ __forceinline__ void patch_origin(const Params& p, const LiveItem& c, int sp, int& py, int& px, int& Y0, int& X0)
+{
+    live_patch_origin(p.g.live, WindowGeom{p.Hp, p.Wp, p.M, p.s}, c, min(sp, c.patches - 1), py, px, Y0, X0);
+}
+__device__ __forceinline__ size_t pair_of(const Params& p, const LiveItem& c)
+{
+    return (((size_t)c.b * p.nWy + c.wy) * p.nWx + c.wx) * p.heads + c.h;
+}
+
+__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// d (16 x 8, fp32) += a (16 x 16, bf16) * b (16 x 8, bf16), warp-level
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <bool B> struct Flag { static constexpr bool value = B; };
+
+__global__ void __launch_bounds__(kThreads, 1)
+rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                    const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_dk, const __grid_constant__ CUtensorMap tm_dv,
+                    const __grid_constant__ Params p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    auto bar = [&](int i) { return base + kOffBar + 8u * i; };
+    // of kSFull, kPReady, kPFree: the barrier of a unit and the parity of its phase.  (Units -1 to -3 have the parity that a barrier without a
+    // completed phase answers yes to.)
+    auto on_unit = [&](int which, uint32_t unit) { return bar(which + (int)(unit & 3)); };
+    auto unit_parity = [](uint32_t unit) { return (unit >> 2) & 1; };
+    auto buffer_after = [](uint32_t buffer, uint32_t units) { buffer += units; return buffer >= kBuffers ? buffer - kBuffers : buffer; };
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + kOffMisc);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + kOffMisc + 4);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int side = 2 * p.M - 1;
+    const long long work = p.g.work[9] * p.heads;
+    const int first_item = first_bias_item(p.g, work * blockIdx.x / gridDim.x);
+    const int last_item = min(first_bias_item(p.g, work * (blockIdx.x + 1) / gridDim.x), p.items);
+
+    if (threadIdx.x == 0) {
+        abort_flag[0] = 0; abort_flag[1] = 0;   // [1] stays 0: used by the drain waits
+        for (int s = 0; s < 2; ++s) { mbar_init(bar(kKVFull + s), 1); mbar_init(bar(kKVEmpty + s), 5); }     // empty: the item's last dQ, and V's slot by the four warps whose dV leaves through it
+        for (int s = 0; s < kQStages; ++s) { mbar_init(bar(kQFull + s), 1); mbar_init(bar(kQEmpty + s), 1); }
+        for (int h = 0; h < 2; ++h) mbar_init(bar(kDSFree + h), 5);        // dQ and the four warps of the bias gradient
+        for (int i = 0; i < 4; ++i) { mbar_init(bar(kSFull + i), 1); mbar_init(bar(kPReady + i), 8); mbar_init(bar(kPFree + i), 1); }
+        mbar_init(bar(kDQFull), 1); mbar_init(bar(kDQFree), 4);
+        mbar_init(bar(kAccFull), 1); mbar_init(bar(kAccFree), 4);
+        mbar_init(bar(kTabDone), kArithmeticThreads / 32); mbar_init(bar(kTabReady), kArithmeticThreads / 32);
+        for (int i = 0; i < 3; ++i) mbar_init(bar(kDrain + i), 1);
+        fence_barrier_init();
+        prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
+        prefetch_tensormap(&tm_do); prefetch_tensormap(&tm_dk); prefetch_tensormap(&tm_dv);
+    }
+    if (warp == 2) {
+        tmem_alloc(base + kOffMisc, kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        // ============================================================ TMA producer (one thread)
+        if (lane == 0) {
+            uint32_t nitem = 0, kv_armed = 0, q_armed = 0;
+            bool ok = true;
+            for (int item = first_item; item < last_item && ok; ++item, ++nitem) {
+                const LiveItem c = decode_bias_item(p.g, item);
+                const uint32_t slot = nitem & 1;
+                if (nitem >= 2 && !mbar_wait(bar(kKVEmpty + slot), ((nitem >> 1) - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+                mbar_arrive_expect_tx(bar(kKVFull + slot), 2 * kContentBytes);
+                ++kv_armed;
+                for (int sub = 0; sub < 2; ++sub) {
+                    int py, px, Y0, X0;
+                    patch_origin(p, c, 2 * c.tp + sub, py, px, Y0, X0);
+                    if (2 * c.tp + sub >= c.patches) X0 = p.Wp;          // beyond the last patch lies nothing: zeros
+                    tma_load_5d(base + kOffK + slot * kContentBytes + sub * kPatchContent, &tm_k, bar(kKVFull + slot), 0, c.h, X0, Y0, c.b);
+                    tma_load_5d(base + kOffV + slot * kContentBytes + sub * kPatchContent, &tm_v, bar(kKVFull + slot), 0, c.h, X0, Y0, c.b);
+                }
+                const size_t pair = pair_of(p, c);
+                const int tiles = (c.patches + 1) >> 1;
+                for (int I = 0; I < tiles; ++I, ++q_armed) {
+                    const uint32_t st = q_armed % kQStages, use = q_armed / kQStages;
+                    if (use > 0 && !mbar_wait(bar(kQEmpty + st), (use - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+                    mbar_arrive_expect_tx(bar(kQFull + st), kRingBytes);
+                    const uint32_t ring = base + kOffRing + st * kRingBytes;
+                    for (int sub = 0; sub < 2; ++sub) {
+                        int py, px, Y0, X0;
+                        patch_origin(p, c, 2 * I + sub, py, px, Y0, X0);
+                        const bool none = 2 * I + sub >= c.patches;
+                        if (none) X0 = p.Wp;
+                        tma_load_5d(ring + kRingQ + sub * kPatchContent, &tm_q, bar(kQFull + st), 0, c.h, X0, Y0, c.b);
+                        tma_load_5d(ring + kRingDO + sub * kPatchContent, &tm_do, bar(kQFull + st), 0, c.h, X0, Y0, c.b);
+                        const size_t at = none ? (size_t)p.no_queries : pair * p.n + 64 * (size_t)((py >> 3) * (p.M >> 3) + (px >> 3));
+                        bulk_load_1d(ring + kRingLD + sub * kLdPatch, p.ld + at, kLdPatch, bar(kQFull + st));
+                    }
+                }
+            }
+            if (!ok) {
+                // Gave up: let the copies already in flight land before the CTA may exit.
+                for (uint32_t b2 = kv_armed > 2u ? kv_armed - 2 : 0; b2 < kv_armed; ++b2)
+                    mbar_wait(bar(kKVFull + (b2 & 1)), (b2 >> 1) & 1, abort_flag + 1, p.status);
+                for (uint32_t b2 = q_armed > (uint32_t)kQStages ? q_armed - kQStages : 0; b2 < q_armed; ++b2)
+                    mbar_wait(bar(kQFull + b2 % kQStages), (b2 / kQStages) & 1, abort_flag + 1, p.status);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 4) {
+        // ============================================ MMA issuers: warps 1-3, the whole warp walks the
+        // loops and waits (warp-uniform outcomes), one elected lane issues
+        constexpr uint64_t kDesc64 = smem_desc_const(16, 512, kSwizzle64B);
+        constexpr uint64_t kDescDS = smem_desc_const(kDSHalf, 1024, kSwizzle128B);    // MN-major: the two 64-query halves one leading step apart
+        auto wait_all = [&](uint32_t b, uint32_t parity) { return mbar_wait_warp(b, parity, abort_flag, p.status); };
+        bool ok = true;
+        uint32_t g = 0, nitem = 0, buf = 0;
+        for (int item = first_item; item < last_item && ok; ++item, ++nitem) {
+            const int tiles = (decode_bias_item(p.g, item).patches + 1) >> 1;
+            const uint32_t slot = nitem & 1;
+            if (warp == 1) {
+                // ---- S^T, dP^T of unit u as soon as dV and dK of unit u - 3 have consumed P^T, dS^T, which lie in the same columns
+                if (!wait_all(bar(kKVFull + slot), (nitem >> 1) & 1)) { ok = false; break; }
+                const uint64_t k = smem_desc_at(kDesc64, base + kOffK + slot * kContentBytes), v = smem_desc_at(kDesc64, base + kOffV + slot * kContentBytes);
+                for (int t = 0; t < tiles && ok; ++t, ++g) {
+                    const uint32_t st = g % kQStages;
+                    if (!wait_all(bar(kQFull + st), (g / kQStages) & 1)) { ok = false; break; }
+#pragma unroll
+                    for (uint32_t h = 0; h < 2; ++h) {
+                        const uint32_t u = 2 * g + h;
+                        if (!wait_all(on_unit(kPFree, u - kBuffers), unit_parity(u - kBuffers))) { ok = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t ring = base + kOffRing + st * kRingBytes + h * kPatchContent;   // rows of patch h
+                            const uint64_t q = smem_desc_at(kDesc64, ring + kRingQ), go = smem_desc_at(kDesc64, ring + kRingDO);
+                            const uint32_t d_s = tmem + kStep * buf;
+                            mma_ss(d_s, k, q, kIdescSS, 0u);
+                            mma_ss(d_s, k + 2, q + 2, kIdescSS, 1u);     // + 32 bytes: second K16 step
+                            mma_ss(d_s + kColDP, v, go, kIdescSS, 0u);
+                            mma_ss(d_s + kColDP, v + 2, go + 2, kIdescSS, 1u);
+                            mma_commit(on_unit(kSFull, u));
+                        }
+                        __syncwarp();
+                        buf = buffer_after(buf, 1);
+                    }
+                }
+            } else if (warp == 2) {
+                // ---- dV_J += P^T dO_u and dK_J += dS^T Q_u (A from tensor memory, 16 queries per step)
+                for (int t = 0; t < tiles && ok; ++t, ++g) {
+                    const uint32_t st = g % kQStages;
+#pragma unroll
+                    for (uint32_t h = 0; h < 2; ++h) {
+                        const uint32_t u = 2 * g + h;
+                        const bool first = t == 0 && h == 0, last = t == tiles - 1 && h == 1;
+                        if (!wait_all(on_unit(kPReady, u), unit_parity(u)) ||
+                            (first && nitem > 0 && !wait_all(bar(kAccFree), (nitem - 1) & 1))) { ok = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t ring = base + kOffRing + st * kRingBytes + h * kPatchContent;
+                            const uint64_t go = smem_desc_at(kDesc64, ring + kRingDO), q = smem_desc_at(kDesc64, ring + kRingQ);
+                            const uint32_t a_p = tmem + kStep * buf;          // 16 queries a step: the first 16 of every 32 columns
+#pragma unroll
+                            for (int kk = 0; kk < kTile / 32; ++kk)
+                                mma_ts(tmem + kColDV, a_p + 32 * (kk >> 1) + 8 * (kk & 1), go + 64 * kk, kIdescT, (kk || !first) ? 1u : 0u);
+#pragma unroll
+                            for (int kk = 0; kk < kTile / 32; ++kk)
+                                mma_ts(tmem + kColDK, a_p + kColDP + 32 * (kk >> 1) + 8 * (kk & 1), q + 64 * kk, kIdescT, (kk || !first) ? 1u : 0u);
+                            mma_commit(on_unit(kPFree, u));
+                            // the tile's query-side rows may go: S^T, dP^T of both halves finished before P^T existed
+                            if (h == 1) mma_commit(bar(kQEmpty + st));
+                            if (last) mma_commit(bar(kAccFull));
+                        }
+                        __syncwarp();
+                        buf = buffer_after(buf, 1);
+                    }
+                }
+            } else {
+                // ---- dQ_I = dS K_J once both halves of dS are in shared memory (16 keys per step)
+                for (int t = 0; t < tiles; ++t, ++g) {
+                    if (!wait_all(on_unit(kPReady, 2 * g), unit_parity(2 * g)) || !wait_all(on_unit(kPReady, 2 * g + 1), unit_parity(2 * g)) ||
+                        (g > 0 && !wait_all(bar(kDQFree), (g - 1) & 1))) { ok = false; break; }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t k = smem_desc_at(kDesc64, base + kOffK + slot * kContentBytes);
+                        const uint64_t ds = smem_desc_at(kDescDS, base + kOffDS + (g & 1) * 2 * kDSHalf);
+#pragma unroll
+                        for (int kk = 0; kk < kTile / 16; ++kk)
+                            mma_ss(tmem + kColDQ, ds + 128 * kk, k + 64 * kk, kIdescQ, kk ? 1u : 0u);
+                        mma_commit(bar(kDSFree + (g & 1)));
+                        mma_commit(bar(kDQFull));
+                        // K_J and V_J may go once the item's last dQ is done (S^T, dP^T finished before it)
+                        if (t == tiles - 1) mma_commit(bar(kKVEmpty + slot));
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        // everything issued by this warp must have finished before TMEM is released
+        if (elect_one()) mma_commit(bar(kDrain + warp - 1));
+        __syncwarp();
+        mbar_wait(bar(kDrain + warp - 1), 0, abort_flag + 1, p.status);
+    } else if (warp < 20) {
+        // ===== P^T and dS^T: group h = warps 4 + 8h .. 11 + 8h takes half-tile (I, h), a warp 32 key rows (4 x 8 tokens) and 32 queries (4 x 8)
+        const int h = (warp - 4) >> 3;
+        const int cg = ((warp - 4) >> 2) & 1;                // queries 32 cg .. 32 cg + 31 of the half-tile
+        const int quarter = warp & 3;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
+        const uint32_t pitch = 4u * side, table_addr = base + kOffTable;
+        uint32_t g = 0, buf = h, ntable = 0;
+        int table_head = -1;
+        bool ok = true;
+        for (int item = first_item; item < last_item && ok; ++item) {
+            const LiveItem c = decode_bias_item(p.g, item);
+            if (c.h != table_head) {
+                // the table of head h: when all arithmetic warps are through with the last one's
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kTabDone));
+                if (!mbar_wait_warp(bar(kTabDone), ntable & 1, abort_flag, p.status)) { ok = false; break; }
+                gather_bias(p.source, c.h, side * side, reinterpret_cast<float*>(base_ptr + kOffTable), threadIdx.x - 128, kArithmeticThreads);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kTabReady));
+                if (!mbar_wait_warp(bar(kTabReady), ntable & 1, abort_flag, p.status)) { ok = false; break; }
+                ++ntable;
+                table_head = c.h;
+            }
+            const int key_patch = 2 * c.tp + (quarter >> 1);
+            const bool key_exists = key_patch < c.patches;
+            int ky, kx, Y0, X0;
+            patch_origin(p, c, key_patch, ky, kx, Y0, X0);
+            const int xk = lane >> 2, key_row0 = 4 * (quarter & 1);
+            // keys of the patch beyond the map's edge get probability 0: a thread's whole column, or the rows from `rows_there` on
+            const bool column_there = X0 + xk < p.W;
+            const int rows_there = p.H - Y0 - key_row0;          // of the thread's four
+            const uint32_t k_addr = table_addr + (ky + key_row0 + p.M - 1) * pitch + 4 * (kx + xk + p.M - 1 - 2 * (lane & 3));
+            const int tiles = (c.patches + 1) >> 1;
+            for (int I = 0; I < tiles; ++I, ++g) {
+                const uint32_t st = g % kQStages;
+                const uint32_t t_s = tmem + lane_base + 32 * cg + kStep * buf, t_dp = t_s + kColDP;
+                buf = buffer_after(buf, 2);
+                int qy, qx, QY0, QX0;
+                patch_origin(p, c, 2 * I + h, qy, qx, QY0, QX0);
+                const uint32_t b_addr = k_addr - (qy + 4 * cg) * pitch - 4 * qx;
+                // warp-uniform outcome: the TMEM accesses below are warp-collective
+                if (!mbar_wait_warp(on_unit(kSFull, 2 * g + h), unit_parity(2 * g), abort_flag, p.status) ||
+                    !mbar_wait_warp(bar(kQFull + st), (g / kQStages) & 1, abort_flag, p.status)) { ok = false; break; }
+                tc_fence_after();
+                // four pieces of 16 keys x 16 queries (piece c: lanes 16 (c % 2) .., queries 16 (c / 2) ..), read as 16-lane fragments: a thread holds 2 key
+                // rows of 2 x 2 queries of a piece
+                const uint32_t ld = base + kOffRing + st * kRingBytes + kRingLD + (32 * h + 16 * cg + (lane & 3)) * 16;
+                auto ldq = [&](int gq) { return make_float4(lds_f32(ld + 64 * gq), lds_f32(ld + 64 * gq + 4), lds_f32(ld + 64 * gq + 8), lds_f32(ld + 64 * gq + 12)); };
+                const uint32_t ds_line = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + (quarter * 32 + 8 * ((lane >> 3) & 1) + (lane & 7)) * 128;
+                auto load = [&](int c4, uint32_t (&s)[8], uint32_t (&dp)[8]) {
+                    const uint32_t at = ((uint32_t)(16 * (c4 & 1)) << 16) + 16 * (c4 >> 1);
+                    tmem_ld_16x256b_x2(t_s + at, s);
+                    tmem_ld_16x256b_x2(t_dp + at, dp);
+                };
+                // biases of key row a against query row b of the warp's rows, a - b = k (the queries' columns go up, so the offsets go down)
+                auto bias = [&](int k) {
+                    const float2 b = make_float2(lds_f32(b_addr + k * (int)pitch), lds_f32(b_addr + k * (int)pitch - 4));
+                    return column_there ? b : make_float2(-INFINITY, -INFINITY);
+                };
+                // bb[i]: a - b = k0 + i - 1 with k0 that of equal fragment rows (gq == rr)
+                auto work4 = [&](auto cut, int c4, const uint32_t (&s)[8], const uint32_t (&dp)[8], const float4 (&t)[2], const float2 (&bb)[3], uint32_t (&pp)[4], uint32_t (&dd)[4]) {
+#pragma unroll
+                    for (int gq = 0; gq < 2; ++gq)
+#pragma unroll
+                        for (int rr = 0; rr < 2; ++rr) {                  // key rows 2 (c % 2) + rr of the warp's, query rows 2 (c / 2) + gq
+                            const int i = 4 * gq + 2 * rr;
+                            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2,
+                                                        __fadd2_rn(make_float2(t[gq].x, t[gq].y), bb[1 + rr - gq]));
+                            float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                            if (cut.value && 2 * (c4 & 1) + rr >= rows_there) e = make_float2(0.f, 0.f);
+                            const float2 d = __fmul2_rn(e, __fadd2_rn(make_float2(__uint_as_float(dp[i]), __uint_as_float(dp[i + 1])), make_float2(t[gq].z, t[gq].w)));
+                            pp[2 * gq + rr] = pack_bf16x2(e.x, e.y);
+                            dd[2 * gq + rr] = pack_bf16x2(d.x, d.y);
+                        }
+                };
+                // dS tile: row = key, 128-byte line = the unit's 64 queries, 16-byte chunks swizzled by the row
+                auto store = [&](int c4, const uint32_t (&pp)[4], const uint32_t (&dd)[4]) {
+                    const uint32_t at = ((uint32_t)(16 * (c4 & 1)) << 16) + 8 * (c4 >> 1);
+                    tmem_st_16x128b_x2(t_s + at, pp);
+                    tmem_st_16x128b_x2(t_dp + at, dd);
+                    stmatrix_x4(ds_line + 16 * (c4 & 1) * 128 + (((cg * 4 + 2 * (c4 >> 1) + (lane >> 4)) ^ (lane & 7)) << 4), dd[0], dd[1], dd[2], dd[3]);
+                };
+                // The tile before the previous one is still read in this dS buffer.  (A barrier that has completed no phase answers yes to
+                // parity 1, which the first tiles ask for.)
+                const uint32_t b_ds = bar(kDSFree + (g & 1)), ds_parity = ((g >> 1) - 1) & 1;
+                uint32_t pp[4], dd[4];
+                if (!key_exists) {
+                    if (!mbar_wait_warp(b_ds, ds_parity, abort_flag, p.status)) { ok = false; break; }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) pp[e] = dd[e] = 0u;
+#pragma unroll
+                    for (int c4 = 0; c4 < 4; ++c4) store(c4, pp, dd);
+                } else {
+                    // Pieces in the order 1, 0, 3, 2: neighbours share pairs of biases (a - b = 1 2 3, -1 0 1, -1 0 1, -3 -2 -1).  A piece is stored while the
+                    // next but one is on its way, over scores that this warp has read.
+                    auto unit = [&](auto cut) -> bool {
+                        uint32_t s0[8], dp0[8], s1[8], dp1[8];
+                        float4 t[2];
+                        float2 bb[3];
+                        const bool ds_free = mbar_try_wait(b_ds, ds_parity);
+                        load(1, s1, dp1);
+                        load(0, s0, dp0);
+                        t[0] = ldq(0); t[1] = ldq(1);                         // queries 8 gq + 2 (lane % 4), + 1
+                        bb[0] = bias(1); bb[1] = bias(2); bb[2] = bias(3);
+                        tmem_wait_ld();
+                        work4(cut, 1, s1, dp1, t, bb, pp, dd);
+                        if (!__all_sync(0xffffffffu, ds_free) && !mbar_wait_warp(b_ds, ds_parity, abort_flag, p.status)) return false;
+                        load(3, s1, dp1);
+                        store(1, pp, dd);
+                        bb[2] = bb[0]; bb[0] = bias(-1); bb[1] = bias(0);
+                        work4(cut, 0, s0, dp0, t, bb, pp, dd);
+                        tmem_wait_ld();
+                        load(2, s0, dp0);
+                        store(0, pp, dd);
+                        t[0] = ldq(2); t[1] = ldq(3);
+                        work4(cut, 3, s1, dp1, t, bb, pp, dd);
+                        tmem_wait_ld();
+                        store(3, pp, dd);
+                        bb[2] = bb[0]; bb[0] = bias(-3); bb[1] = bias(-2);
+                        work4(cut, 2, s0, dp0, t, bb, pp, dd);
+                        store(2, pp, dd);
+                        return true;
+                    };
+                    if (!(rows_there < 4 ? unit(Flag<true>{}) : unit(Flag<false>{}))) { ok = false; break; }
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(on_unit(kPReady, 2 * g + h));
+            }
+        }
+    } else if (warp < 24) {
+        // ================================ drains: dQ after every tile, dV / dK after every item
+        const int quarter = warp & 3;
+        const int row = quarter * 32 + lane;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        auto drain_item = [&](const LiveItem& c, uint32_t nitem) -> bool {
+            // rows leave by TMA, a warp's 32 (half a patch) at a time; rows beyond the map's edge are dropped by it
+            int py, px, Y0, X0;
+            const int sp = 2 * c.tp + (quarter >> 1);
+            patch_origin(p, c, sp, py, px, Y0, X0);
+            const int Y = Y0 + 4 * (quarter & 1);
+            if (!mbar_wait_warp(bar(kAccFull), nitem & 1, abort_flag, p.status)) return false;
+            tc_fence_after();
+            const int sw = (row >> 1) & 3;                    // SWIZZLE_64B
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {         // dV through V's slot, dK through a tile of its own
+                uint8_t* const stage = base_ptr + (which == 0 ? kOffV + (nitem & 1) * kContentBytes : kOffDK) + row * 64;
+                const float f = which == 0 ? 1.f : p.inv_sqrt_d;
+                uint32_t a[32];
+                tmem_ld32(tmem + lane_base + (which == 0 ? kColDV : kColDK), a);
+                tmem_wait_ld();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(__uint_as_float(a[8 * q + 2 * e]) * f, __uint_as_float(a[8 * q + 2 * e + 1]) * f);
+                    *reinterpret_cast<uint4*>(stage + ((q ^ sw) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            tc_fence_before();
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(bar(kAccFree));
+                if (sp < c.patches && Y < p.H) {
+                    tma_store_5d(&tm_dv, base + kOffV + (nitem & 1) * kContentBytes + quarter * (kPatchContent / 2), 0, c.h, X0, Y, c.b);
+                    tma_store_5d(&tm_dk, base + kOffDK + quarter * (kPatchContent / 2), 0, c.h, X0, Y, c.b);
+                    bulk_commit_group();
+                }
+            }
+            return true;
+        };
+        uint32_t g = 0, nitem = 0;
+        bool ok = true;
+        for (int item = first_item; item < last_item && ok; ++item, ++nitem) {
+            const LiveItem c = decode_bias_item(p.g, item);
+            const int tiles = (c.patches + 1) >> 1;
+            float* const acc = p.dq_acc + pair_of(p, c) * kD * p.n;
+            for (int I = 0; I < tiles && ok; ++I, ++g) {
+                // (dV and dK before the item's last dQ: those of the next item wait for the accumulators)
+                if (I == tiles - 1) ok = drain_item(c, nitem);
+                if (!ok || !mbar_wait_warp(bar(kDQFull), g & 1, abort_flag, p.status)) { ok = false; break; }
+                tc_fence_after();
+                const int sp = 2 * I + (quarter >> 1);
+                int py, px, Y0, X0;
+                patch_origin(p, c, sp, py, px, Y0, X0);
+                float* dst = acc + 4 * (64 * (size_t)((py >> 3) * (p.M >> 3) + (px >> 3)) + (row & 63));
+#pragma unroll
+                for (int part = 0; part < kD / 16; ++part) {
+                    uint32_t a[16];
+                    tmem_ld16(tmem + lane_base + kColDQ + 16 * part, a);
+                    tmem_wait_ld();
+                    if (part + 1 == kD / 16) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(kDQFree));
+                    }
+                    if (sp < c.patches) {
+#pragma unroll
+                        for (int col = 0; col < 16; col += 4) {
+                            // The adds of a tile in one burst fill the queue that all warps' loads, stores and fences go through: a pause after each one
+                            red_add_f32x4(dst, a + col);
+                            dst += 4 * (size_t)p.n;
+                            __nanosleep(20);
+                        }
+                    }
+                }
+            }
+            if (ok) {
+                // V's slot, when its dV rows have been read
+                if (lane == 0) {
+                    bulk_wait_group_read<0>();                // (this thread's own stores)
+                    mbar_arrive(bar(kKVEmpty + (nitem & 1)));
+                }
+                __syncwarp();
+            }
+        }
+        if (lane == 0) bulk_wait_group<0>();
+        __syncwarp();
+    } else {
+        // ================================ gradient of the bias: warp 24 + 2 h + sub sums dS of key patch `sub` of the item and the queries of half h
+        const int h = (warp >> 1) & 1, sub = warp & 1;
+        // stacked identities: column lane / 4 of rows 2 (lane % 4), + 1
+        const uint32_t eye = (2 * (lane & 3) == (lane >> 2) ? 0x3F80u : 0u) | (2 * (lane & 3) + 1 == (lane >> 2) ? 0x3F800000u : 0u);
+        const int m = lane >> 3, xrow = lane & 7;             // this lane names row `xrow` of matrix m of an ldmatrix
+        uint32_t g = 0;
+        bool ok = true;
+        for (int item = first_item; item < last_item && ok; ++item) {
+            const LiveItem c = decode_bias_item(p.g, item);
+            const int tiles = (c.patches + 1) >> 1;
+            int ky, kx, Y0, X0;
+            patch_origin(p, c, 2 * c.tp + sub, ky, kx, Y0, X0);
+            const bool key_exists = 2 * c.tp + sub < c.patches;
+            for (int I = 0; I < tiles; ++I, ++g) {
+                if (!mbar_wait_warp(on_unit(kPReady, 2 * g + h), unit_parity(2 * g), abort_flag, p.status)) { ok = false; break; }
+                const uint32_t tile = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + sub * 64 * 128 + xrow * 128;
+                // block (key row a, query row b): 8 lines of 128 bytes from line 8 a, chunk b of each, swizzled by the line
+                auto block = [&](int a, int b) { return tile + a * 1024 + ((b ^ xrow) << 4); };
+                float acc[8][4];                              // [k]: differences a - b = k (rows 0-7 of the product) and -k (rows 8-15); [0]: both 0
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[k][e] = 0.f;
+#pragma unroll
+                for (int k = 1; k < 8; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8 - k; i += 2) {
+                        // matrices 0, 2: blocks (k + i, i) and the next one along the diagonal; 1, 3: (i, k + i) and its next one
+                        const int lo = i + (m >> 1);
+                        const int top = min(k + lo, 7);       // (the diagonal's odd end: the block read twice counts once)
+                        uint32_t a[4];
+                        ldmatrix_x4(m & 1 ? block(lo, top) : block(top, lo), a);
+                        const bool both = i + 1 < 8 - k;
+                        mma_16816(acc[k], a[0], a[1], both ? a[2] : 0u, both ? a[3] : 0u, eye, eye);
+                    }
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    uint32_t a[4];
+                    ldmatrix_x4(block(i + m, i + m), a);
+                    mma_16816(acc[0], a[0], a[1], a[2], a[3], eye, eye);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kDSFree + (g & 1)));
+                if (!key_exists || 2 * I + h >= c.patches) continue;
+                int qy, qx, QY0, QX0;
+                patch_origin(p, c, 2 * I + h, qy, qx, QY0, QX0);
+                double* const to = p.offsets + (size_t)c.h * side * side + (size_t)(ky - qy + p.M - 1) * side + (kx - qx + p.M - 1) + (lane >> 2) - 2 * (lane & 3);
+                acc[0][0] += acc[0][2]; acc[0][1] += acc[0][3];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int e = 0; e < (k ? 4 : 2); ++e)
+                        if (acc[k][e] != 0.f) atomicAdd(to + (e < 2 ? k : -k) * side - (e & 1), (double)acc[k][e]);
+            }
+        }
+    }
+    // ================================================================================ common tail
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 2) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+// ------------------------------------------------------------------ preparation and finishing
+struct AuxParams {
+    const __nv_bfloat16* out;
+    const __nv_bfloat16* dout;
+    const float* lse;
+    float2* ld;
+    float* dq_acc;
+    double* sums;                // BiasGrad, cleared here
+    size_t sum_words;
+    __nv_bfloat16* dq;
+    int H, W, heads, M, s, n, nWy, nWx, pairs, d, Hp, Wp;
+    float inv_sqrt_d;
+};
+
+// Returns false for a window position beyond the image: no token there.
+__device__ __forceinline__ bool decode_pair_token(const AuxParams& p, int pair, int w, size_t& tok, size_t& scalar)
+{
+    const int h = pair % p.heads; pair /= p.heads;
+    const int wx = pair % p.nWx; pair /= p.nWx;
+    const int wy = pair % p.nWy; pair /= p.nWy;
+    const int b = pair;
+    int i, Y, X;
+    window_order_token(WindowGeom{p.Hp, p.Wp, p.M, p.s}, wy, wx, w, i, Y, X);
+    tok = (((size_t)b * p.H + Y) * p.W + X) * p.heads + h;
+    scalar = (((size_t)b * p.heads + h) * p.H + Y) * p.W + X;
+    return Y < p.H && X < p.W;
+}
+
+// Four lanes per (pair, token in window order), 8 channels each: D = dO . O and lse in the layout the main kernel streams; the dQ accumulators and
+// the sums of the bias gradient are cleared as flat arrays.  A query that is no token, or whose row has no key (lse = -inf), reads -inf for -lse:
+// probability 0.
+__global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxParams p)
+{
+    const size_t total = (size_t)p.pairs * p.n;
+    const size_t thread = (size_t)blockIdx.x * blockDim.x + threadIdx.x, t = thread >> 2;
+    const int part = (int)(thread & 3);
+    const size_t nthreads = (size_t)gridDim.x * blockDim.x;
+    for (size_t e = thread; e < p.sum_words; e += nthreads) p.sums[e] = 0.0;
+    if (thread < 32) reinterpret_cast<float4*>(p.ld + total)[thread] = make_float4(-INFINITY, -INFINITY, 0.f, 0.f);      // the patch of no queries
+    if (t >= total) return;                                // (whole warps: total is a multiple of 64)
+    const int pair = (int)(t / p.n), w = (int)(t % p.n);
+    size_t tok, scalar;
+    const bool real = decode_pair_token(p, pair, w, tok, scalar);
+    uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
+    float lse = -INFINITY;
+    if (real && 8 * part < p.d) {
+        x = __ldg(reinterpret_cast<const uint4*>(p.dout + tok * p.d) + part);
+        y = __ldg(reinterpret_cast<const uint4*>(p.out + tok * p.d) + part);
+        if (part == 0) lse = p.lse[scalar];
+    }
+    float4* z4 = reinterpret_cast<float4*>(p.dq_acc);      // pairs * 32 * n floats = total * 8 vectors
+#pragma unroll
+    for (int k = 0; k < kD / 16; ++k) z4[(size_t)k * 4 * total + thread] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    float acc = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        acc = fmaf(__uint_as_float(xs[k] << 16), __uint_as_float(ys[k] << 16), acc);
+        acc = fmaf(__uint_as_float(xs[k] & 0xffff0000u), __uint_as_float(ys[k] & 0xffff0000u), acc);
+    }
+    acc += __shfl_xor_sync(0xffffffffu, acc, 1);
+    acc += __shfl_xor_sync(0xffffffffu, acc, 2);
+    if (part == 0) {
+        float* ldf = reinterpret_cast<float*>(p.ld) + ((t >> 1) << 2) + (t & 1);
+        const bool none = lse == -INFINITY;
+        ldf[0] = none ? -INFINITY : -lse * kLog2e;
+        ldf[2] = none ? 0.f : -acc;
+    }
+}
+
+// dq = bf16(accumulator / sqrt(d)): a thread per token and half row (16 columns: four 16-byte reads, 512 bytes per warp and read).
+__global__ void __launch_bounds__(256) rib_bias_bwd_finish_kernel(const AuxParams p)
+{
+    const size_t total = (size_t)p.pairs * p.n;
+    const size_t thread = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+    // 32 tokens x 2 halves per two warps
+    const size_t t = (thread >> 6) * 32 + (thread & 31);
+    const int half = (int)(thread >> 5) & 1;
+    const int channels = min(16, p.d - 16 * half);
+    if (t >= total || channels <= 0) return;
+    const int pair = (int)(t / p.n), w = (int)(t % p.n);
+    size_t tok, scalar;
+    if (!decode_pair_token(p, pair, w, tok, scalar)) return;
+    const float4* src = reinterpret_cast<const float4*>(p.dq_acc + (size_t)pair * kD * p.n) + (size_t)(4 * half) * p.n + w;
+    uint32_t v[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float4 f = src[(size_t)q * p.n];
+        v[2 * q] = pack_bf16x2(f.x * p.inv_sqrt_d, f.y * p.inv_sqrt_d);
+        v[2 * q + 1] = pack_bf16x2(f.z * p.inv_sqrt_d, f.w * p.inv_sqrt_d);
+    }
+    uint4* dst = reinterpret_cast<uint4*>(p.dq + tok * p.d) + 2 * half;
+    dst[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    if (channels > 8) dst[1] = make_uint4(v[4], v[5], v[6], v[7]);
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+size_t ld_bytes(long long pairs, int n) { return align256(((size_t)pairs * n + 64) * sizeof(float2)); }
+
+}  // namespace
+
+bool sm100_bias_bwd_supported(const Problem& p)
+{
+    BiasItems g;
+    return bias_shape_supported(p) && make_bias_items(p, 2, &g);
+}
+
+size_t sm100_bias_bwd_workspace_bytes(long long pairs, int n) { return ld_bytes(pairs, n) + align256((size_t)pairs * kD * n * sizeof(float)); }
+
+cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t stream)
+{
+    if (!encode_fn()) return cudaErrorNotSupported;
+    uint8_t* ws = static_cast<uint8_t*>(p.workspace);
+    float2* ld = reinterpret_cast<float2*>(ws);
+    float* dq_acc = reinterpret_cast<float*>(ws + ld_bytes(p.pairs, p.n));
+    CUtensorMap tm_q, tm_k, tm_v, tm_do, tm_dk, tm_dv;
+    if (!encode_image_map(&tm_q, p.q, p) || !encode_image_map(&tm_k, p.k, p) || !encode_image_map(&tm_v, p.v, p) || !encode_image_map(&tm_do, p.dout, p) ||
+        !encode_image_map(&tm_dk, p.dk, p, 4) || !encode_image_map(&tm_dv, p.dv, p, 4))
+        return cudaErrorInvalidValue;
+    static KernelSetup setup;
+    int sm_count = 0;
+    if (cudaError_t e = setup.prepare(rib_bias_bwd_kernel, smem_bytes(kBiasMaxWindow), &sm_count)) return e;
+    Params bp{};
+    if (!make_bias_items(p, 2, &bp.g)) return cudaErrorInvalidValue;
+    AuxParams ap{};
+    ap.out = p.out; ap.dout = p.dout; ap.lse = p.lse_in; ap.ld = ld; ap.dq_acc = dq_acc; ap.dq = p.dq;
+    ap.sums = grad.offsets; ap.sum_words = grad.bytes / sizeof(double);
+    ap.H = p.H; ap.W = p.W; ap.heads = p.heads; ap.M = p.M; ap.s = p.s; ap.n = p.n; ap.nWy = p.nWy; ap.nWx = p.nWx;
+    ap.pairs = p.pairs; ap.d = p.d; ap.Hp = p.Hp; ap.Wp = p.Wp;
+    ap.inv_sqrt_d = 1.f / sqrtf((float)p.d);
+    const size_t tokens = (size_t)p.pairs * p.n;
+    { ProfileScope scope(RIB_KERNEL_BIAS_BWD_PREPARE, stream); rib_bias_bwd_prepare_kernel<<<(unsigned)((tokens + 63) / 64), 256, 0, stream>>>(ap); }
+    if (cudaError_t e = cudaGetLastError()) return e;
+    bp.ld = ld; bp.dq_acc = dq_acc; bp.offsets = grad.offsets; bp.status = p.status;
+    bp.no_queries = (long long)tokens;
+    bp.H = p.H; bp.W = p.W; bp.heads = p.heads; bp.M = p.M; bp.s = p.s; bp.n = p.n; bp.nWy = p.nWy; bp.nWx = p.nWx; bp.Hp = p.Hp; bp.Wp = p.Wp;
+    bp.items = bp.g.per_head * p.heads;
+    bp.scale_log2 = kLog2e / sqrtf((float)p.d);
+    bp.inv_sqrt_d = ap.inv_sqrt_d;
+    bp.source = bias_source(p);
+    const int grid = bp.items < sm_count ? bp.items : sm_count;
+    { ProfileScope scope(RIB_KERNEL_BIAS_BWD, stream); rib_bias_bwd_kernel<<<grid, kThreads, smem_bytes(p.M), stream>>>(tm_q, tm_k, tm_v, tm_do, tm_dk, tm_dv, bp); }
+    if (cudaError_t e = cudaGetLastError()) return e;
+    { ProfileScope scope(RIB_KERNEL_BIAS_BWD_FINISH, stream); rib_bias_bwd_finish_kernel<<<(unsigned)((tokens + 127) / 128), 256, 0, stream>>>(ap); }
+    if (cudaError_t e = cudaGetLastError()) return e;
+    return bias_grad_finish(p, grad, stream);
+}
+
+}  // namespace rib

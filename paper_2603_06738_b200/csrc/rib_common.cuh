@@ -93,6 +93,9 @@ cudaError_t bias_grad_clear(const BiasGrad& g, cudaStream_t stream);
 cudaError_t bias_grad_finish(const Problem& p, const BiasGrad& g, cudaStream_t stream);
 bool sm100_bias_fwd_supported(const Problem& p);
 cudaError_t sm100_bias_fwd(const Problem& p, cudaStream_t stream);
+bool sm100_bias_bwd_supported(const Problem& p);
+size_t sm100_bias_bwd_workspace_bytes(long long pairs, int n);
+cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t stream);       // 4 kernels
 
 // Rows of bf16 as whole numbers of 8 bits with a scale each, and back (rib_checkpoint.cu).
 cudaError_t checkpoint_store(const __nv_bfloat16* x, long long rows, int d, int8_t* codes, float* scales, cudaStream_t stream);

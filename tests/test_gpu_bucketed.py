@@ -9,7 +9,9 @@ largest value, those of the rank-r kernels.  lse is fp32: its error is that of l
 
 The gradients are compared with the oracle's for the out and lse that the backward pass was given: D = rowsum(dO o out) of a rounded out is off
 by up to 2^-8 of its terms, which is a property of that input and, where rows are all but one key each or a bucket's sum cancels, larger
-than the gradients themselves."""
+than the gradients themselves.  dbias is a sum of many dS of both signs, which the tcgen05 kernels round to bf16 first: independent errors, so
+in L2 2^-8 / sqrt(3) x |dS| in the mean; four times that is allowed beside the relative bound (`noise`), which counts where the sum of a bucket
+cancels (one bucket for all keys: it is 0)."""
 import numpy as np
 import pytest
 import torch
@@ -60,8 +62,12 @@ def close(name, got, ref, rel_l2=5e-3, noise=0.0):
     if ref.size == 0:
         return
     err, norm = np.abs(got - ref).max(), np.linalg.norm(ref)
-    assert err <= 1e-2 * max(1.0, np.abs(ref).max()), (name, err)
+    assert err <= 1e-2 * max(1.0, np.abs(ref).max()) + noise, (name, err)
     assert np.linalg.norm(got - ref) <= rel_l2 * norm + 1e-5 * np.sqrt(ref.size) + noise, (name, np.linalg.norm(got - ref) / norm)
+
+
+def sum_noise(norm):
+    return 4 * 2.0 ** -8 / 3 ** 0.5 * norm
 
 
 def check(inputs, M, s, masked=False, path="auto", fast=None):
@@ -79,13 +85,14 @@ def check(inputs, M, s, masked=False, path="auto", fast=None):
     assert binding.rib_query_status() == 0
     if fast is not None:
         want = binding.RIB_PATH_SM100 if fast and path != "generic" else binding.RIB_PATH_GENERIC
-        assert used[0] == want
+        assert used == [want, want]
     f = [to_f64(t) for t in (q, k, v, bias)] + [named.numpy()]
     ref_out, ref_lse = orc.fwd(*f, M, s, masked)
     close("out", out, ref_out)
     close("lse", lse, ref_lse)
-    for name, got, ref in zip(("dq", "dk", "dv", "dbias"), grads, orc.bwd(*f, to_f64(dout), M, s, masked, out=to_f64(out), lse=to_f64(lse))):
-        close(name, got, ref)
+    *refs, norm = orc.bwd(*f, to_f64(dout), M, s, masked, out=to_f64(out), lse=to_f64(lse), want_norm=True)
+    for name, got, ref in zip(("dq", "dk", "dv", "dbias"), grads, refs):
+        close(name, got, ref, noise=sum_noise(norm) if name == "dbias" else 0.0)
     assert grads[3].dtype == bias.dtype and grads[3].shape == bias.shape
     return out, lse, grads
 
@@ -197,7 +204,8 @@ def test_strides_between_tables_and_untouched_elements():
                                             *[p(x) for x in grads], p(dwide), p(ws), need, s) == 0
     ref = binding.rib_window_attn_fwd_bucketed(*t[:3], bias.cuda(), t[4], M, 8)
     assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1]) and (dwide[:, count:] == 7.0).all()
-    close("dbias", dwide[:, :count], orc.bwd(*(to_f64(x) for x in (q, k, v, bias)), named.numpy(), to_f64(dout), M, 8, out=to_f64(out), lse=to_f64(lse))[3])
+    *refs, norm = orc.bwd(*(to_f64(x) for x in (q, k, v, bias)), named.numpy(), to_f64(dout), M, 8, out=to_f64(out), lse=to_f64(lse), want_norm=True)
+    close("dbias", dwide[:, :count], refs[3], noise=sum_noise(norm))
 
 
 def test_other_streams_graphs_and_repeats():
@@ -245,6 +253,6 @@ def test_a_training_loop_uses_them_together():
         dout = (out.float() - want.float()).bfloat16()
         grads = binding.rib_window_attn_bwd_bucketed(q, k, v, bias, named, out, lse, dout, M, 8)
         assert all(torch.isfinite(t.float()).all() for t in grads)
-        close("dbias", grads[3], orc.bwd(*(to_f64(t) for t in (q, k, v, bias)), named.cpu().numpy(), to_f64(dout), M, 8, out=to_f64(out), lse=to_f64(lse))[3],
-              noise=2.0 ** -18 * longest * dout.float().norm().item())
+        *refs, norm = orc.bwd(*(to_f64(t) for t in (q, k, v, bias)), named.cpu().numpy(), to_f64(dout), M, 8, out=to_f64(out), lse=to_f64(lse), want_norm=True)
+        close("dbias", grads[3], refs[3], noise=sum_noise(norm) + 2.0 ** -18 * longest * dout.float().norm().item())
         bias -= 2.0 * grads[3]
