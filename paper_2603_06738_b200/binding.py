@@ -7,6 +7,7 @@ raises ``RibLibraryMissing``.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import warnings
 from pathlib import Path
@@ -714,6 +715,17 @@ def rib_window_attn_bwd_noalloc(q, k, v, pq, pk, out, lse, dout, dq, dk, dv, dpq
         raise RibError(rc)
 
 
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+def _on(device, *tensors):
+    """The calls below launch on the device of their tensors, whichever is current (a stream that is given has to be one of its)."""
+    for t in tensors:
+        if t.device != device:
+            raise ValueError(f"all tensors of a call have to be on one device: got {t.device} beside {device}")
+    return _SAME_DEVICE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
 def _check_bias(bias, buckets, heads, window, device):
     """(dtype, elements between the heads' tables, number of buckets) of a bias [heads, buckets] or [buckets] (shared by the heads)."""
     if bias.dtype not in (torch.float32, torch.bfloat16) or not bias.is_contiguous() or bias.device != device:
@@ -732,15 +744,20 @@ def rib_window_attn_fwd_bucketed(q, k, v, bias, buckets, window, shift=0, masked
     the heads), buckets int32 [2 window - 1, 2 window - 1], the bucket of every offset key - query (outside [0, num_buckets): not
     attended to).  Any H and W; `masked` keeps the wrapped parts of shifted windows apart (H, W multiples of the window).
     Returns (out, lse)."""
+    if _marshal is not None:
+        got = _native(_marshal.fwd_bucketed, "rib_window_attn_fwd_bucketed", q, k, v, bias, buckets, window, shift, masked, want_lse, stream)
+        if got is not None:
+            return got
     _check_image("q", q)
     B, H, W, heads, d = q.shape
     _check_image("k", k, q.shape)
     _check_image("v", v, q.shape)
     dtype, stride, count = _check_bias(bias, buckets, heads, window, q.device)
-    out = torch.empty_like(q)
-    lse = torch.empty((B, heads, H, W), dtype=torch.float32, device=q.device) if want_lse else None
-    rc = library().rib_window_attn_fwd_bucketed(_ptr(q), _ptr(k), _ptr(v), _ptr(bias), dtype, stride, _ptr(buckets), count, B, H, W, heads, d,
-                                                window, shift, int(masked), _ptr(out), _ptr(lse), _stream_ptr(stream))
+    with _on(q.device, k, v):
+        out = torch.empty_like(q)
+        lse = torch.empty((B, heads, H, W), dtype=torch.float32, device=q.device) if want_lse else None
+        rc = library().rib_window_attn_fwd_bucketed(_ptr(q), _ptr(k), _ptr(v), _ptr(bias), dtype, stride, _ptr(buckets), count, B, H, W, heads, d,
+                                                    window, shift, int(masked), _ptr(out), _ptr(lse), _stream_ptr(stream))
     if rc != RIB_OK:
         raise RibError(rc)
     return out, lse
@@ -757,6 +774,11 @@ def rib_window_attn_bwd_bucketed_workspace(bias_head_stride, num_buckets, B, H, 
 
 def rib_window_attn_bwd_bucketed(q, k, v, bias, buckets, out, lse, dout, window, shift=0, masked=False, workspace=None, stream=None):
     """Backward pass of rib_window_attn_fwd_bucketed.  Returns (dq, dk, dv bf16, dbias of bias's shape and type)."""
+    if _marshal is not None:
+        call = lambda address, *args: _marshal.bwd_bucketed(address, _lib.rib_addresses["rib_window_attn_bwd_bucketed_workspace"], *args)  # noqa: E731
+        got = _native(call, "rib_window_attn_bwd_bucketed", q, k, v, bias, buckets, out, lse, dout, window, shift, masked, workspace, stream)
+        if got is not None:
+            return got
     _check_image("q", q)
     B, H, W, heads, d = q.shape
     for name, t in (("k", k), ("v", v), ("out", out), ("dout", dout)):
@@ -766,10 +788,11 @@ def rib_window_attn_bwd_bucketed(q, k, v, bias, buckets, out, lse, dout, window,
     if workspace is None:
         need = rib_window_attn_bwd_bucketed_workspace(stride, count, B, H, W, heads, d, window)
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
-    dq, dk, dv, dbias = torch.empty_like(q), torch.empty_like(q), torch.empty_like(q), torch.empty_like(bias)
-    rc = library().rib_window_attn_bwd_bucketed(_ptr(q), _ptr(k), _ptr(v), _ptr(bias), dtype, stride, _ptr(buckets), count, _ptr(out), _ptr(lse),
-                                                _ptr(dout), B, H, W, heads, d, window, shift, int(masked), _ptr(dq), _ptr(dk), _ptr(dv),
-                                                _ptr(dbias), _ptr(workspace), workspace.numel(), _stream_ptr(stream))
+    with _on(q.device, k, v, out, dout, workspace):
+        dq, dk, dv, dbias = torch.empty_like(q), torch.empty_like(q), torch.empty_like(q), torch.empty_like(bias)
+        rc = library().rib_window_attn_bwd_bucketed(_ptr(q), _ptr(k), _ptr(v), _ptr(bias), dtype, stride, _ptr(buckets), count, _ptr(out), _ptr(lse),
+                                                    _ptr(dout), B, H, W, heads, d, window, shift, int(masked), _ptr(dq), _ptr(dk), _ptr(dv),
+                                                    _ptr(dbias), _ptr(workspace), workspace.numel(), _stream_ptr(stream))
     if rc != RIB_OK:
         raise RibError(rc)
     return dq, dk, dv, dbias
@@ -777,6 +800,10 @@ def rib_window_attn_bwd_bucketed(q, k, v, bias, buckets, out, lse, dout, window,
 
 def rib_checkpoint_store(x, stream=None):
     """x bf16 [..., d], d <= 64, as (codes int8 of x's shape, scales fp32 of x's shape without its last dimension)."""
+    if _marshal is not None:
+        got = _native(_marshal.store, "rib_checkpoint_store", x, stream)
+        if got is not None:
+            return got
     if x.dtype != torch.bfloat16 or not x.is_cuda or not x.is_contiguous() or x.dim() < 1:
         raise ValueError("x must be a contiguous CUDA bfloat16 tensor [..., d]")
     d = x.shape[-1]
@@ -784,7 +811,8 @@ def rib_checkpoint_store(x, stream=None):
     scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     if x.numel() == 0 and 0 < d <= 64:
         return codes, scales
-    rc = library().rib_checkpoint_store(_ptr(x), scales.numel(), d, _ptr(codes), _ptr(scales), _stream_ptr(stream))
+    with _on(x.device):
+        rc = library().rib_checkpoint_store(_ptr(x), scales.numel(), d, _ptr(codes), _ptr(scales), _stream_ptr(stream))
     if rc != RIB_OK:
         raise RibError(rc)
     return codes, scales
@@ -799,11 +827,16 @@ def _check_checkpoint(name, codes, scales, shape=None):
 
 def rib_checkpoint_restore(codes, scales, stream=None):
     """What rib_checkpoint_store kept, as bf16."""
+    if _marshal is not None:
+        got = _native(_marshal.restore, "rib_checkpoint_restore", codes, scales, stream)
+        if got is not None:
+            return got[0]
     _check_checkpoint("x", codes, scales)
     x = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device)
     if x.numel() == 0 and 0 < codes.shape[-1] <= 64:
         return x
-    rc = library().rib_checkpoint_restore(_ptr(codes), _ptr(scales), scales.numel(), codes.shape[-1], _ptr(x), _stream_ptr(stream))
+    with _on(x.device):
+        rc = library().rib_checkpoint_restore(_ptr(codes), _ptr(scales), scales.numel(), codes.shape[-1], _ptr(x), _stream_ptr(stream))
     if rc != RIB_OK:
         raise RibError(rc)
     return x
@@ -836,12 +869,13 @@ def rib_window_attn_bwd_checkpointed(q, k, v, out, pq, pk, lse, dout, window, sh
     if workspace is None:
         need = int(library().rib_window_attn_bwd_checkpointed_workspace(stride, B, H, W, heads, d, r, window))
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dout.device)
-    dq, dk, dv = torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(dout)
-    dpq = torch.empty(tuple(pq.shape), dtype=torch.float32, device=dout.device)
-    dpk = torch.empty(tuple(pk.shape), dtype=torch.float32, device=dout.device)
-    rc = library().rib_window_attn_bwd_checkpointed(saved, _ptr(pq), _ptr(pk), stride, _ptr(lse), _ptr(dout), B, H, W, heads, d, r, window, shift,
-                                                    int(masked), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dpq), _ptr(dpk), _ptr(workspace),
-                                                    workspace.numel(), _stream_ptr(stream))
+    with _on(dout.device, q[0], k[0], v[0], out[0], pq, pk, workspace):
+        dq, dk, dv = torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(dout)
+        dpq = torch.empty(tuple(pq.shape), dtype=torch.float32, device=dout.device)
+        dpk = torch.empty(tuple(pk.shape), dtype=torch.float32, device=dout.device)
+        rc = library().rib_window_attn_bwd_checkpointed(saved, _ptr(pq), _ptr(pk), stride, _ptr(lse), _ptr(dout), B, H, W, heads, d, r, window, shift,
+                                                        int(masked), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dpq), _ptr(dpk), _ptr(workspace),
+                                                        workspace.numel(), _stream_ptr(stream))
     if rc != RIB_OK:
         raise RibError(rc)
     return dq, dk, dv, dpq, dpk
@@ -857,10 +891,11 @@ def rib_window_attn_bwd_bucketed_checkpointed(q, k, v, out, bias, buckets, lse, 
     if workspace is None:
         need = int(library().rib_window_attn_bwd_bucketed_checkpointed_workspace(stride, count, B, H, W, heads, d, window))
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dout.device)
-    dq, dk, dv, dbias = torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(bias)
-    rc = library().rib_window_attn_bwd_bucketed_checkpointed(saved, _ptr(bias), dtype, stride, _ptr(buckets), count, _ptr(lse), _ptr(dout), B, H, W,
-                                                             heads, d, window, shift, int(masked), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbias),
-                                                             _ptr(workspace), workspace.numel(), _stream_ptr(stream))
+    with _on(dout.device, q[0], k[0], v[0], out[0], workspace):
+        dq, dk, dv, dbias = torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(bias)
+        rc = library().rib_window_attn_bwd_bucketed_checkpointed(saved, _ptr(bias), dtype, stride, _ptr(buckets), count, _ptr(lse), _ptr(dout), B, H, W,
+                                                                 heads, d, window, shift, int(masked), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbias),
+                                                                 _ptr(workspace), workspace.numel(), _stream_ptr(stream))
     if rc != RIB_OK:
         raise RibError(rc)
     return dq, dk, dv, dbias

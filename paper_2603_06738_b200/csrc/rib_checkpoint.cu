@@ -2,49 +2,193 @@
 //     scale = max_c |x_c| * (1/127),   code_c = round(x_c / scale),   restored x_c = bf16(code_c * scale),
 // rounding half to even, division and products as IEEE fp32.  A row of zeros has scale 0; a row with an infinity or a NaN gets the scale
 // NaN and comes back as NaN, so that an overflow is not lost on the way through the checkpoint.
+//
+// Both directions are bound by memory: 2 d bytes on one side, d + 4 on the other.  Rows of 8, 16, ... 64 channels (16-byte aligned): a thread has 8
+// channels of a row - one 16-byte access to x, one of 8 bytes to the codes, neighbours side by side - and the lanes of a row share its
+// maximum by shuffles.  Other widths: a block takes 64 rows, whose bytes are whole 16-byte words on both sides, through shared memory.
 #include "rib_common.cuh"
 
 namespace rib {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kStagedRows = 64;
 
-// One warp per row, a lane per two channels (d <= 64).
-__global__ void __launch_bounds__(kThreads) rib_checkpoint_store_kernel(const __nv_bfloat16* x, long long rows, int d, int8_t* codes, float* scales)
+// Quotients decide codes, so they are those of the IEEE division; but x * (1 / scale) is off by less than 127 x 2^-22 = 3e-5, and unless it lies that
+// near to a border between two codes it names the same one.  (A scale below 2^-126 has no reciprocal: the test fails for infinities and NaN.)
+__device__ __forceinline__ int code_of(float x, float scale, float inverse)
 {
-    const long long row = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5;
-    const int lane = threadIdx.x & 31;
-    if (row >= rows) return;
-    const float a = lane < d ? __bfloat162float(x[row * d + lane]) : 0.f;
-    const float b = lane + 32 < d ? __bfloat162float(x[row * d + lane + 32]) : 0.f;
-    float most = fmaxf(fabsf(a), fabsf(b));
-    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-    const bool bad = __any_sync(0xffffffffu, !isfinite(a) || !isfinite(b));
-    const float scale = bad ? __int_as_float(0x7fffffff) : most * (1.f / 127.f);
-    const bool zero = bad || scale == 0.f;
-    if (lane < d) codes[row * d + lane] = zero ? 0 : (int8_t)__float2int_rn(__fdiv_rn(a, scale));
-    if (lane + 32 < d) codes[row * d + lane + 32] = zero ? 0 : (int8_t)__float2int_rn(__fdiv_rn(b, scale));
-    if (lane == 0) scales[row] = scale;
+    const float t = x * inverse, n = rintf(t);
+    if (!(fabsf(t - n) < 0.4999f)) return __float2int_rn(__fdiv_rn(x, scale));
+    return (int)n;
+}
+
+struct RowScale { float scale, inverse; bool zero; };
+__device__ __forceinline__ RowScale row_scale(float most, bool bad)
+{
+    RowScale r;
+    r.scale = bad ? __int_as_float(0x7fffffff) : most * (1.f / 127.f);
+    r.zero = bad || r.scale == 0.f;
+    r.inverse = 1.f / r.scale;
+    return r;
+}
+
+// kLanes lanes to a row (a power of two, the last ones without channels where d / 8 is none), kRows rows of kThreads / kLanes per block
+template <int kLanes>
+__global__ void __launch_bounds__(kThreads) rib_checkpoint_store_kernel(const __nv_bfloat16* __restrict__ x, long long rows, int d, int8_t* __restrict__ codes, float* __restrict__ scales)
+{
+    constexpr int kUnroll = 4, kRowsAtOnce = kThreads / kLanes;
+    const int part = threadIdx.x % kLanes;
+    const bool mine = 8 * part < d;
+    const long long row0 = (long long)blockIdx.x * (kUnroll * kRowsAtOnce) + threadIdx.x / kLanes;
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        const long long row = row0 + k * kRowsAtOnce;
+        v[k] = mine && row < rows ? __ldg(reinterpret_cast<const uint4*>(x + row * d) + part) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        const long long row = row0 + k * kRowsAtOnce;
+        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        // the largest magnitude as an integer: magnitudes of bf16 are ordered like their bits, infinity and NaN behind all others
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = max(most, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+#pragma unroll
+        for (int o = kLanes / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+        const RowScale s = row_scale(__uint_as_float(most << 16), most >= 0x7f80u);
+        uint32_t c[2] = {0u, 0u};
+        if (!s.zero) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int lo = code_of(__uint_as_float(w[i] << 16), s.scale, s.inverse), hi = code_of(__uint_as_float(w[i] & 0xffff0000u), s.scale, s.inverse);
+                c[i >> 1] |= ((uint32_t)(lo & 255) | (uint32_t)(hi & 255) << 8) << (16 * (i & 1));
+            }
+        }
+        if (row < rows) {
+            if (mine) *reinterpret_cast<uint2*>(codes + row * d + 8 * part) = make_uint2(c[0], c[1]);
+            if (part == 0) scales[row] = s.scale;
+        }
+    }
+}
+
+// any d: 64 rows of a block through shared memory
+__global__ void __launch_bounds__(kThreads) rib_checkpoint_store_staged_kernel(const __nv_bfloat16* __restrict__ x, long long rows, int d, int8_t* __restrict__ codes, float* __restrict__ scales)
+{
+    __shared__ __align__(16) __nv_bfloat16 xs[kStagedRows * 64];
+    __shared__ __align__(16) int8_t cs[kStagedRows * 64];
+    const long long row0 = (long long)blockIdx.x * kStagedRows;
+    const int here = (int)min((long long)kStagedRows, rows - row0), elements = here * d;
+    const __nv_bfloat16* src = x + row0 * d;
+    for (int e = 8 * threadIdx.x; e < elements; e += 8 * kThreads) {
+        if (e + 8 <= elements) *reinterpret_cast<uint4*>(xs + e) = __ldg(reinterpret_cast<const uint4*>(src + e));
+        else for (int i = e; i < elements; ++i) xs[i] = src[i];
+    }
+    __syncthreads();
+    // four lanes to a row
+    const int r = threadIdx.x >> 2, part = threadIdx.x & 3;
+    float most = 0.f;
+    bool bad = false;
+    if (r < here)
+        for (int c = part; c < d; c += 4) {
+            const float a = fabsf(__bfloat162float(xs[r * d + c]));
+            bad = bad || !isfinite(a);
+            most = fmaxf(most, a);
+        }
+    for (int o = 1; o < 4; o <<= 1) {
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        bad = __shfl_xor_sync(0xffffffffu, bad ? 1 : 0, o) != 0 || bad;
+    }
+    const RowScale s = row_scale(most, bad);
+    if (r < here) {
+        for (int c = part; c < d; c += 4) cs[r * d + c] = s.zero ? 0 : (int8_t)code_of(__bfloat162float(xs[r * d + c]), s.scale, s.inverse);
+        if (part == 0) scales[row0 + r] = s.scale;
+    }
+    __syncthreads();
+    int8_t* dst = codes + row0 * d;
+    for (int e = 16 * threadIdx.x; e < elements; e += 16 * kThreads) {
+        if (e + 16 <= elements) *reinterpret_cast<uint4*>(dst + e) = *reinterpret_cast<const uint4*>(cs + e);
+        else for (int i = e; i < elements; ++i) dst[i] = cs[i];
+    }
 }
 
 struct RestoreArgs { CheckpointRows t[4]; };
 
+__device__ __forceinline__ uint32_t restored_pair(uint32_t codes, int at, float scale)       // codes at, at + 1 (bytes of the word) as bf16
+{
+    const float lo = (float)(int8_t)(codes >> (8 * at)) * scale, hi = (float)(int8_t)(codes >> (8 * at + 8)) * scale;
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <int kLanes>
 __global__ void __launch_bounds__(kThreads) rib_checkpoint_restore_kernel(const RestoreArgs args, long long rows, int d)
 {
+    constexpr int kUnroll = 4, kRowsAtOnce = kThreads / kLanes;
     const CheckpointRows t = args.t[blockIdx.y];
-    const long long row = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5;
-    const int lane = threadIdx.x & 31;
-    if (row >= rows) return;
-    const float scale = t.scales[row];
-    for (int c = lane; c < d; c += 32) t.x[row * d + c] = __float2bfloat16_rn((float)t.codes[row * d + c] * scale);
+    const int part = threadIdx.x % kLanes;
+    if (8 * part >= d) return;
+    const long long row0 = (long long)blockIdx.x * (kUnroll * kRowsAtOnce) + threadIdx.x / kLanes;
+    uint2 c[kUnroll];
+    float scale[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        const long long row = row0 + k * kRowsAtOnce;
+        c[k] = row < rows ? __ldg(reinterpret_cast<const uint2*>(t.codes + row * d + 8 * part)) : make_uint2(0u, 0u);
+        scale[k] = row < rows ? __ldg(t.scales + row) : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        const long long row = row0 + k * kRowsAtOnce;
+        if (row < rows)
+            *reinterpret_cast<uint4*>(t.x + row * d + 8 * part) = make_uint4(restored_pair(c[k].x, 0, scale[k]), restored_pair(c[k].x, 2, scale[k]),
+                                                                             restored_pair(c[k].y, 0, scale[k]), restored_pair(c[k].y, 2, scale[k]));
+    }
 }
+
+__global__ void __launch_bounds__(kThreads) rib_checkpoint_restore_staged_kernel(const RestoreArgs args, long long rows, int d)
+{
+    __shared__ float scale[kStagedRows];
+    const CheckpointRows t = args.t[blockIdx.y];
+    const long long row0 = (long long)blockIdx.x * kStagedRows;
+    const int here = (int)min((long long)kStagedRows, rows - row0), elements = here * d;
+    if (threadIdx.x < here) scale[threadIdx.x] = __ldg(t.scales + row0 + threadIdx.x);
+    __syncthreads();
+    const int8_t* src = t.codes + row0 * d;
+    __nv_bfloat16* dst = t.x + row0 * d;
+    for (int e = 8 * threadIdx.x; e < elements; e += 8 * kThreads) {
+        if (e + 8 <= elements) {
+            const uint2 c = __ldg(reinterpret_cast<const uint2*>(src + e));
+            const uint32_t w[2] = {c.x, c.y};
+            __nv_bfloat162 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = __floats2bfloat162_rn((float)(int8_t)(w[i >> 1] >> (16 * (i & 1))) * scale[(e + 2 * i) / d],
+                                             (float)(int8_t)(w[i >> 1] >> (16 * (i & 1) + 8)) * scale[(e + 2 * i + 1) / d]);
+            *reinterpret_cast<uint4*>(dst + e) = *reinterpret_cast<const uint4*>(v);
+        } else {
+            for (int i = e; i < elements; ++i) dst[i] = __float2bfloat16_rn((float)src[i] * scale[i / d]);
+        }
+    }
+}
+
+// 8 channels to a thread: lanes to a row as a power of two
+int lanes_of(int d) { return d <= 8 ? 1 : d <= 16 ? 2 : d <= 32 ? 4 : 8; }
+unsigned blocks_of(long long rows, int lanes) { const long long per = 4LL * kThreads / lanes; return (unsigned)((rows + per - 1) / per); }
 
 }  // namespace
 
 cudaError_t checkpoint_store(const __nv_bfloat16* x, long long rows, int d, int8_t* codes, float* scales, cudaStream_t stream)
 {
-    const unsigned blocks = (unsigned)((rows * 32 + kThreads - 1) / kThreads);
-    { ProfileScope scope(RIB_KERNEL_CHECKPOINT_STORE, stream); rib_checkpoint_store_kernel<<<blocks, kThreads, 0, stream>>>(x, rows, d, codes, scales); }
+    ProfileScope scope(RIB_KERNEL_CHECKPOINT_STORE, stream);
+    if (d % 8) {
+        rib_checkpoint_store_staged_kernel<<<(unsigned)((rows + kStagedRows - 1) / kStagedRows), kThreads, 0, stream>>>(x, rows, d, codes, scales);
+    } else {
+        const int lanes = lanes_of(d);
+        const auto kernel = lanes == 1 ? rib_checkpoint_store_kernel<1> : lanes == 2 ? rib_checkpoint_store_kernel<2> : lanes == 4 ? rib_checkpoint_store_kernel<4> : rib_checkpoint_store_kernel<8>;
+        kernel<<<blocks_of(rows, lanes), kThreads, 0, stream>>>(x, rows, d, codes, scales);
+    }
     return cudaGetLastError();
 }
 
@@ -52,8 +196,14 @@ cudaError_t checkpoint_restore(const CheckpointRows* tensors, int count, long lo
 {
     RestoreArgs args{};
     for (int i = 0; i < count; ++i) args.t[i] = tensors[i];
-    const dim3 grid((unsigned)((rows * 32 + kThreads - 1) / kThreads), (unsigned)count);
-    { ProfileScope scope(RIB_KERNEL_CHECKPOINT_RESTORE, stream); rib_checkpoint_restore_kernel<<<grid, kThreads, 0, stream>>>(args, rows, d); }
+    ProfileScope scope(RIB_KERNEL_CHECKPOINT_RESTORE, stream);
+    if (d % 8) {
+        rib_checkpoint_restore_staged_kernel<<<dim3((unsigned)((rows + kStagedRows - 1) / kStagedRows), (unsigned)count), kThreads, 0, stream>>>(args, rows, d);
+    } else {
+        const int lanes = lanes_of(d);
+        const auto kernel = lanes == 1 ? rib_checkpoint_restore_kernel<1> : lanes == 2 ? rib_checkpoint_restore_kernel<2> : lanes == 4 ? rib_checkpoint_restore_kernel<4> : rib_checkpoint_restore_kernel<8>;
+        kernel<<<dim3(blocks_of(rows, lanes), (unsigned)count), kThreads, 0, stream>>>(args, rows, d);
+    }
     return cudaGetLastError();
 }
 

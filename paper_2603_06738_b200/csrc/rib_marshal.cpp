@@ -9,6 +9,7 @@
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include <type_traits>
@@ -187,6 +188,148 @@ PyObject* bwd(PyObject*, PyObject* const* a, Py_ssize_t count)
     });
 }
 
+// A bias by buckets and its map, for windows of side `window`, on q's device, which has to be the current one.
+struct Bias { const at::Tensor *table, *buckets; int dtype, count; long long stride; };
+bool get_bias(PyObject* table, PyObject* buckets, const Image& m, Bias* b)
+{
+    b->table = nullptr;
+    for (int dim = 1; dim <= 2 && !b->table; ++dim)
+        for (const at::ScalarType type : {at::kBFloat16, at::kFloat})
+            if (!b->table) b->table = plain(table, type, dim);
+    b->buckets = plain(buckets, at::kInt, 2);
+    if (!b->table || !b->buckets) return false;
+    const int dim = (int)b->table->dim();
+    const int64_t count = b->table->size(dim - 1), side = 2 * (int64_t)m.window - 1;
+    if (count < 1 || count > (1 << 30) || (dim == 2 && b->table->size(0) != m.heads) || b->buckets->size(0) != side || b->buckets->size(1) != side) return false;
+    b->dtype = b->table->scalar_type() == at::kBFloat16 ? RIB_DTYPE_BF16 : RIB_DTYPE_F32;
+    b->count = (int)count;
+    b->stride = dim == 2 ? count : 0;
+    return true;
+}
+bool here(std::initializer_list<const at::Tensor*> tensors)
+{
+    const int current = c10::cuda::current_device();
+    for (const at::Tensor* t : tensors) if (t->get_device() != current) return false;
+    return true;
+}
+
+// q, k, v of one shape and the window, without tables
+bool get_maps(PyObject* const* a, PyObject* window, PyObject* shift, Image* m)
+{
+    m->q = plain(a[0], at::kBFloat16, 5); m->k = plain(a[1], at::kBFloat16, 5); m->v = plain(a[2], at::kBFloat16, 5);
+    if (!m->q || !m->k || !m->v || m->k->sizes() != m->q->sizes() || m->v->sizes() != m->q->sizes()) return false;
+    if (!get_int(window, &m->window) || !get_int(shift, &m->shift) || m->window < 1 || m->window > 32768) return false;
+    const auto s = m->q->sizes();
+    for (int i = 0; i < 5; ++i) if (s[i] > (1ll << 30)) return false;
+    m->B = (int)s[0]; m->H = (int)s[1]; m->W = (int)s[2]; m->heads = (int)s[3]; m->d = (int)s[4];
+    return true;
+}
+
+// fwd_bucketed(address, q, k, v, bias, buckets, window, shift, masked, want_lse, stream)
+PyObject* fwd_bucketed(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        Image m;
+        Bias b;
+        void* stream;
+        if (count != 11 || modes_active() || !get_maps(a + 1, a[6], a[7], &m) || !get_bias(a[4], a[5], m, &b) || !PyBool_Check(a[8]) || !PyBool_Check(a[9]) ||
+            !get_stream(a[10], &stream) || !here({m.q, m.k, m.v, b.table, b.buckets})) Py_RETURN_NONE;
+        const auto fn = reinterpret_cast<decltype(&rib_window_attn_fwd_bucketed)>(address(a[0]));
+        const bool want_lse = a[9] == Py_True;
+        at::Tensor out, lse;
+        int rc;
+        {
+            const Unlocked unlocked;
+            out = at::empty_like(*m.q);
+            if (want_lse) lse = at::empty({m.B, m.heads, m.H, m.W}, m.q->options().dtype(at::kFloat));
+            rc = fn(m.q->const_data_ptr(), m.k->const_data_ptr(), m.v->const_data_ptr(), b.table->const_data_ptr(), b.dtype, b.stride, b.buckets->const_data_ptr<int>(), b.count,
+                    m.B, m.H, m.W, m.heads, m.d, m.window, m.shift, a[8] == Py_True, out.mutable_data_ptr(), lse.defined() ? lse.mutable_data_ptr<float>() : nullptr, stream);
+        }
+        if (rc) return status(rc);
+        return results({&out, &lse});
+    });
+}
+
+// bwd_bucketed(address, address of the workspace's size, q, k, v, bias, buckets, out, lse, dout, window, shift, masked, workspace or None, stream)
+PyObject* bwd_bucketed(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        Image m;
+        Bias b;
+        void* stream;
+        if (count != 15 || modes_active() || !get_maps(a + 2, a[10], a[11], &m) || !get_bias(a[5], a[6], m, &b) || !PyBool_Check(a[12]) || !get_stream(a[14], &stream)) Py_RETURN_NONE;
+        const at::Tensor *out = plain(a[7], at::kBFloat16, 5), *lse = plain(a[8], at::kFloat, 4), *dout = plain(a[9], at::kBFloat16, 5);
+        const at::Tensor* given = a[13] == Py_None ? nullptr : plain(a[13], at::kByte, 1);
+        if (!out || !lse || !dout || (a[13] != Py_None && !given) || out->sizes() != m.q->sizes() || dout->sizes() != m.q->sizes() ||
+            lse->size(0) != m.B || lse->size(1) != m.heads || lse->size(2) != m.H || lse->size(3) != m.W ||
+            !here({m.q, m.k, m.v, b.table, b.buckets, out, lse, dout}) || (given && !here({given}))) Py_RETURN_NONE;
+        const auto fn = reinterpret_cast<decltype(&rib_window_attn_bwd_bucketed)>(address(a[0]));
+        const auto need = reinterpret_cast<decltype(&rib_window_attn_bwd_bucketed_workspace)>(address(a[1]));
+        at::Tensor dq, dk, dv, dbias, ws;
+        int rc;
+        {
+            const Unlocked unlocked;
+            dq = at::empty_like(*m.q); dk = at::empty_like(*m.q); dv = at::empty_like(*m.q); dbias = at::empty_like(*b.table);
+            ws = given ? *given : at::empty({(int64_t)need(b.stride, b.count, m.B, m.H, m.W, m.heads, m.d, m.window) + 256}, m.q->options().dtype(at::kByte));
+            rc = fn(m.q->const_data_ptr(), m.k->const_data_ptr(), m.v->const_data_ptr(), b.table->const_data_ptr(), b.dtype, b.stride, b.buckets->const_data_ptr<int>(), b.count,
+                    out->const_data_ptr(), lse->const_data_ptr<float>(), dout->const_data_ptr(), m.B, m.H, m.W, m.heads, m.d, m.window, m.shift, a[12] == Py_True,
+                    dq.mutable_data_ptr(), dk.mutable_data_ptr(), dv.mutable_data_ptr(), dbias.mutable_data_ptr(), ws.mutable_data_ptr(), (size_t)ws.numel(), stream);
+        }
+        if (rc) return status(rc);
+        return results({&dq, &dk, &dv, &dbias});
+    });
+}
+
+// any number of dimensions
+const at::Tensor* plain_rows(PyObject* o, at::ScalarType type)
+{
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.defined() && !t.is_nested() && t.layout() == at::kStrided && t.dim() > 0 && t.numel() > 0 ? plain(o, type, (int)t.dim()) : nullptr;
+}
+
+// store(address, x, stream)
+PyObject* store(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        void* stream;
+        const at::Tensor* x = count == 3 && !modes_active() ? plain_rows(a[1], at::kBFloat16) : nullptr;
+        if (!x || x->size(-1) > 64 || !get_stream(a[2], &stream) || !here({x})) Py_RETURN_NONE;
+        const auto fn = reinterpret_cast<decltype(&rib_checkpoint_store)>(address(a[0]));
+        at::Tensor codes, scales;
+        int rc;
+        {
+            const Unlocked unlocked;
+            codes = at::empty(x->sizes(), x->options().dtype(at::kChar));
+            scales = at::empty(x->sizes().slice(0, x->dim() - 1), x->options().dtype(at::kFloat));
+            rc = fn(x->const_data_ptr(), scales.numel(), (int)x->size(-1), codes.mutable_data_ptr(), scales.mutable_data_ptr<float>(), stream);
+        }
+        if (rc) return status(rc);
+        return results({&codes, &scales});
+    });
+}
+
+// restore(address, codes, scales, stream)
+PyObject* restore(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        void* stream;
+        const at::Tensor* codes = count == 4 && !modes_active() ? plain_rows(a[1], at::kChar) : nullptr;
+        const at::Tensor* scales = codes && codes->dim() > 1 ? plain_rows(a[2], at::kFloat) : nullptr;
+        if (!scales || codes->size(-1) > 64 || scales->sizes() != codes->sizes().slice(0, codes->dim() - 1) || !get_stream(a[3], &stream) || !here({codes, scales})) Py_RETURN_NONE;
+        const auto fn = reinterpret_cast<decltype(&rib_checkpoint_restore)>(address(a[0]));
+        at::Tensor x;
+        int rc;
+        {
+            const Unlocked unlocked;
+            x = at::empty(codes->sizes(), codes->options().dtype(at::kBFloat16));
+            rc = fn(codes->const_data_ptr(), scales->const_data_ptr<float>(), scales->numel(), (int)codes->size(-1), x.mutable_data_ptr(), stream);
+        }
+        if (rc) return status(rc);
+        return results({&x});
+    });
+}
+
 struct Generator { const at::Tensor *w_h, *b_h, *w_pq, *w_pk; int window, L, dh, r; void* stream; };
 
 bool get_generator(PyObject* const* w, PyObject* window, PyObject* stream, Generator* g)
@@ -247,6 +390,10 @@ PyObject* generate_bwd(PyObject*, PyObject* const* a, Py_ssize_t count)
 PyMethodDef methods[] = {
     {"fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(fwd)), METH_FASTCALL, nullptr},
     {"bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bwd)), METH_FASTCALL, nullptr},
+    {"fwd_bucketed", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(fwd_bucketed)), METH_FASTCALL, nullptr},
+    {"bwd_bucketed", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bwd_bucketed)), METH_FASTCALL, nullptr},
+    {"store", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(store)), METH_FASTCALL, nullptr},
+    {"restore", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(restore)), METH_FASTCALL, nullptr},
     {"generate", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(generate)), METH_FASTCALL, nullptr},
     {"generate_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(generate_bwd)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
