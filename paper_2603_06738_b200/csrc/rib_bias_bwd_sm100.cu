@@ -553,13 +553,42 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (!key_exists || 2 * I + h >= c.patches) continue;
                 int qy, qx, QY0, QX0;
                 patch_origin(p, c, 2 * I + h, qy, qx, QY0, QX0);
-                double* const to = p.offsets + (size_t)c.h * side * side + (size_t)(ky - qy + p.M - 1) * side + (kx - qx + p.M - 1) + (lane >> 2) - 2 * (lane & 3);
-                acc[0][0] += acc[0][2]; acc[0][1] += acc[0][3];
+                // Diagonals of the 15 sums: a lane has column x = lane / 4 of the keys and columns 2 c, 2 c + 1 (c = lane % 4) of the queries, i.e. x - 2 c and
+                // x - 2 c - 1 of each.  A column and the one before it have a lane's second values at the other's first ones: one exchange leaves
+                // every lane with the offset x - 2 c alone, or, for the one value that has no partner, 8 below it.  So lane (x, c) stands for the
+                // offsets r = (x - 2 c) mod 8 and r - 8, four lanes for each, which then share the 16 rows among them.
+                const int x = lane >> 2, c4 = lane & 3;
+                const bool odd = x & 1, above = x >= 2 * c4, orphan = odd && c4 == 0;
+                const int partner = odd ? lane - 4 - c4 + ((c4 + 3) & 3) : lane + 4;
+                float hi[16], lo[16];
+                hi[15] = lo[15] = 0.f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int j = 0; j < 15; ++j) {
+                    const int k = j < 7 ? 7 - j : j - 7, e = j < 7 ? 2 : 0;
+                    const float v0 = k ? acc[k][e] : acc[0][0] + acc[0][2], v1 = k ? acc[k][e + 1] : acc[0][1] + acc[0][3];
+                    const float r = __shfl_sync(0xffffffffu, v1, partner), both = v0 + (orphan ? 0.f : r);
+                    hi[j] = above ? both : 0.f;
+                    lo[j] = above ? (orphan ? r : 0.f) : both;
+                }
+                auto share = [&](bool second, int with, int n) {          // rows 0 .. n - 1 and n .. 2 n - 1: one half is kept, the other's sums go to the partner
 #pragma unroll
-                    for (int e = 0; e < (k ? 4 : 2); ++e)
-                        if (acc[k][e] != 0.f) atomicAdd(to + (e < 2 ? k : -k) * side - (e & 1), (double)acc[k][e]);
+                    for (int j = 0; j < 8; ++j)
+                        if (j < n) {
+                            const float keep_hi = second ? hi[j + n] : hi[j], send_hi = second ? hi[j] : hi[j + n];
+                            const float keep_lo = second ? lo[j + n] : lo[j], send_lo = second ? lo[j] : lo[j + n];
+                            hi[j] = keep_hi + __shfl_sync(0xffffffffu, send_hi, with);
+                            lo[j] = keep_lo + __shfl_sync(0xffffffffu, send_lo, with);
+                        }
+                };
+                share(c4 & 2, lane ^ 18, 8);
+                share(c4 & 1, (((x + (c4 & 1 ? -2 : 2)) & 7) << 2) | (c4 ^ 1), 4);
+                const int r = (x - 2 * c4) & 7;
+                double* const to = p.offsets + (size_t)c.h * side * side + (size_t)(ky - qy + p.M - 1 + 8 * (c4 >> 1) + 4 * (c4 & 1) - 7) * side + (kx - qx + p.M - 1) + r;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (hi[j] != 0.f) atomicAdd(to + j * side, (double)hi[j]);
+                    if (lo[j] != 0.f) atomicAdd(to + j * side - 8, (double)lo[j]);
+                }
             }
         }
     }
