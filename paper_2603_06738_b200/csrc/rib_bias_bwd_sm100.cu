@@ -16,8 +16,8 @@
 //
 // Gradient of the bias: the sum of dS over all pairs of tokens at the same offset.  Four warps of their own take the dS tile that dQ reads from
 // shared memory (bf16, as dQ and dK see it), one patch of keys against one of queries each: 64 blocks of 8 x 8 (key row, query row).
-// The blocks with the same difference of rows are summed in fp32 by warp-level MMAs against stacked identities (four blocks at a time, two to
-// each of two differences), which leaves 15 blocks; those are then summed along their diagonals and added to the sums by offset.
+// Warp-level MMAs against constant 0/1 matrices sum the 4096 of them along both diagonals in fp32, which leaves the 15 x 15 offsets of the two
+// patches, and those are added to the sums by offset in 64 bits.
 #include "rib_bias_sm100.cuh"
 
 namespace rib {
@@ -46,7 +46,8 @@ constexpr uint32_t kOffBar = kOffDK + kContentBytes;
 enum Bar { kKVFull = 0, kKVEmpty = 2, kQFull = 4, kQEmpty = kQFull + kQStages, kSFull = kQEmpty + kQStages, kPReady = kSFull + 4, kPFree = kPReady + 4,
            kDSFree = kPFree + 4, kDQFull = kDSFree + 2, kDQFree, kAccFull, kAccFree, kTabDone, kTabReady, kDrain, kNumBars = kDrain + 3 };
 constexpr uint32_t kOffMisc = kOffBar + kNumBars * 8;
-constexpr uint32_t kOffTable = (kOffMisc + 16 + 15) & ~15u;      // [(2M-1)^2] fp32
+constexpr uint32_t kOffLists = (kOffMisc + 16 + 15) & ~15u;      // PatchLists
+constexpr uint32_t kOffTable = kOffLists + sizeof(PatchLists);   // [(2M-1)^2] fp32
 constexpr uint32_t smem_bytes(int M) { return kOffTable + 4u * (2 * M - 1) * (2 * M - 1) + 1024; }
 static_assert(smem_bytes(kBiasMaxWindow) <= 232448, "shared memory of one CTA");
 static_assert(kOffRing % 1024 == 0 && kRingBytes % 1024 == 0 && kOffDS % 1024 == 0, "swizzle atoms need aligned tiles");
@@ -97,6 +98,13 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ float4 lds_f32x4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
+}
+
 template <bool B> struct Flag { static constexpr bool value = B; };
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -140,6 +148,8 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         tmem_alloc(base + kOffMisc, kTmemCols);
         tmem_relinquish();
     }
+    PatchLists* const lists = reinterpret_cast<PatchLists*>(base_ptr + kOffLists);
+    fill_patch_lists(p.g, p.M, lists, threadIdx.x, kThreads);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -316,15 +326,15 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             // keys of the patch beyond the map's edge get probability 0: a thread's whole column, or the rows from `rows_there` on
             const bool column_there = X0 + xk < p.W;
             const int rows_there = p.H - Y0 - key_row0;          // of the thread's four
-            const uint32_t k_addr = table_addr + (ky + key_row0 + p.M - 1) * pitch + 4 * (kx + xk + p.M - 1 - 2 * (lane & 3));
+            const bool cut_any = rows_there < 4 || X0 + 8 > p.W;
+            const uint32_t k_addr = table_addr + (ky + key_row0 - 4 * cg + p.M - 1) * pitch + 4 * (kx + xk + p.M - 1 - 2 * (lane & 3));
+            const uint16_t* const entries = lists->entry + list_of(c) + h;
             const int tiles = (c.patches + 1) >> 1;
             for (int I = 0; I < tiles; ++I, ++g) {
                 const uint32_t st = g % kQStages;
                 const uint32_t t_s = tmem + lane_base + 32 * cg + kStep * buf, t_dp = t_s + kColDP;
                 buf = buffer_after(buf, 2);
-                int qy, qx, QY0, QX0;
-                patch_origin(p, c, 2 * I + h, qy, qx, QY0, QX0);
-                const uint32_t b_addr = k_addr - (qy + 4 * cg) * pitch - 4 * qx;
+                const uint32_t b_addr = k_addr - entries[2 * I];
                 // warp-uniform outcome: the TMEM accesses below are warp-collective
                 if (!mbar_wait_warp(on_unit(kSFull, 2 * g + h), unit_parity(2 * g), abort_flag, p.status) ||
                     !mbar_wait_warp(bar(kQFull + st), (g / kQStages) & 1, abort_flag, p.status)) { ok = false; break; }
@@ -332,7 +342,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 // four pieces of 16 keys x 16 queries (piece c: lanes 16 (c % 2) .., queries 16 (c / 2) ..), read as 16-lane fragments: a thread holds 2 key
                 // rows of 2 x 2 queries of a piece
                 const uint32_t ld = base + kOffRing + st * kRingBytes + kRingLD + (32 * h + 16 * cg + (lane & 3)) * 16;
-                auto ldq = [&](int gq) { return make_float4(lds_f32(ld + 64 * gq), lds_f32(ld + 64 * gq + 4), lds_f32(ld + 64 * gq + 8), lds_f32(ld + 64 * gq + 12)); };
+                auto ldq = [&](int gq) { return lds_f32x4(ld + 64 * gq); };
                 const uint32_t ds_line = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + (quarter * 32 + 8 * ((lane >> 3) & 1) + (lane & 7)) * 128;
                 auto load = [&](int c4, uint32_t (&s)[8], uint32_t (&dp)[8]) {
                     const uint32_t at = ((uint32_t)(16 * (c4 & 1)) << 16) + 16 * (c4 >> 1);
@@ -340,10 +350,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     tmem_ld_16x256b_x2(t_dp + at, dp);
                 };
                 // biases of key row a against query row b of the warp's rows, a - b = k (the queries' columns go up, so the offsets go down)
-                auto bias = [&](int k) {
-                    const float2 b = make_float2(lds_f32(b_addr + k * (int)pitch), lds_f32(b_addr + k * (int)pitch - 4));
-                    return column_there ? b : make_float2(-INFINITY, -INFINITY);
-                };
+                auto bias = [&](int k) { return make_float2(lds_f32(b_addr + k * (int)pitch), lds_f32(b_addr + k * (int)pitch - 4)); };
                 // bb[i]: a - b = k0 + i - 1 with k0 that of equal fragment rows (gq == rr)
                 auto work4 = [&](auto cut, int c4, const uint32_t (&s)[8], const uint32_t (&dp)[8], const float4 (&t)[2], const float2 (&bb)[3], uint32_t (&pp)[4], uint32_t (&dd)[4]) {
 #pragma unroll
@@ -354,7 +361,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                             const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2,
                                                         __fadd2_rn(make_float2(t[gq].x, t[gq].y), bb[1 + rr - gq]));
                             float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                            if (cut.value && 2 * (c4 & 1) + rr >= rows_there) e = make_float2(0.f, 0.f);
+                            if (cut.value && (!column_there || 2 * (c4 & 1) + rr >= rows_there)) e = make_float2(0.f, 0.f);
                             const float2 d = __fmul2_rn(e, __fadd2_rn(make_float2(__uint_as_float(dp[i]), __uint_as_float(dp[i + 1])), make_float2(t[gq].z, t[gq].w)));
                             pp[2 * gq + rr] = pack_bf16x2(e.x, e.y);
                             dd[2 * gq + rr] = pack_bf16x2(d.x, d.y);
@@ -408,7 +415,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         store(2, pp, dd);
                         return true;
                     };
-                    if (!(rows_there < 4 ? unit(Flag<true>{}) : unit(Flag<false>{}))) { ok = false; break; }
+                    if (!(cut_any ? unit(Flag<true>{}) : unit(Flag<false>{}))) { ok = false; break; }
                 }
                 tmem_wait_st();
                 tc_fence_before();
@@ -470,10 +477,8 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (I == tiles - 1) ok = drain_item(c, nitem);
                 if (!ok || !mbar_wait_warp(bar(kDQFull), g & 1, abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
-                const int sp = 2 * I + (quarter >> 1);
-                int py, px, Y0, X0;
-                patch_origin(p, c, sp, py, px, Y0, X0);
-                float* dst = acc + 4 * (64 * (size_t)((py >> 3) * (p.M >> 3) + (px >> 3)) + (row & 63));
+                const int sp = 2 * I + (quarter >> 1), at = lists->origin[list_of(c) + sp];
+                float* dst = acc + 4 * (64 * (size_t)((at >> 11) * (p.M >> 3) + ((at & 255) >> 3)) + (row & 63));
 #pragma unroll
                 for (int part = 0; part < kD / 16; ++part) {
                     uint32_t a[16];
@@ -508,86 +513,65 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         __syncwarp();
     } else {
         // ================================ gradient of the bias: warp 24 + 2 h + sub sums dS of key patch `sub` of the item and the queries of half h
+        // One MMA of 16 x 8 x 16 takes, of one row of the keys' patch (a) and the 8 rows of the queries', two key columns x: its A has the difference of
+        // rows t = (a - query row) mod 8 as its rows - the lines of an ldmatrix may come from anywhere - and (x, query column) as its columns; where
+        // a - query row is t the row goes to the upper half of A, where it is t - 8 to the lower.  B names for every (x, query column) the
+        // difference of columns.  So the 64 MMAs of 8 key rows x 4 pairs of columns x 2 halves of the 15 differences leave the sums of dS at
+        // the 15 x 15 offsets of the two patches in 8 registers of the warp, and the loop is short: a first version with one product per block
+        // and the diagonals by shuffles was a kilobyte of instructions too long for the instruction cache (1160 us; without any of it 798).
         const int h = (warp >> 1) & 1, sub = warp & 1;
-        // stacked identities: column lane / 4 of rows 2 (lane % 4), + 1
-        const uint32_t eye = (2 * (lane & 3) == (lane >> 2) ? 0x3F80u : 0u) | (2 * (lane & 3) + 1 == (lane >> 2) ? 0x3F800000u : 0u);
-        const int m = lane >> 3, xrow = lane & 7;             // this lane names row `xrow` of matrix m of an ldmatrix
+        const int t = lane & 7, m = lane >> 3;                // of an ldmatrix this lane names line t of matrix m: key column m (and m + 4 of the second one)
+        const int arow = lane >> 2, c2 = 2 * (lane & 3);
+        // B of the pair of columns x, x + 1 and the differences 8 n - 8 .. 8 n - 1 of x - query column: rows (x, 0..7), (x + 1, 0..7); this lane has column
+        // lane / 4 (difference 8 n - 8 + lane / 4) of the rows c2, c2 + 1
+        uint32_t eye[4][2][2];
+#pragma unroll
+        for (int pr = 0; pr < 4; ++pr)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    const int d = 8 * n - 8 + arow, x = 2 * pr + o;
+                    eye[pr][n][o] = (x - c2 == d ? 0x3F80u : 0u) | (x - c2 - 1 == d ? 0x3F800000u : 0u);
+                }
         uint32_t g = 0;
         bool ok = true;
         for (int item = first_item; item < last_item && ok; ++item) {
             const LiveItem c = decode_bias_item(p.g, item);
             const int tiles = (c.patches + 1) >> 1;
-            int ky, kx, Y0, X0;
-            patch_origin(p, c, 2 * c.tp + sub, ky, kx, Y0, X0);
+            const int key_at = lists->origin[list_of(c) + 2 * c.tp + sub];
             const bool key_exists = 2 * c.tp + sub < c.patches;
             for (int I = 0; I < tiles; ++I, ++g) {
                 if (!mbar_wait_warp(on_unit(kPReady, 2 * g + h), unit_parity(2 * g), abort_flag, p.status)) { ok = false; break; }
-                const uint32_t tile = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + sub * 64 * 128 + xrow * 128;
-                // block (key row a, query row b): 8 lines of 128 bytes from line 8 a, chunk b of each, swizzled by the line
-                auto block = [&](int a, int b) { return tile + a * 1024 + ((b ^ xrow) << 4); };
-                float acc[8][4];                              // [k]: differences a - b = k (rows 0-7 of the product) and -k (rows 8-15); [0]: both 0
+                // dS of key (a, x): line 8 a + x of the patch, 128 bytes; the 8 queries of row b: chunk b, swizzled by the line
+                const uint32_t line = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + sub * 64 * 128 + m * 128;
+                float lo[4] = {0.f, 0.f, 0.f, 0.f}, hi[4] = {0.f, 0.f, 0.f, 0.f};      // differences of columns -8 .. -1 and 0 .. 7; [0], [1]: rows t, [2], [3]: rows t - 8
+#pragma unroll 1
+                for (int a = 0; a < 8; ++a) {
+                    const uint32_t addr = line + a * 1024 + ((((a - t) & 7) ^ m) << 4);
+                    uint32_t r[2][4];
+                    ldmatrix_x4(addr, r[0]);                               // key columns 0 .. 3
+                    ldmatrix_x4((addr ^ 64u) + 512u, r[1]);                // 4 .. 7
+                    const bool upper = a >= arow;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[k][e] = 0.f;
-#pragma unroll
-                for (int k = 1; k < 8; ++k)
-#pragma unroll
-                    for (int i = 0; i < 8 - k; i += 2) {
-                        // matrices 0, 2: blocks (k + i, i) and the next one along the diagonal; 1, 3: (i, k + i) and its next one
-                        const int lo = i + (m >> 1);
-                        const int top = min(k + lo, 7);       // (the diagonal's odd end: the block read twice counts once)
-                        uint32_t a[4];
-                        ldmatrix_x4(m & 1 ? block(lo, top) : block(top, lo), a);
-                        const bool both = i + 1 < 8 - k;
-                        mma_16816(acc[k], a[0], a[1], both ? a[2] : 0u, both ? a[3] : 0u, eye, eye);
+                    for (int pr = 0; pr < 4; ++pr) {
+                        const uint32_t u = r[pr >> 1][2 * (pr & 1)], v = r[pr >> 1][2 * (pr & 1) + 1];
+                        const uint32_t a0 = upper ? u : 0u, a1 = upper ? 0u : u, a2 = upper ? v : 0u, a3 = upper ? 0u : v;
+                        mma_16816(lo, a0, a1, a2, a3, eye[pr][0][0], eye[pr][0][1]);
+                        mma_16816(hi, a0, a1, a2, a3, eye[pr][1][0], eye[pr][1][1]);
                     }
-#pragma unroll
-                for (int i = 0; i < 8; i += 4) {
-                    uint32_t a[4];
-                    ldmatrix_x4(block(i + m, i + m), a);
-                    mma_16816(acc[0], a[0], a[1], a[2], a[3], eye, eye);
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(kDSFree + (g & 1)));
                 if (!key_exists || 2 * I + h >= c.patches) continue;
-                int qy, qx, QY0, QX0;
-                patch_origin(p, c, 2 * I + h, qy, qx, QY0, QX0);
-                // Diagonals of the 15 sums: a lane has column x = lane / 4 of the keys and columns 2 c, 2 c + 1 (c = lane % 4) of the queries, i.e. x - 2 c and
-                // x - 2 c - 1 of each.  A column and the one before it have a lane's second values at the other's first ones: one exchange leaves
-                // every lane with the offset x - 2 c alone, or, for the one value that has no partner, 8 below it.  So lane (x, c) stands for the
-                // offsets r = (x - 2 c) mod 8 and r - 8, four lanes for each, which then share the 16 rows among them.
-                const int x = lane >> 2, c4 = lane & 3;
-                const bool odd = x & 1, above = x >= 2 * c4, orphan = odd && c4 == 0;
-                const int partner = odd ? lane - 4 - c4 + ((c4 + 3) & 3) : lane + 4;
-                float hi[16], lo[16];
-                hi[15] = lo[15] = 0.f;
+                const int query_at = lists->origin[list_of(c) + 2 * I + h];
+                const int dy = (key_at >> 8) - (query_at >> 8) + p.M - 1 + arow, dx = (key_at & 255) - (query_at & 255) + p.M - 1 + c2;
+                double* const to = p.offsets + ((size_t)c.h * side + dy) * side + dx;
 #pragma unroll
-                for (int j = 0; j < 15; ++j) {
-                    const int k = j < 7 ? 7 - j : j - 7, e = j < 7 ? 2 : 0;
-                    const float v0 = k ? acc[k][e] : acc[0][0] + acc[0][2], v1 = k ? acc[k][e + 1] : acc[0][1] + acc[0][3];
-                    const float r = __shfl_sync(0xffffffffu, v1, partner), both = v0 + (orphan ? 0.f : r);
-                    hi[j] = above ? both : 0.f;
-                    lo[j] = above ? (orphan ? r : 0.f) : both;
-                }
-                auto share = [&](bool second, int with, int n) {          // rows 0 .. n - 1 and n .. 2 n - 1: one half is kept, the other's sums go to the partner
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j < n) {
-                            const float keep_hi = second ? hi[j + n] : hi[j], send_hi = second ? hi[j] : hi[j + n];
-                            const float keep_lo = second ? lo[j + n] : lo[j], send_lo = second ? lo[j] : lo[j + n];
-                            hi[j] = keep_hi + __shfl_sync(0xffffffffu, send_hi, with);
-                            lo[j] = keep_lo + __shfl_sync(0xffffffffu, send_lo, with);
-                        }
-                };
-                share(c4 & 2, lane ^ 18, 8);
-                share(c4 & 1, (((x + (c4 & 1 ? -2 : 2)) & 7) << 2) | (c4 ^ 1), 4);
-                const int r = (x - 2 * c4) & 7;
-                double* const to = p.offsets + (size_t)c.h * side * side + (size_t)(ky - qy + p.M - 1 + 8 * (c4 >> 1) + 4 * (c4 & 1) - 7) * side + (kx - qx + p.M - 1) + r;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (hi[j] != 0.f) atomicAdd(to + j * side, (double)hi[j]);
-                    if (lo[j] != 0.f) atomicAdd(to + j * side - 8, (double)lo[j]);
+                for (int e = 0; e < 4; ++e) {
+                    double* const at = to + (e & 1) - (e & 2 ? 8 * side : 0);
+                    if (lo[e] != 0.f) atomicAdd(at - 8, (double)lo[e]);
+                    if (hi[e] != 0.f) atomicAdd(at, (double)hi[e]);
                 }
             }
         }

@@ -31,6 +31,31 @@ __device__ __forceinline__ LiveItem decode_bias_item(const BiasItems& g, int ite
     return c;
 }
 
+// The patches of every kind of window, in the order of its list, in shared memory: where they begin in the window (y << 8 | x), and how far into a
+// table by offset they move an entry (4 (y (2M-1) + x) bytes).  Behind the last patch of a list the last one stands in.
+struct PatchLists {
+    static constexpr int kPatches = (kBiasMaxWindow / 8) * (kBiasMaxWindow / 8);
+    uint16_t origin[9 * kPatches], entry[9 * kPatches];
+};
+static_assert(4 * (kBiasMaxWindow - 8) * 2 * kBiasMaxWindow < 65536, "an entry's bytes in 16 bits");
+__device__ __forceinline__ void fill_patch_lists(const BiasItems& g, int M, PatchLists* lists, int thread, int threads)
+{
+    for (int e = thread; e < 9 * PatchLists::kPatches; e += threads) {
+        const int kind = e / PatchLists::kPatches, k = e % PatchLists::kPatches;
+        const AxisKind &ay = g.live.y[kind / 3], &ax = g.live.x[kind % 3];
+        int py = 0, px = 0;
+        if (ay.count * ax.count > 0) {
+            int r, l;
+            ax.by_count.divmod(min(k, ay.count * ax.count - 1), r, l);
+            py = (r < ay.len0 ? ay.start0 + r : ay.start1 + r - ay.len0) << 3;
+            px = (l < ax.len0 ? ax.start0 + l : ax.start1 + l - ax.len0) << 3;
+        }
+        lists->origin[e] = (uint16_t)(py << 8 | px);
+        lists->entry[e] = (uint16_t)(4 * (py * (2 * M - 1) + px));
+    }
+}
+__device__ __forceinline__ int list_of(const LiveItem& c) { return (3 * c.ky + c.kx) * PatchLists::kPatches; }
+
 // The first item whose work begins at or behind `at`, all heads' items laid one behind the other.  CTA c of n takes the items that begin in
 // [c / n, (c + 1) / n) of the work: equal shares to within one item, and neighbours in the order, i.e. mostly one head.
 __device__ __forceinline__ int first_bias_item(const BiasItems& g, long long at)
