@@ -536,11 +536,12 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
         } else {
             e = rib::bias_grad_clear(g, st);
             if (e == cudaSuccess) e = rib::generic_bwd(p, st, g.offsets);
-            if (e == cudaSuccess) e = rib::bias_grad_finish(p, g, st);
+            if (e == cudaSuccess) e = rib::bias_grad_scatter(p, g, st);
+            if (e == cudaSuccess) e = rib::bias_grad_convert(p, g, st);
         }
         if (e != cudaSuccess) return RIB_ERR_CUDA;
         t_last_path = fast ? RIB_PATH_SM100 : RIB_PATH_GENERIC;
-        g_kernel_launches += 4;
+        g_kernel_launches += fast ? 4 : 5;
         return RIB_OK;
     }
     const bool allowed = g_forced_path.load() != RIB_PATH_GENERIC;

@@ -17,7 +17,7 @@
 // Gradient of the bias: the sum of dS over all pairs of tokens at the same offset.  Four warps of their own take the dS tile that dQ reads from
 // shared memory (bf16, as dQ and dK see it), one patch of keys against one of queries each: 64 blocks of 8 x 8 (key row, query row).
 // Warp-level MMAs against constant 0/1 matrices sum the 4096 of them along both diagonals in fp32, which leaves the 15 x 15 offsets of the two
-// patches, and those are added to the sums by offset in 64 bits.
+// patches, and those are added to the sums of the patches' difference (BiasGrad) eight bytes at a time.
 #include "rib_bias_sm100.cuh"
 
 namespace rib {
@@ -46,7 +46,8 @@ constexpr uint32_t kOffBar = kOffDK + kContentBytes;
 enum Bar { kKVFull = 0, kKVEmpty = 2, kQFull = 4, kQEmpty = kQFull + kQStages, kSFull = kQEmpty + kQStages, kPReady = kSFull + 4, kPFree = kPReady + 4,
            kDSFree = kPFree + 4, kDQFull = kDSFree + 2, kDQFree, kAccFull, kAccFree, kTabDone, kTabReady, kDrain, kNumBars = kDrain + 3 };
 constexpr uint32_t kOffMisc = kOffBar + kNumBars * 8;
-constexpr uint32_t kOffLists = (kOffMisc + 16 + 15) & ~15u;      // PatchLists
+constexpr uint32_t kOffZero = (kOffMisc + 16 + 127) & ~127u;     // zeros: four groups of lines 256 bytes apart, read in place of rows that do not count
+constexpr uint32_t kOffLists = kOffZero + 1024;                  // PatchLists
 constexpr uint32_t kOffTable = kOffLists + sizeof(PatchLists);   // [(2M-1)^2] fp32
 constexpr uint32_t smem_bytes(int M) { return kOffTable + 4u * (2 * M - 1) * (2 * M - 1) + 1024; }
 static_assert(smem_bytes(kBiasMaxWindow) <= 232448, "shared memory of one CTA");
@@ -66,7 +67,7 @@ constexpr uint32_t kIdescQ = idesc_bf16_f32_ab(kTile, kD, true, true);        //
 struct Params {
     const float2* ld;          // [pairs][n / 2], patches of the window in rows: per query pair (-lse2, -lse2', -D, -D') as two float2; then one patch of no queries
     float* dq_acc;             // [pairs][32 / 4][n][4] fp32, zeroed by the preparation kernel
-    double* offsets;           // [heads][(2M-1)^2] sums of dS
+    float* blocks;             // BiasGrad::blocks
     int* status;
     long long no_queries;      // element of ld where the patch of no queries begins
     int H, W, heads, M, s, n, nWy, nWx, Hp, Wp;
@@ -103,6 +104,11 @@ __device__ __forceinline__ float4 lds_f32x4(uint32_t addr)
     float4 v;
     asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
     return v;
+}
+
+__device__ __forceinline__ void red_add_f32x2(float* addr, float a, float b)
+{
+    asm volatile("red.relaxed.gpu.global.add.v2.f32 [%0], {%1, %2};" ::"l"(addr), "f"(a), "f"(b) : "memory");
 }
 
 template <bool B> struct Flag { static constexpr bool value = B; };
@@ -150,6 +156,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
     PatchLists* const lists = reinterpret_cast<PatchLists*>(base_ptr + kOffLists);
     fill_patch_lists(p.g, p.M, lists, threadIdx.x, kThreads);
+    if (threadIdx.x < 64) reinterpret_cast<uint4*>(base_ptr + kOffZero)[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -219,7 +226,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 for (int t = 0; t < tiles && ok; ++t, ++g) {
                     const uint32_t st = g % kQStages;
                     if (!wait_all(bar(kQFull + st), (g / kQStages) & 1)) { ok = false; break; }
-#pragma unroll
+#pragma unroll 1                     // (the kernel's loops together just fit the instruction cache)
                     for (uint32_t h = 0; h < 2; ++h) {
                         const uint32_t u = 2 * g + h;
                         if (!wait_all(on_unit(kPFree, u - kBuffers), unit_parity(u - kBuffers))) { ok = false; break; }
@@ -242,7 +249,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 // ---- dV_J += P^T dO_u and dK_J += dS^T Q_u (A from tensor memory, 16 queries per step)
                 for (int t = 0; t < tiles && ok; ++t, ++g) {
                     const uint32_t st = g % kQStages;
-#pragma unroll
+#pragma unroll 1                     // (the kernel's loops together just fit the instruction cache)
                     for (uint32_t h = 0; h < 2; ++h) {
                         const uint32_t u = 2 * g + h;
                         const bool first = t == 0 && h == 0, last = t == tiles - 1 && h == 1;
@@ -520,7 +527,8 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         // the 15 x 15 offsets of the two patches in 8 registers of the warp, and the loop is short: a first version with one product per block
         // and the diagonals by shuffles was a kilobyte of instructions too long for the instruction cache (1160 us; without any of it 798).
         const int h = (warp >> 1) & 1, sub = warp & 1;
-        const int t = lane & 7, m = lane >> 3;                // of an ldmatrix this lane names line t of matrix m: key column m (and m + 4 of the second one)
+        // Of an ldmatrix this lane names line t of matrix m: A's quarter of the upper (m even) or lower rows and of the first or second key column x.
+        const int t = lane & 7, lower = (lane >> 3) & 1, second = lane >> 4;
         const int arow = lane >> 2, c2 = 2 * (lane & 3);
         // B of the pair of columns x, x + 1 and the differences 8 n - 8 .. 8 n - 1 of x - query column: rows (x, 0..7), (x + 1, 0..7); this lane has column
         // lane / 4 (difference 8 n - 8 + lane / 4) of the rows c2, c2 + 1
@@ -534,44 +542,42 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const int d = 8 * n - 8 + arow, x = 2 * pr + o;
                     eye[pr][n][o] = (x - c2 == d ? 0x3F80u : 0u) | (x - c2 - 1 == d ? 0x3F800000u : 0u);
                 }
+        const int across = 2 * (p.M >> 3) - 1;
         uint32_t g = 0;
         bool ok = true;
         for (int item = first_item; item < last_item && ok; ++item) {
             const LiveItem c = decode_bias_item(p.g, item);
             const int tiles = (c.patches + 1) >> 1;
-            const int key_at = lists->origin[list_of(c) + 2 * c.tp + sub];
+            const uint16_t* const list = lists->origin + list_of(c);
+            const int key_at = list[2 * c.tp + sub] + (0x100 + 1) * (p.M - 8);
             const bool key_exists = 2 * c.tp + sub < c.patches;
+            float* const blocks = p.blocks + (size_t)c.h * across * across * 256 + arow * 16 + c2;
             for (int I = 0; I < tiles; ++I, ++g) {
                 if (!mbar_wait_warp(on_unit(kPReady, 2 * g + h), unit_parity(2 * g), abort_flag, p.status)) { ok = false; break; }
                 // dS of key (a, x): line 8 a + x of the patch, 128 bytes; the 8 queries of row b: chunk b, swizzled by the line
-                const uint32_t line = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + sub * 64 * 128 + m * 128;
-                float lo[4] = {0.f, 0.f, 0.f, 0.f}, hi[4] = {0.f, 0.f, 0.f, 0.f};      // differences of columns -8 .. -1 and 0 .. 7; [0], [1]: rows t, [2], [3]: rows t - 8
-#pragma unroll 1
-                for (int a = 0; a < 8; ++a) {
-                    const uint32_t addr = line + a * 1024 + ((((a - t) & 7) ^ m) << 4);
-                    uint32_t r[2][4];
-                    ldmatrix_x4(addr, r[0]);                               // key columns 0 .. 3
-                    ldmatrix_x4((addr ^ 64u) + 512u, r[1]);                // 4 .. 7
-                    const bool upper = a >= arow;
+                uint32_t line = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + sub * 64 * 128 + second * 128;
+                const uint32_t zero = base + kOffZero + second * 128 + (t << 4);
+                float sum[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};      // differences of columns -8 .. -1 and 0 .. 7; [0], [1]: rows t, [2], [3]: rows t - 8
+#pragma unroll 2
+                for (int a = 0; a < 8; ++a, line += 1024) {
+                    const uint32_t addr = (a < t) == (lower != 0) ? line + ((((a - t) & 7) ^ second) << 4) : zero;
+                    uint32_t r[4][4];
 #pragma unroll
-                    for (int pr = 0; pr < 4; ++pr) {
-                        const uint32_t u = r[pr >> 1][2 * (pr & 1)], v = r[pr >> 1][2 * (pr & 1) + 1];
-                        const uint32_t a0 = upper ? u : 0u, a1 = upper ? 0u : u, a2 = upper ? v : 0u, a3 = upper ? 0u : v;
-                        mma_16816(lo, a0, a1, a2, a3, eye[pr][0][0], eye[pr][0][1]);
-                        mma_16816(hi, a0, a1, a2, a3, eye[pr][1][0], eye[pr][1][1]);
-                    }
+                    for (int pr = 0; pr < 4; ++pr) ldmatrix_x4((addr ^ (pr << 5)) + 256 * pr, r[pr]);
+#pragma unroll
+                    for (int pr = 0; pr < 4; ++pr)
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) mma_16816(sum[n], r[pr][0], r[pr][1], r[pr][2], r[pr][3], eye[pr][n][0], eye[pr][n][1]);
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(kDSFree + (g & 1)));
                 if (!key_exists || 2 * I + h >= c.patches) continue;
-                const int query_at = lists->origin[list_of(c) + 2 * I + h];
-                const int dy = (key_at >> 8) - (query_at >> 8) + p.M - 1 + arow, dx = (key_at & 255) - (query_at & 255) + p.M - 1 + c2;
-                double* const to = p.offsets + ((size_t)c.h * side + dy) * side + dx;
+                const int at = key_at - list[2 * I + h];              // (rows << 8) + columns, both 8 (patches' difference + M / 8 - 1) >= 0
+                float* const to = blocks + ((at >> 11) * across + ((at & 255) >> 3)) * 256;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    double* const at = to + (e & 1) - (e & 2 ? 8 * side : 0);
-                    if (lo[e] != 0.f) atomicAdd(at - 8, (double)lo[e]);
-                    if (hi[e] != 0.f) atomicAdd(at, (double)hi[e]);
+                for (int n = 0; n < 2; ++n) {
+                    red_add_f32x2(to + 128 + 8 * n, sum[n][0], sum[n][1]);
+                    red_add_f32x2(to + 8 * n, sum[n][2], sum[n][3]);
                 }
             }
         }
@@ -656,8 +662,10 @@ __global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxPara
 }
 
 // dq = bf16(accumulator / sqrt(d)): a thread per token and half row (16 columns: four 16-byte reads, 512 bytes per warp and read).
-__global__ void __launch_bounds__(256) rib_bias_bwd_finish_kernel(const AuxParams p)
+// Blocks from dq_blocks on add up the gradient of the bias.
+__global__ void __launch_bounds__(256) rib_bias_bwd_finish_kernel(const AuxParams p, const BiasScatter scatter, unsigned dq_blocks)
 {
+    if (blockIdx.x >= dq_blocks) { bias_scatter(scatter, (size_t)(blockIdx.x - dq_blocks) * blockDim.x + threadIdx.x); return; }
     const size_t total = (size_t)p.pairs * p.n;
     const size_t thread = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
     // 32 tokens x 2 halves per two warps
@@ -718,7 +726,7 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     const size_t tokens = (size_t)p.pairs * p.n;
     { ProfileScope scope(RIB_KERNEL_BIAS_BWD_PREPARE, stream); rib_bias_bwd_prepare_kernel<<<(unsigned)((tokens + 63) / 64), 256, 0, stream>>>(ap); }
     if (cudaError_t e = cudaGetLastError()) return e;
-    bp.ld = ld; bp.dq_acc = dq_acc; bp.offsets = grad.offsets; bp.status = p.status;
+    bp.ld = ld; bp.dq_acc = dq_acc; bp.blocks = grad.blocks; bp.status = p.status;
     bp.no_queries = (long long)tokens;
     bp.H = p.H; bp.W = p.W; bp.heads = p.heads; bp.M = p.M; bp.s = p.s; bp.n = p.n; bp.nWy = p.nWy; bp.nWx = p.nWx; bp.Hp = p.Hp; bp.Wp = p.Wp;
     bp.items = bp.g.per_head * p.heads;
@@ -728,9 +736,11 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     const int grid = bp.items < sm_count ? bp.items : sm_count;
     { ProfileScope scope(RIB_KERNEL_BIAS_BWD, stream); rib_bias_bwd_kernel<<<grid, kThreads, smem_bytes(p.M), stream>>>(tm_q, tm_k, tm_v, tm_do, tm_dk, tm_dv, bp); }
     if (cudaError_t e = cudaGetLastError()) return e;
-    { ProfileScope scope(RIB_KERNEL_BIAS_BWD_FINISH, stream); rib_bias_bwd_finish_kernel<<<(unsigned)((tokens + 127) / 128), 256, 0, stream>>>(ap); }
+    const BiasScatter scatter = bias_scatter_args(p, grad, true);
+    const unsigned dq_blocks = (unsigned)((tokens + 127) / 128), all = dq_blocks + (unsigned)(((size_t)p.heads * scatter.side * scatter.side + 255) / 256);
+    { ProfileScope scope(RIB_KERNEL_BIAS_BWD_FINISH, stream); rib_bias_bwd_finish_kernel<<<all, 256, 0, stream>>>(ap, scatter, dq_blocks); }
     if (cudaError_t e = cudaGetLastError()) return e;
-    return bias_grad_finish(p, grad, stream);
+    return bias_grad_convert(p, grad, stream);
 }
 
 }  // namespace rib

@@ -81,16 +81,44 @@ cudaError_t generic_fwd(const Problem& p, cudaStream_t stream);
 cudaError_t generic_bwd(const Problem& p, cudaStream_t stream, double* offset_sums = nullptr);     // offset_sums: BiasGrad::offsets
 cudaError_t rowdot_prepass(const Problem& p, cudaStream_t stream);
 
-// The gradient of a bias by buckets (rib_bias.cu): its scratch lies at the end of a backward workspace.
+// The gradient of a bias by buckets (rib_bias.cu): its scratch lies at the end of a backward workspace and starts at zero.  The any-shape
+// kernels sum dS by offset, in 64 bits; the tcgen05 kernels by the difference of 8 x 8 patches, [heads][(2M/8-1)^2] blocks of 16 x 16 fp32 with the
+// differences -8 .. 7 of rows and columns inside them, of which an offset has up to four.
 struct BiasGrad {
-    double* offsets;      // [heads][(2M-1)^2] sums of dS by offset
+    double* offsets;      // [heads][(2M-1)^2]
+    float* blocks;        // in the same place
     double* tables;       // [tables][num_buckets]
-    unsigned* done;       // blocks of the finishing kernel that are through
-    size_t bytes;         // of all three, which start at zero
+    size_t bytes;
 };
 BiasGrad bias_grad_layout(int heads, int tables, int M, int num_buckets, void* base);
 cudaError_t bias_grad_clear(const BiasGrad& g, cudaStream_t stream);
-cudaError_t bias_grad_finish(const Problem& p, const BiasGrad& g, cudaStream_t stream);
+// Adds the sums of a bucket's offsets (thread `t` of heads * (2M-1)^2).
+struct BiasScatter { const int* buckets; double* tables; const double* offsets; const float* blocks; int num_buckets, side, heads, shared; };
+inline BiasScatter bias_scatter_args(const Problem& p, const BiasGrad& g, bool blocked)
+{
+    return {p.buckets, g.tables, blocked ? nullptr : g.offsets, blocked ? g.blocks : nullptr, p.num_buckets, 2 * p.M - 1, p.heads, bias_tables(p) == 1 ? 1 : 0};
+}
+__device__ inline void bias_scatter(const BiasScatter& s, size_t t)
+{
+    const int entries = s.side * s.side;
+    if (t >= (size_t)s.heads * entries) return;
+    const int h = (int)(t / entries), e = (int)(t % entries), u = s.buckets[e];
+    if ((unsigned)u >= (unsigned)s.num_buckets) return;
+    double sum = 0.0;
+    if (s.blocks) {
+        const int M = (s.side + 1) / 2, across = 2 * (M / 8) - 1, oy = e / s.side + 1, ox = e % s.side + 1;       // (+ M - 1 - offset) + 1: 1 .. 2M - 1
+        // oy = 8 (patches + M / 8 - 1) + row + 8 with row -8 .. 7: block oy / 8 - 1 with row oy % 8, block oy / 8 with row oy % 8 - 8
+        for (int by = oy / 8 - 1; by <= oy / 8; ++by)
+            for (int bx = ox / 8 - 1; bx <= ox / 8; ++bx)
+                if (by >= 0 && by < across && bx >= 0 && bx < across)
+                    sum += (double)s.blocks[(((size_t)h * across + by) * across + bx) * 256 + (oy - 8 * by) * 16 + ox - 8 * bx];
+    } else {
+        sum = s.offsets[t];
+    }
+    atomicAdd(s.tables + (size_t)(s.shared ? 0 : h) * s.num_buckets + u, sum);
+}
+cudaError_t bias_grad_scatter(const Problem& p, const BiasGrad& g, cudaStream_t stream);        // sums by offset -> tables
+cudaError_t bias_grad_convert(const Problem& p, const BiasGrad& g, cudaStream_t stream);        // tables -> dbias
 bool sm100_bias_fwd_supported(const Problem& p);
 cudaError_t sm100_bias_fwd(const Problem& p, cudaStream_t stream);
 bool sm100_bias_bwd_supported(const Problem& p);
