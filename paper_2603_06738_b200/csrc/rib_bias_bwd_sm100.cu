@@ -342,6 +342,9 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 const uint32_t t_s = tmem + lane_base + 32 * cg + kStep * buf, t_dp = t_s + kColDP;
                 buf = buffer_after(buf, 2);
                 const uint32_t b_addr = k_addr - entries[2 * I];
+                // biases of key row a against query row b of the warp's rows, a - b = k (the queries' columns go up, so the offsets go down)
+                auto bias = [&](int k) { return make_float2(lds_f32(b_addr + k * (int)pitch), lds_f32(b_addr + k * (int)pitch - 4)); };
+                float2 bb[3] = {bias(1), bias(2), bias(3)};
                 // warp-uniform outcome: the TMEM accesses below are warp-collective
                 if (!mbar_wait_warp(on_unit(kSFull, 2 * g + h), unit_parity(2 * g), abort_flag, p.status) ||
                     !mbar_wait_warp(bar(kQFull + st), (g / kQStages) & 1, abort_flag, p.status)) { ok = false; break; }
@@ -356,8 +359,6 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     tmem_ld_16x256b_x2(t_s + at, s);
                     tmem_ld_16x256b_x2(t_dp + at, dp);
                 };
-                // biases of key row a against query row b of the warp's rows, a - b = k (the queries' columns go up, so the offsets go down)
-                auto bias = [&](int k) { return make_float2(lds_f32(b_addr + k * (int)pitch), lds_f32(b_addr + k * (int)pitch - 4)); };
                 // bb[i]: a - b = k0 + i - 1 with k0 that of equal fragment rows (gq == rr)
                 auto work4 = [&](auto cut, int c4, const uint32_t (&s)[8], const uint32_t (&dp)[8], const float4 (&t)[2], const float2 (&bb)[3], uint32_t (&pp)[4], uint32_t (&dd)[4]) {
 #pragma unroll
@@ -397,12 +398,10 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     auto unit = [&](auto cut) -> bool {
                         uint32_t s0[8], dp0[8], s1[8], dp1[8];
                         float4 t[2];
-                        float2 bb[3];
                         const bool ds_free = mbar_try_wait(b_ds, ds_parity);
                         load(1, s1, dp1);
                         load(0, s0, dp0);
                         t[0] = ldq(0); t[1] = ldq(1);                         // queries 8 gq + 2 (lane % 4), + 1
-                        bb[0] = bias(1); bb[1] = bias(2); bb[2] = bias(3);
                         tmem_wait_ld();
                         work4(cut, 1, s1, dp1, t, bb, pp, dd);
                         if (!__all_sync(0xffffffffu, ds_free) && !mbar_wait_warp(b_ds, ds_parity, abort_flag, p.status)) return false;
@@ -556,11 +555,11 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (!mbar_wait_warp(on_unit(kPReady, 2 * g + h), unit_parity(2 * g), abort_flag, p.status)) { ok = false; break; }
                 // dS of key (a, x): line 8 a + x of the patch, 128 bytes; the 8 queries of row b: chunk b, swizzled by the line
                 uint32_t line = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + sub * 64 * 128 + second * 128;
-                const uint32_t zero = base + kOffZero + second * 128 + (t << 4);
+                const uint32_t zero = base + kOffZero + second * 128;
                 float sum[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};      // differences of columns -8 .. -1 and 0 .. 7; [0], [1]: rows t, [2], [3]: rows t - 8
-#pragma unroll 2
+#pragma unroll 4
                 for (int a = 0; a < 8; ++a, line += 1024) {
-                    const uint32_t addr = (a < t) == (lower != 0) ? line + ((((a - t) & 7) ^ second) << 4) : zero;
+                    const uint32_t addr = ((a < t) == (lower != 0) ? line : zero) + ((((a - t) & 7) ^ second) << 4);
                     uint32_t r[4][4];
 #pragma unroll
                     for (int pr = 0; pr < 4; ++pr) ldmatrix_x4((addr ^ (pr << 5)) + 256 * pr, r[pr]);

@@ -14,18 +14,44 @@
 // warps of their own, and the row sum l is a 33rd column of the PV contraction, against a tile of ones behind V.
 //
 // What differs is the softmax.  Scores are read as 16-lane fragments: a thread holds four query rows of one column of their patch and, of each key
-// row of the block's patch, two neighbouring keys, and finds their biases in 14 pairs of the table (rib_bias_sm100.cuh).  The reference m is
-// one number for those four rows, the largest of their scores (without bias) over the window's first 32 keys, and is subtracted from the
-// pairs of biases once, so a score costs one multiply-add, one exponential and half a conversion.  A row whose sum of
-// exponentials leaves [2^-64, 2^100) - scores far above the reference, rows without any key - is noted, and its item redone in the same launch
-// by the exact form: running maximum, accumulators per key half, a merge.  Keys beyond the map's edge have zero rows of V and, for l, zeros
-// in the tile of ones: five half tiles for a whole patch, none, and one cut below, right or both.
+// row of the block's patch, two neighbouring keys, and finds their biases in 11 pairs of the table (rib_bias_sm100.cuh).
+// There is no reference m: fp32 and bf16 carry 8 exponent bits, so the exponentials of scores (with bias) up to 69 are as exact as those of
+// small ones, and a score costs one multiply-add, one exponential and half a conversion.  A row whose sum of exponentials leaves
+// [2^-64, 2^100) - large scores of either sign, rows without any key, scores that are not finite - is noted, and its item redone in the same launch
+// by the exact form: running maximum, accumulators per key half, a merge.  (A reference from the window's first 32 keys, as in the rank-r kernel: 302
+// us against REFLESS on 16 x 96 x 96 tokens in windows of 32.)  Every fourth pair of exponentials (kPolyMask) is evaluated on the FMA and integer pipes
+// instead of the MUFU.  Keys beyond the map's edge have zero rows of V and, for l, zeros in the tile of ones: five half tiles for
+// a whole patch, none, and one cut below, right or both.
 #include "rib_bias_sm100.cuh"
+
+#ifndef RIB_BIAS_POLY_MASK
+#define RIB_BIAS_POLY_MASK 0x88u
+#endif
 
 namespace rib {
 namespace {
 
 using namespace sm100;
+
+constexpr uint32_t kPolyMask = RIB_BIAS_POLY_MASK;       // of every 8 pairs of scores: which go to the FMA pipe
+
+// 2^x for a pair of arguments on the FMA and integer pipes.  x = n + f with n = round(x), |f| <= 1/2, n read off the low mantissa bits of
+// x + 1.5 * 2^23.  The cubic (relative error 7.5e-5) is evaluated with coefficients scaled by 2^-120, so its result carries the exponent field 6 or
+// 7 and 2^n is applied by adding n + 120, bounded to [0, 248], to that field: arguments below -120 (masked keys among them) yield about 2^-120, which
+// is nothing beside a row sum of at least 2^-64, and arguments from 128 on at least 2^127, which the epilogue sees in the row sum.
+__device__ __forceinline__ float2 ex2_poly2_bounded(float2 x)
+{
+    constexpr float kS = 7.52316384526264005e-37f;      // 2^-120
+    const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));
+    const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
+    const float2 f = __fadd2_rn(x, make_float2(-n.x, -n.y));
+    float2 q = __ffma2_rn(make_float2(0.05517084f * kS, 0.05517084f * kS), f, make_float2(0.24260935f * kS, 0.24260935f * kS));
+    q = __ffma2_rn(q, f, make_float2(0.69326097f * kS, 0.69326097f * kS));
+    q = __ffma2_rn(q, f, make_float2(0.99992818f * kS, 0.99992818f * kS));
+    // bits(t) = 0x4B400000 + n for |x| < 2^22
+    const int vx = __vimin_s32_relu(__float_as_int(t.x) + (120 - 0x4B400000), 248), vy = __vimin_s32_relu(__float_as_int(t.y) + (120 - 0x4B400000), 248);
+    return make_float2(__int_as_float(__float_as_int(q.x) + (vx << 23)), __int_as_float(__float_as_int(q.y) + (vy << 23)));
+}
 
 constexpr int kStages = 4;            // K/V ring depth
 constexpr int kThreads = 640;
@@ -319,10 +345,8 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (fast) {
                 // ------------------------------------------------------------------ fast form
                 const uint32_t t_o1 = tmem + lane_base + kColO + qt * kFastOCols;
-                // O and l of item i are complete (the caller has waited for its last PV): normalise, store, note overflow.  `ref`: of the thread's
-                // four fragment rows, which are rows lane / 4 mod 8 of the patch's columns; the row this thread stores here is in column lane mod 8.
-                auto epilogue = [&](int i, float ref) {
-                    const float row_ref = __shfl_sync(0xffffffffu, ref, 4 * (lane & 7));
+                // O and l of item i are complete (the caller has waited for its last PV): normalise, store, note overflow
+                auto epilogue = [&](int i) {
                     const LiveItem c = decode_bias_item(p.g, item_at(i));
                     const int sp = 2 * (2 * c.tp + qt) + (row >> 6);
                     int py, px, Y0, X0;
@@ -356,11 +380,9 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                             if (channels > 8) reinterpret_cast<uint4*>(dst)[1] = make_uint4(w[4], w[5], w[6], w[7]);
                         }
                     }
-                    if (p.lse && half == 0) p.lse[(((size_t)c.b * p.heads + c.h) * p.H + Y) * p.W + X] = row_ref * 0.69314718f + logf(l_all);
+                    if (p.lse && half == 0) p.lse[(((size_t)c.b * p.heads + c.h) * p.H + Y) * p.W + X] = logf(l_all);
                 };
-                float ref = 0.f;                                  // log2 units
                 for (int i = 0; i < count && ok; ++i, ++io) {
-                    const float ref_before = ref;
                     const LiveItem c = decode_bias_item(p.g, item_at(i));
                     if (!need_table(c.h)) { ok = false; break; }
                     const int nb = (c.patches + 1) >> 1;
@@ -380,20 +402,8 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         const uint32_t t_s = t_half + sb * kTile;
                         sb = sb == 0 ? 2u : sb - 1;
                         uint32_t a[16], b[16];
-                        if (j == 0) {
-                            // the reference: the maximum over keys 0-31 of the window, the same for both key halves
-                            tmem_ld_16x256b_x4(t_s - half * 64, a);
-                            tmem_ld_16x256b_x4(t_s - half * 64 + (16u << 16), b);
-                            tmem_wait_ld();
-                            float mx = -INFINITY;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) mx = max3(mx, __uint_as_float(a[e]), __uint_as_float(b[e]));
-                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                            ref = mx * p.scale_log2;
-                        }
-                        // biases of key row k of the patch against the thread's first row, minus the reference; row r of it: key row k - r
-                        auto bias = [&](int k) { return make_float2(lds_f32(b_addr + k * (int)pitch) - ref, lds_f32(b_addr + k * (int)pitch + 4) - ref); };
+                        // biases of key row k of the patch against the thread's first row; row r of it: key row k - r
+                        auto bias = [&](int k) { return make_float2(lds_f32(b_addr + k * (int)pitch), lds_f32(b_addr + k * (int)pitch + 4)); };
                         // 4 key rows (k0 ..) x rows 2 f, 2 f + 1; bb[0] is key row k0 - 3
                         auto work4 = [&](const uint32_t (&s)[16], const float2 (&bb)[7], int f, uint32_t t_p) {
                             uint32_t pk[8];
@@ -403,7 +413,8 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                                 for (int rr = 0; rr < 2; ++rr) {
                                     const int e = 4 * g + 2 * rr;
                                     const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale2, bb[g - 2 * f - rr + 3]);
-                                    pk[2 * g + rr] = pack_bf16x2(ex2_approx(x.x), ex2_approx(x.y));
+                                    const float2 v = ((kPolyMask >> (2 * g + rr)) & 1u) ? ex2_poly2_bounded(x) : make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                                    pk[2 * g + rr] = pack_bf16x2(v.x, v.y);
                                 }
                             tmem_st_16x128b_x4(t_p, pk);
                         };
@@ -420,7 +431,8 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         work4(b, bb, 1, t_s + 32 + kLow);
                         tmem_ld_16x256b_x4(t_s + kLow, b);
 #pragma unroll
-                        for (int k = 0; k < 7; ++k) bb[k] = bias(k - 3);
+                        for (int k = 0; k < 3; ++k) { bb[4 + k] = bb[k]; bb[k] = bias(k - 3); }      // (rows 1, 2, 3 serve again)
+                        bb[3] = bias(0);
                         tmem_wait_ld();
                         work4(a, bb, 0, t_s + 48);
                         work4(b, bb, 1, t_s + 48 + kLow);
@@ -428,7 +440,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         if (j == 0 && i > 0) {       // that PV was the last one of the item before
                             if (!mbar_wait_warp(on_block(kPVDone, qt, blk - 1), parity(blk - 1), abort_flag, p.status)) { ok = false; break; }
                             tc_fence_after();
-                            epilogue(i - 1, ref_before);
+                            epilogue(i - 1);
                         }
                         tc_fence_before();
                         __syncwarp();
@@ -437,7 +449,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 }
                 if (ok && count > 0) {
                     // the last item of the pass
-                    if (mbar_wait_warp(on_block(kPVDone, qt, blk - 1), parity(blk - 1), abort_flag, p.status)) { tc_fence_after(); epilogue(count - 1, ref); } else ok = false;
+                    if (mbar_wait_warp(on_block(kPVDone, qt, blk - 1), parity(blk - 1), abort_flag, p.status)) { tc_fence_after(); epilogue(count - 1); } else ok = false;
                 }
             } else {
                 // ------------------------------------------------------------------ exact form: a thread has one query row
@@ -475,8 +487,9 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                             float mx = -INFINITY;
                             auto add_bias = [&](uint32_t& s, int e) {
                                 const int y = e >> 3, x = e & 7;
-                                float v = fmaf(__uint_as_float(s), p.scale_log2, lds_f32(b_addr + y * pitch + 4 * x));
-                                if (y >= rows_there || x >= cols_there) v = -INFINITY;
+                                const float bias = lds_f32(b_addr + y * pitch + 4 * x);
+                                float v = fmaf(__uint_as_float(s), p.scale_log2, bias);
+                                if (bias == kTableMasked || y >= rows_there || x >= cols_there) v = -INFINITY;
                                 s = __float_as_uint(v);
                                 mx = fmaxf(mx, v);
                             };

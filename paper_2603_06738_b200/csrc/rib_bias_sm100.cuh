@@ -13,6 +13,9 @@ namespace sm100 {
 
 constexpr int kBiasMaxWindow = 64;                     // (127^2 fp32 = 64.5 KB beside the tiles)
 constexpr float kLog2e = 1.4426950408889634f;
+// What the table holds for keys that are not attended to: as good as minus infinity beside any score (in log2 units), but finite, so that the
+// polynomial form of the exponential takes it.
+constexpr float kTableMasked = -1e6f;
 
 struct BiasItems {
     LiveWindows live;              // of one head
@@ -111,8 +114,11 @@ __device__ __forceinline__ void gather_bias(const BiasSource& s, int h, int entr
         for (int k = 0; k < kAhead; ++k) u[k] = e0 + k * threads < entries ? __ldg(s.buckets + e0 + k * threads) : -1;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (e0 + k * threads < entries)
-                table[e0 + k * threads] = (unsigned)u[k] < (unsigned)s.num_buckets ? bias_at(s.bias, s.bf16, (long long)h * s.head_stride + u[k]) * kLog2e : -INFINITY;
+            if (e0 + k * threads < entries) {
+                const float b = (unsigned)u[k] < (unsigned)s.num_buckets ? bias_at(s.bias, s.bf16, (long long)h * s.head_stride + u[k]) : -INFINITY;
+                const float v = b * kLog2e;
+                table[e0 + k * threads] = b == -INFINITY ? kTableMasked : v == kTableMasked ? kTableMasked * 1.0001f : v;
+            }
     }
 }
 
