@@ -19,7 +19,7 @@
 // small ones, and a score costs one multiply-add, one exponential and half a conversion.  A row whose sum of exponentials leaves
 // [2^-64, 2^100) - large scores of either sign, rows without any key, scores that are not finite - is noted, and its item redone in the same launch
 // by the exact form: running maximum, accumulators per key half, a merge.  (A reference from the window's first 32 keys, as in the rank-r kernel: 302
-// us against REFLESS on 16 x 96 x 96 tokens in windows of 32.)  Every fourth pair of exponentials (kPolyMask) is evaluated on the FMA and integer pipes
+// us against 278 on 16 x 96 x 96 tokens in windows of 32.)  Every fourth pair of exponentials (kPolyMask) is evaluated on the FMA and integer pipes
 // instead of the MUFU.  Keys beyond the map's edge have zero rows of V and, for l, zeros in the tile of ones: five half tiles for
 // a whole patch, none, and one cut below, right or both.
 #include "rib_bias_sm100.cuh"
@@ -75,7 +75,8 @@ constexpr uint32_t kOffBar = kOffOnes + kOnesTiles * kHalfOnes;
 constexpr uint32_t kOffMisc = kOffBar + kNumBars * 8;                  // tmem base, abort flags, redo count
 constexpr uint32_t kOffRedo = kOffMisc + 16;                           // [kMaxRedo] item ordinals of the exact pass
 constexpr uint32_t kOffMerge = (kOffRedo + kMaxRedo * 4 + 15) & ~15u;  // [2 item parities][2 tiles][2 halves][128 rows] (max, sum)
-constexpr uint32_t kOffTable = kOffMerge + 8 * kTile * 8;              // [(2M-1)^2] fp32
+constexpr uint32_t kOffLists = kOffMerge + 8 * kTile * 8;              // PatchLists
+constexpr uint32_t kOffTable = kOffLists + sizeof(PatchLists);         // [(2M-1)^2] fp32
 constexpr uint32_t smem_bytes(int M) { return kOffTable + 4u * (2 * M - 1) * (2 * M - 1) + 1024; }      // + slack for manual alignment
 static_assert(smem_bytes(kBiasMaxWindow) <= 232448, "shared memory of one CTA");
 
@@ -116,6 +117,166 @@ __device__ __forceinline__ void patch_box(const Params& p, const LiveItem& c, in
     if (sp >= c.patches) X0 = p.Wp;
 }
 
+// The table of head h, when all softmax warps are through with the last one's.  False when a wait ran out.
+__device__ __forceinline__ bool change_table(const Params& p, uint8_t* base_ptr, uint32_t base, int h, int* table_head, uint32_t* ntable)
+{
+    if (h == *table_head) return true;
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + kOffMisc + 4);
+    const uint32_t done = base + kOffBar + 8u * kTabDone, ready = base + kOffBar + 8u * kTabReady;
+    const int lane = threadIdx.x & 31, side = 2 * p.M - 1;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(done);
+    if (!mbar_wait_warp(done, *ntable & 1, abort_flag, p.status)) return false;
+    gather_bias(p.source, h, side * side, reinterpret_cast<float*>(base_ptr + kOffTable), threadIdx.x - 128, kSoftmaxThreads);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(ready);
+    if (!mbar_wait_warp(ready, *ntable & 1, abort_flag, p.status)) return false;
+    ++*ntable;
+    *table_head = h;
+    return true;
+}
+
+// The softmax warps' items in the exact form: a thread has one query row and one half of the keys.  Not inlined: its registers and instructions
+// beside those of the fast form cost that 463 -> 428 us on 256 x 256 tokens in windows of 64.
+struct ExactState { uint32_t base, tmem, blk, sb, ntable; int table_head, count, first_item; bool all_items; };
+__device__ __noinline__ void exact_items(const Params& p, uint8_t* base_ptr, ExactState st)
+{
+    const uint32_t base = st.base;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto bar = [&](int i) { return base + kOffBar + 8u * i; };
+    auto on_block = [&](int which, int tile, uint32_t block) { return bar(which + 2 * tile + (block & 1)); };
+    auto parity = [](uint32_t block) { return (block >> 1) & 1; };
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + kOffMisc + 4);
+    volatile int* redo_list = reinterpret_cast<volatile int*>(base_ptr + kOffRedo);
+    auto first = [&](int i) { return st.first_item + (st.all_items ? i : redo_list[i]); };
+    const int qt = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t lane_base = (uint32_t)(quarter * 32) << 16, t_half = st.tmem + lane_base + half * 64;
+    const uint32_t pitch = 4u * (2 * p.M - 1), table_addr = base + kOffTable;
+    uint32_t nmerge = 0;
+    bool ok = true;
+    const uint32_t t_o = st.tmem + lane_base + kColO + qt * 2 * kD;        // both halves' accumulators
+    // [half][row]; two sets, so that a warp that is an item ahead of its partner does not overwrite what that one still reads
+    float2* const merge_sets = reinterpret_cast<float2*>(base_ptr + kOffMerge) + qt * 2 * kTile;
+    for (int i = 0; i < st.count && ok; ++i, ++nmerge) {
+        const LiveItem c = decode_bias_item(p.g, first(i));
+        if (!change_table(p, base_ptr, base, c.h, &st.table_head, &st.ntable)) { ok = false; break; }
+        float m_used = -INFINITY, l = 0.f;          // log2 units
+        const int nb = (c.patches + 1) >> 1, sp = 2 * (2 * c.tp + qt) + (row >> 6);
+        int qy, qx, QY0, QX0;
+        patch_origin(p, c, sp, qy, qx, QY0, QX0);
+        const uint32_t q_addr = table_addr + (p.M - 1 - qy - ((row >> 3) & 7)) * pitch + 4 * (p.M - 1 - qx - (row & 7));
+        for (int j = 0; j < nb; ++j, ++st.blk) {
+            // warp-uniform outcome: the TMEM loads below are warp-collective
+            if (!mbar_wait_warp(on_block(kSFull, qt, st.blk), parity(st.blk), abort_flag, p.status)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t t_s = t_half + st.sb * kTile;
+            st.sb = st.sb == 0 ? 2u : st.sb - 1;
+            uint32_t pa[16], pb[16];
+            if (2 * j + half >= c.patches) {
+                // half a block without tokens (the last one of an odd number of patches)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) pa[e] = pb[e] = 0u;
+            } else {
+                int py, px, Y0, X0;
+                patch_origin(p, c, 2 * j + half, py, px, Y0, X0);
+                const uint32_t b_addr = q_addr + py * pitch + 4 * px;
+                const int rows_there = p.H - Y0, cols_there = p.W - X0;      // of the patch: keys beyond the edge are none
+                uint32_t sa[32], sc[32];
+                tmem_ld32(t_s, sa);
+                tmem_ld32(t_s + 32, sc);
+                tmem_wait_ld();
+                float mx = -INFINITY;
+                auto add_bias = [&](uint32_t& s, int e) {
+                    const int y = e >> 3, x = e & 7;
+                    const float bias = lds_f32(b_addr + y * pitch + 4 * x);
+                    float v = fmaf(__uint_as_float(s), p.scale_log2, bias);
+                    if (bias == kTableMasked || y >= rows_there || x >= cols_there) v = -INFINITY;
+                    s = __float_as_uint(v);
+                    mx = fmaxf(mx, v);
+                };
+#pragma unroll
+                for (int e = 0; e < 32; ++e) { add_bias(sa[e], e); add_bias(sc[e], e + 32); }
+                if (j == 0) {
+                    m_used = mx;
+                } else {
+                    // Move the reference (and rescale O, l) only when the maximum grew by more than 2^8
+                    const bool need = mx > m_used + 8.f;
+                    if (__any_sync(0xffffffffu, need)) {
+                        if (!mbar_wait_warp(on_block(kPVDone, qt, st.blk - 1), parity(st.blk - 1), abort_flag, p.status)) { ok = false; break; }
+                        tc_fence_after();
+                        const float factor = need ? ex2_approx(m_used - mx) : 1.f;
+                        if (need) { l *= factor; m_used = mx; }
+                        for (int g = 0; g < 4; ++g) {
+                            uint32_t o[8];
+                            tmem_ld8(t_o + half * kD + 8 * g, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                            tmem_st8(t_o + half * kD + 8 * g, o);
+                        }
+                    }
+                }
+                const float m = m_used == -INFINITY ? 0.f : m_used;      // (no key so far: every exponential is 0)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float a0 = ex2_approx(__uint_as_float(sa[2 * e]) - m), a1 = ex2_approx(__uint_as_float(sa[2 * e + 1]) - m);
+                    const float b0 = ex2_approx(__uint_as_float(sc[2 * e]) - m), b1 = ex2_approx(__uint_as_float(sc[2 * e + 1]) - m);
+                    l += (a0 + a1) + (b0 + b1);
+                    pa[e] = pack_bf16x2(a0, a1);
+                    pb[e] = pack_bf16x2(b0, b1);
+                }
+            }
+            tmem_st16(t_s + 32, pa);
+            tmem_st16(t_s + 48, pb);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(on_block(kPReady, qt, st.blk));
+        }
+        if (!ok) break;
+        // ---- merge the two key halves and write this thread's 16 output columns
+        float2* const merge = merge_sets + (nmerge & 1) * 4 * kTile;
+        merge[half * kTile + row] = make_float2(m_used, l);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kMerge + 4 * qt + quarter));
+        // The partner's (m, l) must be there and the item's last PV must have completed.
+        if (!mbar_wait_warp(bar(kMerge + 4 * qt + quarter), nmerge & 1, abort_flag, p.status) ||
+            !mbar_wait_warp(on_block(kPVDone, qt, st.blk - 1), parity(st.blk - 1), abort_flag, p.status)) { ok = false; break; }
+        tc_fence_after();
+        uint32_t oa[16], ob[16];
+        tmem_ld16(t_o + half * 16, oa);
+        tmem_ld16(t_o + kD + half * 16, ob);
+        tmem_wait_ld();
+        const float2 other = merge[(half ^ 1) * kTile + row];
+        tc_fence_before();
+        const float m_a = half ? other.x : m_used, l_a = half ? other.y : l;
+        const float m_b = half ? m_used : other.x, l_b = half ? l : other.y;
+        const float m = fmaxf(m_a, m_b);
+        const bool none = m == -INFINITY;                  // a row without any key: out 0, lse -inf
+        const float f_a = none ? 0.f : ex2_approx(m_a - m), f_b = none ? 0.f : ex2_approx(m_b - m);
+        const float l_all = l_a * f_a + l_b * f_b;
+        const float w_a = none ? 0.f : f_a / l_all, w_b = none ? 0.f : f_b / l_all;
+        const int Y = QY0 + ((row >> 3) & 7), X = QX0 + (row & 7);   // the patch does not straddle the border
+        if (sp >= c.patches || Y >= p.H || X >= p.W) continue;
+        const size_t tok = (((size_t)c.b * p.H + Y) * p.W + X) * p.heads + c.h;
+        uint4* dst = reinterpret_cast<uint4*>(p.out + tok * p.d + half * 16);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            if (half * 16 + 8 * g >= p.d) break;          // a head narrower than 32 channels: the rest of the row is padding
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int e = 8 * g + 2 * k;
+                w[k] = pack_bf16x2(__uint_as_float(oa[e]) * w_a + __uint_as_float(ob[e]) * w_b,
+                                   __uint_as_float(oa[e + 1]) * w_a + __uint_as_float(ob[e + 1]) * w_b);
+            }
+            dst[g] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (p.lse && half == 0)
+            p.lse[(((size_t)c.b * p.heads + c.h) * p.H + Y) * p.W + X] = none ? -INFINITY : m * 0.69314718f + logf(l_all);
+    }
+}
+
 __global__ void __launch_bounds__(kThreads, 1)
 rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                     const __grid_constant__ Params p)
@@ -130,7 +291,6 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + kOffMisc + 4);
     int* redo_count = reinterpret_cast<int*>(base_ptr + kOffMisc + 12);      // notes taken (duplicates included)
     volatile int* redo_list = reinterpret_cast<volatile int*>(base_ptr + kOffRedo);
-    float* const table = reinterpret_cast<float*>(base_ptr + kOffTable);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int side = 2 * p.M - 1;
@@ -170,13 +330,15 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         for (int ck = 0; ck < 4; ++ck) dst[ck] = make_uint4(ck == sw && one ? 0x00003F80u : 0u, 0u, 0u, 0u);
         fence_proxy_async();
     }
+    PatchLists* const lists = reinterpret_cast<PatchLists*>(base_ptr + kOffLists);
+    fill_patch_lists(p.g, p.M, lists, threadIdx.x, kThreads);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
     // Role state that carries over from the first pass to the exact pass: block and item counters give the barrier phases.
-    uint32_t blk = 0, io = 0, nmerge = 0, ntable = 0;
+    uint32_t blk = 0, io = 0, ntable = 0;
     int table_head = -1;
     uint32_t sb = warp == 3 || warp >= 12 ? 1u : 0u;        // score buffer of the next unit: (2 blk + tile) mod kBuffers
     uint32_t q_armed = 0, k_armed = 0, v_armed = 0;
@@ -327,20 +489,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
             const uint32_t pitch = 4u * side, table_addr = base + kOffTable;
 
-            // The table of head h: when all softmax warps are through with the last one's.
-            auto need_table = [&](int h) -> bool {
-                if (h == table_head) return true;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kTabDone));
-                if (!mbar_wait_warp(bar(kTabDone), ntable & 1, abort_flag, p.status)) return false;
-                gather_bias(p.source, h, side * side, table, threadIdx.x - 128, kSoftmaxThreads);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kTabReady));
-                if (!mbar_wait_warp(bar(kTabReady), ntable & 1, abort_flag, p.status)) return false;
-                ++ntable;
-                table_head = h;
-                return true;
-            };
+            auto need_table = [&](int h) { return change_table(p, base_ptr, base, h, &table_head, &ntable); };
 
             if (fast) {
                 // ------------------------------------------------------------------ fast form
@@ -386,24 +535,24 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const LiveItem c = decode_bias_item(p.g, item_at(i));
                     if (!need_table(c.h)) { ok = false; break; }
                     const int nb = (c.patches + 1) >> 1;
-                    uint32_t q_addr;          // table entry of the thread's first row and a key at the window's origin, plus its place among a key row's pairs
-                    {
-                        int py, px, Y0, X0;
-                        patch_origin(p, c, 2 * (2 * c.tp + qt) + (quarter >> 1), py, px, Y0, X0);
-                        q_addr = table_addr + (p.M - 1 - py - 4 * (quarter & 1)) * pitch + 4 * (p.M - 1 - px - (lane >> 2) + 2 * (lane & 3));
-                    }
+                    // table entry of the thread's first row and a key at the window's origin, plus its place among a key row's pairs
+                    const uint16_t* const list = lists->entry + list_of(c);
+                    const uint16_t* const entries = list + half;
+                    const uint32_t q_addr = table_addr + (p.M - 1 - 4 * (quarter & 1)) * pitch + 4 * (p.M - 1 - (lane >> 2) + 2 * (lane & 3)) - list[2 * (2 * c.tp + qt) + (quarter >> 1)];
                     for (int j = 0; j < nb; ++j, ++blk) {
-                        int py, px, Y0, X0;
-                        patch_origin(p, c, 2 * j + half, py, px, Y0, X0);
-                        const uint32_t b_addr = q_addr + py * pitch + 4 * px;
+                        const uint32_t b_addr = q_addr + entries[2 * j];
+                        // biases of key row k of the patch against the thread's first row; row r of it: key row k - r.  Those of the patch's second half
+                        // before the wait for the scores.
+                        auto bias = [&](int k) { return make_float2(lds_f32(b_addr + k * (int)pitch), lds_f32(b_addr + k * (int)pitch + 4)); };
+                        float2 bb[7];
+#pragma unroll
+                        for (int k = 0; k < 7; ++k) bb[k] = bias(k + 1);
                         // warp-uniform outcome: the TMEM loads below are warp-collective
                         if (!mbar_wait_warp(on_block(kSFull, qt, blk), parity(blk), abort_flag, p.status)) { ok = false; break; }
                         tc_fence_after();
                         const uint32_t t_s = t_half + sb * kTile;
                         sb = sb == 0 ? 2u : sb - 1;
                         uint32_t a[16], b[16];
-                        // biases of key row k of the patch against the thread's first row; row r of it: key row k - r
-                        auto bias = [&](int k) { return make_float2(lds_f32(b_addr + k * (int)pitch), lds_f32(b_addr + k * (int)pitch + 4)); };
                         // 4 key rows (k0 ..) x rows 2 f, 2 f + 1; bb[0] is key row k0 - 3
                         auto work4 = [&](const uint32_t (&s)[16], const float2 (&bb)[7], int f, uint32_t t_p) {
                             uint32_t pk[8];
@@ -420,11 +569,8 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         };
                         // P goes to the second half of the columns, whose keys are therefore taken first
                         constexpr uint32_t kLow = 16u << 16;                // lanes 16 .. 31
-                        float2 bb[7];
                         tmem_ld_16x256b_x4(t_s + 32, a);
                         tmem_ld_16x256b_x4(t_s + 32 + kLow, b);
-#pragma unroll
-                        for (int k = 0; k < 7; ++k) bb[k] = bias(k + 1);
                         tmem_wait_ld();
                         work4(a, bb, 0, t_s + 32);
                         tmem_ld_16x256b_x4(t_s, a);
@@ -452,128 +598,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     if (mbar_wait_warp(on_block(kPVDone, qt, blk - 1), parity(blk - 1), abort_flag, p.status)) { tc_fence_after(); epilogue(count - 1); } else ok = false;
                 }
             } else {
-                // ------------------------------------------------------------------ exact form: a thread has one query row
-                const uint32_t t_o = tmem + lane_base + kColO + qt * 2 * kD;        // both halves' accumulators
-                // [half][row]; two sets, so that a warp that is an item ahead of its partner does not overwrite what that one still reads
-                float2* const merge_sets = reinterpret_cast<float2*>(base_ptr + kOffMerge) + qt * 2 * kTile;
-                for (int i = 0; i < count && ok; ++i, ++io, ++nmerge) {
-                    const LiveItem c = decode_bias_item(p.g, item_at(i));
-                    if (!need_table(c.h)) { ok = false; break; }
-                    float m_used = -INFINITY, l = 0.f;          // log2 units
-                    const int nb = (c.patches + 1) >> 1, sp = 2 * (2 * c.tp + qt) + (row >> 6);
-                    int qy, qx, QY0, QX0;
-                    patch_origin(p, c, sp, qy, qx, QY0, QX0);
-                    const uint32_t q_addr = table_addr + (p.M - 1 - qy - ((row >> 3) & 7)) * pitch + 4 * (p.M - 1 - qx - (row & 7));
-                    for (int j = 0; j < nb; ++j, ++blk) {
-                        // warp-uniform outcome: the TMEM loads below are warp-collective
-                        if (!mbar_wait_warp(on_block(kSFull, qt, blk), parity(blk), abort_flag, p.status)) { ok = false; break; }
-                        tc_fence_after();
-                        const uint32_t t_s = t_half + sb * kTile;
-                        sb = sb == 0 ? 2u : sb - 1;
-                        uint32_t pa[16], pb[16];
-                        if (2 * j + half >= c.patches) {
-                            // half a block without tokens (the last one of an odd number of patches)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) pa[e] = pb[e] = 0u;
-                        } else {
-                            int py, px, Y0, X0;
-                            patch_origin(p, c, 2 * j + half, py, px, Y0, X0);
-                            const uint32_t b_addr = q_addr + py * pitch + 4 * px;
-                            const int rows_there = p.H - Y0, cols_there = p.W - X0;      // of the patch: keys beyond the edge are none
-                            uint32_t sa[32], sc[32];
-                            tmem_ld32(t_s, sa);
-                            tmem_ld32(t_s + 32, sc);
-                            tmem_wait_ld();
-                            float mx = -INFINITY;
-                            auto add_bias = [&](uint32_t& s, int e) {
-                                const int y = e >> 3, x = e & 7;
-                                const float bias = lds_f32(b_addr + y * pitch + 4 * x);
-                                float v = fmaf(__uint_as_float(s), p.scale_log2, bias);
-                                if (bias == kTableMasked || y >= rows_there || x >= cols_there) v = -INFINITY;
-                                s = __float_as_uint(v);
-                                mx = fmaxf(mx, v);
-                            };
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) { add_bias(sa[e], e); add_bias(sc[e], e + 32); }
-                            if (j == 0) {
-                                m_used = mx;
-                            } else {
-                                // Move the reference (and rescale O, l) only when the maximum grew by more than 2^8
-                                const bool need = mx > m_used + 8.f;
-                                if (__any_sync(0xffffffffu, need)) {
-                                    if (!mbar_wait_warp(on_block(kPVDone, qt, blk - 1), parity(blk - 1), abort_flag, p.status)) { ok = false; break; }
-                                    tc_fence_after();
-                                    const float factor = need ? ex2_approx(m_used - mx) : 1.f;
-                                    if (need) { l *= factor; m_used = mx; }
-                                    for (int g = 0; g < 4; ++g) {
-                                        uint32_t o[8];
-                                        tmem_ld8(t_o + half * kD + 8 * g, o);
-                                        tmem_wait_ld();
-#pragma unroll
-                                        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                                        tmem_st8(t_o + half * kD + 8 * g, o);
-                                    }
-                                }
-                            }
-                            const float m = m_used == -INFINITY ? 0.f : m_used;      // (no key so far: every exponential is 0)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const float a0 = ex2_approx(__uint_as_float(sa[2 * e]) - m), a1 = ex2_approx(__uint_as_float(sa[2 * e + 1]) - m);
-                                const float b0 = ex2_approx(__uint_as_float(sc[2 * e]) - m), b1 = ex2_approx(__uint_as_float(sc[2 * e + 1]) - m);
-                                l += (a0 + a1) + (b0 + b1);
-                                pa[e] = pack_bf16x2(a0, a1);
-                                pb[e] = pack_bf16x2(b0, b1);
-                            }
-                        }
-                        tmem_st16(t_s + 32, pa);
-                        tmem_st16(t_s + 48, pb);
-                        tmem_wait_st();
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(on_block(kPReady, qt, blk));
-                    }
-                    if (!ok) break;
-                    // ---- merge the two key halves and write this thread's 16 output columns
-                    float2* const merge = merge_sets + (nmerge & 1) * 4 * kTile;
-                    merge[half * kTile + row] = make_float2(m_used, l);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(kMerge + 4 * qt + quarter));
-                    // The partner's (m, l) must be there and the item's last PV must have completed.
-                    if (!mbar_wait_warp(bar(kMerge + 4 * qt + quarter), nmerge & 1, abort_flag, p.status) ||
-                        !mbar_wait_warp(on_block(kPVDone, qt, blk - 1), parity(blk - 1), abort_flag, p.status)) { ok = false; break; }
-                    tc_fence_after();
-                    uint32_t oa[16], ob[16];
-                    tmem_ld16(t_o + half * 16, oa);
-                    tmem_ld16(t_o + kD + half * 16, ob);
-                    tmem_wait_ld();
-                    const float2 other = merge[(half ^ 1) * kTile + row];
-                    tc_fence_before();
-                    const float m_a = half ? other.x : m_used, l_a = half ? other.y : l;
-                    const float m_b = half ? m_used : other.x, l_b = half ? l : other.y;
-                    const float m = fmaxf(m_a, m_b);
-                    const bool none = m == -INFINITY;                  // a row without any key: out 0, lse -inf
-                    const float f_a = none ? 0.f : ex2_approx(m_a - m), f_b = none ? 0.f : ex2_approx(m_b - m);
-                    const float l_all = l_a * f_a + l_b * f_b;
-                    const float w_a = none ? 0.f : f_a / l_all, w_b = none ? 0.f : f_b / l_all;
-                    const int Y = QY0 + ((row >> 3) & 7), X = QX0 + (row & 7);   // the patch does not straddle the border
-                    if (sp >= c.patches || Y >= p.H || X >= p.W) continue;
-                    const size_t tok = (((size_t)c.b * p.H + Y) * p.W + X) * p.heads + c.h;
-                    uint4* dst = reinterpret_cast<uint4*>(p.out + tok * p.d + half * 16);
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        if (half * 16 + 8 * g >= p.d) break;          // a head narrower than 32 channels: the rest of the row is padding
-                        uint32_t w[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int e = 8 * g + 2 * k;
-                            w[k] = pack_bf16x2(__uint_as_float(oa[e]) * w_a + __uint_as_float(ob[e]) * w_b,
-                                               __uint_as_float(oa[e + 1]) * w_a + __uint_as_float(ob[e + 1]) * w_b);
-                        }
-                        dst[g] = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                    if (p.lse && half == 0)
-                        p.lse[(((size_t)c.b * p.heads + c.h) * p.H + Y) * p.W + X] = none ? -INFINITY : m * 0.69314718f + logf(l_all);
-                }
+                exact_items(p, base_ptr, ExactState{base, tmem, blk, sb, ntable, table_head, count, first_item, all_items});      // (the last pass: nothing of the state is needed after it)
             }
         }
         if (pass == 1 || !fast) break;                   // CTA-uniform: `fast` depends on the kernel arguments only
