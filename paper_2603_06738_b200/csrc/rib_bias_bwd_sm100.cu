@@ -111,8 +111,9 @@ __device__ __forceinline__ void red_add_f32x2(float* addr, float a, float b)
     asm volatile("red.relaxed.gpu.global.add.v2.f32 [%0], {%1, %2};" ::"l"(addr), "f"(a), "f"(b) : "memory");
 }
 
-template <bool B> struct Flag { static constexpr bool value = B; };
-
+// kCut: the map's edge cuts patches (H or W is no multiple of 8).  A kernel of its own: what the loops of all roles together take of the instruction cache
+// decides its time, and with both forms of the arithmetic in one kernel it was 850 or 690 us, as the code happened to lie, against 715.
+template <bool kCut>
 __global__ void __launch_bounds__(kThreads, 1)
 rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                     const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_dk, const __grid_constant__ CUtensorMap tm_dv,
@@ -333,7 +334,6 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             // keys of the patch beyond the map's edge get probability 0: a thread's whole column, or the rows from `rows_there` on
             const bool column_there = X0 + xk < p.W;
             const int rows_there = p.H - Y0 - key_row0;          // of the thread's four
-            const bool cut_any = rows_there < 4 || X0 + 8 > p.W;
             const uint32_t k_addr = table_addr + (ky + key_row0 - 4 * cg + p.M - 1) * pitch + 4 * (kx + xk + p.M - 1 - 2 * (lane & 3));
             const uint16_t* const entries = lists->entry + list_of(c) + h;
             const int tiles = (c.patches + 1) >> 1;
@@ -349,80 +349,65 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (!mbar_wait_warp(on_unit(kSFull, 2 * g + h), unit_parity(2 * g), abort_flag, p.status) ||
                     !mbar_wait_warp(bar(kQFull + st), (g / kQStages) & 1, abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
-                // four pieces of 16 keys x 16 queries (piece c: lanes 16 (c % 2) .., queries 16 (c / 2) ..), read as 16-lane fragments: a thread holds 2 key
-                // rows of 2 x 2 queries of a piece
+                // Four pieces of 16 keys x 16 queries, read as 16-lane fragments: piece (o, G) has lanes 16 o .. and queries 16 G .., a thread of it 2 key rows of
+                // 2 x 2 queries.  For each G first o = 1, then o = 0: their differences of rows a - b are 1 2 3 and -1 0 1, less 2 G, so that the
+                // biases of the second piece are those of the next G's first one as well.
                 const uint32_t ld = base + kOffRing + st * kRingBytes + kRingLD + (32 * h + 16 * cg + (lane & 3)) * 16;
-                auto ldq = [&](int gq) { return lds_f32x4(ld + 64 * gq); };
-                const uint32_t ds_line = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + (quarter * 32 + 8 * ((lane >> 3) & 1) + (lane & 7)) * 128;
-                auto load = [&](int c4, uint32_t (&s)[8], uint32_t (&dp)[8]) {
-                    const uint32_t at = ((uint32_t)(16 * (c4 & 1)) << 16) + 16 * (c4 >> 1);
+                // dS tile: row = key, 128-byte line = the unit's 64 queries, 16-byte chunks swizzled by the row
+                const uint32_t ds_at = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + (quarter * 32 + 8 * ((lane >> 3) & 1) + (lane & 7)) * 128 + (((cg * 4 + (lane >> 4)) ^ (lane & 7)) << 4);
+                auto load = [&](int o, int G, uint32_t (&s)[8], uint32_t (&dp)[8]) {
+                    const uint32_t at = ((uint32_t)(16 * o) << 16) + 16 * G;
                     tmem_ld_16x256b_x2(t_s + at, s);
                     tmem_ld_16x256b_x2(t_dp + at, dp);
                 };
-                // bb[i]: a - b = k0 + i - 1 with k0 that of equal fragment rows (gq == rr)
-                auto work4 = [&](auto cut, int c4, const uint32_t (&s)[8], const uint32_t (&dp)[8], const float4 (&t)[2], const float2 (&bb)[3], uint32_t (&pp)[4], uint32_t (&dd)[4]) {
+                // bb[i]: a - b = that of equal fragment rows (gq == rr) + i - 1
+                auto work = [&](int o, const uint32_t (&s)[8], const uint32_t (&dp)[8], const float4 (&t)[2], const float2 (&bb)[3], uint32_t (&pp)[4], uint32_t (&dd)[4]) {
 #pragma unroll
                     for (int gq = 0; gq < 2; ++gq)
 #pragma unroll
-                        for (int rr = 0; rr < 2; ++rr) {                  // key rows 2 (c % 2) + rr of the warp's, query rows 2 (c / 2) + gq
+                        for (int rr = 0; rr < 2; ++rr) {                  // key rows 2 o + rr of the warp's, query rows 2 G + gq
                             const int i = 4 * gq + 2 * rr;
                             const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2,
                                                         __fadd2_rn(make_float2(t[gq].x, t[gq].y), bb[1 + rr - gq]));
                             float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                            if (cut.value && (!column_there || 2 * (c4 & 1) + rr >= rows_there)) e = make_float2(0.f, 0.f);
+                            if (kCut && (!column_there || 2 * o + rr >= rows_there)) e = make_float2(0.f, 0.f);
                             const float2 d = __fmul2_rn(e, __fadd2_rn(make_float2(__uint_as_float(dp[i]), __uint_as_float(dp[i + 1])), make_float2(t[gq].z, t[gq].w)));
                             pp[2 * gq + rr] = pack_bf16x2(e.x, e.y);
                             dd[2 * gq + rr] = pack_bf16x2(d.x, d.y);
                         }
                 };
-                // dS tile: row = key, 128-byte line = the unit's 64 queries, 16-byte chunks swizzled by the row
-                auto store = [&](int c4, const uint32_t (&pp)[4], const uint32_t (&dd)[4]) {
-                    const uint32_t at = ((uint32_t)(16 * (c4 & 1)) << 16) + 8 * (c4 >> 1);
+                auto store = [&](int o, int G, const uint32_t (&pp)[4], const uint32_t (&dd)[4]) {
+                    const uint32_t at = ((uint32_t)(16 * o) << 16) + 8 * G;
                     tmem_st_16x128b_x2(t_s + at, pp);
                     tmem_st_16x128b_x2(t_dp + at, dd);
-                    stmatrix_x4(ds_line + 16 * (c4 & 1) * 128 + (((cg * 4 + 2 * (c4 >> 1) + (lane >> 4)) ^ (lane & 7)) << 4), dd[0], dd[1], dd[2], dd[3]);
+                    stmatrix_x4((ds_at ^ (32 * G)) + 16 * o * 128, dd[0], dd[1], dd[2], dd[3]);
                 };
                 // The tile before the previous one is still read in this dS buffer.  (A barrier that has completed no phase answers yes to
                 // parity 1, which the first tiles ask for.)
                 const uint32_t b_ds = bar(kDSFree + (g & 1)), ds_parity = ((g >> 1) - 1) & 1;
-                uint32_t pp[4], dd[4];
-                if (!key_exists) {
-                    if (!mbar_wait_warp(b_ds, ds_parity, abort_flag, p.status)) { ok = false; break; }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) pp[e] = dd[e] = 0u;
-#pragma unroll
-                    for (int c4 = 0; c4 < 4; ++c4) store(c4, pp, dd);
-                } else {
-                    // Pieces in the order 1, 0, 3, 2: neighbours share pairs of biases (a - b = 1 2 3, -1 0 1, -1 0 1, -3 -2 -1).  A piece is stored while the
-                    // next but one is on its way, over scores that this warp has read.
-                    auto unit = [&](auto cut) -> bool {
-                        uint32_t s0[8], dp0[8], s1[8], dp1[8];
-                        float4 t[2];
-                        const bool ds_free = mbar_try_wait(b_ds, ds_parity);
-                        load(1, s1, dp1);
-                        load(0, s0, dp0);
-                        t[0] = ldq(0); t[1] = ldq(1);                         // queries 8 gq + 2 (lane % 4), + 1
-                        tmem_wait_ld();
-                        work4(cut, 1, s1, dp1, t, bb, pp, dd);
-                        if (!__all_sync(0xffffffffu, ds_free) && !mbar_wait_warp(b_ds, ds_parity, abort_flag, p.status)) return false;
-                        load(3, s1, dp1);
-                        store(1, pp, dd);
-                        bb[2] = bb[0]; bb[0] = bias(-1); bb[1] = bias(0);
-                        work4(cut, 0, s0, dp0, t, bb, pp, dd);
-                        tmem_wait_ld();
-                        load(2, s0, dp0);
-                        store(0, pp, dd);
-                        t[0] = ldq(2); t[1] = ldq(3);
-                        work4(cut, 3, s1, dp1, t, bb, pp, dd);
-                        tmem_wait_ld();
-                        store(3, pp, dd);
-                        bb[2] = bb[0]; bb[0] = bias(-3); bb[1] = bias(-2);
-                        work4(cut, 2, s0, dp0, t, bb, pp, dd);
-                        store(2, pp, dd);
-                        return true;
-                    };
-                    if (!(cut_any ? unit(Flag<true>{}) : unit(Flag<false>{}))) { ok = false; break; }
+                const bool ds_free = mbar_try_wait(b_ds, ds_parity);
+                uint32_t pp[4], dd[4], s0[8], dp0[8], s1[8], dp1[8];
+                load(1, 0, s1, dp1);
+                load(0, 0, s0, dp0);
+                // A piece is stored while the next but one is on its way, over scores that this warp has read.
+#pragma unroll 1
+                for (int G = 0; G < 2; ++G) {
+                    const float4 t[2] = {lds_f32x4(ld + 128 * G), lds_f32x4(ld + 128 * G + 64)};      // queries 16 G + 8 gq + 2 (lane % 4), + 1
+                    tmem_wait_ld();
+                    work(1, s1, dp1, t, bb, pp, dd);
+                    if (!key_exists) pp[0] = pp[1] = pp[2] = pp[3] = dd[0] = dd[1] = dd[2] = dd[3] = 0u;
+                    if (G == 0) {
+                        if (!__all_sync(0xffffffffu, ds_free) && !mbar_wait_warp(b_ds, ds_parity, abort_flag, p.status)) { ok = false; break; }
+                        load(1, 1, s1, dp1);
+                    }
+                    store(1, G, pp, dd);
+                    bb[2] = bb[0]; bb[0] = bias(-1 - 2 * G); bb[1] = bias(-2 * G);
+                    work(0, s0, dp0, t, bb, pp, dd);
+                    if (!key_exists) pp[0] = pp[1] = pp[2] = pp[3] = dd[0] = dd[1] = dd[2] = dd[3] = 0u;
+                    if (G == 0) load(0, 1, s0, dp0);
+                    store(0, G, pp, dd);
                 }
+                if (!ok) break;
                 tmem_wait_st();
                 tc_fence_before();
                 fence_proxy_async();
@@ -711,9 +696,11 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     if (!encode_image_map(&tm_q, p.q, p) || !encode_image_map(&tm_k, p.k, p) || !encode_image_map(&tm_v, p.v, p) || !encode_image_map(&tm_do, p.dout, p) ||
         !encode_image_map(&tm_dk, p.dk, p, 4) || !encode_image_map(&tm_dv, p.dv, p, 4))
         return cudaErrorInvalidValue;
-    static KernelSetup setup;
+    static KernelSetup setup[2];
+    const bool cut = p.H % 8 != 0 || p.W % 8 != 0;
+    const auto kernel = cut ? rib_bias_bwd_kernel<true> : rib_bias_bwd_kernel<false>;
     int sm_count = 0;
-    if (cudaError_t e = setup.prepare(rib_bias_bwd_kernel, smem_bytes(kBiasMaxWindow), &sm_count)) return e;
+    if (cudaError_t e = setup[cut].prepare(kernel, smem_bytes(kBiasMaxWindow), &sm_count)) return e;
     Params bp{};
     if (!make_bias_items(p, 2, &bp.g)) return cudaErrorInvalidValue;
     AuxParams ap{};
@@ -733,7 +720,7 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     bp.inv_sqrt_d = ap.inv_sqrt_d;
     bp.source = bias_source(p);
     const int grid = bp.items < sm_count ? bp.items : sm_count;
-    { ProfileScope scope(RIB_KERNEL_BIAS_BWD, stream); rib_bias_bwd_kernel<<<grid, kThreads, smem_bytes(p.M), stream>>>(tm_q, tm_k, tm_v, tm_do, tm_dk, tm_dv, bp); }
+    { ProfileScope scope(RIB_KERNEL_BIAS_BWD, stream); kernel<<<grid, kThreads, smem_bytes(p.M), stream>>>(tm_q, tm_k, tm_v, tm_do, tm_dk, tm_dv, bp); }
     if (cudaError_t e = cudaGetLastError()) return e;
     const BiasScatter scatter = bias_scatter_args(p, grad, true);
     const unsigned dq_blocks = (unsigned)((tokens + 127) / 128), all = dq_blocks + (unsigned)(((size_t)p.heads * scatter.side * scatter.side + 255) / 256);
