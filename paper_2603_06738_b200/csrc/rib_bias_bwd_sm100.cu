@@ -6,11 +6,13 @@
 // CTA keeps K_J and V_J in shared memory and dV_J, dK_J in tensor memory, and walks the query tiles I of the window.  The pipeline, its roles and
 // its barriers are those of the rank-r backward kernel (rib_bwd_sm100.cu, rank 16), everything transposed (keys on the TMEM lanes), the unit
 // a half-tile u = 2 I + h of the 64 queries of one patch:
-//     S^T  = K_J Q_u^T,   dP^T = V_J dO_u^T                                                      (M128 N64 K32)
-//     P^T  = exp2(S^T * log2(e) / sqrt(d) + b(key - query) - lse_i * log2(e)),   dS^T = P^T o (dP^T - D_i)     (arithmetic warps)
+//     S^T  = K_J Q_u^T - lse_i sqrt(d),   dP^T = V_J dO_u^T - D_i                                (M128 N64 K32 + 16)
+//     P^T  = exp2(S^T * log2(e) / sqrt(d) + b(key - query)),   dS^T = P^T o dP^T                 (arithmetic warps)
 //     dV_J += P^T dO_u,   dK_J += dS^T Q_u                                                       (A from TMEM, N = 32)
 // and once per tile  dQ_I = dS K_J  (A = dS in shared memory, N = 32), added (fp32 red) into a workspace [pair][group of 4 columns][token][4].
 //
+// lse and D of the queries enter through the contractions: their negatives as three bf16 parts (24 bits) against columns of ones, one step of 16 more in
+// each, so that a score costs one multiply-add, one exponential, one product and one conversion (REFPARTS).
 // Biases: an arithmetic warp has 4 x 8 keys and 4 x 8 queries of a unit, a thread 4 rows of one key column and 2 neighbouring query columns of 4
 // rows: 7 pairs of the table in shared memory serve its 32 scores (rib_bias_sm100.cuh).
 //
@@ -25,7 +27,7 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kQStages = 3;           // ring of query-side tiles (Q, dO, lse/D)
+constexpr int kQStages = 3;           // ring of query-side tiles (Q, dO, rows of lse and D)
 constexpr int kThreads = 896;
 constexpr int kArithmeticThreads = 512;
 
@@ -33,9 +35,9 @@ constexpr int kArithmeticThreads = 512;
 constexpr uint32_t kOffK = 0;                                    // [2] (one slot per item in flight)
 constexpr uint32_t kOffV = kOffK + 2 * kContentBytes;            // [2]
 constexpr uint32_t kOffRing = kOffV + 2 * kContentBytes;
-constexpr uint32_t kLdPatch = 64 * 8, kLdBytes = 2 * kLdPatch;   // per patch 32 query pairs x (-lse2, -lse2', -D, -D')
+constexpr uint32_t kLdPatch = 64 * 16, kLdBytes = 2 * kLdPatch;  // per query 8 bf16: -lse sqrt(d) and -D in three parts each, 0, 0
 constexpr uint32_t kRingQ = 0, kRingDO = kContentBytes, kRingLD = kRingDO + kContentBytes;
-constexpr uint32_t kRingBytes = kRingLD + kLdBytes;              // 17408
+constexpr uint32_t kRingBytes = kRingLD + kLdBytes;              // 18432
 constexpr uint32_t kOffDS = kOffRing + kQStages * kRingBytes;    // dS: [2 tiles][2 halves of 64 queries][128 keys][128 B], SWIZZLE_128B
 constexpr uint32_t kDSHalf = kTile * 128;
 constexpr uint32_t kOffDK = kOffDS + 4 * kDSHalf;                // dK rows of an item on their way out (dV rows leave through V's slot)
@@ -46,8 +48,14 @@ constexpr uint32_t kOffBar = kOffDK + kContentBytes;
 enum Bar { kKVFull = 0, kKVEmpty = 2, kQFull = 4, kQEmpty = kQFull + kQStages, kSFull = kQEmpty + kQStages, kPReady = kSFull + 4, kPFree = kPReady + 4,
            kDSFree = kPFree + 4, kDQFull = kDSFree + 2, kDQFree, kAccFull, kAccFree, kTabDone, kTabReady, kDrain, kNumBars = kDrain + 3 };
 constexpr uint32_t kOffMisc = kOffBar + kNumBars * 8;
-constexpr uint32_t kOffZero = (kOffMisc + 16 + 127) & ~127u;     // zeros: four groups of lines 256 bytes apart, read in place of rows that do not count
+constexpr uint32_t kOffMasked = kOffMisc + 16;                   // biases of a key that is none
+// [S, dP] rows of 8 bf16 for all keys: 1 for the parts of -lse sqrt(d) (S) or of -D (dP).  The rows are alike, so the groups of 8 that an MMA reads
+// begin one row behind each other.
+constexpr uint32_t kOnesBytes = (kTile / 8 + 8) * 16;
+constexpr uint32_t kOffOnes = (kOffMasked + 16 + 127) & ~127u;
+constexpr uint32_t kOffZero = kOffOnes + 2 * kOnesBytes;         // zeros: columns 8 .. 15 of the queries' parts, and rows of dS that do not count
 constexpr uint32_t kOffLists = kOffZero + 1024;                  // PatchLists
+static_assert(kOffZero % 128 == 0, "lines of 128 bytes");
 constexpr uint32_t kOffTable = kOffLists + sizeof(PatchLists);   // [(2M-1)^2] fp32
 constexpr uint32_t smem_bytes(int M) { return kOffTable + 4u * (2 * M - 1) * (2 * M - 1) + 1024; }
 static_assert(smem_bytes(kBiasMaxWindow) <= 232448, "shared memory of one CTA");
@@ -65,7 +73,7 @@ constexpr uint32_t kIdescT = idesc_bf16_f32(kTile, kD, true);                 //
 constexpr uint32_t kIdescQ = idesc_bf16_f32_ab(kTile, kD, true, true);        // A and B MN-major
 
 struct Params {
-    const float2* ld;          // [pairs][n / 2], patches of the window in rows: per query pair (-lse2, -lse2', -D, -D') as two float2; then one patch of no queries
+    const uint4* ld;           // [pairs][n], patches of the window in rows: per query the parts of -lse sqrt(d) and -D; then one patch of no queries
     float* dq_acc;             // [pairs][32 / 4][n][4] fp32, zeroed by the preparation kernel
     float* blocks;             // BiasGrad::blocks
     int* status;
@@ -97,13 +105,6 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ float4 lds_f32x4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-    return v;
 }
 
 __device__ __forceinline__ void red_add_f32x2(float* addr, float a, float b)
@@ -157,7 +158,13 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
     PatchLists* const lists = reinterpret_cast<PatchLists*>(base_ptr + kOffLists);
     fill_patch_lists(p.g, p.M, lists, threadIdx.x, kThreads);
-    if (threadIdx.x < 64) reinterpret_cast<uint4*>(base_ptr + kOffZero)[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+    if (threadIdx.x < (2 * kOnesBytes + 1024) / 16) {
+        constexpr uint32_t kTwo = 0x3F803F80u, kFirst = 0x00003F80u, kSecond = 0x3F800000u;
+        const uint32_t at = threadIdx.x * 16;
+        reinterpret_cast<uint4*>(base_ptr + kOffOnes)[threadIdx.x] = at < kOnesBytes ? make_uint4(kTwo, kFirst, 0u, 0u) : at < 2 * kOnesBytes ? make_uint4(0u, kSecond, kTwo, 0u) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (threadIdx.x < 4) reinterpret_cast<float*>(base_ptr + kOffMasked)[threadIdx.x] = kTableMasked;
+    fence_proxy_async();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -223,6 +230,8 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (warp == 1) {
                 // ---- S^T, dP^T of unit u as soon as dV and dK of unit u - 3 have consumed P^T, dS^T, which lie in the same columns
                 if (!wait_all(bar(kKVFull + slot), (nitem >> 1) & 1)) { ok = false; break; }
+                // (columns 8 .. 15 of the ones: the same rows again, against zeros)
+                const uint64_t ones_s = smem_desc(base + kOffOnes, 16, 16, kSwizzleNone), ones_dp = smem_desc(base + kOffOnes + kOnesBytes, 16, 16, kSwizzleNone);
                 const uint64_t k = smem_desc_at(kDesc64, base + kOffK + slot * kContentBytes), v = smem_desc_at(kDesc64, base + kOffV + slot * kContentBytes);
                 for (int t = 0; t < tiles && ok; ++t, ++g) {
                     const uint32_t st = g % kQStages;
@@ -238,8 +247,13 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                             const uint32_t d_s = tmem + kStep * buf;
                             mma_ss(d_s, k, q, kIdescSS, 0u);
                             mma_ss(d_s, k + 2, q + 2, kIdescSS, 1u);     // + 32 bytes: second K16 step
+                            // - lse sqrt(d) of the query, and - D: three bf16 parts of each against ones
+                            const uint32_t rows = st * kRingBytes + kOffRing + kRingLD + h * kLdPatch;
+                            const uint64_t parts = smem_desc(base + rows, kOffZero - rows, 128, kSwizzleNone);
+                            mma_ss(d_s, ones_s, parts, kIdescSS, 1u);
                             mma_ss(d_s + kColDP, v, go, kIdescSS, 0u);
                             mma_ss(d_s + kColDP, v + 2, go + 2, kIdescSS, 1u);
+                            mma_ss(d_s + kColDP, ones_dp, parts, kIdescSS, 1u);
                             mma_commit(on_unit(kSFull, u));
                         }
                         __syncwarp();
@@ -308,7 +322,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const int quarter = warp & 3;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
-        const uint32_t pitch = 4u * side, table_addr = base + kOffTable;
+        const uint32_t table_addr = base + kOffTable;
         uint32_t g = 0, buf = h, ntable = 0;
         int table_head = -1;
         bool ok = true;
@@ -334,25 +348,25 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             // keys of the patch beyond the map's edge get probability 0: a thread's whole column, or the rows from `rows_there` on
             const bool column_there = X0 + xk < p.W;
             const int rows_there = p.H - Y0 - key_row0;          // of the thread's four
-            const uint32_t k_addr = table_addr + (ky + key_row0 - 4 * cg + p.M - 1) * pitch + 4 * (kx + xk + p.M - 1 - 2 * (lane & 3));
+            // (a key that is none, in a whole patch or a column beyond the edge, finds the same two words for every query)
+            const bool there = key_exists && column_there;
+            const uint32_t pitch = there ? 4u * side : 0u, moves = there ? 0xffffu : 0u;
+            const uint32_t k_addr = there ? table_addr + (ky + key_row0 - 4 * cg + p.M - 1) * pitch + 4 * (kx + xk + p.M - 1 - 2 * (lane & 3)) : base + kOffMasked + 4;
             const uint16_t* const entries = lists->entry + list_of(c) + h;
             const int tiles = (c.patches + 1) >> 1;
             for (int I = 0; I < tiles; ++I, ++g) {
-                const uint32_t st = g % kQStages;
                 const uint32_t t_s = tmem + lane_base + 32 * cg + kStep * buf, t_dp = t_s + kColDP;
                 buf = buffer_after(buf, 2);
-                const uint32_t b_addr = k_addr - entries[2 * I];
+                const uint32_t b_addr = k_addr - (entries[2 * I] & moves);
                 // biases of key row a against query row b of the warp's rows, a - b = k (the queries' columns go up, so the offsets go down)
                 auto bias = [&](int k) { return make_float2(lds_f32(b_addr + k * (int)pitch), lds_f32(b_addr + k * (int)pitch - 4)); };
                 float2 bb[3] = {bias(1), bias(2), bias(3)};
                 // warp-uniform outcome: the TMEM accesses below are warp-collective
-                if (!mbar_wait_warp(on_unit(kSFull, 2 * g + h), unit_parity(2 * g), abort_flag, p.status) ||
-                    !mbar_wait_warp(bar(kQFull + st), (g / kQStages) & 1, abort_flag, p.status)) { ok = false; break; }
+                if (!mbar_wait_warp(on_unit(kSFull, 2 * g + h), unit_parity(2 * g), abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
                 // Four pieces of 16 keys x 16 queries, read as 16-lane fragments: piece (o, G) has lanes 16 o .. and queries 16 G .., a thread of it 2 key rows of
                 // 2 x 2 queries.  For each G first o = 1, then o = 0: their differences of rows a - b are 1 2 3 and -1 0 1, less 2 G, so that the
                 // biases of the second piece are those of the next G's first one as well.
-                const uint32_t ld = base + kOffRing + st * kRingBytes + kRingLD + (32 * h + 16 * cg + (lane & 3)) * 16;
                 // dS tile: row = key, 128-byte line = the unit's 64 queries, 16-byte chunks swizzled by the row
                 const uint32_t ds_at = base + kOffDS + ((g & 1) * 2 + h) * kDSHalf + (quarter * 32 + 8 * ((lane >> 3) & 1) + (lane & 7)) * 128 + (((cg * 4 + (lane >> 4)) ^ (lane & 7)) << 4);
                 auto load = [&](int o, int G, uint32_t (&s)[8], uint32_t (&dp)[8]) {
@@ -361,17 +375,16 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     tmem_ld_16x256b_x2(t_dp + at, dp);
                 };
                 // bb[i]: a - b = that of equal fragment rows (gq == rr) + i - 1
-                auto work = [&](int o, const uint32_t (&s)[8], const uint32_t (&dp)[8], const float4 (&t)[2], const float2 (&bb)[3], uint32_t (&pp)[4], uint32_t (&dd)[4]) {
+                auto work = [&](int o, const uint32_t (&s)[8], const uint32_t (&dp)[8], const float2 (&bb)[3], uint32_t (&pp)[4], uint32_t (&dd)[4]) {
 #pragma unroll
                     for (int gq = 0; gq < 2; ++gq)
 #pragma unroll
                         for (int rr = 0; rr < 2; ++rr) {                  // key rows 2 o + rr of the warp's, query rows 2 G + gq
                             const int i = 4 * gq + 2 * rr;
-                            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2,
-                                                        __fadd2_rn(make_float2(t[gq].x, t[gq].y), bb[1 + rr - gq]));
+                            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2, bb[1 + rr - gq]);
                             float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                            if (kCut && (!column_there || 2 * o + rr >= rows_there)) e = make_float2(0.f, 0.f);
-                            const float2 d = __fmul2_rn(e, __fadd2_rn(make_float2(__uint_as_float(dp[i]), __uint_as_float(dp[i + 1])), make_float2(t[gq].z, t[gq].w)));
+                            if (kCut && 2 * o + rr >= rows_there) e = make_float2(0.f, 0.f);
+                            const float2 d = __fmul2_rn(e, make_float2(__uint_as_float(dp[i]), __uint_as_float(dp[i + 1])));
                             pp[2 * gq + rr] = pack_bf16x2(e.x, e.y);
                             dd[2 * gq + rr] = pack_bf16x2(d.x, d.y);
                         }
@@ -392,18 +405,15 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 // A piece is stored while the next but one is on its way, over scores that this warp has read.
 #pragma unroll 1
                 for (int G = 0; G < 2; ++G) {
-                    const float4 t[2] = {lds_f32x4(ld + 128 * G), lds_f32x4(ld + 128 * G + 64)};      // queries 16 G + 8 gq + 2 (lane % 4), + 1
                     tmem_wait_ld();
-                    work(1, s1, dp1, t, bb, pp, dd);
-                    if (!key_exists) pp[0] = pp[1] = pp[2] = pp[3] = dd[0] = dd[1] = dd[2] = dd[3] = 0u;
+                    work(1, s1, dp1, bb, pp, dd);
                     if (G == 0) {
                         if (!__all_sync(0xffffffffu, ds_free) && !mbar_wait_warp(b_ds, ds_parity, abort_flag, p.status)) { ok = false; break; }
                         load(1, 1, s1, dp1);
                     }
                     store(1, G, pp, dd);
                     bb[2] = bb[0]; bb[0] = bias(-1 - 2 * G); bb[1] = bias(-2 * G);
-                    work(0, s0, dp0, t, bb, pp, dd);
-                    if (!key_exists) pp[0] = pp[1] = pp[2] = pp[3] = dd[0] = dd[1] = dd[2] = dd[3] = 0u;
+                    work(0, s0, dp0, bb, pp, dd);
                     if (G == 0) load(0, 1, s0, dp0);
                     store(0, G, pp, dd);
                 }
@@ -580,14 +590,25 @@ struct AuxParams {
     const __nv_bfloat16* out;
     const __nv_bfloat16* dout;
     const float* lse;
-    float2* ld;
+    uint4* ld;
     float* dq_acc;
     double* sums;                // BiasGrad, cleared here
     size_t sum_words;
     __nv_bfloat16* dq;
     int H, W, heads, M, s, n, nWy, nWx, pairs, d, Hp, Wp;
-    float inv_sqrt_d;
+    float inv_sqrt_d, sqrt_d;
 };
+
+// x as the sum of three bf16: exact to 2^-24
+__device__ __forceinline__ void three_parts(float x, uint32_t (&part)[3])
+{
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const __nv_bfloat16 b = __float2bfloat16_rn(x);
+        part[i] = __bfloat16_as_ushort(b);
+        x -= __bfloat162float(b);
+    }
+}
 
 // Returns false for a window position beyond the image: no token there.
 __device__ __forceinline__ bool decode_pair_token(const AuxParams& p, int pair, int w, size_t& tok, size_t& scalar)
@@ -604,8 +625,8 @@ __device__ __forceinline__ bool decode_pair_token(const AuxParams& p, int pair, 
 }
 
 // Four lanes per (pair, token in window order), 8 channels each: D = dO . O and lse in the layout the main kernel streams; the dQ accumulators and
-// the sums of the bias gradient are cleared as flat arrays.  A query that is no token, or whose row has no key (lse = -inf), reads -inf for -lse:
-// probability 0.
+// the sums of the bias gradient are cleared as flat arrays.  A query that is no token, or whose row has no key (lse = -inf), has a score far below
+// all others: probability 0.
 __global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxParams p)
 {
     const size_t total = (size_t)p.pairs * p.n;
@@ -613,7 +634,8 @@ __global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxPara
     const int part = (int)(thread & 3);
     const size_t nthreads = (size_t)gridDim.x * blockDim.x;
     for (size_t e = thread; e < p.sum_words; e += nthreads) p.sums[e] = 0.0;
-    if (thread < 32) reinterpret_cast<float4*>(p.ld + total)[thread] = make_float4(-INFINITY, -INFINITY, 0.f, 0.f);      // the patch of no queries
+    constexpr uint32_t kNone = 0xF149u;                    // -1e30 in bf16
+    if (thread < 64) p.ld[total + thread] = make_uint4(kNone, 0u, 0u, 0u);       // the patch of no queries
     if (t >= total) return;                                // (whole warps: total is a multiple of 64)
     const int pair = (int)(t / p.n), w = (int)(t % p.n);
     size_t tok, scalar;
@@ -638,10 +660,10 @@ __global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxPara
     acc += __shfl_xor_sync(0xffffffffu, acc, 1);
     acc += __shfl_xor_sync(0xffffffffu, acc, 2);
     if (part == 0) {
-        float* ldf = reinterpret_cast<float*>(p.ld) + ((t >> 1) << 2) + (t & 1);
-        const bool none = lse == -INFINITY;
-        ldf[0] = none ? -INFINITY : -lse * kLog2e;
-        ldf[2] = none ? 0.f : -acc;
+        uint32_t l[3], d[3];
+        three_parts(-lse * p.sqrt_d, l);
+        three_parts(-acc, d);
+        p.ld[t] = lse == -INFINITY ? make_uint4(kNone, 0u, 0u, 0u) : make_uint4(l[0] | l[1] << 16, l[2] | d[0] << 16, d[1] | d[2] << 16, 0u);
     }
 }
 
@@ -674,7 +696,7 @@ __global__ void __launch_bounds__(256) rib_bias_bwd_finish_kernel(const AuxParam
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-size_t ld_bytes(long long pairs, int n) { return align256(((size_t)pairs * n + 64) * sizeof(float2)); }
+size_t ld_bytes(long long pairs, int n) { return align256(((size_t)pairs * n + 64) * sizeof(uint4)); }
 
 }  // namespace
 
@@ -690,7 +712,7 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
 {
     if (!encode_fn()) return cudaErrorNotSupported;
     uint8_t* ws = static_cast<uint8_t*>(p.workspace);
-    float2* ld = reinterpret_cast<float2*>(ws);
+    uint4* ld = reinterpret_cast<uint4*>(ws);
     float* dq_acc = reinterpret_cast<float*>(ws + ld_bytes(p.pairs, p.n));
     CUtensorMap tm_q, tm_k, tm_v, tm_do, tm_dk, tm_dv;
     if (!encode_image_map(&tm_q, p.q, p) || !encode_image_map(&tm_k, p.k, p) || !encode_image_map(&tm_v, p.v, p) || !encode_image_map(&tm_do, p.dout, p) ||
@@ -708,7 +730,8 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     ap.sums = grad.offsets; ap.sum_words = grad.bytes / sizeof(double);
     ap.H = p.H; ap.W = p.W; ap.heads = p.heads; ap.M = p.M; ap.s = p.s; ap.n = p.n; ap.nWy = p.nWy; ap.nWx = p.nWx;
     ap.pairs = p.pairs; ap.d = p.d; ap.Hp = p.Hp; ap.Wp = p.Wp;
-    ap.inv_sqrt_d = 1.f / sqrtf((float)p.d);
+    ap.sqrt_d = sqrtf((float)p.d);
+    ap.inv_sqrt_d = 1.f / ap.sqrt_d;
     const size_t tokens = (size_t)p.pairs * p.n;
     { ProfileScope scope(RIB_KERNEL_BIAS_BWD_PREPARE, stream); rib_bias_bwd_prepare_kernel<<<(unsigned)((tokens + 63) / 64), 256, 0, stream>>>(ap); }
     if (cudaError_t e = cudaGetLastError()) return e;
