@@ -16,11 +16,23 @@ constexpr int kStagedRows = 64;
 
 // Quotients decide codes, so they are those of the IEEE division; but x * (1 / scale) is off by less than 127 x 2^-22 = 3e-5, and unless it lies that
 // near to a border between two codes it names the same one.  (A scale below 2^-126 has no reciprocal: the test fails for infinities and NaN.)
-__device__ __forceinline__ int code_of(float x, float scale, float inverse)
+// The nearest whole number n is read off the low bits of t + 1.5 x 2^23 (half to even, as round() does): conversions between floating and whole
+// numbers have an eighth of the rate of additions, and were what these kernels waited for.  Returns a word with the code in its low byte.
+__device__ __forceinline__ uint32_t code_of(float x, float scale, float inverse)
 {
-    const float t = x * inverse, n = rintf(t);
-    if (!(fabsf(t - n) < 0.4999f)) return __float2int_rn(__fdiv_rn(x, scale));
-    return (int)n;
+    const float t = x * inverse, shifted = t + 12582912.f, n = shifted - 12582912.f;
+    if (!(fabsf(t - n) < 0.4999f)) return (uint32_t)__float2int_rn(__fdiv_rn(x, scale));
+    return __float_as_uint(shifted);
+}
+// the low bytes of four words
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+// byte `at` of four codes as a float: 0x4B000000 + (code + 128) is 2^23 + 128 + code
+__device__ __forceinline__ float code_value(uint32_t codes_plus_128, int at)
+{
+    return __uint_as_float(__byte_perm(codes_plus_128, 0x4B000000u, 0x7440 + at)) - 8388736.f;
 }
 
 struct RowScale { float scale, inverse; bool zero; };
@@ -61,10 +73,9 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_store_kernel(const __
         uint32_t c[2] = {0u, 0u};
         if (!s.zero) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int lo = code_of(__uint_as_float(w[i] << 16), s.scale, s.inverse), hi = code_of(__uint_as_float(w[i] & 0xffff0000u), s.scale, s.inverse);
-                c[i >> 1] |= ((uint32_t)(lo & 255) | (uint32_t)(hi & 255) << 8) << (16 * (i & 1));
-            }
+            for (int i = 0; i < 2; ++i)
+                c[i] = low_bytes(code_of(__uint_as_float(w[2 * i] << 16), s.scale, s.inverse), code_of(__uint_as_float(w[2 * i] & 0xffff0000u), s.scale, s.inverse),
+                                 code_of(__uint_as_float(w[2 * i + 1] << 16), s.scale, s.inverse), code_of(__uint_as_float(w[2 * i + 1] & 0xffff0000u), s.scale, s.inverse));
         }
         if (row < rows) {
             if (mine) *reinterpret_cast<uint2*>(codes + row * d + 8 * part) = make_uint2(c[0], c[1]);
@@ -115,9 +126,9 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_store_staged_kernel(c
 
 struct RestoreArgs { CheckpointRows t[4]; };
 
-__device__ __forceinline__ uint32_t restored_pair(uint32_t codes, int at, float scale)       // codes at, at + 1 (bytes of the word) as bf16
+__device__ __forceinline__ uint32_t restored_pair(uint32_t codes, int at, float scale)       // codes at, at + 1 (bytes of the word, 128 added) as bf16
 {
-    const float lo = (float)(int8_t)(codes >> (8 * at)) * scale, hi = (float)(int8_t)(codes >> (8 * at + 8)) * scale;
+    const float lo = code_value(codes, at) * scale, hi = code_value(codes, at + 1) * scale;
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
@@ -136,6 +147,7 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_restore_kernel(const 
     for (int k = 0; k < kUnroll; ++k) {
         const long long row = row0 + k * kRowsAtOnce;
         c[k] = row < rows ? __ldg(reinterpret_cast<const uint2*>(t.codes + row * d + 8 * part)) : make_uint2(0u, 0u);
+        c[k].x ^= 0x80808080u; c[k].y ^= 0x80808080u;
         scale[k] = row < rows ? __ldg(t.scales + row) : 0.f;
     }
 #pragma unroll

@@ -94,16 +94,13 @@ __device__ inline void stage_concat(const Problem& p, const PairCoord& c, const 
                                     const __nv_bfloat16* pos, float sx, float sp, int row0,
                                     int rows, int ld, float* dst)
 {
-    const int dk = p.d + p.r;
-    for (int idx = threadIdx.x; idx < rows * dk; idx += kThreads) {
-        const int rr = idx / dk, col = idx - rr * dk;
+    const int dk = p.d + p.r, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int rr = warp; rr < rows; rr += kWarps) {          // (a row's place is worked out once)
         const int i = row0 + rr;
-        float val = 0.f;
-        if (i < p.n && token_exists(p, c, i)) {
-            val = col < p.d ? __bfloat162float(x[token_offset(p, c, i) + col]) * sx
-                            : __bfloat162float(pos[(size_t)c.h * p.pos_head_stride + (size_t)i * p.r + (col - p.d)]) * sp;
-        }
-        dst[rr * ld + col] = val;
+        const bool real = i < p.n && token_exists(p, c, i);
+        const size_t off = real ? token_offset(p, c, i) : 0, row = (size_t)c.h * p.pos_head_stride + (size_t)i * p.r;
+        for (int col = lane; col < dk; col += 32)
+            dst[rr * ld + col] = !real ? 0.f : col < p.d ? __bfloat162float(x[off + col]) * sx : __bfloat162float(pos[row + (col - p.d)]) * sp;
     }
 }
 
@@ -111,10 +108,12 @@ __device__ inline void stage_concat(const Problem& p, const PairCoord& c, const 
 __device__ inline void stage_plain(const Problem& p, const PairCoord& c, const __nv_bfloat16* x,
                                    int row0, int rows, int ld, float* dst)
 {
-    for (int idx = threadIdx.x; idx < rows * p.d; idx += kThreads) {
-        const int rr = idx / p.d, col = idx - rr * p.d;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int rr = warp; rr < rows; rr += kWarps) {
         const int i = row0 + rr;
-        dst[rr * ld + col] = i < p.n && token_exists(p, c, i) ? __bfloat162float(x[token_offset(p, c, i) + col]) : 0.f;
+        const bool real = i < p.n && token_exists(p, c, i);
+        const size_t off = real ? token_offset(p, c, i) : 0;
+        for (int col = lane; col < p.d; col += 32) dst[rr * ld + col] = real ? __bfloat162float(x[off + col]) : 0.f;
     }
 }
 
