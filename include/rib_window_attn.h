@@ -457,7 +457,8 @@ enum { RIB_KERNEL_FWD_MAIN = 1, RIB_KERNEL_BWD_PREPARE = 2, RIB_KERNEL_BWD_MAIN 
     RIB_KERNEL_FWD_FRAME = 17, RIB_KERNEL_WINDOW8_FWD = 18, RIB_KERNEL_WINDOW8_CLEAR = 19, RIB_KERNEL_WINDOW8_BWD = 20,
     RIB_KERNEL_WINDOW16_FWD = 21, RIB_KERNEL_WINDOW16_CLEAR = 22, RIB_KERNEL_WINDOW16_BWD = 23, RIB_KERNEL_GENERATOR_CLEAR = 24,
     RIB_KERNEL_BIAS_FINISH = 25, RIB_KERNEL_CHECKPOINT_STORE = 26, RIB_KERNEL_CHECKPOINT_RESTORE = 27, RIB_KERNEL_BIAS_FWD = 28,
-    RIB_KERNEL_BIAS_BWD_PREPARE = 29, RIB_KERNEL_BIAS_BWD = 30, RIB_KERNEL_BIAS_BWD_FINISH = 31 };
+    RIB_KERNEL_BIAS_BWD_PREPARE = 29, RIB_KERNEL_BIAS_BWD = 30, RIB_KERNEL_BIAS_BWD_FINISH = 31,
+    RIB_KERNEL_BIAS_SMALL_FWD = 32, RIB_KERNEL_BIAS_SMALL_BWD = 33 };
 int rib_profile_begin(int max_launches);
 int rib_profile_end(int* kernel_ids, float* ms, int capacity);
 

@@ -70,7 +70,8 @@ KERNEL_NAMES = {1: "rib_fwd_sm100_kernel", 2: "rib_bwd_prepare_kernel", 3: "rib_
                 17: "rib_fwd_frame_sm100_kernel", 18: "rib_window8_fwd_kernel", 19: "rib_window8_clear_kernel", 20: "rib_window8_bwd_kernel",
                 21: "rib_window16_fwd_kernel", 22: "rib_window16_clear_kernel", 23: "rib_window16_bwd_kernel", 24: "rib_generator_clear_kernel",
                 25: "rib_bias_scatter_kernel, rib_bias_convert_kernel", 26: "rib_checkpoint_store_kernel", 27: "rib_checkpoint_restore_kernel", 28: "rib_bias_fwd_kernel",
-                29: "rib_bias_bwd_prepare_kernel", 30: "rib_bias_bwd_kernel", 31: "rib_bias_bwd_finish_kernel"}
+                29: "rib_bias_bwd_prepare_kernel", 30: "rib_bias_bwd_kernel", 31: "rib_bias_bwd_finish_kernel",
+                32: "rib_bias_small_fwd_kernel", 33: "rib_bias_small_bwd_kernel"}
 RIB_DTYPE_F32, RIB_DTYPE_BF16 = 0, 1
 RIB_NOALLOC_SCRATCH_BYTES = 32 << 20
 

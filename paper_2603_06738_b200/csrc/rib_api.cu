@@ -385,6 +385,8 @@ int fwd_impl(const void* q, const void* k, const void* v, const void* pq, const 
             launches = 1;
             e = rib::generic_fwd(p, st);
         }
+    } else if (forced != RIB_PATH_GENERIC && rib::bias_small_supported(p)) {
+        e = rib::bias_small_fwd(p, st);
     } else {
         e = rib::generic_fwd(p, st);
     }
@@ -531,17 +533,20 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
                                                       static_cast<unsigned char*>(workspace) + bucketed_attention_bytes(B, H, W, heads, window));
         const bool fast = g_forced_path.load() != RIB_PATH_GENERIC && rib::sm100_bias_bwd_supported(p);
         cudaError_t e;
+        int launches = fast ? 4 : 5;
         if (fast) {
             e = rib::sm100_bias_bwd(p, g, st);
         } else {
             e = rib::bias_grad_clear(g, st);
-            if (e == cudaSuccess) e = rib::generic_bwd(p, st, g.offsets);
+            const bool small = g_forced_path.load() != RIB_PATH_GENERIC && rib::bias_small_supported(p);
+            if (small) launches = 3;
+            if (e == cudaSuccess) e = small ? rib::bias_small_bwd(p, g.offsets, st) : rib::generic_bwd(p, st, g.offsets);
             if (e == cudaSuccess) e = rib::bias_grad_scatter(p, g, st);
             if (e == cudaSuccess) e = rib::bias_grad_convert(p, g, st);
         }
         if (e != cudaSuccess) return RIB_ERR_CUDA;
         t_last_path = fast ? RIB_PATH_SM100 : RIB_PATH_GENERIC;
-        g_kernel_launches += fast ? 4 : 5;
+        g_kernel_launches += launches;
         return RIB_OK;
     }
     const bool allowed = g_forced_path.load() != RIB_PATH_GENERIC;

@@ -119,6 +119,10 @@ __device__ inline void bias_scatter(const BiasScatter& s, size_t t)
 }
 cudaError_t bias_grad_scatter(const Problem& p, const BiasGrad& g, cudaStream_t stream);        // sums by offset -> tables
 cudaError_t bias_grad_convert(const Problem& p, const BiasGrad& g, cudaStream_t stream);        // tables -> dbias
+// Windows of up to 256 tokens outside the tcgen05 kernels' shapes (rib_bias_small.cu).
+bool bias_small_supported(const Problem& p);
+cudaError_t bias_small_fwd(const Problem& p, cudaStream_t stream);
+cudaError_t bias_small_bwd(const Problem& p, double* offset_sums, cudaStream_t stream);
 bool sm100_bias_fwd_supported(const Problem& p);
 cudaError_t sm100_bias_fwd(const Problem& p, cudaStream_t stream);
 bool sm100_bias_bwd_supported(const Problem& p);

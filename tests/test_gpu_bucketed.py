@@ -127,8 +127,8 @@ MAPS = {"log": log_map, "own": own_map, "reach": lambda M: reach_map(M, max(1, M
 @pytest.mark.parametrize("path", ["auto", "exact", "generic"])
 def test_every_element(case, path):
     B, H, W, heads, d, M, s, masked = case
-    if path != "auto" and not takes_tensor_cores(case):
-        pytest.skip("one form only")
+    if path == "exact" and not takes_tensor_cores(case):
+        pytest.skip("the exact softmax form is a form of the tcgen05 kernel")
     for seed, name in enumerate(MAPS):
         check(make(B, H, W, heads, d, M, MAPS[name](M), seed=seed), M, s, masked, path, takes_tensor_cores(case))
 
