@@ -8,10 +8,15 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__global__ void __launch_bounds__(kThreads) rib_bias_scatter_kernel(const BiasScatter s) { bias_scatter(s, (size_t)blockIdx.x * kThreads + threadIdx.x); }
+__global__ void __launch_bounds__(kThreads) rib_bias_scatter_kernel(const BiasScatter s) 
+{
+    cudaGridDependencySynchronize();
+    bias_scatter(s, (size_t)blockIdx.x * kThreads + threadIdx.x);
+}
 
 __global__ void __launch_bounds__(kThreads) rib_bias_convert_kernel(const double* tables, int num_buckets, size_t entries, void* dbias, int bf16, long long head_stride)
 {
+    cudaGridDependencySynchronize();              // (it may have overtaken the kernel that sums)
     const size_t e = (size_t)blockIdx.x * kThreads + threadIdx.x;
     if (e >= entries) return;
     const size_t to = (e / num_buckets) * (size_t)head_stride + e % num_buckets;
@@ -40,16 +45,16 @@ cudaError_t bias_grad_scatter(const Problem& p, const BiasGrad& g, cudaStream_t 
 {
     const BiasScatter s = bias_scatter_args(p, g, false);
     const size_t threads = (size_t)p.heads * s.side * s.side;
-    { ProfileScope scope(RIB_KERNEL_BIAS_FINISH, stream); rib_bias_scatter_kernel<<<(unsigned)((threads + kThreads - 1) / kThreads), kThreads, 0, stream>>>(s); }
-    return cudaGetLastError();
+    ProfileScope scope(RIB_KERNEL_BIAS_FINISH, stream);
+    return launch_overtaking(rib_bias_scatter_kernel, (int)((threads + kThreads - 1) / kThreads), kThreads, 0, stream, s);
 }
 
 cudaError_t bias_grad_convert(const Problem& p, const BiasGrad& g, cudaStream_t stream)
 {
     const size_t entries = (size_t)bias_tables(p) * p.num_buckets;
-    { ProfileScope scope(RIB_KERNEL_BIAS_FINISH, stream);
-      rib_bias_convert_kernel<<<(unsigned)((entries + kThreads - 1) / kThreads), kThreads, 0, stream>>>(g.tables, p.num_buckets, entries, p.dbias, p.bias_bf16, p.bias_head_stride); }
-    return cudaGetLastError();
+    ProfileScope scope(RIB_KERNEL_BIAS_FINISH, stream);
+    return launch_overtaking(rib_bias_convert_kernel, (int)((entries + kThreads - 1) / kThreads), kThreads, 0, stream, static_cast<const double*>(g.tables), p.num_buckets, entries,
+                             p.dbias, p.bias_bf16, p.bias_head_stride);
 }
 
 }  // namespace rib

@@ -169,6 +169,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    cudaGridDependencySynchronize();              // the preparation kernel, which this one may have overtaken: lse and D, cleared sums
 
     if (warp == 0) {
         // ============================================================ TMA producer (one thread)
@@ -671,6 +672,7 @@ __global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxPara
 // Blocks from dq_blocks on add up the gradient of the bias.
 __global__ void __launch_bounds__(256) rib_bias_bwd_finish_kernel(const AuxParams p, const BiasScatter scatter, unsigned dq_blocks)
 {
+    cudaGridDependencySynchronize();
     if (blockIdx.x >= dq_blocks) { bias_scatter(scatter, (size_t)(blockIdx.x - dq_blocks) * blockDim.x + threadIdx.x); return; }
     const size_t total = (size_t)p.pairs * p.n;
     const size_t thread = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
@@ -743,12 +745,17 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     bp.inv_sqrt_d = ap.inv_sqrt_d;
     bp.source = bias_source(p);
     const int grid = bp.items < sm_count ? bp.items : sm_count;
-    { ProfileScope scope(RIB_KERNEL_BIAS_BWD, stream); kernel<<<grid, kThreads, smem_bytes(p.M), stream>>>(tm_q, tm_k, tm_v, tm_do, tm_dk, tm_dv, bp); }
-    if (cudaError_t e = cudaGetLastError()) return e;
+    // (each of the kernels behind the first may start while the one before it ends: its set-up, or at least its launch, is then over)
+    {
+        ProfileScope scope(RIB_KERNEL_BIAS_BWD, stream);
+        if (cudaError_t e = launch_overtaking(kernel, grid, kThreads, smem_bytes(p.M), stream, tm_q, tm_k, tm_v, tm_do, tm_dk, tm_dv, bp)) return e;
+    }
     const BiasScatter scatter = bias_scatter_args(p, grad, true);
     const unsigned dq_blocks = (unsigned)((tokens + 127) / 128), all = dq_blocks + (unsigned)(((size_t)p.heads * scatter.side * scatter.side + 255) / 256);
-    { ProfileScope scope(RIB_KERNEL_BIAS_BWD_FINISH, stream); rib_bias_bwd_finish_kernel<<<all, 256, 0, stream>>>(ap, scatter, dq_blocks); }
-    if (cudaError_t e = cudaGetLastError()) return e;
+    {
+        ProfileScope scope(RIB_KERNEL_BIAS_BWD_FINISH, stream);
+        if (cudaError_t e = launch_overtaking(rib_bias_bwd_finish_kernel, (int)all, 256, 0, stream, ap, scatter, dq_blocks)) return e;
+    }
     return bias_grad_convert(p, grad, stream);
 }
 
