@@ -464,6 +464,23 @@ namespace {
 
 struct BwdBias : BiasArgs { void* gradient; };
 
+// A backward call from checkpoints: the four tensors come back as bf16 at the start of the workspace, what is behind them is the backward
+// pass's own.
+struct Restored {
+    rib::CheckpointRows t[4];
+    long long rows;
+    int d;
+    void* rest;
+    size_t rest_bytes;
+};
+
+int restore(const Restored& r, void* stream)
+{
+    if (rib::checkpoint_restore(r.t, 4, r.rows, r.d, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RIB_ERR_CUDA;
+    g_kernel_launches += 1;
+    return RIB_OK;
+}
+
 // Scratch of a backward pass with a bias: what the attention kernels need, then the sums of the table's gradient.
 size_t bucketed_attention_bytes(int B, int H, int W, int heads, int window)
 {
@@ -490,7 +507,7 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
                     int B, int H, int W, int heads, int d, int r, int window, int shift,
                     void* dq, void* dk, void* dv, float* dpq, float* dpk,
                     void* workspace, size_t workspace_bytes, void* stream, bool masked, bool validate_only = false,
-                    const BwdBias* bias = nullptr)
+                    const BwdBias* bias = nullptr, const Restored* saved = nullptr)
 {
     if (!q || !k || !v || !out || !lse || !dout || !dq || !dk || !dv) return RIB_ERR_NULL;
     if (r > 0 && (!pq || !pk || !dpq || !dpk)) return RIB_ERR_NULL;
@@ -532,6 +549,9 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
         const rib::BiasGrad g = rib::bias_grad_layout(heads, rib::bias_tables(p), window, bias->num_buckets,
                                                       static_cast<unsigned char*>(workspace) + bucketed_attention_bytes(B, H, W, heads, window));
         const bool fast = g_forced_path.load() != RIB_PATH_GENERIC && rib::sm100_bias_bwd_supported(p);
+        if (saved && fast) p.saved = saved->t;
+        else if (saved)
+            if (int rc = restore(*saved, stream)) return rc;
         cudaError_t e;
         int launches = fast ? 4 : 5;
         if (fast) {
@@ -551,6 +571,9 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
     }
     const bool allowed = g_forced_path.load() != RIB_PATH_GENERIC;
     bool fast = allowed && rib::sm100_bwd_supported(p);
+    if (saved && fast && rib::sm100_bwd_takes_saved(p)) p.saved = saved->t;
+    else if (saved)
+        if (int rc = restore(*saved, stream)) return rc;
     int launches = fast ? rib::sm100_bwd_launches(p) : 3;          // any-shape kernels: rowdot, dq, dk/dv
     cudaError_t e;
     if (fast) {
@@ -676,16 +699,6 @@ int check_checkpoint(const void* codes, const float* scales, long long rows, int
 
 size_t image_bytes(int B, int H, int W, int heads, int d) { return (2 * (size_t)B * H * W * heads * d + 255) & ~(size_t)255; }
 
-// A backward call from checkpoints: the four tensors come back as bf16 at the start of the workspace, what is behind them is the backward
-// pass's own.  Every check is made before the first launch (`validate_only` of the pass sees the addresses).
-struct Restored {
-    rib::CheckpointRows t[4];
-    long long rows;
-    int d;
-    void* rest;
-    size_t rest_bytes;
-};
-
 int plan_restore(const rib_checkpoint* saved, int B, int H, int W, int heads, int d, void* workspace, size_t workspace_bytes, Restored* r)
 {
     if (!saved) return RIB_ERR_NULL;
@@ -702,13 +715,6 @@ int plan_restore(const rib_checkpoint* saved, int B, int H, int W, int heads, in
         r->t[i] = {static_cast<const int8_t*>(saved[i].codes), saved[i].scales, reinterpret_cast<__nv_bfloat16*>(at)};
     r->rest = at;
     r->rest_bytes = workspace_bytes - 4 * image;
-    return RIB_OK;
-}
-
-int restore(const Restored& r, void* stream)
-{
-    if (rib::checkpoint_restore(r.t, 4, r.rows, r.d, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RIB_ERR_CUDA;
-    g_kernel_launches += 1;
     return RIB_OK;
 }
 
@@ -765,13 +771,8 @@ int rib_window_attn_bwd_checkpointed(const rib_checkpoint* saved, const void* pq
     if (masked && H > 0 && W > 0 && window > 0 && (H % window || W % window)) return RIB_ERR_SHAPE;
     Restored s;
     if (int rc = plan_restore(saved, B, H, W, heads, d, workspace, workspace_bytes, &s)) return rc;
-    auto pass = [&](bool validate_only) {
-        return bwd_impl(s.t[0].x, s.t[1].x, s.t[2].x, pq, pk, pos_head_stride, s.t[3].x, lse, dout, B, H, W, heads, d, r, window, shift, dq, dk, dv,
-                        dpq, dpk, s.rest, s.rest_bytes, stream, masked != 0, validate_only);
-    };
-    if (int rc = pass(true)) return rc;
-    if (int rc = restore(s, stream)) return rc;
-    return pass(false);
+    return bwd_impl(s.t[0].x, s.t[1].x, s.t[2].x, pq, pk, pos_head_stride, s.t[3].x, lse, dout, B, H, W, heads, d, r, window, shift, dq, dk, dv,
+                    dpq, dpk, s.rest, s.rest_bytes, stream, masked != 0, false, nullptr, &s);
 }
 
 size_t rib_window_attn_bwd_bucketed_checkpointed_workspace(long long bias_head_stride, int num_buckets, int B, int H, int W, int heads, int d, int window)
@@ -790,13 +791,8 @@ int rib_window_attn_bwd_bucketed_checkpointed(const rib_checkpoint* saved, const
     if (int rc = bwd_bias(bias, bias_dtype, bias_head_stride, buckets, num_buckets, dbias, &b)) return rc;
     Restored s;
     if (int rc = plan_restore(saved, B, H, W, heads, d, workspace, workspace_bytes, &s)) return rc;
-    auto pass = [&](bool validate_only) {
-        return bwd_impl(s.t[0].x, s.t[1].x, s.t[2].x, nullptr, nullptr, 0, s.t[3].x, lse, dout, B, H, W, heads, d, 0, window, shift, dq, dk, dv,
-                        nullptr, nullptr, s.rest, s.rest_bytes, stream, masked != 0, validate_only, &b);
-    };
-    if (int rc = pass(true)) return rc;
-    if (int rc = restore(s, stream)) return rc;
-    return pass(false);
+    return bwd_impl(s.t[0].x, s.t[1].x, s.t[2].x, nullptr, nullptr, 0, s.t[3].x, lse, dout, B, H, W, heads, d, 0, window, shift, dq, dk, dv,
+                    nullptr, nullptr, s.rest, s.rest_bytes, stream, masked != 0, false, &b, &s);
 }
 
 int rib_window_attn_bwd_noalloc(const void* q, const void* k, const void* v, const void* pq, const void* pk,

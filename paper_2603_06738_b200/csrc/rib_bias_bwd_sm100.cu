@@ -596,6 +596,7 @@ struct AuxParams {
     double* sums;                // BiasGrad, cleared here
     size_t sum_words;
     __nv_bfloat16* dq;
+    CheckpointRows saved[4];     // kSaved: q, k, v, out
     int H, W, heads, M, s, n, nWy, nWx, pairs, d, Hp, Wp;
     float inv_sqrt_d, sqrt_d;
 };
@@ -628,6 +629,8 @@ __device__ __forceinline__ bool decode_pair_token(const AuxParams& p, int pair, 
 // Four lanes per (pair, token in window order), 8 channels each: D = dO . O and lse in the layout the main kernel streams; the dQ accumulators and
 // the sums of the bias gradient are cleared as flat arrays.  A query that is no token, or whose row has no key (lse = -inf), has a score far below
 // all others: probability 0.
+// kSaved: q, k, v and out are checkpoints; the first three are restored to where the main kernel reads them.
+template <bool kSaved>
 __global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxParams p)
 {
     const size_t total = (size_t)p.pairs * p.n;
@@ -645,7 +648,20 @@ __global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxPara
     float lse = -INFINITY;
     if (real && 8 * part < p.d) {
         x = __ldg(reinterpret_cast<const uint4*>(p.dout + tok * p.d) + part);
-        y = __ldg(reinterpret_cast<const uint4*>(p.out + tok * p.d) + part);
+        if (kSaved) {
+            uint2 c[4];
+            float scale[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c[i] = __ldg(reinterpret_cast<const uint2*>(p.saved[i].codes + tok * p.d) + part);
+                scale[i] = __ldg(p.saved[i].scales + tok);
+            }
+#pragma unroll
+            for (int i = 0; i < 3; ++i) reinterpret_cast<uint4*>(p.saved[i].x + tok * p.d)[part] = restored_chunk(c[i], scale[i]);
+            y = restored_chunk(c[3], scale[3]);
+        } else {
+            y = __ldg(reinterpret_cast<const uint4*>(p.out + tok * p.d) + part);
+        }
         if (part == 0) lse = p.lse[scalar];
     }
     float4* z4 = reinterpret_cast<float4*>(p.dq_acc);      // pairs * 32 * n floats = total * 8 vectors
@@ -732,10 +748,11 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     ap.sums = grad.offsets; ap.sum_words = grad.bytes / sizeof(double);
     ap.H = p.H; ap.W = p.W; ap.heads = p.heads; ap.M = p.M; ap.s = p.s; ap.n = p.n; ap.nWy = p.nWy; ap.nWx = p.nWx;
     ap.pairs = p.pairs; ap.d = p.d; ap.Hp = p.Hp; ap.Wp = p.Wp;
+    if (p.saved) for (int i = 0; i < 4; ++i) ap.saved[i] = p.saved[i];
     ap.sqrt_d = sqrtf((float)p.d);
     ap.inv_sqrt_d = 1.f / ap.sqrt_d;
     const size_t tokens = (size_t)p.pairs * p.n;
-    { ProfileScope scope(RIB_KERNEL_BIAS_BWD_PREPARE, stream); rib_bias_bwd_prepare_kernel<<<(unsigned)((tokens + 63) / 64), 256, 0, stream>>>(ap); }
+    { ProfileScope scope(RIB_KERNEL_BIAS_BWD_PREPARE, stream); (p.saved ? rib_bias_bwd_prepare_kernel<true> : rib_bias_bwd_prepare_kernel<false>)<<<(unsigned)((tokens + 63) / 64), 256, 0, stream>>>(ap); }
     if (cudaError_t e = cudaGetLastError()) return e;
     bp.ld = ld; bp.dq_acc = dq_acc; bp.blocks = grad.blocks; bp.status = p.status;
     bp.no_queries = (long long)tokens;

@@ -605,6 +605,7 @@ struct AuxParams {
     __nv_bfloat16* dq;
     float* dpq;
     float* dpk;
+    CheckpointRows saved[4];     // kSaved: q, k, v, out
     int H, W, heads, M, s, n, nWy, nWx, pairs;
     int d, r;                    // head width and rank of the caller's tensors (the accumulators are 32 + R columns wide)
     int dq_sectors;              // 1: 16 channels of a row of dq are one 32-byte sector
@@ -634,7 +635,8 @@ __device__ __forceinline__ bool decode_pair_token(const AuxParams& p, int pair, 
 // streams; the dQ~ accumulators are cleared with 16-byte stores, (d + r) / 16 per lane, as one flat array;
 // the first threads also stage bf16(Pq sqrt(d/r)) and clear dPq, dPk.
 // kNarrow: the rows of out are p.narrow < d elements wide and aligned to 4 bytes only.
-template <int R, bool kNarrow>
+// kSaved: q, k, v and out are 8-bit checkpoints; the first three are restored to where the main kernel reads them.
+template <int R, bool kNarrow, bool kSaved = false>
 __global__ void __launch_bounds__(256) rib_bwd_prepare_kernel(const AuxParams p)
 {
     constexpr int kDk = kD + R;
@@ -671,6 +673,17 @@ __global__ void __launch_bounds__(256) rib_bwd_prepare_kernel(const AuxParams p)
             if (left > 2) y.y = __ldg(v + 1);
             if (left > 4) y.z = __ldg(v + 2);
             if (left > 6) y.w = __ldg(v + 3);
+        } else if (kSaved) {
+            uint2 c[4];
+            float scale[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c[i] = __ldg(reinterpret_cast<const uint2*>(p.saved[i].codes + tok * p.d) + part);
+                scale[i] = __ldg(p.saved[i].scales + tok);
+            }
+#pragma unroll
+            for (int i = 0; i < 3; ++i) reinterpret_cast<uint4*>(p.saved[i].x + tok * p.d)[part] = restored_chunk(c[i], scale[i]);
+            y = restored_chunk(c[3], scale[3]);
         } else {
             y = __ldg(reinterpret_cast<const uint4*>(p.out + tok * p.d) + part);
         }
@@ -872,9 +885,10 @@ cudaError_t launch_bwd(const Problem& p, cudaStream_t stream)
     ap.pos_scale = sqrtf(scale_width_d(p) / scale_width_r(p));
     ap.inv_sqrt_d = 1.f / sqrtf(scale_width_d(p));
     ap.inv_sqrt_r = 1.f / sqrtf(scale_width_r(p));
+    if (p.saved) for (int i = 0; i < 4; ++i) ap.saved[i] = p.saved[i];
     const size_t tokens = (size_t)p.pairs * p.n;
     const unsigned aux_blocks = (unsigned)((tokens + 63) / 64);
-    { ProfileScope scope(RIB_KERNEL_BWD_PREPARE, stream); (p.narrow ? rib_bwd_prepare_kernel<R, true> : rib_bwd_prepare_kernel<R, false>)<<<aux_blocks, 256, 0, stream>>>(ap); }
+    { ProfileScope scope(RIB_KERNEL_BWD_PREPARE, stream); (p.narrow ? rib_bwd_prepare_kernel<R, true> : p.saved ? rib_bwd_prepare_kernel<R, false, true> : rib_bwd_prepare_kernel<R, false>)<<<aux_blocks, 256, 0, stream>>>(ap); }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
 
@@ -910,6 +924,8 @@ cudaError_t launch_bwd(const Problem& p, cudaStream_t stream)
 }
 
 bool sm100_bwd_takes_narrow(const Problem& p) { return !sm100_window8(p) && !sm100_window16(p); }
+
+bool sm100_bwd_takes_saved(const Problem& p) { return sm100_bwd_supported(p) && sm100_bwd_takes_narrow(p); }
 
 int sm100_bwd_launches(const Problem& p) { return sm100_window8(p) ? 2 : 3; }      // clear, main; else two clears, main or prepare, main, finish
 

@@ -29,12 +29,6 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
 {
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
-// byte `at` of four codes as a float: 0x4B000000 + (code + 128) is 2^23 + 128 + code
-__device__ __forceinline__ float code_value(uint32_t codes_plus_128, int at)
-{
-    return __uint_as_float(__byte_perm(codes_plus_128, 0x4B000000u, 0x7440 + at)) - 8388736.f;
-}
-
 struct RowScale { float scale, inverse; bool zero; };
 __device__ __forceinline__ RowScale row_scale(float most, bool bad)
 {
@@ -126,13 +120,6 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_store_staged_kernel(c
 
 struct RestoreArgs { CheckpointRows t[4]; };
 
-__device__ __forceinline__ uint32_t restored_pair(uint32_t codes, int at, float scale)       // codes at, at + 1 (bytes of the word, 128 added) as bf16
-{
-    const float lo = code_value(codes, at) * scale, hi = code_value(codes, at + 1) * scale;
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-
 template <int kLanes>
 __global__ void __launch_bounds__(kThreads) rib_checkpoint_restore_kernel(const RestoreArgs args, long long rows, int d)
 {
@@ -147,15 +134,13 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_restore_kernel(const 
     for (int k = 0; k < kUnroll; ++k) {
         const long long row = row0 + k * kRowsAtOnce;
         c[k] = row < rows ? __ldg(reinterpret_cast<const uint2*>(t.codes + row * d + 8 * part)) : make_uint2(0u, 0u);
-        c[k].x ^= 0x80808080u; c[k].y ^= 0x80808080u;
         scale[k] = row < rows ? __ldg(t.scales + row) : 0.f;
     }
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
         const long long row = row0 + k * kRowsAtOnce;
         if (row < rows)
-            *reinterpret_cast<uint4*>(t.x + row * d + 8 * part) = make_uint4(restored_pair(c[k].x, 0, scale[k]), restored_pair(c[k].x, 2, scale[k]),
-                                                                             restored_pair(c[k].y, 0, scale[k]), restored_pair(c[k].y, 2, scale[k]));
+            *reinterpret_cast<uint4*>(t.x + row * d + 8 * part) = restored_chunk(c[k], scale[k]);
     }
 }
 

@@ -9,6 +9,9 @@
 
 namespace rib {
 
+// A tensor of rows kept in 8 bits (codes, a scale per row) and where its bf16 form goes.
+struct CheckpointRows { const int8_t* codes; const float* scales; __nv_bfloat16* x; };
+
 // One problem instance.  Image tensors are bf16 [B][H][W][heads][d]; pq/pk bf16 [n][r];
 // lse / rowdot fp32 [B][heads][H][W]; dpq/dpk fp32 [n][r].
 struct Problem {
@@ -48,6 +51,7 @@ struct Problem {
     const int* buckets;               // [2M-1][2M-1]: bucket of the offset (key - query); outside [0, num_buckets): not attended to
     int num_buckets;
     void* dbias;                      // gradient, layout and type of bias
+    const CheckpointRows* saved;      // backward: q, k, v, out as checkpoints, which the preparation kernel restores (q, k, v) and uses (out); null: not
     int narrow;                       // general tcgen05 backward on such copies: width of the rows of `out` and `dq`, which are the caller's; 0 = d
 };
 
@@ -131,8 +135,26 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
 
 // Rows of bf16 as whole numbers of 8 bits with a scale each, and back (rib_checkpoint.cu).
 cudaError_t checkpoint_store(const __nv_bfloat16* x, long long rows, int d, int8_t* codes, float* scales, cudaStream_t stream);
-struct CheckpointRows { const int8_t* codes; const float* scales; __nv_bfloat16* x; };
 cudaError_t checkpoint_restore(const CheckpointRows* tensors, int count, long long rows, int d, cudaStream_t stream);
+// byte `at` of four codes as a float: 0x4B000000 + (code + 128) is 2^23 + 128 + code
+__device__ __forceinline__ float code_value(uint32_t codes_plus_128, int at)
+{
+    return __uint_as_float(__byte_perm(codes_plus_128, 0x4B000000u, 0x7440 + at)) - 8388736.f;
+}
+
+__device__ __forceinline__ uint32_t restored_pair(uint32_t codes, int at, float scale)       // codes at, at + 1 (bytes of the word, 128 added) as bf16
+{
+    const float lo = code_value(codes, at) * scale, hi = code_value(codes, at + 1) * scale;
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// eight codes of a row as bf16
+__device__ __forceinline__ uint4 restored_chunk(uint2 codes, float scale)
+{
+    codes.x ^= 0x80808080u; codes.y ^= 0x80808080u;
+    return make_uint4(restored_pair(codes.x, 0, scale), restored_pair(codes.x, 2, scale), restored_pair(codes.y, 0, scale), restored_pair(codes.y, 2, scale));
+}
 
 bool sm100_fwd_supported(const Problem& p);
 cudaError_t sm100_fwd(const Problem& p, cudaStream_t stream);
@@ -144,6 +166,7 @@ size_t sm100_bwd_workspace_bytes(long long pairs, int n, int tables, int r);
 cudaError_t sm100_bwd(const Problem& p, cudaStream_t stream);
 int sm100_bwd_launches(const Problem& p);     // kernels it enqueues
 bool sm100_bwd_takes_narrow(const Problem& p);    // Problem::narrow may be set
+bool sm100_bwd_takes_saved(const Problem& p);     // Problem::saved may be set
 // Windows of 8 x 8 tokens (rib_window8_sm100.cu); the backward launches 2 kernels.
 bool sm100_window8(const Problem& p);
 cudaError_t sm100_window8_fwd(const Problem& p, cudaStream_t stream);
