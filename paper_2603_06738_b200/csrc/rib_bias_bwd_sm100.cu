@@ -86,11 +86,6 @@ struct Params {
     BiasItems g;
 };
 
-// `sp` counts the patches of the window that hold tokens; beyond the last one the last one stands in
-__device__ __forceinline__ void patch_origin(const Params& p, const LiveItem& c, int sp, int& py, int& px, int& Y0, int& X0)
-{
-    live_patch_origin(p.g.live, WindowGeom{p.Hp, p.Wp, p.M, p.s}, c, min(sp, c.patches - 1), py, px, Y0, X0);
-}
 __device__ __forceinline__ size_t pair_of(const Params& p, const LiveItem& c)
 {
     return (((size_t)c.b * p.nWy + c.wy) * p.nWx + c.wx) * p.heads + c.h;
@@ -134,6 +129,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int side = 2 * p.M - 1;
+    const WindowGeom geom{p.Hp, p.Wp, p.M, p.s};
     const long long work = p.g.work[9] * p.heads;
     const int first_item = first_bias_item(p.g, work * blockIdx.x / gridDim.x);
     const int last_item = min(first_bias_item(p.g, work * (blockIdx.x + 1) / gridDim.x), p.items);
@@ -177,14 +173,14 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             uint32_t nitem = 0, kv_armed = 0, q_armed = 0;
             bool ok = true;
             for (int item = first_item; item < last_item && ok; ++item, ++nitem) {
-                const LiveItem c = decode_bias_item(p.g, item);
+            const LiveItem c = decode_bias_item(p.g, item);
                 const uint32_t slot = nitem & 1;
                 if (nitem >= 2 && !mbar_wait(bar(kKVEmpty + slot), ((nitem >> 1) - 1) & 1, abort_flag, p.status)) { ok = false; break; }
                 mbar_arrive_expect_tx(bar(kKVFull + slot), 2 * kContentBytes);
                 ++kv_armed;
                 for (int sub = 0; sub < 2; ++sub) {
-                    int py, px, Y0, X0;
-                    patch_origin(p, c, 2 * c.tp + sub, py, px, Y0, X0);
+                    int Y0, X0;
+                    patch_place(geom, lists, c, 2 * c.tp + sub, Y0, X0);
                     if (2 * c.tp + sub >= c.patches) X0 = p.Wp;          // beyond the last patch lies nothing: zeros
                     tma_load_5d(base + kOffK + slot * kContentBytes + sub * kPatchContent, &tm_k, bar(kKVFull + slot), 0, c.h, X0, Y0, c.b);
                     tma_load_5d(base + kOffV + slot * kContentBytes + sub * kPatchContent, &tm_v, bar(kKVFull + slot), 0, c.h, X0, Y0, c.b);
@@ -197,13 +193,14 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     mbar_arrive_expect_tx(bar(kQFull + st), kRingBytes);
                     const uint32_t ring = base + kOffRing + st * kRingBytes;
                     for (int sub = 0; sub < 2; ++sub) {
-                        int py, px, Y0, X0;
-                        patch_origin(p, c, 2 * I + sub, py, px, Y0, X0);
+                        int Y0, X0;
+                        patch_place(geom, lists, c, 2 * I + sub, Y0, X0);
+                        const int from = lists->origin[list_of(c) + 2 * I + sub];
                         const bool none = 2 * I + sub >= c.patches;
                         if (none) X0 = p.Wp;
                         tma_load_5d(ring + kRingQ + sub * kPatchContent, &tm_q, bar(kQFull + st), 0, c.h, X0, Y0, c.b);
                         tma_load_5d(ring + kRingDO + sub * kPatchContent, &tm_do, bar(kQFull + st), 0, c.h, X0, Y0, c.b);
-                        const size_t at = none ? (size_t)p.no_queries : pair * p.n + 64 * (size_t)((py >> 3) * (p.M >> 3) + (px >> 3));
+                        const size_t at = none ? (size_t)p.no_queries : pair * p.n + 64 * (size_t)((from >> 11) * (p.M >> 3) + ((from & 255) >> 3));
                         bulk_load_1d(ring + kRingLD + sub * kLdPatch, p.ld + at, kLdPatch, bar(kQFull + st));
                     }
                 }
@@ -226,7 +223,8 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         bool ok = true;
         uint32_t g = 0, nitem = 0, buf = 0;
         for (int item = first_item; item < last_item && ok; ++item, ++nitem) {
-            const int tiles = (decode_bias_item(p.g, item).patches + 1) >> 1;
+            const LiveItem c = decode_bias_item(p.g, item);
+            const int tiles = (c.patches + 1) >> 1;
             const uint32_t slot = nitem & 1;
             if (warp == 1) {
                 // ---- S^T, dP^T of unit u as soon as dV and dK of unit u - 3 have consumed P^T, dS^T, which lie in the same columns
@@ -343,11 +341,12 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
             const int key_patch = 2 * c.tp + (quarter >> 1);
             const bool key_exists = key_patch < c.patches;
-            int ky, kx, Y0, X0;
-            patch_origin(p, c, key_patch, ky, kx, Y0, X0);
+            const int key_at = lists->origin[list_of(c) + key_patch], ky = key_at >> 8, kx = key_at & 255;
+            int Y0 = 0, X0 = 0;
+            if (kCut) patch_place(geom, lists, c, key_patch, Y0, X0);
             const int xk = lane >> 2, key_row0 = 4 * (quarter & 1);
             // keys of the patch beyond the map's edge get probability 0: a thread's whole column, or the rows from `rows_there` on
-            const bool column_there = X0 + xk < p.W;
+            const bool column_there = !kCut || X0 + xk < p.W;
             const int rows_there = p.H - Y0 - key_row0;          // of the thread's four
             // (a key that is none, in a whole patch or a column beyond the edge, finds the same two words for every query)
             const bool there = key_exists && column_there;
@@ -433,9 +432,9 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         auto drain_item = [&](const LiveItem& c, uint32_t nitem) -> bool {
             // rows leave by TMA, a warp's 32 (half a patch) at a time; rows beyond the map's edge are dropped by it
-            int py, px, Y0, X0;
+            int Y0, X0;
             const int sp = 2 * c.tp + (quarter >> 1);
-            patch_origin(p, c, sp, py, px, Y0, X0);
+            patch_place(geom, lists, c, sp, Y0, X0);
             const int Y = Y0 + 4 * (quarter & 1);
             if (!mbar_wait_warp(bar(kAccFull), nitem & 1, abort_flag, p.status)) return false;
             tc_fence_after();

@@ -109,14 +109,6 @@ __device__ __forceinline__ void patch_origin(const Params& p, const LiveItem& c,
 {
     live_patch_origin(p.g.live, WindowGeom{p.Hp, p.Wp, p.M, p.s}, c, min(sp, c.patches - 1), py, px, Y0, X0);
 }
-// for TMA: beyond the last patch lies nothing (zeros)
-__device__ __forceinline__ void patch_box(const Params& p, const LiveItem& c, int sp, int& Y0, int& X0)
-{
-    int py, px;
-    patch_origin(p, c, sp, py, px, Y0, X0);
-    if (sp >= c.patches) X0 = p.Wp;
-}
-
 // The table of head h, when all softmax warps are through with the last one's.  False when a wait ran out.
 __device__ __forceinline__ bool change_table(const Params& p, uint8_t* base_ptr, uint32_t base, int h, int* table_head, uint32_t* ntable)
 {
@@ -294,6 +286,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int side = 2 * p.M - 1;
+    const WindowGeom geom{p.Hp, p.Wp, p.M, p.s};
     const long long work = p.g.work[9] * p.heads;
     const int first_item = first_bias_item(p.g, work * blockIdx.x / gridDim.x);
     const int my_items = min(first_bias_item(p.g, work * (blockIdx.x + 1) / gridDim.x), p.items) - first_item;
@@ -355,6 +348,10 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (warp == 0) {
             // ============================================================ TMA producer (one lane)
             if (lane == 0) {
+                auto box = [&](const LiveItem& c, int sp, int& Y0, int& X0) {          // beyond the last patch lies nothing: zeros
+                    patch_place(geom, lists, c, sp, Y0, X0);
+                    if (sp >= c.patches) X0 = p.Wp;
+                };
                 for (int i = 0; i < count && ok; ++i, ++io) {
                     const LiveItem c = decode_bias_item(p.g, item_at(i));
                     const uint32_t buf = io & 1;
@@ -363,7 +360,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     ++q_armed;
                     for (int qp = 0; qp < 4; ++qp) {
                         int Y0, X0;
-                        patch_box(p, c, 4 * c.tp + qp, Y0, X0);
+                        box(c, 4 * c.tp + qp, Y0, X0);
                         tma_load_5d(base + kOffQ + 2 * buf * kContentBytes + qp * kPatchContent, &tm_q, bar(kQFull + buf), 0, c.h, X0, Y0, c.b);
                     }
                     const int nb = (c.patches + 1) >> 1;
@@ -374,7 +371,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         ++k_armed;
                         int Y0[2], X0[2];
                         for (int sub = 0; sub < 2; ++sub) {
-                            patch_box(p, c, 2 * j + sub, Y0[sub], X0[sub]);
+                            box(c, 2 * j + sub, Y0[sub], X0[sub]);
                             tma_load_5d(base + kOffK + st * kContentBytes + sub * kPatchContent, &tm_k, bar(kKFull + st), 0, c.h, X0[sub], Y0[sub], c.b);
                         }
                         if (use > 0 && !mbar_wait(bar(kVEmpty + st), (use - 1) & 1, abort_flag, p.status)) { ok = false; break; }
@@ -399,9 +396,10 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             // ===================================== issuer of S = Q K^T for both query tiles
             constexpr uint64_t kDesc64 = smem_desc_const(16, 512, kSwizzle64B);
             for (int i = 0; i < count && ok; ++i, ++io) {
+                    const LiveItem c = decode_bias_item(p.g, item_at(i));
                 const uint32_t buf = io & 1;
                 if (!mbar_wait_warp(bar(kQFull + buf), (io >> 1) & 1, abort_flag, p.status)) { ok = false; break; }
-                const int nb = (decode_bias_item(p.g, item_at(i)).patches + 1) >> 1;
+                const int nb = (c.patches + 1) >> 1;
                 for (int j = 0; j < nb && ok; ++j, ++blk) {
                     const uint32_t st = blk % kStages;
                     if (!mbar_wait_warp(bar(kKFull + st), (blk / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
@@ -435,7 +433,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const uint32_t d_o = tmem + kColO + qt * 2 * kD;              // exact form: one accumulator per key half
             const uint32_t d_o1 = tmem + kColO + qt * kFastOCols;         // fast form: one accumulator
             for (int i = 0; i < count && ok; ++i, ++io) {
-                const LiveItem c = decode_bias_item(p.g, item_at(i));
+                    const LiveItem c = decode_bias_item(p.g, item_at(i));
                 const int nb = (c.patches + 1) >> 1;
                 for (int j = 0; j < nb; ++j, ++blk) {
                     const uint32_t st = blk % kStages;
@@ -446,8 +444,8 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     for (int sub = 0; sub < 2; ++sub) {
                         int which = 2 * j + sub < c.patches ? kOnesAll : kOnesNone;
                         if (p.edges && which == kOnesAll) {
-                            int py, px, Y0, X0;
-                            patch_origin(p, c, 2 * j + sub, py, px, Y0, X0);
+                            int Y0, X0;
+                            patch_place(geom, lists, c, 2 * j + sub, Y0, X0);
                             const bool below = Y0 + 8 > p.H, right = X0 + 8 > p.W;
                             which = below ? (right ? kOnesBoth : kOnesBelow) : right ? kOnesRight : kOnesAll;
                         }
@@ -495,14 +493,19 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 // ------------------------------------------------------------------ fast form
                 const uint32_t t_o1 = tmem + lane_base + kColO + qt * kFastOCols;
                 // O and l of item i are complete (the caller has waited for its last PV): normalise, store, note overflow
-                auto epilogue = [&](int i) {
-                    const LiveItem c = decode_bias_item(p.g, item_at(i));
+                // where the thread's row goes: map, pixel of the map (-1: no query) and head
+                struct Place { int b, pixel, h; };
+                auto place_of = [&](const LiveItem& c) -> Place {
                     const int sp = 2 * (2 * c.tp + qt) + (row >> 6);
-                    int py, px, Y0, X0;
-                    patch_origin(p, c, sp, py, px, Y0, X0);
+                    int Y0, X0;
+                    patch_place(geom, lists, c, sp, Y0, X0);
                     const int Y = Y0 + ((row >> 3) & 7), X = X0 + (row & 7);   // the patch does not straddle the border
-                    const bool no_query = sp >= c.patches || Y >= p.H || X >= p.W;
-                    const size_t tok = (((size_t)c.b * p.H + Y) * p.W + X) * p.heads + c.h;
+                    return Place{c.b, sp >= c.patches || Y >= p.H || X >= p.W ? -1 : Y * p.W + X, c.h};
+                };
+                auto epilogue = [&](int i) {
+                    const Place place = place_of(decode_bias_item(p.g, item_at(i)));
+                    const bool no_query = place.pixel < 0;
+                    const size_t map_pixels = (size_t)p.H * p.W, tok = (place.b * map_pixels + place.pixel) * p.heads + place.h;
                     uint32_t o[16], lsum[1];
                     tmem_ld16(t_o1 + half * 16, o);
                     tmem_ld1(t_o1 + kD, lsum);
@@ -529,7 +532,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                             if (channels > 8) reinterpret_cast<uint4*>(dst)[1] = make_uint4(w[4], w[5], w[6], w[7]);
                         }
                     }
-                    if (p.lse && half == 0) p.lse[(((size_t)c.b * p.heads + c.h) * p.H + Y) * p.W + X] = logf(l_all);
+                    if (p.lse && half == 0) p.lse[((size_t)place.b * p.heads + place.h) * map_pixels + place.pixel] = logf(l_all);
                 };
                 for (int i = 0; i < count && ok; ++i, ++io) {
                     const LiveItem c = decode_bias_item(p.g, item_at(i));

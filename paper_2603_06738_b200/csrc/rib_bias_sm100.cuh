@@ -58,6 +58,13 @@ __device__ __forceinline__ void fill_patch_lists(const BiasItems& g, int M, Patc
     }
 }
 __device__ __forceinline__ int list_of(const LiveItem& c) { return (3 * c.ky + c.kx) * PatchLists::kPatches; }
+// Patch `sp` of the item's window in shifted, wrapped coordinates of the (extended) map.
+__device__ __forceinline__ void patch_place(const WindowGeom& g, const PatchLists* lists, const LiveItem& c, int sp, int& Y0, int& X0)
+{
+    const int at = lists->origin[list_of(c) + sp];
+    Y0 = c.wy * g.M + (at >> 8) + g.s; if (Y0 >= g.H) Y0 -= g.H;
+    X0 = c.wx * g.M + (at & 255) + g.s; if (X0 >= g.W) X0 -= g.W;
+}
 
 // The first item whose work begins at or behind `at`, all heads' items laid one behind the other.  CTA c of n takes the items that begin in
 // [c / n, (c + 1) / n) of the work: equal shares to within one item, and neighbours in the order, i.e. mostly one head.
