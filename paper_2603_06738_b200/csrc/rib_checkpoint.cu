@@ -13,37 +13,46 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kStagedRows = 64;
+constexpr int kStoreUnroll = 2, kRestoreUnroll = 8, kRestoreBlocks = 2;
 
-// Quotients decide codes, so they are those of the IEEE division; but x * (1 / scale) is off by less than 127 x 2^-22 = 3e-5, and unless it lies that
-// near to a border between two codes it names the same one.  (A scale below 2^-126 has no reciprocal: the test fails for infinities and NaN.)
-// The nearest whole number n is read off the low bits of t + 1.5 x 2^23 (half to even, as round() does): conversions between floating and whole
-// numbers have an eighth of the rate of additions, and were what these kernels waited for.  Returns a word with the code in its low byte.
+// Quotients decide codes, so they are those of the IEEE division.  With y the reciprocal of the scale, t = x y is off by an ulp or so; the remainder
+// x - t scale is exact, and adding y times it leaves a quotient (Markstein's method) that names the same code for every pair of bf16 mantissas and
+// every distance of their exponents: they are few enough to try them all, and a test does.  Three operations without a branch: a test
+// whether t lies near a border, with the division behind it, took 108 to 116 us
+// where this takes 96 (below), since half the maximum is a border and half of the warps met one.
+// A scale below 2^-100, whose remainders could vanish, takes the division.
+// The nearest whole number is read off the low bits of t + 1.5 x 2^23 (half to even, as round() does): conversions between floating and whole
+// numbers have an eighth of the rate of additions, and were what these kernels waited for.  Both return a word with the code in its low byte.
 __device__ __forceinline__ uint32_t code_of(float x, float scale, float inverse)
 {
-    const float t = x * inverse, shifted = t + 12582912.f, n = shifted - 12582912.f;
-    if (!(fabsf(t - n) < 0.4999f)) return (uint32_t)__float2int_rn(__fdiv_rn(x, scale));
-    return __float_as_uint(shifted);
+    const float t = x * inverse;
+    return __float_as_uint(fmaf(fmaf(-t, scale, x), inverse, t) + 12582912.f);
 }
+__device__ __forceinline__ uint32_t quotient_code(float x, float scale) { return (uint32_t)__float2int_rn(__fdiv_rn(x, scale)); }
 // the low bytes of four words
 __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
-struct RowScale { float scale, inverse; bool zero; };
+struct RowScale { float scale, inverse; bool zero, tiny; };
 __device__ __forceinline__ RowScale row_scale(float most, bool bad)
 {
     RowScale r;
     r.scale = bad ? __int_as_float(0x7fffffff) : most * (1.f / 127.f);
     r.zero = bad || r.scale == 0.f;
     r.inverse = 1.f / r.scale;
+    r.tiny = r.scale < 0x1p-100f;
     return r;
 }
 
-// kLanes lanes to a row (a power of two, the last ones without channels where d / 8 is none), kRows rows of kThreads / kLanes per block
+// kLanes lanes to a row (a power of two, the last ones without channels where d / 8 is none), two runs of kThreads / kLanes rows
+// per block (a layer of 16 x 96 x 96 tokens, 6 heads, d = 32: 96 us for four tensors, 3.7 TB/s; one run 105, four and eight 94 to 96.  Blocks that walk
+// runs with the next one's loads under way, as restore has them, took 8 us more: the shuffles and the reciprocal of a row wait for one another,
+// and what hides that is other warps)
 template <int kLanes>
 __global__ void __launch_bounds__(kThreads) rib_checkpoint_store_kernel(const __nv_bfloat16* __restrict__ x, long long rows, int d, int8_t* __restrict__ codes, float* __restrict__ scales)
 {
-    constexpr int kUnroll = 4, kRowsAtOnce = kThreads / kLanes;
+    constexpr int kUnroll = kStoreUnroll, kRowsAtOnce = kThreads / kLanes;
     const int part = threadIdx.x % kLanes;
     const bool mine = 8 * part < d;
     const long long row0 = (long long)blockIdx.x * (kUnroll * kRowsAtOnce) + threadIdx.x / kLanes;
@@ -70,6 +79,12 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_store_kernel(const __
             for (int i = 0; i < 2; ++i)
                 c[i] = low_bytes(code_of(__uint_as_float(w[2 * i] << 16), s.scale, s.inverse), code_of(__uint_as_float(w[2 * i] & 0xffff0000u), s.scale, s.inverse),
                                  code_of(__uint_as_float(w[2 * i + 1] << 16), s.scale, s.inverse), code_of(__uint_as_float(w[2 * i + 1] & 0xffff0000u), s.scale, s.inverse));
+            if (s.tiny) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    c[i] = low_bytes(quotient_code(__uint_as_float(w[2 * i] << 16), s.scale), quotient_code(__uint_as_float(w[2 * i] & 0xffff0000u), s.scale),
+                                     quotient_code(__uint_as_float(w[2 * i + 1] << 16), s.scale), quotient_code(__uint_as_float(w[2 * i + 1] & 0xffff0000u), s.scale));
+            }
         }
         if (row < rows) {
             if (mine) *reinterpret_cast<uint2*>(codes + row * d + 8 * part) = make_uint2(c[0], c[1]);
@@ -107,7 +122,10 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_store_staged_kernel(c
     }
     const RowScale s = row_scale(most, bad);
     if (r < here) {
-        for (int c = part; c < d; c += 4) cs[r * d + c] = s.zero ? 0 : (int8_t)code_of(__bfloat162float(xs[r * d + c]), s.scale, s.inverse);
+        for (int c = part; c < d; c += 4) {
+            const float v = __bfloat162float(xs[r * d + c]);
+            cs[r * d + c] = s.zero ? 0 : (int8_t)(s.tiny ? quotient_code(v, s.scale) : code_of(v, s.scale, s.inverse));
+        }
         if (part == 0) scales[row0 + r] = s.scale;
     }
     __syncthreads();
@@ -120,27 +138,41 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_store_staged_kernel(c
 
 struct RestoreArgs { CheckpointRows t[4]; };
 
+// A block walks runs of rows and has the next run's loads under way while it writes one (the same layer: 64 us for four tensors, 5.5 TB/s; a run per block 100)
 template <int kLanes>
 __global__ void __launch_bounds__(kThreads) rib_checkpoint_restore_kernel(const RestoreArgs args, long long rows, int d)
 {
-    constexpr int kUnroll = 4, kRowsAtOnce = kThreads / kLanes;
+    constexpr int kRowsAtOnce = kThreads / kLanes;
     const CheckpointRows t = args.t[blockIdx.y];
     const int part = threadIdx.x % kLanes;
     if (8 * part >= d) return;
-    const long long row0 = (long long)blockIdx.x * (kUnroll * kRowsAtOnce) + threadIdx.x / kLanes;
-    uint2 c[kUnroll];
-    float scale[kUnroll];
+    const long long step = (long long)gridDim.x * kRestoreUnroll * kRowsAtOnce;
+    long long row0 = (long long)blockIdx.x * (kRestoreUnroll * kRowsAtOnce) + threadIdx.x / kLanes;
+    const uint2* src = reinterpret_cast<const uint2*>(t.codes + 8 * part);
+    uint4* dst = reinterpret_cast<uint4*>(t.x + 8 * part);
+    const int words = d / 8;
+    uint2 c[kRestoreUnroll], ahead[kRestoreUnroll];
+    float scale[kRestoreUnroll], ahead_scale[kRestoreUnroll];
+    auto load = [&](uint2 (&c)[kRestoreUnroll], float (&scale)[kRestoreUnroll]) {
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-        const long long row = row0 + k * kRowsAtOnce;
-        c[k] = row < rows ? __ldg(reinterpret_cast<const uint2*>(t.codes + row * d + 8 * part)) : make_uint2(0u, 0u);
-        scale[k] = row < rows ? __ldg(t.scales + row) : 0.f;
-    }
+        for (int k = 0; k < kRestoreUnroll; ++k) {
+            const long long row = row0 + k * kRowsAtOnce;
+            c[k] = row < rows ? __ldg(src + row * words) : make_uint2(0u, 0u);
+            scale[k] = row < rows ? __ldg(t.scales + row) : 0.f;
+        }
+    };
+    load(c, scale);
+    while (row0 < rows) {
+        const long long here = row0;
+        row0 += step;
+        load(ahead, ahead_scale);
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-        const long long row = row0 + k * kRowsAtOnce;
-        if (row < rows)
-            *reinterpret_cast<uint4*>(t.x + row * d + 8 * part) = restored_chunk(c[k], scale[k]);
+        for (int k = 0; k < kRestoreUnroll; ++k) {
+            const long long row = here + k * kRowsAtOnce;
+            if (row < rows) dst[row * words] = restored_chunk(c[k], scale[k]);
+            c[k] = ahead[k];
+            scale[k] = ahead_scale[k];
+        }
     }
 }
 
@@ -172,7 +204,12 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_restore_staged_kernel
 
 // 8 channels to a thread: lanes to a row as a power of two
 int lanes_of(int d) { return d <= 8 ? 1 : d <= 16 ? 2 : d <= 32 ? 4 : 8; }
-unsigned blocks_of(long long rows, int lanes) { const long long per = 4LL * kThreads / lanes; return (unsigned)((rows + per - 1) / per); }
+// restore: blocks of a run each, or as many as kRestoreBlocks to an SM (of 148: the same number everywhere, so that a call's shape decides the launch)
+unsigned restore_blocks(long long rows, int lanes, int tensors)
+{
+    const long long per = (long long)kRestoreUnroll * kThreads / lanes, all = (rows + per - 1) / per, most = kRestoreBlocks * 148 / tensors;
+    return (unsigned)(all < most ? all : most);
+}
 
 }  // namespace
 
@@ -184,7 +221,8 @@ cudaError_t checkpoint_store(const __nv_bfloat16* x, long long rows, int d, int8
     } else {
         const int lanes = lanes_of(d);
         const auto kernel = lanes == 1 ? rib_checkpoint_store_kernel<1> : lanes == 2 ? rib_checkpoint_store_kernel<2> : lanes == 4 ? rib_checkpoint_store_kernel<4> : rib_checkpoint_store_kernel<8>;
-        kernel<<<blocks_of(rows, lanes), kThreads, 0, stream>>>(x, rows, d, codes, scales);
+        const long long per = (long long)kStoreUnroll * kThreads / lanes;
+        kernel<<<(unsigned)((rows + per - 1) / per), kThreads, 0, stream>>>(x, rows, d, codes, scales);
     }
     return cudaGetLastError();
 }
@@ -199,7 +237,7 @@ cudaError_t checkpoint_restore(const CheckpointRows* tensors, int count, long lo
     } else {
         const int lanes = lanes_of(d);
         const auto kernel = lanes == 1 ? rib_checkpoint_restore_kernel<1> : lanes == 2 ? rib_checkpoint_restore_kernel<2> : lanes == 4 ? rib_checkpoint_restore_kernel<4> : rib_checkpoint_restore_kernel<8>;
-        kernel<<<dim3(blocks_of(rows, lanes), (unsigned)count), kThreads, 0, stream>>>(args, rows, d);
+        kernel<<<dim3(restore_blocks(rows, lanes, count), (unsigned)count), kThreads, 0, stream>>>(args, rows, d);
     }
     return cudaGetLastError();
 }

@@ -36,6 +36,20 @@ def test_codes_scales_and_values_bit_by_bit(shape):
     assert torch.equal(torch.isnan(back.cpu()), torch.isnan(want)) and torch.equal(back.cpu().nan_to_num(), want.nan_to_num())
 
 
+@pytest.mark.parametrize("d", [64, 63])
+@pytest.mark.parametrize("exponent", [-120, -100, -93, -1, 0, 127])
+def test_codes_of_every_pair_of_mantissas(d, exponent):
+    """Every bf16 mantissa as a row's maximum beside every bf16 value down to 2^-9 of it (smaller ones have code 0): the codes are those of the division."""
+    most = torch.arange(128, 256, dtype=torch.float64) * 2.0 ** (exponent - 7)
+    parts = torch.cat([torch.arange(128, 256, dtype=torch.float64) * 2.0 ** (exponent - 7 - e) for e in range(10)])
+    parts = torch.nn.functional.pad(parts, (0, -len(parts) % (d - 1))).view(-1, d - 1)
+    x = torch.cat([most[:, None, None].expand(-1, len(parts), 1), torch.minimum(parts[None], most[:, None, None])], 2).reshape(-1, d).bfloat16()
+    x[1::2] = -x[1::2]
+    codes, scales = binding.rib_checkpoint_store(x.cuda())
+    want_codes, want_scales = orc.store(x.float().numpy())
+    assert np.array_equal(codes.cpu().numpy(), want_codes) and np.array_equal(scales.cpu().numpy(), want_scales)
+
+
 def test_empty_and_refused():
     codes, scales = binding.rib_checkpoint_store(torch.empty(0, 32, dtype=torch.bfloat16, device="cuda"))
     assert codes.shape == (0, 32) and scales.shape == (0,) and binding.rib_checkpoint_restore(codes, scales).shape == (0, 32)
