@@ -28,13 +28,13 @@ namespace {
 using namespace sm100;
 
 constexpr int kQStages = 3;           // ring of query-side tiles (Q, dO, rows of lse and D)
+constexpr int kMaxSlots = 4;          // K and V of items in flight.  The scores are three half-tiles ahead of the drains, which in windows of 16 is an item: with two
+                                      // slots the next item's K arrived too late (4 x 96 x 96 tokens, 12 heads, d = 16, windows of 16: 142 us; three 119, four 116)
 constexpr int kThreads = 896;
 constexpr int kArithmeticThreads = 512;
 
 // shared-memory map (offsets from a 1024-byte aligned base)
-constexpr uint32_t kOffK = 0;                                    // [2] (one slot per item in flight)
-constexpr uint32_t kOffV = kOffK + 2 * kContentBytes;            // [2]
-constexpr uint32_t kOffRing = kOffV + 2 * kContentBytes;
+constexpr uint32_t kOffRing = 0;
 constexpr uint32_t kLdPatch = 64 * 16, kLdBytes = 2 * kLdPatch;  // per query 8 bf16: -lse sqrt(d) and -D in three parts each, 0, 0
 constexpr uint32_t kRingQ = 0, kRingDO = kContentBytes, kRingLD = kRingDO + kContentBytes;
 constexpr uint32_t kRingBytes = kRingLD + kLdBytes;              // 18432
@@ -45,8 +45,8 @@ constexpr uint32_t kOffBar = kOffDK + kContentBytes;
 // kSFull, kPReady, kPFree: unit mod 4 (on_unit); kDSFree: per dS tile buffer.  A parity wait cannot tell "two phases ahead" from "not yet", so a
 // barrier's next phase must not be able to complete before every waiter has seen the current one: the next phases of kPReady of the units 2 g,
 // 2 g + 1 belong to tile g + 2, whose dS buffer is released by dQ of tile g and by the four warps that sum the bias gradient.
-enum Bar { kKVFull = 0, kKVEmpty = 2, kQFull = 4, kQEmpty = kQFull + kQStages, kSFull = kQEmpty + kQStages, kPReady = kSFull + 4, kPFree = kPReady + 4,
-           kDSFree = kPFree + 4, kDQFull = kDSFree + 2, kDQFree, kAccFull, kAccFree, kTabDone, kTabReady, kDrain, kNumBars = kDrain + 3 };
+enum Bar { kKVFull = 0, kKVEmpty = kMaxSlots, kQFull = 2 * kMaxSlots, kQEmpty = kQFull + kQStages, kSFull = kQEmpty + kQStages, kPReady = kSFull + 4, kPFree = kPReady + 4,
+           kDSFree = kPFree + 4, kDQFull = kDSFree + 2, kDQFree, kAccFull, kAccFree, kTabDone, kTabReady, kItems, kDrain, kNumBars = kDrain + 3 };
 constexpr uint32_t kOffMisc = kOffBar + kNumBars * 8;
 constexpr uint32_t kOffMasked = kOffMisc + 16;                   // biases of a key that is none
 // [S, dP] rows of 8 bf16 for all keys: 1 for the parts of -lse sqrt(d) (S) or of -D (dP).  The rows are alike, so the groups of 8 that an MMA reads
@@ -56,9 +56,25 @@ constexpr uint32_t kOffOnes = (kOffMasked + 16 + 127) & ~127u;
 constexpr uint32_t kOffZero = kOffOnes + 2 * kOnesBytes;         // zeros: columns 8 .. 15 of the queries' parts, and rows of dS that do not count
 constexpr uint32_t kOffLists = kOffZero + 1024;                  // PatchLists
 static_assert(kOffZero % 128 == 0, "lines of 128 bytes");
-constexpr uint32_t kOffTable = kOffLists + sizeof(PatchLists);   // [(2M-1)^2] fp32
-constexpr uint32_t smem_bytes(int M) { return kOffTable + 4u * (2 * M - 1) * (2 * M - 1) + 1024; }
-static_assert(smem_bytes(kBiasMaxWindow) <= 232448, "shared memory of one CTA");
+constexpr uint32_t kOffItems = (kOffLists + sizeof(PatchLists) + 15) & ~15u;      // ItemRing
+constexpr uint32_t kOffTable = kOffItems + sizeof(ItemRing);     // [(2M-1)^2] fp32
+// behind the table: K and V of the items in flight, as many as there is room for
+constexpr uint32_t kMaxShared = 232448, kSlotBytes = 2 * kContentBytes;
+constexpr uint32_t slots_offset(int M) { return (kOffTable + 4u * (2 * M - 1) * (2 * M - 1) + 1023u) & ~1023u; }
+constexpr int slots_of(int M)
+{
+    int slots = 2;
+    while (slots < kMaxSlots && slots_offset(M) + (slots + 1) * kSlotBytes + 1024 <= kMaxShared) ++slots;
+    return slots;
+}
+constexpr uint32_t smem_bytes(int M) { return slots_offset(M) + slots_of(M) * kSlotBytes + 1024; }      // + slack for manual alignment
+constexpr uint32_t most_shared()
+{
+    uint32_t most = 0;
+    for (int M = 8; M <= kBiasMaxWindow; M += 8) most = smem_bytes(M) > most ? smem_bytes(M) : most;
+    return most;
+}
+static_assert(most_shared() <= kMaxShared, "shared memory of one CTA");
 static_assert(kOffRing % 1024 == 0 && kRingBytes % 1024 == 0 && kOffDS % 1024 == 0, "swizzle atoms need aligned tiles");
 
 // tensor-memory columns: S^T of unit u in buffer u mod 3 (64 fp32 columns) and dP^T beside it; a warp writes P^T over its own scores and dS^T over its
@@ -80,6 +96,8 @@ struct Params {
     long long no_queries;      // element of ld where the patch of no queries begins
     int H, W, heads, M, s, n, nWy, nWx, Hp, Wp;
     int items;
+    int slots;                 // of K and V
+    uint32_t slots_at;         // in shared memory
     float scale_log2;          // log2(e) / sqrt(d)
     float inv_sqrt_d;
     BiasSource source;
@@ -124,6 +142,10 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     auto on_unit = [&](int which, uint32_t unit) { return bar(which + (int)(unit & 3)); };
     auto unit_parity = [](uint32_t unit) { return (unit >> 2) & 1; };
     auto buffer_after = [](uint32_t buffer, uint32_t units) { buffer += units; return buffer >= kBuffers ? buffer - kBuffers : buffer; };
+    // an item's slot and how often the slots have gone round, odd or even
+    const uint32_t slots = p.slots;
+    auto k_slot = [&](uint32_t slot) { return base + p.slots_at + slot * kSlotBytes; };
+    auto next_slot = [&](uint32_t& slot, uint32_t& round) { if (++slot == slots) { slot = 0; round ^= 1; } };
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + kOffMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + kOffMisc + 4);
 
@@ -136,13 +158,14 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
     if (threadIdx.x == 0) {
         abort_flag[0] = 0; abort_flag[1] = 0;   // [1] stays 0: used by the drain waits
-        for (int s = 0; s < 2; ++s) { mbar_init(bar(kKVFull + s), 1); mbar_init(bar(kKVEmpty + s), 5); }     // empty: the item's last dQ, and V's slot by the four warps whose dV leaves through it
+        for (int s = 0; s < kMaxSlots; ++s) { mbar_init(bar(kKVFull + s), 1); mbar_init(bar(kKVEmpty + s), 5); }     // empty: the item's last dQ, and V's slot by the four warps whose dV leaves through it
         for (int s = 0; s < kQStages; ++s) { mbar_init(bar(kQFull + s), 1); mbar_init(bar(kQEmpty + s), 1); }
         for (int h = 0; h < 2; ++h) mbar_init(bar(kDSFree + h), 5);        // dQ and the four warps of the bias gradient
         for (int i = 0; i < 4; ++i) { mbar_init(bar(kSFull + i), 1); mbar_init(bar(kPReady + i), 8); mbar_init(bar(kPFree + i), 1); }
         mbar_init(bar(kDQFull), 1); mbar_init(bar(kDQFree), 4);
         mbar_init(bar(kAccFull), 1); mbar_init(bar(kAccFree), 4);
         mbar_init(bar(kTabDone), kArithmeticThreads / 32); mbar_init(bar(kTabReady), kArithmeticThreads / 32);
+        mbar_init(bar(kItems), 1);
         for (int i = 0; i < 3; ++i) mbar_init(bar(kDrain + i), 1);
         fence_barrier_init();
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
@@ -154,6 +177,8 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
     PatchLists* const lists = reinterpret_cast<PatchLists*>(base_ptr + kOffLists);
     fill_patch_lists(p.g, p.M, lists, threadIdx.x, kThreads);
+    ItemRing* const items = reinterpret_cast<ItemRing*>(base_ptr + kOffItems);
+    auto items_ready = [&](uint32_t n) { return !ItemRing::begins(n) || mbar_wait_warp(bar(kItems), ItemRing::parity(n), abort_flag, p.status); };
     if (threadIdx.x < (2 * kOnesBytes + 1024) / 16) {
         constexpr uint32_t kTwo = 0x3F803F80u, kFirst = 0x00003F80u, kSecond = 0x3F800000u;
         const uint32_t at = threadIdx.x * 16;
@@ -168,50 +193,59 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     cudaGridDependencySynchronize();              // the preparation kernel, which this one may have overtaken: lse and D, cleared sums
 
     if (warp == 0) {
-        // ============================================================ TMA producer (one thread)
-        if (lane == 0) {
-            uint32_t nitem = 0, kv_armed = 0, q_armed = 0;
-            bool ok = true;
-            for (int item = first_item; item < last_item && ok; ++item, ++nitem) {
-            const LiveItem c = decode_bias_item(p.g, item);
-                const uint32_t slot = nitem & 1;
-                if (nitem >= 2 && !mbar_wait(bar(kKVEmpty + slot), ((nitem >> 1) - 1) & 1, abort_flag, p.status)) { ok = false; break; }
-                mbar_arrive_expect_tx(bar(kKVFull + slot), 2 * kContentBytes);
-                ++kv_armed;
-                for (int sub = 0; sub < 2; ++sub) {
-                    int Y0, X0;
-                    patch_place(geom, lists, c, 2 * c.tp + sub, Y0, X0);
-                    if (2 * c.tp + sub >= c.patches) X0 = p.Wp;          // beyond the last patch lies nothing: zeros
-                    tma_load_5d(base + kOffK + slot * kContentBytes + sub * kPatchContent, &tm_k, bar(kKVFull + slot), 0, c.h, X0, Y0, c.b);
-                    tma_load_5d(base + kOffV + slot * kContentBytes + sub * kPatchContent, &tm_v, bar(kKVFull + slot), 0, c.h, X0, Y0, c.b);
+        // ============================================================ TMA producer: one lane, the others decode items
+        uint32_t slot = 0, round = 0, kv_armed = 0, q_armed = 0;
+        bool ok = true;
+        for (uint32_t nitem = 0; first_item + (int)nitem < last_item && ok; ++nitem, next_slot(slot, round)) {
+            if (ItemRing::begins(nitem)) {
+                const int item = first_item + (int)nitem + lane;
+                if (lane < ItemRing::kEight && item < last_item) items->at(nitem + lane) = decode_bias_item(p.g, item);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kItems));
+            }
+            if (lane == 0) {
+                const LiveItem c = items->at(nitem);
+                // (a barrier that has completed no phase answers yes to parity 1)
+                ok = mbar_wait(bar(kKVEmpty + slot), round ^ 1, abort_flag, p.status);
+                if (ok) {
+                    mbar_arrive_expect_tx(bar(kKVFull + slot), kSlotBytes);
+                    ++kv_armed;
+                    for (int sub = 0; sub < 2; ++sub) {
+                        int Y0, X0;
+                        patch_place(geom, lists, c, 2 * c.tp + sub, Y0, X0);
+                        if (2 * c.tp + sub >= c.patches) X0 = p.Wp;          // beyond the last patch lies nothing: zeros
+                        tma_load_5d(k_slot(slot) + sub * kPatchContent, &tm_k, bar(kKVFull + slot), 0, c.h, X0, Y0, c.b);
+                        tma_load_5d(k_slot(slot) + kContentBytes + sub * kPatchContent, &tm_v, bar(kKVFull + slot), 0, c.h, X0, Y0, c.b);
+                    }
                 }
                 const size_t pair = pair_of(p, c);
                 const int tiles = (c.patches + 1) >> 1;
-                for (int I = 0; I < tiles; ++I, ++q_armed) {
+                for (int I = 0; I < tiles && ok; ++I, ++q_armed) {
                     const uint32_t st = q_armed % kQStages, use = q_armed / kQStages;
                     if (use > 0 && !mbar_wait(bar(kQEmpty + st), (use - 1) & 1, abort_flag, p.status)) { ok = false; break; }
                     mbar_arrive_expect_tx(bar(kQFull + st), kRingBytes);
-                    const uint32_t ring = base + kOffRing + st * kRingBytes;
+                    const uint32_t to = base + kOffRing + st * kRingBytes;
                     for (int sub = 0; sub < 2; ++sub) {
                         int Y0, X0;
                         patch_place(geom, lists, c, 2 * I + sub, Y0, X0);
                         const int from = lists->origin[list_of(c) + 2 * I + sub];
                         const bool none = 2 * I + sub >= c.patches;
                         if (none) X0 = p.Wp;
-                        tma_load_5d(ring + kRingQ + sub * kPatchContent, &tm_q, bar(kQFull + st), 0, c.h, X0, Y0, c.b);
-                        tma_load_5d(ring + kRingDO + sub * kPatchContent, &tm_do, bar(kQFull + st), 0, c.h, X0, Y0, c.b);
+                        tma_load_5d(to + kRingQ + sub * kPatchContent, &tm_q, bar(kQFull + st), 0, c.h, X0, Y0, c.b);
+                        tma_load_5d(to + kRingDO + sub * kPatchContent, &tm_do, bar(kQFull + st), 0, c.h, X0, Y0, c.b);
                         const size_t at = none ? (size_t)p.no_queries : pair * p.n + 64 * (size_t)((from >> 11) * (p.M >> 3) + ((from & 255) >> 3));
-                        bulk_load_1d(ring + kRingLD + sub * kLdPatch, p.ld + at, kLdPatch, bar(kQFull + st));
+                        bulk_load_1d(to + kRingLD + sub * kLdPatch, p.ld + at, kLdPatch, bar(kQFull + st));
                     }
                 }
             }
-            if (!ok) {
-                // Gave up: let the copies already in flight land before the CTA may exit.
-                for (uint32_t b2 = kv_armed > 2u ? kv_armed - 2 : 0; b2 < kv_armed; ++b2)
-                    mbar_wait(bar(kKVFull + (b2 & 1)), (b2 >> 1) & 1, abort_flag + 1, p.status);
-                for (uint32_t b2 = q_armed > (uint32_t)kQStages ? q_armed - kQStages : 0; b2 < q_armed; ++b2)
-                    mbar_wait(bar(kQFull + b2 % kQStages), (b2 / kQStages) & 1, abort_flag + 1, p.status);
-            }
+            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        }
+        if (lane == 0 && !ok) {
+            // Gave up: let the copies already in flight land before the CTA may exit.
+            for (uint32_t b2 = kv_armed > slots ? kv_armed - slots : 0; b2 < kv_armed; ++b2)
+                mbar_wait(bar(kKVFull + b2 % slots), (b2 / slots) & 1, abort_flag + 1, p.status);
+            for (uint32_t b2 = q_armed > (uint32_t)kQStages ? q_armed - kQStages : 0; b2 < q_armed; ++b2)
+                mbar_wait(bar(kQFull + b2 % kQStages), (b2 / kQStages) & 1, abort_flag + 1, p.status);
         }
         __syncwarp();
     } else if (warp < 4) {
@@ -221,17 +255,16 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         constexpr uint64_t kDescDS = smem_desc_const(kDSHalf, 1024, kSwizzle128B);    // MN-major: the two 64-query halves one leading step apart
         auto wait_all = [&](uint32_t b, uint32_t parity) { return mbar_wait_warp(b, parity, abort_flag, p.status); };
         bool ok = true;
-        uint32_t g = 0, nitem = 0, buf = 0;
-        for (int item = first_item; item < last_item && ok; ++item, ++nitem) {
-            const LiveItem c = decode_bias_item(p.g, item);
-            const int tiles = (c.patches + 1) >> 1;
-            const uint32_t slot = nitem & 1;
+        uint32_t g = 0, nitem = 0, buf = 0, slot = 0, round = 0;
+        for (int item = first_item; item < last_item && ok; ++item, ++nitem, next_slot(slot, round)) {
+            if (!items_ready(nitem)) { ok = false; break; }
+            const int tiles = (items->at(nitem).patches + 1) >> 1;
             if (warp == 1) {
                 // ---- S^T, dP^T of unit u as soon as dV and dK of unit u - 3 have consumed P^T, dS^T, which lie in the same columns
-                if (!wait_all(bar(kKVFull + slot), (nitem >> 1) & 1)) { ok = false; break; }
+                if (!wait_all(bar(kKVFull + slot), round)) { ok = false; break; }
                 // (columns 8 .. 15 of the ones: the same rows again, against zeros)
                 const uint64_t ones_s = smem_desc(base + kOffOnes, 16, 16, kSwizzleNone), ones_dp = smem_desc(base + kOffOnes + kOnesBytes, 16, 16, kSwizzleNone);
-                const uint64_t k = smem_desc_at(kDesc64, base + kOffK + slot * kContentBytes), v = smem_desc_at(kDesc64, base + kOffV + slot * kContentBytes);
+                const uint64_t k = smem_desc_at(kDesc64, k_slot(slot)), v = smem_desc_at(kDesc64, k_slot(slot) + kContentBytes);
                 for (int t = 0; t < tiles && ok; ++t, ++g) {
                     const uint32_t st = g % kQStages;
                     if (!wait_all(bar(kQFull + st), (g / kQStages) & 1)) { ok = false; break; }
@@ -296,7 +329,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         (g > 0 && !wait_all(bar(kDQFree), (g - 1) & 1))) { ok = false; break; }
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint64_t k = smem_desc_at(kDesc64, base + kOffK + slot * kContentBytes);
+                        const uint64_t k = smem_desc_at(kDesc64, k_slot(slot));
                         const uint64_t ds = smem_desc_at(kDescDS, base + kOffDS + (g & 1) * 2 * kDSHalf);
 #pragma unroll
                         for (int kk = 0; kk < kTile / 16; ++kk)
@@ -326,7 +359,9 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         int table_head = -1;
         bool ok = true;
         for (int item = first_item; item < last_item && ok; ++item) {
-            const LiveItem c = decode_bias_item(p.g, item);
+            const uint32_t nitem = (uint32_t)(item - first_item);
+            if (!items_ready(nitem)) { ok = false; break; }
+            const LiveItem c = items->at(nitem);
             if (c.h != table_head) {
                 // the table of head h: when all arithmetic warps are through with the last one's
                 __syncwarp();
@@ -430,7 +465,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const int quarter = warp & 3;
         const int row = quarter * 32 + lane;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-        auto drain_item = [&](const LiveItem& c, uint32_t nitem) -> bool {
+        auto drain_item = [&](const LiveItem& c, uint32_t nitem, uint32_t v_slot) -> bool {
             // rows leave by TMA, a warp's 32 (half a patch) at a time; rows beyond the map's edge are dropped by it
             int Y0, X0;
             const int sp = 2 * c.tp + (quarter >> 1);
@@ -441,7 +476,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const int sw = (row >> 1) & 3;                    // SWIZZLE_64B
 #pragma unroll
             for (int which = 0; which < 2; ++which) {         // dV through V's slot, dK through a tile of its own
-                uint8_t* const stage = base_ptr + (which == 0 ? kOffV + (nitem & 1) * kContentBytes : kOffDK) + row * 64;
+                uint8_t* const stage = base_ptr + (which == 0 ? v_slot : kOffDK) + row * 64;
                 const float f = which == 0 ? 1.f : p.inv_sqrt_d;
                 uint32_t a[32];
                 tmem_ld32(tmem + lane_base + (which == 0 ? kColDV : kColDK), a);
@@ -460,22 +495,23 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (lane == 0) {
                 mbar_arrive(bar(kAccFree));
                 if (sp < c.patches && Y < p.H) {
-                    tma_store_5d(&tm_dv, base + kOffV + (nitem & 1) * kContentBytes + quarter * (kPatchContent / 2), 0, c.h, X0, Y, c.b);
+                    tma_store_5d(&tm_dv, base + v_slot + quarter * (kPatchContent / 2), 0, c.h, X0, Y, c.b);
                     tma_store_5d(&tm_dk, base + kOffDK + quarter * (kPatchContent / 2), 0, c.h, X0, Y, c.b);
                     bulk_commit_group();
                 }
             }
             return true;
         };
-        uint32_t g = 0, nitem = 0;
+        uint32_t g = 0, nitem = 0, slot = 0, round = 0;
         bool ok = true;
-        for (int item = first_item; item < last_item && ok; ++item, ++nitem) {
-            const LiveItem c = decode_bias_item(p.g, item);
+        for (int item = first_item; item < last_item && ok; ++item, ++nitem, next_slot(slot, round)) {
+            if (!items_ready(nitem)) { ok = false; break; }
+            const LiveItem c = items->at(nitem);
             const int tiles = (c.patches + 1) >> 1;
             float* const acc = p.dq_acc + pair_of(p, c) * kD * p.n;
             for (int I = 0; I < tiles && ok; ++I, ++g) {
                 // (dV and dK before the item's last dQ: those of the next item wait for the accumulators)
-                if (I == tiles - 1) ok = drain_item(c, nitem);
+                if (I == tiles - 1) ok = drain_item(c, nitem, p.slots_at + slot * kSlotBytes + kContentBytes);
                 if (!ok || !mbar_wait_warp(bar(kDQFull), g & 1, abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
                 const int sp = 2 * I + (quarter >> 1), at = lists->origin[list_of(c) + sp];
@@ -505,7 +541,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 // V's slot, when its dV rows have been read
                 if (lane == 0) {
                     bulk_wait_group_read<0>();                // (this thread's own stores)
-                    mbar_arrive(bar(kKVEmpty + (nitem & 1)));
+                    mbar_arrive(bar(kKVEmpty + slot));
                 }
                 __syncwarp();
             }
@@ -540,7 +576,9 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         uint32_t g = 0;
         bool ok = true;
         for (int item = first_item; item < last_item && ok; ++item) {
-            const LiveItem c = decode_bias_item(p.g, item);
+            const uint32_t nitem = (uint32_t)(item - first_item);
+            if (!items_ready(nitem)) { ok = false; break; }
+            const LiveItem c = items->at(nitem);
             const int tiles = (c.patches + 1) >> 1;
             const uint16_t* const list = lists->origin + list_of(c);
             const int key_at = list[2 * c.tp + sub] + (0x100 + 1) * (p.M - 8);
@@ -739,7 +777,7 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     const bool cut = p.H % 8 != 0 || p.W % 8 != 0;
     const auto kernel = cut ? rib_bias_bwd_kernel<true> : rib_bias_bwd_kernel<false>;
     int sm_count = 0;
-    if (cudaError_t e = setup[cut].prepare(kernel, smem_bytes(kBiasMaxWindow), &sm_count)) return e;
+    if (cudaError_t e = setup[cut].prepare(kernel, most_shared(), &sm_count)) return e;
     Params bp{};
     if (!make_bias_items(p, 2, &bp.g)) return cudaErrorInvalidValue;
     AuxParams ap{};
@@ -757,6 +795,8 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     bp.no_queries = (long long)tokens;
     bp.H = p.H; bp.W = p.W; bp.heads = p.heads; bp.M = p.M; bp.s = p.s; bp.n = p.n; bp.nWy = p.nWy; bp.nWx = p.nWx; bp.Hp = p.Hp; bp.Wp = p.Wp;
     bp.items = bp.g.per_head * p.heads;
+    bp.slots = slots_of(p.M);
+    bp.slots_at = slots_offset(p.M);
     bp.scale_log2 = kLog2e / sqrtf((float)p.d);
     bp.inv_sqrt_d = ap.inv_sqrt_d;
     bp.source = bias_source(p);

@@ -34,6 +34,20 @@ __device__ __forceinline__ LiveItem decode_bias_item(const BiasItems& g, int ite
     return c;
 }
 
+// The items that the roles of a CTA walk, decoded once by the producer's warp, eight at a time, instead of by every warp (a chain of divisions and of
+// loads from the parameters by kind; in windows of 16 an item is some 3 us of work: 4 x 96 x 96 tokens, 12 heads, d = 16, backward
+// 116 -> 105 us).  `n` counts the CTA's items; every 8th one a
+// role waits for the barrier whose phases are the eights.  Nothing says that an eight may be overwritten, and nothing has to: the producer
+// writes eight c + 2 when it has begun to load item 8 c + 15, and K, V (backward) or Q (forward) of that item went where those of item
+// 8 c + 11 or 8 c + 13 had been, by when no role is more than six items behind.
+struct ItemRing {
+    static constexpr uint32_t kEight = 8;
+    LiveItem items[2 * kEight];
+    __device__ __forceinline__ static bool begins(uint32_t n) { return n % kEight == 0; }
+    __device__ __forceinline__ static uint32_t parity(uint32_t n) { return (n / kEight) & 1; }
+    __device__ __forceinline__ LiveItem& at(uint32_t n) { return items[n % (2 * kEight)]; }
+};
+
 // The patches of every kind of window, in the order of its list, in shared memory: where they begin in the window (y << 8 | x), and how far into a
 // table by offset they move an entry (4 (y (2M-1) + x) bytes).  Behind the last patch of a list the last one stands in.
 struct PatchLists {
