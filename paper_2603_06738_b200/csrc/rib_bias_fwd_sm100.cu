@@ -60,7 +60,7 @@ constexpr int kMaxRedo = 64;          // items a CTA can note for the exact pass
 
 // kSFull, kPReady, kPVDone: 2 * tile + parity of the block (on_block); kDrain: one per issuing warp; kMerge: 4 * tile + quarter of the rows; kTabDone,
 // kTabReady: all softmax warps are through with the old table, have written the new one
-enum Bar { kQFull = 0, kQEmpty = 2, kSFull = 4, kPReady = 8, kPVDone = 12, kDrain = 16, kMerge = 19, kTabDone = 27, kTabReady, kKFull,
+enum Bar { kQFull = 0, kQEmpty = 2, kSFull = 4, kPReady = 8, kPVDone = 12, kDrain = 16, kMerge = 19, kTabDone = 27, kTabReady, kItems, kKFull,
            kKEmpty = kKFull + kStages, kVFull = kKEmpty + kStages, kVEmpty = kVFull + kStages, kNumBars = kVEmpty + kStages };
 
 constexpr uint32_t kHalfOnes = kContentBytes / 2;
@@ -76,7 +76,8 @@ constexpr uint32_t kOffMisc = kOffBar + kNumBars * 8;                  // tmem b
 constexpr uint32_t kOffRedo = kOffMisc + 16;                           // [kMaxRedo] item ordinals of the exact pass
 constexpr uint32_t kOffMerge = (kOffRedo + kMaxRedo * 4 + 15) & ~15u;  // [2 item parities][2 tiles][2 halves][128 rows] (max, sum)
 constexpr uint32_t kOffLists = kOffMerge + 8 * kTile * 8;              // PatchLists
-constexpr uint32_t kOffTable = kOffLists + sizeof(PatchLists);         // [(2M-1)^2] fp32
+constexpr uint32_t kOffItems = (kOffLists + sizeof(PatchLists) + 15) & ~15u;      // ItemRing
+constexpr uint32_t kOffTable = kOffItems + sizeof(ItemRing);           // [(2M-1)^2] fp32
 constexpr uint32_t smem_bytes(int M) { return kOffTable + 4u * (2 * M - 1) * (2 * M - 1) + 1024; }      // + slack for manual alignment
 static_assert(smem_bytes(kBiasMaxWindow) <= 232448, "shared memory of one CTA");
 
@@ -299,6 +300,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             for (int q4 = 0; q4 < 4; ++q4) mbar_init(bar(kMerge + 4 * i + q4), 2);
         }
         for (int i = 0; i < 4; ++i) { mbar_init(bar(kSFull + i), 1); mbar_init(bar(kPVDone + i), 1); mbar_init(bar(kPReady + i), 8); }
+        mbar_init(bar(kItems), 1);
         for (int i = 0; i < 3; ++i) mbar_init(bar(kDrain + i), 1);
         mbar_init(bar(kTabDone), kSoftmaxThreads / 32); mbar_init(bar(kTabReady), kSoftmaxThreads / 32);
         for (int s = 0; s < kStages; ++s) {     // keys: one commit of the S issuer; values: one commit of each PV issuer
@@ -325,6 +327,8 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
     PatchLists* const lists = reinterpret_cast<PatchLists*>(base_ptr + kOffLists);
     fill_patch_lists(p.g, p.M, lists, threadIdx.x, kThreads);
+    ItemRing* const items = reinterpret_cast<ItemRing*>(base_ptr + kOffItems);
+    auto items_ready = [&](uint32_t n) { return !ItemRing::begins(n) || mbar_wait_warp(bar(kItems), ItemRing::parity(n), abort_flag, p.status); };
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -332,6 +336,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
     // Role state that carries over from the first pass to the exact pass: block and item counters give the barrier phases.
     uint32_t blk = 0, io = 0, ntable = 0;
+    uint32_t ni = 0;                                        // place in the ring of items: each pass begins with a new eight
     int table_head = -1;
     uint32_t sb = warp == 3 || warp >= 12 ? 1u : 0u;        // score buffer of the next unit: (2 blk + tile) mod kBuffers
     uint32_t q_armed = 0, k_armed = 0, v_armed = 0;
@@ -345,26 +350,34 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const int count = all_items ? my_items : noted;
         auto item_at = [&](int i) { return first_item + (all_items ? i : redo_list[i]); };
 
+        ni = (ni + ItemRing::kEight - 1) / ItemRing::kEight * ItemRing::kEight;
         if (warp == 0) {
-            // ============================================================ TMA producer (one lane)
-            if (lane == 0) {
-                auto box = [&](const LiveItem& c, int sp, int& Y0, int& X0) {          // beyond the last patch lies nothing: zeros
-                    patch_place(geom, lists, c, sp, Y0, X0);
-                    if (sp >= c.patches) X0 = p.Wp;
-                };
-                for (int i = 0; i < count && ok; ++i, ++io) {
-                    const LiveItem c = decode_bias_item(p.g, item_at(i));
+            // ============================================================ TMA producer: one lane, the others decode items
+            auto box = [&](const LiveItem& c, int sp, int& Y0, int& X0) {          // beyond the last patch lies nothing: zeros
+                patch_place(geom, lists, c, sp, Y0, X0);
+                if (sp >= c.patches) X0 = p.Wp;
+            };
+            for (int i = 0; i < count && ok; ++i, ++io, ++ni) {
+                if (ItemRing::begins(ni)) {
+                    if (lane < ItemRing::kEight && i + lane < count) items->at(ni + lane) = decode_bias_item(p.g, item_at(i + lane));
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(kItems));
+                }
+                if (lane == 0) {
+                    const LiveItem c = items->at(ni);
                     const uint32_t buf = io & 1;
-                    if (io >= 2 && !mbar_wait(bar(kQEmpty + buf), ((io >> 1) - 1) & 1, abort_flag, p.status)) { ok = false; break; }
-                    mbar_arrive_expect_tx(bar(kQFull + buf), 2 * kContentBytes);
-                    ++q_armed;
-                    for (int qp = 0; qp < 4; ++qp) {
-                        int Y0, X0;
-                        box(c, 4 * c.tp + qp, Y0, X0);
-                        tma_load_5d(base + kOffQ + 2 * buf * kContentBytes + qp * kPatchContent, &tm_q, bar(kQFull + buf), 0, c.h, X0, Y0, c.b);
+                    if (io >= 2) ok = mbar_wait(bar(kQEmpty + buf), ((io >> 1) - 1) & 1, abort_flag, p.status);
+                    if (ok) {
+                        mbar_arrive_expect_tx(bar(kQFull + buf), 2 * kContentBytes);
+                        ++q_armed;
+                        for (int qp = 0; qp < 4; ++qp) {
+                            int Y0, X0;
+                            box(c, 4 * c.tp + qp, Y0, X0);
+                            tma_load_5d(base + kOffQ + 2 * buf * kContentBytes + qp * kPatchContent, &tm_q, bar(kQFull + buf), 0, c.h, X0, Y0, c.b);
+                        }
                     }
                     const int nb = (c.patches + 1) >> 1;
-                    for (int j = 0; j < nb; ++j, ++blk) {
+                    for (int j = 0; j < nb && ok; ++j, ++blk) {
                         const uint32_t st = blk % kStages, use = blk / kStages;
                         if (use > 0 && !mbar_wait(bar(kKEmpty + st), (use - 1) & 1, abort_flag, p.status)) { ok = false; break; }
                         mbar_arrive_expect_tx(bar(kKFull + st), kContentBytes);
@@ -381,22 +394,24 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                             tma_load_5d(base + kOffV + st * kContentBytes + sub * kPatchContent, &tm_v, bar(kVFull + st), 0, c.h, X0[sub], Y0[sub], c.b);
                     }
                 }
-                if (!ok) {
-                    // Gave up: let the copies already in flight land before the CTA may exit.
-                    for (uint32_t b2 = q_armed > 2u ? q_armed - 2 : 0; b2 < q_armed; ++b2)
-                        mbar_wait(bar(kQFull + (b2 & 1)), (b2 >> 1) & 1, abort_flag + 1, p.status);
-                    for (uint32_t b2 = k_armed > (uint32_t)kStages ? k_armed - kStages : 0; b2 < k_armed; ++b2)
-                        mbar_wait(bar(kKFull + b2 % kStages), (b2 / kStages) & 1, abort_flag + 1, p.status);
-                    for (uint32_t b2 = v_armed > (uint32_t)kStages ? v_armed - kStages : 0; b2 < v_armed; ++b2)
-                        mbar_wait(bar(kVFull + b2 % kStages), (b2 / kStages) & 1, abort_flag + 1, p.status);
-                }
+                ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+            }
+            if (lane == 0 && !ok) {
+                // Gave up: let the copies already in flight land before the CTA may exit.
+                for (uint32_t b2 = q_armed > 2u ? q_armed - 2 : 0; b2 < q_armed; ++b2)
+                    mbar_wait(bar(kQFull + (b2 & 1)), (b2 >> 1) & 1, abort_flag + 1, p.status);
+                for (uint32_t b2 = k_armed > (uint32_t)kStages ? k_armed - kStages : 0; b2 < k_armed; ++b2)
+                    mbar_wait(bar(kKFull + b2 % kStages), (b2 / kStages) & 1, abort_flag + 1, p.status);
+                for (uint32_t b2 = v_armed > (uint32_t)kStages ? v_armed - kStages : 0; b2 < v_armed; ++b2)
+                    mbar_wait(bar(kVFull + b2 % kStages), (b2 / kStages) & 1, abort_flag + 1, p.status);
             }
             __syncwarp();
         } else if (warp == 1) {
             // ===================================== issuer of S = Q K^T for both query tiles
             constexpr uint64_t kDesc64 = smem_desc_const(16, 512, kSwizzle64B);
-            for (int i = 0; i < count && ok; ++i, ++io) {
-                    const LiveItem c = decode_bias_item(p.g, item_at(i));
+            for (int i = 0; i < count && ok; ++i, ++io, ++ni) {
+                if (!items_ready(ni)) { ok = false; break; }
+                const LiveItem c = items->at(ni);
                 const uint32_t buf = io & 1;
                 if (!mbar_wait_warp(bar(kQFull + buf), (io >> 1) & 1, abort_flag, p.status)) { ok = false; break; }
                 const int nb = (c.patches + 1) >> 1;
@@ -432,8 +447,9 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             constexpr uint64_t kDesc64 = smem_desc_const(16, 512, kSwizzle64B);
             const uint32_t d_o = tmem + kColO + qt * 2 * kD;              // exact form: one accumulator per key half
             const uint32_t d_o1 = tmem + kColO + qt * kFastOCols;         // fast form: one accumulator
-            for (int i = 0; i < count && ok; ++i, ++io) {
-                    const LiveItem c = decode_bias_item(p.g, item_at(i));
+            for (int i = 0; i < count && ok; ++i, ++ni) {
+                if (!items_ready(ni)) { ok = false; break; }
+                const LiveItem c = items->at(ni);
                 const int nb = (c.patches + 1) >> 1;
                 for (int j = 0; j < nb; ++j, ++blk) {
                     const uint32_t st = blk % kStages;
@@ -503,7 +519,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     return Place{c.b, sp >= c.patches || Y >= p.H || X >= p.W ? -1 : Y * p.W + X, c.h};
                 };
                 auto epilogue = [&](int i) {
-                    const Place place = place_of(decode_bias_item(p.g, item_at(i)));
+                    const Place place = place_of(items->at(i));
                     const bool no_query = place.pixel < 0;
                     const size_t map_pixels = (size_t)p.H * p.W, tok = (place.b * map_pixels + place.pixel) * p.heads + place.h;
                     uint32_t o[16], lsum[1];
@@ -534,8 +550,9 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     }
                     if (p.lse && half == 0) p.lse[((size_t)place.b * p.heads + place.h) * map_pixels + place.pixel] = logf(l_all);
                 };
-                for (int i = 0; i < count && ok; ++i, ++io) {
-                    const LiveItem c = decode_bias_item(p.g, item_at(i));
+                for (int i = 0; i < count && ok; ++i) {              // (the first pass: item i is the ring's i-th)
+                    if (!items_ready(i)) { ok = false; break; }
+                    const LiveItem c = items->at(i);
                     if (!need_table(c.h)) { ok = false; break; }
                     const int nb = (c.patches + 1) >> 1;
                     // table entry of the thread's first row and a key at the window's origin, plus its place among a key row's pairs
