@@ -855,6 +855,11 @@ def rib_window_attn_bwd_checkpointed(q, k, v, out, pq, pk, lse, dout, window, sh
     """Backward pass of a layer that kept q, k, v and out as checkpoints (codes, scales); pq, pk [n, r] or [heads, n, r].  On a map whose
     sides are not multiples of the window as rib_window_attn_bwd_padded, with `masked` as rib_window_attn_bwd_masked.
     Returns (dq, dk, dv bf16, dpq, dpk fp32 of the shape of pq)."""
+    if _marshal is not None:
+        call = lambda address, *args: _marshal.bwd_checkpointed(address, _lib.rib_addresses["rib_window_attn_bwd_checkpointed_workspace"], *args)  # noqa: E731
+        got = _native(call, "rib_window_attn_bwd_checkpointed", q, k, v, out, pq, pk, lse, dout, window, shift, masked, workspace, stream)
+        if got is not None:
+            return got
     saved = _saved(q, k, v, out, dout)
     B, H, W, heads, d = dout.shape
     n = window * window
@@ -885,6 +890,11 @@ def rib_window_attn_bwd_checkpointed(q, k, v, out, pq, pk, lse, dout, window, sh
 def rib_window_attn_bwd_bucketed_checkpointed(q, k, v, out, bias, buckets, lse, dout, window, shift=0, masked=False, workspace=None, stream=None):
     """Backward pass of rib_window_attn_fwd_bucketed for a layer that kept q, k, v and out as checkpoints (codes, scales).
     Returns (dq, dk, dv bf16, dbias of bias's shape and type)."""
+    if _marshal is not None:
+        call = lambda address, *args: _marshal.bwd_bucketed_checkpointed(address, _lib.rib_addresses["rib_window_attn_bwd_bucketed_checkpointed_workspace"], *args)  # noqa: E731
+        got = _native(call, "rib_window_attn_bwd_bucketed_checkpointed", q, k, v, out, bias, buckets, lse, dout, window, shift, masked, workspace, stream)
+        if got is not None:
+            return got
     saved = _saved(q, k, v, out, dout)
     B, H, W, heads, d = dout.shape
     dtype, stride, count = _check_bias(bias, buckets, heads, window, dout.device)

@@ -65,19 +65,22 @@ bool get_stream(PyObject* o, void** s)
 
 struct Image { const at::Tensor *q, *k, *v, *pq, *pk; int B, H, W, heads, d, r, n, window, shift; long long stride; };
 
-// q, k, v of one shape [B, H, W, heads, d] and the tables [n, r] (tables: 1), [heads, n, r] (2) or either (3)
-bool get_image(PyObject* const* a, int tables, PyObject* window, PyObject* shift, Image* m)
+// the sides of an image [B, H, W, heads, d], and the window
+bool get_sides(const at::Tensor& image, PyObject* window, PyObject* shift, Image* m)
 {
-    m->q = plain(a[0], at::kBFloat16, 5); m->k = plain(a[1], at::kBFloat16, 5); m->v = plain(a[2], at::kBFloat16, 5);
-    if (!m->q || !m->k || !m->v || m->k->sizes() != m->q->sizes() || m->v->sizes() != m->q->sizes()) return false;
     if (!get_int(window, &m->window) || !get_int(shift, &m->shift) || m->window < 1 || m->window > 32768) return false;
-    const auto s = m->q->sizes();
+    const auto s = image.sizes();
     for (int i = 0; i < 5; ++i) if (s[i] > (1ll << 30)) return false;
     m->B = (int)s[0]; m->H = (int)s[1]; m->W = (int)s[2]; m->heads = (int)s[3]; m->d = (int)s[4];
     m->n = m->window * m->window;
+    return true;
+}
+// the tables a[0], a[1]: [n, r] (tables: 1), [heads, n, r] (2) or either (3)
+bool get_tables(PyObject* const* a, int tables, Image* m)
+{
     for (int dim = 2; dim <= 3; ++dim) {
         if (!(tables & (dim - 1))) continue;
-        m->pq = plain(a[3], at::kBFloat16, dim); m->pk = plain(a[4], at::kBFloat16, dim);
+        m->pq = plain(a[0], at::kBFloat16, dim); m->pk = plain(a[1], at::kBFloat16, dim);
         if (!m->pq || !m->pk) continue;
         if (m->pq->size(dim - 2) != m->n || m->pk->size(dim - 2) != m->n) return false;
         if (dim == 3 && (m->pq->size(0) != m->heads || m->pk->size(0) != m->heads)) return false;
@@ -87,6 +90,13 @@ bool get_image(PyObject* const* a, int tables, PyObject* window, PyObject* shift
         return true;
     }
     return false;
+}
+// q, k, v of one shape [B, H, W, heads, d] and the tables
+bool get_image(PyObject* const* a, int tables, PyObject* window, PyObject* shift, Image* m)
+{
+    m->q = plain(a[0], at::kBFloat16, 5); m->k = plain(a[1], at::kBFloat16, 5); m->v = plain(a[2], at::kBFloat16, 5);
+    if (!m->q || !m->k || !m->v || m->k->sizes() != m->q->sizes() || m->v->sizes() != m->q->sizes()) return false;
+    return get_sides(*m->q, window, shift, m) && get_tables(a + 3, tables, m);
 }
 
 // The types of the C calls, from their header: a signature that changes there does not compile here.
@@ -218,11 +228,7 @@ bool get_maps(PyObject* const* a, PyObject* window, PyObject* shift, Image* m)
 {
     m->q = plain(a[0], at::kBFloat16, 5); m->k = plain(a[1], at::kBFloat16, 5); m->v = plain(a[2], at::kBFloat16, 5);
     if (!m->q || !m->k || !m->v || m->k->sizes() != m->q->sizes() || m->v->sizes() != m->q->sizes()) return false;
-    if (!get_int(window, &m->window) || !get_int(shift, &m->shift) || m->window < 1 || m->window > 32768) return false;
-    const auto s = m->q->sizes();
-    for (int i = 0; i < 5; ++i) if (s[i] > (1ll << 30)) return false;
-    m->B = (int)s[0]; m->H = (int)s[1]; m->W = (int)s[2]; m->heads = (int)s[3]; m->d = (int)s[4];
-    return true;
+    return get_sides(*m->q, window, shift, m);
 }
 
 // fwd_bucketed(address, q, k, v, bias, buckets, window, shift, masked, want_lse, stream)
@@ -330,6 +336,80 @@ PyObject* restore(PyObject*, PyObject* const* a, Py_ssize_t count)
     });
 }
 
+// a checkpoint (codes, scales) of a tensor of dout's shape
+bool get_saved(PyObject* pair, const at::Tensor& dout, rib_checkpoint* saved)
+{
+    if (!PyTuple_CheckExact(pair) || PyTuple_GET_SIZE(pair) != 2) return false;
+    const at::Tensor *codes = plain(PyTuple_GET_ITEM(pair, 0), at::kChar, 5), *scales = plain(PyTuple_GET_ITEM(pair, 1), at::kFloat, 4);
+    if (!codes || !scales || codes->sizes() != dout.sizes() || scales->sizes() != dout.sizes().slice(0, 4) || !here({codes, scales})) return false;
+    saved->codes = codes->const_data_ptr();
+    saved->scales = scales->const_data_ptr<float>();
+    return true;
+}
+// what the two passes below share: the checkpoints a[0 .. 3], lse, dout, the window, and a workspace or None
+struct Kept { Image m; rib_checkpoint saved[4]; const at::Tensor *lse, *dout, *given; void* stream; };
+bool get_kept(PyObject* const* pairs, PyObject* lse, PyObject* dout, PyObject* window, PyObject* shift, PyObject* masked, PyObject* workspace, PyObject* stream, Kept* x)
+{
+    x->lse = plain(lse, at::kFloat, 4); x->dout = plain(dout, at::kBFloat16, 5);
+    if (!x->lse || !x->dout || !get_sides(*x->dout, window, shift, &x->m) || !PyBool_Check(masked) || !get_stream(stream, &x->stream) || !here({x->lse, x->dout})) return false;
+    const Image& m = x->m;
+    if (x->lse->size(0) != m.B || x->lse->size(1) != m.heads || x->lse->size(2) != m.H || x->lse->size(3) != m.W) return false;
+    for (int i = 0; i < 4; ++i) if (!get_saved(pairs[i], *x->dout, x->saved + i)) return false;
+    x->given = workspace == Py_None ? nullptr : plain(workspace, at::kByte, 1);
+    return workspace == Py_None || (x->given && here({x->given}));
+}
+
+// bwd_checkpointed(address, address of the workspace's size, q, k, v, out, pq, pk, lse, dout, window, shift, masked, workspace or None, stream)
+PyObject* bwd_checkpointed(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        Kept x;
+        if (count != 15 || modes_active() || !get_kept(a + 2, a[8], a[9], a[10], a[11], a[12], a[13], a[14], &x) || !get_tables(a + 6, 3, &x.m) || !here({x.m.pq, x.m.pk})) Py_RETURN_NONE;
+        const Image& m = x.m;
+        const auto fn = reinterpret_cast<decltype(&rib_window_attn_bwd_checkpointed)>(address(a[0]));
+        const auto need = reinterpret_cast<decltype(&rib_window_attn_bwd_checkpointed_workspace)>(address(a[1]));
+        const auto f32 = x.dout->options().dtype(at::kFloat);
+        at::Tensor dq, dk, dv, dpq, dpk, ws;
+        int rc;
+        {
+            const Unlocked unlocked;
+            dq = at::empty_like(*x.dout); dk = at::empty_like(*x.dout); dv = at::empty_like(*x.dout);
+            dpq = at::empty(m.pq->sizes(), f32); dpk = at::empty(m.pq->sizes(), f32);
+            ws = x.given ? *x.given : at::empty({(int64_t)need(m.stride, m.B, m.H, m.W, m.heads, m.d, m.r, m.window) + 256}, x.dout->options().dtype(at::kByte));
+            rc = fn(x.saved, m.pq->const_data_ptr(), m.pk->const_data_ptr(), m.stride, x.lse->const_data_ptr<float>(), x.dout->const_data_ptr(), m.B, m.H, m.W, m.heads, m.d, m.r,
+                    m.window, m.shift, a[12] == Py_True, dq.mutable_data_ptr(), dk.mutable_data_ptr(), dv.mutable_data_ptr(), dpq.mutable_data_ptr<float>(),
+                    dpk.mutable_data_ptr<float>(), ws.mutable_data_ptr(), (size_t)ws.numel(), x.stream);
+        }
+        if (rc) return status(rc);
+        return results({&dq, &dk, &dv, &dpq, &dpk});
+    });
+}
+
+// bwd_bucketed_checkpointed(address, address of the workspace's size, q, k, v, out, bias, buckets, lse, dout, window, shift, masked, workspace or None, stream)
+PyObject* bwd_bucketed_checkpointed(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        Kept x;
+        Bias b;
+        if (count != 15 || modes_active() || !get_kept(a + 2, a[8], a[9], a[10], a[11], a[12], a[13], a[14], &x) || !get_bias(a[6], a[7], x.m, &b) || !here({b.table, b.buckets})) Py_RETURN_NONE;
+        const Image& m = x.m;
+        const auto fn = reinterpret_cast<decltype(&rib_window_attn_bwd_bucketed_checkpointed)>(address(a[0]));
+        const auto need = reinterpret_cast<decltype(&rib_window_attn_bwd_bucketed_checkpointed_workspace)>(address(a[1]));
+        at::Tensor dq, dk, dv, dbias, ws;
+        int rc;
+        {
+            const Unlocked unlocked;
+            dq = at::empty_like(*x.dout); dk = at::empty_like(*x.dout); dv = at::empty_like(*x.dout); dbias = at::empty_like(*b.table);
+            ws = x.given ? *x.given : at::empty({(int64_t)need(b.stride, b.count, m.B, m.H, m.W, m.heads, m.d, m.window) + 256}, x.dout->options().dtype(at::kByte));
+            rc = fn(x.saved, b.table->const_data_ptr(), b.dtype, b.stride, b.buckets->const_data_ptr<int>(), b.count, x.lse->const_data_ptr<float>(), x.dout->const_data_ptr(),
+                    m.B, m.H, m.W, m.heads, m.d, m.window, m.shift, a[12] == Py_True, dq.mutable_data_ptr(), dk.mutable_data_ptr(), dv.mutable_data_ptr(), dbias.mutable_data_ptr(),
+                    ws.mutable_data_ptr(), (size_t)ws.numel(), x.stream);
+        }
+        if (rc) return status(rc);
+        return results({&dq, &dk, &dv, &dbias});
+    });
+}
+
 struct Generator { const at::Tensor *w_h, *b_h, *w_pq, *w_pk; int window, L, dh, r; void* stream; };
 
 bool get_generator(PyObject* const* w, PyObject* window, PyObject* stream, Generator* g)
@@ -392,6 +472,8 @@ PyMethodDef methods[] = {
     {"bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bwd)), METH_FASTCALL, nullptr},
     {"fwd_bucketed", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(fwd_bucketed)), METH_FASTCALL, nullptr},
     {"bwd_bucketed", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bwd_bucketed)), METH_FASTCALL, nullptr},
+    {"bwd_checkpointed", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bwd_checkpointed)), METH_FASTCALL, nullptr},
+    {"bwd_bucketed_checkpointed", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bwd_bucketed_checkpointed)), METH_FASTCALL, nullptr},
     {"store", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(store)), METH_FASTCALL, nullptr},
     {"restore", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(restore)), METH_FASTCALL, nullptr},
     {"generate", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(generate)), METH_FASTCALL, nullptr},
