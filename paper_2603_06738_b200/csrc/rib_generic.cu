@@ -59,8 +59,8 @@ __device__ inline float pair_bias(const Problem& p, int h, int i, int j)
     const int u = __ldg(p.buckets + bias_offset(p, i, j));
     return (unsigned)u < (unsigned)p.num_buckets ? bias_at(p.bias, p.bias_bf16, (long long)h * p.bias_head_stride + u) : -INFINITY;
 }
-// exp(s - lse).  A row without any key has lse = -inf, and so has every s of it.
-__device__ inline float probability(float s, float lse) { return s == -INFINITY ? 0.f : expf(s - lse); }
+// exp(s - lse).  A row that a bias leaves no key has lse = -inf, and so has every s of it; without a bias such a row is one of infinite inputs, and NaN.
+__device__ inline float probability(const Problem& p, float s, float lse) { return p.bias && s == -INFINITY ? 0.f : expf(s - lse); }
 
 // element offset of channel 0 of token i of the pair in a [B][H][W][heads][d] tensor (the token must exist)
 __device__ inline size_t token_offset(const Problem& p, const PairCoord& c, int i)
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kThreads) generic_fwd_kernel(const Problem p)
         const int i = row0 + warp * kRowsPerWarp + rr;
         if (i >= p.n || !token_exists(p, c, i)) continue;
         const size_t off = token_offset(p, c, i);
-        const float inv = l[rr] > 0.f ? 1.f / l[rr] : 0.f;          // (0: a bias that leaves the row no key)
+        const float inv = p.bias && l[rr] == 0.f ? 0.f : 1.f / l[rr];          // (0: a bias that leaves the row no key)
         const float g0 = p.gate && lane < p.d ? __bfloat162float(p.gate[off + lane]) : 1.f;            // Eq. 9
         const float g1 = p.gate && lane + 32 < p.d ? __bfloat162float(p.gate[off + lane + 32]) : 1.f;
         if (lane < p.d) p.out_w[off + lane] = __float2bfloat16_rn(o[rr][0] * inv * g0);
@@ -256,8 +256,8 @@ __global__ void __launch_bounds__(kThreads) generic_bwd_dq_kernel(const Problem 
             // keys beyond the window or, on an extended map, beyond the image have probability 0
             const int qi = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
             if (p.bias) { s0 += pair_bias(p, c.h, qi, min(j0 + lane, p.n - 1)); s1 += pair_bias(p, c.h, qi, min(j0 + lane + 32, p.n - 1)); }
-            const float p0 = j0 + lane < p.n && token_exists(p, c, j0 + lane) && pair_allowed(p, c, qi, j0 + lane) ? probability(s0, lse[rr]) : 0.f;
-            const float p1 = j0 + lane + 32 < p.n && token_exists(p, c, j0 + lane + 32) && pair_allowed(p, c, qi, j0 + lane + 32) ? probability(s1, lse[rr]) : 0.f;
+            const float p0 = j0 + lane < p.n && token_exists(p, c, j0 + lane) && pair_allowed(p, c, qi, j0 + lane) ? probability(p, s0, lse[rr]) : 0.f;
+            const float p1 = j0 + lane + 32 < p.n && token_exists(p, c, j0 + lane + 32) && pair_allowed(p, c, qi, j0 + lane + 32) ? probability(p, s1, lse[rr]) : 0.f;
             float* srow = Ss + (warp * kRowsPerWarp + rr) * kTile;
             const float ds0 = p0 * (g0 - Di[rr]), ds1 = p1 * (g1 - Di[rr]);
             srow[lane] = ds0;
@@ -344,8 +344,8 @@ __global__ void __launch_bounds__(kThreads) generic_bwd_dkv_kernel(const Problem
             }
             const int kj = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
             if (p.bias) { s0 += pair_bias(p, c.h, min(i0 + lane, p.n - 1), kj); s1 += pair_bias(p, c.h, min(i0 + lane + 32, p.n - 1), kj); }
-            const float p0 = i0 + lane < p.n && pair_allowed(p, c, i0 + lane, kj) ? probability(s0, Lt[lane]) : 0.f;
-            const float p1 = i0 + lane + 32 < p.n && pair_allowed(p, c, i0 + lane + 32, kj) ? probability(s1, Lt[lane + 32]) : 0.f;
+            const float p0 = i0 + lane < p.n && pair_allowed(p, c, i0 + lane, kj) ? probability(p, s0, Lt[lane]) : 0.f;
+            const float p1 = i0 + lane + 32 < p.n && pair_allowed(p, c, i0 + lane + 32, kj) ? probability(p, s1, Lt[lane + 32]) : 0.f;
             float* prow = Ps + (warp * kRowsPerWarp + rr) * kTile;
             float* srow = Ss + (warp * kRowsPerWarp + rr) * kTile;
             prow[lane] = p0; prow[lane + 32] = p1;
