@@ -671,23 +671,23 @@ __device__ __forceinline__ bool decode_token(const AuxParams& p, int index, int 
     return Y < p.H && X < p.W;
 }
 
-// Four lanes per (pair, token in window order), 8 channels each: D = dO . O and lse in the layout the main kernel streams; the dQ accumulators and
+// kLanes (2 for heads of up to 16 channels, else 4) per (pair, token in window order), 8 channels each: D = dO . O and lse in the layout the main kernel streams; the dQ accumulators and
 // the sums of the bias gradient are cleared as flat arrays.  A query that is no token, or whose row has no key (lse = -inf), has a score far below
 // all others: probability 0.
 // kSaved: q, k, v and out are checkpoints; the first three are restored to where the main kernel reads them.
-template <bool kSaved>
-__global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxParams p)
+template <bool kSaved, int kLanes>
+__global__ void __launch_bounds__(64 * kLanes) rib_bias_bwd_prepare_kernel(const AuxParams p)
 {
     const size_t total = (size_t)p.patches * 64;
-    const size_t thread = (size_t)blockIdx.x * blockDim.x + threadIdx.x, t = thread >> 2;        // (a block has a patch)
-    const int part = (int)(thread & 3);
+    const size_t thread = (size_t)blockIdx.x * blockDim.x + threadIdx.x, t = thread / kLanes;        // (a block has a patch)
+    const int part = threadIdx.x % kLanes;
     const size_t nthreads = (size_t)gridDim.x * blockDim.x;
     for (size_t e = thread; e < p.sum_words; e += nthreads) p.sums[e] = 0.0;
     constexpr uint32_t kNone = 0xF149u;                    // -1e30 in bf16
     if (thread < 64) p.ld[total + thread] = make_uint4(kNone, 0u, 0u, 0u);       // the patch of no queries
     int pair, patch;
     size_t tok, scalar;
-    const bool real = decode_token(p, blockIdx.x, threadIdx.x >> 2, pair, patch, tok, scalar);
+    const bool real = decode_token(p, blockIdx.x, threadIdx.x / kLanes, pair, patch, tok, scalar);
     uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
     float lse = -INFINITY;
     if (real && 8 * part < p.d) {
@@ -710,8 +710,8 @@ __global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxPara
     }
     float4* z4 = reinterpret_cast<float4*>(p.dq_acc);      // pairs * d * n floats
 #pragma unroll
-    for (int k = 0; k < kD / 16; ++k)
-        if (k * 4 * total + thread < total * (p.d / 4)) z4[k * 4 * total + thread] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < 2; ++k)
+        if (k * kLanes * total + thread < total * (p.d / 4)) z4[k * kLanes * total + thread] = make_float4(0.f, 0.f, 0.f, 0.f);
     const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
     float acc = 0.f;
 #pragma unroll
@@ -720,7 +720,7 @@ __global__ void __launch_bounds__(256) rib_bias_bwd_prepare_kernel(const AuxPara
         acc = fmaf(__uint_as_float(xs[k] & 0xffff0000u), __uint_as_float(ys[k] & 0xffff0000u), acc);
     }
     acc += __shfl_xor_sync(0xffffffffu, acc, 1);
-    acc += __shfl_xor_sync(0xffffffffu, acc, 2);
+    if (kLanes > 2) acc += __shfl_xor_sync(0xffffffffu, acc, 2);
     if (part == 0) {
         uint32_t l[3], d[3];
         three_parts(-lse * p.sqrt_d, l);
@@ -796,7 +796,9 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     ap.sqrt_d = sqrtf((float)p.d);
     ap.inv_sqrt_d = 1.f / ap.sqrt_d;
     const size_t tokens = (size_t)p.pairs * p.n;
-    { ProfileScope scope(RIB_KERNEL_BIAS_BWD_PREPARE, stream); (p.saved ? rib_bias_bwd_prepare_kernel<true> : rib_bias_bwd_prepare_kernel<false>)<<<ap.patches, 256, 0, stream>>>(ap); }
+    const auto prepare = p.d <= 16 ? (p.saved ? rib_bias_bwd_prepare_kernel<true, 2> : rib_bias_bwd_prepare_kernel<false, 2>)
+                                   : (p.saved ? rib_bias_bwd_prepare_kernel<true, 4> : rib_bias_bwd_prepare_kernel<false, 4>);
+    { ProfileScope scope(RIB_KERNEL_BIAS_BWD_PREPARE, stream); prepare<<<ap.patches, p.d <= 16 ? 128 : 256, 0, stream>>>(ap); }
     if (cudaError_t e = cudaGetLastError()) return e;
     bp.ld = ld; bp.dq_acc = dq_acc; bp.blocks = grad.blocks; bp.status = p.status;
     bp.no_queries = (long long)tokens;
