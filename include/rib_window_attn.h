@@ -385,6 +385,9 @@ long long rib_kernel_launches(void);
  * query) and is the same for all heads; several offsets may share a bucket.  A key whose offset has a bucket outside
  * [0, num_buckets) (-1, say) or a bias of -1e30 or less (minus infinity, the lowest value of a type) is not attended to.  A row that
  * is left without any key gets out = 0 and lse = -infinity, and no gradient.  Other biases are finite.
+ * Infinities and NaN in a row of q or k reach out and lse of the rows that attend to it, and no others of the forward pass; those in v reach every row of the
+ * window and head, with weight 0 (as in a product of matrices).  In the backward pass they may reach every gradient of the window and
+ * head, and dbias.
  *   bias     RIB_DTYPE_F32 or RIB_DTYPE_BF16, [heads][num_buckets], the heads' tables bias_head_stride (>= num_buckets) elements
  *            apart; bias_head_stride = 0: one table [num_buckets] that all heads share.  Aligned to its element type.
  *   buckets  int32 [2M-1][2M-1], 4-byte aligned.

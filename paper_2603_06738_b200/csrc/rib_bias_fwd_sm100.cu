@@ -245,7 +245,7 @@ __device__ __noinline__ void exact_items(const Params& p, uint8_t* base_ptr, Exa
         const float m_a = half ? other.x : m_used, l_a = half ? other.y : l;
         const float m_b = half ? m_used : other.x, l_b = half ? l : other.y;
         const float m = fmaxf(m_a, m_b);
-        const bool none = m == -INFINITY;                  // a row without any key: out 0, lse -inf
+        const bool none = m == -INFINITY && l_a == 0.f && l_b == 0.f;        // a row without any key: out 0, lse -inf (one of NaN: NaN)
         const float f_a = none ? 0.f : ex2_approx(m_a - m), f_b = none ? 0.f : ex2_approx(m_b - m);
         const float l_all = l_a * f_a + l_b * f_b;
         const float w_a = none ? 0.f : f_a / l_all, w_b = none ? 0.f : f_b / l_all;

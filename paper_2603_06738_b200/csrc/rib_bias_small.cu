@@ -215,10 +215,12 @@ __global__ void __launch_bounds__(2 * kMaxTokens) rib_bias_small_fwd_kernel(cons
                     const int2 keys = *reinterpret_cast<const int2*>(s.place + key + 16 * sub + 8 * t + c2);
                     float (&y)[4] = x[2 * sub + t];
                     const int ex = keys.x & 0xffff, ey = keys.y & 0xffff, px = keys.x >> 16, py = keys.y >> 16;
-                    y[0] = px == part0 ? fmaf(y[0], scale, bias0[ex]) : -INFINITY;
-                    y[1] = py == part0 ? fmaf(y[1], scale, bias0[ey]) : -INFINITY;
-                    y[2] = px == part1 ? fmaf(y[2], scale, bias1[ex]) : -INFINITY;
-                    y[3] = py == part1 ? fmaf(y[3], scale, bias1[ey]) : -INFINITY;
+                    // (a key that is not attended to counts as such whatever its own row holds)
+                    auto score = [&](float y, bool same, float b) { return same && b != -INFINITY ? fmaf(y, scale, b) : -INFINITY; };
+                    y[0] = score(y[0], px == part0, bias0[ex]);
+                    y[1] = score(y[1], py == part0, bias0[ey]);
+                    y[2] = score(y[2], px == part1, bias1[ex]);
+                    y[3] = score(y[3], py == part1, bias1[ey]);
                     most0 = fmaxf(most0, fmaxf(y[0], y[1]));
                     most1 = fmaxf(most1, fmaxf(y[2], y[3]));
                 }

@@ -59,6 +59,12 @@ __device__ inline float pair_bias(const Problem& p, int h, int i, int j)
     const int u = __ldg(p.buckets + bias_offset(p, i, j));
     return (unsigned)u < (unsigned)p.num_buckets ? bias_at(p.bias, p.bias_bf16, (long long)h * p.bias_head_stride + u) : -INFINITY;
 }
+// The score with that bias (a key that is not attended to counts as such whatever its own row holds).
+__device__ inline float with_bias(const Problem& p, int h, float s, int i, int j)
+{
+    const float b = pair_bias(p, h, i, j);
+    return b == -INFINITY ? -INFINITY : s + b;
+}
 // exp(s - lse).  A row that a bias leaves no key has lse = -inf, and so has every s of it; without a bias such a row is one of infinite inputs, and NaN.
 __device__ inline float probability(const Problem& p, float s, float lse) { return p.bias && s == -INFINITY ? 0.f : expf(s - lse); }
 
@@ -150,14 +156,15 @@ __global__ void __launch_bounds__(kThreads) generic_fwd_kernel(const Problem p)
                 s1 = fmaf(a, Kt[(lane + 32) * ldk + col], s1);
             }
             const int qi = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
-            if (p.bias) { s0 += pair_bias(p, c.h, qi, min(j0 + lane, p.n - 1)); s1 += pair_bias(p, c.h, qi, min(j0 + lane + 32, p.n - 1)); }
+            if (p.bias) { s0 = with_bias(p, c.h, s0, qi, min(j0 + lane, p.n - 1)); s1 = with_bias(p, c.h, s1, qi, min(j0 + lane + 32, p.n - 1)); }
             if (j0 + lane >= p.n || !token_exists(p, c, j0 + lane) || !pair_allowed(p, c, qi, j0 + lane)) s0 = -INFINITY;
             if (j0 + lane + 32 >= p.n || !token_exists(p, c, j0 + lane + 32) || !pair_allowed(p, c, qi, j0 + lane + 32)) s1 = -INFINITY;
             const float m_new = fmaxf(m[rr], warp_max(fmaxf(s0, s1)));
             // -inf only while no key of the row's window has been seen yet (extended maps): nothing to add then
             const bool none = m_new == -INFINITY;
             const float alpha = none ? 1.f : expf(m[rr] - m_new);
-            const float p0 = none ? 0.f : expf(s0 - m_new), p1 = none ? 0.f : expf(s1 - m_new);
+            // (under a bias such a row has l = 0 and is one without keys, unless its scores are no numbers)
+            const float p0 = none && !(p.bias && isnan(s0)) ? 0.f : expf(s0 - m_new), p1 = none && !(p.bias && isnan(s1)) ? 0.f : expf(s1 - m_new);
             l[rr] = l[rr] * alpha + warp_sum(p0 + p1);
             m[rr] = m_new;
             o[rr][0] *= alpha; o[rr][1] *= alpha;
@@ -255,7 +262,7 @@ __global__ void __launch_bounds__(kThreads) generic_bwd_dq_kernel(const Problem 
             }
             // keys beyond the window or, on an extended map, beyond the image have probability 0
             const int qi = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
-            if (p.bias) { s0 += pair_bias(p, c.h, qi, min(j0 + lane, p.n - 1)); s1 += pair_bias(p, c.h, qi, min(j0 + lane + 32, p.n - 1)); }
+            if (p.bias) { s0 = with_bias(p, c.h, s0, qi, min(j0 + lane, p.n - 1)); s1 = with_bias(p, c.h, s1, qi, min(j0 + lane + 32, p.n - 1)); }
             const float p0 = j0 + lane < p.n && token_exists(p, c, j0 + lane) && pair_allowed(p, c, qi, j0 + lane) ? probability(p, s0, lse[rr]) : 0.f;
             const float p1 = j0 + lane + 32 < p.n && token_exists(p, c, j0 + lane + 32) && pair_allowed(p, c, qi, j0 + lane + 32) ? probability(p, s1, lse[rr]) : 0.f;
             float* srow = Ss + (warp * kRowsPerWarp + rr) * kTile;
@@ -343,7 +350,7 @@ __global__ void __launch_bounds__(kThreads) generic_bwd_dkv_kernel(const Problem
                 g1 = fmaf(a, Gt[(lane + 32) * ldv + col], g1);
             }
             const int kj = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
-            if (p.bias) { s0 += pair_bias(p, c.h, min(i0 + lane, p.n - 1), kj); s1 += pair_bias(p, c.h, min(i0 + lane + 32, p.n - 1), kj); }
+            if (p.bias) { s0 = with_bias(p, c.h, s0, min(i0 + lane, p.n - 1), kj); s1 = with_bias(p, c.h, s1, min(i0 + lane + 32, p.n - 1), kj); }
             const float p0 = i0 + lane < p.n && pair_allowed(p, c, i0 + lane, kj) ? probability(p, s0, Lt[lane]) : 0.f;
             const float p1 = i0 + lane + 32 < p.n && pair_allowed(p, c, i0 + lane + 32, kj) ? probability(p, s1, Lt[lane + 32]) : 0.f;
             float* prow = Ps + (warp * kRowsPerWarp + rr) * kTile;

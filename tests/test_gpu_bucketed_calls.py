@@ -193,3 +193,51 @@ def test_more_than_2_31_elements(M, d, s):
     assert torch.equal(codes[B - 1], first[0][0]) and torch.equal(scales[B - 1], first[1][0])
     back = binding.rib_checkpoint_restore(codes, scales)
     assert torch.equal(back[B - 1], binding.rib_checkpoint_restore(*first)[0])
+
+
+@pytest.mark.parametrize("M,d,s", [(16, 32, 8), (32, 32, 16), (7, 20, 3), (16, 32, 3), (20, 10, 4)])
+@pytest.mark.parametrize("path", [binding.RIB_PATH_NONE, binding.RIB_PATH_GENERIC])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_rows_that_are_no_numbers(M, d, s, path, value):
+    """In q: that row of out and lse and no other.  In k, where half of the offsets are not attended to: the rows that attend to it and no others.  All
+    paths have the same rows.  (A row of q against keys whose channels have both signs: infinities of both signs, so NaN.)
+
+    The other rows of that window and head may come from the exact form of the softmax in place of the fast one.  P is rounded to bf16 in both, 2^-9 of
+    every weight and of their sum each, and out once more, so the two differ by at most (2 + 2 + 2) 2^-9 max |v|, as the weights add up to 1."""
+    B, H, W, heads = 1, 40, 33, 2
+    q, k, v, _, bias, named = make(B, H, W, heads, d, M, log_map(M), torch.float32, seed=10)
+    named = torch.where((torch.arange((2 * M - 1) ** 2).view(2 * M - 1, -1) * 7) % 5 < 2, -1, named).int()
+    named[M - 1, M - 1] = 0
+    old = binding.rib_set_path(path)
+    try:
+        clean, _ = binding.rib_window_attn_fwd_bucketed(*(t.cuda() for t in (q, k, v, bias, named)), M, s)
+        y, x = 5, 9
+        bad = q.clone()
+        bad[0, y, x, 1, 2] = value
+        out, lse = binding.rib_window_attn_fwd_bucketed(*(t.cuda() for t in (bad, k, v, bias, named)), M, s)
+        hit = torch.zeros(B, H, W, heads, dtype=torch.bool)
+        hit[0, y, x, 1] = True
+        assert torch.equal(torch.isnan(out).all(-1).cpu(), hit) and torch.equal(torch.isnan(out).any(-1).cpu(), hit)
+        assert torch.equal(torch.isnan(lse).cpu(), hit.permute(0, 3, 1, 2))
+        others = [out, clean]
+        bad = k.clone()
+        bad[0, y, x, 1] = value                                    # (against q of both signs: infinities of both signs or NaN, per row one of them)
+        out, _ = binding.rib_window_attn_fwd_bucketed(*(t.cuda() for t in (q, bad, v, bias, named)), M, s)
+    finally:
+        binding.rib_set_path(old)
+    place = lambda at, size: ((at - s) % (-(-size // M) * M))  # noqa: E731  (in the shifted map)
+    ky, kx = place(y, H), place(x, W)
+    most = 6 * 2.0 ** -9 * float(v.float().abs().max())
+    got, first, clean = out[0].float().cpu(), others[0][0].float().cpu(), others[1][0].float().cpu()
+    for Y in range(H):
+        for X in range(W):
+            qy, qx = place(Y, H), place(X, W)
+            near = qy // M == ky // M and qx // M == kx // M
+            attends = near and named[ky - qy + M - 1, kx - qx + M - 1] >= 0
+            bound = torch.tensor([0.0, most if near else 0.0])[:, None]
+            if (Y, X) != (y, x):
+                assert ((first[Y, X] - clean[Y, X]).abs() <= bound).all(), (Y, X)
+            if not attends:
+                assert ((got[Y, X] - clean[Y, X]).abs() <= bound).all(), (Y, X)
+            elif value != value:
+                assert torch.isnan(got[Y, X, 1]).all(), (Y, X)
