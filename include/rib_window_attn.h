@@ -413,7 +413,8 @@ int rib_window_attn_bwd_bucketed(const void* q, const void* k, const void* v, co
 /*
  * Activation checkpoints in 8 bits.  A row of d <= 64 bf16 channels (one token of one head) becomes d int8 codes and one fp32 scale,
  *     scale = max|x| * (1/127),   code = round(x / scale)   (half to even),   restored x = bf16(code * scale).
- * A row of zeros has scale 0.  A row that holds an infinity or a NaN has scale NaN and is restored as NaNs.  `rows` may be 0.
+ * A row of zeros has scale 0.  A row that holds an infinity or a NaN has scale NaN and is restored as NaNs.  `rows` may be 0, and is at
+ * most 2^31.
  *   x bf16 [rows][d], codes int8 [rows][d], scales fp32 [rows]; all 16-byte aligned.
  */
 int rib_checkpoint_store(const void* x, long long rows, int d, void* codes, float* scales, void* stream);

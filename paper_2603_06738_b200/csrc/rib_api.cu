@@ -703,7 +703,9 @@ int plan_restore(const rib_checkpoint* saved, int B, int H, int W, int heads, in
 {
     if (!saved) return RIB_ERR_NULL;
     if (B <= 0 || H <= 0 || W <= 0 || heads <= 0) return RIB_ERR_SHAPE;
-    r->rows = (long long)B * H * W * heads;
+    const __int128 rows = (__int128)B * H * W * heads;
+    if (rows > (1ll << 31)) return RIB_ERR_UNSUPPORTED;
+    r->rows = (long long)rows;
     r->d = d;
     for (int i = 0; i < 4; ++i)
         if (int rc = check_checkpoint(saved[i].codes, saved[i].scales, r->rows, d)) return rc;

@@ -91,3 +91,11 @@ def test_the_binding_checks_its_tensors():
             check(bias, m)
     with pytest.raises(ValueError):
         check(torch.zeros(2, 3), named, "meta")
+
+
+def test_checkpoints_of_too_many_rows_are_refused(lib):
+    """Sides whose product is beyond 64 bits as well."""
+    saved = (ctypes.c_void_p * 8)(*range(256, 256 * 9, 256))
+    for B, H, W, heads in ((1 << 16, 1 << 16, 16, 1), (1 << 30, 1 << 30, 1 << 30, 1 << 30), (1 << 30, 1 << 30, 16, 1 << 30)):
+        assert lib.rib_window_attn_bwd_bucketed_checkpointed(saved, 1024, 0, 9, 2048, 9, 8192, 12288, B, H, W, heads, 32, 16, 0, 0, 16384, 20480, 24576, 28672, 32768, 1 << 62, None) in (-2, -3)
+        assert lib.rib_window_attn_bwd_checkpointed(saved, 1024, 2048, 0, 8192, 12288, B, H, W, heads, 32, 16, 16, 0, 0, 16384, 20480, 24576, 28672, 30720, 32768, 1 << 62, None) in (-2, -3)

@@ -4,6 +4,8 @@ old values in the results, two graphs that share a workspace, and tensors of mor
 What is compared is compared bit by bit where the arithmetic has one order.  dq and dbias are sums of fp32 atomics, whose order may differ: their
 difference is a few rounding steps of the sums, 2^-24 each, of terms that are larger than the result by a factor that stays below 2^6 for the
 inputs here, and for what is rounded to bf16 behind it one step more of a few values: 1e-3 in relative L2 for those, 1e-5 for fp32."""
+import ctypes
+
 import pytest
 import torch
 
@@ -13,6 +15,7 @@ from test_gpu_bucketed import log_map, make
 from test_gpu_checkpoints import kept
 from test_gpu_marshal import both, same
 from test_gpu_overtaking import LATE
+from test_gpu_safety import Guarded
 
 pytestmark = pytest.mark.gpu
 
@@ -109,7 +112,6 @@ def layer(M, d, s, B=2, H=40, W=33, heads=2, masked=False, seed=5):
         assert rc == 0
         grads = [p(t) for t in results]
         if checkpointed:
-            import ctypes
             for t, (codes, scales) in zip((q, k, v, out), saved):
                 assert lib.rib_checkpoint_store(p(t), B * H * W * heads, d, p(codes), p(scales), stream) == 0
             array = (ctypes.c_void_p * 8)(*[p(t) for pair in saved for t in pair])
@@ -241,3 +243,44 @@ def test_rows_that_are_no_numbers(M, d, s, path, value):
                 assert ((got[Y, X] - clean[Y, X]).abs() <= bound).all(), (Y, X)
             elif value != value:
                 assert torch.isnan(got[Y, X, 1]).all(), (Y, X)
+
+
+# B, H, W, heads, d, M, s, masked: tcgen05 kernels (whole and cut patches, region mask, one short window), warp-level MMAs (every width of a load), any-shape
+GUARDED = [(2, 32, 48, 2, 32, 16, 8, False), (1, 35, 41, 3, 16, 32, 8, False), (2, 32, 32, 2, 24, 16, 8, True), (1, 5, 9, 1, 8, 64, 0, False), (1, 72, 72, 2, 32, 64, 40, False),
+           (2, 23, 31, 3, 20, 7, 3, False), (1, 24, 16, 2, 48, 8, 3, True), (1, 13, 17, 2, 33, 5, 2, False), (1, 20, 33, 2, 30, 12, 7, False), (1, 33, 18, 1, 64, 16, 5, False),
+           (1, 21, 22, 2, 10, 18, 4, False), (3, 1, 1, 1, 1, 1, 0, False)]
+
+
+@pytest.mark.parametrize("case", GUARDED, ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_results_and_workspaces_stay_inside_their_buffers(case, dtype):
+    B, H, W, heads, d, M, s, masked = case
+    q, k, v, dout, bias, named = (t.cuda() for t in make(B, H, W, heads, d, M, log_map(M), dtype, seed=12))
+    lib, p, count, size, kind = binding.library(), lambda t: t.data_ptr(), bias.shape[1], (B, H, W, heads, d, M), int(dtype == torch.bfloat16)
+    g = Guarded()
+    out, lse = g.tensor(q.shape, torch.bfloat16), g.tensor((B, heads, H, W), torch.float32)
+    assert lib.rib_window_attn_fwd_bucketed(p(q), p(k), p(v), p(bias), kind, count, p(named), count, *size, s, int(masked), p(out), p(lse), None) == 0
+    saved = [(g.tensor(q.shape, torch.int8, fill=99), g.tensor(q.shape[:4], torch.float32)) for _ in range(4)]
+    for t, (codes, scales) in zip((q, k, v, out), saved):
+        assert lib.rib_checkpoint_store(p(t), B * H * W * heads, d, p(codes), p(scales), None) == 0
+    back = g.tensor(q.shape, torch.bfloat16)
+    assert lib.rib_checkpoint_restore(p(saved[0][0]), p(saved[0][1]), B * H * W * heads, d, p(back), None) == 0
+    torch.cuda.synchronize()
+    g.check("forward and checkpoints")
+    assert not any(torch.isnan(t.float()).any() for t in (out, lse, back, *(x[1] for x in saved)))
+    array = (ctypes.c_void_p * 8)(*[p(t) for pair in saved for t in pair])
+    for checkpointed in (False, True):
+        g = Guarded()
+        results = [g.tensor(q.shape, torch.bfloat16) for _ in range(3)] + [g.tensor(bias.shape, dtype)]
+        need = getattr(lib, "rib_window_attn_bwd_bucketed" + ("_checkpointed" if checkpointed else "") + "_workspace")(count, count, *size)
+        ws = g.tensor((need,), torch.uint8)
+        tail = (*size, s, int(masked), *(p(t) for t in results), p(ws), need, None)
+        if checkpointed:
+            rc = lib.rib_window_attn_bwd_bucketed_checkpointed(array, p(bias), kind, count, p(named), count, p(lse), p(dout), *tail)
+        else:
+            rc = lib.rib_window_attn_bwd_bucketed(p(q), p(k), p(v), p(bias), kind, count, p(named), count, p(out), p(lse), p(dout), *tail)
+        assert rc == 0
+        torch.cuda.synchronize()
+        assert binding.rib_query_status() == 0
+        g.check("backward")
+        assert not any(torch.isnan(t.float()).any() for t in results)
