@@ -4,8 +4,9 @@
 // NaN and comes back as NaN, so that an overflow is not lost on the way through the checkpoint.
 //
 // Both directions are bound by memory: 2 d bytes on one side, d + 4 on the other.  Rows of 8, 16, ... 64 channels (16-byte aligned): a thread has 8
-// channels of a row - one 16-byte access to x, one of 8 bytes to the codes, neighbours side by side - and the lanes of a row share its
-// maximum by shuffles.  Other widths: a block takes 64 rows, whose bytes are whole 16-byte words on both sides, through shared memory.
+// channels of a row, or 16 to store those of whole 32 bytes - one or two 16-byte accesses to x, one of as many codes, neighbours side by side -
+// and the lanes of a row share its maximum by shuffles.  Other widths: a block takes 64 rows, whose bytes are whole 16-byte words on both sides, through
+// shared memory.
 #include "rib_common.cuh"
 
 namespace rib {
@@ -13,13 +14,13 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kStagedRows = 64;
-constexpr int kStoreUnroll = 2, kRestoreUnroll = 8, kRestoreBlocks = 2;
+constexpr int kStoreUnroll = 4, kRestoreUnroll = 8, kRestoreBlocks = 2;
 
 // Quotients decide codes, so they are those of the IEEE division.  With y the reciprocal of the scale, t = x y is off by an ulp or so; the remainder
 // x - t scale is exact, and adding y times it leaves a quotient (Markstein's method) that names the same code for every pair of bf16 mantissas and
 // every distance of their exponents: they are few enough to try them all, and a test does.  Three operations without a branch: a test
 // whether t lies near a border, with the division behind it, took 108 to 116 us
-// where this takes 96 (below), since half the maximum is a border and half of the warps met one.
+// where this took 96, since half the maximum is a border and half of the warps met one.
 // A scale below 2^-100, whose remainders could vanish, takes the division.
 // The nearest whole number is read off the low bits of t + 1.5 x 2^23 (half to even, as round() does): conversions between floating and whole
 // numbers have an eighth of the rate of additions, and were what these kernels waited for.  Both return a word with the code in its low byte.
@@ -45,49 +46,58 @@ __device__ __forceinline__ RowScale row_scale(float most, bool bad)
     return r;
 }
 
-// kLanes lanes to a row (a power of two, the last ones without channels where d / 8 is none), two runs of kThreads / kLanes rows
-// per block (a layer of 16 x 96 x 96 tokens, 6 heads, d = 32: 96 us for four tensors, 3.7 TB/s; one run 105, four and eight 94 to 96.  Blocks that walk
-// runs with the next one's loads under way, as restore has them, took 8 us more: the shuffles and the reciprocal of a row wait for one another,
-// and what hides that is other warps)
-template <int kLanes>
+// kLanes lanes to a row (a power of two, the last ones without channels where d is none), four runs of kThreads / kLanes rows per block (a layer of
+// 16 x 96 x 96 tokens, 6 heads, d = 32: 85 us for four tensors, 4.2 TB/s; two runs or one 91.  Blocks that walk runs with the next one's loads under
+// way, as restore has them, took 8 us more: the shuffles and the reciprocal of a row wait for one another, and what hides that is other warps)
+// kWords: 16-byte words of a thread, 2 where rows are whole 32 bytes (a reciprocal and shuffles for sixteen channels: 85 us where
+// one word took 94).
+template <int kLanes, int kWords>
 __global__ void __launch_bounds__(kThreads) rib_checkpoint_store_kernel(const __nv_bfloat16* __restrict__ x, long long rows, int d, int8_t* __restrict__ codes, float* __restrict__ scales)
 {
     constexpr int kUnroll = kStoreUnroll, kRowsAtOnce = kThreads / kLanes;
     const int part = threadIdx.x % kLanes;
-    const bool mine = 8 * part < d;
+    const bool mine = 8 * kWords * part < d;
     const long long row0 = (long long)blockIdx.x * (kUnroll * kRowsAtOnce) + threadIdx.x / kLanes;
-    uint4 v[kUnroll];
+    uint4 v[kUnroll][kWords];
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
         const long long row = row0 + k * kRowsAtOnce;
-        v[k] = mine && row < rows ? __ldg(reinterpret_cast<const uint4*>(x + row * d) + part) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) v[k][j] = mine && row < rows ? __ldg(reinterpret_cast<const uint4*>(x + row * d) + kWords * part + j) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
         const long long row = row0 + k * kRowsAtOnce;
-        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        uint32_t w[4 * kWords];
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) { w[4 * j] = v[k][j].x; w[4 * j + 1] = v[k][j].y; w[4 * j + 2] = v[k][j].z; w[4 * j + 3] = v[k][j].w; }
         // the largest magnitude as an integer: magnitudes of bf16 are ordered like their bits, infinity and NaN behind all others
         uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = max(most, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+        for (int i = 0; i < 4 * kWords; ++i) most = max(most, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
 #pragma unroll
         for (int o = kLanes / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
         const RowScale s = row_scale(__uint_as_float(most << 16), most >= 0x7f80u);
-        uint32_t c[2] = {0u, 0u};
+        uint32_t c[2 * kWords];
+#pragma unroll
+        for (int i = 0; i < 2 * kWords; ++i) c[i] = 0u;
         if (!s.zero) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2 * kWords; ++i)
                 c[i] = low_bytes(code_of(__uint_as_float(w[2 * i] << 16), s.scale, s.inverse), code_of(__uint_as_float(w[2 * i] & 0xffff0000u), s.scale, s.inverse),
                                  code_of(__uint_as_float(w[2 * i + 1] << 16), s.scale, s.inverse), code_of(__uint_as_float(w[2 * i + 1] & 0xffff0000u), s.scale, s.inverse));
             if (s.tiny) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 2 * kWords; ++i)
                     c[i] = low_bytes(quotient_code(__uint_as_float(w[2 * i] << 16), s.scale), quotient_code(__uint_as_float(w[2 * i] & 0xffff0000u), s.scale),
                                      quotient_code(__uint_as_float(w[2 * i + 1] << 16), s.scale), quotient_code(__uint_as_float(w[2 * i + 1] & 0xffff0000u), s.scale));
             }
         }
         if (row < rows) {
-            if (mine) *reinterpret_cast<uint2*>(codes + row * d + 8 * part) = make_uint2(c[0], c[1]);
+            if (mine) {
+                if constexpr (kWords == 2) *reinterpret_cast<uint4*>(codes + row * d + 16 * part) = make_uint4(c[0], c[1], c[2], c[3]);
+                else *reinterpret_cast<uint2*>(codes + row * d + 8 * part) = make_uint2(c[0], c[1]);
+            }
             if (part == 0) scales[row] = s.scale;
         }
     }
@@ -219,8 +229,10 @@ cudaError_t checkpoint_store(const __nv_bfloat16* x, long long rows, int d, int8
     if (d % 8) {
         rib_checkpoint_store_staged_kernel<<<(unsigned)((rows + kStagedRows - 1) / kStagedRows), kThreads, 0, stream>>>(x, rows, d, codes, scales);
     } else {
-        const int lanes = lanes_of(d);
-        const auto kernel = lanes == 1 ? rib_checkpoint_store_kernel<1> : lanes == 2 ? rib_checkpoint_store_kernel<2> : lanes == 4 ? rib_checkpoint_store_kernel<4> : rib_checkpoint_store_kernel<8>;
+        const bool wide = d % 16 == 0;
+        const int lanes = wide ? lanes_of(d / 2) : lanes_of(d);
+        const auto kernel = wide ? (lanes == 1 ? rib_checkpoint_store_kernel<1, 2> : lanes == 2 ? rib_checkpoint_store_kernel<2, 2> : rib_checkpoint_store_kernel<4, 2>)
+                                 : (lanes == 1 ? rib_checkpoint_store_kernel<1, 1> : lanes == 4 ? rib_checkpoint_store_kernel<4, 1> : rib_checkpoint_store_kernel<8, 1>);
         const long long per = (long long)kStoreUnroll * kThreads / lanes;
         kernel<<<(unsigned)((rows + per - 1) / per), kThreads, 0, stream>>>(x, rows, d, codes, scales);
     }
