@@ -185,7 +185,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const uint32_t at = threadIdx.x * 16;
         reinterpret_cast<uint4*>(base_ptr + kOffOnes)[threadIdx.x] = at < kOnesBytes ? make_uint4(kTwo, kFirst, 0u, 0u) : at < 2 * kOnesBytes ? make_uint4(0u, kSecond, kTwo, 0u) : make_uint4(0u, 0u, 0u, 0u);
     }
-    if (threadIdx.x < 4) reinterpret_cast<float*>(base_ptr + kOffMasked)[threadIdx.x] = kTableMasked;
+    if (threadIdx.x < 4) reinterpret_cast<float*>(base_ptr + kOffMasked)[threadIdx.x] = -INFINITY;
     fence_proxy_async();
     tc_fence_before();
     __syncthreads();
@@ -368,7 +368,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(kTabDone));
                 if (!mbar_wait_warp(bar(kTabDone), ntable & 1, abort_flag, p.status)) { ok = false; break; }
-                gather_bias(p.source, c.h, side * side, reinterpret_cast<float*>(base_ptr + kOffTable), threadIdx.x - 128, kArithmeticThreads);
+                gather_bias(p.source, c.h, side * side, -INFINITY, reinterpret_cast<float*>(base_ptr + kOffTable), threadIdx.x - 128, kArithmeticThreads);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(kTabReady));
                 if (!mbar_wait_warp(bar(kTabReady), ntable & 1, abort_flag, p.status)) { ok = false; break; }

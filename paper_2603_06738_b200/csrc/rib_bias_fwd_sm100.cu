@@ -120,7 +120,7 @@ __device__ __forceinline__ bool change_table(const Params& p, uint8_t* base_ptr,
     __syncwarp();
     if (lane == 0) mbar_arrive(done);
     if (!mbar_wait_warp(done, *ntable & 1, abort_flag, p.status)) return false;
-    gather_bias(p.source, h, side * side, reinterpret_cast<float*>(base_ptr + kOffTable), threadIdx.x - 128, kSoftmaxThreads);
+    gather_bias(p.source, h, side * side, kTableMasked, reinterpret_cast<float*>(base_ptr + kOffTable), threadIdx.x - 128, kSoftmaxThreads);
     __syncwarp();
     if (lane == 0) mbar_arrive(ready);
     if (!mbar_wait_warp(ready, *ntable & 1, abort_flag, p.status)) return false;

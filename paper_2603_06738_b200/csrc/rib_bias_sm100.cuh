@@ -13,8 +13,9 @@ namespace sm100 {
 
 constexpr int kBiasMaxWindow = 64;                     // (127^2 fp32 = 64.5 KB beside the tiles)
 constexpr float kLog2e = 1.4426950408889634f;
-// What the table holds for keys that are not attended to: as good as minus infinity beside any score (in log2 units), but finite, so that the
-// polynomial form of the exponential takes it.
+// What the forward's table holds for keys that are not attended to: as good as minus infinity beside any score (in log2 units), but finite, so that the
+// polynomial form of the exponential takes it.  The backward's holds minus infinity: there is no polynomial there, and beside any finite score, however large,
+// the probability is 0.
 constexpr float kTableMasked = -1e6f;
 
 struct BiasItems {
@@ -125,8 +126,8 @@ inline bool make_bias_items(const Problem& p, int patches_per_item, BiasItems* g
 struct BiasSource { const void* bias; const int* buckets; long long head_stride; int bf16, num_buckets; };
 inline BiasSource bias_source(const Problem& p) { return {p.bias, p.buckets, p.bias_head_stride, p.bias_bf16, p.num_buckets}; }
 
-// Threads `thread` of `threads` write head h's biases by offset, times log2(e), to shared memory.
-__device__ __forceinline__ void gather_bias(const BiasSource& s, int h, int entries, float* table, int thread, int threads)
+// Threads `thread` of `threads` write head h's biases by offset, times log2(e), to shared memory; `masked` for keys that are not attended to.
+__device__ __forceinline__ void gather_bias(const BiasSource& s, int h, int entries, float masked, float* table, int thread, int threads)
 {
     constexpr int kAhead = 4;
     for (int e0 = thread; e0 < entries; e0 += kAhead * threads) {
@@ -138,7 +139,7 @@ __device__ __forceinline__ void gather_bias(const BiasSource& s, int h, int entr
             if (e0 + k * threads < entries) {
                 const float b = (unsigned)u[k] < (unsigned)s.num_buckets ? bias_at(s.bias, s.bf16, (long long)h * s.head_stride + u[k]) : -INFINITY;
                 const float v = b * kLog2e;
-                table[e0 + k * threads] = b == -INFINITY ? kTableMasked : v == kTableMasked ? kTableMasked * 1.0001f : v;
+                table[e0 + k * threads] = b == -INFINITY ? masked : v == kTableMasked ? kTableMasked * 1.0001f : v;
             }
     }
 }

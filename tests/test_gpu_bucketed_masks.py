@@ -1,0 +1,79 @@
+"""Keys that are not attended to, under a bias by buckets, whatever their finite logits and the other biases are.
+
+Tolerances are those of tests/test_gpu_bucketed.py.  The large channels of a marked query and a marked key meet no others: every logit that counts is one of
+ordinary inputs, so what holds for those holds here.  Where a channel is large the results are compared without it as well."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rib_bias_oracle as orc
+from paper_2603_06738_b200 import binding
+
+from parity_util import to_f64
+from test_gpu_bucketed import close, log_map, make, sum_noise
+
+pytestmark = pytest.mark.gpu
+
+# B, H, W, heads, d, M, s: tcgen05 kernels (whole patches, an odd number of them, a map that cuts them, one large window), warp-level MMAs, any-shape
+SHAPES = [(1, 32, 48, 2, 32, 16, 8), (1, 24, 40, 2, 32, 8, 0), (1, 48, 24, 2, 16, 24, 8), (1, 41, 53, 2, 32, 16, 0), (1, 64, 64, 1, 32, 64, 32),
+          (1, 23, 31, 2, 20, 7, 3), (1, 20, 40, 2, 10, 20, 4)]
+
+
+def places(size, M, s):
+    """Shifted place of every row (or column) of the map."""
+    return (np.arange(size) - s) % (-(-size // M) * M)
+
+
+def marked(case, named, q_row, k_row):
+    """Inputs of the case whose query at one token and key at another of its window hold q_row and k_row, channels that are 0 in all other rows; the offset
+    of the two is not attended to.  Returns them, the head and the two tokens."""
+    B, H, W, heads, d, M, s = case
+    q, k, v, dout, bias, named = make(B, H, W, heads, d, M, named, torch.float32, seed=31)
+    py, px = places(H, M, s), places(W, M, s)
+    h, Y, X = heads - 1, int(np.where(py == 4)[0][0]), int(np.where(px == 5)[0][0])
+    KY, KX = int(np.where(py == 2)[0][0]), int(np.where(px == 6)[0][0])
+    width = len(q_row)
+    q[..., :width] = 0
+    k[..., :width] = 0
+    q[0, Y, X, h] = 0
+    k[0, KY, KX, h] = 0
+    q[0, Y, X, h, :width] = torch.tensor(q_row)
+    k[0, KY, KX, h, :width] = torch.tensor(k_row)
+    assert q[0, Y, X, h, :width].tolist() == list(q_row) and k[0, KY, KX, h, :width].tolist() == list(k_row)
+    named[2 - 4 + M - 1, 6 - 5 + M - 1] = -1
+    return (q, k, v, dout, bias, named)
+
+
+def run(inputs, M, s, path=binding.RIB_PATH_NONE):
+    q, k, v, dout, bias, named = (t.cuda() for t in inputs)
+    old = binding.rib_set_path(path)
+    try:
+        out, lse = binding.rib_window_attn_fwd_bucketed(q, k, v, bias, named, M, s)
+        grads = binding.rib_window_attn_bwd_bucketed(q, k, v, bias, named, out, lse, dout, M, s)
+    finally:
+        binding.rib_set_path(old)
+    torch.cuda.synchronize()
+    assert binding.rib_query_status() == 0
+    return out, lse, grads
+
+
+def compare(inputs, M, s, out, lse, grads, width):
+    q, k, v, dout, bias, named = inputs
+    f = [to_f64(t) for t in (q, k, v, bias)] + [named.numpy()]
+    ref_out, ref_lse = orc.fwd(*f, M, s)
+    close("out", out, ref_out)
+    close("lse", lse, ref_lse)
+    *refs, norm = orc.bwd(*f, to_f64(dout), M, s, out=to_f64(out), lse=to_f64(lse), want_norm=True)
+    for name, got, ref in zip(("dq", "dk", "dv", "dbias"), grads, refs):
+        close(name, got, ref, noise=sum_noise(norm) if name == "dbias" else 0.0)
+        if name in ("dq", "dk"):
+            close(name + " without the large channels", got[..., width:], ref[..., width:])
+
+
+@pytest.mark.parametrize("case", SHAPES, ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("size", [2560.0, 2.0 ** 30])
+def test_a_key_out_of_reach_with_a_large_logit(case, size):
+    """The logit of the pair is 10^6 and more above the others of the row, and finite."""
+    d, M, s = case[4:]
+    inputs = marked(case, log_map(M), (size,), (size,))
+    compare(inputs, M, s, *run(inputs, M, s), 1)
