@@ -13,10 +13,10 @@ namespace sm100 {
 
 constexpr int kBiasMaxWindow = 64;                     // (127^2 fp32 = 64.5 KB beside the tiles)
 constexpr float kLog2e = 1.4426950408889634f;
-// What the forward's table holds for keys that are not attended to: as good as minus infinity beside any score (in log2 units), but finite, so that the
-// polynomial form of the exponential takes it.  The backward's holds minus infinity: there is no polynomial there, and beside any finite score, however large,
-// the probability is 0.
-constexpr float kTableMasked = -1e6f;
+// What the forward's table holds for keys that are not attended to: finite, so that the polynomial form of the exponential takes it, and further
+// below 0 than a score in log2 units can lie above it (a finite fp32 product times log2(e) / sqrt(d), at most 3.41e38 x 0.511 = 1.74e38 for d >= 8).  The sum
+// is minus infinity for the lowest scores only, which the exact form takes.  The backward's table holds minus infinity: there is no polynomial there.
+constexpr float kTableMasked = -1.8e38f;
 
 struct BiasItems {
     LiveWindows live;              // of one head
@@ -138,8 +138,7 @@ __device__ __forceinline__ void gather_bias(const BiasSource& s, int h, int entr
         for (int k = 0; k < kAhead; ++k)
             if (e0 + k * threads < entries) {
                 const float b = (unsigned)u[k] < (unsigned)s.num_buckets ? bias_at(s.bias, s.bf16, (long long)h * s.head_stride + u[k]) : -INFINITY;
-                const float v = b * kLog2e;
-                table[e0 + k * threads] = b == -INFINITY ? masked : v == kTableMasked ? kTableMasked * 1.0001f : v;
+                table[e0 + k * threads] = b == -INFINITY ? masked : b * kLog2e;         // (other biases lie above -1.5e30)
             }
     }
 }

@@ -77,3 +77,15 @@ def test_a_key_out_of_reach_with_a_large_logit(case, size):
     d, M, s = case[4:]
     inputs = marked(case, log_map(M), (size,), (size,))
     compare(inputs, M, s, *run(inputs, M, s), 1)
+
+
+@pytest.mark.parametrize("case", SHAPES, ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("k_row", [(4000.0, 43.0), (4000.0, 45.0), (3984.0, 2.0), (3.0e32, 0.0), (1.0e35, 0.0)])
+def test_a_key_out_of_reach_whose_logit_meets_a_stand_in(case, k_row):
+    """Rows attend to their own token and two others, so that one weight too many shows.  Logits of the pair around 10^6 (in log2 units), and large ones."""
+    d, M, s = case[4:]
+    named = np.full((2 * M - 1, 2 * M - 1), -1)
+    named[M - 1, M - 1], named[M - 1, M], named[M - 2, M - 1] = 0, 1, 2
+    k_row = torch.tensor(k_row).bfloat16().tolist()
+    inputs = marked(case, named, (980.0, 24.0), k_row)
+    compare(inputs, M, s, *run(inputs, M, s), 2)
