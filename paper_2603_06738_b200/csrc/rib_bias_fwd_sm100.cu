@@ -17,7 +17,7 @@
 // row of the block's patch, two neighbouring keys, and finds their biases in 11 pairs of the table (rib_bias_sm100.cuh).
 // There is no reference m: fp32 and bf16 carry 8 exponent bits, so the exponentials of scores (with bias) up to 69 are as exact as those of
 // small ones, and a score costs one multiply-add, one exponential and half a conversion.  A row whose sum of exponentials leaves
-// [2^-64, 2^100) - large scores of either sign, rows without any key, scores that are not finite - is noted, and its item redone in the same launch
+// [2^-32, 2^100) - large scores of either sign, rows without any key, scores that are not finite - is noted, and its item redone in the same launch
 // by the exact form: running maximum, accumulators per key half, a merge.  (A reference from the window's first 32 keys, as in the rank-r kernel: 302
 // us against 278 on 16 x 96 x 96 tokens in windows of 32.)  Every fourth pair of exponentials (kPolyMask) is evaluated on the FMA and integer pipes
 // instead of the MUFU.  Keys beyond the map's edge have zero rows of V and, for l, zeros in the tile of ones: five half tiles for
@@ -38,7 +38,8 @@ constexpr uint32_t kPolyMask = RIB_BIAS_POLY_MASK;       // of every 8 pairs of 
 // 2^x for a pair of arguments on the FMA and integer pipes.  x = n + f with n = round(x), |f| <= 1/2, n read off the low mantissa bits of
 // x + 1.5 * 2^23.  The cubic (relative error 7.5e-5) is evaluated with coefficients scaled by 2^-120, so its result carries the exponent field 6 or
 // 7 and 2^n is applied by adding n + 120, bounded to [0, 248], to that field: arguments below -120 (masked keys among them) yield about 2^-120, which
-// is nothing beside a row sum of at least 2^-64, and arguments from 128 on at least 2^127, which the epilogue sees in the row sum.
+// is nothing beside a row sum of at least 2^-32 (arguments of -2^46 .. -2^47, beside which 1.5 * 2^23 is lost by rounding, up to 2^-55: 4096 of them 2^-11 of
+// such a sum), and arguments from 128 on at least 2^127, which the epilogue sees in the row sum, as do some around -2^24.
 __device__ __forceinline__ float2 ex2_poly2_bounded(float2 x)
 {
     constexpr float kS = 7.52316384526264005e-37f;      // 2^-120
@@ -528,7 +529,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     tmem_wait_ld();
                     tc_fence_before();
                     const float l_all = __uint_as_float(lsum[0]);
-                    const bool bad = !no_query && !(l_all > 5.4210109e-20f && l_all < 1.2676506e30f);     // 2^-64, 2^100
+                    const bool bad = !no_query && !(l_all > 0x1p-32f && l_all < 0x1p100f);
                     if (__any_sync(0xffffffffu, bad) && lane == 0) {
                         const int slot = atomicAdd(redo_count, 1);
                         if (slot < kMaxRedo) redo_list[slot] = i;

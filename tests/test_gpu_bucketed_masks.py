@@ -89,3 +89,15 @@ def test_a_key_out_of_reach_whose_logit_meets_a_stand_in(case, k_row):
     k_row = torch.tensor(k_row).bfloat16().tolist()
     inputs = marked(case, named, (980.0, 24.0), k_row)
     compare(inputs, M, s, *run(inputs, M, s), 2)
+
+
+@pytest.mark.parametrize("case", SHAPES, ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("low", [-7e13, -6e13, -1e9, -1e7, -1e4])
+def test_low_biases_beside_very_low_ones(case, low):
+    """Half of the offsets have a bias of -40, the others one that leaves them no weight beside those."""
+    B, H, W, heads, d, M, s = case
+    named = (np.add.outer(np.arange(2 * M - 1) * 5, np.arange(2 * M - 1) * 3) % 7 < 3).astype(int)
+    named[M - 1, M - 1] = 0
+    q, k, v, dout, bias, named = inputs = make(B, H, W, heads, d, M, named, torch.float32, seed=35)
+    bias[:, 0], bias[:, 1] = -40.0, low
+    compare(inputs, M, s, *run(inputs, M, s), 0)
