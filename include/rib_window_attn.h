@@ -384,7 +384,9 @@ long long rib_kernel_launches(void);
  * with (y, x) the place of a token inside its window.  `buckets` names a bucket for each of the (2M-1)^2 offsets (key minus
  * query) and is the same for all heads; several offsets may share a bucket.  A key whose offset has a bucket outside
  * [0, num_buckets) (-1, say) or a bias of -1e30 or less (minus infinity, the lowest value of a type) is not attended to.  A row that
- * is left without any key gets out = 0 and lse = -infinity, and no gradient.  Other biases are finite.
+ * is left without any key gets out = 0 and lse = -infinity, and no gradient.  Other biases are finite, at most 1e30.
+ * Logits and lse are fp32: beside a bias of 10^6 what a row's logits differ in is known to 0.1, and the probabilities that the backward pass recomputes
+ * from lse are off by up to a factor of exp(|lse| 2^-21) (and at most 1).
  * Infinities and NaN in a row of q or k reach out and lse of the rows that attend to it, and no others of the forward pass; those in v reach every row of the
  * window and head, with weight 0 (as in a product of matrices).  In the backward pass they may reach every gradient of the window and
  * head, and dbias.

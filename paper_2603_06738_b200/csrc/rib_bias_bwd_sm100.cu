@@ -418,7 +418,8 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         for (int rr = 0; rr < 2; ++rr) {                  // key rows 2 o + rr of the warp's, query rows 2 G + gq
                             const int i = 4 * gq + 2 * rr;
                             const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2, bb[1 + rr - gq]);
-                            float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                            // (a probability is at most 1, however little of its digits a large lse has left; NaN stays)
+                            float2 e = make_float2(ex2_approx(min_nan(x.x, 0.f)), ex2_approx(min_nan(x.y, 0.f)));
                             if (kCut && 2 * o + rr >= rows_there) e = make_float2(0.f, 0.f);
                             const float2 d = __fmul2_rn(e, make_float2(__uint_as_float(dp[i]), __uint_as_float(dp[i + 1])));
                             pp[2 * gq + rr] = pack_bf16x2(e.x, e.y);

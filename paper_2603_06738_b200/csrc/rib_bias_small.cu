@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(2 * kMaxTokens) rib_bias_small_bwd_kernel(cons
                         const int place = e & 1 ? places.y : places.x, entry = (e & 2 ? entry1 : entry0) - (place & 0xffff);
                         const float b = table[entry];
                         const bool seen = (e & 2 ? there1 : there0) && (place >> 16) == (e & 2 ? part1 : part0) && b != -INFINITY;
-                        pr[e] = seen ? ex2_approx(fmaf(x[t][e], scale, b - (e & 1 ? ls.y : ls.x))) : 0.f;
+                        pr[e] = seen ? ex2_approx(min_nan(fmaf(x[t][e], scale, b - (e & 1 ? ls.y : ls.x)), 0.f)) : 0.f;      // (at most 1, whatever lse has left of its digits)
                         d[e] = seen ? pr[e] * (dp[t][e] - (e & 1 ? dd.y : dd.x)) : 0.f;
                         if (seen) atomicAdd(sums + entry, d[e]);
                     }

@@ -66,7 +66,12 @@ __device__ inline float with_bias(const Problem& p, int h, float s, int i, int j
     return b == -INFINITY ? -INFINITY : s + b;
 }
 // exp(s - lse).  A row that a bias leaves no key has lse = -inf, and so has every s of it; without a bias such a row is one of infinite inputs, and NaN.
-__device__ inline float probability(const Problem& p, float s, float lse) { return p.bias && s == -INFINITY ? 0.f : expf(s - lse); }
+// Under a bias, which may be large, it is held to 1 whatever lse has left of its digits (NaN stays).
+__device__ inline float probability(const Problem& p, float s, float lse)
+{
+    const float x = s - lse;
+    return !p.bias ? expf(x) : s == -INFINITY ? 0.f : expf(x > 0.f ? 0.f : x);
+}
 
 // element offset of channel 0 of token i of the pair in a [B][H][W][heads][d] tensor (the token must exist)
 __device__ inline size_t token_offset(const Problem& p, const PairCoord& c, int i)

@@ -367,6 +367,13 @@ __device__ __forceinline__ float ex2_approx(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// the smaller of two; NaN where one is (fminf takes the other)
+__device__ __forceinline__ float min_nan(float a, float b)
+{
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
 // tanh on the special-function unit (absolute error about 2^-11)
 __device__ __forceinline__ float tanh_approx(float x)
 {

@@ -101,3 +101,33 @@ def test_low_biases_beside_very_low_ones(case, low):
     q, k, v, dout, bias, named = inputs = make(B, H, W, heads, d, M, named, torch.float32, seed=35)
     bias[:, 0], bias[:, 1] = -40.0, low
     compare(inputs, M, s, *run(inputs, M, s), 0)
+
+
+@pytest.mark.parametrize("case", SHAPES, ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("low", [-1e6, -1e9, -9e29])
+def test_rows_whose_biases_are_all_very_low(case, low):
+    """A finite bias counts, however low: the offsets that have a bucket share `low`, others have none.
+
+    lse is fp32, so probabilities recomputed from it carry |lse| 2^-24 of its last place, and with sqrt(d) <= 5.7 the tcgen05 kernels' accumulators a
+    few units of 2^23.  At 10^6 that is, in log2 units: the accumulator's last place 0.5 and half of it, and the rounding of sqrt(d) 0.34, times log2(e) / sqrt(d) = 0.255:
+    0.28; the rounding of that factor 0.17; of bias log2(e) 0.1: a probability is off by up to a factor of 2^0.55 < 1.5.  Beyond, nothing is left of the
+    digits; a probability is still at most 1, so dv is at most the sum of |dO|, and the rest is finite."""
+    B, H, W, heads, d, M, s = case
+    named = np.where(np.add.outer(np.arange(2 * M - 1) * 5, np.arange(2 * M - 1) * 3) % 7 < 2, -1, 0)
+    named[M - 1, M - 1] = 0
+    q, k, v, dout, bias, named = inputs = make(B, H, W, heads, d, M, named, torch.float32, seed=32)
+    bias.fill_(low)
+    for path in (binding.RIB_PATH_NONE, binding.RIB_PATH_GENERIC):
+        out, lse, grads = run(inputs, M, s, path)
+        assert all(torch.isfinite(t.float()).all() for t in (out, lse, *grads))
+        dq, dk, dv, dbias = (to_f64(t) for t in grads)
+        assert (np.abs(dv) <= 1.01 * np.abs(to_f64(dout)).sum((0, 1, 2))).all()
+        if low < -1e6:
+            continue
+        f = [to_f64(t) for t in (q, k, v, bias)] + [named.numpy()]
+        given = dict(out=to_f64(out), lse=to_f64(lse))
+        ref_dq, ref_dk, ref_dv, _, norm = orc.bwd(*f, to_f64(dout), M, s, **given, want_norm=True)
+        _, _, reach, _ = orc.bwd(*f, np.abs(to_f64(dout)), M, s, **given)                 # P^T |dO|
+        assert (np.abs(dv - ref_dv) <= 0.5 * reach + 2.0 ** -8 * np.abs(ref_dv) + 1e-6).all()
+        for got, ref, other in ((dq, ref_dq, k), (dk, ref_dk, q)):
+            assert np.linalg.norm(got - ref) <= 0.5 * norm * np.linalg.norm(to_f64(other)) / np.sqrt(d)
