@@ -199,6 +199,41 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
+def _elsewhere(stream) -> bool:
+    """Is the stream that a call is given another one than the current one?"""
+    return int(stream.cuda_stream) != int(torch.cuda.current_stream(getattr(stream, "device", None)).cuda_stream)
+
+
+def _tensors(x):
+    if isinstance(x, torch.Tensor):
+        yield x
+    elif isinstance(x, (tuple, list)):
+        for y in x:
+            yield from _tensors(y)
+
+
+def _beside(stream, call, *args):
+    """A call on a stream that is not the current one: made with that stream current, so that its results and its scratch are memory of that stream, which
+    nothing on the current one still uses; and no tensor of the call is handed out again before the call (its arguments) or what the current stream does
+    with them (its results) is through."""
+    given = [t for t in _tensors(args) if t.is_cuda]
+    device = given[0].device if given else None
+    current = torch.cuda.current_stream(device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream.cuda_stream), device=device)
+    if device is not None and stream.device != device:
+        raise ValueError(f"stream is one of {stream.device}, the tensors are on {device}")
+    try:
+        with torch.cuda.stream(stream):
+            results = call(*args)
+    finally:
+        for t in given:
+            t.record_stream(stream)
+    for t in _tensors(results):
+        t.record_stream(current)
+    return results
+
+
 def _ptr(t) -> int | None:
     return None if t is None else int(t.data_ptr())
 
@@ -285,6 +320,8 @@ def rib_window_attn_bwd_workspace(B, H, W, heads, d, r, window) -> int:
 
 def rib_window_attn_fwd(q, k, v, pq, pk, window, shift=0, out=None, lse=None, stream=None, want_lse=True):
     """Enqueue the forward pass; returns (out bf16 [B,H,W,heads,d], lse fp32 [B,heads,H,W] or None)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_fwd, q, k, v, pq, pk, window, shift, out, lse, None, want_lse)
     if _marshal is not None and out is None and lse is None:
         got = _native(_marshal.fwd, "rib_window_attn_fwd_headwise", q, k, v, pq, pk, 1, window, shift, want_lse, stream)
         if got is not None:
@@ -310,6 +347,8 @@ def rib_window_attn_fwd(q, k, v, pq, pk, window, shift=0, out=None, lse=None, st
 
 def rib_window_attn_bwd(q, k, v, pq, pk, out, lse, dout, window, shift=0, workspace=None, stream=None):
     """Enqueue the backward pass; returns (dq, dk, dv bf16, dpq, dpk fp32 [n,r])."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_bwd, q, k, v, pq, pk, out, lse, dout, window, shift, workspace)
     if _marshal is not None and workspace is not None:
         got = _native(_marshal.bwd, "rib_window_attn_bwd_headwise", q, k, v, pq, pk, out, lse, dout, 1, window, shift, workspace, stream)
         if got is not None:
@@ -345,6 +384,8 @@ def rib_window_attn_bwd_headwise_workspace(pos_head_stride, B, H, W, heads, d, r
 
 def rib_window_attn_fwd_headwise(q, k, v, pq, pk, window, shift=0, stream=None, want_lse=True):
     """Forward pass with one Pq/Pk table per head: pq, pk bf16 [heads, n, r]; returns (out, lse)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_fwd_headwise, q, k, v, pq, pk, window, shift, None, want_lse)
     if _marshal is not None:
         got = _native(_marshal.fwd, "rib_window_attn_fwd_headwise", q, k, v, pq, pk, 2, window, shift, want_lse, stream)
         if got is not None:
@@ -369,6 +410,8 @@ def rib_window_attn_fwd_headwise(q, k, v, pq, pk, window, shift=0, stream=None, 
 def rib_window_attn_fwd_padded(q, k, v, pq, pk, window, shift=0, stream=None, want_lse=True):
     """Forward pass on a map whose sides need not be multiples of the window (positions of the extended map
     beyond H x W are not tokens); pq, pk are [n, r] or [heads, n, r].  Returns (out, lse)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_fwd_padded, q, k, v, pq, pk, window, shift, None, want_lse)
     if _marshal is not None:
         got = _native(_marshal.fwd, "rib_window_attn_fwd_padded", q, k, v, pq, pk, 3, window, shift, want_lse, stream)
         if got is not None:
@@ -398,6 +441,8 @@ def rib_window_attn_fwd_padded(q, k, v, pq, pk, window, shift=0, stream=None, wa
 def rib_window_cycle_fwd(qs, ks, vs, pqs, pks, windows, shifts=None, stream=None, want_lse=True):
     """The cyclic window strategy in one call: layer l attends qs[l], ks[l], vs[l] in windows of side windows[l] with the tables
     pqs[l], pks[l] ([windows[l]^2, r]).  Returns (outs, lses), one tensor per layer."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_cycle_fwd, qs, ks, vs, pqs, pks, windows, shifts, None, want_lse)
     layers = len(windows)
     if not (len(qs) == len(ks) == len(vs) == len(pqs) == len(pks) == layers) or (shifts is not None and len(shifts) != layers):
         raise ValueError("one q, k, v, pq, pk (and shift) per layer")
@@ -425,6 +470,8 @@ def rib_window_cycle_fwd(qs, ks, vs, pqs, pks, windows, shifts=None, stream=None
 
 def rib_window_cycle_bwd(qs, ks, vs, pqs, pks, outs, lses, douts, windows, shifts=None, workspace=None, stream=None):
     """Backward passes of the layers of rib_window_cycle_fwd.  Returns (dqs, dks, dvs, dpqs, dpks), one tensor per layer."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_cycle_bwd, qs, ks, vs, pqs, pks, outs, lses, douts, windows, shifts, workspace)
     layers = len(windows)
     lists = (qs, ks, vs, pqs, pks, outs, lses, douts)
     if any(len(x) != layers for x in lists) or (shifts is not None and len(shifts) != layers):
@@ -459,6 +506,8 @@ def rib_window_cycle_bwd(qs, ks, vs, pqs, pks, outs, lses, douts, windows, shift
 def rib_window_attn_bwd_padded(q, k, v, pq, pk, out, lse, dout, window, shift=0, workspace=None, stream=None):
     """Backward pass on a map whose sides need not be multiples of the window; pq, pk [n, r] or [heads, n, r].
     Returns (dq, dk, dv bf16, dpq, dpk fp32 of the shape of pq)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_bwd_padded, q, k, v, pq, pk, out, lse, dout, window, shift, workspace)
     if _marshal is not None and workspace is not None:
         got = _native(_marshal.bwd, "rib_window_attn_bwd_padded", q, k, v, pq, pk, out, lse, dout, 3, window, shift, workspace, stream)
         if got is not None:
@@ -496,6 +545,8 @@ def rib_window_attn_bwd_padded(q, k, v, pq, pk, out, lse, dout, window, shift=0,
 def rib_window_attn_fwd_masked(q, k, v, pq, pk, window, shift=0, stream=None, want_lse=True):
     """Forward pass with shifted windows whose wrapped parts do not attend to each other (H, W multiples of the
     window); pq, pk are [n, r] or [heads, n, r].  Returns (out, lse)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_fwd_masked, q, k, v, pq, pk, window, shift, None, want_lse)
     if _marshal is not None:
         got = _native(_marshal.fwd, "rib_window_attn_fwd_masked", q, k, v, pq, pk, 3, window, shift, want_lse, stream)
         if got is not None:
@@ -525,6 +576,8 @@ def rib_window_attn_fwd_masked(q, k, v, pq, pk, window, shift=0, stream=None, wa
 def rib_window_attn_bwd_masked(q, k, v, pq, pk, out, lse, dout, window, shift=0, workspace=None, stream=None):
     """Backward pass of rib_window_attn_fwd_masked; pq, pk [n, r] or [heads, n, r].
     Returns (dq, dk, dv bf16, dpq, dpk fp32 of the shape of pq)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_bwd_masked, q, k, v, pq, pk, out, lse, dout, window, shift, workspace)
     if _marshal is not None and workspace is not None:
         got = _native(_marshal.bwd, "rib_window_attn_bwd_masked", q, k, v, pq, pk, out, lse, dout, 3, window, shift, workspace, stream)
         if got is not None:
@@ -562,6 +615,8 @@ def rib_window_attn_bwd_masked(q, k, v, pq, pk, out, lse, dout, window, shift=0,
 def rib_cla_gate(x, w_dw, b_dw, w_pw, b_pw, stream=None):
     """CLA gate (Eq. 8): x bf16 [B,H,W,D]; w_dw fp32 [D,3,3]; b_dw fp32 [D]; w_pw fp32 [D,D] (out, in); b_pw fp32 [D].
     Returns the gate, bf16 [B,H,W,D]."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_cla_gate, x, w_dw, b_dw, w_pw, b_pw)
     if x.dtype != torch.bfloat16 or not x.is_cuda or not x.is_contiguous() or x.dim() != 4:
         raise ValueError("x must be a contiguous CUDA bfloat16 tensor [B,H,W,D]")
     B, H, W, D = x.shape
@@ -584,6 +639,8 @@ def _check_bf16_like(name, t, like=None):
 
 def rib_cla_product(out, gate, stream=None):
     """Eq. 9 on its own: out [B,H,W,heads,d] (or [B,H,W,D]) times gate [B,H,W,D], both bf16; returns out's shape."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_cla_product, out, gate)
     _check_bf16_like("out", out)
     _check_bf16_like("gate", gate, out)
     res = torch.empty_like(out)
@@ -595,6 +652,8 @@ def rib_cla_product(out, gate, stream=None):
 
 def rib_cla_product_bwd(out, gate, dout_gated, stream=None):
     """Chain rule of Eq. 9: returns (dout in out's shape, dgate in gate's shape), bf16."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_cla_product_bwd, out, gate, dout_gated)
     _check_bf16_like("out", out)
     _check_bf16_like("gate", gate, out)
     _check_bf16_like("dout_gated", dout_gated, out)
@@ -610,6 +669,8 @@ def rib_cla_product_bwd(out, gate, dout_gated, stream=None):
 def rib_cla_gate_bwd(x, w_dw, b_dw, w_pw, b_pw, dgate, workspace=None, stream=None):
     """Chain rule of Eq. 8: x, dgate bf16 [B,H,W,D]; weights as for rib_cla_gate.
     Returns (dx bf16 [B,H,W,D], dw_dw [D,3,3], db_dw [D], dw_pw [D,D], db_pw [D] fp32)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_cla_gate_bwd, x, w_dw, b_dw, w_pw, b_pw, dgate, workspace)
     if x.dtype != torch.bfloat16 or not x.is_cuda or not x.is_contiguous() or x.dim() != 4:
         raise ValueError("x must be a contiguous CUDA bfloat16 tensor [B,H,W,D]")
     B, H, W, D = x.shape
@@ -633,6 +694,8 @@ def rib_cla_gate_bwd(x, w_dw, b_dw, w_pw, b_pw, dgate, workspace=None, stream=No
 def rib_window_attn_fwd_gated(q, k, v, pq, pk, gate, window, shift=0, stream=None, want_lse=True):
     """Forward pass whose output is multiplied by the CLA gate (Eq. 9); gate bf16 [B,H,W,heads*d]; pq, pk [n,r] or
     [heads,n,r].  Returns (out, lse)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_fwd_gated, q, k, v, pq, pk, gate, window, shift, None, want_lse)
     _check_image("q", q)
     B, H, W, heads, d = q.shape
     _check_image("k", k, q.shape)
@@ -659,6 +722,8 @@ def rib_window_attn_fwd_gated(q, k, v, pq, pk, gate, window, shift=0, stream=Non
 
 def rib_window_attn_bwd_headwise(q, k, v, pq, pk, out, lse, dout, window, shift=0, workspace=None, stream=None):
     """Backward pass with one Pq/Pk table per head; returns (dq, dk, dv bf16, dpq, dpk fp32 [heads, n, r])."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_bwd_headwise, q, k, v, pq, pk, out, lse, dout, window, shift, workspace)
     if _marshal is not None and workspace is not None:
         got = _native(_marshal.bwd, "rib_window_attn_bwd_headwise", q, k, v, pq, pk, out, lse, dout, 2, window, shift, workspace, stream)
         if got is not None:
@@ -696,6 +761,8 @@ def rib_window_attn_bwd_noalloc(q, k, v, pq, pk, out, lse, dout, dq, dk, dv, dpq
     scratch raise ``RibError`` (RIB_ERR_TOO_LARGE).  Calls on one device share the scratch: keep
     them on one stream.
     """
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_bwd_noalloc, q, k, v, pq, pk, out, lse, dout, dq, dk, dv, dpq, dpk, window, shift)
     _check_image("q", q)
     B, H, W, heads, d = q.shape
     for name, t in (("k", k), ("v", v), ("out", out), ("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv)):
@@ -745,6 +812,8 @@ def rib_window_attn_fwd_bucketed(q, k, v, bias, buckets, window, shift=0, masked
     the heads), buckets int32 [2 window - 1, 2 window - 1], the bucket of every offset key - query (outside [0, num_buckets): not
     attended to).  Any H and W; `masked` keeps the wrapped parts of shifted windows apart (H, W multiples of the window).
     Returns (out, lse)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_fwd_bucketed, q, k, v, bias, buckets, window, shift, masked, None, want_lse)
     if _marshal is not None:
         got = _native(_marshal.fwd_bucketed, "rib_window_attn_fwd_bucketed", q, k, v, bias, buckets, window, shift, masked, want_lse, stream)
         if got is not None:
@@ -775,6 +844,8 @@ def rib_window_attn_bwd_bucketed_workspace(bias_head_stride, num_buckets, B, H, 
 
 def rib_window_attn_bwd_bucketed(q, k, v, bias, buckets, out, lse, dout, window, shift=0, masked=False, workspace=None, stream=None):
     """Backward pass of rib_window_attn_fwd_bucketed.  Returns (dq, dk, dv bf16, dbias of bias's shape and type)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_bwd_bucketed, q, k, v, bias, buckets, out, lse, dout, window, shift, masked, workspace)
     if _marshal is not None:
         call = lambda address, *args: _marshal.bwd_bucketed(address, _lib.rib_addresses["rib_window_attn_bwd_bucketed_workspace"], *args)  # noqa: E731
         got = _native(call, "rib_window_attn_bwd_bucketed", q, k, v, bias, buckets, out, lse, dout, window, shift, masked, workspace, stream)
@@ -801,6 +872,8 @@ def rib_window_attn_bwd_bucketed(q, k, v, bias, buckets, out, lse, dout, window,
 
 def rib_checkpoint_store(x, stream=None):
     """x bf16 [..., d], d <= 64, as (codes int8 of x's shape, scales fp32 of x's shape without its last dimension)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_checkpoint_store, x)
     if _marshal is not None:
         got = _native(_marshal.store, "rib_checkpoint_store", x, stream)
         if got is not None:
@@ -828,6 +901,8 @@ def _check_checkpoint(name, codes, scales, shape=None):
 
 def rib_checkpoint_restore(codes, scales, stream=None):
     """What rib_checkpoint_store kept, as bf16."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_checkpoint_restore, codes, scales)
     if _marshal is not None:
         got = _native(_marshal.restore, "rib_checkpoint_restore", codes, scales, stream)
         if got is not None:
@@ -855,6 +930,8 @@ def rib_window_attn_bwd_checkpointed(q, k, v, out, pq, pk, lse, dout, window, sh
     """Backward pass of a layer that kept q, k, v and out as checkpoints (codes, scales); pq, pk [n, r] or [heads, n, r].  On a map whose
     sides are not multiples of the window as rib_window_attn_bwd_padded, with `masked` as rib_window_attn_bwd_masked.
     Returns (dq, dk, dv bf16, dpq, dpk fp32 of the shape of pq)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_bwd_checkpointed, q, k, v, out, pq, pk, lse, dout, window, shift, masked, workspace)
     if _marshal is not None:
         call = lambda address, *args: _marshal.bwd_checkpointed(address, _lib.rib_addresses["rib_window_attn_bwd_checkpointed_workspace"], *args)  # noqa: E731
         got = _native(call, "rib_window_attn_bwd_checkpointed", q, k, v, out, pq, pk, lse, dout, window, shift, masked, workspace, stream)
@@ -890,6 +967,8 @@ def rib_window_attn_bwd_checkpointed(q, k, v, out, pq, pk, lse, dout, window, sh
 def rib_window_attn_bwd_bucketed_checkpointed(q, k, v, out, bias, buckets, lse, dout, window, shift=0, masked=False, workspace=None, stream=None):
     """Backward pass of rib_window_attn_fwd_bucketed for a layer that kept q, k, v and out as checkpoints (codes, scales).
     Returns (dq, dk, dv bf16, dbias of bias's shape and type)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_window_attn_bwd_bucketed_checkpointed, q, k, v, out, bias, buckets, lse, dout, window, shift, masked, workspace)
     if _marshal is not None:
         call = lambda address, *args: _marshal.bwd_bucketed_checkpointed(address, _lib.rib_addresses["rib_window_attn_bwd_bucketed_checkpointed_workspace"], *args)  # noqa: E731
         got = _native(call, "rib_window_attn_bwd_bucketed_checkpointed", q, k, v, out, bias, buckets, lse, dout, window, shift, masked, workspace, stream)
@@ -919,6 +998,8 @@ def _check_f32(name, t, shape):
 
 def rib_generate_features(w_h, b_h, w_pq, w_pk, window, stream=None):
     """Pq, Pk (bf16 [window^2, r]) from the generator weights (Eq. 1-3); L is read off w_h's height 2 + 4 L."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_generate_features, w_h, b_h, w_pq, w_pk, window)
     if _marshal is not None:
         got = _native(_marshal.generate, "rib_generate_features", w_h, b_h, w_pq, w_pk, window, stream)
         if got is not None:
@@ -938,6 +1019,8 @@ def rib_generate_features(w_h, b_h, w_pq, w_pk, window, stream=None):
 
 def rib_generate_features_bwd(w_h, b_h, w_pq, w_pk, dpq, dpk, window, stream=None):
     """Gradients (dw_h, db_h, dw_pq, dw_pk) of the generator weights given dpq, dpk fp32 [window^2, r]."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_generate_features_bwd, w_h, b_h, w_pq, w_pk, dpq, dpk, window)
     if _marshal is not None:
         got = _native(_marshal.generate_bwd, "rib_generate_features_bwd", w_h, b_h, w_pq, w_pk, dpq, dpk, window, stream)
         if got is not None:
