@@ -511,13 +511,13 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 const uint32_t t_o1 = tmem + lane_base + kColO + qt * kFastOCols;
                 // O and l of item i are complete (the caller has waited for its last PV): normalise, store, note overflow
                 // where the thread's row goes: map, pixel of the map (-1: no query) and head
-                struct Place { int b, pixel, h; };
+                struct Place { int b, h; long long pixel; };
                 auto place_of = [&](const LiveItem& c) -> Place {
                     const int sp = 2 * (2 * c.tp + qt) + (row >> 6);
                     int Y0, X0;
                     patch_place(geom, lists, c, sp, Y0, X0);
                     const int Y = Y0 + ((row >> 3) & 7), X = X0 + (row & 7);   // the patch does not straddle the border
-                    return Place{c.b, sp >= c.patches || Y >= p.H || X >= p.W ? -1 : Y * p.W + X, c.h};
+                    return Place{c.b, c.h, sp >= c.patches || Y >= p.H || X >= p.W ? -1 : (long long)Y * p.W + X};
                 };
                 auto epilogue = [&](int i) {
                     const Place place = place_of(items->at(i));

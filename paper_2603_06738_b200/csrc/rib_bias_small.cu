@@ -48,7 +48,7 @@ __host__ __device__ inline size_t table_floats(int M) { return (size_t)((2 * M -
 size_t shared_bytes(int n, int d, int M, bool backward)
 {
     const size_t rows = rows_of(n), pitch = (d + 15) / 16 * 16 + 8;
-    return (backward ? 4 : 3) * rows * pitch * 2 + (backward ? rows * kDSPitch * 2 : 0) + (backward ? 2 : 1) * table_floats(M) * 4 + (backward ? 4 : 2) * rows * 4;
+    return (backward ? 4 : 3) * rows * pitch * 2 + (backward ? rows * kDSPitch * 2 : 0) + (backward ? 2 : 1) * table_floats(M) * 4 + (backward ? 5 : 3) * rows * 4;
 }
 
 // The lane's part of what an x4 load names, for a tile of 16 rows x 16 columns: matrices as the A operand has them (rows, then columns 8 ..), and as
@@ -74,17 +74,18 @@ __device__ __forceinline__ Block decode_window(const Problem& p, int per_head, i
 
 // Shared memory of a block beside its rows.  place[i] = entry y side + x of window position i in the table by offset, its part of the window above
 // it (kNoPart: no token), pixel[i] = its pixel in the map or -1.
-struct Places { int *pixel, *place; };
+struct Places { long long* pixel; int* place; };
 __device__ inline void find_places(const Problem& p, const Block& w, int rows, const Places& s)
 {
     for (int i = threadIdx.x; i < rows; i += blockDim.x) {
-        int pixel = -1, place = kNoPart << 16;
+        long long pixel = -1;
+        int place = kNoPart << 16;
         if (i < p.n) {
             int Y, X;
             token_pixel(p.Hp, p.Wp, p.M, p.s, w.wy, w.wx, i, Y, X);
             const int y = i / p.M, x = i - y * p.M;
             if (Y < p.H && X < p.W) {
-                pixel = Y * p.W + X;
+                pixel = (long long)Y * p.W + X;
                 place = y * (2 * p.M - 1) + x | (p.masked ? window_part(p.M, p.s, w.wy == p.nWy - 1, w.wx == p.nWx - 1, y, x) << 16 : 0);
             }
         }
@@ -104,7 +105,7 @@ __device__ inline void gather_table(const Problem& p, int h, float* table)
 // the last channel and the last row is not touched.
 template <int kCount> struct Staged { const __nv_bfloat16* from[kCount]; __nv_bfloat16* to[kCount]; };
 template <int kP, typename T, int kCount>
-__device__ __forceinline__ void stage_as(const Problem& p, const FastDiv& by_words, const Block& w, const int* pixel, const Staged<kCount>& x)
+__device__ __forceinline__ void stage_as(const Problem& p, const FastDiv& by_words, const Block& w, const long long* pixel, const Staged<kCount>& x)
 {
     constexpr int kPer = sizeof(T) / 2;
     const size_t origin = ((size_t)w.b * p.H * p.W * p.heads + w.h) * p.d, step = (size_t)p.heads * p.d;
@@ -113,7 +114,7 @@ __device__ __forceinline__ void stage_as(const Problem& p, const FastDiv& by_wor
     for (int e = threadIdx.x; e < p.n * words; e += blockDim.x) {
         int row, c;
         by_words.divmod(e, row, c);
-        const int px = pixel[row];
+        const long long px = pixel[row];
         const size_t at = origin + px * step + c * kPer;
         T v[kCount];
 #pragma unroll
@@ -127,7 +128,7 @@ __device__ __forceinline__ void stage_as(const Problem& p, const FastDiv& by_wor
 }
 __host__ __device__ inline int elements_of_word(int d) { return d % 8 == 0 ? 8 : d % 4 == 0 ? 4 : d % 2 == 0 ? 2 : 1; }
 template <int kP, int kCount>
-__device__ __forceinline__ void stage(const Problem& p, const FastDiv& by_words, const Block& w, const int* pixel, const Staged<kCount>& x)
+__device__ __forceinline__ void stage(const Problem& p, const FastDiv& by_words, const Block& w, const long long* pixel, const Staged<kCount>& x)
 {
     switch (elements_of_word(p.d)) {
     case 8: stage_as<kP, uint4>(p, by_words, w, pixel, x); break;
@@ -147,11 +148,11 @@ __device__ __forceinline__ void store_pair(const Problem& p, __nv_bfloat16* row,
         if (c + 1 < p.d) row[c + 1] = __float2bfloat16_rn(b);
     }
 }
-__device__ __forceinline__ __nv_bfloat16* row_at(const Problem& p, const Block& w, __nv_bfloat16* x, int pixel)
+__device__ __forceinline__ __nv_bfloat16* row_at(const Problem& p, const Block& w, __nv_bfloat16* x, long long pixel)
 {
     return x + (((size_t)w.b * p.H * p.W + pixel) * p.heads + w.h) * p.d;
 }
-__device__ __forceinline__ size_t scalar_at(const Problem& p, const Block& w, int pixel) { return ((size_t)w.b * p.heads + w.h) * p.H * p.W + pixel; }
+__device__ __forceinline__ size_t scalar_at(const Problem& p, const Block& w, long long pixel) { return ((size_t)w.b * p.heads + w.h) * p.H * p.W + pixel; }
 
 // zeros behind the last channel of the rows and behind the last row, which stay
 __device__ inline void clear_rows(__nv_bfloat16* rows, int elements)
@@ -167,7 +168,8 @@ __global__ void __launch_bounds__(2 * kMaxTokens) rib_bias_small_fwd_kernel(cons
     const int rows = rows_of(p.n), side = 2 * p.M - 1, lane = threadIdx.x & 31, tile = (threadIdx.x >> 5) * 16, c2 = 2 * (lane & 3);
     __nv_bfloat16 *const qs = reinterpret_cast<__nv_bfloat16*>(sm), *const ks = qs + rows * kP, *const vs = ks + rows * kP;
     float* const table = reinterpret_cast<float*>(vs + rows * kP);
-    const Places s{reinterpret_cast<int*>(table + table_floats(p.M)), reinterpret_cast<int*>(table + table_floats(p.M)) + rows};
+    long long* const pixels = reinterpret_cast<long long*>(table + table_floats(p.M));
+    const Places s{pixels, reinterpret_cast<int*>(pixels + rows)};
     const int per_head = p.pairs / p.heads;
     const int first = (int)((long long)p.pairs * blockIdx.x / gridDim.x), last = (int)((long long)p.pairs * (blockIdx.x + 1) / gridDim.x);
     const float scale = rsqrtf((float)p.d) * kLog2e;
@@ -263,7 +265,7 @@ __global__ void __launch_bounds__(2 * kMaxTokens) rib_bias_small_fwd_kernel(cons
         for (int step = 1; step < 4; step <<= 1) { l0 += __shfl_xor_sync(0xffffffffu, l0, step); l1 += __shfl_xor_sync(0xffffffffu, l1, step); }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int pixel = s.pixel[r0 + 8 * half];
+            const long long pixel = s.pixel[r0 + 8 * half];
             if (pixel < 0) continue;
             const float l = half ? l1 : l0, f = l == 0.f ? 0.f : 1.f / l;             // a row without any key: out 0, lse minus infinity
             __nv_bfloat16* const to = row_at(p, w, p.out_w, pixel);
@@ -284,7 +286,8 @@ __global__ void __launch_bounds__(2 * kMaxTokens) rib_bias_small_bwd_kernel(cons
     __nv_bfloat16* const ds = gs + rows * kP;              // [key][kDSPitch]; before that, the rows of out
     float *const table = reinterpret_cast<float*>(ds + rows * kDSPitch), *const sums = table + table_floats(p.M);
     float *const lse = sums + table_floats(p.M), *const D = lse + rows;
-    const Places s{reinterpret_cast<int*>(D + rows), reinterpret_cast<int*>(D + rows) + rows};
+    long long* const pixels = reinterpret_cast<long long*>(D + rows);
+    const Places s{pixels, reinterpret_cast<int*>(pixels + rows)};
     const int per_head = p.pairs / p.heads;
     const int first = (int)((long long)p.pairs * blockIdx.x / gridDim.x), last = (int)((long long)p.pairs * (blockIdx.x + 1) / gridDim.x);
     const float isd = rsqrtf((float)p.d), scale = isd * kLog2e;
@@ -414,7 +417,7 @@ __global__ void __launch_bounds__(2 * kMaxTokens) rib_bias_small_bwd_kernel(cons
                 }
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const int pixel = s.pixel[block + query + (lane >> 2) + 8 * half];
+                    const long long pixel = s.pixel[block + query + (lane >> 2) + 8 * half];
                     if (pixel < 0) continue;
                     __nv_bfloat16* const to = row_at(p, w, p.dq, pixel);
 #pragma unroll
@@ -425,7 +428,7 @@ __global__ void __launch_bounds__(2 * kMaxTokens) rib_bias_small_bwd_kernel(cons
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int pixel = s.pixel[r0 + 8 * half];
+            const long long pixel = s.pixel[r0 + 8 * half];
             if (pixel < 0) continue;
             __nv_bfloat16 *const to_v = row_at(p, w, p.dv, pixel), *const to_k = row_at(p, w, p.dk, pixel);
 #pragma unroll
