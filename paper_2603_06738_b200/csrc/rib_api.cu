@@ -23,7 +23,11 @@ int check_shape(int B, int H, int W, int heads, int d, int r, int window, int sh
     if (!partial_windows && (H % window || W % window)) return RIB_ERR_SHAPE;
     if (shift < 0 || shift >= window) return RIB_ERR_SHAPE;
     if (d > 64 || r > 64) return RIB_ERR_UNSUPPORTED;      // any width up to 64: the any-shape kernels read element by element
-    const long long pairs = (long long)B * ((H + window - 1) / window) * ((W + window - 1) / window) * heads;
+    // places of windows laid over the map, shifted and not yet wrapped, are ints
+    const long long rows = ((long long)H + window - 1) / window, columns = ((long long)W + window - 1) / window;
+    if ((rows + 1) * window > 0x7fffffffLL || (columns + 1) * window > 0x7fffffffLL) return RIB_ERR_UNSUPPORTED;
+    if (rows * columns > 0x7fffffffLL || rows * columns * B > 0x7fffffffLL) return RIB_ERR_SHAPE;          // (each factor below 2^31: no product passes 64 bits)
+    const long long pairs = rows * columns * B * heads;
     if (pairs > 0x7fffffffLL || (long long)window * window > (1 << 20)) return RIB_ERR_SHAPE;
     // launch limits of the kernels: the any-shape kernels put n / 16 row groups on grid.y, the tcgen05 kernels count
     // pairs * key blocks in an int
@@ -54,7 +58,7 @@ int device_status_ptr(int** out)
 void fill_shape(rib::Problem& p, int B, int H, int W, int heads, int d, int r, int window, int shift)
 {
     p.B = B; p.H = H; p.W = W; p.heads = heads; p.d = d; p.r = r; p.M = window; p.s = shift;
-    p.nWy = (H + window - 1) / window; p.nWx = (W + window - 1) / window;   // exact in the plain calls (H, W multiples of window)
+    p.nWy = (int)(((long long)H + window - 1) / window); p.nWx = (int)(((long long)W + window - 1) / window);   // exact in the plain calls (H, W multiples of window)
     p.Hp = p.nWy * window; p.Wp = p.nWx * window;
     p.n = window * window;
     p.pairs = B * p.nWy * p.nWx * heads;
