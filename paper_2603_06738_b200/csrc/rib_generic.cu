@@ -67,10 +67,11 @@ __device__ inline float with_bias(const Problem& p, int h, float s, int i, int j
 }
 // exp(s - lse).  A row that a bias leaves no key has lse = -inf, and so has every s of it; without a bias such a row is one of infinite inputs, and NaN.
 // Under a bias, which may be large, it is held to 1 whatever lse has left of its digits (NaN stays).
-__device__ inline float probability(const Problem& p, float s, float lse)
+template <bool kBias>
+__device__ inline float probability(float s, float lse)
 {
     const float x = s - lse;
-    return !p.bias ? expf(x) : s == -INFINITY ? 0.f : expf(x > 0.f ? 0.f : x);
+    return !kBias ? expf(x) : s == -INFINITY ? 0.f : expf(x > 0.f ? 0.f : x);
 }
 
 // element offset of channel 0 of token i of the pair in a [B][H][W][heads][d] tensor (the token must exist)
@@ -99,18 +100,23 @@ __device__ inline float warp_sum(float v)
     return v;
 }
 
+// Lanes that share a row to stage it, 2^log_lanes, of four to eight elements each (narrow rows: one lane).  Each works the row's place out, which a lane per element, or a
+// warp per row, does too often, and the fewer they are, the further apart the elements that they read together.  (Two maps of 64 x 64 tokens, 2 heads, d = 40, r = 24, windows
+// of 16, forward / backward 125 / 395 us, a lane per element 224 / 775, a warp per row 175 / 518; d = 5, windows of 30: 369 / 1303, 419 / 1599, 812 / 2291.)
+__device__ inline int log_lanes(int width) { return width <= 8 ? 0 : width <= 16 ? 1 : width <= 32 ? 2 : width <= 64 ? 3 : 4; }
+
 // Stage rows [row0, row0+rows) of the pair as concatenated fp32 rows [x_i * sx, p_i * sp] with
 // leading dimension ld; rows beyond n are zero.  x is an image tensor, pos is pq or pk.
 __device__ inline void stage_concat(const Problem& p, const PairCoord& c, const __nv_bfloat16* x,
                                     const __nv_bfloat16* pos, float sx, float sp, int row0,
                                     int rows, int ld, float* dst)
 {
-    const int dk = p.d + p.r, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int rr = warp; rr < rows; rr += kWarps) {          // (a row's place is worked out once)
+    const int dk = p.d + p.r, log = log_lanes(dk);
+    for (int rr = threadIdx.x >> log; rr < rows; rr += kThreads >> log) {
         const int i = row0 + rr;
         const bool real = i < p.n && token_exists(p, c, i);
         const size_t off = real ? token_offset(p, c, i) : 0, row = (size_t)c.h * p.pos_head_stride + (size_t)i * p.r;
-        for (int col = lane; col < dk; col += 32)
+        for (int col = threadIdx.x & ((1 << log) - 1); col < dk; col += 1 << log)
             dst[rr * ld + col] = !real ? 0.f : col < p.d ? __bfloat162float(x[off + col]) * sx : __bfloat162float(pos[row + (col - p.d)]) * sp;
     }
 }
@@ -119,17 +125,19 @@ __device__ inline void stage_concat(const Problem& p, const PairCoord& c, const 
 __device__ inline void stage_plain(const Problem& p, const PairCoord& c, const __nv_bfloat16* x,
                                    int row0, int rows, int ld, float* dst)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int rr = warp; rr < rows; rr += kWarps) {
+    const int log = log_lanes(p.d);
+    for (int rr = threadIdx.x >> log; rr < rows; rr += kThreads >> log) {
         const int i = row0 + rr;
         const bool real = i < p.n && token_exists(p, c, i);
         const size_t off = real ? token_offset(p, c, i) : 0;
-        for (int col = lane; col < p.d; col += 32) dst[rr * ld + col] = real ? __bfloat162float(x[off + col]) : 0.f;
+        for (int col = threadIdx.x & ((1 << log) - 1); col < p.d; col += 1 << log) dst[rr * ld + col] = real ? __bfloat162float(x[off + col]) : 0.f;
     }
 }
 
 // ---------------------------------------------------------------------------------- forward
 // grid (pairs, ceil(n / kRows)).  Online softmax over key tiles of kTile.
+// kBias: a bias by buckets.  A form of its own: its tests in the loops, not taken, cost narrow heads 9 % (d = 1, windows of 5: 137 -> 150 us).
+template <bool kBias>
 __global__ void __launch_bounds__(kThreads) generic_fwd_kernel(const Problem p)
 {
     extern __shared__ float sm[];
@@ -161,7 +169,7 @@ __global__ void __launch_bounds__(kThreads) generic_fwd_kernel(const Problem p)
                 s1 = fmaf(a, Kt[(lane + 32) * ldk + col], s1);
             }
             const int qi = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
-            if (p.bias) { s0 = with_bias(p, c.h, s0, qi, min(j0 + lane, p.n - 1)); s1 = with_bias(p, c.h, s1, qi, min(j0 + lane + 32, p.n - 1)); }
+            if (kBias) { s0 = with_bias(p, c.h, s0, qi, min(j0 + lane, p.n - 1)); s1 = with_bias(p, c.h, s1, qi, min(j0 + lane + 32, p.n - 1)); }
             if (j0 + lane >= p.n || !token_exists(p, c, j0 + lane) || !pair_allowed(p, c, qi, j0 + lane)) s0 = -INFINITY;
             if (j0 + lane + 32 >= p.n || !token_exists(p, c, j0 + lane + 32) || !pair_allowed(p, c, qi, j0 + lane + 32)) s1 = -INFINITY;
             const float m_new = fmaxf(m[rr], warp_max(fmaxf(s0, s1)));
@@ -169,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) generic_fwd_kernel(const Problem p)
             const bool none = m_new == -INFINITY;
             const float alpha = none ? 1.f : expf(m[rr] - m_new);
             // (under a bias such a row has l = 0 and is one without keys, unless its scores are no numbers)
-            const float p0 = none && !(p.bias && isnan(s0)) ? 0.f : expf(s0 - m_new), p1 = none && !(p.bias && isnan(s1)) ? 0.f : expf(s1 - m_new);
+            const float p0 = none && !(kBias && isnan(s0)) ? 0.f : expf(s0 - m_new), p1 = none && !(kBias && isnan(s1)) ? 0.f : expf(s1 - m_new);
             l[rr] = l[rr] * alpha + warp_sum(p0 + p1);
             m[rr] = m_new;
             o[rr][0] *= alpha; o[rr][1] *= alpha;
@@ -192,7 +200,7 @@ __global__ void __launch_bounds__(kThreads) generic_fwd_kernel(const Problem p)
         const int i = row0 + warp * kRowsPerWarp + rr;
         if (i >= p.n || !token_exists(p, c, i)) continue;
         const size_t off = token_offset(p, c, i);
-        const float inv = p.bias && l[rr] == 0.f ? 0.f : 1.f / l[rr];          // (0: a bias that leaves the row no key)
+        const float inv = kBias && l[rr] == 0.f ? 0.f : 1.f / l[rr];          // (0: a bias that leaves the row no key)
         const float g0 = p.gate && lane < p.d ? __bfloat162float(p.gate[off + lane]) : 1.f;            // Eq. 9
         const float g1 = p.gate && lane + 32 < p.d ? __bfloat162float(p.gate[off + lane + 32]) : 1.f;
         if (lane < p.d) p.out_w[off + lane] = __float2bfloat16_rn(o[rr][0] * inv * g0);
@@ -221,6 +229,7 @@ __global__ void rowdot_kernel(const Problem p, size_t items)
 // ------------------------------------------------------- backward: dq and dPq (by query row)
 // dQ~_i = sum_j dS_ij [k_j, pk_j]; columns < d give dq (times 1/sqrt d), the rest dPq (1/sqrt r).
 // With a bias by buckets dS is also summed by offset, in 64 bits: the order of the adds is then lost in the rounding to the result.
+template <bool kBias>
 __global__ void __launch_bounds__(kThreads) generic_bwd_dq_kernel(const Problem p, double* offset_sums)
 {
     extern __shared__ float sm[];
@@ -267,14 +276,14 @@ __global__ void __launch_bounds__(kThreads) generic_bwd_dq_kernel(const Problem 
             }
             // keys beyond the window or, on an extended map, beyond the image have probability 0
             const int qi = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
-            if (p.bias) { s0 = with_bias(p, c.h, s0, qi, min(j0 + lane, p.n - 1)); s1 = with_bias(p, c.h, s1, qi, min(j0 + lane + 32, p.n - 1)); }
-            const float p0 = j0 + lane < p.n && token_exists(p, c, j0 + lane) && pair_allowed(p, c, qi, j0 + lane) ? probability(p, s0, lse[rr]) : 0.f;
-            const float p1 = j0 + lane + 32 < p.n && token_exists(p, c, j0 + lane + 32) && pair_allowed(p, c, qi, j0 + lane + 32) ? probability(p, s1, lse[rr]) : 0.f;
+            if (kBias) { s0 = with_bias(p, c.h, s0, qi, min(j0 + lane, p.n - 1)); s1 = with_bias(p, c.h, s1, qi, min(j0 + lane + 32, p.n - 1)); }
+            const float p0 = j0 + lane < p.n && token_exists(p, c, j0 + lane) && pair_allowed(p, c, qi, j0 + lane) ? probability<kBias>(s0, lse[rr]) : 0.f;
+            const float p1 = j0 + lane + 32 < p.n && token_exists(p, c, j0 + lane + 32) && pair_allowed(p, c, qi, j0 + lane + 32) ? probability<kBias>(s1, lse[rr]) : 0.f;
             float* srow = Ss + (warp * kRowsPerWarp + rr) * kTile;
             const float ds0 = p0 * (g0 - Di[rr]), ds1 = p1 * (g1 - Di[rr]);
             srow[lane] = ds0;
             srow[lane + 32] = ds1;
-            if (p.bias && row0 + warp * kRowsPerWarp + rr < p.n && token_exists(p, c, qi)) {
+            if (kBias && row0 + warp * kRowsPerWarp + rr < p.n && token_exists(p, c, qi)) {
                 double* sums = offset_sums + (size_t)c.h * (2 * p.M - 1) * (2 * p.M - 1);
                 if (p0 != 0.f) atomicAdd(sums + bias_offset(p, qi, j0 + lane), (double)ds0);
                 if (p1 != 0.f) atomicAdd(sums + bias_offset(p, qi, j0 + lane + 32), (double)ds1);
@@ -305,6 +314,7 @@ __global__ void __launch_bounds__(kThreads) generic_bwd_dq_kernel(const Problem 
 
 // ------------------------------------------------ backward: dk, dv and dPk (by key row)
 // dK~_j = sum_i dS_ij [q_i/sqrt d, pq_i/sqrt r]; dV_j = sum_i P_ij dO_i.
+template <bool kBias>
 __global__ void __launch_bounds__(kThreads) generic_bwd_dkv_kernel(const Problem p)
 {
     extern __shared__ float sm[];
@@ -355,9 +365,9 @@ __global__ void __launch_bounds__(kThreads) generic_bwd_dkv_kernel(const Problem
                 g1 = fmaf(a, Gt[(lane + 32) * ldv + col], g1);
             }
             const int kj = min(row0 + warp * kRowsPerWarp + rr, p.n - 1);
-            if (p.bias) { s0 = with_bias(p, c.h, s0, min(i0 + lane, p.n - 1), kj); s1 = with_bias(p, c.h, s1, min(i0 + lane + 32, p.n - 1), kj); }
-            const float p0 = i0 + lane < p.n && pair_allowed(p, c, i0 + lane, kj) ? probability(p, s0, Lt[lane]) : 0.f;
-            const float p1 = i0 + lane + 32 < p.n && pair_allowed(p, c, i0 + lane + 32, kj) ? probability(p, s1, Lt[lane + 32]) : 0.f;
+            if (kBias) { s0 = with_bias(p, c.h, s0, min(i0 + lane, p.n - 1), kj); s1 = with_bias(p, c.h, s1, min(i0 + lane + 32, p.n - 1), kj); }
+            const float p0 = i0 + lane < p.n && pair_allowed(p, c, i0 + lane, kj) ? probability<kBias>(s0, Lt[lane]) : 0.f;
+            const float p1 = i0 + lane + 32 < p.n && pair_allowed(p, c, i0 + lane + 32, kj) ? probability<kBias>(s1, Lt[lane + 32]) : 0.f;
             float* prow = Ps + (warp * kRowsPerWarp + rr) * kTile;
             float* srow = Ss + (warp * kRowsPerWarp + rr) * kTile;
             prow[lane] = p0; prow[lane + 32] = p1;
@@ -408,10 +418,11 @@ cudaError_t generic_fwd(const Problem& p, cudaStream_t stream)
 {
     const int dk = p.d + p.r;
     const size_t smem = sizeof(float) * ((size_t)kTile * (dk | 1) + (size_t)kTile * p.d + (size_t)kRows * dk + (size_t)kRows * kTile);
-    cudaError_t e = set_smem(generic_fwd_kernel, smem);
+    const auto kernel = p.bias ? generic_fwd_kernel<true> : generic_fwd_kernel<false>;
+    cudaError_t e = set_smem(kernel, smem);
     if (e != cudaSuccess) return e;
     dim3 grid(p.pairs, (p.n + kRows - 1) / kRows);
-    { ProfileScope scope(RIB_KERNEL_ANY_FWD, stream); generic_fwd_kernel<<<grid, kThreads, smem, stream>>>(p); }
+    { ProfileScope scope(RIB_KERNEL_ANY_FWD, stream); kernel<<<grid, kThreads, smem, stream>>>(p); }
     return cudaGetLastError();
 }
 
@@ -438,16 +449,18 @@ cudaError_t generic_bwd(const Problem& p, cudaStream_t stream, double* offset_su
     dim3 grid(p.pairs, (p.n + kRows - 1) / kRows);
     const size_t smem_q = sizeof(float) * ((size_t)kTile * (dk | 1) + (size_t)kTile * (p.d | 1) + (size_t)kRows * dk +
                                            (size_t)kRows * p.d + (size_t)kRows * kTile);
-    e = set_smem(generic_bwd_dq_kernel, smem_q);
+    const auto dq_kernel = p.bias ? generic_bwd_dq_kernel<true> : generic_bwd_dq_kernel<false>;
+    e = set_smem(dq_kernel, smem_q);
     if (e != cudaSuccess) return e;
-    { ProfileScope scope(RIB_KERNEL_ANY_BWD_DQ, stream); generic_bwd_dq_kernel<<<grid, kThreads, smem_q, stream>>>(p, offset_sums); }
+    { ProfileScope scope(RIB_KERNEL_ANY_BWD_DQ, stream); dq_kernel<<<grid, kThreads, smem_q, stream>>>(p, offset_sums); }
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const size_t smem_k = sizeof(float) * ((size_t)kTile * (dk | 1) + (size_t)kTile * (p.d | 1) + 2 * (size_t)kTile +
                                            (size_t)kRows * dk + (size_t)kRows * p.d + 2 * (size_t)kRows * kTile);
-    e = set_smem(generic_bwd_dkv_kernel, smem_k);
+    const auto dkv_kernel = p.bias ? generic_bwd_dkv_kernel<true> : generic_bwd_dkv_kernel<false>;
+    e = set_smem(dkv_kernel, smem_k);
     if (e != cudaSuccess) return e;
-    { ProfileScope scope(RIB_KERNEL_ANY_BWD_DKV, stream); generic_bwd_dkv_kernel<<<grid, kThreads, smem_k, stream>>>(p); }
+    { ProfileScope scope(RIB_KERNEL_ANY_BWD_DKV, stream); dkv_kernel<<<grid, kThreads, smem_k, stream>>>(p); }
     return cudaGetLastError();
 }
 
