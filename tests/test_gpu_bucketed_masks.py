@@ -131,3 +131,39 @@ def test_rows_whose_biases_are_all_very_low(case, low):
         assert (np.abs(dv - ref_dv) <= 0.5 * reach + 2.0 ** -8 * np.abs(ref_dv) + 1e-6).all()
         for got, ref, other in ((dq, ref_dq, k), (dk, ref_dk, q)):
             assert np.linalg.norm(got - ref) <= 0.5 * norm * np.linalg.norm(to_f64(other)) / np.sqrt(d)
+
+
+@pytest.mark.parametrize("case", SHAPES, ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("path", [binding.RIB_PATH_NONE, binding.RIB_PATH_SM100_EXACT, binding.RIB_PATH_GENERIC])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf")])
+def test_a_key_with_an_infinite_channel(case, path, value):
+    """The sign of a query's channel decides: a logit of plus infinity makes out and lse of the row NaN, one of minus infinity is a weight of 0, and the row is what a very
+    low logit leaves of it.  Rows that do not attend to the key do not notice it.  Every path has the same rows."""
+    B, H, W, heads, d, M, s = case
+    named = log_map(M)
+    named[np.add.outer(np.arange(2 * M - 1) * 5, np.arange(2 * M - 1) * 3) % 7 < 3] = -1
+    named[M - 1, M - 1] = 0
+    q, k, v, _, bias, named = make(B, H, W, heads, d, M, named, torch.float32, seed=37)
+    q[..., 1] = torch.where(q[..., 1] == 0, 0.5, q[..., 1].float()).bfloat16()
+    py, px = places(H, M, s), places(W, M, s)
+    h, KY, KX = heads - 1, int(np.where(py == 2)[0][0]), int(np.where(px == 6)[0][0])
+    far, bad = k.clone(), k.clone()
+    bad[0, KY, KX, h, 1] = value
+    far[0, KY, KX, h, 1] = float(np.sign(value)) * 1e30
+    old = binding.rib_set_path(path)
+    try:
+        out, lse = binding.rib_window_attn_fwd_bucketed(*(t.cuda() for t in (q, bad, v, bias, named)), M, s)
+    finally:
+        binding.rib_set_path(old)
+    ref_out, ref_lse = orc.fwd(*(to_f64(t) for t in (q, far, v, bias)), named.numpy(), M, s)
+    lost = np.zeros((H, W, heads), dtype=bool)
+    for Y in range(H):
+        for X in range(W):
+            dy, dx = 2 - py[Y], 6 - px[X]
+            if py[Y] // M == 0 and px[X] // M == 0 and named[dy + M - 1, dx + M - 1] >= 0:
+                lost[Y, X, h] = float(q[0, Y, X, h, 1]) * value > 0
+    assert 0 < lost.sum() < M * M - 1
+    got_out, got_lse = to_f64(out)[0], to_f64(lse)[0].transpose(1, 2, 0)
+    assert np.array_equal(np.isnan(got_lse), lost) and np.array_equal(np.isnan(got_out).all(-1), lost) and np.array_equal(np.isnan(got_out).any(-1), lost)
+    close("out", torch.from_numpy(got_out[~lost]), ref_out[0][~lost])
+    close("lse", torch.from_numpy(got_lse[~lost]), ref_lse[0].transpose(1, 2, 0)[~lost])
