@@ -426,6 +426,8 @@ int rib_checkpoint_restore(const void* codes, const float* scales, long long row
  * The backward passes of a layer whose q, k, v and out (in this order in `saved`) are kept as checkpoints of
  * B * H * W * heads rows each, in the layout of the tensors.  lse is the one of the forward pass; everything else is as for
  * rib_window_attn_bwd_padded / _masked (pos_head_stride, masked) and rib_window_attn_bwd_bucketed.
+ * The values are code * scale rounded to bf16 (as rib_checkpoint_restore gives them); with heads of 8 and 16 channels the tcgen05 kernels take more of their digits
+ * where those decide (q and k in the logits, k in dq).
  */
 typedef struct rib_checkpoint { const void* codes; const float* scales; } rib_checkpoint;
 size_t rib_window_attn_bwd_checkpointed_workspace(long long pos_head_stride, int B, int H, int W, int heads, int d, int r, int window);

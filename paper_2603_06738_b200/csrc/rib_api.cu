@@ -478,9 +478,10 @@ struct Restored {
     size_t rest_bytes;
 };
 
-int restore(const Restored& r, void* stream)
+int restore(const Restored& r, void* stream, bool wide = false)
 {
-    if (rib::checkpoint_restore(r.t, 4, r.rows, r.d, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RIB_ERR_CUDA;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if ((wide ? rib::checkpoint_restore_wide(r.t, r.rows, r.d, st) : rib::checkpoint_restore(r.t, 4, r.rows, r.d, st)) != cudaSuccess) return RIB_ERR_CUDA;
     g_kernel_launches += 1;
     return RIB_OK;
 }
@@ -553,6 +554,7 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
         const rib::BiasGrad g = rib::bias_grad_layout(heads, rib::bias_tables(p), window, bias->num_buckets,
                                                       static_cast<unsigned char*>(workspace) + bucketed_attention_bytes(B, H, W, heads, window));
         const bool fast = g_forced_path.load() != RIB_PATH_GENERIC && rib::sm100_bias_bwd_supported(p);
+        if (saved && fast && rib::restored_width(d) != d) p.qk_width = rib::restored_width(d);
         if (saved && fast) p.saved = saved->t;
         else if (saved)
             if (int rc = restore(*saved, stream)) return rc;
@@ -575,9 +577,10 @@ static int bwd_impl(const void* q, const void* k, const void* v, const void* pq,
     }
     const bool allowed = g_forced_path.load() != RIB_PATH_GENERIC;
     bool fast = allowed && rib::sm100_bwd_supported(p);
+    if (saved && fast && rib::restored_width(d) != d) p.qk_width = rib::restored_width(d);
     if (saved && fast && rib::sm100_bwd_takes_saved(p)) p.saved = saved->t;
     else if (saved)
-        if (int rc = restore(*saved, stream)) return rc;
+        if (int rc = restore(*saved, stream, p.qk_width != 0)) return rc;
     int launches = fast ? rib::sm100_bwd_launches(p) : 3;          // any-shape kernels: rowdot, dq, dk/dv
     cudaError_t e;
     if (fast) {
@@ -702,6 +705,11 @@ int check_checkpoint(const void* codes, const float* scales, long long rows, int
 }
 
 size_t image_bytes(int B, int H, int W, int heads, int d) { return (2 * (size_t)B * H * W * heads * d + 255) & ~(size_t)255; }
+// q and k (which may be restored to wider rows), v and out
+size_t restored_bytes(int B, int H, int W, int heads, int d)
+{
+    return 2 * (image_bytes(B, H, W, heads, rib::restored_width(d)) + image_bytes(B, H, W, heads, d));
+}
 
 int plan_restore(const rib_checkpoint* saved, int B, int H, int W, int heads, int d, void* workspace, size_t workspace_bytes, Restored* r)
 {
@@ -713,14 +721,14 @@ int plan_restore(const rib_checkpoint* saved, int B, int H, int W, int heads, in
     r->d = d;
     for (int i = 0; i < 4; ++i)
         if (int rc = check_checkpoint(saved[i].codes, saved[i].scales, r->rows, d)) return rc;
-    const size_t image = image_bytes(B, H, W, heads, d);
-    if (!workspace || workspace_bytes < 4 * image) return RIB_ERR_WORKSPACE;
+    const size_t all = restored_bytes(B, H, W, heads, d);
+    if (!workspace || workspace_bytes < all) return RIB_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return RIB_ERR_ALIGN;
     unsigned char* at = static_cast<unsigned char*>(workspace);
-    for (int i = 0; i < 4; ++i, at += image)
+    for (int i = 0; i < 4; at += image_bytes(B, H, W, heads, i < 2 ? rib::restored_width(d) : d), ++i)
         r->t[i] = {static_cast<const int8_t*>(saved[i].codes), saved[i].scales, reinterpret_cast<__nv_bfloat16*>(at)};
     r->rest = at;
-    r->rest_bytes = workspace_bytes - 4 * image;
+    r->rest_bytes = workspace_bytes - all;
     return RIB_OK;
 }
 
@@ -767,7 +775,7 @@ int rib_checkpoint_restore(const void* codes, const float* scales, long long row
 size_t rib_window_attn_bwd_checkpointed_workspace(long long pos_head_stride, int B, int H, int W, int heads, int d, int r, int window)
 {
     const size_t need = rib_window_attn_bwd_padded_workspace(pos_head_stride, B, H, W, heads, d, r, window);
-    return need ? need + 4 * image_bytes(B, H, W, heads, d) : 0;
+    return need ? need + restored_bytes(B, H, W, heads, d) : 0;
 }
 
 int rib_window_attn_bwd_checkpointed(const rib_checkpoint* saved, const void* pq, const void* pk, long long pos_head_stride, const float* lse,
@@ -784,7 +792,7 @@ int rib_window_attn_bwd_checkpointed(const rib_checkpoint* saved, const void* pq
 size_t rib_window_attn_bwd_bucketed_checkpointed_workspace(long long bias_head_stride, int num_buckets, int B, int H, int W, int heads, int d, int window)
 {
     const size_t need = bucketed_workspace(bias_head_stride, num_buckets, B, H, W, heads, d, window);
-    return need ? need + 4 * image_bytes(B, H, W, heads, d) : 0;
+    return need ? need + restored_bytes(B, H, W, heads, d) : 0;
 }
 
 int rib_window_attn_bwd_bucketed_checkpointed(const rib_checkpoint* saved, const void* bias, int bias_dtype, long long bias_head_stride,

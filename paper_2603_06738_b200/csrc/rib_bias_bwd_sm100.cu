@@ -91,11 +91,11 @@ constexpr uint32_t kIdescQ = idesc_bf16_f32_ab(kTile, kD, true, true);        //
 
 struct Params {
     const uint4* ld;           // [pairs][n], patches of the window in rows: per query the parts of -lse sqrt(d) and -D; then one patch of no queries
-    float* dq_acc;             // [pairs][d / 4][n][4] fp32, zeroed by the preparation kernel
+    float* dq_acc;             // [pairs][columns / 4][n][4] fp32, zeroed by the preparation kernel
     float* blocks;             // BiasGrad::blocks
     int* status;
     long long no_queries;      // element of ld where the patch of no queries begins
-    int H, W, heads, d, M, s, n, nWy, nWx, Hp, Wp;
+    int H, W, heads, columns, M, s, n, nWy, nWx, Hp, Wp;
     int items;
     int slots;                 // of K and V
     uint32_t slots_at;         // in shared memory
@@ -510,7 +510,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (!items_ready(nitem)) { ok = false; break; }
             const LiveItem c = items->at(nitem);
             const int tiles = (c.patches + 1) >> 1;
-            float* const acc = p.dq_acc + pair_of(p, c) * p.d * p.n;
+            float* const acc = p.dq_acc + pair_of(p, c) * p.columns * p.n;
             for (int I = 0; I < tiles && ok; ++I, ++g) {
                 // (dV and dK before the item's last dQ: those of the next item wait for the accumulators)
                 if (I == tiles - 1) ok = drain_item(c, nitem, p.slots_at + slot * kSlotBytes + kContentBytes);
@@ -531,7 +531,7 @@ rib_bias_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     if (sp < c.patches) {
 #pragma unroll
                         for (int col = 0; col < 16; col += 4) {
-                            if (16 * part + col >= p.d) break;          // (a head narrower than 32 channels)
+                            if (16 * part + col >= p.columns) break;          // (a head narrower than 32 channels)
                             // The adds of a tile in one burst fill the queue that all warps' loads, stores and fences go through: a pause after each one
                             red_add_f32x4(dst, a + col);
                             dst += 4 * (size_t)p.n;
@@ -638,6 +638,8 @@ struct AuxParams {
     __nv_bfloat16* dq;
     CheckpointRows saved[4];     // kSaved: q, k, v, out
     int H, W, heads, M, s, n, patches, d, Hp, Wp;      // patches: of all pairs
+    int columns;                 // of the dQ accumulators: d, or 32 where those from 16 on have dS times what the rounding of k left
+    int wide;                    // kSaved: 1: q and k are restored to rows of 32 columns (restore_wide)
     FastDiv by_patches, by_heads, by_nwx, by_nwy, by_row;
     float inv_sqrt_d, sqrt_d;
 };
@@ -691,6 +693,15 @@ __global__ void __launch_bounds__(64 * kLanes) rib_bias_bwd_prepare_kernel(const
     const bool real = decode_token(p, blockIdx.x, threadIdx.x / kLanes, pair, patch, tok, scalar);
     uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
     float lse = -INFINITY;
+    const bool wide = kSaved && kLanes == 2 && p.wide;
+    if (wide && real) {
+        // (logits of 8 channels; those of 16 lose less, and stay those of the call from the restored tensors)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            if (p.d == 8) restore_wide<true>(p.saved, tok, 8, part + 2 * half);
+            else restore_wide<false>(p.saved, tok, 16, part + 2 * half);
+        }
+    }
     if (real && 8 * part < p.d) {
         x = __ldg(reinterpret_cast<const uint4*>(p.dout + tok * p.d) + part);
         if (kSaved) {
@@ -702,17 +713,18 @@ __global__ void __launch_bounds__(64 * kLanes) rib_bias_bwd_prepare_kernel(const
                 scale[i] = __ldg(p.saved[i].scales + tok);
             }
 #pragma unroll
-            for (int i = 0; i < 3; ++i) reinterpret_cast<uint4*>(p.saved[i].x + tok * p.d)[part] = restored_chunk(c[i], scale[i]);
+            for (int i = 0; i < 3; ++i)
+                if (i == 2 || !wide) reinterpret_cast<uint4*>(p.saved[i].x + tok * p.d)[part] = restored_chunk(c[i], scale[i]);
             y = restored_chunk(c[3], scale[3]);
         } else {
             y = __ldg(reinterpret_cast<const uint4*>(p.out + tok * p.d) + part);
         }
         if (part == 0) lse = p.lse[scalar];
     }
-    float4* z4 = reinterpret_cast<float4*>(p.dq_acc);      // pairs * d * n floats
+    float4* z4 = reinterpret_cast<float4*>(p.dq_acc);      // pairs * columns * n floats
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-        if (k * kLanes * total + thread < total * (p.d / 4)) z4[k * kLanes * total + thread] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < (kSaved && kLanes == 2 ? 4 : 2); ++k)
+        if (k * kLanes * total + thread < total * (p.columns / 4)) z4[k * kLanes * total + thread] = make_float4(0.f, 0.f, 0.f, 0.f);
     const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
     float acc = 0.f;
 #pragma unroll
@@ -743,11 +755,15 @@ __global__ void __launch_bounds__(256) rib_bias_bwd_finish_kernel(const AuxParam
     int pair, patch;
     size_t tok, scalar;
     if (!decode_token(p, index, at, pair, patch, tok, scalar)) return;
-    const float4* src = reinterpret_cast<const float4*>(p.dq_acc + (size_t)pair * p.d * p.n) + (size_t)(4 * half) * p.n + 64 * patch + at;
+    const float4* src = reinterpret_cast<const float4*>(p.dq_acc + (size_t)pair * p.columns * p.n) + (size_t)(4 * half) * p.n + 64 * patch + at;
     uint32_t v[8];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const float4 f = 4 * q < channels ? src[(size_t)q * p.n] : make_float4(0.f, 0.f, 0.f, 0.f);
+        float4 f = 4 * q < channels ? src[(size_t)q * p.n] : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p.columns != p.d) {          // (16 channels)
+            const float4 rest = src[(size_t)(4 + q) * p.n];
+            f.x += rest.x; f.y += rest.y; f.z += rest.z; f.w += rest.w;
+        }
         v[2 * q] = pack_bf16x2(f.x * p.inv_sqrt_d, f.y * p.inv_sqrt_d);
         v[2 * q + 1] = pack_bf16x2(f.z * p.inv_sqrt_d, f.w * p.inv_sqrt_d);
     }
@@ -776,7 +792,7 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     uint4* ld = reinterpret_cast<uint4*>(ws);
     float* dq_acc = reinterpret_cast<float*>(ws + ld_bytes(p.pairs, p.n));
     CUtensorMap tm_q, tm_k, tm_v, tm_do, tm_dk, tm_dv;
-    if (!encode_image_map(&tm_q, p.q, p) || !encode_image_map(&tm_k, p.k, p) || !encode_image_map(&tm_v, p.v, p) || !encode_image_map(&tm_do, p.dout, p) ||
+    if (!encode_qk_map(&tm_q, p.q, p) || !encode_qk_map(&tm_k, p.k, p) || !encode_image_map(&tm_v, p.v, p) || !encode_image_map(&tm_do, p.dout, p) ||
         !encode_image_map(&tm_dk, p.dk, p, 4) || !encode_image_map(&tm_dv, p.dv, p, 4))
         return cudaErrorInvalidValue;
     static KernelSetup setup[2];
@@ -786,10 +802,12 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     if (cudaError_t e = setup[cut].prepare(kernel, most_shared(), &sm_count)) return e;
     Params bp{};
     if (!make_bias_items(p, 2, &bp.g)) return cudaErrorInvalidValue;
+    bp.columns = p.qk_width && p.d == 16 ? 32 : p.d;
     AuxParams ap{};
     ap.out = p.out; ap.dout = p.dout; ap.lse = p.lse_in; ap.ld = ld; ap.dq_acc = dq_acc; ap.dq = p.dq;
     ap.sums = grad.offsets; ap.sum_words = grad.bytes / sizeof(double);
-    ap.H = p.H; ap.W = p.W; ap.heads = p.heads; ap.M = p.M; ap.s = p.s; ap.n = p.n; ap.d = p.d;
+    ap.H = p.H; ap.W = p.W; ap.heads = p.heads; ap.M = p.M; ap.s = p.s; ap.n = p.n; ap.d = p.d; ap.columns = bp.columns;
+    ap.wide = p.qk_width != 0;
     ap.patches = (int)((long long)p.pairs * (p.n / 64));
     ap.by_patches = make_fast_div(p.n / 64); ap.by_heads = make_fast_div(p.heads); ap.by_nwx = make_fast_div(p.nWx); ap.by_nwy = make_fast_div(p.nWy); ap.by_row = make_fast_div(p.M / 8);
     ap.Hp = p.Hp; ap.Wp = p.Wp;
@@ -803,7 +821,7 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
     if (cudaError_t e = cudaGetLastError()) return e;
     bp.ld = ld; bp.dq_acc = dq_acc; bp.blocks = grad.blocks; bp.status = p.status;
     bp.no_queries = (long long)tokens;
-    bp.H = p.H; bp.W = p.W; bp.heads = p.heads; bp.d = p.d; bp.M = p.M; bp.s = p.s; bp.n = p.n; bp.nWy = p.nWy; bp.nWx = p.nWx; bp.Hp = p.Hp; bp.Wp = p.Wp;
+    bp.H = p.H; bp.W = p.W; bp.heads = p.heads; bp.M = p.M; bp.s = p.s; bp.n = p.n; bp.nWy = p.nWy; bp.nWx = p.nWx; bp.Hp = p.Hp; bp.Wp = p.Wp;
     bp.items = bp.g.per_head * p.heads;
     bp.slots = slots_of(p.M);
     bp.slots_at = slots_offset(p.M);

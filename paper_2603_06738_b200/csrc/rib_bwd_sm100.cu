@@ -606,6 +606,7 @@ struct AuxParams {
     float* dpq;
     float* dpk;
     CheckpointRows saved[4];     // kSaved: q, k, v, out
+    int wide;                    // kSaved: 1: q and k are restored to rows of 32 columns (restore_wide)
     int H, W, heads, M, s, n, nWy, nWx, pairs;
     int d, r;                    // head width and rank of the caller's tensors (the accumulators are 32 + R columns wide)
     int dq_sectors;              // 1: 16 channels of a row of dq are one 32-byte sector
@@ -664,6 +665,7 @@ __global__ void __launch_bounds__(256) rib_bwd_prepare_kernel(const AuxParams p)
     const bool real = decode_pair_token(p, pair, w, i, tok, scalar);
     uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
     float lse = 0.f;
+    if (kSaved && p.wide && real) restore_wide<true>(p.saved, tok, p.d, part);
     if (real && 8 * part < p.d) {
         x = __ldg(reinterpret_cast<const uint4*>(p.dout + tok * p.d) + part);
         if (kNarrow) {
@@ -682,7 +684,8 @@ __global__ void __launch_bounds__(256) rib_bwd_prepare_kernel(const AuxParams p)
                 scale[i] = __ldg(p.saved[i].scales + tok);
             }
 #pragma unroll
-            for (int i = 0; i < 3; ++i) reinterpret_cast<uint4*>(p.saved[i].x + tok * p.d)[part] = restored_chunk(c[i], scale[i]);
+            for (int i = 0; i < 3; ++i)
+                if (i == 2 || !p.wide) reinterpret_cast<uint4*>(p.saved[i].x + tok * p.d)[part] = restored_chunk(c[i], scale[i]);
             y = restored_chunk(c[3], scale[3]);
         } else {
             y = __ldg(reinterpret_cast<const uint4*>(p.out + tok * p.d) + part);
@@ -864,7 +867,7 @@ cudaError_t launch_bwd(const Problem& p, cudaStream_t stream)
     __nv_bfloat16* pq_scaled = reinterpret_cast<__nv_bfloat16*>(ws + wl.pq_scaled);
 
     CUtensorMap tm_q, tm_k, tm_v, tm_do, tm_pqs, tm_pk, tm_dk, tm_dv;
-    if (!encode_image_map(&tm_q, p.q, p) || !encode_image_map(&tm_k, p.k, p) || !encode_image_map(&tm_v, p.v, p) ||
+    if (!encode_qk_map(&tm_q, p.q, p) || !encode_qk_map(&tm_k, p.k, p) || !encode_image_map(&tm_v, p.v, p) ||
         !encode_image_map(&tm_do, p.dout, p) || !encode_pos_map_padded(&tm_pqs, pq_scaled, p, tables, (long long)p.n * R, R) ||
         !encode_pos_map_padded(&tm_pk, p.pk, p, tables, p.pos_head_stride, p.r) || !encode_image_map(&tm_dk, p.dk, p, 4) || !encode_image_map(&tm_dv, p.dv, p, 4))
         return cudaErrorInvalidValue;
@@ -886,6 +889,7 @@ cudaError_t launch_bwd(const Problem& p, cudaStream_t stream)
     ap.inv_sqrt_d = 1.f / sqrtf(scale_width_d(p));
     ap.inv_sqrt_r = 1.f / sqrtf(scale_width_r(p));
     if (p.saved) for (int i = 0; i < 4; ++i) ap.saved[i] = p.saved[i];
+    ap.wide = p.qk_width != 0;
     const size_t tokens = (size_t)p.pairs * p.n;
     const unsigned aux_blocks = (unsigned)((tokens + 63) / 64);
     { ProfileScope scope(RIB_KERNEL_BWD_PREPARE, stream); (p.narrow ? rib_bwd_prepare_kernel<R, true> : p.saved ? rib_bwd_prepare_kernel<R, false, true> : rib_bwd_prepare_kernel<R, false>)<<<aux_blocks, 256, 0, stream>>>(ap); }

@@ -212,6 +212,20 @@ __global__ void __launch_bounds__(kThreads) rib_checkpoint_restore_staged_kernel
     }
 }
 
+// q, k, v and out of a layer with heads of 8 or 16 channels: four lanes to a row, q and k to rows of 32 columns
+__global__ void __launch_bounds__(kThreads) rib_checkpoint_restore_wide_kernel(const RestoreArgs args, long long rows, int d)
+{
+    const long long thread = (long long)blockIdx.x * kThreads + threadIdx.x, row = thread >> 2;
+    const int part = (int)(thread & 3);
+    if (row >= rows) return;
+    restore_wide<true>(args.t, (size_t)row, d, part);
+    if (8 * part >= d) return;
+#pragma unroll
+    for (int i = 2; i < 4; ++i)
+        reinterpret_cast<uint4*>(args.t[i].x + row * d)[part] =
+            restored_chunk(__ldg(reinterpret_cast<const uint2*>(args.t[i].codes + row * d) + part), __ldg(args.t[i].scales + row));
+}
+
 // 8 channels to a thread: lanes to a row as a power of two
 int lanes_of(int d) { return d <= 8 ? 1 : d <= 16 ? 2 : d <= 32 ? 4 : 8; }
 // restore: blocks of a run each, or as many as kRestoreBlocks to an SM (of 148: the same number everywhere, so that a call's shape decides the launch)
@@ -251,6 +265,15 @@ cudaError_t checkpoint_restore(const CheckpointRows* tensors, int count, long lo
         const auto kernel = lanes == 1 ? rib_checkpoint_restore_kernel<1> : lanes == 2 ? rib_checkpoint_restore_kernel<2> : lanes == 4 ? rib_checkpoint_restore_kernel<4> : rib_checkpoint_restore_kernel<8>;
         kernel<<<dim3(restore_blocks(rows, lanes, count), (unsigned)count), kThreads, 0, stream>>>(args, rows, d);
     }
+    return cudaGetLastError();
+}
+
+cudaError_t checkpoint_restore_wide(const CheckpointRows* tensors, long long rows, int d, cudaStream_t stream)
+{
+    RestoreArgs args{};
+    for (int i = 0; i < 4; ++i) args.t[i] = tensors[i];
+    ProfileScope scope(RIB_KERNEL_CHECKPOINT_RESTORE, stream);
+    rib_checkpoint_restore_wide_kernel<<<(unsigned)((4 * rows + kThreads - 1) / kThreads), kThreads, 0, stream>>>(args, rows, d);
     return cudaGetLastError();
 }
 

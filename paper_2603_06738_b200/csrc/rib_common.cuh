@@ -52,6 +52,7 @@ struct Problem {
     int num_buckets;
     void* dbias;                      // gradient, layout and type of bias
     const CheckpointRows* saved;      // backward: q, k, v, out as checkpoints, which the preparation kernel restores (q, k, v) and uses (out); null: not
+    int qk_width;                     // backward from checkpoints, narrow heads: q and k lie in rows of that width (restored_width); 0: d
     int narrow;                       // general tcgen05 backward on such copies: width of the rows of `out` and `dq`, which are the caller's; 0 = d
 };
 
@@ -136,6 +137,7 @@ cudaError_t sm100_bias_bwd(const Problem& p, const BiasGrad& grad, cudaStream_t 
 // Rows of bf16 as whole numbers of 8 bits with a scale each, and back (rib_checkpoint.cu).
 cudaError_t checkpoint_store(const __nv_bfloat16* x, long long rows, int d, int8_t* codes, float* scales, cudaStream_t stream);
 cudaError_t checkpoint_restore(const CheckpointRows* tensors, int count, long long rows, int d, cudaStream_t stream);
+cudaError_t checkpoint_restore_wide(const CheckpointRows* tensors, long long rows, int d, cudaStream_t stream);      // q, k (restore_wide), v, out
 // byte `at` of four codes as a float: 0x4B000000 + (code + 128) is 2^23 + 128 + code
 __device__ __forceinline__ float code_value(uint32_t codes_plus_128, int at)
 {
@@ -154,6 +156,39 @@ __device__ __forceinline__ uint4 restored_chunk(uint2 codes, float scale)
 {
     codes.x ^= 0x80808080u; codes.y ^= 0x80808080u;
     return make_uint4(restored_pair(codes.x, 0, scale), restored_pair(codes.x, 2, scale), restored_pair(codes.y, 0, scale), restored_pair(codes.y, 2, scale));
+}
+
+// Narrow heads.  A logit of 8 or 16 channels is a sum of few products, the largest logits have the largest errors, and with q and k rounded to bf16 the gradients are further
+// off than a backward pass's own roundings put them (dq 5.7e-3 in relative L2 of 5e-3).  So for the tcgen05 kernels q and k are restored to rows of 32 columns, which the tiles
+// have anyhow, with what the rounding leaves (lo) in the free ones.  kLogits: q = hi lo hi 0, k = hi hi lo 0 in pieces of the head's width (16 channels: the first two), so
+// that a row of one times a row of the other is their product in 16 bits, or with 16 channels that with k rounded.  Else (16 channels under a bias, whose logits lose
+// less): q = hi 0, k = hi lo, which leaves the logits as they are and puts the rest of dS k into columns 16 .. 31.
+inline int restored_width(int d) { return d == 8 || d == 16 ? 32 : d; }
+__device__ __forceinline__ void restored_parts(uint2 codes, float scale, uint4& hi, uint4& lo)
+{
+    hi = restored_chunk(codes, scale);
+    const uint32_t c[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u}, h[4] = {hi.x, hi.y, hi.z, hi.w};
+    uint32_t rest[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = code_value(c[i >> 1], 2 * (i & 1)) * scale, b = code_value(c[i >> 1], 2 * (i & 1) + 1) * scale;
+        const __nv_bfloat162 v = __floats2bfloat162_rn(a - __uint_as_float(h[i] << 16), b - __uint_as_float(h[i] & 0xffff0000u));
+        rest[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    lo = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+}
+// 8 channels `part` (0 .. 3) of the wide rows of token `tok` of q and k, heads of d channels
+template <bool kLogits>
+__device__ __forceinline__ void restore_wide(const CheckpointRows* qk, size_t tok, int d, int part)
+{
+    const int chunk = d == 16 ? part & 1 : 0, copy = d == 16 ? part >> 1 : part;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint4 hi, lo;
+        restored_parts(__ldg(reinterpret_cast<const uint2*>(qk[i].codes + tok * d) + chunk), __ldg(qk[i].scales + tok), hi, lo);
+        const bool is_hi = copy == 0 || (kLogits && copy == 2 - i), is_lo = kLogits ? copy == 1 + i : copy == 1 && i == 1;
+        reinterpret_cast<uint4*>(qk[i].x + tok * 32)[part] = is_hi ? hi : is_lo ? lo : make_uint4(0u, 0u, 0u, 0u);
+    }
 }
 
 bool sm100_fwd_supported(const Problem& p);

@@ -295,6 +295,14 @@ inline bool encode_image_map(CUtensorMap* map, const void* ptr, const Problem& p
     return cached_map(map, key, [&](CUtensorMap* m) { return encode_image_map_now(m, ptr, p, rows); });
 }
 
+// q or k of a backward pass
+inline bool encode_qk_map(CUtensorMap* map, const void* ptr, const Problem& p)
+{
+    Problem rows = p;
+    if (p.qk_width) rows.d = p.qk_width;
+    return encode_image_map(map, ptr, rows);
+}
+
 inline bool encode_pos_map_now(CUtensorMap* map, const void* ptr, const Problem& p, int tables, long long table_stride,
                                cuuint32_t box_inner, CUtensorMapSwizzle swz, int cols)
 {

@@ -588,7 +588,7 @@ cudaError_t launch_win8_bwd(const Problem& p, cudaStream_t stream)
 {
     CUtensorMap tm_q, tm_k, tm_v, tm_do, tm_o, tm_dq, tm_dk, tm_dv;
     if (!encode_fn()) return cudaErrorNotSupported;
-    if (!encode_image_map(&tm_q, p.q, p) || !encode_image_map(&tm_k, p.k, p) || !encode_image_map(&tm_v, p.v, p) || !encode_image_map(&tm_do, p.dout, p) ||
+    if (!encode_qk_map(&tm_q, p.q, p) || !encode_qk_map(&tm_k, p.k, p) || !encode_image_map(&tm_v, p.v, p) || !encode_image_map(&tm_do, p.dout, p) ||
         !encode_image_map(&tm_o, p.out, p) || !encode_image_map(&tm_dq, p.dq, p) || !encode_image_map(&tm_dk, p.dk, p) || !encode_image_map(&tm_dv, p.dv, p))
         return cudaErrorInvalidValue;
     static KernelSetup setup;
