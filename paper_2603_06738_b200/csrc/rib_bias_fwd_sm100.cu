@@ -17,7 +17,7 @@
 // row of the block's patch, two neighbouring keys, and finds their biases in 11 pairs of the table (rib_bias_sm100.cuh).
 // There is no reference m: fp32 and bf16 carry 8 exponent bits, so the exponentials of scores (with bias) up to 69 are as exact as those of
 // small ones, and a score costs one multiply-add, one exponential and half a conversion.  A row whose sum of exponentials leaves
-// [2^-32, 2^100) - large scores of either sign, rows without any key, scores that are not finite - is noted, and its item redone in the same launch
+// [2^-32, 2^100) or whose output overflows - large scores of either sign or values, rows without any key, scores that are not finite - is noted, and its item redone in the same launch
 // by the exact form: running maximum, accumulators per key half, a merge.  (A reference from the window's first 32 keys, as in the rank-r kernel: 302
 // us against 278 on 16 x 96 x 96 tokens in windows of 32.)  Every fourth pair of exponentials (kPolyMask) is evaluated on the FMA and integer pipes
 // instead of the MUFU.  Keys beyond the map's edge have zero rows of V and, for l, zeros in the tile of ones: five half tiles for
@@ -529,7 +529,10 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     tmem_wait_ld();
                     tc_fence_before();
                     const float l_all = __uint_as_float(lsum[0]);
-                    const bool bad = !no_query && !(l_all > 0x1p-32f && l_all < 0x1p100f);
+                    float2 none = make_float2(0.f, 0.f);             // 0 times the sums: NaN where one has overflowed, weights of up to 2^100 times large values
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) none = __ffma2_rn(make_float2(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])), make_float2(0.f, 0.f), none);
+                    const bool bad = !no_query && !(l_all > 0x1p-32f && l_all < 0x1p100f && none.x + none.y == 0.f);
                     if (__any_sync(0xffffffffu, bad) && lane == 0) {
                         const int slot = atomicAdd(redo_count, 1);
                         if (slot < kMaxRedo) redo_list[slot] = i;

@@ -167,3 +167,16 @@ def test_a_key_with_an_infinite_channel(case, path, value):
     assert np.array_equal(np.isnan(got_lse), lost) and np.array_equal(np.isnan(got_out).all(-1), lost) and np.array_equal(np.isnan(got_out).any(-1), lost)
     close("out", torch.from_numpy(got_out[~lost]), ref_out[0][~lost])
     close("lse", torch.from_numpy(got_lse[~lost]), ref_lse[0].transpose(1, 2, 0)[~lost])
+
+
+@pytest.mark.parametrize("case", SHAPES, ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("bias_level,v_scale", [(60.0, 2.0 ** 20), (60.0, 2.0 ** 60), (30.0, 2.0 ** 100), (-20.0, 2.0 ** 100), (0.0, 2.0 ** -60)])
+def test_large_and_small_values_beside_large_biases(case, bias_level, v_scale):
+    """A level that all biases share changes no weight, and the output is of the size of the values, whatever both are."""
+    B, H, W, heads, d, M, s = case
+    q, k, v, dout, bias, named = make(B, H, W, heads, d, M, log_map(M), torch.float32, seed=41)
+    bias += bias_level
+    out, lse, grads = run((q, k, (v.float() * v_scale).bfloat16(), dout, bias, named), M, s)
+    inputs = (q, k, v, dout, bias, named)
+    back = lambda t: t.float() / v_scale  # noqa: E731  (a power of two: exact)
+    compare(inputs, M, s, back(out), lse, (back(grads[0]), back(grads[1]), grads[2], back(grads[3])), 0)
