@@ -465,8 +465,15 @@ rib_fwd_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     tmem_wait_ld();
                     tc_fence_before();
                     const float l_all = __uint_as_float(lsum[0]);
-                    // a score left the range the fixed reference covers: the exact form redoes the item
-                    const bool bad = !no_query && !(l_all > 0.f && l_all < 1.2676506e30f);     // 2^100
+                    // a score left the range the fixed reference covers, or large weights times large values overflowed (0 times those sums is NaN; with weights of up
+                    // to 2^20 the exact form would overflow as well): the exact form redoes the item
+                    bool bad = !no_query && !(l_all > 0.f && l_all < 0x1p100f);
+                    if (l_all > 0x1p20f) {
+                        float none = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) none = fmaf(__uint_as_float(o[e]), 0.f, none);
+                        bad = bad || (!no_query && none != 0.f);
+                    }
                     if (__any_sync(0xffffffffu, bad) && lane == 0) {
                         const int slot = atomicAdd(redo_count, 1);
                         if (slot < kMaxRedo) redo_list[slot] = i;
