@@ -400,6 +400,7 @@ long long rib_kernel_launches(void);
  * The backward pass recomputes the probabilities from lse.  dbias has bias's type and layout; it is the sum of dS over all windows
  * and pairs of tokens whose offset has the bucket, and over the heads where they share a table.  Buckets that no offset
  * names get 0.  Elements between the heads' tables are left as they are.
+ * dq (tcgen05 kernels) and the sums behind dbias are accumulated with fp32 atomic adds, so their last bits may differ from run to run.
  */
 enum { RIB_DTYPE_F32 = 0, RIB_DTYPE_BF16 = 1 };
 int rib_window_attn_fwd_bucketed(const void* q, const void* k, const void* v, const void* bias, int bias_dtype, long long bias_head_stride,

@@ -57,7 +57,8 @@ __device__ __forceinline__ float2 ex2_poly2_bounded(float2 x)
 constexpr int kStages = 4;            // K/V ring depth
 constexpr int kThreads = 640;
 constexpr int kSoftmaxThreads = 512;
-constexpr int kMaxRedo = 64;          // items a CTA can note for the exact pass (more: all of its items are redone)
+constexpr int kMaxRedo = 64;          // notes a CTA takes for the exact pass, one of each softmax warp with such a row: up to 16 an item (more: all of its items are redone;
+                                      // 256 x 256 tokens in windows of 64 with every row redone: 2150 us, 410 with none)
 
 // kSFull, kPReady, kPVDone: 2 * tile + parity of the block (on_block); kDrain: one per issuing warp; kMerge: 4 * tile + quarter of the rows; kTabDone,
 // kTabReady: all softmax warps are through with the old table, have written the new one
