@@ -17,41 +17,36 @@
 // row of the block's patch, two neighbouring keys, and finds their biases in 11 pairs of the table (rib_bias_sm100.cuh).
 // There is no reference m: fp32 and bf16 carry 8 exponent bits, so the exponentials of scores (with bias) up to 69 are as exact as those of
 // small ones, and a score costs one multiply-add, one exponential and half a conversion.  A row whose sum of exponentials leaves
-// [2^-32, 2^100) or whose output overflows - large scores of either sign or values, rows without any key, scores that are not finite - is noted, and its item redone in the same launch
+// [2^-64, 2^100) or whose output overflows - large scores of either sign or values, rows without any key, scores that are not finite - is noted, and its item redone in the same launch
 // by the exact form: running maximum, accumulators per key half, a merge.  (A reference from the window's first 32 keys, as in the rank-r kernel: 302
-// us against 278 on 16 x 96 x 96 tokens in windows of 32.)  Every fourth pair of exponentials (kPolyMask) is evaluated on the FMA and integer pipes
+// us against 278 on 16 x 96 x 96 tokens in windows of 32.)  Every eighth pair of exponentials (kPolyMask) is evaluated on the FMA and integer pipes
 // instead of the MUFU.  Keys beyond the map's edge have zero rows of V and, for l, zeros in the tile of ones: five half tiles for
 // a whole patch, none, and one cut below, right or both.
 #include "rib_bias_sm100.cuh"
-
-#ifndef RIB_BIAS_POLY_MASK
-#define RIB_BIAS_POLY_MASK 0x88u
-#endif
 
 namespace rib {
 namespace {
 
 using namespace sm100;
 
-constexpr uint32_t kPolyMask = RIB_BIAS_POLY_MASK;       // of every 8 pairs of scores: which go to the FMA pipe
+// Of every 8 pairs of scores: which go to the FMA pipe.  256 x 256 tokens in windows of 64: none 444 us, the fourth 407, the eighth 418, two 417 to 425.
+constexpr uint32_t kPolyMask = 0x08u;
 
 // 2^x for a pair of arguments on the FMA and integer pipes.  x = n + f with n = round(x), |f| <= 1/2, n read off the low mantissa bits of
-// x + 1.5 * 2^23.  The cubic (relative error 7.5e-5) is evaluated with coefficients scaled by 2^-120, so its result carries the exponent field 6 or
-// 7 and 2^n is applied by adding n + 120, bounded to [0, 248], to that field: arguments below -120 (masked keys among them) yield about 2^-120, which
-// is nothing beside a row sum of at least 2^-32 (arguments of -2^46 .. -2^47, beside which 1.5 * 2^23 is lost by rounding, up to 2^-55: 4096 of them 2^-11 of
-// such a sum), and arguments from 128 on at least 2^127, which the epilogue sees in the row sum, as do some around -2^24.
+// x + 1.5 * 2^23; the cubic in f (relative error 7.5e-5) times 2^n, whose exponent field n + 127 is bounded to [0, 254]: arguments below -127 (masked keys among them)
+// yield 0, and those from 127 on, as some around -2^24, at least 2^126, which the epilogue sees in the row sum.  (With 2^n added to the exponent of a cubic that is scaled by 2^-120, an
+// instruction less, masked keys kept a weight of 2^-120, and arguments around -2^46, whose f is large, one of up to 2^-55; with two of eight pairs 404 us.)
 __device__ __forceinline__ float2 ex2_poly2_bounded(float2 x)
 {
-    constexpr float kS = 7.52316384526264005e-37f;      // 2^-120
     const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));
     const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
     const float2 f = __fadd2_rn(x, make_float2(-n.x, -n.y));
-    float2 q = __ffma2_rn(make_float2(0.05517084f * kS, 0.05517084f * kS), f, make_float2(0.24260935f * kS, 0.24260935f * kS));
-    q = __ffma2_rn(q, f, make_float2(0.69326097f * kS, 0.69326097f * kS));
-    q = __ffma2_rn(q, f, make_float2(0.99992818f * kS, 0.99992818f * kS));
+    float2 q = __ffma2_rn(make_float2(0.05517084f, 0.05517084f), f, make_float2(0.24260935f, 0.24260935f));
+    q = __ffma2_rn(q, f, make_float2(0.69326097f, 0.69326097f));
+    q = __ffma2_rn(q, f, make_float2(0.99992818f, 0.99992818f));
     // bits(t) = 0x4B400000 + n for |x| < 2^22
-    const int vx = __vimin_s32_relu(__float_as_int(t.x) + (120 - 0x4B400000), 248), vy = __vimin_s32_relu(__float_as_int(t.y) + (120 - 0x4B400000), 248);
-    return make_float2(__int_as_float(__float_as_int(q.x) + (vx << 23)), __int_as_float(__float_as_int(q.y) + (vy << 23)));
+    const int vx = __vimin_s32_relu(__float_as_int(t.x) + (127 - 0x4B400000), 254), vy = __vimin_s32_relu(__float_as_int(t.y) + (127 - 0x4B400000), 254);
+    return __fmul2_rn(q, make_float2(__int_as_float(vx << 23), __int_as_float(vy << 23)));
 }
 
 constexpr int kStages = 4;            // K/V ring depth
@@ -533,7 +528,7 @@ rib_bias_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     float2 none = make_float2(0.f, 0.f);             // 0 times the sums: NaN where one has overflowed, weights of up to 2^100 times large values
 #pragma unroll
                     for (int e = 0; e < 8; ++e) none = __ffma2_rn(make_float2(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])), make_float2(0.f, 0.f), none);
-                    const bool bad = !no_query && !(l_all > 0x1p-32f && l_all < 0x1p100f && none.x + none.y == 0.f);
+                    const bool bad = !no_query && !(l_all > 0x1p-64f && l_all < 0x1p100f && none.x + none.y == 0.f);
                     if (__any_sync(0xffffffffu, bad) && lane == 0) {
                         const int slot = atomicAdd(redo_count, 1);
                         if (slot < kMaxRedo) redo_list[slot] = i;

@@ -180,3 +180,32 @@ def test_large_and_small_values_beside_large_biases(case, bias_level, v_scale):
     inputs = (q, k, v, dout, bias, named)
     back = lambda t: t.float() / v_scale  # noqa: E731  (a power of two: exact)
     compare(inputs, M, s, back(out), lse, (back(grads[0]), back(grads[1]), grads[2], back(grads[3])), 0)
+
+
+@pytest.mark.parametrize("case", SHAPES, ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("huge", [1e24, 3e38])
+@pytest.mark.parametrize("level", [0.0, -20.0])
+def test_a_key_out_of_reach_with_a_huge_value(case, huge, level):
+    """A finite value has no part in the rows that do not attend to its key; in all heads, every fifth token of the map has one."""
+    B, H, W, heads, d, M, s = case
+    named = np.full((2 * M - 1, 2 * M - 1), -1)
+    named[M - 1, M - 1], named[M - 1, M], named[M - 2, M - 1] = 0, 1, 2          # itself, the token to the right and the one above
+    q, k, v, _, bias, named = make(B, H, W, heads, d, M, named, torch.float32, seed=42)
+    bias += level
+    far = torch.arange(H)[:, None] * 2 + torch.arange(W)[None, :]
+    marked = (far % 5 == 0)
+    plain = v.clone()
+    v[:, marked] = huge
+    out, lse = binding.rib_window_attn_fwd_bucketed(*(t.cuda() for t in (q, k, v, bias, named)), M, s)
+    ref, ref_lse = orc.fwd(*(to_f64(t) for t in (q, k, plain, bias)), named.numpy(), M, s)
+    py, px = places(H, M, s), places(W, M, s)
+    at = {(int(a), int(b)): (Y, X) for Y, a in enumerate(py) for X, b in enumerate(px)}
+    clean = np.ones((H, W), dtype=bool)
+    for (a, b), (Y, X) in at.items():
+        for dy, dx in ((0, 0), (0, 1), (-1, 0)):
+            other = at.get((a + dy, b + dx))
+            if other is not None and (a + dy) // M == a // M and (b + dx) // M == b // M and marked[other]:
+                clean[Y, X] = False
+    assert 0.2 < clean.mean() < 0.9
+    close("out", out[:, torch.from_numpy(clean)], ref[:, clean])
+    close("lse", lse, ref_lse)
