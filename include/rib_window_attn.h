@@ -389,7 +389,7 @@ long long rib_kernel_launches(void);
  * from lse are off by up to a factor of exp(|lse| 2^-21) (and at most 1).
  * Infinities and NaN in a row of q or k reach out and lse of the rows that attend to it, and no others of the forward pass; those in v reach every row of the
  * window and head, with weight 0 (as in a product of matrices).  In the backward pass they may reach every gradient of the window and
- * head, and dbias.
+ * head, and dbias, as may finite numbers whose dot products pass fp32.
  *   bias     RIB_DTYPE_F32 or RIB_DTYPE_BF16, [heads][num_buckets], the heads' tables bias_head_stride (>= num_buckets) elements
  *            apart; bias_head_stride = 0: one table [num_buckets] that all heads share.  Aligned to its element type.
  *   buckets  int32 [2M-1][2M-1], 4-byte aligned.
