@@ -209,3 +209,40 @@ def test_a_key_out_of_reach_with_a_huge_value(case, huge, level):
     assert 0.2 < clean.mean() < 0.9
     close("out", out[:, torch.from_numpy(clean)], ref[:, clean])
     close("lse", lse, ref_lse)
+
+
+@pytest.mark.parametrize("case", SHAPES, ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("which", ["q", "k", "v", "dout"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("checkpointed", [False, True])
+def test_what_is_no_number_stays_in_its_window_and_head(case, which, value, checkpointed):
+    """One row of one input: the gradients of the other windows and heads are those without it (sums of fp32 atomics in another order, rounded to bf16: 1e-3 as in
+    tests/test_gpu_bucketed_calls.py), and so are the sums of the other heads' tables."""
+    B, H, W, heads, d, M, s = case
+    if which == "dout" and checkpointed:
+        pytest.skip("dout is no checkpoint")
+    q, k, v, dout, bias, named = (t.cuda() for t in make(B, H, W, heads, d, M, log_map(M), torch.float32, seed=43))
+
+    def gradients(**bad):
+        x = {**dict(q=q, k=k, v=v, dout=dout), **bad}
+        out, lse = binding.rib_window_attn_fwd_bucketed(x["q"], x["k"], x["v"], bias, named, M, s)
+        if not checkpointed:
+            return binding.rib_window_attn_bwd_bucketed(x["q"], x["k"], x["v"], bias, named, out, lse, x["dout"], M, s)
+        saved = [binding.rib_checkpoint_store(t) for t in (x["q"], x["k"], x["v"], out)]
+        return binding.rib_window_attn_bwd_bucketed_checkpointed(*saved, bias, named, lse, x["dout"], M, s)
+
+    clean = gradients()
+    py, px = places(H, M, s), places(W, M, s)
+    h, Y, X = heads - 1, int(np.where(py == 2)[0][0]), int(np.where(px == 5)[0][0])
+    bad = dict(q=q, k=k, v=v, dout=dout)[which].clone()
+    bad[0, Y, X, h, d // 2] = value
+    got = gradients(**{which: bad})
+    other = torch.ones(B, H, W, heads, dtype=torch.bool)
+    rows, cols = torch.from_numpy(py // M == 0), torch.from_numpy(px // M == 0)
+    other[0, :, :, h] = ~(rows[:, None] & cols[None, :])
+    assert other.any() or heads * B == 1
+    for a, b in zip(got[:3], clean[:3]):
+        a, b = a.float().cpu()[other], b.float().cpu()[other]
+        assert torch.isfinite(a).all() and float((a - b).norm()) <= 1e-3 * float(b.norm())
+    a, b = got[3][:h], clean[3][:h]
+    assert torch.isfinite(a).all() and float((a - b).norm()) <= 1e-5 * float(b.norm())
