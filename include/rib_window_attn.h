@@ -442,6 +442,68 @@ int rib_window_attn_bwd_bucketed_checkpointed(const rib_checkpoint* saved, const
                                               void* dq, void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Norms of queries and keys for each head and the rotation by position, in one pass over the projection's output.  For every token and head
+ *     xhat = x / sqrt(mean_c x_c^2 + eps),   z = weight o xhat,   y = R z,
+ * where R turns pairs of the first `rot` channels, channels (2i, 2i + 1) if `interleaved` and (i, i + rot / 2) if not, by the angle
+ *     (y0 + Y) f[0][i] + (x0 + X) f[1][i]
+ * of the token at row Y, column X of its map, and leaves the other channels as they are.  One axis alone (a sequence) is a map of one column.
+ *
+ * rib_rope_table takes the cosines and sines of the map's rows and columns, which a program makes once for its map (Sec. 3.1 treats Pq and Pk the same way):
+ *   frequencies : fp32 [2][pairs], pairs = rot / 2.   table : fp32 [H + W][pairs][2], overwritten; those of the rows times `magnitude`, a factor of y's rotated
+ *                 channels (1, or the temperature that scaled frequencies go with).
+ *   Angles are taken in 64 bits, so that far positions (|y0|, |x0| up to 2^40) keep their digits.
+ * rib_qk_norm_rope_fwd:
+ *   q, k        : bf16, token t of a tensor at element t * q_stride (k_stride), its heads behind one another ([heads][d], [kv_heads][d]): slices of the output of one
+ *                 projection need no copy.  Strides at least heads * d.  k may be NULL (kv_heads = 0).  Aligned to 2 bytes; the widest words that pointers,
+ *                 strides, d and rot allow are used (16 bytes: all of them multiples of 16 bytes, rot a multiple of 16; else 4, else 2).
+ *   q_weight, k_weight : fp32 [d], or [heads][d] and [kv_heads][d] with weight_per_head; NULL: that tensor is not normalised.
+ *   table       : as above; NULL with rot = 0: no rotation.
+ *   q_out, k_out: bf16 [B][H][W][heads][d], [B][H][W][kv_heads][d], overwritten.
+ * rib_qk_norm_rope_bwd: dq_out, dk_out are the gradients of q_out and k_out, in their layout; dq and dk those of q and k, with token strides of their own;
+ *   dq_weight, dk_weight those of the weights, in their layout (required where the weight is given).  Frequencies are constants.  All outputs are overwritten; sums are fp32
+ *   in a fixed order.  workspace: at least rib_qk_norm_rope_bwd_workspace(...) bytes, 256-byte aligned, as for rib_window_attn_bwd.
+ * Limits: d <= 64, rot even and at most d, B * H * W and the tokens times heads below 2^31; RIB_ERR_UNSUPPORTED beyond the first and last, RIB_ERR_SHAPE for the second.  Tables, weights and their
+ * gradients 16-byte aligned.  Inputs never alias outputs.
+ */
+int rib_rope_table(const float* frequencies, int H, int W, int pairs, long long y0, long long x0, float magnitude, float* table, void* stream);
+int rib_qk_norm_rope_fwd(const void* q, long long q_stride, const void* k, long long k_stride, const float* q_weight, const float* k_weight, int weight_per_head,
+                         const float* table, int B, int H, int W, int heads, int kv_heads, int d, int rot, int interleaved, float eps,
+                         void* q_out, void* k_out, void* stream);
+size_t rib_qk_norm_rope_bwd_workspace(int B, int H, int W, int heads, int kv_heads, int d, int weight_per_head);
+int rib_qk_norm_rope_bwd(const void* q, long long q_stride, const void* k, long long k_stride, const float* q_weight, const float* k_weight, int weight_per_head,
+                         const float* table, const void* dq_out, const void* dk_out,
+                         int B, int H, int W, int heads, int kv_heads, int d, int rot, int interleaved, float eps,
+                         void* dq, long long dq_stride, void* dk, long long dk_stride, float* dq_weight, float* dk_weight,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of a map's tokens to a sequence of states of another length (a text, an encoder's output, a learned dictionary):
+ *     S_ij = (q_i . k_j) / sqrt(d) over the states j < length,   P = SoftMax(S),   O = P V.
+ *   q, out      : bf16 [B][H][W][heads][d].
+ *   k, v        : bf16 [contexts][L][kv_heads][d]; contexts = B, or 1: all maps of the batch attend to the same states.  heads is a multiple of kv_heads, and query head
+ *                 h reads head h / (heads / kv_heads) of the states.
+ *   lengths     : int32 [contexts], device memory, the states of each context that are attended to (values outside [0, L] count as the nearer of the two); NULL: all L.
+ *                 What lies behind them is read but has no influence, whatever it holds.
+ *   lse         : fp32 [B][heads][H][W], natural log of sum_j exp(S_ij); may be NULL.
+ * A map without states (length 0) has out 0 and lse minus infinity, and passes no gradient on.  A row whose logits are all minus infinity though it has states is NaN, as
+ * SoftMax has it.
+ * Backward, given dout: dv, dk over the rows of the heads (and, with one context, the maps) that share them; dk and dv of states behind a length are 0.
+ *   out and lse are the forward results.  dq, dk, dv in the layout of q, k, v, overwritten.  All sums are fp32 in a fixed order: results are the same from run to run.
+ *   P and dS are rounded to bf16 for the products.  Probabilities recomputed from lse are held to 1.
+ * Both calls take scratch: workspace of at least rib_cross_attn_fwd_workspace / _bwd_workspace bytes (may be 0: NULL then), 256-byte aligned, as for rib_window_attn_bwd.
+ * Limits: d <= 64, heads / kv_heads <= 64, B H W heads and contexts L kv_heads below 2^31 (RIB_ERR_UNSUPPORTED), L >= 1.  d that is no multiple of 8 runs on
+ * copies in the workspace filled up with zero channels.  There is one kernel family: rib_set_path has no effect.
+ */
+size_t rib_cross_attn_fwd_workspace(int B, int H, int W, int heads, int kv_heads, int d, int L, int contexts);
+int rib_cross_attn_fwd(const void* q, const void* k, const void* v, const int* lengths,
+                       int B, int H, int W, int heads, int kv_heads, int d, int L, int contexts,
+                       void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t rib_cross_attn_bwd_workspace(int B, int H, int W, int heads, int kv_heads, int d, int L, int contexts);
+int rib_cross_attn_bwd(const void* q, const void* k, const void* v, const int* lengths, const void* out, const float* lse, const void* dout,
+                       int B, int H, int W, int heads, int kv_heads, int d, int L, int contexts,
+                       void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The tcgen05 kernels address their operands through TMA tensor maps, which depend on the base pointer and the
  * shape only; the library keeps 2048 of them (256 sets of 8, least recently asked for out first), more than both
  * passes of 64 layers need, so a call that repeats an earlier call's buffers and shape encodes none.  Writes how many maps were served from that cache (`hits`) and how many had to be encoded
@@ -467,7 +529,10 @@ enum { RIB_KERNEL_FWD_MAIN = 1, RIB_KERNEL_BWD_PREPARE = 2, RIB_KERNEL_BWD_MAIN 
     RIB_KERNEL_WINDOW16_FWD = 21, RIB_KERNEL_WINDOW16_CLEAR = 22, RIB_KERNEL_WINDOW16_BWD = 23, RIB_KERNEL_GENERATOR_CLEAR = 24,
     RIB_KERNEL_BIAS_FINISH = 25, RIB_KERNEL_CHECKPOINT_STORE = 26, RIB_KERNEL_CHECKPOINT_RESTORE = 27, RIB_KERNEL_BIAS_FWD = 28,
     RIB_KERNEL_BIAS_BWD_PREPARE = 29, RIB_KERNEL_BIAS_BWD = 30, RIB_KERNEL_BIAS_BWD_FINISH = 31,
-    RIB_KERNEL_BIAS_SMALL_FWD = 32, RIB_KERNEL_BIAS_SMALL_BWD = 33 };
+    RIB_KERNEL_BIAS_SMALL_FWD = 32, RIB_KERNEL_BIAS_SMALL_BWD = 33,
+    RIB_KERNEL_ROPE_TABLE = 34, RIB_KERNEL_QK_NORM_ROPE_FWD = 35, RIB_KERNEL_QK_NORM_ROPE_BWD = 36, RIB_KERNEL_QK_NORM_ROPE_SUM = 37,
+    RIB_KERNEL_CROSS_FWD = 38, RIB_KERNEL_CROSS_JOIN = 39, RIB_KERNEL_CROSS_BWD_PREPARE = 40, RIB_KERNEL_CROSS_BWD_DQ = 41, RIB_KERNEL_CROSS_BWD_DKV = 42,
+    RIB_KERNEL_CROSS_BWD_SUM = 43 };
 int rib_profile_begin(int max_launches);
 int rib_profile_end(int* kernel_ids, float* ms, int capacity);
 

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import warnings
 from pathlib import Path
 
@@ -61,6 +62,8 @@ EXPORTS = (
     "rib_checkpoint_store", "rib_checkpoint_restore",
     "rib_window_attn_bwd_checkpointed", "rib_window_attn_bwd_checkpointed_workspace",
     "rib_window_attn_bwd_bucketed_checkpointed", "rib_window_attn_bwd_bucketed_checkpointed_workspace",
+    "rib_rope_table", "rib_qk_norm_rope_fwd", "rib_qk_norm_rope_bwd", "rib_qk_norm_rope_bwd_workspace",
+    "rib_cross_attn_fwd", "rib_cross_attn_fwd_workspace", "rib_cross_attn_bwd", "rib_cross_attn_bwd_workspace",
 )
 KERNEL_NAMES = {1: "rib_fwd_sm100_kernel", 2: "rib_bwd_prepare_kernel", 3: "rib_bwd_sm100_kernel",
                 4: "rib_bwd_finish_kernel", 6: "generic_fwd_kernel",
@@ -71,7 +74,10 @@ KERNEL_NAMES = {1: "rib_fwd_sm100_kernel", 2: "rib_bwd_prepare_kernel", 3: "rib_
                 21: "rib_window16_fwd_kernel", 22: "rib_window16_clear_kernel", 23: "rib_window16_bwd_kernel", 24: "rib_generator_clear_kernel",
                 25: "rib_bias_scatter_kernel, rib_bias_convert_kernel", 26: "rib_checkpoint_store_kernel", 27: "rib_checkpoint_restore_kernel", 28: "rib_bias_fwd_kernel",
                 29: "rib_bias_bwd_prepare_kernel", 30: "rib_bias_bwd_kernel", 31: "rib_bias_bwd_finish_kernel",
-                32: "rib_bias_small_fwd_kernel", 33: "rib_bias_small_bwd_kernel"}
+                32: "rib_bias_small_fwd_kernel", 33: "rib_bias_small_bwd_kernel",
+                34: "rib_rope_table_kernel", 35: "rib_qk_norm_rope_kernel", 36: "rib_qk_norm_rope_kernel (backward)", 37: "rib_qk_norm_rope_sum_kernel",
+                38: "rib_cross_fwd_kernel", 39: "rib_cross_join_kernel", 40: "rib_cross_bwd_prepare_kernel", 41: "rib_cross_bwd_dq_kernel", 42: "rib_cross_bwd_dkv_kernel",
+                43: "rib_cross_bwd_sum_kernel"}
 RIB_DTYPE_F32, RIB_DTYPE_BF16 = 0, 1
 RIB_NOALLOC_SCRATCH_BYTES = 32 << 20
 
@@ -181,6 +187,22 @@ def library() -> ctypes.CDLL:
         lib.rib_window_attn_bwd_bucketed_checkpointed.argtypes = [vp, vp, ci, ll, vp, ci, vp, vp] + [ci] * 8 + [vp] * 5 + [size, vp]
         lib.rib_window_attn_bwd_bucketed_checkpointed_workspace.restype = size
         lib.rib_window_attn_bwd_bucketed_checkpointed_workspace.argtypes = [ll] + [ci] * 7
+        f32 = ctypes.c_float
+        lib.rib_rope_table.restype = ci
+        lib.rib_rope_table.argtypes = [vp, ci, ci, ci, ll, ll, f32, vp, vp]
+        lib.rib_qk_norm_rope_fwd.restype = ci
+        lib.rib_qk_norm_rope_fwd.argtypes = [vp, ll, vp, ll, vp, vp, ci, vp] + [ci] * 8 + [f32, vp, vp, vp]
+        lib.rib_qk_norm_rope_bwd_workspace.restype = size
+        lib.rib_qk_norm_rope_bwd_workspace.argtypes = [ci] * 7
+        lib.rib_qk_norm_rope_bwd.restype = ci
+        lib.rib_qk_norm_rope_bwd.argtypes = [vp, ll, vp, ll, vp, vp, ci, vp, vp, vp] + [ci] * 8 + [f32, vp, ll, vp, ll, vp, vp, vp, size, vp]
+        for name in ("rib_cross_attn_fwd_workspace", "rib_cross_attn_bwd_workspace"):
+            getattr(lib, name).restype = size
+            getattr(lib, name).argtypes = [ci] * 8
+        lib.rib_cross_attn_fwd.restype = ci
+        lib.rib_cross_attn_fwd.argtypes = [vp] * 4 + [ci] * 8 + [vp, vp, vp, size, vp]
+        lib.rib_cross_attn_bwd.restype = ci
+        lib.rib_cross_attn_bwd.argtypes = [vp] * 7 + [ci] * 8 + [vp] * 4 + [size, vp]
         lib.rib_addresses = {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS}
         _lib = lib
     return _lib
@@ -1036,3 +1058,216 @@ def rib_generate_features_bwd(w_h, b_h, w_pq, w_pk, dpq, dpk, window, stream=Non
     if rc != RIB_OK:
         raise RibError(rc)
     return outs
+
+
+def rib_rope_frequencies(rot, base=100.0, sequence=False, scaling=None, scale=1.0, trained=None, device="cuda"):
+    """Frequencies fp32 [2, rot / 2] for rib_rope_table: geometric from 1 down to 1 / base, the first half of the pairs (the larger, when their number is odd) along
+    the rows and the second along the columns; with `sequence` all along the rows.  For maps larger than those a model was trained on, by a factor `scale`:
+    `scaling` "linear" divides every frequency by it, "base" raises the base such that the lowest frequency is divided by it and the highest is kept, and
+    "by_parts" divides those that turn less than once over `trained` positions, keeps those that turn more than 32 times, and goes over linearly in between."""
+    if rot < 2 or rot % 2 or not base > 0 or not scale > 0:
+        raise ValueError(f"rot has to be even and positive, base and scale positive: got {rot}, {base}, {scale}")
+    if scaling not in (None, "linear", "base", "by_parts") or (scaling == "by_parts") != (trained is not None):
+        raise ValueError('scaling is None, "linear", "base" or "by_parts", and `trained` (positions) goes with the last')
+    pairs = rot // 2
+    counts = (pairs, 0) if sequence else ((pairs + 1) // 2, pairs // 2)
+    frequencies = torch.zeros(2, pairs, dtype=torch.float64)
+    for axis, (first, count) in enumerate(zip((0, counts[0]), counts)):
+        along = torch.arange(count, dtype=torch.float64) / max(1, count)
+        raised = base * scale ** (count / (count - 1)) if scaling == "base" and count > 1 else base
+        f = raised ** -along
+        if scaling == "linear":
+            f = f / scale
+        elif scaling == "by_parts":
+            kept = ((trained * f / (2 * math.pi) - 1) / 31).clamp(0, 1)
+            f = f * kept + f / scale * (1 - kept)
+        frequencies[axis, first:first + count] = f
+    return frequencies.float().to(device)
+
+
+def rib_rope_table(frequencies, H, W, y0=0, x0=0, magnitude=1.0, stream=None):
+    """Cosines and sines of a map's rows and columns, fp32 [H + W, rot / 2, 2], from frequencies fp32 [2, rot / 2] (per row, per column); (y0, x0) is the place of the
+    map's first token, `magnitude` a factor of the rotated channels.  A sequence of L tokens is a map of L rows and one column."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_rope_table, frequencies, H, W, y0, x0, magnitude)
+    if frequencies.dtype != torch.float32 or not frequencies.is_cuda or not frequencies.is_contiguous() or frequencies.dim() != 2 or frequencies.shape[0] != 2:
+        raise ValueError("frequencies must be a contiguous CUDA float32 tensor [2, rot / 2]")
+    pairs = frequencies.shape[1]
+    if H < 1 or W < 1 or pairs < 1:
+        raise ValueError(f"a table needs rows, columns and pairs: got H={H}, W={W}, {pairs} pairs")
+    with _on(frequencies.device):
+        table = torch.empty((H + W, pairs, 2), dtype=torch.float32, device=frequencies.device)
+        rc = library().rib_rope_table(_ptr(frequencies), H, W, pairs, y0, x0, magnitude, _ptr(table), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return table
+
+
+def _token_rows(name, t, like=None):
+    """Elements between the tokens of a bf16 tensor [B, H, W, heads, d] whose heads lie behind one another: contiguous, or a slice of heads of a contiguous one."""
+    if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 5:
+        raise ValueError(f"{name} must be a CUDA bfloat16 tensor [B,H,W,heads,d]")
+    if like is not None and tuple(t.shape) != tuple(like):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(like)}")
+    B, H, W, heads, d = t.shape
+    strides = t.stride()
+    for size, stride, want in ((d, strides[4], 1), (heads, strides[3], d)):
+        if size > 1 and stride != want:
+            raise ValueError(f"the heads of a token of {name} have to lie behind one another, got strides {strides}")
+    token, tokens = None, 1                         # strides of axes of size 1 say nothing
+    for size, stride in ((W, strides[2]), (H, strides[1]), (B, strides[0])):
+        if size > 1:
+            if token is None:
+                token = stride // tokens
+            if stride != token * tokens:
+                raise ValueError(f"the tokens of {name} have to be evenly spaced, got strides {strides}")
+        tokens *= size
+    return heads * d if token is None else token
+
+
+def _check_rope(q, k, q_weight, k_weight, table):
+    """(q_stride, k_stride, kv_heads, weights per head, rot)"""
+    q_stride = _token_rows("q", q)
+    B, H, W, heads, d = q.shape
+    k_stride, kv_heads = 0, 0
+    if k is not None:
+        k_stride = _token_rows("k", k)
+        kv_heads = k.shape[3]
+        if tuple(k.shape) != (B, H, W, kv_heads, d):
+            raise ValueError(f"k has shape {tuple(k.shape)}, expected [{B},{H},{W},kv_heads,{d}]")
+    elif k_weight is not None:
+        raise ValueError("k_weight is given without k")
+    per_head = None
+    for name, w, count in (("q_weight", q_weight, heads), ("k_weight", k_weight, kv_heads)):
+        if w is None:
+            continue
+        if w.dtype != torch.float32 or not w.is_contiguous() or w.device != q.device or tuple(w.shape) not in ((d,), (count, d)):
+            raise ValueError(f"{name} must be a contiguous float32 tensor [{d}] or [{count}, {d}] on q's device")
+        if per_head is not None and per_head != (w.dim() == 2):
+            raise ValueError("q_weight and k_weight are both per head or both shared by the heads")
+        per_head = w.dim() == 2
+    rot = 0
+    if table is not None:
+        if table.dtype != torch.float32 or not table.is_contiguous() or table.device != q.device or table.dim() != 3 or table.shape[0] != H + W or table.shape[2] != 2:
+            raise ValueError(f"table must be a contiguous float32 tensor [{H + W}, rot / 2, 2] on q's device")
+        rot = 2 * table.shape[1]
+        if rot > d:
+            raise ValueError(f"the table rotates {rot} channels of a head of {d}")
+    return q_stride, k_stride, kv_heads, int(bool(per_head)), rot
+
+
+def rib_qk_norm_rope_fwd(q, k, q_weight=None, k_weight=None, table=None, interleaved=False, eps=1e-6, stream=None):
+    """Norm of each head and rotation by position, in one pass: q bf16 [B,H,W,heads,d], k bf16 [B,H,W,kv_heads,d] or None, contiguous or slices of heads of one
+    projection's output; weights fp32 [d] or [heads, d] ([kv_heads, d]), None: not normalised; table from rib_rope_table, None: not rotated.
+    Returns (q, k), contiguous (k None if there is none)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_qk_norm_rope_fwd, q, k, q_weight, k_weight, table, interleaved, eps)
+    q_stride, k_stride, kv_heads, per_head, rot = _check_rope(q, k, q_weight, k_weight, table)
+    B, H, W, heads, d = q.shape
+    with _on(q.device, *([] if k is None else [k])):
+        q_out = torch.empty((B, H, W, heads, d), dtype=q.dtype, device=q.device)
+        k_out = None if k is None else torch.empty((B, H, W, kv_heads, d), dtype=q.dtype, device=q.device)
+        rc = library().rib_qk_norm_rope_fwd(_ptr(q), q_stride, _ptr(k), k_stride, _ptr(q_weight), _ptr(k_weight), per_head, _ptr(table), B, H, W, heads, kv_heads, d, rot,
+                                            int(interleaved), eps, _ptr(q_out), _ptr(k_out), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return q_out, k_out
+
+
+def rib_qk_norm_rope_bwd_workspace(B, H, W, heads, kv_heads, d, weight_per_head) -> int:
+    return int(library().rib_qk_norm_rope_bwd_workspace(B, H, W, heads, kv_heads, d, int(weight_per_head)))
+
+
+def rib_qk_norm_rope_bwd(q, k, q_weight, k_weight, table, dq_out, dk_out, interleaved=False, eps=1e-6, dq=None, dk=None, workspace=None, stream=None):
+    """Backward pass of rib_qk_norm_rope_fwd, given the gradients dq_out, dk_out of its results.  Returns (dq, dk, dq_weight, dk_weight), the weights' fp32 in their
+    shape (None where there is none).  dq and dk may be given: tensors, or slices of heads of the gradient of one projection's output, that are written."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_qk_norm_rope_bwd, q, k, q_weight, k_weight, table, dq_out, dk_out, interleaved, eps, dq, dk, workspace)
+    q_stride, k_stride, kv_heads, per_head, rot = _check_rope(q, k, q_weight, k_weight, table)
+    B, H, W, heads, d = q.shape
+    _check_image("dq_out", dq_out, q.shape)
+    if (k is None) != (dk_out is None) or (k is None and dk is not None):
+        raise ValueError("dk_out (and dk) go with k")
+    if k is not None:
+        _check_image("dk_out", dk_out, k.shape)
+    if workspace is None:
+        workspace = torch.empty(max(rib_qk_norm_rope_bwd_workspace(B, H, W, heads, kv_heads, d, per_head), 256), dtype=torch.uint8, device=q.device)
+    given = [t for t in (k, dq_out, dk_out, dq, dk, workspace) if t is not None]
+    with _on(q.device, *given):
+        if dq is None:
+            dq = torch.empty((B, H, W, heads, d), dtype=q.dtype, device=q.device)
+        if dk is None and k is not None:
+            dk = torch.empty((B, H, W, kv_heads, d), dtype=q.dtype, device=q.device)
+        dq_stride, dk_stride = _token_rows("dq", dq, q.shape), 0 if k is None else _token_rows("dk", dk, k.shape)
+        dq_weight, dk_weight = (None if w is None else torch.empty_like(w) for w in (q_weight, k_weight))
+        rc = library().rib_qk_norm_rope_bwd(_ptr(q), q_stride, _ptr(k), k_stride, _ptr(q_weight), _ptr(k_weight), per_head, _ptr(table), _ptr(dq_out), _ptr(dk_out),
+                                            B, H, W, heads, kv_heads, d, rot, int(interleaved), eps, _ptr(dq), dq_stride, _ptr(dk), dk_stride, _ptr(dq_weight),
+                                            _ptr(dk_weight), _ptr(workspace), workspace.numel(), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return dq, dk, dq_weight, dk_weight
+
+
+def _check_states(q, k, v, lengths):
+    """(kv_heads, L, contexts)"""
+    _check_image("q", q)
+    B, _, _, heads, d = q.shape
+    for name, t in (("k", k), ("v", v)):
+        if t.dtype != torch.bfloat16 or not t.is_cuda or not t.is_contiguous() or t.dim() != 4:
+            raise ValueError(f"{name} must be a contiguous CUDA bfloat16 tensor [contexts,L,kv_heads,d]")
+        if t.shape[0] not in (1, B) or t.shape[3] != d or t.shape != k.shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{B} or 1,L,kv_heads,{d}], k and v alike")
+    contexts, L, kv_heads, _ = k.shape
+    if kv_heads < 1 or heads % kv_heads:
+        raise ValueError(f"{heads} query heads do not divide among {kv_heads} heads of states")
+    if lengths is not None and (lengths.dtype != torch.int32 or not lengths.is_contiguous() or lengths.device != q.device or tuple(lengths.shape) != (contexts,)):
+        raise ValueError(f"lengths must be a contiguous int32 tensor [{contexts}] on q's device")
+    return kv_heads, L, contexts
+
+
+def rib_cross_attn_fwd_workspace(B, H, W, heads, kv_heads, d, L, contexts) -> int:
+    return int(library().rib_cross_attn_fwd_workspace(B, H, W, heads, kv_heads, d, L, contexts))
+
+
+def rib_cross_attn_fwd(q, k, v, lengths=None, workspace=None, stream=None, want_lse=True):
+    """Attention of a map's tokens q bf16 [B,H,W,heads,d] to states k, v bf16 [B,L,kv_heads,d] ([1,L,kv_heads,d]: the same for all maps); lengths int32 [B] (or [1]):
+    the states of each context that are attended to.  Returns (out, lse)."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_cross_attn_fwd, q, k, v, lengths, workspace, None, want_lse)
+    kv_heads, L, contexts = _check_states(q, k, v, lengths)
+    B, H, W, heads, d = q.shape
+    need = rib_cross_attn_fwd_workspace(B, H, W, heads, kv_heads, d, L, contexts)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    with _on(q.device, k, v, *([] if workspace is None else [workspace])):
+        out = torch.empty_like(q)
+        lse = torch.empty((B, heads, H, W), dtype=torch.float32, device=q.device) if want_lse else None
+        rc = library().rib_cross_attn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(lengths), B, H, W, heads, kv_heads, d, L, contexts, _ptr(out), _ptr(lse),
+                                          _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return out, lse
+
+
+def rib_cross_attn_bwd_workspace(B, H, W, heads, kv_heads, d, L, contexts) -> int:
+    return int(library().rib_cross_attn_bwd_workspace(B, H, W, heads, kv_heads, d, L, contexts))
+
+
+def rib_cross_attn_bwd(q, k, v, out, lse, dout, lengths=None, workspace=None, stream=None):
+    """Backward pass of rib_cross_attn_fwd.  Returns (dq, dk, dv), bf16 in the shapes of q, k, v."""
+    if stream is not None and _elsewhere(stream):
+        return _beside(stream, rib_cross_attn_bwd, q, k, v, out, lse, dout, lengths, workspace)
+    kv_heads, L, contexts = _check_states(q, k, v, lengths)
+    B, H, W, heads, d = q.shape
+    for name, t in (("out", out), ("dout", dout)):
+        _check_image(name, t, q.shape)
+    _check_lse(lse, B, heads, H, W, q.device)
+    if workspace is None:
+        workspace = torch.empty(max(rib_cross_attn_bwd_workspace(B, H, W, heads, kv_heads, d, L, contexts), 256), dtype=torch.uint8, device=q.device)
+    with _on(q.device, k, v, out, dout, workspace):
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        rc = library().rib_cross_attn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(lengths), _ptr(out), _ptr(lse), _ptr(dout), B, H, W, heads, kv_heads, d, L, contexts,
+                                          _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace), workspace.numel(), _stream_ptr(stream))
+    if rc != RIB_OK:
+        raise RibError(rc)
+    return dq, dk, dv

@@ -2,6 +2,7 @@
 // The contract of every entry point is stated in include/rib_window_attn.h.
 #include "../../include/rib_window_attn.h"
 #include "rib_common.cuh"
+#include "rib_cross.cuh"
 
 #include <atomic>
 #include <mutex>
@@ -853,6 +854,186 @@ int rib_generate_features_bwd(const float* w_h, const float* b_h, const float* w
                                              static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return RIB_ERR_CUDA;
     g_kernel_launches += 2;          // clearing of the gradients, main kernel
+    return RIB_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// below 2^31: B H W, and that times heads
+int check_tokens(int B, int H, int W, int heads)
+{
+    const __int128 tokens = (__int128)B * H * W;
+    return tokens > 0x7fffffffLL || tokens * heads > 0x7fffffffLL ? RIB_ERR_UNSUPPORTED : RIB_OK;
+}
+
+bool element_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 1u) == 0; }
+
+struct RopeCall { const void *q, *k; long long q_stride, k_stride; const float *q_weight, *k_weight; int per_head; const float* table; int B, H, W, heads, kv_heads, d, rot, interleaved; float eps; };
+
+int check_rope_shape(int B, int H, int W, int heads, int kv_heads, int d)
+{
+    if (B <= 0 || H <= 0 || W <= 0 || heads <= 0 || kv_heads < 0 || d <= 0) return RIB_ERR_SHAPE;
+    if (d > 64 || heads > 65535 || kv_heads > 65535 - heads) return RIB_ERR_UNSUPPORTED;      // (a head to a row of the grid with weights per head)
+    return check_tokens(B, H, W, heads > kv_heads ? heads : kv_heads);
+}
+
+int rope_problem(const RopeCall& c, rib::RopeProblem* p)
+{
+    if (!c.q || (c.k == nullptr) != (c.kv_heads == 0)) return RIB_ERR_NULL;
+    if ((!c.table) != (c.rot == 0) || (c.kv_heads == 0 && c.k_weight)) return RIB_ERR_NULL;
+    if (int rc = check_rope_shape(c.B, c.H, c.W, c.heads, c.kv_heads, c.d)) return rc;
+    if (c.rot < 0 || c.rot > c.d || c.rot % 2 || !(c.eps >= 0.f)) return RIB_ERR_SHAPE;
+    if (c.q_stride < (long long)c.heads * c.d || (c.kv_heads && c.k_stride < (long long)c.kv_heads * c.d)) return RIB_ERR_SHAPE;
+    if (c.q_stride > (1ll << 31) || c.k_stride > (1ll << 31)) return RIB_ERR_UNSUPPORTED;
+    if (!element_aligned(c.q) || !element_aligned(c.k) || !aligned16(c.q_weight) || !aligned16(c.k_weight) || !aligned16(c.table)) return RIB_ERR_ALIGN;
+    *p = rib::RopeProblem{};
+    p->t[0].x = static_cast<const __nv_bfloat16*>(c.q); p->t[0].x_stride = c.q_stride; p->t[0].w = c.q_weight;
+    p->t[1].x = static_cast<const __nv_bfloat16*>(c.k); p->t[1].x_stride = c.kv_heads ? c.k_stride : 0; p->t[1].w = c.k_weight;
+    p->table = c.table; p->tokens = (long long)c.B * c.H * c.W; p->H = c.H; p->W = c.W; p->heads = c.heads; p->kv_heads = c.kv_heads; p->d = c.d; p->rot = c.rot;
+    p->interleaved = c.interleaved != 0; p->per_head = c.per_head != 0; p->eps = c.eps;
+    return RIB_OK;
+}
+
+int cross_problem(int B, int H, int W, int heads, int kv_heads, int d, int L, int contexts, rib::CrossProblem* p)
+{
+    if (B <= 0 || H <= 0 || W <= 0 || heads <= 0 || kv_heads <= 0 || d <= 0 || L <= 0) return RIB_ERR_SHAPE;
+    if (heads % kv_heads || (contexts != B && contexts != 1)) return RIB_ERR_SHAPE;
+    if (d > 64 || heads / kv_heads > 64) return RIB_ERR_UNSUPPORTED;
+    if (int rc = check_tokens(B, H, W, heads)) return rc;
+    const __int128 states = (__int128)contexts * L * kv_heads;
+    if (states > 0x7fffffffLL || L > 0x7fffff00) return RIB_ERR_UNSUPPORTED;
+    *p = rib::CrossProblem{};
+    p->B = B; p->heads = heads; p->kv_heads = kv_heads; p->d = d; p->L = L; p->contexts = contexts;
+    p->pixels = (long long)H * W; p->tokens = contexts == B ? p->pixels : B * p->pixels;
+    // items, tiles and CTAs are counted in ints
+    const rib::CrossPlan plan = rib::cross_plan(*p);
+    if ((__int128)plan.groups * plan.tiles * plan.splits > 0x7fffffffLL || (__int128)plan.groups * plan.key_tiles * plan.row_splits > 0x7fffffffLL) return RIB_ERR_UNSUPPORTED;
+    return RIB_OK;
+}
+
+int check_cross_workspace(const void* workspace, size_t bytes, size_t need)
+{
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return RIB_ERR_ALIGN;
+    return need && (!workspace || bytes < need) ? RIB_ERR_WORKSPACE : RIB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rib_rope_table(const float* frequencies, int H, int W, int pairs, long long y0, long long x0, float magnitude, float* table, void* stream)
+{
+    if (!frequencies || !table) return RIB_ERR_NULL;
+    if (H <= 0 || W <= 0 || pairs <= 0) return RIB_ERR_SHAPE;
+    const long long far = 1ll << 40;
+    if (pairs > 32 || y0 < -far || y0 > far || x0 < -far || x0 > far) return RIB_ERR_UNSUPPORTED;
+    if (!aligned16(frequencies) || !aligned16(table)) return RIB_ERR_ALIGN;
+    if (rib::rope_table(frequencies, H, W, pairs, y0, x0, magnitude, table, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RIB_ERR_CUDA;
+    g_kernel_launches += 1;
+    return RIB_OK;
+}
+
+int rib_qk_norm_rope_fwd(const void* q, long long q_stride, const void* k, long long k_stride, const float* q_weight, const float* k_weight, int weight_per_head,
+                         const float* table, int B, int H, int W, int heads, int kv_heads, int d, int rot, int interleaved, float eps,
+                         void* q_out, void* k_out, void* stream)
+{
+    rib::RopeProblem p;
+    if (!q_out || (k_out == nullptr) != (kv_heads == 0)) return RIB_ERR_NULL;
+    if (int rc = rope_problem(RopeCall{q, k, q_stride, k_stride, q_weight, k_weight, weight_per_head, table, B, H, W, heads, kv_heads, d, rot, interleaved, eps}, &p)) return rc;
+    if (!aligned16(q_out) || !aligned16(k_out)) return RIB_ERR_ALIGN;
+    p.t[0].y = static_cast<__nv_bfloat16*>(q_out); p.t[0].y_stride = (long long)heads * d;
+    p.t[1].y = static_cast<__nv_bfloat16*>(k_out); p.t[1].y_stride = (long long)kv_heads * d;
+    if (rib::qk_norm_rope_fwd(p, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RIB_ERR_CUDA;
+    g_kernel_launches += 1;
+    return RIB_OK;
+}
+
+size_t rib_qk_norm_rope_bwd_workspace(int B, int H, int W, int heads, int kv_heads, int d, int weight_per_head)
+{
+    if (check_rope_shape(B, H, W, heads, kv_heads, d)) return 0;
+    rib::RopeProblem p{};
+    p.tokens = (long long)B * H * W; p.heads = heads; p.kv_heads = kv_heads; p.d = d; p.per_head = weight_per_head != 0;
+    return rib::qk_norm_rope_bwd_workspace(p);
+}
+
+int rib_qk_norm_rope_bwd(const void* q, long long q_stride, const void* k, long long k_stride, const float* q_weight, const float* k_weight, int weight_per_head,
+                         const float* table, const void* dq_out, const void* dk_out,
+                         int B, int H, int W, int heads, int kv_heads, int d, int rot, int interleaved, float eps,
+                         void* dq, long long dq_stride, void* dk, long long dk_stride, float* dq_weight, float* dk_weight,
+                         void* workspace, size_t workspace_bytes, void* stream)
+{
+    rib::RopeProblem p;
+    if (!dq_out || !dq || (dk_out == nullptr) != (kv_heads == 0) || (dk == nullptr) != (kv_heads == 0)) return RIB_ERR_NULL;
+    if ((q_weight && !dq_weight) || (k_weight && !dk_weight)) return RIB_ERR_NULL;
+    if (int rc = rope_problem(RopeCall{q, k, q_stride, k_stride, q_weight, k_weight, weight_per_head, table, B, H, W, heads, kv_heads, d, rot, interleaved, eps}, &p)) return rc;
+    if (dq_stride < (long long)heads * d || (kv_heads && dk_stride < (long long)kv_heads * d)) return RIB_ERR_SHAPE;
+    if (dq_stride > (1ll << 31) || dk_stride > (1ll << 31)) return RIB_ERR_UNSUPPORTED;
+    if (!aligned16(dq_out) || !aligned16(dk_out) || !element_aligned(dq) || !element_aligned(dk) || !aligned16(dq_weight) || !aligned16(dk_weight)) return RIB_ERR_ALIGN;
+    if (int rc = check_cross_workspace(workspace, workspace_bytes, rib::qk_norm_rope_bwd_workspace(p))) return rc;
+    p.t[0].g = static_cast<const __nv_bfloat16*>(dq_out); p.t[0].y = static_cast<__nv_bfloat16*>(dq); p.t[0].y_stride = dq_stride; p.t[0].dw = q_weight ? dq_weight : nullptr;
+    p.t[1].g = static_cast<const __nv_bfloat16*>(dk_out); p.t[1].y = static_cast<__nv_bfloat16*>(dk); p.t[1].y_stride = kv_heads ? dk_stride : 0; p.t[1].dw = k_weight ? dk_weight : nullptr;
+    int launches = 0;
+    if (rib::qk_norm_rope_bwd(p, static_cast<float*>(workspace), &launches, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RIB_ERR_CUDA;
+    g_kernel_launches += launches;
+    return RIB_OK;
+}
+
+size_t rib_cross_attn_fwd_workspace(int B, int H, int W, int heads, int kv_heads, int d, int L, int contexts)
+{
+    rib::CrossProblem p;
+    return cross_problem(B, H, W, heads, kv_heads, d, L, contexts, &p) == RIB_OK ? rib::cross_fwd_workspace(p) : 0;
+}
+
+int rib_cross_attn_fwd(const void* q, const void* k, const void* v, const int* lengths,
+                       int B, int H, int W, int heads, int kv_heads, int d, int L, int contexts,
+                       void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!q || !k || !v || !out) return RIB_ERR_NULL;
+    rib::CrossProblem p;
+    if (int rc = cross_problem(B, H, W, heads, kv_heads, d, L, contexts, &p)) return rc;
+    const void* ptrs[] = {q, k, v, out, lse};
+    for (const void* ptr : ptrs)
+        if (!aligned16(ptr)) return RIB_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(lengths) & 3u) return RIB_ERR_ALIGN;
+    if (int rc = check_cross_workspace(workspace, workspace_bytes, rib::cross_fwd_workspace(p))) return rc;
+    if (int rc = device_status_ptr(&p.status)) return rc;
+    p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k); p.v = static_cast<const __nv_bfloat16*>(v); p.lengths = lengths;
+    p.out_w = static_cast<__nv_bfloat16*>(out); p.lse_w = lse; p.workspace = workspace;
+    int launches = 0;
+    if (rib::cross_fwd(p, static_cast<cudaStream_t>(stream), &launches) != cudaSuccess) return RIB_ERR_CUDA;
+    t_last_path = RIB_PATH_SM100;
+    g_kernel_launches += launches;
+    return RIB_OK;
+}
+
+size_t rib_cross_attn_bwd_workspace(int B, int H, int W, int heads, int kv_heads, int d, int L, int contexts)
+{
+    rib::CrossProblem p;
+    return cross_problem(B, H, W, heads, kv_heads, d, L, contexts, &p) == RIB_OK ? rib::cross_bwd_workspace(p) : 0;
+}
+
+int rib_cross_attn_bwd(const void* q, const void* k, const void* v, const int* lengths, const void* out, const float* lse, const void* dout,
+                       int B, int H, int W, int heads, int kv_heads, int d, int L, int contexts,
+                       void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!q || !k || !v || !out || !lse || !dout || !dq || !dk || !dv) return RIB_ERR_NULL;
+    rib::CrossProblem p;
+    if (int rc = cross_problem(B, H, W, heads, kv_heads, d, L, contexts, &p)) return rc;
+    const void* ptrs[] = {q, k, v, out, lse, dout, dq, dk, dv};
+    for (const void* ptr : ptrs)
+        if (!aligned16(ptr)) return RIB_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(lengths) & 3u) return RIB_ERR_ALIGN;
+    if (int rc = check_cross_workspace(workspace, workspace_bytes, rib::cross_bwd_workspace(p))) return rc;
+    if (int rc = device_status_ptr(&p.status)) return rc;
+    p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k); p.v = static_cast<const __nv_bfloat16*>(v); p.lengths = lengths;
+    p.out = static_cast<const __nv_bfloat16*>(out); p.lse_in = lse; p.dout = static_cast<const __nv_bfloat16*>(dout);
+    p.dq = static_cast<__nv_bfloat16*>(dq); p.dk = static_cast<__nv_bfloat16*>(dk); p.dv = static_cast<__nv_bfloat16*>(dv); p.workspace = workspace;
+    int launches = 0;
+    if (rib::cross_bwd(p, static_cast<cudaStream_t>(stream), &launches) != cudaSuccess) return RIB_ERR_CUDA;
+    t_last_path = RIB_PATH_SM100;
+    g_kernel_launches += launches;
     return RIB_OK;
 }
 

@@ -247,6 +247,14 @@ cudaError_t generator_fwd(const float* w_h, const float* b_h, const float* w_pq,
 cudaError_t generator_bwd(const float* w_h, const float* b_h, const float* w_pq, const float* w_pk, const float* dpq, const float* dpk,
                           int window, int L, int dh, int r, float* dw_h, float* db_h, float* dw_pq, float* dw_pk, cudaStream_t stream);
 
+// Norms of queries and keys for each head and the rotation by position (rib_rope.cu).
+struct RopeRows { const __nv_bfloat16 *x, *g; __nv_bfloat16* y; long long x_stride, y_stride; const float* w; float* dw; };      // y: result, or gradient of x; strides of tokens; w null: no norm
+struct RopeProblem { RopeRows t[2]; const float* table; long long tokens; int H, W, heads, kv_heads, d, rot, interleaved, per_head; float eps; };      // q, k (kv_heads = 0: no k)
+cudaError_t rope_table(const float* frequencies, int H, int W, int pairs, long long y0, long long x0, float magnitude, float* table, cudaStream_t stream);
+cudaError_t qk_norm_rope_fwd(const RopeProblem& p, cudaStream_t stream);
+size_t qk_norm_rope_bwd_workspace(const RopeProblem& p);
+cudaError_t qk_norm_rope_bwd(const RopeProblem& p, float* workspace, int* launches, cudaStream_t stream);
+
 // Hits and misses of the host-side tensor-map cache (rib_fwd_sm100.cu).
 void tensor_map_cache_counts(long long* hits, long long* misses);
 

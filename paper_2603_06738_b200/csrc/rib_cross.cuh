@@ -1,0 +1,108 @@
+// Attention of a map's tokens to a sequence of states of another length: what the forward and the backward kernels share.
+//
+//     S = q k^T / sqrt(d) over the keys j < length,   out = SoftMax(S) v,   lse = log sum exp S
+//
+// q [B][H][W][heads][d]; k, v [contexts][L][kv_heads][d], contexts = B, or 1 when the maps of the batch share one sequence: the batch is then one map of B H W
+// tokens, which is the same memory.  heads / kv_heads = G query heads share a head of keys and values; the rows of a (context, kv head) group are its
+// tokens times its G heads, token by token, and that is one TMA box {d, G heads, 128 / G tokens} per tile of up to 128 rows.
+#pragma once
+#include "rib_sm100_common.cuh"
+
+namespace rib {
+
+struct CrossProblem {
+    const __nv_bfloat16 *q, *k, *v;       // rows of `width` channels
+    const __nv_bfloat16 *out, *dout;      // backward; rows of d channels (out) and `width` channels (dout)
+    const float* lse_in;                  // backward
+    const int* lengths;                   // [contexts], or null: L
+    __nv_bfloat16 *out_w, *dq, *dk, *dv;  // rows of d channels
+    float* lse_w;                         // may be null
+    int B, heads, kv_heads, d, L, contexts;
+    int width;                            // channels of a row in q, k, v and dout: d, or d rounded up to a multiple of 8 on padded copies
+    long long pixels, tokens;             // H W; tokens per context (pixels, or B pixels when the context is shared)
+    int* status;
+    void* workspace;
+};
+
+// sizes of the launches, from the shape alone
+struct CrossPlan {
+    int G, rows_per_tile, tokens_per_tile, tiles, groups, blocks;      // groups: contexts x kv_heads; blocks: of 64 keys
+    long long rows;                                                    // of a group: tokens x G
+    int splits, blocks_per_split;                                      // out, dQ: runs of key blocks that are computed apart and joined
+    int key_tiles, row_splits, row_tiles_per_split;                    // dK and dV: tiles of 128 keys, runs of tiles of 64 rows
+    int row_tiles, kv_rows_per_tile, kv_tokens_per_tile;
+};
+
+constexpr int kCrossSms = 148;            // the same number everywhere, so that a call's shape decides the launch
+constexpr int kCrossBlock = 64;           // keys of a block
+
+CrossPlan cross_plan(const CrossProblem& p);
+bool cross_padded(const CrossProblem& p);                                       // rows that TMA cannot address: copies filled up with zero channels
+size_t cross_fwd_workspace(const CrossProblem& p);
+size_t cross_bwd_workspace(const CrossProblem& p);
+cudaError_t cross_fwd(CrossProblem p, cudaStream_t stream, int* launches);
+cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches);
+
+// Fills up rows of d channels with zeros to rows of `width`, up to four tensors in one launch (rib_cross_fwd_sm100.cu).
+struct CrossPad { const __nv_bfloat16* src[4]; __nv_bfloat16* dst[4]; long long rows[4]; int tensors, d, width; };
+cudaError_t cross_pad(const CrossPad& args, cudaStream_t stream);
+
+namespace sm100 {
+
+inline size_t cross_align(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+// bf16 [contexts][tokens][heads][width], box = `tokens_in_box` tokens of `heads_in_box` heads, DP channels wide (zeros beyond the width)
+inline bool cross_rows_map(CUtensorMap* map, const void* ptr, long long contexts, long long tokens, int heads, int width, int dp, int heads_in_box, int tokens_in_box)
+{
+    const MapKey key{ptr, contexts, tokens, 6, heads, width, dp, heads_in_box, tokens_in_box};
+    return cached_map(map, key, [&](CUtensorMap* m) {
+        const cuuint64_t row = (cuuint64_t)width * 2;
+        const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)contexts};
+        const cuuint64_t strides[3] = {row, row * heads, row * heads * (cuuint64_t)tokens};
+        const cuuint32_t box[4] = {(cuuint32_t)dp, (cuuint32_t)heads_in_box, (cuuint32_t)tokens_in_box, 1};
+        const cuuint32_t estr[4] = {1, 1, 1, 1};
+        return encode_fn()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           dp == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    });
+}
+
+// Tiles of rows of DP = 32 or 64 channels in shared memory: 64-byte rows under SWIZZLE_64B, 128-byte rows under SWIZZLE_128B; eight rows are
+// an atom.  The same descriptor serves a K-major operand (a K16 step is 32 bytes on) and an MN-major one whose contraction runs over the rows (16 rows on).
+template <int DP> struct CrossTile {
+    static constexpr uint32_t kRow = DP * 2;
+    static constexpr uint64_t kDesc = smem_desc_const(16, 8 * kRow, DP == 32 ? kSwizzle64B : kSwizzle128B);
+    static constexpr uint32_t kStepK = 2, kStepRows = kRow;            // in units of 16 bytes: 32 bytes; 16 rows
+};
+
+// scores of one lowest finite reference: a row whose keys all give minus infinity (infinite inputs) has weights 0 and 0 / 0 as its result
+constexpr float kCrossLowest = -1.8e38f;
+
+// `count` (a multiple of 8) fp32 values as bf16 to dst, of a row of d channels beginning at channel c0; `vector`: rows are whole 16-byte words
+template <int count>
+__device__ __forceinline__ void cross_store_row(__nv_bfloat16* row, int c0, int d, const float (&x)[count], bool vector)
+{
+    if (vector) {
+#pragma unroll
+        for (int g = 0; g < count / 8; ++g)
+            if (c0 + 8 * g < d)
+                *reinterpret_cast<uint4*>(row + c0 + 8 * g) = make_uint4(pack_bf16x2(x[8 * g], x[8 * g + 1]), pack_bf16x2(x[8 * g + 2], x[8 * g + 3]),
+                                                                         pack_bf16x2(x[8 * g + 4], x[8 * g + 5]), pack_bf16x2(x[8 * g + 6], x[8 * g + 7]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < count; ++e)
+            if (c0 + e < d) row[c0 + e] = __float2bfloat16_rn(x[e]);
+    }
+}
+
+// Rows of a tile that no token fills are zero for good, since the boxes end before them; a tile of shared memory that a role
+// writes by hand is handed over to the asynchronous copies and products by the fence.
+__device__ __forceinline__ void cross_zero_rows(uint8_t* tile, uint32_t row_bytes, int first, int last, int thread, int threads)
+{
+    uint4* at = reinterpret_cast<uint4*>(tile + (size_t)first * row_bytes);
+    const int words = (last - first) * (int)(row_bytes / 16);
+    for (int i = thread; i < words; i += threads) at[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+}  // namespace sm100
+}  // namespace rib

@@ -1,0 +1,701 @@
+// Backward pass of the attention to states (rib_cross.cuh) for B200 (sm_100a), two kernels over tcgen05 products:
+//     P = exp(S - lse),   dS = P o (dO V^T - D),   D = rowsum(dO o O)
+//     dQ = dS K / sqrt(d)                      rows on the lanes, a CTA per tile of rows, walking the keys
+//     dV = P^T dO,  dK = dS^T Q / sqrt(d)      keys on the lanes, a CTA per tile of 128 keys, walking the rows
+// Each computes P for itself: an exponential more per score than one kernel for all three would take, and no sum of dQ over key tiles in memory, so that
+// every sum has one order and the results are the same from run to run.  Where there are too few tiles to fill the card, keys (dQ) or rows (dK, dV) are dealt
+// out to several CTAs, whose fp32 sums a last kernel adds.  A first kernel takes D and brings lse and D into the order in which tiles of rows read them.
+// P and dS enter the products as bf16 (a rounding of 2^-9 of each, as everywhere in this library); sums are fp32.
+#include "rib_cross.cuh"
+
+namespace rib {
+namespace {
+
+using namespace sm100;
+
+constexpr int kRows = 128, kKvRows = 64;             // rows of a tile: dQ; dK and dV
+constexpr float kLog2e = 1.4426950408889634f;
+
+// (-lse log2 e, -D) of the rows of a group, in tiles of kKvRows entries of which kv_rows_per_tile are used: entries that are no row have (-infinity, 0), a weight of 0
+struct RowStats { float2* at; int tokens_per_tile, tiles, G; FastDiv by_tokens; };
+__device__ __forceinline__ long long stats_index(const RowStats& s, long long group, long long token, int head)
+{
+    int tile, t;
+    s.by_tokens.divmod((int)token, tile, t);
+    return (group * s.tiles + tile) * kKvRows + t * s.G + head;
+}
+
+// ------------------------------------------------------------------------------------------------ D, lse
+struct PrepareParams {
+    const __nv_bfloat16 *out, *dout;
+    const float* lse;
+    RowStats stats;
+    long long rows, entries, tokens, pixels;         // rows: tokens of all contexts x heads; entries: of the statistics
+    int d, heads, kv_heads, G, lanes, row_blocks;
+    FastDiv by_heads, by_group, by_pixels, by_tokens_of_context;
+    int vector;
+};
+__global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const PrepareParams p)
+{
+    if ((int)blockIdx.x >= p.row_blocks) {            // entries that are no row
+        const long long e = (long long)(blockIdx.x - p.row_blocks) * 256 + threadIdx.x;
+        if (e >= p.entries) return;
+        const int within = (int)(e % kKvRows), tile = (int)(e / kKvRows % p.stats.tiles);
+        if (within >= p.stats.tokens_per_tile * p.G || (long long)tile * p.stats.tokens_per_tile + within / p.G >= p.tokens) p.stats.at[e] = make_float2(-INFINITY, 0.f);
+        return;
+    }
+    // rows in the order of memory, `lanes` lanes (a power of two) to a row
+    const long long thread = (long long)blockIdx.x * 256 + threadIdx.x, row = thread / p.lanes;
+    const int part = (int)(thread & (p.lanes - 1));
+    float sum = 0.f;
+    if (row < p.rows) {
+        const __nv_bfloat16 *o = p.out + row * p.d, *g = p.dout + row * p.d;
+        if (p.vector) {
+            if (8 * part < p.d) {
+                const uint4 a = __ldg(reinterpret_cast<const uint4*>(o) + part), b = __ldg(reinterpret_cast<const uint4*>(g) + part);
+                const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sum = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum);
+                    sum = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), sum);
+                }
+            }
+        } else {
+            for (int c = part; c < p.d; c += p.lanes) sum = fmaf(__bfloat162float(o[c]), __bfloat162float(g[c]), sum);
+        }
+    }
+    for (int o = p.lanes / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (row >= p.rows || part != 0) return;
+    int token_of_all, head, image, pixel, context, token, kv, g;
+    const long long wide = row / p.heads;             // (rows may pass 2^31)
+    token_of_all = (int)wide; head = (int)(row - wide * p.heads);
+    p.by_pixels.divmod(token_of_all, image, pixel);
+    p.by_tokens_of_context.divmod(token_of_all, context, token);
+    p.by_group.divmod(head, kv, g);
+    const float lse = p.lse[((long long)image * p.heads + head) * p.pixels + pixel];
+    p.stats.at[stats_index(p.stats, (long long)context * p.kv_heads + kv, token, g)] = make_float2(-lse * kLog2e, -sum);
+}
+
+// -------------------------------------------------------------------------------------------------- dQ
+constexpr int kDqThreads = 160;
+constexpr uint32_t kDqTmemCols = 128, kDqColAcc = 64;
+
+template <int DP> struct DqCfg {
+    static constexpr int kStages = 2, kTiles = DP == 32 ? 2 : 1, kBlocksPerSm = DP == 32 ? 4 : 3;
+    static constexpr uint32_t kRow = DP * 2, kQBytes = kRows * kRow, kKBytes = kCrossBlock * kRow;
+    static constexpr uint32_t kOffQ = 0, kOffDO = kTiles * kQBytes, kOffK = 2 * kTiles * kQBytes, kOffV = kOffK + kStages * kKBytes, kOffBar = kOffV + kStages * kKBytes;
+    // barriers: query tiles, key blocks, scores there, scores read, dP there, dS there, dS K done, all products done
+    static constexpr int kQFull = 0, kKFull = kTiles, kSFull = kKFull + kStages, kSRead = kSFull + 1, kDPFull = kSFull + 2, kDSReady = kSFull + 3, kDQDone = kSFull + 4,
+                         kDrain = kSFull + 5, kBars = kSFull + 6;
+    static constexpr uint32_t kOffMisc = kOffBar + kBars * 8, kSmem = kOffMisc + 16 + 1024;
+    static_assert(kBlocksPerSm * (kSmem + 1024) <= 233472, "shared memory of an SM");
+};
+
+struct DqParams {
+    const int* lengths;
+    __nv_bfloat16* dq;
+    float* part;                         // splits > 1: [splits][groups][rows][DP]
+    int* status;
+    RowStats stats;
+    int d, L, heads, kv_heads, G, rows_per_tile, tokens_per_tile, blocks_per_split, splits, items, vector;
+    long long tokens, rows, groups;
+    float scale_log2, inv_sqrt_d;
+    FastDiv by_tiles, by_splits, by_kv, by_group;
+};
+
+struct DqItem { int tile, split, group, context, kv, first, blocks, length; };
+__device__ __forceinline__ DqItem decode(const DqParams& p, int item)
+{
+    DqItem c;
+    p.by_tiles.divmod(item, item, c.tile);
+    p.by_splits.divmod(item, c.group, c.split);
+    p.by_kv.divmod(c.group, c.context, c.kv);
+    c.length = p.lengths ? min(max(__ldg(p.lengths + c.context), 0), p.L) : p.L;
+    c.first = c.split * p.blocks_per_split;
+    c.blocks = max(0, min(c.first + p.blocks_per_split, (c.length + kCrossBlock - 1) / kCrossBlock) - c.first);
+    return c;
+}
+
+// Tensor memory: 64 columns for the scores, which dP takes over once the scores are in registers and dS once dP is; dQ behind them.  As in the forward pass several
+// CTAs to an SM overlap what runs one after the other inside each.
+template <int DP>
+__global__ void __launch_bounds__(kDqThreads, DqCfg<DP>::kBlocksPerSm)
+rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                        const __grid_constant__ DqParams p)
+{
+    using C = DqCfg<DP>;
+    using T = CrossTile<DP>;
+    constexpr int kStages = C::kStages, kTiles = C::kTiles;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + C::kOffMisc);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kOffMisc + 4);      // [1] stays 0: used by the drain waits
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        abort_flag[0] = 0; abort_flag[1] = 0;
+        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i == C::kSRead || i == C::kDSReady ? 4 : 1);
+        fence_barrier_init();
+        prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_do); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
+    }
+    if (warp == 4) {
+        tmem_alloc(base + C::kOffMisc, kDqTmemCols);
+        tmem_relinquish();
+    }
+    for (int i = 0; i < 2 * kTiles; ++i) cross_zero_rows(base_ptr + i * C::kQBytes, C::kRow, p.rows_per_tile, kRows, threadIdx.x, kDqThreads);
+    fence_proxy_async();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    bool ok = true;
+
+    if (warp == 4) {
+        // ============================================ loads and products
+        uint32_t step = 0, live = 0, loaded = 0, q_loaded = 0;
+        int next = blockIdx.x, next_block = 0;
+        auto load_ahead = [&]() {
+            while (next < p.items) {
+                const DqItem c = decode(p, next);
+                if (c.blocks) {
+                    if (next_block == 0 && q_loaded == live + kTiles) return;
+                    if (loaded == step + kStages) return;
+                    if (elect_one()) {
+                        if (next_block == 0) {
+                            const uint32_t buf = q_loaded % kTiles;
+                            mbar_arrive_expect_tx(bar(C::kQFull + buf), 2u * (uint32_t)p.rows_per_tile * C::kRow);
+                            tma_load_4d(base + C::kOffQ + buf * C::kQBytes, &tm_q, bar(C::kQFull + buf), 0, c.kv * p.G, c.tile * p.tokens_per_tile, c.context);
+                            tma_load_4d(base + C::kOffDO + buf * C::kQBytes, &tm_do, bar(C::kQFull + buf), 0, c.kv * p.G, c.tile * p.tokens_per_tile, c.context);
+                        }
+                        const uint32_t st = loaded % kStages;
+                        const int key = (c.first + next_block) * kCrossBlock;
+                        mbar_arrive_expect_tx(bar(C::kKFull + st), 2 * C::kKBytes);
+                        tma_load_4d(base + C::kOffK + st * C::kKBytes, &tm_k, bar(C::kKFull + st), 0, c.kv, key, c.context);
+                        tma_load_4d(base + C::kOffV + st * C::kKBytes, &tm_v, bar(C::kKFull + st), 0, c.kv, key, c.context);
+                    }
+                    __syncwarp();
+                    if (next_block == 0) ++q_loaded;
+                    ++loaded;
+                    if (++next_block < c.blocks) continue;
+                }
+                next += gridDim.x;
+                next_block = 0;
+            }
+        };
+        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            const DqItem c = decode(p, item);
+            if (!c.blocks) continue;
+            const uint32_t buf = live % kTiles;
+            for (int j = 0; j < c.blocks; ++j, ++step) {
+                load_ahead();
+                const uint32_t st = step % kStages;
+                const int keys = min(kCrossBlock, c.length - (c.first + j) * kCrossBlock), columns = (keys + 15) & ~15;
+                if ((j == 0 && !mbar_wait_warp(bar(C::kQFull + buf), (live / kTiles) & 1, abort_flag, p.status)) ||
+                    !mbar_wait_warp(bar(C::kKFull + st), (step / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
+                if (keys < columns) {      // keys behind the last one: dS of 0 times what lies there must not become NaN
+                    cross_zero_rows(base_ptr + C::kOffK + st * C::kKBytes, C::kRow, keys, columns, lane, 32);
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                const uint64_t k = smem_desc_at(T::kDesc, base + C::kOffK + st * C::kKBytes);
+                const uint32_t idesc = idesc_bf16_f32(kRows, columns, false);
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + buf * C::kQBytes);
+#pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem, q + T::kStepK * kk, k + T::kStepK * kk, idesc, kk ? 1u : 0u);
+                    mma_commit(bar(C::kSFull));
+                }
+                __syncwarp();
+                if (!mbar_wait_warp(bar(C::kSRead), step & 1, abort_flag, p.status)) { ok = false; break; }
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t g = smem_desc_at(T::kDesc, base + C::kOffDO + buf * C::kQBytes), v = smem_desc_at(T::kDesc, base + C::kOffV + st * C::kKBytes);
+#pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem, g + T::kStepK * kk, v + T::kStepK * kk, idesc, kk ? 1u : 0u);
+                    mma_commit(bar(C::kDPFull));
+                }
+                __syncwarp();
+                if (!mbar_wait_warp(bar(C::kDSReady), step & 1, abort_flag, p.status)) { ok = false; break; }
+                tc_fence_after();
+                if (elect_one()) {
+                    constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
+                    for (int kk = 0; kk < columns / 16; ++kk) mma_ts(tmem + kDqColAcc, tmem + 8 * kk, k + T::kStepRows * kk, kIdesc, (j || kk) ? 1u : 0u);
+                    mma_commit(bar(C::kDQDone));
+                }
+                __syncwarp();
+                if (!mbar_wait_warp(bar(C::kDQDone), step & 1, abort_flag, p.status)) { ok = false; break; }
+            }
+            ++live;
+        }
+        if (!ok) {      // gave up: copies in flight land before the CTA may exit
+            for (uint32_t i = step; i < loaded; ++i) mbar_wait_warp(bar(C::kKFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
+            for (uint32_t i = live; i < q_loaded; ++i) mbar_wait_warp(bar(C::kQFull + i % kTiles), (i / kTiles) & 1, abort_flag + 1, p.status);
+        }
+        if (elect_one()) mma_commit(bar(C::kDrain));
+        __syncwarp();
+        mbar_wait_warp(bar(C::kDrain), 0, abort_flag + 1, p.status);
+    } else {
+        // ============================================ P, dS and dQ: a row to a thread
+        const int row = threadIdx.x;
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16, t_s = tmem + lanes, t_acc = tmem + lanes + kDqColAcc;
+        const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
+        int row_token, row_head;
+        p.by_group.divmod(row, row_token, row_head);
+        uint32_t step = 0;
+        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            const DqItem c = decode(p, item);
+            const long long token = (long long)c.tile * p.tokens_per_tile + row_token;
+            const bool mine = row < p.rows_per_tile && token < p.tokens;
+            const float2 stats = mine ? p.stats.at[stats_index(p.stats, c.group, token, row_head)] : make_float2(-INFINITY, 0.f);
+            const float2 neg2 = make_float2(stats.x, stats.x), d2 = make_float2(stats.y, stats.y);
+            for (int j = 0; j < c.blocks; ++j, ++step) {
+                if (!mbar_wait_warp(bar(C::kSFull), step & 1, abort_flag, p.status)) { ok = false; break; }
+                tc_fence_after();
+                uint32_t a[32], b[32];
+                tmem_ld32(t_s, a);
+                tmem_ld32(t_s + 32, b);
+                tmem_wait_ld();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::kSRead));
+                const int keys = c.length - (c.first + j) * kCrossBlock;
+                auto weight = [&](uint32_t (&s)[32]) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale2, neg2);
+                        // (a weight is at most 1, whatever the roundings of large scores and lse make of it)
+                        s[e] = __float_as_uint(ex2_approx(min_nan(x.x, 0.f)));
+                        s[e + 1] = __float_as_uint(ex2_approx(min_nan(x.y, 0.f)));
+                    }
+                };
+                weight(a);
+                weight(b);
+                if (keys < kCrossBlock) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        if (e >= keys) a[e] = 0u;
+                        if (e + 32 >= keys) b[e] = 0u;
+                    }
+                }
+                if (!mbar_wait_warp(bar(C::kDPFull), step & 1, abort_flag, p.status)) { ok = false; break; }
+                tc_fence_after();
+                // dS over dP, 16 keys at a time: they go where keys lie that have been read
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    uint32_t dp[16], packed[8];
+                    tmem_ld16(t_s + 16 * g, dp);
+                    tmem_wait_ld();
+                    if (keys < kCrossBlock) {      // (what lies behind the last key may be no number)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (16 * g + e >= keys) dp[e] = 0u;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int e = (16 * g + 2 * i) & 31;
+                        const float2 w = g < 2 ? make_float2(__uint_as_float(a[e]), __uint_as_float(a[e + 1])) : make_float2(__uint_as_float(b[e]), __uint_as_float(b[e + 1]));
+                        const float2 z = __fmul2_rn(w, __fadd2_rn(make_float2(__uint_as_float(dp[2 * i]), __uint_as_float(dp[2 * i + 1])), d2));
+                        packed[i] = pack_bf16x2(z.x, z.y);
+                    }
+                    tmem_st8(t_s + 8 * g, packed);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::kDSReady));
+            }
+            if (!ok) break;
+            const bool none = c.blocks == 0;
+            if (!none) {
+                if (!mbar_wait_warp(bar(C::kDQDone), (step - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+                tc_fence_after();
+            }
+            const long long at = ((long long)c.split * p.groups + c.group) * p.rows + token * p.G + row_head;
+            __nv_bfloat16* dst = p.dq + (((long long)c.context * p.tokens + token) * p.heads + c.kv * p.G + row_head) * p.d;
+#pragma unroll
+            for (int g = 0; g < DP / 32; ++g) {
+                uint32_t o[32];
+                float x[32];
+                if (!none) { tmem_ld32(t_acc + 32 * g, o); tmem_wait_ld(); }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = none ? 0.f : __uint_as_float(o[e]) * p.inv_sqrt_d;
+                if (mine && p.splits > 1) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(p.part + at * DP + 32 * g + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                } else if (mine) {
+                    cross_store_row(dst, 32 * g, p.d, x, p.vector != 0);
+                }
+                __syncwarp();
+            }
+            tc_fence_before();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 4) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kDqTmemCols);
+    }
+}
+
+// ----------------------------------------------------------------------------------------------- dK, dV
+// A CTA has one tile of 128 keys of a group, K and V of it in shared memory, dV and dK in tensor memory, and walks a run of the group's tiles of 64 rows:
+//     S^T = K Q^T,  dP^T = V dO^T   (M128 N64)      P^T, dS^T over them, a key to a thread      dV += P^T dO,  dK += dS^T Q   (A from tensor memory)
+// Three sets of 64 + 64 columns rotate among the tiles, each with four warps of its own, so that one set's exponentials run under the others' products.
+constexpr int kKvThreads = 512, kSets = 3;
+constexpr uint32_t kKvTmemCols = 512, kColDV = kSets * 128;
+
+template <int DP> struct KvCfg {
+    static constexpr int kStages = 6;
+    static constexpr uint32_t kRow = DP * 2, kKeyBytes = kRows * kRow, kRowBytes = kKvRows * kRow, kStatBytes = kKvRows * 8;
+    static constexpr uint32_t kOffK = 0, kOffV = kKeyBytes, kOffQ = 2 * kKeyBytes, kOffDO = kOffQ + kStages * kRowBytes, kOffStats = kOffDO + kStages * kRowBytes,
+                              kOffBar = kOffStats + kStages * kStatBytes;
+    static constexpr int kKVFull = 0, kFull = 1, kEmpty = kFull + kStages, kSFull = kEmpty + kStages, kReady = kSFull + kSets, kFree = kReady + kSets, kAccFull = kFree + kSets,
+                         kDrain = kAccFull + 1, kBars = kDrain + 2;
+    static constexpr uint32_t kOffMisc = kOffBar + kBars * 8, kSmem = kOffMisc + 16 + 1024;
+    static_assert(kRowBytes % 1024 == 0 && kSmem <= 232448, "swizzle atoms need aligned tiles; shared memory of a CTA");
+    static_assert(kColDV + 2 * DP <= kKvTmemCols, "tensor memory has 512 columns");
+};
+
+struct KvParams {
+    const int* lengths;
+    const float2* stats;
+    __nv_bfloat16 *dk, *dv;
+    float *part_dk, *part_dv;            // splits > 1: [splits][groups][L][DP]
+    int* status;
+    int d, L, kv_heads, G, key_tiles, splits, row_tiles, tiles_per_split, rows_per_tile, tokens_per_tile, vector;
+    long long groups;
+    float scale_log2, inv_sqrt_d;
+};
+
+template <int DP>
+__global__ void __launch_bounds__(kKvThreads, 1)
+rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                         const __grid_constant__ KvParams p)
+{
+    using C = KvCfg<DP>;
+    using T = CrossTile<DP>;
+    constexpr int kStages = C::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + C::kOffMisc);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kOffMisc + 4);      // [1] stays 0: used by the drain waits
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int rest = blockIdx.x;
+    const int split = rest % p.splits; rest /= p.splits;
+    const int key_tile = rest % p.key_tiles, group = rest / p.key_tiles, context = group / p.kv_heads, kv = group - context * p.kv_heads;
+    const int length = p.lengths ? min(max(__ldg(p.lengths + context), 0), p.L) : p.L;
+    const int first = split * p.tiles_per_split, key0 = key_tile * kRows;
+    const int tiles = key0 < length ? min(p.row_tiles - first, p.tiles_per_split) : 0;       // CTA-uniform
+
+    if (threadIdx.x == 0) {
+        abort_flag[0] = 0; abort_flag[1] = 0;
+        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i >= C::kReady && i < C::kReady + kSets ? 4 : 1);
+        fence_barrier_init();
+        prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_do); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
+    }
+    if (warp == 12) {
+        tmem_alloc(base + C::kOffMisc, kKvTmemCols);
+        tmem_relinquish();
+    }
+    for (int i = 0; i < 2 * kStages; ++i) cross_zero_rows(base_ptr + C::kOffQ + i * C::kRowBytes, C::kRow, p.rows_per_tile, kKvRows, threadIdx.x, kKvThreads);
+    fence_proxy_async();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    bool ok = true;
+
+    if (warp == 12) {
+        // ============================================ loads
+        int t = 0;
+        if (tiles > 0 && elect_one()) {
+            mbar_arrive_expect_tx(bar(C::kKVFull), 2 * C::kKeyBytes);
+            tma_load_4d(base + C::kOffK, &tm_k, bar(C::kKVFull), 0, kv, key0, context);
+            tma_load_4d(base + C::kOffV, &tm_v, bar(C::kKVFull), 0, kv, key0, context);
+        }
+        __syncwarp();
+        for (; t < tiles; ++t) {
+            const uint32_t st = t % kStages, use = t / kStages;
+            if (use > 0 && !mbar_wait_warp(bar(C::kEmpty + st), (use - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+            if (elect_one()) {
+                const int tile = first + t;
+                mbar_arrive_expect_tx(bar(C::kFull + st), 2u * (uint32_t)p.rows_per_tile * C::kRow + C::kStatBytes);
+                tma_load_4d(base + C::kOffQ + st * C::kRowBytes, &tm_q, bar(C::kFull + st), 0, kv * p.G, tile * p.tokens_per_tile, context);
+                tma_load_4d(base + C::kOffDO + st * C::kRowBytes, &tm_do, bar(C::kFull + st), 0, kv * p.G, tile * p.tokens_per_tile, context);
+                bulk_load_1d(base + C::kOffStats + st * C::kStatBytes, p.stats + ((long long)group * p.row_tiles + tile) * kKvRows, C::kStatBytes, bar(C::kFull + st));
+            }
+            __syncwarp();
+        }
+        if (!ok) {      // gave up: copies in flight land before the CTA may exit
+            for (int i = t > kStages ? t - kStages : 0; i < t; ++i) mbar_wait_warp(bar(C::kFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
+            if (tiles > 0) mbar_wait_warp(bar(C::kKVFull), 0, abort_flag + 1, p.status);
+        }
+    } else if (warp == 13) {
+        // ============================================ S^T and dP^T
+        if (tiles > 0) ok = mbar_wait_warp(bar(C::kKVFull), 0, abort_flag, p.status);
+        for (int t = 0; t < tiles && ok; ++t) {
+            const uint32_t st = t % kStages, set = t % kSets, round = t / kSets;
+            if (!mbar_wait_warp(bar(C::kFull + st), (t / kStages) & 1, abort_flag, p.status) ||
+                (round > 0 && !mbar_wait_warp(bar(C::kFree + set), (round - 1) & 1, abort_flag, p.status))) { ok = false; break; }
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t k = smem_desc_at(T::kDesc, base + C::kOffK), v = smem_desc_at(T::kDesc, base + C::kOffV);
+                const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + st * C::kRowBytes), g = smem_desc_at(T::kDesc, base + C::kOffDO + st * C::kRowBytes);
+                constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, kKvRows, false);
+#pragma unroll
+                for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem + set * 128, k + T::kStepK * kk, q + T::kStepK * kk, kIdesc, kk ? 1u : 0u);
+#pragma unroll
+                for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem + set * 128 + 64, v + T::kStepK * kk, g + T::kStepK * kk, kIdesc, kk ? 1u : 0u);
+                mma_commit(bar(C::kSFull + set));
+            }
+            __syncwarp();
+        }
+    } else if (warp == 14) {
+        // ============================================ dV and dK
+        for (int t = 0; t < tiles; ++t) {
+            const uint32_t st = t % kStages, set = t % kSets, round = t / kSets;
+            if (!mbar_wait_warp(bar(C::kReady + set), round & 1, abort_flag, p.status)) { ok = false; break; }
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + st * C::kRowBytes), g = smem_desc_at(T::kDesc, base + C::kOffDO + st * C::kRowBytes);
+                constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
+#pragma unroll
+                for (int kk = 0; kk < kKvRows / 16; ++kk) mma_ts(tmem + kColDV, tmem + set * 128 + 8 * kk, g + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
+#pragma unroll
+                for (int kk = 0; kk < kKvRows / 16; ++kk) mma_ts(tmem + kColDV + DP, tmem + set * 128 + 64 + 8 * kk, q + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
+                mma_commit(bar(C::kFree + set));
+                mma_commit(bar(C::kEmpty + st));
+                if (t == tiles - 1) mma_commit(bar(C::kAccFull));
+            }
+            __syncwarp();
+        }
+    } else if (warp < 12) {
+        // ============================================ P^T and dS^T, a key to a thread; then dV and dK
+        const int set = warp >> 2;
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + set * 128, t_dp = t_s + 64;
+        const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
+        for (int t = set; t < tiles; t += kSets) {
+            const uint32_t st = t % kStages, round = t / kSets;
+            // (the statistics arrive with the rows: what the scores were computed from has landed, and this wait shows it to this thread)
+            if (!mbar_wait_warp(bar(C::kSFull + set), round & 1, abort_flag, p.status) || !mbar_wait_warp(bar(C::kFull + st), (t / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
+            tc_fence_after();
+            const float4* stats = reinterpret_cast<const float4*>(base_ptr + C::kOffStats + st * C::kStatBytes);     // two rows each
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                uint32_t s[16], dp[16], pp[8], pd[8];
+                tmem_ld16(t_s + 16 * g, s);
+                tmem_ld16(t_dp + 16 * g, dp);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float4 ld = stats[8 * g + i];
+                    const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, make_float2(ld.x, ld.z));
+                    const float2 w = make_float2(ex2_approx(min_nan(x.x, 0.f)), ex2_approx(min_nan(x.y, 0.f)));
+                    const float2 z = __fmul2_rn(w, __fadd2_rn(make_float2(__uint_as_float(dp[2 * i]), __uint_as_float(dp[2 * i + 1])), make_float2(ld.y, ld.w)));
+                    pp[i] = pack_bf16x2(w.x, w.y);
+                    pd[i] = pack_bf16x2(z.x, z.y);
+                }
+                tmem_st8(t_s + 8 * g, pp);
+                tmem_st8(t_dp + 8 * g, pd);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::kReady + set));
+        }
+        if (ok && tiles > 0 && set < 2) {
+            ok = mbar_wait_warp(bar(C::kAccFull), 0, abort_flag, p.status);
+            tc_fence_after();
+        }
+        // four warps store dV, four dK
+        if (ok && set < 2) {
+            const int key = key0 + row;
+            const bool mine = key < p.L, zero = tiles <= 0 || key >= length;
+            const float scale = set == 0 ? 1.f : p.inv_sqrt_d;
+            __nv_bfloat16* dst = (set == 0 ? p.dv : p.dk) + (((long long)context * p.L + key) * p.kv_heads + kv) * p.d;
+            float* part = (set == 0 ? p.part_dv : p.part_dk) + (((long long)split * p.groups + group) * p.L + key) * DP;
+#pragma unroll
+            for (int g = 0; g < DP / 32; ++g) {
+                uint32_t o[32];
+                float x[32];
+                if (tiles > 0) { tmem_ld32(tmem + lanes + kColDV + set * DP + 32 * g, o); tmem_wait_ld(); }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = zero ? 0.f : __uint_as_float(o[e]) * scale;
+                if (mine && p.splits > 1) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + 32 * g + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                } else if (mine) {
+                    cross_store_row(dst, 32 * g, p.d, x, p.vector != 0);
+                }
+                __syncwarp();
+            }
+        }
+    }
+    if (warp == 13 || warp == 14) {
+        // everything issued by this warp has finished before the tensor memory is released
+        if (elect_one()) mma_commit(bar(C::kDrain + warp - 13));
+        __syncwarp();
+        mbar_wait_warp(bar(C::kDrain + warp - 13), 0, abort_flag + 1, p.status);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 12) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kKvTmemCols);
+    }
+}
+
+// ------------------------------------------------------------------------------------ sums of the splits
+struct SumTensor { const float* part; __nv_bfloat16* dst; long long rows; int splits, G, heads; long long rows_of_group, tokens; };      // rows of all groups; dst [contexts][tokens][heads][d], heads = groups of a context x G
+struct SumParams { SumTensor t[3]; int d, stride, chunks, vector; };
+__global__ void __launch_bounds__(256) rib_cross_bwd_sum_kernel(const SumParams p)
+{
+    const SumTensor t = p.t[blockIdx.y];
+    const long long thread = (long long)blockIdx.x * 256 + threadIdx.x, at = thread / p.chunks;
+    const int chunk = (int)(thread - at * p.chunks);
+    if (at >= t.rows) return;
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    for (int s = 0; s < t.splits; ++s) {
+        const float4* src = reinterpret_cast<const float4*>(t.part + (s * t.rows + at) * p.stride + 8 * chunk);
+        const float4 lo = src[0], hi = src[1];
+        x[0] += lo.x; x[1] += lo.y; x[2] += lo.z; x[3] += lo.w;
+        x[4] += hi.x; x[5] += hi.y; x[6] += hi.z; x[7] += hi.w;
+    }
+    const long long group = at / t.rows_of_group, r = at - group * t.rows_of_group, token = r / t.G;
+    const int per_context = t.heads / t.G;
+    const long long context = group / per_context;
+    const int head = (int)(group - context * per_context) * t.G + (int)(r - token * t.G);
+    cross_store_row(t.dst + ((context * t.tokens + token) * t.heads + head) * p.d, 8 * chunk, p.d, x, p.vector != 0);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+int tile_width(int d) { return d <= 32 ? 32 : 64; }
+
+struct BwdLayout { size_t q, dout, k, v, stats, part_dq, part_dk, part_dv, bytes; };
+BwdLayout bwd_layout(const CrossProblem& p, const CrossPlan& plan)
+{
+    BwdLayout l{};
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += cross_align(bytes); return here; };
+    if (cross_padded(p)) {
+        const size_t width = (p.d + 7) / 8 * 8, queries = 2 * width * p.tokens * p.contexts * p.heads, keys = 2 * width * p.L * p.contexts * p.kv_heads;
+        l.q = take(queries); l.dout = take(queries); l.k = take(keys); l.v = take(keys);
+    }
+    l.stats = take(sizeof(float2) * kKvRows * plan.row_tiles * plan.groups);
+    const size_t row = sizeof(float) * tile_width(p.d);
+    if (plan.splits > 1) l.part_dq = take(row * plan.splits * plan.groups * plan.rows);
+    if (plan.row_splits > 1) {
+        l.part_dk = take(row * plan.row_splits * plan.groups * p.L);
+        l.part_dv = take(row * plan.row_splits * plan.groups * p.L);
+    }
+    l.bytes = at;
+    return l;
+}
+
+template <int DP>
+cudaError_t launch_bwd(const CrossProblem& p, const CrossPlan& plan, const RowStats& stats, float* part_dq, float* part_dk, float* part_dv, cudaStream_t stream)
+{
+    if (!encode_fn()) return cudaErrorNotSupported;
+    CUtensorMap tm_q, tm_do, tm_k, tm_v, kv_q, kv_do, kv_k, kv_v;
+    const auto rows = [&](CUtensorMap* m, const void* x, int tokens) { return cross_rows_map(m, x, p.contexts, p.tokens, p.heads, p.width, DP, plan.G, tokens); };
+    const auto keys = [&](CUtensorMap* m, const void* x, int n) { return cross_rows_map(m, x, p.contexts, p.L, p.kv_heads, p.width, DP, 1, n); };
+    if (!rows(&tm_q, p.q, plan.tokens_per_tile) || !rows(&tm_do, p.dout, plan.tokens_per_tile) || !rows(&kv_q, p.q, plan.kv_tokens_per_tile) || !rows(&kv_do, p.dout, plan.kv_tokens_per_tile) ||
+        !keys(&tm_k, p.k, kCrossBlock) || !keys(&tm_v, p.v, kCrossBlock) || !keys(&kv_k, p.k, kRows) || !keys(&kv_v, p.v, kRows))
+        return cudaErrorInvalidValue;
+    static KernelSetup dq_setup, kv_setup;
+    int sms = 0;
+    if (cudaError_t e = dq_setup.prepare(rib_cross_bwd_dq_kernel<DP>, DqCfg<DP>::kSmem, &sms)) return e;
+    if (cudaError_t e = kv_setup.prepare(rib_cross_bwd_dkv_kernel<DP>, KvCfg<DP>::kSmem, &sms)) return e;
+    const float scale_log2 = kLog2e / sqrtf((float)p.d), inv_sqrt_d = 1.f / sqrtf((float)p.d);
+    DqParams a{};
+    a.lengths = p.lengths; a.dq = p.dq; a.part = part_dq; a.status = p.status; a.stats = stats;
+    a.d = p.d; a.L = p.L; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.rows_per_tile = plan.rows_per_tile; a.tokens_per_tile = plan.tokens_per_tile;
+    a.blocks_per_split = plan.blocks_per_split; a.splits = plan.splits; a.items = plan.groups * plan.splits * plan.tiles; a.vector = p.d % 8 == 0;
+    a.tokens = p.tokens; a.rows = plan.rows; a.groups = plan.groups; a.scale_log2 = scale_log2; a.inv_sqrt_d = inv_sqrt_d;
+    a.by_tiles = make_fast_div(plan.tiles); a.by_splits = make_fast_div(plan.splits); a.by_kv = make_fast_div(p.kv_heads); a.by_group = make_fast_div(plan.G);
+    const int slots = kCrossSms * DqCfg<DP>::kBlocksPerSm, grid = a.items < slots ? a.items : slots;
+    {
+        ProfileScope scope(RIB_KERNEL_CROSS_BWD_DQ, stream);
+        rib_cross_bwd_dq_kernel<DP><<<grid, kDqThreads, DqCfg<DP>::kSmem, stream>>>(tm_q, tm_do, tm_k, tm_v, a);
+    }
+    if (cudaError_t e = cudaGetLastError()) return e;
+    KvParams b{};
+    b.lengths = p.lengths; b.stats = stats.at; b.dk = p.dk; b.dv = p.dv; b.part_dk = part_dk; b.part_dv = part_dv; b.status = p.status;
+    b.d = p.d; b.L = p.L; b.kv_heads = p.kv_heads; b.G = plan.G; b.key_tiles = plan.key_tiles; b.splits = plan.row_splits; b.row_tiles = plan.row_tiles;
+    b.tiles_per_split = plan.row_tiles_per_split; b.rows_per_tile = plan.kv_rows_per_tile; b.tokens_per_tile = plan.kv_tokens_per_tile; b.vector = p.d % 8 == 0;
+    b.groups = plan.groups; b.scale_log2 = scale_log2; b.inv_sqrt_d = inv_sqrt_d;
+    ProfileScope scope(RIB_KERNEL_CROSS_BWD_DKV, stream);
+    rib_cross_bwd_dkv_kernel<DP><<<(unsigned)(plan.groups * plan.key_tiles * plan.row_splits), kKvThreads, KvCfg<DP>::kSmem, stream>>>(kv_q, kv_do, kv_k, kv_v, b);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t cross_bwd_workspace(const CrossProblem& p) { return bwd_layout(p, cross_plan(p)).bytes; }
+
+cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches)
+{
+    const CrossPlan plan = cross_plan(p);
+    const BwdLayout l = bwd_layout(p, plan);
+    uint8_t* ws = static_cast<uint8_t*>(p.workspace);
+    *launches = 3;
+    RowStats stats{};
+    stats.at = reinterpret_cast<float2*>(ws + l.stats);
+    stats.tokens_per_tile = plan.kv_tokens_per_tile; stats.tiles = plan.row_tiles; stats.G = plan.G; stats.by_tokens = make_fast_div(plan.kv_tokens_per_tile);
+    PrepareParams a{};
+    a.out = p.out; a.dout = p.dout; a.lse = p.lse_in; a.stats = stats;
+    a.rows = p.tokens * p.contexts * p.heads; a.entries = (long long)plan.groups * plan.row_tiles * kKvRows; a.tokens = p.tokens; a.pixels = p.pixels;
+    a.d = p.d; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.vector = p.d % 8 == 0;
+    a.lanes = p.d <= 8 ? 1 : p.d <= 16 ? 2 : p.d <= 32 ? 4 : 8;
+    a.row_blocks = (int)((a.rows * a.lanes + 255) / 256);
+    a.by_group = make_fast_div(plan.G); a.by_pixels = make_fast_div((int)p.pixels); a.by_tokens_of_context = make_fast_div((int)p.tokens);
+    {
+        ProfileScope scope(RIB_KERNEL_CROSS_BWD_PREPARE, stream);
+        rib_cross_bwd_prepare_kernel<<<(unsigned)(a.row_blocks + (a.entries + 255) / 256), 256, 0, stream>>>(a);
+    }
+    if (cudaError_t e = cudaGetLastError()) return e;
+    p.width = p.d;
+    if (cross_padded(p)) {
+        CrossPad pad{};
+        pad.tensors = 4; pad.d = p.d; pad.width = (p.d + 7) / 8 * 8;
+        const __nv_bfloat16** src[4] = {&p.q, &p.dout, &p.k, &p.v};
+        const size_t off[4] = {l.q, l.dout, l.k, l.v};
+        for (int i = 0; i < 4; ++i) {
+            pad.src[i] = *src[i];
+            pad.dst[i] = reinterpret_cast<__nv_bfloat16*>(ws + off[i]);
+            pad.rows[i] = p.contexts * (i >= 2 ? (long long)p.L * p.kv_heads : p.tokens * p.heads);
+            *src[i] = pad.dst[i];
+        }
+        p.width = pad.width;
+        if (cudaError_t e = cross_pad(pad, stream)) return e;
+        ++*launches;
+    }
+    float *part_dq = reinterpret_cast<float*>(ws + l.part_dq), *part_dk = reinterpret_cast<float*>(ws + l.part_dk), *part_dv = reinterpret_cast<float*>(ws + l.part_dv);
+    if (cudaError_t e = tile_width(p.d) == 32 ? launch_bwd<32>(p, plan, stats, part_dq, part_dk, part_dv, stream) : launch_bwd<64>(p, plan, stats, part_dq, part_dk, part_dv, stream)) return e;
+    SumParams s{};
+    int tensors = 0;
+    if (plan.splits > 1) s.t[tensors++] = SumTensor{part_dq, p.dq, plan.groups * plan.rows, plan.splits, plan.G, p.heads, plan.rows, p.tokens};
+    if (plan.row_splits > 1) {
+        s.t[tensors++] = SumTensor{part_dk, p.dk, (long long)plan.groups * p.L, plan.row_splits, 1, p.kv_heads, p.L, p.L};
+        s.t[tensors++] = SumTensor{part_dv, p.dv, (long long)plan.groups * p.L, plan.row_splits, 1, p.kv_heads, p.L, p.L};
+    }
+    if (!tensors) return cudaSuccess;
+    s.d = p.d; s.stride = tile_width(p.d); s.chunks = (p.d + 7) / 8; s.vector = p.d % 8 == 0;
+    long long most = 0;
+    for (int i = 0; i < tensors; ++i) most = s.t[i].rows > most ? s.t[i].rows : most;
+    ++*launches;
+    ProfileScope scope(RIB_KERNEL_CROSS_BWD_SUM, stream);
+    rib_cross_bwd_sum_kernel<<<dim3((unsigned)((most * s.chunks + 255) / 256), (unsigned)tensors), 256, 0, stream>>>(s);
+    return cudaGetLastError();
+}
+
+}  // namespace rib
