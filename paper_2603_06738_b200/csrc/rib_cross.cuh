@@ -28,7 +28,8 @@ struct CrossProblem {
 struct CrossPlan {
     int G, rows_per_tile, tokens_per_tile, tiles, groups, blocks;      // groups: contexts x kv_heads; blocks: of 64 keys
     long long rows;                                                    // of a group: tokens x G
-    int splits, blocks_per_split;                                      // out, dQ: runs of key blocks that are computed apart and joined
+    int splits, blocks_per_split;                                      // forward: runs of key blocks that are computed apart and joined
+    int dq_tiles, dq_splits, dq_blocks_per_split;                      // dQ: tiles of two row tiles, and such runs
     int key_tiles, row_splits, row_tiles_per_split;                    // dK and dV: tiles of 128 keys, runs of tiles of 64 rows
     int row_tiles, kv_rows_per_tile, kv_tokens_per_tile;
 };

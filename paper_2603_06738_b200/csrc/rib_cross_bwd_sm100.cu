@@ -13,16 +13,58 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kRows = 128, kKvRows = 64;             // rows of a tile: dQ; dK and dV
+constexpr int kRows = 128, kRowTile = 64;            // lanes of a product; rows of a tile of the statistics
 constexpr float kLog2e = 1.4426950408889634f;
 
-// (-lse log2 e, -D) of the rows of a group, in tiles of kKvRows entries of which kv_rows_per_tile are used: entries that are no row have (-infinity, 0), a weight of 0
-struct RowStats { float2* at; int tokens_per_tile, tiles, G; FastDiv by_tokens; };
+// -lse log2 e and -D of the rows of a group, in tiles of 64 entries of which tokens_per_tile x G are used, two by two: (-lse, -lse', -D, -D').  Entries that are
+// no row have (-infinity, 0), a weight of 0.  `tiles` is even: dQ takes two of them at a time.
+struct RowStats { float* at; int tokens_per_tile, tiles, G; FastDiv by_tokens; };
+__device__ __forceinline__ float* stats_entry(float* at, long long entry) { return at + 4 * (entry >> 1) + (entry & 1); }      // -lse; -D two behind
 __device__ __forceinline__ long long stats_index(const RowStats& s, long long group, long long token, int head)
 {
     int tile, t;
     s.by_tokens.divmod((int)token, tile, t);
-    return (group * s.tiles + tile) * kKvRows + t * s.G + head;
+    return (group * s.tiles + tile) * kRowTile + t * s.G + head;
+}
+
+// 64 columns of scores s and dP of a lane -> P and dS as bf16, in place.  x = s scale + neg, P = 2^x held to 1 whatever the roundings of large scores and lse make of it, dS = P (dP + d).
+// A chunk of 16 columns is loaded under the arithmetic of the one before; P and dS go where columns lie that have been read.  `stats(i)` gives (neg, neg', d, d') of
+// columns 2 i, 2 i + 1; columns from `columns` on weigh nothing, whatever they hold, and chunks that have none of them are left out.
+template <typename Stats>
+__device__ __forceinline__ void weights_in_place(uint32_t t_s, uint32_t t_dp, int columns, float2 scale2, Stats stats)
+{
+    uint32_t s[2][16], dp[2][16];
+    tmem_ld16(t_s, s[0]);
+    tmem_ld16(t_dp, dp[0]);
+    tmem_wait_ld();
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        if (16 * g >= columns) break;
+        if (g < 3) {
+            tmem_ld16(t_s + 16 * (g + 1), s[(g + 1) & 1]);
+            tmem_ld16(t_dp + 16 * (g + 1), dp[(g + 1) & 1]);
+        }
+        uint32_t (&a)[16] = s[g & 1], (&b)[16] = dp[g & 1];
+        if (columns < 16 * g + 16) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (16 * g + e >= columns) { a[e] = 0xff800000u; b[e] = 0u; }
+        }
+        uint32_t pp[8], pd[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 st = stats(8 * g + i);
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), scale2, make_float2(st.x, st.y));
+            const float2 w = make_float2(ex2_approx(min_nan(x.x, 0.f)), ex2_approx(min_nan(x.y, 0.f)));
+            const float2 z = __fmul2_rn(w, __fadd2_rn(make_float2(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])), make_float2(st.z, st.w)));
+            pp[i] = pack_bf16x2(w.x, w.y);
+            pd[i] = pack_bf16x2(z.x, z.y);
+        }
+        if (g < 3) tmem_wait_ld();
+        tmem_st8(t_s + 8 * g, pp);
+        tmem_st8(t_dp + 8 * g, pd);
+    }
+    tmem_wait_st();
 }
 
 // ------------------------------------------------------------------------------------------------ D, lse
@@ -32,7 +74,7 @@ struct PrepareParams {
     RowStats stats;
     long long rows, entries, tokens, pixels;         // rows: tokens of all contexts x heads; entries: of the statistics
     int d, heads, kv_heads, G, lanes, row_blocks;
-    FastDiv by_heads, by_group, by_pixels, by_tokens_of_context;
+    FastDiv by_group, by_pixels, by_tokens_of_context;
     int vector;
 };
 __global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const PrepareParams p)
@@ -40,8 +82,11 @@ __global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const Prepar
     if ((int)blockIdx.x >= p.row_blocks) {            // entries that are no row
         const long long e = (long long)(blockIdx.x - p.row_blocks) * 256 + threadIdx.x;
         if (e >= p.entries) return;
-        const int within = (int)(e % kKvRows), tile = (int)(e / kKvRows % p.stats.tiles);
-        if (within >= p.stats.tokens_per_tile * p.G || (long long)tile * p.stats.tokens_per_tile + within / p.G >= p.tokens) p.stats.at[e] = make_float2(-INFINITY, 0.f);
+        const int within = (int)(e % kRowTile), tile = (int)(e / kRowTile % p.stats.tiles);
+        if (within >= p.stats.tokens_per_tile * p.G || (long long)tile * p.stats.tokens_per_tile + within / p.G >= p.tokens) {
+            float* at = stats_entry(p.stats.at, e);
+            at[0] = -INFINITY; at[2] = 0.f;
+        }
         return;
     }
     // rows in the order of memory, `lanes` lanes (a power of two) to a row
@@ -73,22 +118,30 @@ __global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const Prepar
     p.by_tokens_of_context.divmod(token_of_all, context, token);
     p.by_group.divmod(head, kv, g);
     const float lse = p.lse[((long long)image * p.heads + head) * p.pixels + pixel];
-    p.stats.at[stats_index(p.stats, (long long)context * p.kv_heads + kv, token, g)] = make_float2(-lse * kLog2e, -sum);
+    float* at = stats_entry(p.stats.at, stats_index(p.stats, (long long)context * p.kv_heads + kv, token, g));
+    at[0] = -lse * kLog2e; at[2] = -sum;
 }
 
 // -------------------------------------------------------------------------------------------------- dQ
-constexpr int kDqThreads = 160;
-constexpr uint32_t kDqTmemCols = 128, kDqColAcc = 64;
+// Work item = two tiles of rows of a group (128 lanes) x a run of its key blocks of 64; a persistent CTA walks items, whose key blocks are one stream of steps:
+//     S = Q K^T,  dP = dO V^T   (M128 N64)     P, dS over them, a row to a thread     dQ += dS K   (A from tensor memory)
+// Three sets of 64 + 64 columns rotate among the steps, each with four warps of its own, so that one set's exponentials run under the others' products; dQ has two
+// accumulators, and four warps that store one while the next item is under way.
+// (The first form had four CTAs to an SM with one set of 64 columns each, S and dP one after the other: 256 x 256 tokens to 1024 states 283 us.)
+constexpr int kDqThreads = 640, kSets = 3;
+constexpr uint32_t kTmemCols = 512, kColAcc = kSets * 128;
 
 template <int DP> struct DqCfg {
-    static constexpr int kStages = 2, kTiles = DP == 32 ? 2 : 1, kBlocksPerSm = DP == 32 ? 4 : 3;
-    static constexpr uint32_t kRow = DP * 2, kQBytes = kRows * kRow, kKBytes = kCrossBlock * kRow;
-    static constexpr uint32_t kOffQ = 0, kOffDO = kTiles * kQBytes, kOffK = 2 * kTiles * kQBytes, kOffV = kOffK + kStages * kKBytes, kOffBar = kOffV + kStages * kKBytes;
-    // barriers: query tiles, key blocks, scores there, scores read, dP there, dS there, dS K done, all products done
-    static constexpr int kQFull = 0, kKFull = kTiles, kSFull = kKFull + kStages, kSRead = kSFull + 1, kDPFull = kSFull + 2, kDSReady = kSFull + 3, kDQDone = kSFull + 4,
-                         kDrain = kSFull + 5, kBars = kSFull + 6;
+    static constexpr int kStages = DP == 32 ? 8 : 6, kTiles = DP == 32 ? 4 : 3;
+    static constexpr uint32_t kRow = DP * 2, kQBytes = kRows * kRow, kKBytes = kCrossBlock * kRow, kStatBytes = kRows * 8;
+    static constexpr uint32_t kOffQ = 0, kOffDO = kTiles * kQBytes, kOffK = 2 * kTiles * kQBytes, kOffV = kOffK + kStages * kKBytes, kOffStats = kOffV + kStages * kKBytes,
+                              kOffInfo = kOffStats + kTiles * kStatBytes, kOffBar = (kOffInfo + kStages * 4 + 7) & ~7u;
+    // barriers: rows, key blocks, there and free again; of a set: scores and dP there, P and dS there, dS K done; of an accumulator: complete, stored; all products done
+    static constexpr int kQFull = 0, kQEmpty = kQFull + kTiles, kKFull = kQEmpty + kTiles, kKEmpty = kKFull + kStages, kSFull = kKEmpty + kStages, kReady = kSFull + kSets,
+                         kFree = kReady + kSets, kAccFull = kFree + kSets, kAccFree = kAccFull + 2, kDrain = kAccFree + 2, kBars = kDrain + 2;
     static constexpr uint32_t kOffMisc = kOffBar + kBars * 8, kSmem = kOffMisc + 16 + 1024;
-    static_assert(kBlocksPerSm * (kSmem + 1024) <= 233472, "shared memory of an SM");
+    static_assert(kSmem <= 232448, "shared memory of a CTA");
+    static_assert(kColAcc + 2 * DP <= kTmemCols, "tensor memory has 512 columns");
 };
 
 struct DqParams {
@@ -96,14 +149,14 @@ struct DqParams {
     __nv_bfloat16* dq;
     float* part;                         // splits > 1: [splits][groups][rows][DP]
     int* status;
-    RowStats stats;
-    int d, L, heads, kv_heads, G, rows_per_tile, tokens_per_tile, blocks_per_split, splits, items, vector;
+    const float* stats;
+    int d, L, heads, kv_heads, G, rows_per_tile, tokens_per_tile, row_tiles, blocks_per_split, splits, items, vector;
     long long tokens, rows, groups;
     float scale_log2, inv_sqrt_d;
     FastDiv by_tiles, by_splits, by_kv, by_group;
 };
 
-struct DqItem { int tile, split, group, context, kv, first, blocks, length; };
+struct DqItem { int tile, split, group, context, kv, first, blocks, length; };      // tile: of 128 rows
 __device__ __forceinline__ DqItem decode(const DqParams& p, int item)
 {
     DqItem c;
@@ -116,35 +169,35 @@ __device__ __forceinline__ DqItem decode(const DqParams& p, int item)
     return c;
 }
 
-// Tensor memory: 64 columns for the scores, which dP takes over once the scores are in registers and dS once dP is; dQ behind them.  As in the forward pass several
-// CTAs to an SM overlap what runs one after the other inside each.
 template <int DP>
-__global__ void __launch_bounds__(kDqThreads, DqCfg<DP>::kBlocksPerSm)
+__global__ void __launch_bounds__(kDqThreads, 1)
 rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                         const __grid_constant__ DqParams p)
 {
     using C = DqCfg<DP>;
     using T = CrossTile<DP>;
-    constexpr int kStages = C::kStages, kTiles = C::kTiles;
+    constexpr uint32_t kStages = C::kStages, kTiles = C::kTiles;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
     auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + C::kOffMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kOffMisc + 4);      // [1] stays 0: used by the drain waits
+    volatile int* info = reinterpret_cast<volatile int*>(base_ptr + C::kOffInfo);               // of a key block's stage: keys + 128 x (slot of its rows + 8 x parity of their barrier's phase)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         abort_flag[0] = 0; abort_flag[1] = 0;
-        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i == C::kSRead || i == C::kDSReady ? 4 : 1);
+        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), (i >= C::kReady && i < C::kFree) || (i >= C::kAccFree && i < C::kDrain) ? 4 : 1);
         fence_barrier_init();
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_do); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
     }
-    if (warp == 4) {
-        tmem_alloc(base + C::kOffMisc, kDqTmemCols);
+    if (warp == 12) {
+        tmem_alloc(base + C::kOffMisc, kTmemCols);
         tmem_relinquish();
     }
-    for (int i = 0; i < 2 * kTiles; ++i) cross_zero_rows(base_ptr + i * C::kQBytes, C::kRow, p.rows_per_tile, kRows, threadIdx.x, kDqThreads);
+    // rows that the boxes do not reach (G does not divide 64)
+    for (uint32_t i = 0; i < 4 * kTiles; ++i) cross_zero_rows(base_ptr + i * (C::kQBytes / 2), C::kRow, p.rows_per_tile, kRowTile, threadIdx.x, kDqThreads);
     fence_proxy_async();
     tc_fence_before();
     __syncthreads();
@@ -152,169 +205,146 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
 
-    if (warp == 4) {
-        // ============================================ loads and products
-        uint32_t step = 0, live = 0, loaded = 0, q_loaded = 0;
-        int next = blockIdx.x, next_block = 0;
-        auto load_ahead = [&]() {
-            while (next < p.items) {
-                const DqItem c = decode(p, next);
-                if (c.blocks) {
-                    if (next_block == 0 && q_loaded == live + kTiles) return;
-                    if (loaded == step + kStages) return;
-                    if (elect_one()) {
-                        if (next_block == 0) {
-                            const uint32_t buf = q_loaded % kTiles;
-                            mbar_arrive_expect_tx(bar(C::kQFull + buf), 2u * (uint32_t)p.rows_per_tile * C::kRow);
-                            tma_load_4d(base + C::kOffQ + buf * C::kQBytes, &tm_q, bar(C::kQFull + buf), 0, c.kv * p.G, c.tile * p.tokens_per_tile, c.context);
-                            tma_load_4d(base + C::kOffDO + buf * C::kQBytes, &tm_do, bar(C::kQFull + buf), 0, c.kv * p.G, c.tile * p.tokens_per_tile, c.context);
-                        }
-                        const uint32_t st = loaded % kStages;
-                        const int key = (c.first + next_block) * kCrossBlock;
-                        mbar_arrive_expect_tx(bar(C::kKFull + st), 2 * C::kKBytes);
-                        tma_load_4d(base + C::kOffK + st * C::kKBytes, &tm_k, bar(C::kKFull + st), 0, c.kv, key, c.context);
-                        tma_load_4d(base + C::kOffV + st * C::kKBytes, &tm_v, bar(C::kKFull + st), 0, c.kv, key, c.context);
-                    }
-                    __syncwarp();
-                    if (next_block == 0) ++q_loaded;
-                    ++loaded;
-                    if (++next_block < c.blocks) continue;
-                }
-                next += gridDim.x;
-                next_block = 0;
-            }
-        };
+    if (warp == 12) {
+        // ============================================ loads
+        uint32_t step = 0, live = 0, asked = 0;            // asked: items whose rows have been asked for
         for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
             const DqItem c = decode(p, item);
             if (!c.blocks) continue;
-            const uint32_t buf = live % kTiles;
+            const uint32_t slot = live % kTiles;
+            if (live >= kTiles && !mbar_wait_warp(bar(C::kQEmpty + slot), (live / kTiles - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+            if (elect_one()) {
+                const uint32_t at = slot * C::kQBytes, half = C::kQBytes / 2, full = bar(C::kQFull + slot);
+                const int token = 2 * c.tile * p.tokens_per_tile;
+                mbar_arrive_expect_tx(full, 4u * (uint32_t)p.rows_per_tile * C::kRow + C::kStatBytes);
+                for (int i = 0; i < 2; ++i) {
+                    tma_load_4d(base + C::kOffQ + at + i * half, &tm_q, full, 0, c.kv * p.G, token + i * p.tokens_per_tile, c.context);
+                    tma_load_4d(base + C::kOffDO + at + i * half, &tm_do, full, 0, c.kv * p.G, token + i * p.tokens_per_tile, c.context);
+                }
+                bulk_load_1d(base + C::kOffStats + slot * C::kStatBytes, p.stats + ((long long)c.group * p.row_tiles + 2 * c.tile) * (2 * kRowTile), C::kStatBytes, full);
+            }
+            __syncwarp();
+            ++asked;
             for (int j = 0; j < c.blocks; ++j, ++step) {
-                load_ahead();
                 const uint32_t st = step % kStages;
+                if (step >= kStages && !mbar_wait_warp(bar(C::kKEmpty + st), (step / kStages - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+                if (elect_one()) {
+                    const int key = (c.first + j) * kCrossBlock;
+                    info[st] = min(kCrossBlock, c.length - key) + 128 * (int)(slot + 8 * (live / kTiles & 1));
+                    mbar_arrive_expect_tx(bar(C::kKFull + st), 2 * C::kKBytes);
+                    tma_load_4d(base + C::kOffK + st * C::kKBytes, &tm_k, bar(C::kKFull + st), 0, c.kv, key, c.context);
+                    tma_load_4d(base + C::kOffV + st * C::kKBytes, &tm_v, bar(C::kKFull + st), 0, c.kv, key, c.context);
+                }
+                __syncwarp();
+            }
+            ++live;
+        }
+        if (!ok) {      // gave up: copies in flight land before the CTA may exit
+            for (uint32_t i = step > kStages ? step - kStages : 0; i < step; ++i) mbar_wait_warp(bar(C::kKFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
+            for (uint32_t i = asked > kTiles ? asked - kTiles : 0; i < asked; ++i) mbar_wait_warp(bar(C::kQFull + i % kTiles), (i / kTiles) & 1, abort_flag + 1, p.status);
+        }
+    } else if (warp == 13) {
+        // ============================================ S and dP
+        uint32_t step = 0, live = 0;
+        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            const DqItem c = decode(p, item);
+            if (!c.blocks) continue;
+            const uint32_t slot = live % kTiles;
+            if (!mbar_wait_warp(bar(C::kQFull + slot), (live / kTiles) & 1, abort_flag, p.status)) { ok = false; break; }
+            ++live;
+            for (int j = 0; j < c.blocks; ++j, ++step) {
+                const uint32_t st = step % kStages, set = step % kSets, round = step / kSets;
                 const int keys = min(kCrossBlock, c.length - (c.first + j) * kCrossBlock), columns = (keys + 15) & ~15;
-                if ((j == 0 && !mbar_wait_warp(bar(C::kQFull + buf), (live / kTiles) & 1, abort_flag, p.status)) ||
-                    !mbar_wait_warp(bar(C::kKFull + st), (step / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
+                if (!mbar_wait_warp(bar(C::kKFull + st), (step / kStages) & 1, abort_flag, p.status) ||
+                    (round > 0 && !mbar_wait_warp(bar(C::kFree + set), (round - 1) & 1, abort_flag, p.status))) { ok = false; break; }
                 if (keys < columns) {      // keys behind the last one: dS of 0 times what lies there must not become NaN
                     cross_zero_rows(base_ptr + C::kOffK + st * C::kKBytes, C::kRow, keys, columns, lane, 32);
                     fence_proxy_async();
                     __syncwarp();
                 }
-                const uint64_t k = smem_desc_at(T::kDesc, base + C::kOffK + st * C::kKBytes);
-                const uint32_t idesc = idesc_bf16_f32(kRows, columns, false);
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + buf * C::kQBytes);
+                    const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + slot * C::kQBytes), g = smem_desc_at(T::kDesc, base + C::kOffDO + slot * C::kQBytes);
+                    const uint64_t k = smem_desc_at(T::kDesc, base + C::kOffK + st * C::kKBytes), v = smem_desc_at(T::kDesc, base + C::kOffV + st * C::kKBytes);
+                    const uint32_t idesc = idesc_bf16_f32(kRows, columns, false);
 #pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem, q + T::kStepK * kk, k + T::kStepK * kk, idesc, kk ? 1u : 0u);
-                    mma_commit(bar(C::kSFull));
+                    for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem + set * 128, q + T::kStepK * kk, k + T::kStepK * kk, idesc, kk ? 1u : 0u);
+#pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem + set * 128 + 64, g + T::kStepK * kk, v + T::kStepK * kk, idesc, kk ? 1u : 0u);
+                    mma_commit(bar(C::kSFull + set));
                 }
                 __syncwarp();
-                if (!mbar_wait_warp(bar(C::kSRead), step & 1, abort_flag, p.status)) { ok = false; break; }
+            }
+        }
+    } else if (warp == 14) {
+        // ============================================ dQ
+        uint32_t step = 0, live = 0;
+        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            const DqItem c = decode(p, item);
+            if (!c.blocks) continue;
+            const uint32_t slot = live % kTiles, acc = live & 1;
+            for (int j = 0; j < c.blocks; ++j, ++step) {
+                const uint32_t st = step % kStages, set = step % kSets, round = step / kSets;
+                if (!mbar_wait_warp(bar(C::kReady + set), round & 1, abort_flag, p.status) ||
+                    (j == 0 && live >= 2 && !mbar_wait_warp(bar(C::kAccFree + acc), (live / 2 - 1) & 1, abort_flag, p.status))) { ok = false; break; }
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t g = smem_desc_at(T::kDesc, base + C::kOffDO + buf * C::kQBytes), v = smem_desc_at(T::kDesc, base + C::kOffV + st * C::kKBytes);
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem, g + T::kStepK * kk, v + T::kStepK * kk, idesc, kk ? 1u : 0u);
-                    mma_commit(bar(C::kDPFull));
-                }
-                __syncwarp();
-                if (!mbar_wait_warp(bar(C::kDSReady), step & 1, abort_flag, p.status)) { ok = false; break; }
-                tc_fence_after();
-                if (elect_one()) {
+                    const uint64_t k = smem_desc_at(T::kDesc, base + C::kOffK + st * C::kKBytes);
                     constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
-                    for (int kk = 0; kk < columns / 16; ++kk) mma_ts(tmem + kDqColAcc, tmem + 8 * kk, k + T::kStepRows * kk, kIdesc, (j || kk) ? 1u : 0u);
-                    mma_commit(bar(C::kDQDone));
+                    const int k_steps = (min(kCrossBlock, c.length - (c.first + j) * kCrossBlock) + 15) / 16;
+                    for (int kk = 0; kk < k_steps; ++kk) mma_ts(tmem + kColAcc + acc * DP, tmem + set * 128 + 64 + 8 * kk, k + T::kStepRows * kk, kIdesc, (j || kk) ? 1u : 0u);
+                    mma_commit(bar(C::kFree + set));
+                    mma_commit(bar(C::kKEmpty + st));
+                    if (j == c.blocks - 1) {
+                        mma_commit(bar(C::kAccFull + acc));
+                        mma_commit(bar(C::kQEmpty + slot));
+                    }
                 }
                 __syncwarp();
-                if (!mbar_wait_warp(bar(C::kDQDone), step & 1, abort_flag, p.status)) { ok = false; break; }
             }
             ++live;
         }
-        if (!ok) {      // gave up: copies in flight land before the CTA may exit
-            for (uint32_t i = step; i < loaded; ++i) mbar_wait_warp(bar(C::kKFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
-            for (uint32_t i = live; i < q_loaded; ++i) mbar_wait_warp(bar(C::kQFull + i % kTiles), (i / kTiles) & 1, abort_flag + 1, p.status);
-        }
-        if (elect_one()) mma_commit(bar(C::kDrain));
-        __syncwarp();
-        mbar_wait_warp(bar(C::kDrain), 0, abort_flag + 1, p.status);
-    } else {
-        // ============================================ P, dS and dQ: a row to a thread
-        const int row = threadIdx.x;
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16, t_s = tmem + lanes, t_acc = tmem + lanes + kDqColAcc;
+    } else if (warp < 12) {
+        // ============================================ P and dS, a row to a thread
+        const int set = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + set * 128;
         const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
+        uint32_t steps = 0;
+        for (long long item = blockIdx.x + (long long)lane * gridDim.x; item < p.items; item += 32ll * gridDim.x) steps += (uint32_t)decode(p, (int)item).blocks;
+        steps = __reduce_add_sync(0xffffffffu, steps);
+        for (uint32_t step = set; step < steps; step += kSets) {
+            const uint32_t st = step % kStages;
+            // (all of these have arrived when the scores are there: the waits show this thread what the producer wrote beside the key block, and the statistics)
+            if (!mbar_wait_warp(bar(C::kSFull + set), (step / kSets) & 1, abort_flag, p.status) || !mbar_wait_warp(bar(C::kKFull + st), (step / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
+            const int here = info[st], keys = here & 127, slot = here >> 7 & 7;
+            if (!mbar_wait_warp(bar(C::kQFull + slot), here >> 10, abort_flag, p.status)) { ok = false; break; }
+            tc_fence_after();
+            const float* stats = stats_entry(reinterpret_cast<float*>(base_ptr + C::kOffStats + slot * C::kStatBytes), row);
+            const float neg = stats[0], d = stats[2];
+            weights_in_place(t_s, t_s + 64, keys, scale2, [&](int) { return make_float4(neg, neg, d, d); });
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::kReady + set));
+        }
+    } else if (warp >= 16) {
+        // ============================================ stores of dQ
+        const int row = (warp & 3) * 32 + lane, within = row & (kRowTile - 1);
         int row_token, row_head;
-        p.by_group.divmod(row, row_token, row_head);
-        uint32_t step = 0;
+        p.by_group.divmod(within, row_token, row_head);
+        uint32_t live = 0;
         for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
             const DqItem c = decode(p, item);
-            const long long token = (long long)c.tile * p.tokens_per_tile + row_token;
-            const bool mine = row < p.rows_per_tile && token < p.tokens;
-            const float2 stats = mine ? p.stats.at[stats_index(p.stats, c.group, token, row_head)] : make_float2(-INFINITY, 0.f);
-            const float2 neg2 = make_float2(stats.x, stats.x), d2 = make_float2(stats.y, stats.y);
-            for (int j = 0; j < c.blocks; ++j, ++step) {
-                if (!mbar_wait_warp(bar(C::kSFull), step & 1, abort_flag, p.status)) { ok = false; break; }
-                tc_fence_after();
-                uint32_t a[32], b[32];
-                tmem_ld32(t_s, a);
-                tmem_ld32(t_s + 32, b);
-                tmem_wait_ld();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(C::kSRead));
-                const int keys = c.length - (c.first + j) * kCrossBlock;
-                auto weight = [&](uint32_t (&s)[32]) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale2, neg2);
-                        // (a weight is at most 1, whatever the roundings of large scores and lse make of it)
-                        s[e] = __float_as_uint(ex2_approx(min_nan(x.x, 0.f)));
-                        s[e + 1] = __float_as_uint(ex2_approx(min_nan(x.y, 0.f)));
-                    }
-                };
-                weight(a);
-                weight(b);
-                if (keys < kCrossBlock) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        if (e >= keys) a[e] = 0u;
-                        if (e + 32 >= keys) b[e] = 0u;
-                    }
-                }
-                if (!mbar_wait_warp(bar(C::kDPFull), step & 1, abort_flag, p.status)) { ok = false; break; }
-                tc_fence_after();
-                // dS over dP, 16 keys at a time: they go where keys lie that have been read
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    uint32_t dp[16], packed[8];
-                    tmem_ld16(t_s + 16 * g, dp);
-                    tmem_wait_ld();
-                    if (keys < kCrossBlock) {      // (what lies behind the last key may be no number)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (16 * g + e >= keys) dp[e] = 0u;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int e = (16 * g + 2 * i) & 31;
-                        const float2 w = g < 2 ? make_float2(__uint_as_float(a[e]), __uint_as_float(a[e + 1])) : make_float2(__uint_as_float(b[e]), __uint_as_float(b[e + 1]));
-                        const float2 z = __fmul2_rn(w, __fadd2_rn(make_float2(__uint_as_float(dp[2 * i]), __uint_as_float(dp[2 * i + 1])), d2));
-                        packed[i] = pack_bf16x2(z.x, z.y);
-                    }
-                    tmem_st8(t_s + 8 * g, packed);
-                }
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(C::kDSReady));
-            }
-            if (!ok) break;
             const bool none = c.blocks == 0;
+            const uint32_t acc = live & 1;
             if (!none) {
-                if (!mbar_wait_warp(bar(C::kDQDone), (step - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+                if (!mbar_wait_warp(bar(C::kAccFull + acc), (live / 2) & 1, abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
             }
+            const long long token = (long long)(2 * c.tile + (row >= kRowTile ? 1 : 0)) * p.tokens_per_tile + row_token;
+            const bool mine = within < p.rows_per_tile && token < p.tokens;
             const long long at = ((long long)c.split * p.groups + c.group) * p.rows + token * p.G + row_head;
             __nv_bfloat16* dst = p.dq + (((long long)c.context * p.tokens + token) * p.heads + c.kv * p.G + row_head) * p.d;
+            const uint32_t t_acc = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kColAcc + acc * DP;
 #pragma unroll
             for (int g = 0; g < DP / 32; ++g) {
                 uint32_t o[32];
@@ -322,6 +352,11 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 if (!none) { tmem_ld32(t_acc + 32 * g, o); tmem_wait_ld(); }
 #pragma unroll
                 for (int e = 0; e < 32; ++e) x[e] = none ? 0.f : __uint_as_float(o[e]) * p.inv_sqrt_d;
+                if (g == DP / 32 - 1 && !none) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(C::kAccFree + acc));
+                }
                 if (mine && p.splits > 1) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(p.part + at * DP + 32 * g + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
@@ -330,14 +365,20 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 }
                 __syncwarp();
             }
-            tc_fence_before();
+            if (!none) ++live;
         }
+    }
+    if (warp == 13 || warp == 14) {
+        // everything issued by this warp has finished before the tensor memory is released
+        if (elect_one()) mma_commit(bar(C::kDrain + warp - 13));
+        __syncwarp();
+        mbar_wait_warp(bar(C::kDrain + warp - 13), 0, abort_flag + 1, p.status);
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 4) {
+    if (warp == 12) {
         tc_fence_after();
-        tmem_dealloc(tmem, kDqTmemCols);
+        tmem_dealloc(tmem, kTmemCols);
     }
 }
 
@@ -345,28 +386,28 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 // A CTA has one tile of 128 keys of a group, K and V of it in shared memory, dV and dK in tensor memory, and walks a run of the group's tiles of 64 rows:
 //     S^T = K Q^T,  dP^T = V dO^T   (M128 N64)      P^T, dS^T over them, a key to a thread      dV += P^T dO,  dK += dS^T Q   (A from tensor memory)
 // Three sets of 64 + 64 columns rotate among the tiles, each with four warps of its own, so that one set's exponentials run under the others' products.
-constexpr int kKvThreads = 512, kSets = 3;
-constexpr uint32_t kKvTmemCols = 512, kColDV = kSets * 128;
+constexpr int kKvThreads = 512;
+constexpr uint32_t kColDV = kColAcc;
 
 template <int DP> struct KvCfg {
     static constexpr int kStages = 6;
-    static constexpr uint32_t kRow = DP * 2, kKeyBytes = kRows * kRow, kRowBytes = kKvRows * kRow, kStatBytes = kKvRows * 8;
+    static constexpr uint32_t kRow = DP * 2, kKeyBytes = kRows * kRow, kRowBytes = kRowTile * kRow, kStatBytes = kRowTile * 8;
     static constexpr uint32_t kOffK = 0, kOffV = kKeyBytes, kOffQ = 2 * kKeyBytes, kOffDO = kOffQ + kStages * kRowBytes, kOffStats = kOffDO + kStages * kRowBytes,
                               kOffBar = kOffStats + kStages * kStatBytes;
     static constexpr int kKVFull = 0, kFull = 1, kEmpty = kFull + kStages, kSFull = kEmpty + kStages, kReady = kSFull + kSets, kFree = kReady + kSets, kAccFull = kFree + kSets,
                          kDrain = kAccFull + 1, kBars = kDrain + 2;
     static constexpr uint32_t kOffMisc = kOffBar + kBars * 8, kSmem = kOffMisc + 16 + 1024;
     static_assert(kRowBytes % 1024 == 0 && kSmem <= 232448, "swizzle atoms need aligned tiles; shared memory of a CTA");
-    static_assert(kColDV + 2 * DP <= kKvTmemCols, "tensor memory has 512 columns");
+    static_assert(kColDV + 2 * DP <= kTmemCols, "tensor memory has 512 columns");
 };
 
 struct KvParams {
     const int* lengths;
-    const float2* stats;
+    const float* stats;
     __nv_bfloat16 *dk, *dv;
     float *part_dk, *part_dv;            // splits > 1: [splits][groups][L][DP]
     int* status;
-    int d, L, kv_heads, G, key_tiles, splits, row_tiles, tiles_per_split, rows_per_tile, tokens_per_tile, vector;
+    int d, L, kv_heads, G, key_tiles, splits, row_tiles, stat_tiles, tiles_per_split, rows_per_tile, tokens_per_tile, vector;
     long long groups;
     float scale_log2, inv_sqrt_d;
 };
@@ -400,10 +441,10 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_do); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
     }
     if (warp == 12) {
-        tmem_alloc(base + C::kOffMisc, kKvTmemCols);
+        tmem_alloc(base + C::kOffMisc, kTmemCols);
         tmem_relinquish();
     }
-    for (int i = 0; i < 2 * kStages; ++i) cross_zero_rows(base_ptr + C::kOffQ + i * C::kRowBytes, C::kRow, p.rows_per_tile, kKvRows, threadIdx.x, kKvThreads);
+    for (int i = 0; i < 2 * kStages; ++i) cross_zero_rows(base_ptr + C::kOffQ + i * C::kRowBytes, C::kRow, p.rows_per_tile, kRowTile, threadIdx.x, kKvThreads);
     fence_proxy_async();
     tc_fence_before();
     __syncthreads();
@@ -428,7 +469,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
                 mbar_arrive_expect_tx(bar(C::kFull + st), 2u * (uint32_t)p.rows_per_tile * C::kRow + C::kStatBytes);
                 tma_load_4d(base + C::kOffQ + st * C::kRowBytes, &tm_q, bar(C::kFull + st), 0, kv * p.G, tile * p.tokens_per_tile, context);
                 tma_load_4d(base + C::kOffDO + st * C::kRowBytes, &tm_do, bar(C::kFull + st), 0, kv * p.G, tile * p.tokens_per_tile, context);
-                bulk_load_1d(base + C::kOffStats + st * C::kStatBytes, p.stats + ((long long)group * p.row_tiles + tile) * kKvRows, C::kStatBytes, bar(C::kFull + st));
+                bulk_load_1d(base + C::kOffStats + st * C::kStatBytes, p.stats + ((long long)group * p.stat_tiles + tile) * (2 * kRowTile), C::kStatBytes, bar(C::kFull + st));
             }
             __syncwarp();
         }
@@ -447,7 +488,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             if (elect_one()) {
                 const uint64_t k = smem_desc_at(T::kDesc, base + C::kOffK), v = smem_desc_at(T::kDesc, base + C::kOffV);
                 const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + st * C::kRowBytes), g = smem_desc_at(T::kDesc, base + C::kOffDO + st * C::kRowBytes);
-                constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, kKvRows, false);
+                constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, kRowTile, false);
 #pragma unroll
                 for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem + set * 128, k + T::kStepK * kk, q + T::kStepK * kk, kIdesc, kk ? 1u : 0u);
 #pragma unroll
@@ -466,9 +507,9 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
                 const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + st * C::kRowBytes), g = smem_desc_at(T::kDesc, base + C::kOffDO + st * C::kRowBytes);
                 constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
 #pragma unroll
-                for (int kk = 0; kk < kKvRows / 16; ++kk) mma_ts(tmem + kColDV, tmem + set * 128 + 8 * kk, g + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
+                for (int kk = 0; kk < kRowTile / 16; ++kk) mma_ts(tmem + kColDV, tmem + set * 128 + 8 * kk, g + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
 #pragma unroll
-                for (int kk = 0; kk < kKvRows / 16; ++kk) mma_ts(tmem + kColDV + DP, tmem + set * 128 + 64 + 8 * kk, q + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
+                for (int kk = 0; kk < kRowTile / 16; ++kk) mma_ts(tmem + kColDV + DP, tmem + set * 128 + 64 + 8 * kk, q + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
                 mma_commit(bar(C::kFree + set));
                 mma_commit(bar(C::kEmpty + st));
                 if (t == tiles - 1) mma_commit(bar(C::kAccFull));
@@ -486,26 +527,8 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             // (the statistics arrive with the rows: what the scores were computed from has landed, and this wait shows it to this thread)
             if (!mbar_wait_warp(bar(C::kSFull + set), round & 1, abort_flag, p.status) || !mbar_wait_warp(bar(C::kFull + st), (t / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
             tc_fence_after();
-            const float4* stats = reinterpret_cast<const float4*>(base_ptr + C::kOffStats + st * C::kStatBytes);     // two rows each
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                uint32_t s[16], dp[16], pp[8], pd[8];
-                tmem_ld16(t_s + 16 * g, s);
-                tmem_ld16(t_dp + 16 * g, dp);
-                tmem_wait_ld();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float4 ld = stats[8 * g + i];
-                    const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, make_float2(ld.x, ld.z));
-                    const float2 w = make_float2(ex2_approx(min_nan(x.x, 0.f)), ex2_approx(min_nan(x.y, 0.f)));
-                    const float2 z = __fmul2_rn(w, __fadd2_rn(make_float2(__uint_as_float(dp[2 * i]), __uint_as_float(dp[2 * i + 1])), make_float2(ld.y, ld.w)));
-                    pp[i] = pack_bf16x2(w.x, w.y);
-                    pd[i] = pack_bf16x2(z.x, z.y);
-                }
-                tmem_st8(t_s + 8 * g, pp);
-                tmem_st8(t_dp + 8 * g, pd);
-            }
-            tmem_wait_st();
+            const float4* stats = reinterpret_cast<const float4*>(base_ptr + C::kOffStats + st * C::kStatBytes);
+            weights_in_place(t_s, t_dp, kRowTile, scale2, [&](int i) { return stats[i]; });
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::kReady + set));
@@ -548,7 +571,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
     __syncthreads();
     if (warp == 12) {
         tc_fence_after();
-        tmem_dealloc(tmem, kKvTmemCols);
+        tmem_dealloc(tmem, kTmemCols);
     }
 }
 
@@ -580,6 +603,8 @@ __global__ void __launch_bounds__(256) rib_cross_bwd_sum_kernel(const SumParams 
 // ------------------------------------------------------------------------------------------------ host
 int tile_width(int d) { return d <= 32 ? 32 : 64; }
 
+int stat_tiles(const CrossPlan& plan) { return (plan.row_tiles + 1) / 2 * 2; }
+
 struct BwdLayout { size_t q, dout, k, v, stats, part_dq, part_dk, part_dv, bytes; };
 BwdLayout bwd_layout(const CrossProblem& p, const CrossPlan& plan)
 {
@@ -590,9 +615,9 @@ BwdLayout bwd_layout(const CrossProblem& p, const CrossPlan& plan)
         const size_t width = (p.d + 7) / 8 * 8, queries = 2 * width * p.tokens * p.contexts * p.heads, keys = 2 * width * p.L * p.contexts * p.kv_heads;
         l.q = take(queries); l.dout = take(queries); l.k = take(keys); l.v = take(keys);
     }
-    l.stats = take(sizeof(float2) * kKvRows * plan.row_tiles * plan.groups);
+    l.stats = take(sizeof(float) * 2 * kRowTile * stat_tiles(plan) * plan.groups);
     const size_t row = sizeof(float) * tile_width(p.d);
-    if (plan.splits > 1) l.part_dq = take(row * plan.splits * plan.groups * plan.rows);
+    if (plan.dq_splits > 1) l.part_dq = take(row * plan.dq_splits * plan.groups * plan.rows);
     if (plan.row_splits > 1) {
         l.part_dk = take(row * plan.row_splits * plan.groups * p.L);
         l.part_dv = take(row * plan.row_splits * plan.groups * p.L);
@@ -605,11 +630,10 @@ template <int DP>
 cudaError_t launch_bwd(const CrossProblem& p, const CrossPlan& plan, const RowStats& stats, float* part_dq, float* part_dk, float* part_dv, cudaStream_t stream)
 {
     if (!encode_fn()) return cudaErrorNotSupported;
-    CUtensorMap tm_q, tm_do, tm_k, tm_v, kv_q, kv_do, kv_k, kv_v;
-    const auto rows = [&](CUtensorMap* m, const void* x, int tokens) { return cross_rows_map(m, x, p.contexts, p.tokens, p.heads, p.width, DP, plan.G, tokens); };
+    CUtensorMap tm_q, tm_do, tm_k, tm_v, kv_k, kv_v;
+    const auto rows = [&](CUtensorMap* m, const void* x) { return cross_rows_map(m, x, p.contexts, p.tokens, p.heads, p.width, DP, plan.G, plan.kv_tokens_per_tile); };
     const auto keys = [&](CUtensorMap* m, const void* x, int n) { return cross_rows_map(m, x, p.contexts, p.L, p.kv_heads, p.width, DP, 1, n); };
-    if (!rows(&tm_q, p.q, plan.tokens_per_tile) || !rows(&tm_do, p.dout, plan.tokens_per_tile) || !rows(&kv_q, p.q, plan.kv_tokens_per_tile) || !rows(&kv_do, p.dout, plan.kv_tokens_per_tile) ||
-        !keys(&tm_k, p.k, kCrossBlock) || !keys(&tm_v, p.v, kCrossBlock) || !keys(&kv_k, p.k, kRows) || !keys(&kv_v, p.v, kRows))
+    if (!rows(&tm_q, p.q) || !rows(&tm_do, p.dout) || !keys(&tm_k, p.k, kCrossBlock) || !keys(&tm_v, p.v, kCrossBlock) || !keys(&kv_k, p.k, kRows) || !keys(&kv_v, p.v, kRows))
         return cudaErrorInvalidValue;
     static KernelSetup dq_setup, kv_setup;
     int sms = 0;
@@ -617,12 +641,12 @@ cudaError_t launch_bwd(const CrossProblem& p, const CrossPlan& plan, const RowSt
     if (cudaError_t e = kv_setup.prepare(rib_cross_bwd_dkv_kernel<DP>, KvCfg<DP>::kSmem, &sms)) return e;
     const float scale_log2 = kLog2e / sqrtf((float)p.d), inv_sqrt_d = 1.f / sqrtf((float)p.d);
     DqParams a{};
-    a.lengths = p.lengths; a.dq = p.dq; a.part = part_dq; a.status = p.status; a.stats = stats;
-    a.d = p.d; a.L = p.L; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.rows_per_tile = plan.rows_per_tile; a.tokens_per_tile = plan.tokens_per_tile;
-    a.blocks_per_split = plan.blocks_per_split; a.splits = plan.splits; a.items = plan.groups * plan.splits * plan.tiles; a.vector = p.d % 8 == 0;
+    a.lengths = p.lengths; a.dq = p.dq; a.part = part_dq; a.status = p.status; a.stats = stats.at;
+    a.d = p.d; a.L = p.L; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.rows_per_tile = plan.kv_rows_per_tile; a.tokens_per_tile = plan.kv_tokens_per_tile;
+    a.row_tiles = stats.tiles; a.blocks_per_split = plan.dq_blocks_per_split; a.splits = plan.dq_splits; a.items = plan.groups * plan.dq_splits * plan.dq_tiles; a.vector = p.d % 8 == 0;
     a.tokens = p.tokens; a.rows = plan.rows; a.groups = plan.groups; a.scale_log2 = scale_log2; a.inv_sqrt_d = inv_sqrt_d;
-    a.by_tiles = make_fast_div(plan.tiles); a.by_splits = make_fast_div(plan.splits); a.by_kv = make_fast_div(p.kv_heads); a.by_group = make_fast_div(plan.G);
-    const int slots = kCrossSms * DqCfg<DP>::kBlocksPerSm, grid = a.items < slots ? a.items : slots;
+    a.by_tiles = make_fast_div(plan.dq_tiles); a.by_splits = make_fast_div(plan.dq_splits); a.by_kv = make_fast_div(p.kv_heads); a.by_group = make_fast_div(plan.G);
+    const int grid = a.items < kCrossSms ? a.items : kCrossSms;
     {
         ProfileScope scope(RIB_KERNEL_CROSS_BWD_DQ, stream);
         rib_cross_bwd_dq_kernel<DP><<<grid, kDqThreads, DqCfg<DP>::kSmem, stream>>>(tm_q, tm_do, tm_k, tm_v, a);
@@ -630,11 +654,11 @@ cudaError_t launch_bwd(const CrossProblem& p, const CrossPlan& plan, const RowSt
     if (cudaError_t e = cudaGetLastError()) return e;
     KvParams b{};
     b.lengths = p.lengths; b.stats = stats.at; b.dk = p.dk; b.dv = p.dv; b.part_dk = part_dk; b.part_dv = part_dv; b.status = p.status;
-    b.d = p.d; b.L = p.L; b.kv_heads = p.kv_heads; b.G = plan.G; b.key_tiles = plan.key_tiles; b.splits = plan.row_splits; b.row_tiles = plan.row_tiles;
+    b.d = p.d; b.L = p.L; b.kv_heads = p.kv_heads; b.G = plan.G; b.key_tiles = plan.key_tiles; b.splits = plan.row_splits; b.row_tiles = plan.row_tiles; b.stat_tiles = stats.tiles;
     b.tiles_per_split = plan.row_tiles_per_split; b.rows_per_tile = plan.kv_rows_per_tile; b.tokens_per_tile = plan.kv_tokens_per_tile; b.vector = p.d % 8 == 0;
     b.groups = plan.groups; b.scale_log2 = scale_log2; b.inv_sqrt_d = inv_sqrt_d;
     ProfileScope scope(RIB_KERNEL_CROSS_BWD_DKV, stream);
-    rib_cross_bwd_dkv_kernel<DP><<<(unsigned)(plan.groups * plan.key_tiles * plan.row_splits), kKvThreads, KvCfg<DP>::kSmem, stream>>>(kv_q, kv_do, kv_k, kv_v, b);
+    rib_cross_bwd_dkv_kernel<DP><<<(unsigned)(plan.groups * plan.key_tiles * plan.row_splits), kKvThreads, KvCfg<DP>::kSmem, stream>>>(tm_q, tm_do, kv_k, kv_v, b);
     return cudaGetLastError();
 }
 
@@ -649,11 +673,11 @@ cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches)
     uint8_t* ws = static_cast<uint8_t*>(p.workspace);
     *launches = 3;
     RowStats stats{};
-    stats.at = reinterpret_cast<float2*>(ws + l.stats);
-    stats.tokens_per_tile = plan.kv_tokens_per_tile; stats.tiles = plan.row_tiles; stats.G = plan.G; stats.by_tokens = make_fast_div(plan.kv_tokens_per_tile);
+    stats.at = reinterpret_cast<float*>(ws + l.stats);
+    stats.tokens_per_tile = plan.kv_tokens_per_tile; stats.tiles = stat_tiles(plan); stats.G = plan.G; stats.by_tokens = make_fast_div(plan.kv_tokens_per_tile);
     PrepareParams a{};
     a.out = p.out; a.dout = p.dout; a.lse = p.lse_in; a.stats = stats;
-    a.rows = p.tokens * p.contexts * p.heads; a.entries = (long long)plan.groups * plan.row_tiles * kKvRows; a.tokens = p.tokens; a.pixels = p.pixels;
+    a.rows = p.tokens * p.contexts * p.heads; a.entries = (long long)plan.groups * stats.tiles * kRowTile; a.tokens = p.tokens; a.pixels = p.pixels;
     a.d = p.d; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.vector = p.d % 8 == 0;
     a.lanes = p.d <= 8 ? 1 : p.d <= 16 ? 2 : p.d <= 32 ? 4 : 8;
     a.row_blocks = (int)((a.rows * a.lanes + 255) / 256);
@@ -683,7 +707,7 @@ cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches)
     if (cudaError_t e = tile_width(p.d) == 32 ? launch_bwd<32>(p, plan, stats, part_dq, part_dk, part_dv, stream) : launch_bwd<64>(p, plan, stats, part_dq, part_dk, part_dv, stream)) return e;
     SumParams s{};
     int tensors = 0;
-    if (plan.splits > 1) s.t[tensors++] = SumTensor{part_dq, p.dq, plan.groups * plan.rows, plan.splits, plan.G, p.heads, plan.rows, p.tokens};
+    if (plan.dq_splits > 1) s.t[tensors++] = SumTensor{part_dq, p.dq, plan.groups * plan.rows, plan.dq_splits, plan.G, p.heads, plan.rows, p.tokens};
     if (plan.row_splits > 1) {
         s.t[tensors++] = SumTensor{part_dk, p.dk, (long long)plan.groups * p.L, plan.row_splits, 1, p.kv_heads, p.L, p.L};
         s.t[tensors++] = SumTensor{part_dv, p.dv, (long long)plan.groups * p.L, plan.row_splits, 1, p.kv_heads, p.L, p.L};

@@ -5,12 +5,13 @@
 //     S = Q K^T           (M128, N = 64, or what the last block has rounded up to 16; K = 32 or 64 channels)
 //     P = exp2((S - m) log2e / sqrt(d)), a row to a thread, written over S as bf16
 //     O (+)= P V          (A from tensor memory, V an MN-major tile)
-// with a running maximum m per row that moves, and rescales O and the row's sum, only when a block exceeds it by more than 2^8 in the exponentials.  Inside a CTA
-// everything runs one after the other - scores, exponentials, product, next scores -; what fills the pipes is that 4 CTAs share an SM (128 columns of tensor
-// memory each: S 64, O 32 or 64; 3 CTAs with rows of 64 channels, whose tiles take 66 KB of shared memory).  The exponentials bound it: 128 x 64 of them take 512 cycles
-// of the SM's special-function units, the products about 130 (d = 32) to 260 cycles.
+// with a running maximum m per row that moves, and rescales O and the row's sum, only when a block exceeds it by more than 2^8 in the exponentials.
+// The key blocks of all items of a CTA are one stream of steps: three buffers of scores, so that the scores of the next two steps, which may belong to the next item, are there or under
+// way while the softmax warps work, and an item's output is normalised and stored behind the exponentials of the next item's first block, when its last product is long complete.
+// The exponentials bound it: 128 x 64 of them take 512 cycles of the SM's special-function units, the products about 130 (d = 32) to 260 cycles; two CTAs to an SM
+// (256 columns of tensor memory each) fill one another's gaps.
 //
-// Roles: warps 0-3 softmax and output of rows 32 w .. 32 w + 31; warp 4 loads (two query tiles, a ring of key blocks) and issues the products.  Every wait is bounded.
+// Roles: warps 0-3 softmax and output of rows 32 w .. 32 w + 31; warp 4 loads (query tiles, a ring of key blocks) and issues the products.  Every wait is bounded.
 #include "rib_cross.cuh"
 
 namespace rib {
@@ -18,18 +19,21 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kThreads = 160, kRows = 128;
-constexpr uint32_t kTmemCols = 128, kColO = 64;
+constexpr int kThreads = 160, kRows = 128, kBlocksPerSm = 2;
+constexpr uint32_t kBuffers = 3, kTmemCols = 256, kColO = kBuffers * kCrossBlock;
 
 template <int DP> struct Cfg {
-    static constexpr int kStages = DP == 32 ? 4 : 2, kBlocksPerSm = DP == 32 ? 4 : 3;
+    static constexpr int kStages = DP == 32 ? 8 : 4, kTiles = DP == 32 ? 4 : 3;
     static constexpr uint32_t kRow = DP * 2, kQBytes = kRows * kRow, kKBytes = kCrossBlock * kRow;
-    static constexpr uint32_t kOffQ = 0, kOffK = 2 * kQBytes, kOffV = kOffK + kStages * kKBytes, kOffBar = kOffV + kStages * kKBytes;
-    // barriers: query tiles, key blocks, scores there, P there, P V done, all products done
-    static constexpr int kQFull = 0, kKFull = 2, kSFull = kKFull + kStages, kPReady = kSFull + 1, kPVDone = kSFull + 2, kDrain = kSFull + 3, kBars = kSFull + 4;
-    static constexpr uint32_t kOffMisc = kOffBar + kBars * 8, kSmem = kOffMisc + 16 + 1024;
+    static constexpr uint32_t kOffQ = 0, kOffK = kTiles * kQBytes, kOffV = kOffK + kStages * kKBytes, kOffBar = kOffV + kStages * kKBytes;
+    // barriers: query tiles, key blocks; of each buffer of scores: scores there, P there, P V done; all products done.  (A parity wait cannot tell its own phase
+    // from one two phases on: a buffer's next phases need what the waiter does after this one.)
+    static constexpr int kQFull = 0, kKFull = kTiles, kSFull = kKFull + kStages, kPReady = kSFull + kBuffers, kPVDone = kPReady + kBuffers, kDrain = kPVDone + kBuffers, kBars = kDrain + 1;
+    static constexpr uint32_t kOffMisc = kOffBar + kBars * 8, kSmem = kOffMisc + 16;
+    static_assert(kTiles >= (int)kBuffers && kStages > (int)kBuffers, "the scores of kBuffers steps, each of an item of its own, are taken before the first product");
     static_assert(kQBytes % 1024 == 0 && kKBytes % 1024 == 0, "swizzle atoms need aligned tiles");
     static_assert(kBlocksPerSm * (kSmem + 1024) <= 233472, "shared memory of an SM");
+    static_assert(kColO + DP <= kTmemCols, "tensor memory of a CTA");
 };
 
 struct Params {
@@ -60,24 +64,56 @@ __device__ __forceinline__ Item decode(const Params& p, int item)
     return c;
 }
 
+// A place in the CTA's stream of steps (key blocks of its items, one item after the other; items without keys have none).
+struct Cursor {
+    Item c;
+    int item, block;
+    uint32_t step, live;                 // steps and items with steps before it
+    __device__ __forceinline__ void settle(const Params& p)          // to the next item that has a block
+    {
+        while (item < p.items) {
+            c = decode(p, item);
+            if (c.blocks) return;
+            item += gridDim.x;
+        }
+    }
+    __device__ __forceinline__ void begin(const Params& p) { item = blockIdx.x; block = 0; step = live = 0; settle(p); }
+    __device__ __forceinline__ bool there(const Params& p) const { return item < p.items; }
+    __device__ __forceinline__ void advance(const Params& p)
+    {
+        ++step;
+        if (++block < c.blocks) return;
+        block = 0;
+        ++live;
+        item += gridDim.x;
+        settle(p);
+    }
+    __device__ __forceinline__ int keys() const { return min(kCrossBlock, c.length - (c.first + block) * kCrossBlock); }
+};
+
 template <int DP>
-__global__ void __launch_bounds__(kThreads, Cfg<DP>::kBlocksPerSm)
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
 rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params p)
 {
     using C = Cfg<DP>;
     using T = CrossTile<DP>;
-    constexpr int kStages = C::kStages;
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    constexpr int kStages = C::kStages, kTiles = C::kTiles;
+    extern __shared__ __align__(1024) uint8_t base_ptr[];
+    const uint32_t base = smem_u32(base_ptr);
     auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
+    auto on_step = [&](int which, uint32_t step) { return bar(which + step % kBuffers); };
+    auto parity = [](uint32_t step) { return (step / kBuffers) & 1; };
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + C::kOffMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kOffMisc + 4);      // [1] stays 0: used by the drain waits
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (base & 1023u) {                                   // (never seen: the declaration above asks for it; swizzled tiles would be misread)
+        if (threadIdx.x == 0) atomicExch(p.status, 1);
+        return;
+    }
 
     if (threadIdx.x == 0) {
         abort_flag[0] = 0; abort_flag[1] = 0;
-        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i == C::kPReady ? 4 : 1);
+        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i >= C::kPReady && i < C::kPVDone ? 4 : 1);
         fence_barrier_init();
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
     }
@@ -86,7 +122,7 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         tmem_relinquish();
     }
     // rows that the boxes of Q do not reach (G does not divide 128)
-    for (int i = 0; i < 2; ++i) cross_zero_rows(base_ptr + C::kOffQ + i * C::kQBytes, C::kRow, p.rows_per_tile, kRows, threadIdx.x, kThreads);
+    for (int i = 0; i < kTiles; ++i) cross_zero_rows(base_ptr + C::kOffQ + i * C::kQBytes, C::kRow, p.rows_per_tile, kRows, threadIdx.x, kThreads);
     fence_proxy_async();
     tc_fence_before();
     __syncthreads();
@@ -96,78 +132,78 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 
     if (warp == 4) {
         // ============================================ loads and products: the whole warp walks, one elected lane issues
-        uint32_t step = 0, live = 0;                      // key blocks and items (with blocks) whose products are complete
-        uint32_t loaded = 0, q_loaded = 0;                // key blocks and query tiles asked for
-        int next = blockIdx.x, next_block = 0;            // the load that comes next
-        // Loads as far ahead as there is room: a stage is free once its block's P V is complete, a query tile once its item's last one is.
-        auto load_ahead = [&]() {
-            while (next < p.items) {
-                const Item c = decode(p, next);
-                if (c.blocks) {
-                    if (next_block == 0 && q_loaded == live + 2) return;
-                    if (loaded == step + kStages) return;
-                    if (elect_one()) {
-                        if (next_block == 0) {
-                            const uint32_t buf = q_loaded & 1;
-                            mbar_arrive_expect_tx(bar(C::kQFull + buf), (uint32_t)p.rows_per_tile * C::kRow);
-                            tma_load_4d(base + C::kOffQ + buf * C::kQBytes, &tm_q, bar(C::kQFull + buf), 0, c.kv * p.G, c.tile * p.tokens_per_tile, c.context);
-                        }
-                        const uint32_t st = loaded % kStages;
-                        const int key = (c.first + next_block) * kCrossBlock;
-                        mbar_arrive_expect_tx(bar(C::kKFull + st), 2 * C::kKBytes);
-                        tma_load_4d(base + C::kOffK + st * C::kKBytes, &tm_k, bar(C::kKFull + st), 0, c.kv, key, c.context);
-                        tma_load_4d(base + C::kOffV + st * C::kKBytes, &tm_v, bar(C::kKFull + st), 0, c.kv, key, c.context);
+        Cursor load, score, value;                        // the next step to load, to take the scores of, to multiply with its values
+        load.begin(p); score.begin(p); value.begin(p);
+        uint32_t q_loaded = 0;
+        // Loads as far ahead as there is room: a stage is free once its step's P V is complete (all before value.step are), a query tile once its item's
+        // scores are (`scored` items).
+        auto load_ahead = [&](uint32_t scored) {
+            for (; load.there(p); load.advance(p)) {
+                if (load.step == value.step + kStages) return;
+                if (load.block == 0 && load.live == scored + kTiles) return;
+                if (elect_one()) {
+                    if (load.block == 0) {
+                        const uint32_t buf = load.live % kTiles;
+                        mbar_arrive_expect_tx(bar(C::kQFull + buf), (uint32_t)p.rows_per_tile * C::kRow);
+                        tma_load_4d(base + C::kOffQ + buf * C::kQBytes, &tm_q, bar(C::kQFull + buf), 0, load.c.kv * p.G, load.c.tile * p.tokens_per_tile, load.c.context);
                     }
-                    __syncwarp();
-                    if (next_block == 0) ++q_loaded;
-                    ++loaded;
-                    if (++next_block < c.blocks) continue;
+                    const uint32_t st = load.step % kStages;
+                    const int key = (load.c.first + load.block) * kCrossBlock;
+                    mbar_arrive_expect_tx(bar(C::kKFull + st), 2 * C::kKBytes);
+                    tma_load_4d(base + C::kOffK + st * C::kKBytes, &tm_k, bar(C::kKFull + st), 0, load.c.kv, key, load.c.context);
+                    tma_load_4d(base + C::kOffV + st * C::kKBytes, &tm_v, bar(C::kKFull + st), 0, load.c.kv, key, load.c.context);
                 }
-                next += gridDim.x;
-                next_block = 0;
+                __syncwarp();
+                if (load.block == 0) ++q_loaded;
             }
         };
-        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-            const Item c = decode(p, item);
-            if (!c.blocks) continue;
-            for (int j = 0; j < c.blocks; ++j, ++step) {
-                load_ahead();
-                const uint32_t st = step % kStages;
-                const int keys = min(kCrossBlock, c.length - (c.first + j) * kCrossBlock), columns = (keys + 15) & ~15;
-                if ((j == 0 && !mbar_wait_warp(bar(C::kQFull + (live & 1)), (live >> 1) & 1, abort_flag, p.status)) ||
-                    !mbar_wait_warp(bar(C::kKFull + st), (step / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
-                if (keys < columns) {      // values behind the last key: weights of 0 times what lies there must not become NaN
-                    cross_zero_rows(base_ptr + C::kOffV + st * C::kKBytes, C::kRow, keys, columns, lane, 32);
-                    fence_proxy_async();
-                    __syncwarp();
-                }
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + (live & 1) * C::kQBytes), k = smem_desc_at(T::kDesc, base + C::kOffK + st * C::kKBytes);
-                    const uint32_t idesc = idesc_bf16_f32(kRows, columns, false);
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem, q + T::kStepK * kk, k + T::kStepK * kk, idesc, kk ? 1u : 0u);
-                    mma_commit(bar(C::kSFull));
-                }
+        // The scores of the next step, into the buffer whose P the product before the last one has read.
+        auto issue_scores = [&]() -> bool {
+            const uint32_t st = score.step % kStages, buf = score.live % kTiles;
+            const int keys = score.keys(), columns = (keys + 15) & ~15;
+            if ((score.block == 0 && !mbar_wait_warp(bar(C::kQFull + buf), (score.live / kTiles) & 1, abort_flag, p.status)) ||
+                !mbar_wait_warp(bar(C::kKFull + st), (score.step / kStages) & 1, abort_flag, p.status)) return false;
+            if (keys < columns) {      // values behind the last key: weights of 0 times what lies there must not become NaN
+                cross_zero_rows(base_ptr + C::kOffV + st * C::kKBytes, C::kRow, keys, columns, lane, 32);
+                fence_proxy_async();
                 __syncwarp();
-                // (the first product of an item overwrites O: the softmax warps have read it before they hand over P)
-                if (!mbar_wait_warp(bar(C::kPReady), step & 1, abort_flag, p.status)) { ok = false; break; }
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint64_t v = smem_desc_at(T::kDesc, base + C::kOffV + st * C::kKBytes);
-                    constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
-                    for (int kk = 0; kk < columns / 16; ++kk) mma_ts(tmem + kColO, tmem + 8 * kk, v + T::kStepRows * kk, kIdesc, (j || kk) ? 1u : 0u);
-                    mma_commit(bar(C::kPVDone));
-                }
-                __syncwarp();
-                // the next scores go where P lies
-                if (!mbar_wait_warp(bar(C::kPVDone), step & 1, abort_flag, p.status)) { ok = false; break; }
             }
-            ++live;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + buf * C::kQBytes), k = smem_desc_at(T::kDesc, base + C::kOffK + st * C::kKBytes);
+                const uint32_t idesc = idesc_bf16_f32(kRows, columns, false), at = tmem + score.step % kBuffers * kCrossBlock;
+#pragma unroll
+                for (int kk = 0; kk < DP / 16; ++kk) mma_ss(at, q + T::kStepK * kk, k + T::kStepK * kk, idesc, kk ? 1u : 0u);
+                mma_commit(on_step(C::kSFull, score.step));
+            }
+            __syncwarp();
+            score.advance(p);
+            return true;
+        };
+        load_ahead(0);
+        for (uint32_t i = 0; i < kBuffers && ok && score.there(p); ++i) ok = issue_scores();
+        while (ok && value.there(p)) {
+            // (the first product of an item overwrites O: the softmax warps have read it before they hand over P)
+            if (!mbar_wait_warp(on_step(C::kPReady, value.step), parity(value.step), abort_flag, p.status)) { ok = false; break; }
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t v = smem_desc_at(T::kDesc, base + C::kOffV + (value.step % kStages) * C::kKBytes);
+                constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
+                const int k_steps = (value.keys() + 15) / 16;
+                const uint32_t at = tmem + value.step % kBuffers * kCrossBlock;
+                for (int kk = 0; kk < k_steps; ++kk) mma_ts(tmem + kColO, at + 8 * kk, v + T::kStepRows * kk, kIdesc, (value.block || kk) ? 1u : 0u);
+                mma_commit(on_step(C::kPVDone, value.step));
+            }
+            __syncwarp();
+            // The product before this one is complete by now, or soon: its buffer takes the scores of the step after the next, and its stage another block.
+            if (value.step > 0 && !mbar_wait_warp(on_step(C::kPVDone, value.step - 1), parity(value.step - 1), abort_flag, p.status)) { ok = false; break; }
+            load_ahead(value.live + (value.block + 1 == value.c.blocks ? 1u : 0u));
+            if (value.step > 0 && score.there(p)) ok = issue_scores();
+            value.advance(p);
         }
-        if (!ok) {      // gave up: copies in flight land before the CTA may exit
-            for (uint32_t i = step; i < loaded; ++i) mbar_wait_warp(bar(C::kKFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
-            for (uint32_t i = live; i < q_loaded; ++i) mbar_wait_warp(bar(C::kQFull + (i & 1)), (i >> 1) & 1, abort_flag + 1, p.status);
+        if (!ok) {      // gave up: copies in flight land before the CTA may exit (waiting for those that have been waited for is harmless)
+            for (uint32_t i = value.step; i < load.step; ++i) mbar_wait_warp(bar(C::kKFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
+            for (uint32_t i = value.live; i < q_loaded; ++i) mbar_wait_warp(bar(C::kQFull + i % kTiles), (i / kTiles) & 1, abort_flag + 1, p.status);
         }
         // what has been issued is complete before the tensor memory is released
         if (elect_one()) mma_commit(bar(C::kDrain));
@@ -176,94 +212,17 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     } else {
         // ============================================ softmax and output: a row to a thread
         const int row = threadIdx.x;
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16, t_s = tmem + lanes, t_o = tmem + lanes + kColO;
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16, t_o = tmem + lanes + kColO;
         const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
         const float threshold = 8.f / p.scale_log2;
         int row_token, row_head;
         p.by_group.divmod(row, row_token, row_head);
         uint32_t step = 0;
-        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-            const Item c = decode(p, item);
-            float m = 0.f, l = 0.f;
-            for (int j = 0; j < c.blocks; ++j, ++step) {
-                if (!mbar_wait_warp(bar(C::kSFull), step & 1, abort_flag, p.status)) { ok = false; break; }
-                tc_fence_after();
-                const int keys = c.length - (c.first + j) * kCrossBlock;
-                // the scores are read twice, for their maximum and for the exponentials: 64 of them and their P do not fit the registers of a thread
-                float mx0 = kCrossLowest, mx1 = kCrossLowest;
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    uint32_t a[32];
-                    tmem_ld32(t_s + 32 * g, a);
-                    tmem_wait_ld();
-                    if (keys < kCrossBlock) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (32 * g + e >= keys) a[e] = 0xff800000u;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        mx0 = max3(mx0, __uint_as_float(a[e]), __uint_as_float(a[e + 1]));
-                        mx1 = max3(mx1, __uint_as_float(a[e + 2]), __uint_as_float(a[e + 3]));
-                    }
-                }
-                const float mx = fmaxf(mx0, mx1);
-                if (j == 0) {
-                    m = mx;
-                } else {
-                    // The reference moves, and O and l with it, only when the maximum grew by more than the threshold: the result is exact after
-                    // the division since l carries the same reference.  (The last P V is complete: these scores were issued behind it.)
-                    const bool need = mx > m + threshold;
-                    if (__any_sync(0xffffffffu, need)) {
-                        const float factor = need ? ex2_approx((m - mx) * p.scale_log2) : 1.f;
-                        if (need) { l *= factor; m = mx; }
-#pragma unroll
-                        for (int g = 0; g < DP / 8; ++g) {
-                            uint32_t o[8];
-                            tmem_ld8(t_o + 8 * g, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                            tmem_st8(t_o + 8 * g, o);
-                        }
-                    }
-                }
-                const float2 neg2 = make_float2(-m * p.scale_log2, -m * p.scale_log2);
-                float2 sum_a = make_float2(0.f, 0.f), sum_b = make_float2(0.f, 0.f);
-                // P goes where scores lie that have been read
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    uint32_t a[16], packed[8];
-                    tmem_ld16(t_s + 16 * g, a);
-                    tmem_wait_ld();
-                    if (keys < kCrossBlock) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (16 * g + e >= keys) a[e] = 0xff800000u;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), scale2, neg2);
-                        const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                        if (i & 1) sum_b = __fadd2_rn(sum_b, e); else sum_a = __fadd2_rn(sum_a, e);
-                        packed[i] = pack_bf16x2(e.x, e.y);
-                    }
-                    tmem_st8(t_s + 8 * g, packed);
-                }
-                l += (sum_a.x + sum_a.y) + (sum_b.x + sum_b.y);
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(C::kPReady));
-            }
-            if (!ok) break;
-            if (c.blocks) {
-                if (!mbar_wait_warp(bar(C::kPVDone), (step - 1) & 1, abort_flag, p.status)) { ok = false; break; }
-                tc_fence_after();
-            }
+        // Normalises and stores a row of the item; O is complete.
+        auto output = [&](const Item& c, float m, float l) {
+            const bool none = c.blocks == 0;
             const long long token = (long long)c.tile * p.tokens_per_tile + row_token;
             const bool mine = row < p.rows_per_tile && token < p.tokens;
-            const bool none = c.blocks == 0;
             const float inverse = none || (p.splits > 1 && l == 0.f) ? 0.f : 1.f / l;      // (a run of keys that all weigh nothing adds nothing)
             const float lse = none ? -INFINITY : m * p.inv_sqrt_d + logf(l);
             const int head = c.kv * p.G + row_head;
@@ -284,7 +243,6 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 }
                 __syncwarp();
             }
-            tc_fence_before();
             if (mine && p.splits > 1) {
                 p.part_lse[at] = l == 0.f ? -INFINITY : lse;
             } else if (mine && p.lse) {
@@ -292,6 +250,88 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 p.by_pixels.divmod((int)(c.context * p.tokens + token), image, pixel);
                 p.lse[((long long)image * p.heads + head) * p.pixels + pixel] = lse;
             }
+        };
+        int pending = -1;                                 // the item whose output is still to be stored, with its reference and sum
+        float m_before = 0.f, l_before = 0.f;
+        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            const Item c = decode(p, item);
+            if (!c.blocks) { output(c, 0.f, 0.f); continue; }
+            float m = 0.f, l = 0.f;
+            for (int j = 0; j < c.blocks; ++j, ++step) {
+                if (!mbar_wait_warp(on_step(C::kSFull, step), parity(step), abort_flag, p.status)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t t_s = tmem + lanes + step % kBuffers * kCrossBlock;
+                uint32_t a[64];
+                tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(a));
+                tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(a + 32));
+                tmem_wait_ld();
+                const int keys = c.length - (c.first + j) * kCrossBlock;
+                if (keys < kCrossBlock) {
+#pragma unroll
+                    for (int e = 0; e < 64; ++e)
+                        if (e >= keys) a[e] = 0xff800000u;
+                }
+                float mx[4] = {kCrossLowest, kCrossLowest, kCrossLowest, kCrossLowest};
+#pragma unroll
+                for (int e = 0; e < 64; e += 8) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(a[e + 2 * i]), __uint_as_float(a[e + 2 * i + 1]));
+                }
+                const float most = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+                if (j == 0) {
+                    m = most;
+                } else {
+                    // The reference moves, and O and l with it, only when the maximum grew by more than the threshold: the result is exact after
+                    // the division since l carries the same reference.
+                    const bool need = most > m + threshold;
+                    if (__any_sync(0xffffffffu, need)) {
+                        if (!mbar_wait_warp(on_step(C::kPVDone, step - 1), parity(step - 1), abort_flag, p.status)) { ok = false; break; }
+                        tc_fence_after();
+                        const float factor = need ? ex2_approx((m - most) * p.scale_log2) : 1.f;
+                        if (need) { l *= factor; m = most; }
+#pragma unroll
+                        for (int g = 0; g < DP / 8; ++g) {
+                            uint32_t o[8];
+                            tmem_ld8(t_o + 8 * g, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                            tmem_st8(t_o + 8 * g, o);
+                        }
+                    }
+                }
+                const float2 neg2 = make_float2(-m * p.scale_log2, -m * p.scale_log2);
+                float2 sum_a = make_float2(0.f, 0.f), sum_b = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    if (16 * g >= keys) break;            // (the product takes the keys there are, rounded up to 16)
+                    uint32_t packed[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(a[16 * g + 2 * i]), __uint_as_float(a[16 * g + 2 * i + 1])), scale2, neg2);
+                        const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                        if (i & 1) sum_b = __fadd2_rn(sum_b, e); else sum_a = __fadd2_rn(sum_a, e);
+                        packed[i] = pack_bf16x2(e.x, e.y);
+                    }
+                    tmem_st8(t_s + 8 * g, packed);
+                }
+                l += (sum_a.x + sum_a.y) + (sum_b.x + sum_b.y);
+                tmem_wait_st();
+                if (j == 0 && pending >= 0) {
+                    if (!mbar_wait_warp(on_step(C::kPVDone, step - 1), parity(step - 1), abort_flag, p.status)) { ok = false; break; }
+                    tc_fence_after();
+                    output(decode(p, pending), m_before, l_before);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(on_step(C::kPReady, step));
+            }
+            pending = item;
+            m_before = m; l_before = l;
+        }
+        if (ok && pending >= 0 && mbar_wait_warp(on_step(C::kPVDone, step - 1), parity(step - 1), abort_flag, p.status)) {
+            tc_fence_after();
+            output(decode(p, pending), m_before, l_before);
         }
     }
     // ================================================================================ common tail
@@ -385,7 +425,7 @@ cudaError_t launch_fwd(const CrossProblem& p, const CrossPlan& plan, float* part
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)p.d); a.inv_sqrt_d = 1.f / sqrtf((float)p.d);
     a.by_tiles = make_fast_div(plan.tiles); a.by_splits = make_fast_div(plan.splits); a.by_kv = make_fast_div(p.kv_heads);
     a.by_pixels = make_fast_div((int)p.pixels); a.by_group = make_fast_div(plan.G); a.pixels = (int)p.pixels;
-    const int slots = kCrossSms * Cfg<DP>::kBlocksPerSm, grid = a.items < slots ? a.items : slots;
+    const int slots = kCrossSms * kBlocksPerSm, grid = a.items < slots ? a.items : slots;
     ProfileScope scope(RIB_KERNEL_CROSS_FWD, stream);
     rib_cross_fwd_kernel<DP><<<grid, kThreads, Cfg<DP>::kSmem, stream>>>(tm_q, tm_k, tm_v, a);
     return cudaGetLastError();
@@ -445,11 +485,15 @@ CrossPlan cross_plan(const CrossProblem& p)
     c.blocks = (p.L + kCrossBlock - 1) / kCrossBlock;
     c.rows = p.tokens * c.G;
     // Fewer items than CTAs that the card holds: the key blocks are dealt out to several, whose results are joined.
-    const long long items = (long long)c.groups * c.tiles, slots = (long long)kCrossSms * (p.d <= 32 ? 4 : 3);
-    long long splits = items >= slots ? 1 : slots / items;
-    if (splits > c.blocks) splits = c.blocks;
-    c.blocks_per_split = (int)((c.blocks + splits - 1) / splits);
-    c.splits = (c.blocks + c.blocks_per_split - 1) / c.blocks_per_split;
+    auto split = [&](long long items, long long slots, int* splits, int* per) {
+        long long n = items >= slots ? 1 : slots / items;
+        if (n > c.blocks) n = c.blocks;
+        *per = (int)((c.blocks + n - 1) / n);
+        *splits = (c.blocks + *per - 1) / *per;
+    };
+    split((long long)c.groups * c.tiles, (long long)kCrossSms * kBlocksPerSm, &c.splits, &c.blocks_per_split);
+    c.dq_tiles = (c.row_tiles + 1) / 2;
+    split((long long)c.groups * c.dq_tiles, kCrossSms, &c.dq_splits, &c.dq_blocks_per_split);
     // dK and dV: a CTA to an SM; runs of row tiles such that the last round of CTAs is not a mostly empty one.  In us: 0.3 a tile, 3 for what a CTA begins and
     // ends with, and the way of the partial sums to memory and back.
     c.key_tiles = (p.L + 127) / 128;

@@ -157,3 +157,12 @@ def test_results_are_the_same_from_run_to_run():
     first, second = run_both(q, k, v, dout), run_both(q, k, v, dout)
     for a, b in zip((*first[:2], *first[2]), (*second[:2], *second[2])):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("L", [1, 16, 64, 77, 130])
+@pytest.mark.parametrize("heads,kv,d", [(6, 6, 32), (6, 3, 64), (3, 1, 20)])
+def test_many_tiles_for_each_block_of_the_grid(L, heads, kv, d):
+    """Items follow one another without a pause, some of them without keys."""
+    q, k, v, dout = inputs(6, 64, 50, heads, kv, d, L, seed=L)
+    check_all(q, k, v, dout)
+    check_all(q, k, v, dout, torch.tensor([L, 0, (L + 1) // 2, 1, 0, L], dtype=torch.int32, device="cuda"))
