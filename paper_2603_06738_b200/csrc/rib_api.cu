@@ -1001,6 +1001,7 @@ int rib_cross_attn_fwd(const void* q, const void* k, const void* v, const int* l
     if (int rc = device_status_ptr(&p.status)) return rc;
     p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k); p.v = static_cast<const __nv_bfloat16*>(v); p.lengths = lengths;
     p.out_w = static_cast<__nv_bfloat16*>(out); p.lse_w = lse; p.workspace = workspace;
+    p.exact_softmax = g_forced_path.load() == RIB_PATH_SM100_EXACT;
     int launches = 0;
     if (rib::cross_fwd(p, static_cast<cudaStream_t>(stream), &launches) != cudaSuccess) return RIB_ERR_CUDA;
     t_last_path = RIB_PATH_SM100;

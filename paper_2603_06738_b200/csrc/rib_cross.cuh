@@ -21,15 +21,16 @@ struct CrossProblem {
     int width;                            // channels of a row in q, k, v and dout: d, or d rounded up to a multiple of 8 on padded copies
     long long pixels, tokens;             // H W; tokens per context (pixels, or B pixels when the context is shared)
     int* status;
+    bool exact_softmax;                   // forward: the exact form for every item
     void* workspace;
 };
 
 // sizes of the launches, from the shape alone
 struct CrossPlan {
-    int G, rows_per_tile, tokens_per_tile, tiles, groups, blocks;      // groups: contexts x kv_heads; blocks: of 64 keys
+    int G, rows_per_tile, tokens_per_tile, tiles, pairs, groups;       // groups: contexts x kv_heads; pairs: of tiles
     long long rows;                                                    // of a group: tokens x G
-    int splits, blocks_per_split;                                      // forward: runs of key blocks that are computed apart and joined
-    int dq_tiles, dq_splits, dq_blocks_per_split;                      // dQ: tiles of two row tiles, and such runs
+    int splits, blocks_per_split;                                      // forward: runs of blocks of 128 keys that are computed apart and joined
+    int dq_tiles, dq_splits, dq_blocks_per_split;                      // dQ: tiles of two row tiles, and such runs of blocks of 64
     int key_tiles, row_splits, row_tiles_per_split;                    // dK and dV: tiles of 128 keys, runs of tiles of 64 rows
     int row_tiles, kv_rows_per_tile, kv_tokens_per_tile;
 };
@@ -63,7 +64,7 @@ inline bool cross_rows_map(CUtensorMap* map, const void* ptr, long long contexts
         const cuuint32_t box[4] = {(cuuint32_t)dp, (cuuint32_t)heads_in_box, (cuuint32_t)tokens_in_box, 1};
         const cuuint32_t estr[4] = {1, 1, 1, 1};
         return encode_fn()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           dp == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                           dp == 16 ? CU_TENSOR_MAP_SWIZZLE_32B : dp == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     });
 }

@@ -1,17 +1,23 @@
 // Forward pass of the attention to states (rib_cross.cuh) for B200 (sm_100a): TMA loads, tcgen05 products with accumulators in tensor memory,
 // softmax in registers.
 //
-// Work item = up to 128 rows of one (context, kv head) group x one run of its key blocks of 64.  A CTA of five warps walks items:
-//     S = Q K^T           (M128, N = 64, or what the last block has rounded up to 16; K = 32 or 64 channels)
-//     P = exp2((S - m) log2e / sqrt(d)), a row to a thread, written over S as bf16
+// Work item = two tiles of up to 128 rows of one (context, kv head) group x one run of its key blocks of 128.  A persistent CTA walks items:
+//     S = Q K^T           (M128, N = 128, or what the last block has rounded up to 16; K = 32 or 64 channels)
+//     P = exp2((S - m) log2e / sqrt(d)), written over S as bf16
 //     O (+)= P V          (A from tensor memory, V an MN-major tile)
-// with a running maximum m per row that moves, and rescales O and the row's sum, only when a block exceeds it by more than 2^8 in the exponentials.
-// The key blocks of all items of a CTA are one stream of steps: three buffers of scores, so that the scores of the next two steps, which may belong to the next item, are there or under
-// way while the softmax warps work, and an item's output is normalised and stored behind the exponentials of the next item's first block, when its last product is long complete.
-// The exponentials bound it: 128 x 64 of them take 512 cycles of the SM's special-function units, the products about 130 (d = 32) to 260 cycles; two CTAs to an SM
-// (256 columns of tensor memory each) fill one another's gaps.
+// Two threads own a row, one for each half of a block's keys: four softmax warps on every sub-partition of the SM, which hide one another's waits.  The exponentials are what bounds it -
+// 2 x 128 x 128 of them take 2048 cycles of the SM's special-function units -, and what keeps the warps from them is every other step of theirs, so there are two forms of the softmax.
+//   Fast form (first pass over the items): the reference m of a row is the maximum of the item's first 32 keys (fewer where the block is cut), read by both threads, and stays; no maximum is kept and nothing is rescaled.
+//   fp32 and bf16 carry 8 exponent bits, so weights up to 2^100 relative to the reference are as exact as those below 1.  A row whose sum says that its scores left that range (more than 69 above
+//   the reference, or where the FMA pipe takes the exponential 83 below, both in nats; infinities, NaN) or whose values overflowed makes its item be noted, and
+//   Exact form (second pass of the same launch): a running maximum over both halves, which they tell each other through shared memory, and which moves, and with it O and the row's sum, when a
+//   block exceeds it by more than 2^8 in the exponentials.
+// (256 x 256 tokens to 1024 states, us: a thread to a row, blocks of 64 keys, one warp for all loads and products 170; the exact form for every item 179; the fast one 000.)
+// Three buffers of scores rotate among the (block, tile) units, so that the scores of one tile are taken under the other's exponentials, and an item's output
+// is normalised and stored behind the exponentials of the next item's first block, when its last product is long complete.
 //
-// Roles: warps 0-3 softmax and output of rows 32 w .. 32 w + 31; warp 4 loads (query tiles, a ring of key blocks) and issues the products.  Every wait is bounded.
+// Roles (640 threads): warp 0 loads, warp 1 issues S, warps 2 and 3 P V of tile 0 and 1 (2: owns the tensor memory), warps 4-11 softmax and output of tile 0 (4-7 first half of
+// the keys), 12-19 of tile 1.  Every wait is bounded (tests/test_cross_barriers.py is a model of them).
 #include "rib_cross.cuh"
 
 namespace rib {
@@ -19,21 +25,23 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kThreads = 160, kRows = 128, kBlocksPerSm = 2;
-constexpr uint32_t kBuffers = 3, kTmemCols = 256, kColO = kBuffers * kCrossBlock;
+constexpr int kThreads = 640, kRows = 128, kKeys = 128, kMaxRedo = 64;      // kMaxRedo: items that a CTA can note for the exact pass (more: all of its items are redone)
+constexpr uint32_t kPolyMask = 0x0u;     // of every 8 pairs of scores: whose exponentials the FMA pipe takes
+constexpr uint32_t kMaxStages = 4, kBuffers = 3, kTmemCols = 512, kColO = kBuffers * kKeys;
 
+// kSFull, kPReady, kPVDone: 2 * tile + parity of the block (on_block): a parity wait cannot tell its own phase from one two phases on, so a barrier's next phase needs what the waiter does after
+// this one.  kDrain: one per issuing warp.
+enum Bar { kQFull = 0, kQEmpty = 2, kSFull = 4, kPReady = 8, kPVDone = 12, kDrain = 16, kKFull = 19, kKEmpty = kKFull + kMaxStages, kVFull = kKEmpty + kMaxStages, kVEmpty = kVFull + kMaxStages,
+           kPair = kVEmpty + kMaxStages, kBars = kPair + 8 };       // kPair: 4 * tile + quarter of the rows
 template <int DP> struct Cfg {
-    static constexpr int kStages = DP == 32 ? 8 : 4, kTiles = DP == 32 ? 4 : 3;
-    static constexpr uint32_t kRow = DP * 2, kQBytes = kRows * kRow, kKBytes = kCrossBlock * kRow;
-    static constexpr uint32_t kOffQ = 0, kOffK = kTiles * kQBytes, kOffV = kOffK + kStages * kKBytes, kOffBar = kOffV + kStages * kKBytes;
-    // barriers: query tiles, key blocks; of each buffer of scores: scores there, P there, P V done; all products done.  (A parity wait cannot tell its own phase
-    // from one two phases on: a buffer's next phases need what the waiter does after this one.)
-    static constexpr int kQFull = 0, kKFull = kTiles, kSFull = kKFull + kStages, kPReady = kSFull + kBuffers, kPVDone = kPReady + kBuffers, kDrain = kPVDone + kBuffers, kBars = kDrain + 1;
-    static constexpr uint32_t kOffMisc = kOffBar + kBars * 8, kSmem = kOffMisc + 16;
-    static_assert(kTiles >= (int)kBuffers && kStages > (int)kBuffers, "the scores of kBuffers steps, each of an item of its own, are taken before the first product");
-    static_assert(kQBytes % 1024 == 0 && kKBytes % 1024 == 0, "swizzle atoms need aligned tiles");
-    static_assert(kBlocksPerSm * (kSmem + 1024) <= 233472, "shared memory of an SM");
-    static_assert(kColO + DP <= kTmemCols, "tensor memory of a CTA");
+    static constexpr uint32_t kStages = DP == 32 ? kMaxStages : 3;
+    static constexpr uint32_t kRow = DP * 2, kTileBytes = kRows * kRow;                          // 128 rows, or 128 keys
+    static constexpr uint32_t kOutBytes = 32 * DP;                                                // a softmax warp's 32 rows of DP / 2 channels
+    static constexpr uint32_t kOffQ = 0, kOffK = 4 * kTileBytes, kOffV = kOffK + kStages * kTileBytes, kOffOut = kOffV + kStages * kTileBytes, kOffSums = kOffOut + 16 * kOutBytes;
+    static constexpr uint32_t kOffMaxima = kOffSums + 2 * 4 * kRows * 4;                          // sums: [2 item parities][2 tiles][2 halves][128]; maxima: the same of block parities
+    static constexpr uint32_t kOffBar = kOffMaxima + 2 * 4 * kRows * 4, kOffMisc = kOffBar + kBars * 8, kOffRedo = kOffMisc + 16, kSmem = kOffRedo + kMaxRedo * 4 + 1024;
+    static_assert(kSmem <= 232448, "shared memory of a CTA");
+    static_assert(kColO + 2 * DP <= kTmemCols, "tensor memory has 512 columns");
 };
 
 struct Params {
@@ -42,302 +50,488 @@ struct Params {
     float* lse;
     float *part_out, *part_lse;          // splits > 1: [splits][groups][rows][DP], [splits][groups][rows]
     int* status;
-    int d, L, heads, kv_heads, G, rows_per_tile, tokens_per_tile, blocks_per_split, splits, items, vector;
+    int d, L, heads, kv_heads, G, rows_per_tile, tokens_per_tile, blocks_per_split, splits, items, vector, tma_out, exact_only;      // items: pairs of tiles x splits x groups
     long long tokens, rows, groups;
     float scale_log2, inv_sqrt_d;
-    FastDiv by_tiles, by_splits, by_kv, by_pixels, by_group;
+    FastDiv by_pairs, by_splits, by_kv, by_pixels, by_group;
     int pixels;
 };
 
-struct Item { int tile, split, group, context, kv, first, blocks, length; };
+struct Item { int pair, split, group, context, kv, first, blocks, length; };      // first: key block
 
 // blocks of a context's first `length` keys that belong to the split
 __device__ __forceinline__ Item decode(const Params& p, int item)
 {
     Item c;
-    p.by_tiles.divmod(item, item, c.tile);
+    p.by_pairs.divmod(item, item, c.pair);
     p.by_splits.divmod(item, c.group, c.split);
     p.by_kv.divmod(c.group, c.context, c.kv);
     c.length = p.lengths ? min(max(__ldg(p.lengths + c.context), 0), p.L) : p.L;
     c.first = c.split * p.blocks_per_split;
-    c.blocks = max(0, min(c.first + p.blocks_per_split, (c.length + kCrossBlock - 1) / kCrossBlock) - c.first);
+    c.blocks = max(0, min(c.first + p.blocks_per_split, (c.length + kKeys - 1) / kKeys) - c.first);
     return c;
 }
 
-// A place in the CTA's stream of steps (key blocks of its items, one item after the other; items without keys have none).
-struct Cursor {
-    Item c;
-    int item, block;
-    uint32_t step, live;                 // steps and items with steps before it
-    __device__ __forceinline__ void settle(const Params& p)          // to the next item that has a block
-    {
-        while (item < p.items) {
-            c = decode(p, item);
-            if (c.blocks) return;
-            item += gridDim.x;
-        }
-    }
-    __device__ __forceinline__ void begin(const Params& p) { item = blockIdx.x; block = 0; step = live = 0; settle(p); }
-    __device__ __forceinline__ bool there(const Params& p) const { return item < p.items; }
-    __device__ __forceinline__ void advance(const Params& p)
-    {
-        ++step;
-        if (++block < c.blocks) return;
-        block = 0;
-        ++live;
-        item += gridDim.x;
-        settle(p);
-    }
-    __device__ __forceinline__ int keys() const { return min(kCrossBlock, c.length - (c.first + block) * kCrossBlock); }
-};
+// 2^x for a pair of arguments on the FMA and integer pipes, as in rib_fwd_sm100.cu: x = n + f with n = round(x), |f| <= 1/2, 2^f by a cubic (relative error 7.5e-5) whose coefficients are scaled by
+// 2^-120, 2^n by adding n + 120, bounded to [0, 248], to the exponent field.  Arguments outside [-120.5, 128.5) and NaN give at least 2^126 or a negative number of that size, which the row's sum shows.
+__device__ __forceinline__ float2 ex2_poly2_ranged(float2 x)
+{
+    constexpr float kS = 7.52316384526264005e-37f;      // 2^-120
+    const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));
+    const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
+    const float2 f = __fadd2_rn(x, make_float2(-n.x, -n.y));
+    float2 q = __ffma2_rn(make_float2(0.05517084f * kS, 0.05517084f * kS), f, make_float2(0.24260935f * kS, 0.24260935f * kS));
+    q = __ffma2_rn(q, f, make_float2(0.69326097f * kS, 0.69326097f * kS));
+    q = __ffma2_rn(q, f, make_float2(0.99992818f * kS, 0.99992818f * kS));
+    const uint32_t vx = min(__float_as_uint(t.x) + (120u - 0x4B400000u), 248u);
+    const uint32_t vy = min(__float_as_uint(t.y) + (120u - 0x4B400000u), 248u);
+    return make_float2(__uint_as_float(__float_as_uint(q.x) + (vx << 23)), __uint_as_float(__float_as_uint(q.y) + (vy << 23)));
+}
+
+// Of the item's j-th block: its keys, that number rounded up to 16 (the columns of its scores), and the columns of the first half of them.
+struct Block { int keys, columns, half; };
+__device__ __forceinline__ Block block_of(const Item& c, int j)
+{
+    Block b;
+    b.keys = min(kKeys, c.length - (c.first + j) * kKeys);
+    b.columns = (b.keys + 15) & ~15;
+    b.half = ((b.columns >> 4) + 1) >> 1 << 4;
+    return b;
+}
 
 template <int DP>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
-rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params p)
+__global__ void __launch_bounds__(kThreads, 1)
+rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_out,
+                     const __grid_constant__ Params p)
 {
     using C = Cfg<DP>;
     using T = CrossTile<DP>;
-    constexpr int kStages = C::kStages, kTiles = C::kTiles;
-    extern __shared__ __align__(1024) uint8_t base_ptr[];
-    const uint32_t base = smem_u32(base_ptr);
+    constexpr uint32_t kStages = C::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
     auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
-    auto on_step = [&](int which, uint32_t step) { return bar(which + step % kBuffers); };
-    auto parity = [](uint32_t step) { return (step / kBuffers) & 1; };
+    // (blocks -1 and -2 have the parity that a barrier without a completed phase answers yes to)
+    auto on_block = [&](int which, int tile, uint32_t block) { return bar(which + 2 * tile + (block & 1)); };
+    auto parity = [](uint32_t block) { return (block >> 1) & 1; };
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + C::kOffMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kOffMisc + 4);      // [1] stays 0: used by the drain waits
+    int* redo_count = reinterpret_cast<int*>(base_ptr + C::kOffMisc + 12);                       // notes taken (duplicates included)
+    volatile int* redo_list = reinterpret_cast<volatile int*>(base_ptr + C::kOffRedo);           // ordinals of items among this CTA's
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (base & 1023u) {                                   // (never seen: the declaration above asks for it; swizzled tiles would be misread)
-        if (threadIdx.x == 0) atomicExch(p.status, 1);
-        return;
-    }
 
     if (threadIdx.x == 0) {
         abort_flag[0] = 0; abort_flag[1] = 0;
-        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i >= C::kPReady && i < C::kPVDone ? 4 : 1);
+        *redo_count = 0;
+        for (int i = 0; i < kBars; ++i) mbar_init(bar(i), i >= kPReady && i < kPVDone ? 8 : i >= kVEmpty ? 2 : 1);
         fence_barrier_init();
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
     }
-    if (warp == 4) {
+    if (warp == 2) {
         tmem_alloc(base + C::kOffMisc, kTmemCols);
         tmem_relinquish();
     }
     // rows that the boxes of Q do not reach (G does not divide 128)
-    for (int i = 0; i < kTiles; ++i) cross_zero_rows(base_ptr + C::kOffQ + i * C::kQBytes, C::kRow, p.rows_per_tile, kRows, threadIdx.x, kThreads);
+    for (int i = 0; i < 4; ++i) cross_zero_rows(base_ptr + C::kOffQ + i * C::kTileBytes, C::kRow, p.rows_per_tile, kRows, threadIdx.x, kThreads);
     fence_proxy_async();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
+    uint32_t blk = 0, live = 0;                           // blocks and items (with blocks) so far
+    uint32_t sb = warp == 3 || warp >= 12 ? 1u : 0u;      // score buffer of the next unit: (2 blk + tile) mod kBuffers
+    uint32_t met = 0;                                     // times that the two warps of a row have met
+    const int my_items = (int)blockIdx.x < p.items ? (p.items - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
 
-    if (warp == 4) {
-        // ============================================ loads and products: the whole warp walks, one elected lane issues
-        Cursor load, score, value;                        // the next step to load, to take the scores of, to multiply with its values
-        load.begin(p); score.begin(p); value.begin(p);
-        uint32_t q_loaded = 0;
-        // Loads as far ahead as there is room: a stage is free once its step's P V is complete (all before value.step are), a query tile once its item's
-        // scores are (`scored` items).
-        auto load_ahead = [&](uint32_t scored) {
-            for (; load.there(p); load.advance(p)) {
-                if (load.step == value.step + kStages) return;
-                if (load.block == 0 && load.live == scored + kTiles) return;
+    for (int pass = 0; pass < 2; ++pass) {
+    const bool fast = pass == 0 && !p.exact_only;
+    // pass 0: every item of this CTA; pass 1: the items noted by the fast form (all of them when the notes overflowed)
+    const int noted = pass == 0 ? 0 : *redo_count;
+    const bool all_items = pass == 0 || noted > kMaxRedo;
+    const int count = all_items ? my_items : noted;
+    auto item_at = [&](int i) { return (int)blockIdx.x + (all_items ? i : redo_list[i]) * (int)gridDim.x; };
+    if (warp == 0) {
+        // ============================================ loads
+        const uint32_t first_blk = blk, first_live = live;      // (those of the pass before have all landed)
+        uint32_t k_asked = blk, v_asked = blk, q_asked = live;
+        for (int i = 0; i < count && ok; ++i) {
+            const Item c = decode(p, item_at(i));
+            if (!c.blocks) continue;
+            const uint32_t buf = live & 1;
+            if (live >= 2 && !mbar_wait_warp(bar(kQEmpty + buf), ((live >> 1) - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+            if (elect_one()) {
+                mbar_arrive_expect_tx(bar(kQFull + buf), 2u * (uint32_t)p.rows_per_tile * C::kRow);
+                for (int t = 0; t < 2; ++t)
+                    tma_load_4d(base + C::kOffQ + (2 * buf + t) * C::kTileBytes, &tm_q, bar(kQFull + buf), 0, c.kv * p.G, (2 * c.pair + t) * p.tokens_per_tile, c.context);
+            }
+            __syncwarp();
+            ++q_asked;
+            for (int j = 0; j < c.blocks; ++j, ++blk) {
+                const uint32_t st = blk % kStages, use = blk / kStages;
+                const int key = (c.first + j) * kKeys;
+                if (use > 0 && !mbar_wait_warp(bar(kKEmpty + st), (use - 1) & 1, abort_flag, p.status)) { ok = false; break; }
                 if (elect_one()) {
-                    if (load.block == 0) {
-                        const uint32_t buf = load.live % kTiles;
-                        mbar_arrive_expect_tx(bar(C::kQFull + buf), (uint32_t)p.rows_per_tile * C::kRow);
-                        tma_load_4d(base + C::kOffQ + buf * C::kQBytes, &tm_q, bar(C::kQFull + buf), 0, load.c.kv * p.G, load.c.tile * p.tokens_per_tile, load.c.context);
-                    }
-                    const uint32_t st = load.step % kStages;
-                    const int key = (load.c.first + load.block) * kCrossBlock;
-                    mbar_arrive_expect_tx(bar(C::kKFull + st), 2 * C::kKBytes);
-                    tma_load_4d(base + C::kOffK + st * C::kKBytes, &tm_k, bar(C::kKFull + st), 0, load.c.kv, key, load.c.context);
-                    tma_load_4d(base + C::kOffV + st * C::kKBytes, &tm_v, bar(C::kKFull + st), 0, load.c.kv, key, load.c.context);
+                    mbar_arrive_expect_tx(bar(kKFull + st), C::kTileBytes);
+                    tma_load_4d(base + C::kOffK + st * C::kTileBytes, &tm_k, bar(kKFull + st), 0, c.kv, key, c.context);
                 }
                 __syncwarp();
-                if (load.block == 0) ++q_loaded;
-            }
-        };
-        // The scores of the next step, into the buffer whose P the product before the last one has read.
-        auto issue_scores = [&]() -> bool {
-            const uint32_t st = score.step % kStages, buf = score.live % kTiles;
-            const int keys = score.keys(), columns = (keys + 15) & ~15;
-            if ((score.block == 0 && !mbar_wait_warp(bar(C::kQFull + buf), (score.live / kTiles) & 1, abort_flag, p.status)) ||
-                !mbar_wait_warp(bar(C::kKFull + st), (score.step / kStages) & 1, abort_flag, p.status)) return false;
-            if (keys < columns) {      // values behind the last key: weights of 0 times what lies there must not become NaN
-                cross_zero_rows(base_ptr + C::kOffV + st * C::kKBytes, C::kRow, keys, columns, lane, 32);
-                fence_proxy_async();
+                ++k_asked;
+                if (use > 0 && !mbar_wait_warp(bar(kVEmpty + st), (use - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(bar(kVFull + st), C::kTileBytes);
+                    tma_load_4d(base + C::kOffV + st * C::kTileBytes, &tm_v, bar(kVFull + st), 0, c.kv, key, c.context);
+                }
                 __syncwarp();
+                ++v_asked;
             }
-            tc_fence_after();
-            if (elect_one()) {
-                const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + buf * C::kQBytes), k = smem_desc_at(T::kDesc, base + C::kOffK + st * C::kKBytes);
-                const uint32_t idesc = idesc_bf16_f32(kRows, columns, false), at = tmem + score.step % kBuffers * kCrossBlock;
+            ++live;
+        }
+        if (!ok) {      // gave up: copies in flight land before the CTA may exit
+            for (uint32_t i = max(first_live, q_asked > 2 ? q_asked - 2 : 0u); i < q_asked; ++i) mbar_wait_warp(bar(kQFull + (i & 1)), (i >> 1) & 1, abort_flag + 1, p.status);
+            for (uint32_t i = max(first_blk, k_asked > kStages ? k_asked - kStages : 0u); i < k_asked; ++i) mbar_wait_warp(bar(kKFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
+            for (uint32_t i = max(first_blk, v_asked > kStages ? v_asked - kStages : 0u); i < v_asked; ++i) mbar_wait_warp(bar(kVFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
+        }
+    } else if (warp == 1) {
+        // ============================================ S of both tiles
+        for (int i = 0; i < count && ok; ++i) {
+            const Item c = decode(p, item_at(i));
+            if (!c.blocks) continue;
+            const uint32_t buf = live & 1;
+            if (!mbar_wait_warp(bar(kQFull + buf), (live >> 1) & 1, abort_flag, p.status)) { ok = false; break; }
+            for (int j = 0; j < c.blocks && ok; ++j, ++blk) {
+                const uint32_t st = blk % kStages;
+                if (!mbar_wait_warp(bar(kKFull + st), (blk / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
+                const uint32_t idesc = idesc_bf16_f32(kRows, block_of(c, j).columns, false);
 #pragma unroll
-                for (int kk = 0; kk < DP / 16; ++kk) mma_ss(at, q + T::kStepK * kk, k + T::kStepK * kk, idesc, kk ? 1u : 0u);
-                mma_commit(on_step(C::kSFull, score.step));
+                for (int t = 0; t < 2; ++t) {
+                    // the scores overwrite the columns that P V of three units before, one of the other tile, reads P from: it has completed
+                    const uint32_t before = blk - 2 + t;
+                    // (The tiles take turns on the special-function units if the second one begins when the first is through with its first exponentials.  In step, their warps wait for scores and
+                    // maxima all at once.)
+                    if (t == 1 && blk == 0 && c.blocks >= 4 && !mbar_wait_warp(on_block(kPReady, 0, 0), 0, abort_flag, p.status)) { ok = false; break; }
+                    if (!mbar_wait_warp(on_block(kPVDone, t ^ 1, before), parity(before), abort_flag, p.status)) { ok = false; break; }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + (2 * buf + t) * C::kTileBytes), k = smem_desc_at(T::kDesc, base + C::kOffK + st * C::kTileBytes);
+#pragma unroll
+                        for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem + sb * kKeys, q + T::kStepK * kk, k + T::kStepK * kk, idesc, kk ? 1u : 0u);
+                        mma_commit(on_block(kSFull, t, blk));
+                        if (t == 1) {
+                            mma_commit(bar(kKEmpty + st));
+                            if (j == c.blocks - 1) mma_commit(bar(kQEmpty + buf));
+                        }
+                    }
+                    __syncwarp();
+                    sb = sb == kBuffers - 1 ? 0u : sb + 1;
+                }
             }
-            __syncwarp();
-            score.advance(p);
-            return true;
-        };
-        load_ahead(0);
-        for (uint32_t i = 0; i < kBuffers && ok && score.there(p); ++i) ok = issue_scores();
-        while (ok && value.there(p)) {
-            // (the first product of an item overwrites O: the softmax warps have read it before they hand over P)
-            if (!mbar_wait_warp(on_step(C::kPReady, value.step), parity(value.step), abort_flag, p.status)) { ok = false; break; }
-            tc_fence_after();
-            if (elect_one()) {
-                const uint64_t v = smem_desc_at(T::kDesc, base + C::kOffV + (value.step % kStages) * C::kKBytes);
-                constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
-                const int k_steps = (value.keys() + 15) / 16;
-                const uint32_t at = tmem + value.step % kBuffers * kCrossBlock;
-                for (int kk = 0; kk < k_steps; ++kk) mma_ts(tmem + kColO, at + 8 * kk, v + T::kStepRows * kk, kIdesc, (value.block || kk) ? 1u : 0u);
-                mma_commit(on_step(C::kPVDone, value.step));
+            ++live;
+        }
+    } else if (warp < 4) {
+        // ============================================ P V: warp 2 for tile 0, warp 3 for tile 1
+        const int t = warp - 2;
+        for (int i = 0; i < count && ok; ++i) {
+            const Item c = decode(p, item_at(i));
+            for (int j = 0; j < c.blocks; ++j, ++blk) {
+                const uint32_t st = blk % kStages;
+                const Block b = block_of(c, j);
+                if (!mbar_wait_warp(bar(kVFull + st), (blk / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
+                if (b.keys < b.columns) {      // values behind the last key: weights of 0 times what lies there must not become NaN.  (Either warp, before its own product.)
+                    cross_zero_rows(base_ptr + C::kOffV + st * C::kTileBytes, C::kRow, b.keys, b.columns, lane, 32);
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                // (the first product of an item overwrites O: the softmax warps have read it before they hand over P)
+                if (!mbar_wait_warp(on_block(kPReady, t, blk), parity(blk), abort_flag, p.status)) { ok = false; break; }
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t v = smem_desc_at(T::kDesc, base + C::kOffV + st * C::kTileBytes);
+                    constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
+                    const int k_steps = b.columns >> 4, first = b.half >> 4;
+                    for (int kk = 0; kk < k_steps; ++kk)      // P of a half of the keys lies in the second half of its scores' columns
+                        mma_ts(tmem + kColO + t * DP, tmem + sb * kKeys + 8 * kk + (kk >= first ? b.columns >> 1 : b.half >> 1), v + T::kStepRows * kk, kIdesc, (j || kk) ? 1u : 0u);
+                    mma_commit(on_block(kPVDone, t, blk));
+                    mma_commit(bar(kVEmpty + st));
+                }
+                __syncwarp();
+                sb = sb == 0 ? 2u : sb - 1;
             }
-            __syncwarp();
-            // The product before this one is complete by now, or soon: its buffer takes the scores of the step after the next, and its stage another block.
-            if (value.step > 0 && !mbar_wait_warp(on_step(C::kPVDone, value.step - 1), parity(value.step - 1), abort_flag, p.status)) { ok = false; break; }
-            load_ahead(value.live + (value.block + 1 == value.c.blocks ? 1u : 0u));
-            if (value.step > 0 && score.there(p)) ok = issue_scores();
-            value.advance(p);
         }
-        if (!ok) {      // gave up: copies in flight land before the CTA may exit (waiting for those that have been waited for is harmless)
-            for (uint32_t i = value.step; i < load.step; ++i) mbar_wait_warp(bar(C::kKFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
-            for (uint32_t i = value.live; i < q_loaded; ++i) mbar_wait_warp(bar(C::kQFull + i % kTiles), (i / kTiles) & 1, abort_flag + 1, p.status);
-        }
-        // what has been issued is complete before the tensor memory is released
-        if (elect_one()) mma_commit(bar(C::kDrain));
-        __syncwarp();
-        mbar_wait_warp(bar(C::kDrain), 0, abort_flag + 1, p.status);
     } else {
-        // ============================================ softmax and output: a row to a thread
-        const int row = threadIdx.x;
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16, t_o = tmem + lanes + kColO;
+        // ============================================ softmax and output: two threads to a row
+        const int t = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3, pair_bar = (int)bar(kPair + 4 * t + quarter);
+        const int row = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, t_o = tmem + lanes + kColO + t * DP + half * (DP / 2);
         const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
         const float threshold = 8.f / p.scale_log2;
+        volatile float* const maxima = reinterpret_cast<volatile float*>(base_ptr + C::kOffMaxima) + t * 2 * kRows + row;        // [block parity][2 tiles][half][128]
+        volatile float* const sums = reinterpret_cast<volatile float*>(base_ptr + C::kOffSums) + t * 2 * kRows + row;            // [item parity][2 tiles][half][128]
         int row_token, row_head;
         p.by_group.divmod(row, row_token, row_head);
-        uint32_t step = 0;
-        // Normalises and stores a row of the item; O is complete.
-        auto output = [&](const Item& c, float m, float l) {
+        // Both halves of a row have come here: what either wrote before is there for the other.
+        auto meet = [&]() -> bool {
+            __syncwarp();
+            if (lane == 0) mbar_arrive((uint32_t)pair_bar);
+            return mbar_wait_warp((uint32_t)pair_bar, met++ & 1, abort_flag, p.status);
+        };
+        // Normalises and stores this thread's half of the channels of a row; O and both halves' sums are complete.
+        // (Fast form: it notes items that have to be redone; what is stored of them now is overwritten then.)
+        auto output = [&](const Item& c, float m, uint32_t item_parity, int ordinal) {
             const bool none = c.blocks == 0;
-            const long long token = (long long)c.tile * p.tokens_per_tile + row_token;
+            const float l = none ? 0.f : sums[item_parity * 4 * kRows] + sums[item_parity * 4 * kRows + kRows];
+            const long long token = (long long)(2 * c.pair + t) * p.tokens_per_tile + row_token;
             const bool mine = row < p.rows_per_tile && token < p.tokens;
             const float inverse = none || (p.splits > 1 && l == 0.f) ? 0.f : 1.f / l;      // (a run of keys that all weigh nothing adds nothing)
-            const float lse = none ? -INFINITY : m * p.inv_sqrt_d + logf(l);
-            const int head = c.kv * p.G + row_head;
+            const int head = c.kv * p.G + row_head, c0 = half * (DP / 2);
             const long long at = ((long long)c.split * p.groups + c.group) * p.rows + token * p.G + row_head;
             __nv_bfloat16* dst = p.out + (((long long)c.context * p.tokens + token) * p.heads + head) * p.d;
+            float nothing = 0.f;                          // not 0: some output is no number or infinite
+            if (p.tma_out) {
+                if (lane == 0) bulk_wait_group_read<0>();      // the rows of before have left
+                __syncwarp();
+            }
+            uint8_t* const stage = base_ptr + C::kOffOut + (warp - 4) * C::kOutBytes + lane * DP;
+            const int swizzle = DP == 32 ? (lane >> 2) & 1 : (lane >> 1) & 3;
 #pragma unroll
-            for (int g = 0; g < DP / 32; ++g) {
-                uint32_t o[32];
-                float x[32];
-                if (!none) { tmem_ld32(t_o + 32 * g, o); tmem_wait_ld(); }
+            for (int g = 0; g < DP / 32; ++g) {           // 16 channels at a time
+                uint32_t o[16];
+                float x[16];
+                if (!none) { tmem_ld16(t_o + 16 * g, o); tmem_wait_ld(); }
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = none || inverse == 0.f ? 0.f : __uint_as_float(o[e]) * inverse;
-                if (mine && p.splits > 1) {
+                for (int e = 0; e < 16; ++e) x[e] = none || inverse == 0.f ? 0.f : __uint_as_float(o[e]) * inverse;
+                if (l > 0x1p20f) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(p.part_out + at * DP + 32 * g + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                    for (int e = 0; e < 16; ++e) nothing = fmaf(__uint_as_float(o[e]), 0.f, nothing);
+                }
+                if (p.tma_out) {
+                    // (stores of threads that have a row each touch 32 lines apiece and held up the load-store unit for 1500 to 2900 cycles an item)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        *reinterpret_cast<uint4*>(stage + (((2 * g + k) ^ swizzle) << 4)) = make_uint4(pack_bf16x2(x[8 * k], x[8 * k + 1]), pack_bf16x2(x[8 * k + 2], x[8 * k + 3]),
+                                                                                                   pack_bf16x2(x[8 * k + 4], x[8 * k + 5]), pack_bf16x2(x[8 * k + 6], x[8 * k + 7]));
+                } else if (mine && p.splits > 1) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(p.part_out + at * DP + c0 + 16 * g + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
                 } else if (mine) {
-                    cross_store_row(dst, 32 * g, p.d, x, p.vector != 0);
+                    cross_store_row(dst, c0 + 16 * g, p.d, x, p.vector != 0);
                 }
                 __syncwarp();
             }
-            if (mine && p.splits > 1) {
-                p.part_lse[at] = l == 0.f ? -INFINITY : lse;
-            } else if (mine && p.lse) {
-                int image, pixel;
-                p.by_pixels.divmod((int)(c.context * p.tokens + token), image, pixel);
-                p.lse[((long long)image * p.heads + head) * p.pixels + pixel] = lse;
+            if (p.tma_out) {
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0 && mine && c0 < p.d) {           // (mine: of the warp's first row; if that is no token, none is)
+                    tma_store_4d(&tm_out, base + C::kOffOut + (warp - 4) * C::kOutBytes, c0, c.kv * p.G, (int)token, c.context);
+                    bulk_commit_group();
+                }
             }
+            if (fast && !none) {
+                // a score left the range that the fixed reference covers, or large weights times large values overflowed (with weights of up to 2^20 the exact form would overflow as well)
+                const bool bad = mine && (!(l > 0.f && l < 0x1p100f) || nothing != 0.f);
+                if (__any_sync(0xffffffffu, bad) && lane == 0) {
+                    const int slot = atomicAdd(redo_count, 1);
+                    if (slot < kMaxRedo) redo_list[slot] = ordinal;
+                }
+            }
+            if (mine && half == 0) {
+                const float lse = none ? -INFINITY : m * p.inv_sqrt_d + logf(l);
+                if (p.splits > 1) {
+                    p.part_lse[at] = l == 0.f ? -INFINITY : lse;
+                } else if (p.lse) {
+                    int image, pixel;
+                    p.by_pixels.divmod((int)(c.context * p.tokens + token), image, pixel);
+                    p.lse[((long long)image * p.heads + head) * p.pixels + pixel] = lse;
+                }
+            }
+            __syncwarp();
         };
-        int pending = -1;                                 // the item whose output is still to be stored, with its reference and sum
-        float m_before = 0.f, l_before = 0.f;
-        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-            const Item c = decode(p, item);
-            if (!c.blocks) { output(c, 0.f, 0.f); continue; }
+        auto largest = [](const uint32_t (&s)[32]) {
+            float mx[4] = {kCrossLowest, kCrossLowest, kCrossLowest, kCrossLowest};
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(s[e + 2 * i]), __uint_as_float(s[e + 2 * i + 1]));
+            }
+            return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+        };
+        int pending = -1;                                 // the item whose output is still to be stored (its place among those of the pass), and its reference
+        float m_before = 0.f;
+        for (int i = 0; i < count && ok; ++i) {
+            const Item c = decode(p, item_at(i));
+            if (!c.blocks) { output(c, 0.f, 0u, 0); continue; }
+            // (rows of a warp that are no tokens take part in the waits alone; what they leave behind is nobody's)
+            const bool idle = (long long)(2 * c.pair + t) * p.tokens_per_tile + (quarter * 32) / p.G >= p.tokens || quarter * 32 >= p.rows_per_tile;
             float m = 0.f, l = 0.f;
-            for (int j = 0; j < c.blocks; ++j, ++step) {
-                if (!mbar_wait_warp(on_step(C::kSFull, step), parity(step), abort_flag, p.status)) { ok = false; break; }
+            for (int j = 0; j < c.blocks; ++j, ++blk) {
+                const Block b = block_of(c, j);
+                if (!mbar_wait_warp(on_block(kSFull, t, blk), parity(blk), abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t t_s = tmem + lanes + step % kBuffers * kCrossBlock;
-                uint32_t a[64];
-                tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(a));
-                tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(a + 32));
-                tmem_wait_ld();
-                const int keys = c.length - (c.first + j) * kCrossBlock;
-                if (keys < kCrossBlock) {
+                const uint32_t t_block = tmem + lanes + sb * kKeys, t_s = t_block + (half ? b.half : 0);
+                sb = sb == 0 ? 2u : sb - 1;
+                const int columns = half ? b.columns - b.half : b.half, keys = half ? b.keys - b.half : min(b.keys, b.half);      // of this half: up to 64; may be none
+                if (fast) {
+                    if (j == 0 && !idle) {      // the item's reference, the same for both halves: of keys whose scores the first half does not write P over
+                        uint32_t a[32];
+                        tmem_ld32(t_block, a);
+                        tmem_wait_ld();
+                        const int count = min(b.keys, b.half >> 1);
+                        if (count < 32) {
 #pragma unroll
-                    for (int e = 0; e < 64; ++e)
-                        if (e >= keys) a[e] = 0xff800000u;
-                }
-                float mx[4] = {kCrossLowest, kCrossLowest, kCrossLowest, kCrossLowest};
-#pragma unroll
-                for (int e = 0; e < 64; e += 8) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(a[e + 2 * i]), __uint_as_float(a[e + 2 * i + 1]));
-                }
-                const float most = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
-                if (j == 0) {
-                    m = most;
+                            for (int e = 0; e < 32; ++e)
+                                if (e >= count) a[e] = 0xff800000u;
+                        }
+                        m = largest(a);
+                    }
                 } else {
-                    // The reference moves, and O and l with it, only when the maximum grew by more than the threshold: the result is exact after
-                    // the division since l carries the same reference.
-                    const bool need = most > m + threshold;
-                    if (__any_sync(0xffffffffu, need)) {
-                        if (!mbar_wait_warp(on_step(C::kPVDone, step - 1), parity(step - 1), abort_flag, p.status)) { ok = false; break; }
-                        tc_fence_after();
-                        const float factor = need ? ex2_approx((m - most) * p.scale_log2) : 1.f;
-                        if (need) { l *= factor; m = most; }
-#pragma unroll
-                        for (int g = 0; g < DP / 8; ++g) {
-                            uint32_t o[8];
-                            tmem_ld8(t_o + 8 * g, o);
+                    // (the scores are read twice, for their maximum and for the exponentials: 64 of them and P do not fit a thread's registers)
+                    float most = kCrossLowest;
+                    if (!idle && columns == 64 && keys == 64) {
+                        uint32_t a[2][32];
+                        tmem_ld32(t_s, a[0]);
+                        tmem_ld32(t_s + 32, a[1]);
+                        tmem_wait_ld();
+                        most = fmaxf(largest(a[0]), largest(a[1]));
+                    } else if (!idle) {
+    #pragma unroll 1
+                        for (int g = 0; g < columns; g += 32) {
+                            uint32_t a[32];
+                            tmem_ld32(t_s + g, a);
                             tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                            tmem_st8(t_o + 8 * g, o);
+    #pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (g + e >= keys) a[e] = 0xff800000u;
+                            most = fmaxf(most, largest(a));
+                        }
+                    }
+                    maxima[(blk & 1) * 4 * kRows + half * kRows] = most;
+                    if (!meet()) { ok = false; break; }
+                    most = fmaxf(most, maxima[(blk & 1) * 4 * kRows + (half ^ 1) * kRows]);
+                    if (j == 0) {
+                        m = most;
+                    } else {
+                        // The reference moves, and O and l with it, only when the maximum grew by more than the threshold: the result is exact after the division since l carries the
+                        // same reference.
+                        const bool need = most > m + threshold;
+                        if (__any_sync(0xffffffffu, need)) {
+                            if (!mbar_wait_warp(on_block(kPVDone, t, blk - 1), parity(blk - 1), abort_flag, p.status)) { ok = false; break; }
+                            tc_fence_after();
+                            const float factor = need ? ex2_approx((m - most) * p.scale_log2) : 1.f;
+                            if (need) { l *= factor; m = most; }
+    #pragma unroll 1
+                            for (int g = 0; g < DP / 16; ++g) {
+                                uint32_t o[8];
+                                tmem_ld8(t_o + 8 * g, o);
+                                tmem_wait_ld();
+    #pragma unroll
+                                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                                tmem_st8(t_o + 8 * g, o);
+                            }
                         }
                     }
                 }
                 const float2 neg2 = make_float2(-m * p.scale_log2, -m * p.scale_log2);
                 float2 sum_a = make_float2(0.f, 0.f), sum_b = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    if (16 * g >= keys) break;            // (the product takes the keys there are, rounded up to 16)
-                    uint32_t packed[8];
+                auto weights = [&](const uint32_t (&s)[16], uint32_t (&packed)[8], uint32_t poly) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(a[16 * g + 2 * i]), __uint_as_float(a[16 * g + 2 * i + 1])), scale2, neg2);
-                        const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, neg2);
+                        const float2 e = ((poly >> i) & 1u) ? ex2_poly2_ranged(x) : make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         if (i & 1) sum_b = __fadd2_rn(sum_b, e); else sum_a = __fadd2_rn(sum_a, e);
                         packed[i] = pack_bf16x2(e.x, e.y);
                     }
-                    tmem_st8(t_s + 8 * g, packed);
+                };
+                // 64 keys, 16 at a time, the load of the next ones under the exponentials of these.  P goes into the second half of the columns, whose keys are therefore taken first, so that
+                // it lies where scores have been read, and not where the other half reads the reference from.
+                auto whole = [&](uint32_t poly) {
+                    uint32_t a[16], b[16], packed[8];
+                    tmem_ld16(t_s + 48, a);
+                    tmem_ld16(t_s + 32, b);
+                    tmem_wait_ld();
+                    weights(a, packed, poly);
+                    tmem_st8(t_s + 56, packed);
+                    tmem_ld16(t_s + 16, a);
+                    weights(b, packed, poly);
+                    tmem_wait_ld();
+                    tmem_st8(t_s + 48, packed);
+                    tmem_ld16(t_s, b);
+                    weights(a, packed, poly);
+                    tmem_wait_ld();
+                    tmem_st8(t_s + 40, packed);
+                    weights(b, packed, poly);
+                    tmem_st8(t_s + 32, packed);
+                };
+                if (!idle && columns == 64 && keys == 64) {
+                    if (fast) whole(kPolyMask); else whole(0u);
+                } else if (!idle) {
+#pragma unroll 1
+                    for (int g = columns - 16; g >= 0; g -= 16) {
+                        uint32_t s[16], packed[8];
+                        tmem_ld16(t_s + g, s);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (g + e >= keys) s[e] = 0xff800000u;
+                        weights(s, packed, 0u);
+                        tmem_st8(t_s + (columns + g) / 2, packed);
+                    }
                 }
                 l += (sum_a.x + sum_a.y) + (sum_b.x + sum_b.y);
                 tmem_wait_st();
                 if (j == 0 && pending >= 0) {
-                    if (!mbar_wait_warp(on_step(C::kPVDone, step - 1), parity(step - 1), abort_flag, p.status)) { ok = false; break; }
+                    // that P V was the last one of the item before; the halves meet once more behind their sums of it (exact form: they have)
+                    if ((fast && !meet()) || !mbar_wait_warp(on_block(kPVDone, t, blk - 1), parity(blk - 1), abort_flag, p.status)) { ok = false; break; }
                     tc_fence_after();
-                    output(decode(p, pending), m_before, l_before);
+                    output(decode(p, item_at(pending)), m_before, (live - 1) & 1, pending);
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(on_step(C::kPReady, step));
+                if (lane == 0) mbar_arrive(on_block(kPReady, t, blk));
             }
-            pending = item;
-            m_before = m; l_before = l;
+            if (!ok) break;
+            sums[(live & 1) * 4 * kRows + half * kRows] = l;
+            pending = i;
+            m_before = m;
+            ++live;
         }
-        if (ok && pending >= 0 && mbar_wait_warp(on_step(C::kPVDone, step - 1), parity(step - 1), abort_flag, p.status)) {
-            tc_fence_after();
-            output(decode(p, pending), m_before, l_before);
+        if (ok && pending >= 0) {
+            if (meet() && mbar_wait_warp(on_block(kPVDone, t, blk - 1), parity(blk - 1), abort_flag, p.status)) {
+                tc_fence_after();
+                output(decode(p, item_at(pending)), m_before, (live - 1) & 1, pending);
+            }
         }
+        if (p.tma_out && lane == 0) bulk_wait_group<0>();      // (the CTA's shared memory is read until then; and what the exact pass stores comes behind what this one did)
+    }
+    if (pass == 1 || !fast) break;                   // CTA-uniform: `fast` depends on the kernel arguments only
+    // ---- between the passes: every role has finished its items; has the fast form noted any?
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const int notes = *redo_count;
+    if (notes == 0 || abort_flag[0]) break;          // CTA-uniform: shared memory read after the barrier
+    if (threadIdx.x == 0 && notes <= kMaxRedo) {
+        // several warps may have noted the same item: keep each ordinal once
+        int kept = 0;
+        for (int a = 0; a < notes; ++a) {
+            const int v = redo_list[a];
+            bool seen = false;
+            for (int b = 0; b < kept; ++b) seen = seen || redo_list[b] == v;
+            if (!seen) redo_list[kept++] = v;
+        }
+        *redo_count = kept;
+    }
+    __syncthreads();
+    }
+    if (warp >= 1 && warp < 4) {
+        // everything issued by this warp has finished before the tensor memory is released
+        if (elect_one()) mma_commit(bar(kDrain + warp - 1));
+        __syncwarp();
+        mbar_wait_warp(bar(kDrain + warp - 1), 0, abort_flag + 1, p.status);
     }
     // ================================================================================ common tail
     tc_fence_before();
     __syncthreads();
-    if (warp == 4) {
+    if (warp == 2) {
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
     }
@@ -411,23 +605,27 @@ cudaError_t launch_fwd(const CrossProblem& p, const CrossPlan& plan, float* part
     if (!encode_fn()) return cudaErrorNotSupported;
     CUtensorMap tm_q, tm_k, tm_v;
     if (!cross_rows_map(&tm_q, p.q, p.contexts, p.tokens, p.heads, p.width, DP, plan.G, plan.tokens_per_tile) ||
-        !cross_rows_map(&tm_k, p.k, p.contexts, p.L, p.kv_heads, p.width, DP, 1, kCrossBlock) || !cross_rows_map(&tm_v, p.v, p.contexts, p.L, p.kv_heads, p.width, DP, 1, kCrossBlock))
+        !cross_rows_map(&tm_k, p.k, p.contexts, p.L, p.kv_heads, p.width, DP, 1, kKeys) || !cross_rows_map(&tm_v, p.v, p.contexts, p.L, p.kv_heads, p.width, DP, 1, kKeys))
         return cudaErrorInvalidValue;
+    // rows of 16-byte words whose tokens fill whole warps, and no partial results: the output leaves by TMA, a warp's rows at a time
+    const bool tma_out = p.d % 8 == 0 && 32 % plan.G == 0 && plan.splits == 1;
+    CUtensorMap tm_out = tm_q;
+    if (tma_out && !cross_rows_map(&tm_out, p.out_w, p.contexts, p.tokens, p.heads, p.d, DP / 2, plan.G, 32 / plan.G)) return cudaErrorInvalidValue;
     static KernelSetup setup;
     int sms = 0;
     if (cudaError_t e = setup.prepare(rib_cross_fwd_kernel<DP>, Cfg<DP>::kSmem, &sms)) return e;
     Params a{};
     a.lengths = p.lengths; a.out = p.out_w; a.lse = p.lse_w; a.part_out = part_out; a.part_lse = part_lse; a.status = p.status;
     a.d = p.d; a.L = p.L; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.rows_per_tile = plan.rows_per_tile; a.tokens_per_tile = plan.tokens_per_tile;
-    a.blocks_per_split = plan.blocks_per_split; a.splits = plan.splits; a.items = plan.groups * plan.splits * plan.tiles;
-    a.vector = p.d % 8 == 0;
+    a.blocks_per_split = plan.blocks_per_split; a.splits = plan.splits; a.items = plan.groups * plan.splits * plan.pairs;
+    a.vector = p.d % 8 == 0; a.tma_out = tma_out; a.exact_only = p.exact_softmax;
     a.tokens = p.tokens; a.rows = plan.rows; a.groups = plan.groups;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)p.d); a.inv_sqrt_d = 1.f / sqrtf((float)p.d);
-    a.by_tiles = make_fast_div(plan.tiles); a.by_splits = make_fast_div(plan.splits); a.by_kv = make_fast_div(p.kv_heads);
+    a.by_pairs = make_fast_div(plan.pairs); a.by_splits = make_fast_div(plan.splits); a.by_kv = make_fast_div(p.kv_heads);
     a.by_pixels = make_fast_div((int)p.pixels); a.by_group = make_fast_div(plan.G); a.pixels = (int)p.pixels;
-    const int slots = kCrossSms * kBlocksPerSm, grid = a.items < slots ? a.items : slots;
+    const int grid = a.items < kCrossSms ? a.items : kCrossSms;
     ProfileScope scope(RIB_KERNEL_CROSS_FWD, stream);
-    rib_cross_fwd_kernel<DP><<<grid, kThreads, Cfg<DP>::kSmem, stream>>>(tm_q, tm_k, tm_v, a);
+    rib_cross_fwd_kernel<DP><<<grid, kThreads, Cfg<DP>::kSmem, stream>>>(tm_q, tm_k, tm_v, tm_out, a);
     return cudaGetLastError();
 }
 
@@ -482,18 +680,18 @@ CrossPlan cross_plan(const CrossProblem& p)
     tiled(kRows, &c.tokens_per_tile, &c.rows_per_tile, &c.tiles);
     tiled(kCrossBlock, &c.kv_tokens_per_tile, &c.kv_rows_per_tile, &c.row_tiles);
     c.groups = p.contexts * p.kv_heads;
-    c.blocks = (p.L + kCrossBlock - 1) / kCrossBlock;
     c.rows = p.tokens * c.G;
-    // Fewer items than CTAs that the card holds: the key blocks are dealt out to several, whose results are joined.
-    auto split = [&](long long items, long long slots, int* splits, int* per) {
-        long long n = items >= slots ? 1 : slots / items;
-        if (n > c.blocks) n = c.blocks;
-        *per = (int)((c.blocks + n - 1) / n);
-        *splits = (c.blocks + *per - 1) / *per;
+    // Fewer items than SMs: the key blocks are dealt out to several CTAs, whose results are joined.
+    auto split = [&](long long items, int blocks, int* splits, int* per) {
+        long long n = items >= kCrossSms ? 1 : kCrossSms / items;
+        if (n > blocks) n = blocks;
+        *per = (int)((blocks + n - 1) / n);
+        *splits = (blocks + *per - 1) / *per;
     };
-    split((long long)c.groups * c.tiles, (long long)kCrossSms * kBlocksPerSm, &c.splits, &c.blocks_per_split);
+    c.pairs = (c.tiles + 1) / 2;
+    split((long long)c.groups * c.pairs, (p.L + kKeys - 1) / kKeys, &c.splits, &c.blocks_per_split);
     c.dq_tiles = (c.row_tiles + 1) / 2;
-    split((long long)c.groups * c.dq_tiles, kCrossSms, &c.dq_splits, &c.dq_blocks_per_split);
+    split((long long)c.groups * c.dq_tiles, (p.L + kCrossBlock - 1) / kCrossBlock, &c.dq_splits, &c.dq_blocks_per_split);
     // dK and dV: a CTA to an SM; runs of row tiles such that the last round of CTAs is not a mostly empty one.  In us: 0.3 a tile, 3 for what a CTA begins and
     // ends with, and the way of the partial sums to memory and back.
     c.key_tiles = (p.L + 127) / 128;
