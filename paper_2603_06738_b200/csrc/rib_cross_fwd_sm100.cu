@@ -9,7 +9,7 @@
 // 2 x 128 x 128 of them take 2048 cycles of the SM's special-function units -, and what keeps the warps from them is every other step of theirs, so there are two forms of the softmax.
 //   Fast form (first pass over the items): the reference m of a row is the maximum of the item's first 32 keys (fewer where the block is cut), read by both threads, and stays; no maximum is kept and nothing is rescaled.
 //   fp32 and bf16 carry 8 exponent bits, so weights up to 2^100 relative to the reference are as exact as those below 1.  A row whose sum says that its scores left that range (more than 69 above
-//   the reference, or where the FMA pipe takes the exponential 83 below, both in nats; infinities, NaN) or whose values overflowed makes its item be noted, and
+//   the reference, in nats; infinities, NaN) or whose values overflowed makes its item be noted, and
 //   Exact form (second pass of the same launch): a running maximum over both halves, which they tell each other through shared memory, and which moves, and with it O and the row's sum, when a
 //   block exceeds it by more than 2^8 in the exponentials.
 // (256 x 256 tokens to 1024 states, us: a thread to a row, blocks of 64 keys, one warp for all loads and products 170; the exact form for every item 179; the fast one 000.)
@@ -26,7 +26,6 @@ namespace {
 using namespace sm100;
 
 constexpr int kThreads = 640, kRows = 128, kKeys = 128, kMaxRedo = 64;      // kMaxRedo: items that a CTA can note for the exact pass (more: all of its items are redone)
-constexpr uint32_t kPolyMask = 0x0u;     // of every 8 pairs of scores: whose exponentials the FMA pipe takes
 constexpr uint32_t kMaxStages = 4, kBuffers = 3, kTmemCols = 512, kColO = kBuffers * kKeys;
 
 // kSFull, kPReady, kPVDone: 2 * tile + parity of the block (on_block): a parity wait cannot tell its own phase from one two phases on, so a barrier's next phase needs what the waiter does after
@@ -51,7 +50,8 @@ struct Params {
     float *part_out, *part_lse;          // splits > 1: [splits][groups][rows][DP], [splits][groups][rows]
     int* status;
     int d, L, heads, kv_heads, G, rows_per_tile, tokens_per_tile, blocks_per_split, splits, items, vector, tma_out, exact_only;      // items: pairs of tiles x splits x groups
-    long long tokens, rows, groups;
+    int tokens, shared;                  // tokens of a context; shared: one context, several maps
+    long long rows, groups;
     float scale_log2, inv_sqrt_d;
     FastDiv by_pairs, by_splits, by_kv, by_pixels, by_group;
     int pixels;
@@ -72,21 +72,8 @@ __device__ __forceinline__ Item decode(const Params& p, int item)
     return c;
 }
 
-// 2^x for a pair of arguments on the FMA and integer pipes, as in rib_fwd_sm100.cu: x = n + f with n = round(x), |f| <= 1/2, 2^f by a cubic (relative error 7.5e-5) whose coefficients are scaled by
-// 2^-120, 2^n by adding n + 120, bounded to [0, 248], to the exponent field.  Arguments outside [-120.5, 128.5) and NaN give at least 2^126 or a negative number of that size, which the row's sum shows.
-__device__ __forceinline__ float2 ex2_poly2_ranged(float2 x)
-{
-    constexpr float kS = 7.52316384526264005e-37f;      // 2^-120
-    const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));
-    const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
-    const float2 f = __fadd2_rn(x, make_float2(-n.x, -n.y));
-    float2 q = __ffma2_rn(make_float2(0.05517084f * kS, 0.05517084f * kS), f, make_float2(0.24260935f * kS, 0.24260935f * kS));
-    q = __ffma2_rn(q, f, make_float2(0.69326097f * kS, 0.69326097f * kS));
-    q = __ffma2_rn(q, f, make_float2(0.99992818f * kS, 0.99992818f * kS));
-    const uint32_t vx = min(__float_as_uint(t.x) + (120u - 0x4B400000u), 248u);
-    const uint32_t vy = min(__float_as_uint(t.y) + (120u - 0x4B400000u), 248u);
-    return make_float2(__uint_as_float(__float_as_uint(q.x) + (vx << 23)), __uint_as_float(__float_as_uint(q.y) + (vy << 23)));
-}
+// Where the rows of one of an item's tiles go: their first token and its context, their first head, split x groups + group.
+struct Place { int token0, context, head0, group; };
 
 // Of the item's j-th block: its keys, that number rounded up to 16 (the columns of its scores), and the columns of the first half of them.
 struct Block { int keys, columns, half; };
@@ -277,15 +264,12 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         };
         // Normalises and stores this thread's half of the channels of a row; O and both halves' sums are complete.
         // (Fast form: it notes items that have to be redone; what is stored of them now is overwritten then.)
-        auto output = [&](const Item& c, float m, uint32_t item_parity, int ordinal) {
-            const bool none = c.blocks == 0;
-            const float l = none ? 0.f : sums[item_parity * 4 * kRows] + sums[item_parity * 4 * kRows + kRows];
-            const long long token = (long long)(2 * c.pair + t) * p.tokens_per_tile + row_token;
+        const int c0 = half * (DP / 2);
+        auto output = [&](const Place& c, float m, uint32_t item_parity, int ordinal) {
+            const float l = sums[item_parity * 4 * kRows] + sums[item_parity * 4 * kRows + kRows];
+            const int token = c.token0 + row_token;
             const bool mine = row < p.rows_per_tile && token < p.tokens;
-            const float inverse = none || (p.splits > 1 && l == 0.f) ? 0.f : 1.f / l;      // (a run of keys that all weigh nothing adds nothing)
-            const int head = c.kv * p.G + row_head, c0 = half * (DP / 2);
-            const long long at = ((long long)c.split * p.groups + c.group) * p.rows + token * p.G + row_head;
-            __nv_bfloat16* dst = p.out + (((long long)c.context * p.tokens + token) * p.heads + head) * p.d;
+            const float inverse = p.splits > 1 && l == 0.f ? 0.f : __fdividef(1.f, l);      // (a run of keys that all weigh nothing adds nothing)
             float nothing = 0.f;                          // not 0: some output is no number or infinite
             if (p.tma_out) {
                 if (lane == 0) bulk_wait_group_read<0>();      // the rows of before have left
@@ -297,9 +281,10 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             for (int g = 0; g < DP / 32; ++g) {           // 16 channels at a time
                 uint32_t o[16];
                 float x[16];
-                if (!none) { tmem_ld16(t_o + 16 * g, o); tmem_wait_ld(); }
+                tmem_ld16(t_o + 16 * g, o);
+                tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = none || inverse == 0.f ? 0.f : __uint_as_float(o[e]) * inverse;
+                for (int e = 0; e < 16; ++e) x[e] = inverse == 0.f ? 0.f : __uint_as_float(o[e]) * inverse;
                 if (l > 0x1p20f) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) nothing = fmaf(__uint_as_float(o[e]), 0.f, nothing);
@@ -311,10 +296,11 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         *reinterpret_cast<uint4*>(stage + (((2 * g + k) ^ swizzle) << 4)) = make_uint4(pack_bf16x2(x[8 * k], x[8 * k + 1]), pack_bf16x2(x[8 * k + 2], x[8 * k + 3]),
                                                                                                    pack_bf16x2(x[8 * k + 4], x[8 * k + 5]), pack_bf16x2(x[8 * k + 6], x[8 * k + 7]));
                 } else if (mine && p.splits > 1) {
+                    float* const part = p.part_out + ((long long)c.group * p.rows + token * p.G + row_head) * DP + c0 + 16 * g;
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(p.part_out + at * DP + c0 + 16 * g + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                    for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(part + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
                 } else if (mine) {
-                    cross_store_row(dst, c0 + 16 * g, p.d, x, p.vector != 0);
+                    cross_store_row(p.out + ((long long)(c.context * p.tokens + token) * p.heads + c.head0 + row_head) * p.d, c0 + 16 * g, p.d, x, p.vector != 0);
                 }
                 __syncwarp();
             }
@@ -322,11 +308,11 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0 && mine && c0 < p.d) {           // (mine: of the warp's first row; if that is no token, none is)
-                    tma_store_4d(&tm_out, base + C::kOffOut + (warp - 4) * C::kOutBytes, c0, c.kv * p.G, (int)token, c.context);
+                    tma_store_4d(&tm_out, base + C::kOffOut + (warp - 4) * C::kOutBytes, c0, c.head0, token, c.context);
                     bulk_commit_group();
                 }
             }
-            if (fast && !none) {
+            if (fast) {
                 // a score left the range that the fixed reference covers, or large weights times large values overflowed (with weights of up to 2^20 the exact form would overflow as well)
                 const bool bad = mine && (!(l > 0.f && l < 0x1p100f) || nothing != 0.f);
                 if (__any_sync(0xffffffffu, bad) && lane == 0) {
@@ -335,16 +321,37 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 }
             }
             if (mine && half == 0) {
-                const float lse = none ? -INFINITY : m * p.inv_sqrt_d + logf(l);
+                const float lse = m * p.inv_sqrt_d + __logf(l);
                 if (p.splits > 1) {
-                    p.part_lse[at] = l == 0.f ? -INFINITY : lse;
+                    p.part_lse[(long long)c.group * p.rows + token * p.G + row_head] = l == 0.f ? -INFINITY : lse;
                 } else if (p.lse) {
-                    int image, pixel;
-                    p.by_pixels.divmod((int)(c.context * p.tokens + token), image, pixel);
-                    p.lse[((long long)image * p.heads + head) * p.pixels + pixel] = lse;
+                    int image = c.context, pixel = token;
+                    if (p.shared) p.by_pixels.divmod(token, image, pixel);
+                    p.lse[(long long)(image * p.heads + c.head0 + row_head) * p.pixels + pixel] = lse;
                 }
             }
             __syncwarp();
+        };
+        // Rows of an item without keys.
+        auto nothing_to_attend_to = [&](const Place& c) {
+            const int token = c.token0 + row_token;
+            if (row >= p.rows_per_tile || token >= p.tokens) return;
+            if (p.splits > 1) {
+                const long long at = (long long)c.group * p.rows + token * p.G + row_head;
+                if (half == 0) p.part_lse[at] = -INFINITY;
+#pragma unroll 1
+                for (int e = c0; e < c0 + DP / 2; ++e) p.part_out[at * DP + e] = 0.f;
+                return;
+            }
+            const int head = c.head0 + row_head;
+            __nv_bfloat16* dst = p.out + ((long long)(c.context * p.tokens + token) * p.heads + head) * p.d;
+#pragma unroll 1
+            for (int e = c0; e < min(p.d, c0 + DP / 2); ++e) dst[e] = __float2bfloat16_rn(0.f);
+            if (p.lse && half == 0) {
+                int image = c.context, pixel = token;
+                if (p.shared) p.by_pixels.divmod(token, image, pixel);
+                p.lse[(long long)(image * p.heads + head) * p.pixels + pixel] = -INFINITY;
+            }
         };
         auto largest = [](const uint32_t (&s)[32]) {
             float mx[4] = {kCrossLowest, kCrossLowest, kCrossLowest, kCrossLowest};
@@ -355,15 +362,25 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             }
             return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
         };
-        int pending = -1;                                 // the item whose output is still to be stored (its place among those of the pass), and its reference
+        int pending = -1;                                 // the item whose output is still to be stored (its number among those of the pass), where its rows go, and its reference
+        Place before{};
         float m_before = 0.f;
-        for (int i = 0; i < count && ok; ++i) {
-            const Item c = decode(p, item_at(i));
-            if (!c.blocks) { output(c, 0.f, 0u, 0); continue; }
+        const int warp_token = __shfl_sync(0xffffffffu, row_token, 0);
+        // (The code of the output stands once: behind the first block of an item, and behind the last item once more without one.  Twice the code, three sites, missed the instruction
+        // cache on every fourth fetch.)
+#pragma unroll 1
+        for (int i = 0; i <= count && ok; ++i) {
+            const bool last = i == count;
+            const Item c = decode(p, item_at(last ? 0 : i));
+            const Place here{(2 * c.pair + t) * p.tokens_per_tile, c.context, c.kv * p.G, c.split * (int)p.groups + c.group};
+            if (!last && !c.blocks) { nothing_to_attend_to(here); continue; }
+            if (last && pending < 0) break;
             // (rows of a warp that are no tokens take part in the waits alone; what they leave behind is nobody's)
-            const bool idle = (long long)(2 * c.pair + t) * p.tokens_per_tile + (quarter * 32) / p.G >= p.tokens || quarter * 32 >= p.rows_per_tile;
+            const bool idle = here.token0 + warp_token >= p.tokens || quarter * 32 >= p.rows_per_tile;
             float m = 0.f, l = 0.f;
-            for (int j = 0; j < c.blocks; ++j, ++blk) {
+#pragma unroll 1
+            for (int j = 0; j < (last ? 1 : c.blocks); ++j, ++blk) {
+                if (!last) {
                 const Block b = block_of(c, j);
                 if (!mbar_wait_warp(on_block(kSFull, t, blk), parity(blk), abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
@@ -432,73 +449,69 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 }
                 const float2 neg2 = make_float2(-m * p.scale_log2, -m * p.scale_log2);
                 float2 sum_a = make_float2(0.f, 0.f), sum_b = make_float2(0.f, 0.f);
-                auto weights = [&](const uint32_t (&s)[16], uint32_t (&packed)[8], uint32_t poly) {
+                auto weights = [&](const uint32_t (&s)[16], uint32_t (&packed)[8]) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, neg2);
-                        const float2 e = ((poly >> i) & 1u) ? ex2_poly2_ranged(x) : make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                        const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         if (i & 1) sum_b = __fadd2_rn(sum_b, e); else sum_a = __fadd2_rn(sum_a, e);
                         packed[i] = pack_bf16x2(e.x, e.y);
                     }
                 };
                 // 64 keys, 16 at a time, the load of the next ones under the exponentials of these.  P goes into the second half of the columns, whose keys are therefore taken first, so that
                 // it lies where scores have been read, and not where the other half reads the reference from.
-                auto whole = [&](uint32_t poly) {
+                if (!idle && columns == 64 && keys == 64) {
                     uint32_t a[16], b[16], packed[8];
                     tmem_ld16(t_s + 48, a);
                     tmem_ld16(t_s + 32, b);
                     tmem_wait_ld();
-                    weights(a, packed, poly);
+                    weights(a, packed);
                     tmem_st8(t_s + 56, packed);
                     tmem_ld16(t_s + 16, a);
-                    weights(b, packed, poly);
+                    weights(b, packed);
                     tmem_wait_ld();
                     tmem_st8(t_s + 48, packed);
                     tmem_ld16(t_s, b);
-                    weights(a, packed, poly);
+                    weights(a, packed);
                     tmem_wait_ld();
                     tmem_st8(t_s + 40, packed);
-                    weights(b, packed, poly);
+                    weights(b, packed);
                     tmem_st8(t_s + 32, packed);
-                };
-                if (!idle && columns == 64 && keys == 64) {
-                    if (fast) whole(kPolyMask); else whole(0u);
                 } else if (!idle) {
 #pragma unroll 1
                     for (int g = columns - 16; g >= 0; g -= 16) {
                         uint32_t s[16], packed[8];
                         tmem_ld16(t_s + g, s);
                         tmem_wait_ld();
+                        if (g + 16 > keys) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (g + e >= keys) s[e] = 0xff800000u;
-                        weights(s, packed, 0u);
+                            for (int e = 0; e < 16; ++e)
+                                if (g + e >= keys) s[e] = 0xff800000u;
+                        }
+                        weights(s, packed);
                         tmem_st8(t_s + (columns + g) / 2, packed);
                     }
                 }
                 l += (sum_a.x + sum_a.y) + (sum_b.x + sum_b.y);
                 tmem_wait_st();
+                }
                 if (j == 0 && pending >= 0) {
                     // that P V was the last one of the item before; the halves meet once more behind their sums of it (exact form: they have)
-                    if ((fast && !meet()) || !mbar_wait_warp(on_block(kPVDone, t, blk - 1), parity(blk - 1), abort_flag, p.status)) { ok = false; break; }
+                    if (((fast || last) && !meet()) || !mbar_wait_warp(on_block(kPVDone, t, blk - 1), parity(blk - 1), abort_flag, p.status)) { ok = false; break; }
                     tc_fence_after();
-                    output(decode(p, item_at(pending)), m_before, (live - 1) & 1, pending);
+                    output(before, m_before, (live - 1) & 1, pending);
                 }
+                if (last) break;
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(on_block(kPReady, t, blk));
             }
-            if (!ok) break;
+            if (!ok || last) break;
             sums[(live & 1) * 4 * kRows + half * kRows] = l;
             pending = i;
+            before = here;
             m_before = m;
             ++live;
-        }
-        if (ok && pending >= 0) {
-            if (meet() && mbar_wait_warp(on_block(kPVDone, t, blk - 1), parity(blk - 1), abort_flag, p.status)) {
-                tc_fence_after();
-                output(decode(p, item_at(pending)), m_before, (live - 1) & 1, pending);
-            }
         }
         if (p.tma_out && lane == 0) bulk_wait_group<0>();      // (the CTA's shared memory is read until then; and what the exact pass stores comes behind what this one did)
     }
@@ -619,7 +632,7 @@ cudaError_t launch_fwd(const CrossProblem& p, const CrossPlan& plan, float* part
     a.d = p.d; a.L = p.L; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.rows_per_tile = plan.rows_per_tile; a.tokens_per_tile = plan.tokens_per_tile;
     a.blocks_per_split = plan.blocks_per_split; a.splits = plan.splits; a.items = plan.groups * plan.splits * plan.pairs;
     a.vector = p.d % 8 == 0; a.tma_out = tma_out; a.exact_only = p.exact_softmax;
-    a.tokens = p.tokens; a.rows = plan.rows; a.groups = plan.groups;
+    a.tokens = (int)p.tokens; a.shared = p.tokens != p.pixels; a.rows = plan.rows; a.groups = plan.groups;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)p.d); a.inv_sqrt_d = 1.f / sqrtf((float)p.d);
     a.by_pairs = make_fast_div(plan.pairs); a.by_splits = make_fast_div(plan.splits); a.by_kv = make_fast_div(p.kv_heads);
     a.by_pixels = make_fast_div((int)p.pixels); a.by_group = make_fast_div(plan.G); a.pixels = (int)p.pixels;
