@@ -5,8 +5,11 @@
 // the complex product of an entry of the map's row and one of its column, so that a table of H + W rows, with far angles taken in 64 bits, serves the map.
 // Backward, with g the gradient of y:  gz = R^T g,   dw = sum gz o xhat,   dx = (w o gz - xhat mean_c(w o gz o xhat)) / sqrt(...).
 //
-// Bound by memory: 4 bytes a channel forward, 6 backward.  A thread has a unit of 2 V channels of a token - V pairs: two runs of V channels rot / 2 apart, or one of
-// 2 V - and walks the heads with the token's cosines and sines in registers; the lanes of a head's row share its sums by shuffles.
+// Bound by memory: 4 bytes a channel forward, 6 backward.  A thread has a unit of 2 V channels - V pairs: two runs of V channels rot / 2 apart, or one of 2 V - of one row (a head of q or k)
+// and walks tokens, kUnroll of them with their loads under way at once: a warp's accesses cover neighbouring rows of a token, whole lines, and weights and their gradients stay in registers.  The lanes
+// of a row share its sums by shuffles.  A block takes tiles of tokens and puts their cosines and sines into shared memory first, once for all heads.
+// (A thread to a token that walks the heads, table entries in registers: 32 lines touched by every access and few of them in flight, 16 x 96 x 96 tokens, 6 heads of 32, forward and backward 172 us
+// against 000.)
 #include "rib_common.cuh"
 #include "rib_sm100_common.cuh"
 
@@ -16,23 +19,22 @@ namespace {
 using sm100::FastDiv;
 using sm100::make_fast_div;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kMaxTile = 64, kMaxBlocks = 4 * 148;
 
 struct RopeTensor {
     const __nv_bfloat16 *x, *g;          // x: tokens x_stride elements apart; g (backward): [tokens][heads][d]
     __nv_bfloat16* y;                    // y or dx: tokens y_stride elements apart
     const float* w;                      // [d] or [heads][d]; null: no norm
-    float* part;                         // backward: [chunks][blocks][d] sums of dw
     long long x_stride, y_stride;
-    int heads, chunks, first_chunk;      // chunks of heads_per_chunk heads: blockIdx.y
+    int heads;
 };
 struct RopeParams {
     RopeTensor t[2];
     const float2* table;                 // [H + W][rot / 2]
-    long long tokens;
-    int H, W, d, rot, pairs, interleaved, per_head, heads_per_chunk, lanes;
+    float* part;                         // backward, sums of dw: [chunks][blocks][2 or rows_per_chunk][d]
+    int tokens, tile, tiles, H, W, d, rot, pairs, interleaved, per_head, lanes, rows, rows_per_chunk, tokens_at_once;      // rows: heads of q, then of k; blockIdx.y: a chunk of them
     float eps, inverse_d;
-    FastDiv by_pixels, by_w;
+    FastDiv by_pixels, by_w, by_pairs, by_slots;
 };
 
 template <int V> struct Word;
@@ -63,82 +65,100 @@ template <int V> __device__ __forceinline__ typename Word<V>::type pack(const fl
     return word;
 }
 
-// kUnroll heads of a token have their loads under way at once.
 template <int V, bool kBackward>
-__global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const RopeParams p)
+__global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const __grid_constant__ RopeParams p)
 {
-    constexpr int kUnroll = kBackward ? 2 : 4;
+    constexpr int kUnroll = V == 8 ? (kBackward ? 2 : 4) : 4;
     using W = typename Word<V>::type;
-    const RopeTensor& t = p.t[(int)blockIdx.y >= p.t[1].first_chunk ? 1 : 0];
-    const int chunk = blockIdx.y - t.first_chunk, head0 = chunk * p.heads_per_chunk, head1 = min(head0 + p.heads_per_chunk, t.heads);
-    const int unit = threadIdx.x & (p.lanes - 1), turned = p.pairs / V;
+    extern __shared__ __align__(16) float2 turns[];              // [tile][pairs] cosines and sines; backward, at the end: [threads][2 V] sums
+    // this thread: unit of a row of the chunk, and which of the tokens that are walked at once
+    int at_once, slot;
+    p.by_slots.divmod(threadIdx.x, at_once, slot);               // slots: rows of a chunk x lanes of a row
+    const int unit = slot & (p.lanes - 1), chunk_row = slot / p.lanes, row = blockIdx.y * p.rows_per_chunk + chunk_row;
+    const bool works = at_once < p.tokens_at_once && row < p.rows;
+    const bool is_k = row >= p.t[0].heads;
+    const RopeTensor& t = p.t[is_k ? 1 : 0];
+    const int head = is_k ? row - p.t[0].heads : row;
     // channels of the unit's two runs; beyond d: none
+    const int turned = p.pairs / V;
     const bool rotates = unit < turned;
     int ca, cb;
     if (rotates) { ca = p.interleaved ? 2 * V * unit : V * unit; cb = p.interleaved ? ca + V : ca + p.rot / 2; }
     else { ca = p.rot + 2 * V * (unit - turned); cb = ca + V; }
-    const bool has_a = ca < p.d, has_b = cb < p.d;
-    const bool norm = t.w != nullptr;
-    float w[2 * V];
+    const bool has_a = works && ca < p.d, has_b = works && cb < p.d;
+    const bool norm = works && t.w != nullptr;
+    float w[2 * V], dw[2 * V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {        // (weights per head: a chunk is one head)
-        const float* src = t.w + (p.per_head ? (long long)head0 * p.d : 0);
+    for (int i = 0; i < V; ++i) {
+        const float* src = t.w + (p.per_head ? head * p.d : 0);
         w[i] = norm && has_a ? __ldg(src + ca + i) : 1.f;
         w[V + i] = norm && has_b ? __ldg(src + cb + i) : 1.f;
     }
-    float dw[2 * V];
-    if constexpr (kBackward) {
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) dw[i] = 0.f;
-    }
-    const long long step = (long long)gridDim.x * (kThreads / p.lanes);
-    const long long rounds = (p.tokens + step - 1) / step;       // the same for all lanes: they meet in shuffles
-    long long token = (long long)blockIdx.x * (kThreads / p.lanes) + threadIdx.x / p.lanes;
-    for (long long round = 0; round < rounds; ++round, token += step) {
-        const bool there = token < p.tokens;
-        float c[V], s[V];
-        if (rotates && there) {
-            int image, pixel, y, x;
-            p.by_pixels.divmod((int)token, image, pixel);
-            p.by_w.divmod(pixel, y, x);
-            const float2 *row = p.table + (long long)y * p.pairs + V * unit, *column = p.table + (long long)(p.H + x) * p.pairs + V * unit;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float2 a = __ldg(row + i), b = __ldg(column + i);
-                c[i] = a.x * b.x - a.y * b.y;
-                s[i] = a.y * b.x + a.x * b.y;
+    for (int i = 0; i < 2 * V; ++i) dw[i] = 0.f;
+    const __nv_bfloat16 *x_at = t.x + head * p.d, *g_at = kBackward ? t.g + head * p.d : nullptr;
+    __nv_bfloat16* y_at = t.y + head * p.d;
+    const long long x_stride = t.x_stride, y_stride = t.y_stride;
+    const int g_stride = t.heads * p.d;
+
+    for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+        const int token0 = tile * p.tile, here = min(p.tile, p.tokens - token0);
+        if (p.rot) {
+            __syncthreads();                                     // the tile before has been used
+            for (int e = threadIdx.x; e < here * p.pairs; e += kThreads) {
+                int token, i, image, pixel, y, x;
+                p.by_pairs.divmod(e, token, i);
+                p.by_pixels.divmod(token0 + token, image, pixel);
+                p.by_w.divmod(pixel, y, x);
+                const float2 a = __ldg(p.table + (long long)y * p.pairs + i), b = __ldg(p.table + (long long)(p.H + x) * p.pairs + i);
+                turns[e] = make_float2(a.x * b.x - a.y * b.y, a.y * b.x + a.x * b.y);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) { c[i] = 1.f; s[i] = 0.f; }
+            __syncthreads();
         }
-        for (int h0 = head0; h0 < head1; h0 += kUnroll) {
+        // (all lanes walk alike: those of a row meet in shuffles)
+        for (int k0 = 0; k0 < here; k0 += kUnroll * p.tokens_at_once) {
             W xa[kUnroll], xb[kUnroll], ga[kUnroll], gb[kUnroll];
 #pragma unroll
             for (int k = 0; k < kUnroll; ++k) {
-                const int h = h0 + k;
-                const bool here = there && h < head1;
+                const int token = k0 + k * p.tokens_at_once + at_once;
+                const bool there = token < here;
                 xa[k] = W{}; xb[k] = W{}; ga[k] = W{}; gb[k] = W{};
-                const __nv_bfloat16* src = t.x + token * t.x_stride + h * p.d;
-                if (here && has_a) xa[k] = __ldg(reinterpret_cast<const W*>(src + ca));
-                if (here && has_b) xb[k] = __ldg(reinterpret_cast<const W*>(src + cb));
+                const __nv_bfloat16* src = x_at + (token0 + token) * x_stride;
+                if (there && has_a) xa[k] = __ldg(reinterpret_cast<const W*>(src + ca));
+                if (there && has_b) xb[k] = __ldg(reinterpret_cast<const W*>(src + cb));
                 if constexpr (kBackward) {
-                    const __nv_bfloat16* grad = t.g + (token * t.heads + h) * p.d;
-                    if (here && has_a) ga[k] = __ldg(reinterpret_cast<const W*>(grad + ca));
-                    if (here && has_b) gb[k] = __ldg(reinterpret_cast<const W*>(grad + cb));
+                    const __nv_bfloat16* grad = g_at + (long long)(token0 + token) * g_stride;
+                    if (there && has_a) ga[k] = __ldg(reinterpret_cast<const W*>(grad + ca));
+                    if (there && has_b) gb[k] = __ldg(reinterpret_cast<const W*>(grad + cb));
                 }
             }
 #pragma unroll
             for (int k = 0; k < kUnroll; ++k) {
-                const int h = h0 + k;
-                if (h >= head1) break;                       // (the same for all lanes)
+                if (k0 + k * p.tokens_at_once >= here) break;    // (the same for all threads)
+                const int token = k0 + k * p.tokens_at_once + at_once;
+                const bool there = token < here;
+                float c[V], s[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) { c[i] = 1.f; s[i] = 0.f; }
+                if (rotates && there) {
+                    if constexpr (V == 8) {
+                        const float4* src = reinterpret_cast<const float4*>(turns + token * p.pairs + V * unit);
+#pragma unroll
+                        for (int i = 0; i < V / 2; ++i) {
+                            const float4 q = src[i];
+                            c[2 * i] = q.x; s[2 * i] = q.y; c[2 * i + 1] = q.z; s[2 * i + 1] = q.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) { const float2 q = turns[token * p.pairs + V * unit + i]; c[i] = q.x; s[i] = q.y; }
+                    }
+                }
                 float x[2 * V], z[2 * V];
                 unpack<V>(xa[k], x);
                 unpack<V>(xb[k], x + V);
-                float squares = 0.f;
+                float squares = 0.f, along = 0.f;
 #pragma unroll
                 for (int i = 0; i < 2 * V; ++i) squares = fmaf(x[i], x[i], squares);
-                float along = 0.f;
                 if constexpr (kBackward) {
                     float g[2 * V];
                     unpack<V>(ga[k], g);
@@ -160,14 +180,11 @@ __global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const RopePa
 #pragma unroll
                     for (int i = 0; i < 2 * V; ++i) along = fmaf(z[i] * w[i], x[i], along);
                 }
-                float inverse = 1.f;
-                if (norm) {
-                    for (int o = p.lanes / 2; o; o >>= 1) {
-                        squares += __shfl_xor_sync(0xffffffffu, squares, o);
-                        if constexpr (kBackward) along += __shfl_xor_sync(0xffffffffu, along, o);
-                    }
-                    inverse = 1.f / sqrtf(fmaf(squares, p.inverse_d, p.eps));
+                for (int o = p.lanes / 2; o; o >>= 1) {          // (rows without a norm beside rows with one: all take part)
+                    squares += __shfl_xor_sync(0xffffffffu, squares, o);
+                    if constexpr (kBackward) along += __shfl_xor_sync(0xffffffffu, along, o);
                 }
+                const float inverse = norm ? rsqrtf(fmaf(squares, p.inverse_d, p.eps)) : 1.f;
                 if constexpr (kBackward) {
                     const float mean = norm ? along * inverse * p.inverse_d : 0.f;       // mean_c(w gz xhat)
 #pragma unroll
@@ -195,7 +212,7 @@ __global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const RopePa
                     }
                 }
                 if (there) {
-                    __nv_bfloat16* dst = t.y + token * t.y_stride + h * p.d;
+                    __nv_bfloat16* dst = y_at + (token0 + token) * y_stride;
                     if (has_a) *reinterpret_cast<W*>(dst + ca) = pack<V>(z);
                     if (has_b) *reinterpret_cast<W*>(dst + cb) = pack<V>(z + V);
                 }
@@ -203,47 +220,61 @@ __global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const RopePa
         }
     }
     if constexpr (kBackward) {
-        // sums of the block: lanes of the same unit, then warps, in a fixed order
-        if (!norm) return;                                   // (the same for the block)
-        __shared__ float sums[kThreads / 32][32][2 * V];
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll
-        for (int i = 0; i < 2 * V; ++i)
-            for (int o = p.lanes; o < 32; o <<= 1) dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
-        if (lane < p.lanes) {
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) sums[warp][lane][i] = dw[i];
-        }
+        if (!p.part) return;
+        // Sums of the block in a fixed order: of a row's channel over the tokens at once, or of a tensor's over its rows of the chunk too.
+        float* const sums = reinterpret_cast<float*>(turns);
         __syncthreads();
-        if ((int)threadIdx.x < p.lanes) {
-            float* dst = t.part + ((long long)chunk * gridDim.x + blockIdx.x) * p.d;
 #pragma unroll
-            for (int i = 0; i < 2 * V; ++i) {
-                float total = 0.f;
-                for (int k = 0; k < kThreads / 32; ++k) total += sums[k][threadIdx.x][i];
-                if (i < V ? has_a : has_b) dst[(i < V ? ca : cb - V) + i] = total;
+        for (int i = 0; i < 2 * V; ++i) sums[threadIdx.x * 2 * V + i] = dw[i];
+        __syncthreads();
+        const int slots = p.rows_per_chunk * p.lanes, outputs = p.per_head ? p.rows_per_chunk : 2;
+        float* const dst = p.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * outputs * p.d;
+        for (int e = threadIdx.x; e < outputs * p.d; e += kThreads) {
+            const int which = e / p.d, ch = e - which * p.d;
+            // the unit and place of the channel
+            int u, place;
+            if (ch < p.rot) {
+                const int half = p.rot / 2;
+                if (p.interleaved) { u = ch / (2 * V); place = ch - u * 2 * V; }
+                else { const int in = ch < half ? ch : ch - half; u = in / V; place = in - u * V + (ch < half ? 0 : V); }
+            } else {
+                const int in = ch - p.rot;
+                u = turned + in / (2 * V); place = in % (2 * V);
             }
+            const int row0 = blockIdx.y * p.rows_per_chunk;
+            int first = which, end = which + 1;                  // rows of the chunk
+            if (!p.per_head) {
+                first = which ? max(0, p.t[0].heads - row0) : 0;
+                end = which ? min(p.rows_per_chunk, p.rows - row0) : min(p.rows_per_chunk, p.t[0].heads - row0);
+            }
+            float total = 0.f;
+            for (int r = first; r < end; ++r)
+                for (int k = 0; k < p.tokens_at_once; ++k) total += sums[(k * slots + r * p.lanes + u) * 2 * V + place];
+            dst[e] = total;
         }
     }
 }
 
-// dw of a tensor (or of one of its heads) from the blocks' sums: block (head, tensor), in a fixed order
-struct RopeSum { const float* part; float* dw; int sums, heads; };      // sums: of d floats each, behind one another
-__global__ void __launch_bounds__(1024) rib_qk_norm_rope_sum_kernel(RopeSum q, RopeSum k, int d)
+// dw of a tensor (or of one of its heads) from the blocks' sums: block (output of a chunk, or of all chunks), in a fixed order
+struct RopeSum { const float* part; float* dw[2]; int d, blocks, chunks, outputs, per_head, rows_per_chunk, heads, rows; };
+__global__ void __launch_bounds__(1024) rib_qk_norm_rope_sum_kernel(const RopeSum t)
 {
-    const RopeSum& t = blockIdx.y ? k : q;
-    if ((int)blockIdx.x >= t.heads || !t.dw) return;
     __shared__ float sums[1024];
     const int c = threadIdx.x & 63, run = threadIdx.x >> 6;
-    const float* src = t.part + (long long)blockIdx.x * t.sums * d;
+    // per head: blockIdx.x is a row, in one chunk; else a tensor, in all of them
+    const int chunk = t.per_head ? blockIdx.x / t.rows_per_chunk : 0, output = t.per_head ? blockIdx.x % t.rows_per_chunk : blockIdx.x, chunks = t.per_head ? 1 : t.chunks;
+    const bool is_k = t.per_head ? (int)blockIdx.x >= t.heads : blockIdx.x == 1;
+    float* const dst = t.dw[is_k ? 1 : 0];
+    cudaGridDependencySynchronize();                             // it may have overtaken the kernel before
+    if (!dst) return;
     float total = 0.f;
-    if (c < d)
-        for (int i = run; i < t.sums; i += 16) total += src[(long long)i * d + c];
+    if (c < t.d)
+        for (int i = run; i < chunks * t.blocks; i += 16) total += t.part[((long long)chunk * t.blocks + i) * t.outputs * t.d + output * t.d + c];
     sums[threadIdx.x] = total;
     __syncthreads();
-    if (threadIdx.x < 64 && c < d) {
+    if (threadIdx.x < 64 && c < t.d) {
         for (int i = 1; i < 16; ++i) total += sums[64 * i + c];
-        t.dw[(long long)blockIdx.x * d + c] = total;
+        dst[(t.per_head ? (int)blockIdx.x - (is_k ? t.heads : 0) : 0) * t.d + c] = total;
     }
 }
 
@@ -261,14 +292,33 @@ __global__ void __launch_bounds__(128) rib_rope_table_kernel(const float* __rest
     table[e] = make_float2((float)(scale * cosine), (float)(scale * sine));
 }
 
-struct Plan { int V, lanes, heads_per_chunk, chunks[2], blocks; };
+struct Plan { int V, lanes, rows, rows_per_chunk, chunks, tokens_at_once, tile, tiles, blocks; };
 
 int lanes_of(int units) { int l = 1; while (l < units) l *= 2; return l; }
+
+// rows of a chunk and blocks along the tokens, for rows of `lanes` lanes
+void rope_grid(const RopeProblem& p, int lanes, Plan* plan)
+{
+    plan->lanes = lanes;
+    plan->rows = p.heads + p.kv_heads;
+    const int most = kThreads / lanes;
+    plan->chunks = (plan->rows + most - 1) / most;
+    plan->rows_per_chunk = (plan->rows + plan->chunks - 1) / plan->chunks;
+    plan->chunks = (plan->rows + plan->rows_per_chunk - 1) / plan->rows_per_chunk;
+    plan->tokens_at_once = kThreads / (plan->rows_per_chunk * lanes);
+    // tiles such that a small map still gives every SM two of them
+    long long tile = p.tokens / (2 * 148);
+    if (tile < plan->tokens_at_once) tile = plan->tokens_at_once;
+    if (tile > kMaxTile) tile = kMaxTile;
+    plan->tile = (int)tile;
+    plan->tiles = (int)((p.tokens + tile - 1) / tile);
+    const int cap = (kMaxBlocks + plan->chunks - 1) / plan->chunks;
+    plan->blocks = plan->tiles < cap ? plan->tiles : cap;
+}
 
 // the widest words that every row allows
 Plan rope_plan(const RopeProblem& p)
 {
-    Plan plan{};
     auto fits = [&](int V) {
         if (p.d % V || p.rot % (2 * V)) return false;
         for (int i = 0; i < (p.kv_heads ? 2 : 1); ++i) {
@@ -277,24 +327,13 @@ Plan rope_plan(const RopeProblem& p)
         }
         return true;
     };
+    Plan plan{};
     plan.V = fits(8) ? 8 : fits(2) ? 2 : 1;
-    plan.lanes = lanes_of(p.rot / (2 * plan.V) + (p.d - p.rot + 2 * plan.V - 1) / (2 * plan.V));
+    rope_grid(p, lanes_of(p.rot / (2 * plan.V) + (p.d - p.rot + 2 * plan.V - 1) / (2 * plan.V)), &plan);
     return plan;
 }
 
-// Chunks of heads: all of a tensor's where the map fills the card, fewer where it does not; one where weights are per head.  (From the shape alone: the workspace's size depends on it.)
-void rope_grid(const RopeProblem& p, int lanes, Plan* plan)
-{
-    const int most = p.heads > p.kv_heads ? p.heads : p.kv_heads;
-    const long long per_block = kThreads / lanes, blocks = (p.tokens + per_block - 1) / per_block;
-    plan->heads_per_chunk = most;
-    while (plan->heads_per_chunk > 1 && blocks * (2 * (most / plan->heads_per_chunk)) < 2 * 148) plan->heads_per_chunk = (plan->heads_per_chunk + 1) / 2;
-    if (p.per_head) plan->heads_per_chunk = 1;
-    plan->chunks[0] = (p.heads + plan->heads_per_chunk - 1) / plan->heads_per_chunk;
-    plan->chunks[1] = (p.kv_heads + plan->heads_per_chunk - 1) / plan->heads_per_chunk;
-    const int chunks = plan->chunks[0] + plan->chunks[1], cap = (148 * 8 + chunks - 1) / chunks;
-    plan->blocks = (int)(blocks < cap ? blocks : cap);
-}
+size_t part_floats(const Plan& plan, int d, bool per_head) { return (size_t)plan.chunks * plan.blocks * (per_head ? plan.rows_per_chunk : 2) * d; }
 
 template <bool kBackward>
 cudaError_t launch(const RopeProblem& p, float* part, const Plan& plan, cudaStream_t stream)
@@ -302,17 +341,20 @@ cudaError_t launch(const RopeProblem& p, float* part, const Plan& plan, cudaStre
     RopeParams a{};
     for (int i = 0; i < 2; ++i) {
         const RopeRows& t = p.t[i];
-        a.t[i] = RopeTensor{t.x, t.g, t.y, t.w, part, t.x_stride, t.y_stride, i ? p.kv_heads : p.heads, plan.chunks[i], i ? plan.chunks[0] : 0};
-        if (part) part += (long long)plan.chunks[i] * plan.blocks * p.d;
+        a.t[i] = RopeTensor{t.x, t.g, t.y, t.w, t.x_stride, t.y_stride, i ? p.kv_heads : p.heads};
     }
-    a.table = reinterpret_cast<const float2*>(p.table); a.tokens = p.tokens; a.H = p.H; a.W = p.W; a.d = p.d; a.rot = p.rot; a.pairs = p.rot / 2;
-    a.interleaved = p.interleaved; a.per_head = p.per_head; a.heads_per_chunk = plan.heads_per_chunk; a.lanes = plan.lanes; a.eps = p.eps; a.inverse_d = 1.f / (float)p.d;
-    a.by_pixels = make_fast_div((int)((long long)p.H * p.W)); a.by_w = make_fast_div(p.W);
-    const dim3 grid((unsigned)plan.blocks, (unsigned)(plan.chunks[0] + plan.chunks[1]));
+    a.table = reinterpret_cast<const float2*>(p.table); a.part = part; a.tokens = (int)p.tokens; a.tile = plan.tile; a.tiles = plan.tiles; a.H = p.H; a.W = p.W; a.d = p.d; a.rot = p.rot;
+    a.pairs = p.rot / 2; a.interleaved = p.interleaved; a.per_head = p.per_head; a.lanes = plan.lanes; a.rows = plan.rows; a.rows_per_chunk = plan.rows_per_chunk;
+    a.tokens_at_once = plan.tokens_at_once; a.eps = p.eps; a.inverse_d = 1.f / (float)p.d;
+    a.by_pixels = make_fast_div((int)((long long)p.H * p.W)); a.by_w = make_fast_div(p.W); a.by_pairs = make_fast_div(p.rot ? p.rot / 2 : 1);
+    a.by_slots = make_fast_div(plan.rows_per_chunk * plan.lanes);
+    const dim3 grid((unsigned)plan.blocks, (unsigned)plan.chunks);
+    size_t smem = sizeof(float2) * plan.tile * a.pairs;                                  // up to 16 KB
+    if (kBackward && part && smem < sizeof(float) * kThreads * 2 * plan.V) smem = sizeof(float) * kThreads * 2 * plan.V;
     ProfileScope scope(kBackward ? RIB_KERNEL_QK_NORM_ROPE_BWD : RIB_KERNEL_QK_NORM_ROPE_FWD, stream);
-    if (plan.V == 8) rib_qk_norm_rope_kernel<8, kBackward><<<grid, kThreads, 0, stream>>>(a);
-    else if (plan.V == 2) rib_qk_norm_rope_kernel<2, kBackward><<<grid, kThreads, 0, stream>>>(a);
-    else rib_qk_norm_rope_kernel<1, kBackward><<<grid, kThreads, 0, stream>>>(a);
+    if (plan.V == 8) rib_qk_norm_rope_kernel<8, kBackward><<<grid, kThreads, smem, stream>>>(a);
+    else if (plan.V == 2) rib_qk_norm_rope_kernel<2, kBackward><<<grid, kThreads, smem, stream>>>(a);
+    else rib_qk_norm_rope_kernel<1, kBackward><<<grid, kThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
 
@@ -326,21 +368,16 @@ cudaError_t rope_table(const float* frequencies, int H, int W, int pairs, long l
     return cudaGetLastError();
 }
 
-cudaError_t qk_norm_rope_fwd(const RopeProblem& p, cudaStream_t stream)
-{
-    Plan plan = rope_plan(p);
-    rope_grid(p, plan.lanes, &plan);
-    return launch<false>(p, nullptr, plan, stream);
-}
+cudaError_t qk_norm_rope_fwd(const RopeProblem& p, cudaStream_t stream) { return launch<false>(p, nullptr, rope_plan(p), stream); }
 
-// room for the largest number of blocks of any alignment (the number of lanes is at most 32)
+// room for the sums of any alignment (a row has 1 to 32 lanes)
 size_t qk_norm_rope_bwd_workspace(const RopeProblem& p)
 {
     size_t most = 0;
     for (int lanes = 1; lanes <= 32; lanes *= 2) {
         Plan plan{};
         rope_grid(p, lanes, &plan);
-        const size_t bytes = sizeof(float) * (size_t)(plan.chunks[0] + plan.chunks[1]) * plan.blocks * p.d;
+        const size_t bytes = sizeof(float) * part_floats(plan, p.d, p.per_head != 0);
         most = bytes > most ? bytes : most;
     }
     return (most + 255) & ~(size_t)255;
@@ -348,22 +385,15 @@ size_t qk_norm_rope_bwd_workspace(const RopeProblem& p)
 
 cudaError_t qk_norm_rope_bwd(const RopeProblem& p, float* workspace, int* launches, cudaStream_t stream)
 {
-    Plan plan = rope_plan(p);
-    rope_grid(p, plan.lanes, &plan);
+    const Plan plan = rope_plan(p);
+    const bool weights = p.t[0].dw || p.t[1].dw;
     *launches = 1;
-    if (cudaError_t e = launch<true>(p, workspace, plan, stream)) return e;
-    if (!p.t[0].dw && !p.t[1].dw) return cudaSuccess;
-    RopeSum s[2]{};
-    const float* part = workspace;
-    for (int i = 0; i < 2; ++i) {
-        s[i] = RopeSum{part, p.t[i].dw, p.per_head ? plan.blocks : plan.chunks[i] * plan.blocks, p.per_head ? (i ? p.kv_heads : p.heads) : 1};
-        part += (long long)plan.chunks[i] * plan.blocks * p.d;
-    }
-    const int heads = s[0].heads > s[1].heads ? s[0].heads : s[1].heads;
+    if (cudaError_t e = launch<true>(p, weights ? workspace : nullptr, plan, stream)) return e;
+    if (!weights) return cudaSuccess;
+    const RopeSum s{workspace, {p.t[0].dw, p.t[1].dw}, p.d, plan.blocks, plan.chunks, p.per_head ? plan.rows_per_chunk : 2, p.per_head, plan.rows_per_chunk, p.heads, plan.rows};
     *launches = 2;
     ProfileScope scope(RIB_KERNEL_QK_NORM_ROPE_SUM, stream);
-    rib_qk_norm_rope_sum_kernel<<<dim3((unsigned)heads, 2), 1024, 0, stream>>>(s[0], s[1], p.d);
-    return cudaGetLastError();
+    return launch_overtaking(rib_qk_norm_rope_sum_kernel, p.per_head ? plan.rows : 2, 1024, 0, stream, s);
 }
 
 }  // namespace rib

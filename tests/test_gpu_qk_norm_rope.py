@@ -154,7 +154,10 @@ def test_queries_alone():
     g = normal(*q.shape).bfloat16()
     dq, dk, dqw, dkw = rib.rib_qk_norm_rope_bwd(q, None, w, None, table, g, None)
     full = rib.rib_qk_norm_rope_bwd(q, q, w, w, table, g, g)
-    assert dk is None and dkw is None and torch.equal(dq, full[0]) and torch.equal(dqw, full[2])
+    assert dk is None and dkw is None and torch.equal(dq, full[0])
+    _, want, _, bound = backward(q, w, angles(rib.rib_rope_frequencies(32), 5, 6, 0, 0), False, g)
+    check("dq_weight", dqw, want, bound)
+    check("dq_weight", full[2], want, bound)
 
 
 def test_one_weight_alone():
