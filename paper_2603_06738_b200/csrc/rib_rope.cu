@@ -5,7 +5,7 @@
 // the complex product of an entry of the map's row and one of its column, so that a table of H + W rows, with far angles taken in 64 bits, serves the map.
 // Backward, with g the gradient of y:  gz = R^T g,   dw = sum gz o xhat,   dx = (w o gz - xhat mean_c(w o gz o xhat)) / sqrt(...).
 //
-// Bound by memory: 4 bytes a channel forward, 6 backward.  A thread has a unit of 2 V channels - V pairs: two runs of V channels rot / 2 apart, or one of 2 V - of one row (a head of q or k)
+// Bound by memory: 4 bytes a channel forward, 6 backward.  A thread has a unit of 2 V channels - V pairs: two runs of V channels rot / 2 apart - of one row (a head of q or k)
 // and walks tokens, kUnroll of them with their loads under way at once: a warp's accesses cover neighbouring rows of a token, whole lines, and weights and their gradients stay in registers.  The lanes
 // of a row share its sums by shuffles.  A block takes tiles of tokens and puts their cosines and sines into shared memory first, once for all heads.
 // (A thread to a token that walks the heads, table entries in registers: 32 lines touched by every access and few of them in flight, 16 x 96 x 96 tokens, 6 heads of 32, forward and backward 172 us
@@ -19,7 +19,11 @@ namespace {
 using sm100::FastDiv;
 using sm100::make_fast_div;
 
-constexpr int kThreads = 256, kMaxTile = 64, kMaxBlocks = 4 * 148;
+#ifndef RIB_ROPE_UNROLL
+#define RIB_ROPE_UNROLL (kBackward ? 2 : 4)
+#define RIB_ROPE_BLOCKS 2
+#endif
+constexpr int kThreads = 256, kMaxTurns = 2048, kMaxBlocks = 4 * 148, kUnrollMost = 4;
 
 struct RopeTensor {
     const __nv_bfloat16 *x, *g;          // x: tokens x_stride elements apart; g (backward): [tokens][heads][d]
@@ -32,7 +36,7 @@ struct RopeParams {
     RopeTensor t[2];
     const float2* table;                 // [H + W][rot / 2]
     float* part;                         // backward, sums of dw: [chunks][blocks][2 or rows_per_chunk][d]
-    int tokens, tile, tiles, H, W, d, rot, pairs, interleaved, per_head, lanes, rows, rows_per_chunk, tokens_at_once;      // rows: heads of q, then of k; blockIdx.y: a chunk of them
+    int tokens, tile, tiles, H, W, d, rot, pairs, per_head, lanes, rows, rows_per_chunk, tokens_at_once;      // rows: heads of q, then of k; blockIdx.y: a chunk of them
     float eps, inverse_d;
     FastDiv by_pixels, by_w, by_pairs, by_slots;
 };
@@ -42,35 +46,63 @@ template <> struct Word<8> { using type = uint4; };
 template <> struct Word<2> { using type = uint32_t; };
 template <> struct Word<1> { using type = unsigned short; };
 
-template <int V> __device__ __forceinline__ void unpack(const typename Word<V>::type& word, float* x)
+// A unit's V pairs as two vectors, the pairs' first and second channels, two by two for the packed instructions (V = 1: the second of two is 0).  Halves: the two runs as they lie; interleaved: the
+// low and the high half of every word, of both runs.  (V = 1 looks the same either way.)
+template <int V> struct Pairs { float2 a[(V + 1) / 2], b[(V + 1) / 2]; };
+__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+template <int V, bool kInterleaved> __device__ __forceinline__ Pairs<V> unpack(const typename Word<V>::type& wa, const typename Word<V>::type& wb)
+{
+    Pairs<V> x;
+    if constexpr (V == 1) {
+        x.a[0] = make_float2(low(wa), 0.f);
+        x.b[0] = make_float2(low(wb), 0.f);
+    } else {
+        const uint32_t *p = reinterpret_cast<const uint32_t*>(&wa), *q = reinterpret_cast<const uint32_t*>(&wb);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            if constexpr (kInterleaved) {
+                const uint32_t u = 2 * i < V / 2 ? p[(2 * i) % (V / 2)] : q[(2 * i) % (V / 2)], v = 2 * i + 1 < V / 2 ? p[(2 * i + 1) % (V / 2)] : q[(2 * i + 1) % (V / 2)];
+                x.a[i] = make_float2(low(u), low(v));
+                x.b[i] = make_float2(high(u), high(v));
+            } else {
+                x.a[i] = make_float2(low(p[i]), high(p[i]));
+                x.b[i] = make_float2(low(q[i]), high(q[i]));
+            }
+        }
+    }
+    return x;
+}
+template <int V, bool kInterleaved> __device__ __forceinline__ void pack(const Pairs<V>& x, typename Word<V>::type& wa, typename Word<V>::type& wb)
 {
     if constexpr (V == 1) {
-        x[0] = __uint_as_float((uint32_t)word << 16);
+        wa = __bfloat16_as_ushort(__float2bfloat16_rn(x.a[0].x));
+        wb = __bfloat16_as_ushort(__float2bfloat16_rn(x.b[0].x));
     } else {
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(&word);
+        uint32_t *p = reinterpret_cast<uint32_t*>(&wa), *q = reinterpret_cast<uint32_t*>(&wb);
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        for (int i = 0; i < V / 2; ++i) {
+            if constexpr (kInterleaved) {
+                const uint32_t u = sm100::pack_bf16x2(x.a[i].x, x.b[i].x), v = sm100::pack_bf16x2(x.a[i].y, x.b[i].y);
+                if (2 * i < V / 2) p[(2 * i) % (V / 2)] = u; else q[(2 * i) % (V / 2)] = u;
+                if (2 * i + 1 < V / 2) p[(2 * i + 1) % (V / 2)] = v; else q[(2 * i + 1) % (V / 2)] = v;
+            } else {
+                p[i] = sm100::pack_bf16x2(x.a[i].x, x.a[i].y);
+                q[i] = sm100::pack_bf16x2(x.b[i].x, x.b[i].y);
+            }
+        }
     }
 }
-template <int V> __device__ __forceinline__ typename Word<V>::type pack(const float* x)
-{
-    typename Word<V>::type word;
-    if constexpr (V == 1) {
-        word = __bfloat16_as_ushort(__float2bfloat16_rn(x[0]));
-    } else {
-        uint32_t* w = reinterpret_cast<uint32_t*>(&word);
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) w[i] = sm100::pack_bf16x2(x[2 * i], x[2 * i + 1]);
-    }
-    return word;
-}
+__device__ __forceinline__ float2 twice(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 negated(float2 x) { return make_float2(-x.x, -x.y); }
 
-template <int V, bool kBackward>
-__global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const __grid_constant__ RopeParams p)
+template <int V, bool kInterleaved, bool kBackward>
+__global__ void __launch_bounds__(kThreads, V == 8 ? RIB_ROPE_BLOCKS : 4) rib_qk_norm_rope_kernel(const __grid_constant__ RopeParams p)
 {
-    constexpr int kUnroll = V == 8 ? (kBackward ? 2 : 4) : 4;
+    constexpr int kUnroll = V == 8 ? RIB_ROPE_UNROLL : 4, kTwos = (V + 1) / 2;
+    constexpr bool kOddPairs = kInterleaved && V == 1;           // a pair's channels are neighbours, and not in one word
     using W = typename Word<V>::type;
-    extern __shared__ __align__(16) float2 turns[];              // [tile][pairs] cosines and sines; backward, at the end: [threads][2 V] sums
+    extern __shared__ __align__(16) float turns[];               // [tile][pairs] cosines, then sines; backward, at the end: [threads][2 V] sums
     // this thread: unit of a row of the chunk, and which of the tokens that are walked at once
     int at_once, slot;
     p.by_slots.divmod(threadIdx.x, at_once, slot);               // slots: rows of a chunk x lanes of a row
@@ -83,27 +115,55 @@ __global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const __grid
     const int turned = p.pairs / V;
     const bool rotates = unit < turned;
     int ca, cb;
-    if (rotates) { ca = p.interleaved ? 2 * V * unit : V * unit; cb = p.interleaved ? ca + V : ca + p.rot / 2; }
+    if (rotates) { ca = kOddPairs ? 2 * unit : V * unit; cb = kOddPairs ? ca + 1 : ca + p.rot / 2; }
     else { ca = p.rot + 2 * V * (unit - turned); cb = ca + V; }
     const bool has_a = works && ca < p.d, has_b = works && cb < p.d;
     const bool norm = works && t.w != nullptr;
-    float w[2 * V], dw[2 * V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
+    // place of a pair's two channels among the unit's 2 V
+    auto place_a = [](int i) { return kInterleaved && V > 1 ? 2 * i : i; };
+    auto place_b = [](int i) { return kInterleaved && V > 1 ? 2 * i + 1 : V + i; };
+    Pairs<V> w, dw;
+    {
         const float* src = t.w + (p.per_head ? head * p.d : 0);
-        w[i] = norm && has_a ? __ldg(src + ca + i) : 1.f;
-        w[V + i] = norm && has_b ? __ldg(src + cb + i) : 1.f;
-    }
+        auto weight = [&](int place) { return norm && (place < V ? has_a : has_b) ? __ldg(src + (place < V ? ca + place : cb + place - V)) : 1.f; };
 #pragma unroll
-    for (int i = 0; i < 2 * V; ++i) dw[i] = 0.f;
+        for (int i = 0; i < kTwos; ++i) {
+            w.a[i] = make_float2(weight(place_a(2 * i)), V > 1 ? weight(place_a(2 * i + 1)) : 0.f);
+            w.b[i] = make_float2(weight(place_b(2 * i)), V > 1 ? weight(place_b(2 * i + 1)) : 0.f);
+            dw.a[i] = dw.b[i] = make_float2(0.f, 0.f);
+        }
+    }
     const __nv_bfloat16 *x_at = t.x + head * p.d, *g_at = kBackward ? t.g + head * p.d : nullptr;
     __nv_bfloat16* y_at = t.y + head * p.d;
     const long long x_stride = t.x_stride, y_stride = t.y_stride;
     const int g_stride = t.heads * p.d;
+    // of the unit's pairs: V that follow one another, or (interleaved) V / 2 of each run
+    const int second = kInterleaved && V > 1 ? p.rot / 4 : V / 2;
+    const float* const cosines = turns + (kInterleaved && V > 1 ? V / 2 * unit : V * unit);
+    const float* const sines = cosines + p.tile * p.pairs;
 
     for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
         const int token0 = tile * p.tile, here = min(p.tile, p.tokens - token0);
-        if (p.rot) {
+        W xa[kUnroll], xb[kUnroll], ga[kUnroll], gb[kUnroll];
+        auto load = [&](int k0) {
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                const int token = k0 + k * p.tokens_at_once + at_once;
+                const bool there = token < here;
+                xa[k] = W{}; xb[k] = W{}; ga[k] = W{}; gb[k] = W{};
+                const __nv_bfloat16* src = x_at + (token0 + token) * x_stride;
+                const bool needed = !kBackward || norm;          // (the gradient of a row without a norm does not depend on it)
+                if (there && needed && has_a) xa[k] = __ldg(reinterpret_cast<const W*>(src + ca));
+                if (there && needed && has_b) xb[k] = __ldg(reinterpret_cast<const W*>(src + cb));
+                if constexpr (kBackward) {
+                    const __nv_bfloat16* grad = g_at + (long long)(token0 + token) * g_stride;
+                    if (there && has_a) ga[k] = __ldg(reinterpret_cast<const W*>(grad + ca));
+                    if (there && has_b) gb[k] = __ldg(reinterpret_cast<const W*>(grad + cb));
+                }
+            }
+        };
+        load(0);
+        if (p.rot) {                                             // (under the loads)
             __syncthreads();                                     // the tile before has been used
             for (int e = threadIdx.x; e < here * p.pairs; e += kThreads) {
                 int token, i, image, pixel, y, x;
@@ -111,110 +171,82 @@ __global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const __grid
                 p.by_pixels.divmod(token0 + token, image, pixel);
                 p.by_w.divmod(pixel, y, x);
                 const float2 a = __ldg(p.table + (long long)y * p.pairs + i), b = __ldg(p.table + (long long)(p.H + x) * p.pairs + i);
-                turns[e] = make_float2(a.x * b.x - a.y * b.y, a.y * b.x + a.x * b.y);
+                turns[e] = a.x * b.x - a.y * b.y;
+                turns[p.tile * p.pairs + e] = a.y * b.x + a.x * b.y;
             }
             __syncthreads();
         }
         // (all lanes walk alike: those of a row meet in shuffles)
         for (int k0 = 0; k0 < here; k0 += kUnroll * p.tokens_at_once) {
-            W xa[kUnroll], xb[kUnroll], ga[kUnroll], gb[kUnroll];
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                const int token = k0 + k * p.tokens_at_once + at_once;
-                const bool there = token < here;
-                xa[k] = W{}; xb[k] = W{}; ga[k] = W{}; gb[k] = W{};
-                const __nv_bfloat16* src = x_at + (token0 + token) * x_stride;
-                if (there && has_a) xa[k] = __ldg(reinterpret_cast<const W*>(src + ca));
-                if (there && has_b) xb[k] = __ldg(reinterpret_cast<const W*>(src + cb));
-                if constexpr (kBackward) {
-                    const __nv_bfloat16* grad = g_at + (long long)(token0 + token) * g_stride;
-                    if (there && has_a) ga[k] = __ldg(reinterpret_cast<const W*>(grad + ca));
-                    if (there && has_b) gb[k] = __ldg(reinterpret_cast<const W*>(grad + cb));
-                }
-            }
+            if (k0) load(k0);
 #pragma unroll
             for (int k = 0; k < kUnroll; ++k) {
                 if (k0 + k * p.tokens_at_once >= here) break;    // (the same for all threads)
                 const int token = k0 + k * p.tokens_at_once + at_once;
                 const bool there = token < here;
-                float c[V], s[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) { c[i] = 1.f; s[i] = 0.f; }
+                float2 c[kTwos], s[kTwos];
                 if (rotates && there) {
+                    const float *cp = cosines + token * p.pairs, *sp = sines + token * p.pairs;
                     if constexpr (V == 8) {
-                        const float4* src = reinterpret_cast<const float4*>(turns + token * p.pairs + V * unit);
 #pragma unroll
-                        for (int i = 0; i < V / 2; ++i) {
-                            const float4 q = src[i];
-                            c[2 * i] = q.x; s[2 * i] = q.y; c[2 * i + 1] = q.z; s[2 * i + 1] = q.w;
+                        for (int i = 0; i < 2; ++i) {
+                            const float4 u = *reinterpret_cast<const float4*>(cp + i * second), v = *reinterpret_cast<const float4*>(sp + i * second);
+                            c[2 * i] = make_float2(u.x, u.y); c[2 * i + 1] = make_float2(u.z, u.w);
+                            s[2 * i] = make_float2(v.x, v.y); s[2 * i + 1] = make_float2(v.z, v.w);
                         }
                     } else {
-#pragma unroll
-                        for (int i = 0; i < V; ++i) { const float2 q = turns[token * p.pairs + V * unit + i]; c[i] = q.x; s[i] = q.y; }
-                    }
-                }
-                float x[2 * V], z[2 * V];
-                unpack<V>(xa[k], x);
-                unpack<V>(xb[k], x + V);
-                float squares = 0.f, along = 0.f;
-#pragma unroll
-                for (int i = 0; i < 2 * V; ++i) squares = fmaf(x[i], x[i], squares);
-                if constexpr (kBackward) {
-                    float g[2 * V];
-                    unpack<V>(ga[k], g);
-                    unpack<V>(gb[k], g + V);
-                    // back by the transposed rotation
-                    if (p.interleaved) {
-#pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            z[2 * i] = fmaf(c[i], g[2 * i], s[i] * g[2 * i + 1]);
-                            z[2 * i + 1] = fmaf(c[i], g[2 * i + 1], -s[i] * g[2 * i]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            z[i] = fmaf(c[i], g[i], s[i] * g[V + i]);
-                            z[V + i] = fmaf(c[i], g[V + i], -s[i] * g[i]);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) along = fmaf(z[i] * w[i], x[i], along);
-                }
-                for (int o = p.lanes / 2; o; o >>= 1) {          // (rows without a norm beside rows with one: all take part)
-                    squares += __shfl_xor_sync(0xffffffffu, squares, o);
-                    if constexpr (kBackward) along += __shfl_xor_sync(0xffffffffu, along, o);
-                }
-                const float inverse = norm ? rsqrtf(fmaf(squares, p.inverse_d, p.eps)) : 1.f;
-                if constexpr (kBackward) {
-                    const float mean = norm ? along * inverse * p.inverse_d : 0.f;       // mean_c(w gz xhat)
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) {
-                        const float unit_x = x[i] * inverse;
-                        if (there) dw[i] = fmaf(z[i], unit_x, dw[i]);
-                        z[i] = norm ? inverse * fmaf(-unit_x, mean, z[i] * w[i]) : z[i];
+                        c[0] = make_float2(cp[0], V > 1 ? cp[second] : 0.f);
+                        s[0] = make_float2(sp[0], V > 1 ? sp[second] : 0.f);
                     }
                 } else {
-                    float n[2 * V];
 #pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) n[i] = norm ? x[i] * inverse * w[i] : x[i];
-                    if (p.interleaved) {
+                    for (int i = 0; i < kTwos; ++i) { c[i] = twice(1.f); s[i] = twice(0.f); }
+                }
+                const Pairs<V> x = unpack<V, kInterleaved>(xa[k], xb[k]);
+                Pairs<V> z;
+                float2 squares = twice(0.f), along = twice(0.f);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            z[2 * i] = fmaf(c[i], n[2 * i], -s[i] * n[2 * i + 1]);
-                            z[2 * i + 1] = fmaf(c[i], n[2 * i + 1], s[i] * n[2 * i]);
-                        }
-                    } else {
+                for (int i = 0; i < kTwos; ++i) squares = __ffma2_rn(x.b[i], x.b[i], __ffma2_rn(x.a[i], x.a[i], squares));
+                if constexpr (kBackward) {
+                    const Pairs<V> g = unpack<V, kInterleaved>(ga[k], gb[k]);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            z[i] = fmaf(c[i], n[i], -s[i] * n[V + i]);
-                            z[V + i] = fmaf(c[i], n[V + i], s[i] * n[i]);
-                        }
+                    for (int i = 0; i < kTwos; ++i) {            // back by the transposed rotation
+                        z.a[i] = __ffma2_rn(c[i], g.a[i], __fmul2_rn(s[i], g.b[i]));
+                        z.b[i] = __ffma2_rn(c[i], g.b[i], __fmul2_rn(negated(s[i]), g.a[i]));
+                        along = __ffma2_rn(__fmul2_rn(z.b[i], w.b[i]), x.b[i], __ffma2_rn(__fmul2_rn(z.a[i], w.a[i]), x.a[i], along));
+                    }
+                }
+                float of_squares = squares.x + squares.y, of_along = along.x + along.y;
+                for (int o = p.lanes / 2; o; o >>= 1) {          // (rows without a norm beside rows with one: all take part)
+                    of_squares += __shfl_xor_sync(0xffffffffu, of_squares, o);
+                    if constexpr (kBackward) of_along += __shfl_xor_sync(0xffffffffu, of_along, o);
+                }
+                const float inverse = norm ? rsqrtf(fmaf(of_squares, p.inverse_d, p.eps)) : 1.f;
+                const float2 inverse2 = twice(inverse);
+                if constexpr (kBackward) {
+                    const float2 mean = twice(norm ? -of_along * inverse * p.inverse_d : 0.f);       // - mean_c(w gz xhat)
+#pragma unroll
+                    for (int i = 0; i < kTwos; ++i) {
+                        const float2 ua = __fmul2_rn(x.a[i], inverse2), ub = __fmul2_rn(x.b[i], inverse2);
+                        if (there) { dw.a[i] = __ffma2_rn(z.a[i], ua, dw.a[i]); dw.b[i] = __ffma2_rn(z.b[i], ub, dw.b[i]); }
+                        z.a[i] = __fmul2_rn(inverse2, __ffma2_rn(ua, mean, __fmul2_rn(z.a[i], w.a[i])));
+                        z.b[i] = __fmul2_rn(inverse2, __ffma2_rn(ub, mean, __fmul2_rn(z.b[i], w.b[i])));
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kTwos; ++i) {
+                        const float2 na = __fmul2_rn(__fmul2_rn(x.a[i], inverse2), w.a[i]), nb = __fmul2_rn(__fmul2_rn(x.b[i], inverse2), w.b[i]);
+                        z.a[i] = __ffma2_rn(c[i], na, __fmul2_rn(negated(s[i]), nb));
+                        z.b[i] = __ffma2_rn(c[i], nb, __fmul2_rn(s[i], na));
                     }
                 }
                 if (there) {
+                    W ya, yb;
+                    if (!kBackward && !norm && !rotates) { ya = xa[k]; yb = xb[k]; }      // (as it was, NaN and all)
+                    else pack<V, kInterleaved>(z, ya, yb);
                     __nv_bfloat16* dst = y_at + (token0 + token) * y_stride;
-                    if (has_a) *reinterpret_cast<W*>(dst + ca) = pack<V>(z);
-                    if (has_b) *reinterpret_cast<W*>(dst + cb) = pack<V>(z + V);
+                    if (has_a) *reinterpret_cast<W*>(dst + ca) = ya;
+                    if (has_b) *reinterpret_cast<W*>(dst + cb) = yb;
                 }
             }
         }
@@ -222,10 +254,13 @@ __global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const __grid
     if constexpr (kBackward) {
         if (!p.part) return;
         // Sums of the block in a fixed order: of a row's channel over the tokens at once, or of a tensor's over its rows of the chunk too.
-        float* const sums = reinterpret_cast<float*>(turns);
+        float* const sums = turns;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) sums[threadIdx.x * 2 * V + i] = dw[i];
+        for (int i = 0; i < V; ++i) {
+            sums[threadIdx.x * 2 * V + place_a(i)] = i & 1 ? dw.a[i >> 1].y : dw.a[i >> 1].x;
+            sums[threadIdx.x * 2 * V + place_b(i)] = i & 1 ? dw.b[i >> 1].y : dw.b[i >> 1].x;
+        }
         __syncthreads();
         const int slots = p.rows_per_chunk * p.lanes, outputs = p.per_head ? p.rows_per_chunk : 2;
         float* const dst = p.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * outputs * p.d;
@@ -235,7 +270,7 @@ __global__ void __launch_bounds__(kThreads) rib_qk_norm_rope_kernel(const __grid
             int u, place;
             if (ch < p.rot) {
                 const int half = p.rot / 2;
-                if (p.interleaved) { u = ch / (2 * V); place = ch - u * 2 * V; }
+                if (kOddPairs) { u = ch / 2; place = ch & 1; }
                 else { const int in = ch < half ? ch : ch - half; u = in / V; place = in - u * V + (ch < half ? 0 : V); }
             } else {
                 const int in = ch - p.rot;
@@ -306,10 +341,11 @@ void rope_grid(const RopeProblem& p, int lanes, Plan* plan)
     plan->rows_per_chunk = (plan->rows + plan->chunks - 1) / plan->chunks;
     plan->chunks = (plan->rows + plan->rows_per_chunk - 1) / plan->rows_per_chunk;
     plan->tokens_at_once = kThreads / (plan->rows_per_chunk * lanes);
-    // tiles such that a small map still gives every SM two of them
-    long long tile = p.tokens / (2 * 148);
-    if (tile < plan->tokens_at_once) tile = plan->tokens_at_once;
-    if (tile > kMaxTile) tile = kMaxTile;
+    // a tile is what a block has under way at once, as far as its cosines and sines have room, and such that a small map still gives every SM two tiles
+    long long tile = p.tokens / (2 * 148), most_tokens = kUnrollMost * plan->tokens_at_once;
+    if (tile > most_tokens) tile = most_tokens;
+    if (tile > kMaxTurns / (p.rot > 2 ? p.rot / 2 : 1)) tile = kMaxTurns / (p.rot > 2 ? p.rot / 2 : 1);
+    tile = tile < plan->tokens_at_once ? plan->tokens_at_once : tile / plan->tokens_at_once * plan->tokens_at_once;
     plan->tile = (int)tile;
     plan->tiles = (int)((p.tokens + tile - 1) / tile);
     const int cap = (kMaxBlocks + plan->chunks - 1) / plan->chunks;
@@ -344,17 +380,18 @@ cudaError_t launch(const RopeProblem& p, float* part, const Plan& plan, cudaStre
         a.t[i] = RopeTensor{t.x, t.g, t.y, t.w, t.x_stride, t.y_stride, i ? p.kv_heads : p.heads};
     }
     a.table = reinterpret_cast<const float2*>(p.table); a.part = part; a.tokens = (int)p.tokens; a.tile = plan.tile; a.tiles = plan.tiles; a.H = p.H; a.W = p.W; a.d = p.d; a.rot = p.rot;
-    a.pairs = p.rot / 2; a.interleaved = p.interleaved; a.per_head = p.per_head; a.lanes = plan.lanes; a.rows = plan.rows; a.rows_per_chunk = plan.rows_per_chunk;
+    a.pairs = p.rot / 2; a.per_head = p.per_head; a.lanes = plan.lanes; a.rows = plan.rows; a.rows_per_chunk = plan.rows_per_chunk;
     a.tokens_at_once = plan.tokens_at_once; a.eps = p.eps; a.inverse_d = 1.f / (float)p.d;
     a.by_pixels = make_fast_div((int)((long long)p.H * p.W)); a.by_w = make_fast_div(p.W); a.by_pairs = make_fast_div(p.rot ? p.rot / 2 : 1);
     a.by_slots = make_fast_div(plan.rows_per_chunk * plan.lanes);
     const dim3 grid((unsigned)plan.blocks, (unsigned)plan.chunks);
-    size_t smem = sizeof(float2) * plan.tile * a.pairs;                                  // up to 16 KB
+    size_t smem = sizeof(float2) * plan.tile * a.pairs;                                  // up to 16 KB, or 256 tokens of one row's pairs
     if (kBackward && part && smem < sizeof(float) * kThreads * 2 * plan.V) smem = sizeof(float) * kThreads * 2 * plan.V;
     ProfileScope scope(kBackward ? RIB_KERNEL_QK_NORM_ROPE_BWD : RIB_KERNEL_QK_NORM_ROPE_FWD, stream);
-    if (plan.V == 8) rib_qk_norm_rope_kernel<8, kBackward><<<grid, kThreads, smem, stream>>>(a);
-    else if (plan.V == 2) rib_qk_norm_rope_kernel<2, kBackward><<<grid, kThreads, smem, stream>>>(a);
-    else rib_qk_norm_rope_kernel<1, kBackward><<<grid, kThreads, smem, stream>>>(a);
+    const auto kernel = plan.V == 8 ? (p.interleaved ? rib_qk_norm_rope_kernel<8, true, kBackward> : rib_qk_norm_rope_kernel<8, false, kBackward>)
+                      : plan.V == 2 ? (p.interleaved ? rib_qk_norm_rope_kernel<2, true, kBackward> : rib_qk_norm_rope_kernel<2, false, kBackward>)
+                                    : (p.interleaved ? rib_qk_norm_rope_kernel<1, true, kBackward> : rib_qk_norm_rope_kernel<1, false, kBackward>);
+    kernel<<<grid, kThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
 
@@ -377,6 +414,9 @@ size_t qk_norm_rope_bwd_workspace(const RopeProblem& p)
     for (int lanes = 1; lanes <= 32; lanes *= 2) {
         Plan plan{};
         rope_grid(p, lanes, &plan);
+        // (the tiles' size depends on `rot` too; they are no smaller than the tokens that are walked at once)
+        const long long tiles = (p.tokens + plan.tokens_at_once - 1) / plan.tokens_at_once, cap = (kMaxBlocks + plan.chunks - 1) / plan.chunks;
+        plan.blocks = (int)(tiles < cap ? tiles : cap);
         const size_t bytes = sizeof(float) * part_floats(plan, p.d, p.per_head != 0);
         most = bytes > most ? bytes : most;
     }
