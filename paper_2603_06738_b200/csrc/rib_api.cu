@@ -909,7 +909,7 @@ int cross_problem(int B, int H, int W, int heads, int kv_heads, int d, int L, in
     p->pixels = (long long)H * W; p->tokens = contexts == B ? p->pixels : B * p->pixels;
     // items, tiles and CTAs are counted in ints
     const rib::CrossPlan plan = rib::cross_plan(*p);
-    if ((__int128)plan.groups * plan.tiles * plan.splits > 0x7fff0000LL || (__int128)plan.groups * plan.dq_tiles * plan.dq_splits > 0x7fff0000LL || (__int128)plan.groups * plan.key_tiles * plan.row_splits > 0x7fff0000LL) return RIB_ERR_UNSUPPORTED;
+    if ((__int128)plan.groups * plan.tiles * plan.splits > 0x7fff0000LL || (__int128)plan.groups * (plan.row_tiles + 1) * 64 > 0x7fff0000LL || (__int128)plan.groups * plan.dq_tiles * plan.dq_splits > 0x7fff0000LL || (__int128)plan.groups * plan.key_tiles * plan.row_splits > 0x7fff0000LL) return RIB_ERR_UNSUPPORTED;
     return RIB_OK;
 }
 

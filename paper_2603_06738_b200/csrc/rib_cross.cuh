@@ -33,10 +33,14 @@ struct CrossPlan {
     int dq_tiles, dq_splits, dq_blocks_per_split;                      // dQ: tiles of two row tiles, and such runs of blocks of 64
     int key_tiles, row_splits, row_tiles_per_split;                    // dK and dV: tiles of 128 keys, runs of tiles of 64 rows
     int row_tiles, kv_rows_per_tile, kv_tokens_per_tile;
+    bool few_rows;                                                     // forward on the plain pipes; splits are then runs of a context's own keys
 };
 
 constexpr int kCrossSms = 148;            // the same number everywhere, so that a call's shape decides the launch
 constexpr int kCrossBlock = 64;           // keys of a block
+// Rows of a group (tokens x heads that share a head of keys) up to which the forward pass takes the plain pipes.  Plain pipes / tensor cores, us with the join: 1 row, 64 contexts of up to 4096, 6 heads
+// of 32 35 / 63; 2 rows, 64 x 4096, 6 heads of keys of 32 65 / 99, 16 x 4096, 2 of 64 25 / 26; 4 rows, 16 x 4096, 2 of 64 31 / 26; 8 rows 45 / 25.
+constexpr int kCrossFewRows = 2;
 
 CrossPlan cross_plan(const CrossProblem& p);
 bool cross_padded(const CrossProblem& p);                                       // rows that TMA cannot address: copies filled up with zero channels
@@ -44,6 +48,8 @@ size_t cross_fwd_workspace(const CrossProblem& p);
 size_t cross_bwd_workspace(const CrossProblem& p);
 cudaError_t cross_fwd(CrossProblem p, cudaStream_t stream, int* launches);
 cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches);
+// Forward of few rows (rib_cross_rows.cu), without the join of the splits, whose outputs are rows of `stride` floats.
+cudaError_t cross_fwd_rows(const CrossProblem& p, const CrossPlan& plan, float* part_out, float* part_lse, int stride, cudaStream_t stream);
 
 // Fills up rows of d channels with zeros to rows of `width`, up to four tensors in one launch (rib_cross_fwd_sm100.cu).
 struct CrossPad { const __nv_bfloat16* src[4]; __nv_bfloat16* dst[4]; long long rows[4]; int tensors, d, width; };

@@ -72,54 +72,74 @@ struct PrepareParams {
     const __nv_bfloat16 *out, *dout;
     const float* lse;
     RowStats stats;
-    long long rows, entries, tokens, pixels;         // rows: tokens of all contexts x heads; entries: of the statistics
-    int d, heads, kv_heads, G, lanes, row_blocks;
-    FastDiv by_group, by_pixels, by_tokens_of_context;
-    int vector;
+    int rows, entries, tokens, pixels;               // rows: tokens of all contexts x heads; entries: of the statistics
+    int d, heads, kv_heads, G, lane_bits, row_blocks, vector;
+    FastDiv by_heads, by_group, by_pixels, by_tokens_of_context, by_tiles;
 };
-__global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const PrepareParams p)
+constexpr int kPrepareRows = 4;                      // of a thread, their loads under way at once
+__global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const __grid_constant__ PrepareParams p)
 {
     if ((int)blockIdx.x >= p.row_blocks) {            // entries that are no row
-        const long long e = (long long)(blockIdx.x - p.row_blocks) * 256 + threadIdx.x;
+        const int e = (blockIdx.x - p.row_blocks) * 256 + threadIdx.x;
         if (e >= p.entries) return;
-        const int within = (int)(e % kRowTile), tile = (int)(e / kRowTile % p.stats.tiles);
-        if (within >= p.stats.tokens_per_tile * p.G || (long long)tile * p.stats.tokens_per_tile + within / p.G >= p.tokens) {
+        const int within = e % kRowTile;
+        int group, tile, t, g;
+        p.by_tiles.divmod(e / kRowTile, group, tile);
+        p.by_group.divmod(within, t, g);
+        if (t >= p.stats.tokens_per_tile || (long long)tile * p.stats.tokens_per_tile + t >= p.tokens) {
             float* at = stats_entry(p.stats.at, e);
             at[0] = -INFINITY; at[2] = 0.f;
         }
         return;
     }
-    // rows in the order of memory, `lanes` lanes (a power of two) to a row
-    const long long thread = (long long)blockIdx.x * 256 + threadIdx.x, row = thread / p.lanes;
-    const int part = (int)(thread & (p.lanes - 1));
-    float sum = 0.f;
-    if (row < p.rows) {
-        const __nv_bfloat16 *o = p.out + row * p.d, *g = p.dout + row * p.d;
-        if (p.vector) {
-            if (8 * part < p.d) {
-                const uint4 a = __ldg(reinterpret_cast<const uint4*>(o) + part), b = __ldg(reinterpret_cast<const uint4*>(g) + part);
-                const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    // rows in the order of memory, 2^lane_bits lanes to a row
+    const int part = threadIdx.x & ((1 << p.lane_bits) - 1), rows_at_once = 256 >> p.lane_bits;
+    const long long first = (long long)blockIdx.x * (kPrepareRows * rows_at_once) + (threadIdx.x >> p.lane_bits);
+    float sum[kPrepareRows];
+    if (p.vector) {
+        uint4 a[kPrepareRows], b[kPrepareRows];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sum = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum);
-                    sum = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), sum);
-                }
+        for (int k = 0; k < kPrepareRows; ++k) {
+            const long long row = first + k * rows_at_once;
+            const bool there = row < p.rows && 8 * part < p.d;
+            a[k] = there ? __ldg(reinterpret_cast<const uint4*>(p.out + row * p.d) + part) : make_uint4(0u, 0u, 0u, 0u);
+            b[k] = there ? __ldg(reinterpret_cast<const uint4*>(p.dout + row * p.d) + part) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int k = 0; k < kPrepareRows; ++k) {
+            const uint32_t x[4] = {a[k].x, a[k].y, a[k].z, a[k].w}, y[4] = {b[k].x, b[k].y, b[k].z, b[k].w};
+            sum[k] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sum[k] = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum[k]);
+                sum[k] = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), sum[k]);
             }
-        } else {
-            for (int c = part; c < p.d; c += p.lanes) sum = fmaf(__bfloat162float(o[c]), __bfloat162float(g[c]), sum);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < kPrepareRows; ++k) {
+            const long long row = first + k * rows_at_once;
+            sum[k] = 0.f;
+            if (row < p.rows)
+                for (int c = part; c < p.d; c += 1 << p.lane_bits) sum[k] = fmaf(__bfloat162float(p.out[row * p.d + c]), __bfloat162float(p.dout[row * p.d + c]), sum[k]);
         }
     }
-    for (int o = p.lanes / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (row >= p.rows || part != 0) return;
-    int token_of_all, head, image, pixel, context, token, kv, g;
-    const long long wide = row / p.heads;             // (rows may pass 2^31)
-    token_of_all = (int)wide; head = (int)(row - wide * p.heads);
-    p.by_pixels.divmod(token_of_all, image, pixel);
-    p.by_tokens_of_context.divmod(token_of_all, context, token);
-    p.by_group.divmod(head, kv, g);
-    const float lse = p.lse[((long long)image * p.heads + head) * p.pixels + pixel];
-    float* at = stats_entry(p.stats.at, stats_index(p.stats, (long long)context * p.kv_heads + kv, token, g));
-    at[0] = -lse * kLog2e; at[2] = -sum;
+#pragma unroll
+    for (int k = 0; k < kPrepareRows; ++k)
+        for (int o = (1 << p.lane_bits) >> 1; o; o >>= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
+#pragma unroll
+    for (int k = 0; k < kPrepareRows; ++k) {
+        const long long row = first + k * rows_at_once;
+        if (row >= p.rows || part != 0) continue;
+        int token_of_all, head, image, pixel, context, token, kv, g;
+        p.by_heads.divmod((int)row, token_of_all, head);
+        p.by_pixels.divmod(token_of_all, image, pixel);
+        p.by_tokens_of_context.divmod(token_of_all, context, token);
+        p.by_group.divmod(head, kv, g);
+        const float lse = p.lse[((long long)image * p.heads + head) * p.pixels + pixel];
+        float* at = stats_entry(p.stats.at, stats_index(p.stats, (long long)context * p.kv_heads + kv, token, g));
+        at[0] = -lse * kLog2e; at[2] = -sum[k];
+    }
 }
 
 // -------------------------------------------------------------------------------------------------- dQ
@@ -204,6 +224,7 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
+    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before: statistics, copies
 
     if (warp == 12) {
         // ============================================ loads
@@ -321,7 +342,9 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             tc_fence_after();
             const float* stats = stats_entry(reinterpret_cast<float*>(base_ptr + C::kOffStats + slot * C::kStatBytes), row);
             const float neg = stats[0], d = stats[2];
-            weights_in_place(t_s, t_s + 64, keys, scale2, [&](int) { return make_float4(neg, neg, d, d); });
+            const auto of_row = [&](int) { return make_float4(neg, neg, d, d); };
+            if (keys == kCrossBlock) weights_in_place(t_s, t_s + 64, kCrossBlock, scale2, of_row);
+            else weights_in_place(t_s, t_s + 64, keys, scale2, of_row);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::kReady + set));
@@ -451,6 +474,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
+    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before: statistics, copies
 
     if (warp == 12) {
         // ============================================ loads
@@ -577,13 +601,14 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
 
 // ------------------------------------------------------------------------------------ sums of the splits
 struct SumTensor { const float* part; __nv_bfloat16* dst; long long rows; int splits, G, heads; long long rows_of_group, tokens; };      // rows of all groups; dst [contexts][tokens][heads][d], heads = groups of a context x G
-struct SumParams { SumTensor t[3]; int d, stride, chunks, vector; };
-__global__ void __launch_bounds__(256) rib_cross_bwd_sum_kernel(const SumParams p)
+struct SumParams { SumTensor t[3]; int d, stride, chunks, vector, blocks; };      // blocks: of a tensor
+__global__ void __launch_bounds__(256) rib_cross_bwd_sum_kernel(const __grid_constant__ SumParams p)
 {
-    const SumTensor t = p.t[blockIdx.y];
-    const long long thread = (long long)blockIdx.x * 256 + threadIdx.x, at = thread / p.chunks;
+    const SumTensor t = p.t[blockIdx.x / p.blocks];
+    const long long thread = (long long)(blockIdx.x % p.blocks) * 256 + threadIdx.x, at = thread / p.chunks;
     const int chunk = (int)(thread - at * p.chunks);
     if (at >= t.rows) return;
+    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = 0.f;
@@ -649,17 +674,15 @@ cudaError_t launch_bwd(const CrossProblem& p, const CrossPlan& plan, const RowSt
     const int grid = a.items < kCrossSms ? a.items : kCrossSms;
     {
         ProfileScope scope(RIB_KERNEL_CROSS_BWD_DQ, stream);
-        rib_cross_bwd_dq_kernel<DP><<<grid, kDqThreads, DqCfg<DP>::kSmem, stream>>>(tm_q, tm_do, tm_k, tm_v, a);
+        if (cudaError_t e = launch_overtaking(rib_cross_bwd_dq_kernel<DP>, grid, kDqThreads, DqCfg<DP>::kSmem, stream, tm_q, tm_do, tm_k, tm_v, a)) return e;
     }
-    if (cudaError_t e = cudaGetLastError()) return e;
     KvParams b{};
     b.lengths = p.lengths; b.stats = stats.at; b.dk = p.dk; b.dv = p.dv; b.part_dk = part_dk; b.part_dv = part_dv; b.status = p.status;
     b.d = p.d; b.L = p.L; b.kv_heads = p.kv_heads; b.G = plan.G; b.key_tiles = plan.key_tiles; b.splits = plan.row_splits; b.row_tiles = plan.row_tiles; b.stat_tiles = stats.tiles;
     b.tiles_per_split = plan.row_tiles_per_split; b.rows_per_tile = plan.kv_rows_per_tile; b.tokens_per_tile = plan.kv_tokens_per_tile; b.vector = p.d % 8 == 0;
     b.groups = plan.groups; b.scale_log2 = scale_log2; b.inv_sqrt_d = inv_sqrt_d;
     ProfileScope scope(RIB_KERNEL_CROSS_BWD_DKV, stream);
-    rib_cross_bwd_dkv_kernel<DP><<<(unsigned)(plan.groups * plan.key_tiles * plan.row_splits), kKvThreads, KvCfg<DP>::kSmem, stream>>>(tm_q, tm_do, kv_k, kv_v, b);
-    return cudaGetLastError();
+    return launch_overtaking(rib_cross_bwd_dkv_kernel<DP>, plan.groups * plan.key_tiles * plan.row_splits, kKvThreads, KvCfg<DP>::kSmem, stream, tm_q, tm_do, kv_k, kv_v, b);
 }
 
 }  // namespace
@@ -677,11 +700,13 @@ cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches)
     stats.tokens_per_tile = plan.kv_tokens_per_tile; stats.tiles = stat_tiles(plan); stats.G = plan.G; stats.by_tokens = make_fast_div(plan.kv_tokens_per_tile);
     PrepareParams a{};
     a.out = p.out; a.dout = p.dout; a.lse = p.lse_in; a.stats = stats;
-    a.rows = p.tokens * p.contexts * p.heads; a.entries = (long long)plan.groups * stats.tiles * kRowTile; a.tokens = p.tokens; a.pixels = p.pixels;
+    a.rows = (int)(p.tokens * p.contexts * p.heads); a.entries = plan.groups * stats.tiles * kRowTile; a.tokens = (int)p.tokens; a.pixels = (int)p.pixels;
     a.d = p.d; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.vector = p.d % 8 == 0;
-    a.lanes = p.d <= 8 ? 1 : p.d <= 16 ? 2 : p.d <= 32 ? 4 : 8;
-    a.row_blocks = (int)((a.rows * a.lanes + 255) / 256);
-    a.by_group = make_fast_div(plan.G); a.by_pixels = make_fast_div((int)p.pixels); a.by_tokens_of_context = make_fast_div((int)p.tokens);
+    a.lane_bits = p.d <= 8 ? 0 : p.d <= 16 ? 1 : p.d <= 32 ? 2 : 3;
+    const int per_block = kPrepareRows * (256 >> a.lane_bits);
+    a.row_blocks = a.rows / per_block + (a.rows % per_block != 0);
+    a.by_heads = make_fast_div(p.heads); a.by_group = make_fast_div(plan.G); a.by_pixels = make_fast_div((int)p.pixels); a.by_tokens_of_context = make_fast_div((int)p.tokens);
+    a.by_tiles = make_fast_div(stats.tiles);
     {
         ProfileScope scope(RIB_KERNEL_CROSS_BWD_PREPARE, stream);
         rib_cross_bwd_prepare_kernel<<<(unsigned)(a.row_blocks + (a.entries + 255) / 256), 256, 0, stream>>>(a);
@@ -718,8 +743,8 @@ cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches)
     for (int i = 0; i < tensors; ++i) most = s.t[i].rows > most ? s.t[i].rows : most;
     ++*launches;
     ProfileScope scope(RIB_KERNEL_CROSS_BWD_SUM, stream);
-    rib_cross_bwd_sum_kernel<<<dim3((unsigned)((most * s.chunks + 255) / 256), (unsigned)tensors), 256, 0, stream>>>(s);
-    return cudaGetLastError();
+    s.blocks = (int)((most * s.chunks + 255) / 256);
+    return launch_overtaking(rib_cross_bwd_sum_kernel, s.blocks * tensors, 256, 0, stream, s);
 }
 
 }  // namespace rib

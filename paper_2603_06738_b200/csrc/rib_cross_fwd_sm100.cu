@@ -560,25 +560,43 @@ struct JoinParams {
     long long groups, rows, tokens;
     FastDiv by_pixels;
 };
-__global__ void __launch_bounds__(256) rib_cross_join_kernel(const JoinParams p)
+__global__ void __launch_bounds__(128) rib_cross_join_kernel(const JoinParams p)
 {
-    const long long thread = (long long)blockIdx.x * 256 + threadIdx.x, all = p.groups * p.rows;
+    const long long thread = (long long)blockIdx.x * 128 + threadIdx.x, all = p.groups * p.rows;
     const long long at = thread / p.chunks;
     const int chunk = (int)(thread - at * p.chunks);
     if (at >= all) return;
+    cudaGridDependencySynchronize();                     // it may have overtaken the kernel that computes the splits
+    // eight splits' loads under way at once
+    constexpr int kAtOnce = 8;
     float most = -INFINITY, total = 0.f, x[8];
-    for (int s = 0; s < p.splits; ++s) most = fmaxf(most, p.part_lse[s * all + at]);
+    for (int s0 = 0; s0 < p.splits; s0 += kAtOnce) {
+        float lse[kAtOnce];
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) lse[s] = s0 + s < p.splits ? p.part_lse[(s0 + s) * all + at] : -INFINITY;
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) most = fmaxf(most, lse[s]);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
-        const float lse = p.part_lse[s * all + at];
-        if (lse == -INFINITY) continue;
-        const float w = expf(lse - most);
-        const float4* src = reinterpret_cast<const float4*>(p.part_out + (s * all + at) * p.stride + 8 * chunk);
-        const float4 lo = src[0], hi = src[1];
-        total += w;
-        x[0] += w * lo.x; x[1] += w * lo.y; x[2] += w * lo.z; x[3] += w * lo.w;
-        x[4] += w * hi.x; x[5] += w * hi.y; x[6] += w * hi.z; x[7] += w * hi.w;
+    for (int s0 = 0; s0 < p.splits; s0 += kAtOnce) {
+        float lse[kAtOnce];
+        float4 lo[kAtOnce], hi[kAtOnce];
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) {
+            const int split = min(s0 + s, p.splits - 1);
+            lse[s] = s0 + s < p.splits ? p.part_lse[split * all + at] : -INFINITY;
+            const float4* src = reinterpret_cast<const float4*>(p.part_out + (split * all + at) * p.stride + 8 * chunk);
+            lo[s] = src[0]; hi[s] = src[1];
+        }
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) {
+            if (lse[s] == -INFINITY) continue;           // (no keys, or none that weighs anything)
+            const float w = expf(lse[s] - most);
+            total += w;
+            x[0] += w * lo[s].x; x[1] += w * lo[s].y; x[2] += w * lo[s].z; x[3] += w * lo[s].w;
+            x[4] += w * hi[s].x; x[5] += w * hi[s].y; x[6] += w * hi[s].z; x[7] += w * hi[s].w;
+        }
     }
     const long long group = at / p.rows, r = at - group * p.rows, token = r / p.G;
     const int context = (int)(group / p.kv_heads), head = (int)(group - (long long)context * p.kv_heads) * p.G + (int)(r - token * p.G);
@@ -650,8 +668,7 @@ cudaError_t join(const CrossProblem& p, const CrossPlan& plan, const float* part
     j.vector = p.d % 8 == 0; j.pixels = (int)p.pixels; j.groups = plan.groups; j.rows = plan.rows; j.tokens = p.tokens; j.by_pixels = make_fast_div((int)p.pixels);
     const long long threads = j.groups * j.rows * j.chunks;
     ProfileScope scope(RIB_KERNEL_CROSS_JOIN, stream);
-    rib_cross_join_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, stream>>>(j);
-    return cudaGetLastError();
+    return launch_overtaking(rib_cross_join_kernel, (int)((threads + 127) / 128), 128, 0, stream, j);
 }
 
 int tile_width(int d) { return d <= 32 ? 32 : 64; }
@@ -703,6 +720,11 @@ CrossPlan cross_plan(const CrossProblem& p)
     };
     c.pairs = (c.tiles + 1) / 2;
     split((long long)c.groups * c.pairs, (p.L + kKeys - 1) / kKeys, &c.splits, &c.blocks_per_split);
+    c.few_rows = c.rows <= kCrossFewRows;
+    if (c.few_rows) {      // eight blocks to an SM, of 128 keys or more
+        const long long most = 8 * kCrossSms / c.groups, runs = (p.L + 127) / 128;
+        c.splits = (int)(most < 1 ? 1 : most < runs ? most : runs);
+    }
     c.dq_tiles = (c.row_tiles + 1) / 2;
     split((long long)c.groups * c.dq_tiles, (p.L + kCrossBlock - 1) / kCrossBlock, &c.dq_splits, &c.dq_blocks_per_split);
     // dK and dV: a CTA to an SM; runs of row tiles such that the last round of CTAs is not a mostly empty one.  In us: 0.3 a tile, 3 for what a CTA begins and
@@ -753,7 +775,7 @@ cudaError_t cross_fwd(CrossProblem p, cudaStream_t stream, int* launches)
         ++*launches;
     }
     float *part_out = reinterpret_cast<float*>(ws + l.part_out), *part_lse = reinterpret_cast<float*>(ws + l.part_lse);
-    if (cudaError_t e = tile_width(p.d) == 32 ? launch_fwd<32>(p, plan, part_out, part_lse, stream) : launch_fwd<64>(p, plan, part_out, part_lse, stream)) return e;
+    if (cudaError_t e = plan.few_rows ? cross_fwd_rows(p, plan, part_out, part_lse, tile_width(p.d), stream) : tile_width(p.d) == 32 ? launch_fwd<32>(p, plan, part_out, part_lse, stream) : launch_fwd<64>(p, plan, part_out, part_lse, stream)) return e;
     if (plan.splits > 1) {
         ++*launches;
         return join(p, plan, part_out, part_lse, tile_width(p.d), stream);
