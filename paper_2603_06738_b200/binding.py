@@ -1090,6 +1090,10 @@ def rib_rope_table(frequencies, H, W, y0=0, x0=0, magnitude=1.0, stream=None):
     map's first token, `magnitude` a factor of the rotated channels.  A sequence of L tokens is a map of L rows and one column."""
     if stream is not None and _elsewhere(stream):
         return _beside(stream, rib_rope_table, frequencies, H, W, y0, x0, magnitude)
+    if _marshal is not None:
+        got = _native(_marshal.rope_table, "rib_rope_table", frequencies, H, W, y0, x0, magnitude, stream)
+        if got is not None:
+            return got[0]
     if frequencies.dtype != torch.float32 or not frequencies.is_cuda or not frequencies.is_contiguous() or frequencies.dim() != 2 or frequencies.shape[0] != 2:
         raise ValueError("frequencies must be a contiguous CUDA float32 tensor [2, rot / 2]")
     pairs = frequencies.shape[1]
@@ -1162,6 +1166,10 @@ def rib_qk_norm_rope_fwd(q, k, q_weight=None, k_weight=None, table=None, interle
     Returns (q, k), contiguous (k None if there is none)."""
     if stream is not None and _elsewhere(stream):
         return _beside(stream, rib_qk_norm_rope_fwd, q, k, q_weight, k_weight, table, interleaved, eps)
+    if _marshal is not None:
+        got = _native(_marshal.rope_fwd, "rib_qk_norm_rope_fwd", q, k, q_weight, k_weight, table, interleaved, eps, stream)
+        if got is not None:
+            return got
     q_stride, k_stride, kv_heads, per_head, rot = _check_rope(q, k, q_weight, k_weight, table)
     B, H, W, heads, d = q.shape
     with _on(q.device, *([] if k is None else [k])):
@@ -1183,6 +1191,11 @@ def rib_qk_norm_rope_bwd(q, k, q_weight, k_weight, table, dq_out, dk_out, interl
     shape (None where there is none).  dq and dk may be given: tensors, or slices of heads of the gradient of one projection's output, that are written."""
     if stream is not None and _elsewhere(stream):
         return _beside(stream, rib_qk_norm_rope_bwd, q, k, q_weight, k_weight, table, dq_out, dk_out, interleaved, eps, dq, dk, workspace)
+    if _marshal is not None and dq is None and dk is None:
+        call = lambda address, *args: _marshal.rope_bwd(address, _lib.rib_addresses["rib_qk_norm_rope_bwd_workspace"], *args)  # noqa: E731
+        got = _native(call, "rib_qk_norm_rope_bwd", q, k, q_weight, k_weight, table, dq_out, dk_out, interleaved, eps, workspace, stream)
+        if got is not None:
+            return got
     q_stride, k_stride, kv_heads, per_head, rot = _check_rope(q, k, q_weight, k_weight, table)
     B, H, W, heads, d = q.shape
     _check_image("dq_out", dq_out, q.shape)
@@ -1234,6 +1247,11 @@ def rib_cross_attn_fwd(q, k, v, lengths=None, workspace=None, stream=None, want_
     the states of each context that are attended to.  Returns (out, lse)."""
     if stream is not None and _elsewhere(stream):
         return _beside(stream, rib_cross_attn_fwd, q, k, v, lengths, workspace, None, want_lse)
+    if _marshal is not None:
+        call = lambda address, *args: _marshal.cross_fwd(address, _lib.rib_addresses["rib_cross_attn_fwd_workspace"], *args)  # noqa: E731
+        got = _native(call, "rib_cross_attn_fwd", q, k, v, lengths, workspace, want_lse, stream)
+        if got is not None:
+            return got
     kv_heads, L, contexts = _check_states(q, k, v, lengths)
     B, H, W, heads, d = q.shape
     need = rib_cross_attn_fwd_workspace(B, H, W, heads, kv_heads, d, L, contexts)
@@ -1257,6 +1275,11 @@ def rib_cross_attn_bwd(q, k, v, out, lse, dout, lengths=None, workspace=None, st
     """Backward pass of rib_cross_attn_fwd.  Returns (dq, dk, dv), bf16 in the shapes of q, k, v."""
     if stream is not None and _elsewhere(stream):
         return _beside(stream, rib_cross_attn_bwd, q, k, v, out, lse, dout, lengths, workspace)
+    if _marshal is not None:
+        call = lambda address, *args: _marshal.cross_bwd(address, _lib.rib_addresses["rib_cross_attn_bwd_workspace"], *args)  # noqa: E731
+        got = _native(call, "rib_cross_attn_bwd", q, k, v, out, lse, dout, lengths, workspace, stream)
+        if got is not None:
+            return got
     kv_heads, L, contexts = _check_states(q, k, v, lengths)
     B, H, W, heads, d = q.shape
     for name, t in (("out", out), ("dout", dout)):

@@ -18,12 +18,12 @@
 
 namespace {
 
-// The tensor behind a plain torch.Tensor of the given type: dense CUDA memory of its own, contiguous; else null.
-const at::Tensor* plain(PyObject* o, at::ScalarType type, int dim)
+// The tensor behind a plain torch.Tensor of the given type: dense CUDA memory of its own, contiguous (or, `strided`, a view); else null.
+const at::Tensor* plain(PyObject* o, at::ScalarType type, int dim, bool strided = false)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.defined() || t.is_nested() || t.layout() != at::kStrided || !t.is_cuda() || t.scalar_type() != type || t.dim() != dim || !t.has_storage() || !t.is_contiguous()) return nullptr;
+    if (!t.defined() || t.is_nested() || t.layout() != at::kStrided || !t.is_cuda() || t.scalar_type() != type || t.dim() != dim || !t.has_storage() || !(strided || t.is_contiguous())) return nullptr;
     const auto keys = t.key_set();
     if (keys.has_any(c10::DispatchKeySet({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper,
                                           c10::DispatchKey::Functionalize, c10::DispatchKey::Conjugate, c10::DispatchKey::Negative, c10::DispatchKey::ZeroTensor}))) return nullptr;
@@ -467,7 +467,219 @@ PyObject* generate_bwd(PyObject*, PyObject* const* a, Py_ssize_t count)
     });
 }
 
+// states k, v [contexts, L, kv_heads, d] beside q, and lengths or None
+struct States { const at::Tensor *q, *k, *v, *lengths, *given; int B, H, W, heads, kv_heads, d, L, contexts; void* stream; };
+bool get_states(PyObject* const* a, PyObject* lengths, PyObject* workspace, PyObject* stream, States* x)
+{
+    x->q = plain(a[0], at::kBFloat16, 5); x->k = plain(a[1], at::kBFloat16, 4); x->v = plain(a[2], at::kBFloat16, 4);
+    if (!x->q || !x->k || !x->v || x->v->sizes() != x->k->sizes() || !here({x->q, x->k, x->v}) || !get_stream(stream, &x->stream)) return false;
+    const auto q = x->q->sizes(), k = x->k->sizes();
+    for (int i = 0; i < 5; ++i) if (q[i] < 1 || q[i] > (1ll << 30)) return false;
+    for (int i = 0; i < 4; ++i) if (k[i] < 1 || k[i] > (1ll << 30)) return false;
+    if ((k[0] != 1 && k[0] != q[0]) || k[3] != q[4] || q[3] % k[2]) return false;
+    x->B = (int)q[0]; x->H = (int)q[1]; x->W = (int)q[2]; x->heads = (int)q[3]; x->d = (int)q[4];
+    x->contexts = (int)k[0]; x->L = (int)k[1]; x->kv_heads = (int)k[2];
+    x->lengths = lengths == Py_None ? nullptr : plain(lengths, at::kInt, 1);
+    if (lengths != Py_None && (!x->lengths || x->lengths->size(0) != k[0] || !here({x->lengths}))) return false;
+    x->given = workspace == Py_None ? nullptr : plain(workspace, at::kByte, 1);
+    return workspace == Py_None || (x->given && here({x->given}));
+}
+
+// cross_fwd(address, address of the workspace's size, q, k, v, lengths or None, workspace or None, want_lse, stream)
+PyObject* cross_fwd(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        States x;
+        if (count != 9 || modes_active() || !PyBool_Check(a[7]) || !get_states(a + 2, a[5], a[6], a[8], &x)) Py_RETURN_NONE;
+        const auto fn = reinterpret_cast<decltype(&rib_cross_attn_fwd)>(address(a[0]));
+        const auto need = reinterpret_cast<decltype(&rib_cross_attn_fwd_workspace)>(address(a[1]));
+        const bool want_lse = a[7] == Py_True;
+        at::Tensor out, lse, ws;
+        int rc;
+        {
+            const Unlocked unlocked;
+            if (x.given) {
+                ws = *x.given;
+            } else if (const size_t bytes = need(x.B, x.H, x.W, x.heads, x.kv_heads, x.d, x.L, x.contexts)) {
+                ws = at::empty({(int64_t)bytes}, x.q->options().dtype(at::kByte));
+            }
+            out = at::empty_like(*x.q);
+            if (want_lse) lse = at::empty({x.B, x.heads, x.H, x.W}, x.q->options().dtype(at::kFloat));
+            rc = fn(x.q->const_data_ptr(), x.k->const_data_ptr(), x.v->const_data_ptr(), x.lengths ? x.lengths->const_data_ptr<int>() : nullptr, x.B, x.H, x.W, x.heads, x.kv_heads, x.d, x.L,
+                    x.contexts, out.mutable_data_ptr(), lse.defined() ? lse.mutable_data_ptr<float>() : nullptr, ws.defined() ? ws.mutable_data_ptr() : nullptr,
+                    ws.defined() ? (size_t)ws.numel() : 0, x.stream);
+        }
+        if (rc) return status(rc);
+        return results({&out, &lse});
+    });
+}
+
+// cross_bwd(address, address of the workspace's size, q, k, v, out, lse, dout, lengths or None, workspace or None, stream)
+PyObject* cross_bwd(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        States x;
+        if (count != 11 || modes_active() || !get_states(a + 2, a[8], a[9], a[10], &x)) Py_RETURN_NONE;
+        const at::Tensor *out = plain(a[5], at::kBFloat16, 5), *lse = plain(a[6], at::kFloat, 4), *dout = plain(a[7], at::kBFloat16, 5);
+        if (!out || !lse || !dout || out->sizes() != x.q->sizes() || dout->sizes() != x.q->sizes() || lse->size(0) != x.B || lse->size(1) != x.heads || lse->size(2) != x.H ||
+            lse->size(3) != x.W || !here({out, lse, dout})) Py_RETURN_NONE;
+        const auto fn = reinterpret_cast<decltype(&rib_cross_attn_bwd)>(address(a[0]));
+        const auto need = reinterpret_cast<decltype(&rib_cross_attn_bwd_workspace)>(address(a[1]));
+        at::Tensor dq, dk, dv, ws;
+        int rc;
+        {
+            const Unlocked unlocked;
+            ws = x.given ? *x.given : at::empty({(int64_t)need(x.B, x.H, x.W, x.heads, x.kv_heads, x.d, x.L, x.contexts) + 256}, x.q->options().dtype(at::kByte));
+            dq = at::empty_like(*x.q); dk = at::empty_like(*x.k); dv = at::empty_like(*x.k);
+            rc = fn(x.q->const_data_ptr(), x.k->const_data_ptr(), x.v->const_data_ptr(), x.lengths ? x.lengths->const_data_ptr<int>() : nullptr, out->const_data_ptr(), lse->const_data_ptr<float>(),
+                    dout->const_data_ptr(), x.B, x.H, x.W, x.heads, x.kv_heads, x.d, x.L, x.contexts, dq.mutable_data_ptr(), dk.mutable_data_ptr(), dv.mutable_data_ptr(),
+                    ws.mutable_data_ptr(), (size_t)ws.numel(), x.stream);
+        }
+        if (rc) return status(rc);
+        return results({&dq, &dk, &dv});
+    });
+}
+
+// Elements between the tokens of [B, H, W, heads, d] whose heads lie behind one another and whose tokens are evenly spaced; -1: not so.
+long long token_stride(const at::Tensor& t)
+{
+    const auto size = t.sizes(), stride = t.strides();
+    if ((size[4] > 1 && stride[4] != 1) || (size[3] > 1 && stride[3] != size[4])) return -1;
+    long long token = -1, tokens = 1;
+    for (int i = 2; i >= 0; --i) {
+        if (size[i] > 1) {
+            if (token < 0) token = stride[i] / tokens;
+            if (stride[i] != token * tokens || token < 1) return -1;
+        }
+        tokens *= size[i];
+    }
+    return token < 0 ? size[3] * size[4] : token;
+}
+
+// q, k or None, their weights or None, the table or None
+struct Rope { const at::Tensor *q, *k, *q_weight, *k_weight, *table; long long q_stride, k_stride; int B, H, W, heads, kv_heads, d, rot, per_head; float eps; bool interleaved; void* stream; };
+bool get_rope(PyObject* const* a, PyObject* interleaved, PyObject* eps, PyObject* stream, Rope* x)
+{
+    x->q = plain(a[0], at::kBFloat16, 5, true);
+    x->k = a[1] == Py_None ? nullptr : plain(a[1], at::kBFloat16, 5, true);
+    if (!x->q || (a[1] != Py_None && !x->k) || !PyBool_Check(interleaved) || !PyFloat_CheckExact(eps) || !get_stream(stream, &x->stream) || !here({x->q}) || (x->k && !here({x->k}))) return false;
+    const auto q = x->q->sizes();
+    for (int i = 0; i < 5; ++i) if (q[i] < 1 || q[i] > (1ll << 30)) return false;
+    x->B = (int)q[0]; x->H = (int)q[1]; x->W = (int)q[2]; x->heads = (int)q[3]; x->d = (int)q[4];
+    x->q_stride = token_stride(*x->q); x->k_stride = 0; x->kv_heads = 0;
+    if (x->q_stride < 0) return false;
+    if (x->k) {
+        const auto k = x->k->sizes();
+        if (k[0] != q[0] || k[1] != q[1] || k[2] != q[2] || k[4] != q[4] || k[3] < 1 || k[3] > (1ll << 30)) return false;
+        x->kv_heads = (int)k[3];
+        x->k_stride = token_stride(*x->k);
+        if (x->k_stride < 0) return false;
+    } else if (a[3] != Py_None) {
+        return false;
+    }
+    x->per_head = -1;
+    const at::Tensor** weights[2] = {&x->q_weight, &x->k_weight};
+    for (int i = 0; i < 2; ++i) {
+        *weights[i] = nullptr;
+        if (a[2 + i] == Py_None) continue;
+        const at::Tensor* w = plain(a[2 + i], at::kFloat, 1);
+        const int per_head = w ? 0 : 1;
+        if (!w) w = plain(a[2 + i], at::kFloat, 2);
+        if (!w || !here({w}) || w->size(-1) != x->d || (per_head && w->size(0) != (i ? x->kv_heads : x->heads)) || (x->per_head >= 0 && x->per_head != per_head)) return false;
+        x->per_head = per_head;
+        *weights[i] = w;
+    }
+    if (x->per_head < 0) x->per_head = 0;
+    x->table = a[4] == Py_None ? nullptr : plain(a[4], at::kFloat, 3);
+    if (a[4] != Py_None && (!x->table || !here({x->table}) || x->table->size(0) != (int64_t)x->H + x->W || x->table->size(2) != 2 || 2 * x->table->size(1) > x->d || x->table->size(1) < 1)) return false;
+    x->rot = x->table ? 2 * (int)x->table->size(1) : 0;
+    x->eps = (float)PyFloat_AS_DOUBLE(eps);
+    x->interleaved = interleaved == Py_True;
+    return true;
+}
+const float* floats(const at::Tensor* t) { return t ? t->const_data_ptr<float>() : nullptr; }
+
+// rope_fwd(address, q, k or None, q_weight or None, k_weight or None, table or None, interleaved, eps, stream)
+PyObject* rope_fwd(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        Rope x;
+        if (count != 9 || modes_active() || !get_rope(a + 1, a[6], a[7], a[8], &x)) Py_RETURN_NONE;
+        const auto fn = reinterpret_cast<decltype(&rib_qk_norm_rope_fwd)>(address(a[0]));
+        at::Tensor q, k;
+        int rc;
+        {
+            const Unlocked unlocked;
+            q = at::empty({x.B, x.H, x.W, x.heads, x.d}, x.q->options());
+            if (x.k) k = at::empty({x.B, x.H, x.W, x.kv_heads, x.d}, x.q->options());
+            rc = fn(x.q->const_data_ptr(), x.q_stride, x.k ? x.k->const_data_ptr() : nullptr, x.k_stride, floats(x.q_weight), floats(x.k_weight), x.per_head, floats(x.table), x.B, x.H, x.W,
+                    x.heads, x.kv_heads, x.d, x.rot, x.interleaved, x.eps, q.mutable_data_ptr(), x.k ? k.mutable_data_ptr() : nullptr, x.stream);
+        }
+        if (rc) return status(rc);
+        return results({&q, &k});
+    });
+}
+
+// rope_bwd(address, address of the workspace's size, q, k or None, q_weight or None, k_weight or None, table or None, dq_out, dk_out or None, interleaved, eps, workspace or None, stream)
+PyObject* rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        Rope x;
+        if (count != 13 || modes_active() || !get_rope(a + 2, a[9], a[10], a[12], &x)) Py_RETURN_NONE;
+        const at::Tensor *gq = plain(a[7], at::kBFloat16, 5), *gk = a[8] == Py_None ? nullptr : plain(a[8], at::kBFloat16, 5);
+        const at::Tensor* given = a[11] == Py_None ? nullptr : plain(a[11], at::kByte, 1);
+        if (!gq || (x.k != nullptr) != (gk != nullptr) || (a[8] != Py_None && !gk) || (a[11] != Py_None && !given) || gq->sizes() != x.q->sizes() || !here({gq}) ||
+            (gk && (gk->sizes() != x.k->sizes() || !here({gk}))) || (given && !here({given}))) Py_RETURN_NONE;
+        const auto fn = reinterpret_cast<decltype(&rib_qk_norm_rope_bwd)>(address(a[0]));
+        const auto need = reinterpret_cast<decltype(&rib_qk_norm_rope_bwd_workspace)>(address(a[1]));
+        at::Tensor dq, dk, dqw, dkw, ws;
+        int rc;
+        {
+            const Unlocked unlocked;
+            ws = given ? *given : at::empty({(int64_t)need(x.B, x.H, x.W, x.heads, x.kv_heads, x.d, x.per_head) + 256}, x.q->options().dtype(at::kByte));
+            dq = at::empty({x.B, x.H, x.W, x.heads, x.d}, x.q->options());
+            if (x.k) dk = at::empty({x.B, x.H, x.W, x.kv_heads, x.d}, x.q->options());
+            if (x.q_weight) dqw = at::empty_like(*x.q_weight);
+            if (x.k_weight) dkw = at::empty_like(*x.k_weight);
+            rc = fn(x.q->const_data_ptr(), x.q_stride, x.k ? x.k->const_data_ptr() : nullptr, x.k_stride, floats(x.q_weight), floats(x.k_weight), x.per_head, floats(x.table),
+                    gq->const_data_ptr(), gk ? gk->const_data_ptr() : nullptr, x.B, x.H, x.W, x.heads, x.kv_heads, x.d, x.rot, x.interleaved, x.eps, dq.mutable_data_ptr(),
+                    (long long)x.heads * x.d, x.k ? dk.mutable_data_ptr() : nullptr, (long long)x.kv_heads * x.d, dqw.defined() ? dqw.mutable_data_ptr<float>() : nullptr,
+                    dkw.defined() ? dkw.mutable_data_ptr<float>() : nullptr, ws.mutable_data_ptr(), (size_t)ws.numel(), x.stream);
+        }
+        if (rc) return status(rc);
+        return results({&dq, &dk, &dqw, &dkw});
+    });
+}
+
+// rope_table(address, frequencies, H, W, y0, x0, magnitude, stream)
+PyObject* rope_table(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject* {
+        int H, W, y0, x0;
+        void* stream;
+        const at::Tensor* f = count == 8 && !modes_active() ? plain(a[1], at::kFloat, 2) : nullptr;
+        if (!f || f->size(0) != 2 || f->size(1) < 1 || f->size(1) > (1 << 20) || !get_int(a[2], &H) || !get_int(a[3], &W) || H < 1 || W < 1 || !get_int(a[4], &y0) || !get_int(a[5], &x0) ||
+            !PyFloat_CheckExact(a[6]) || !get_stream(a[7], &stream) || !here({f})) Py_RETURN_NONE;
+        const auto fn = reinterpret_cast<decltype(&rib_rope_table)>(address(a[0]));
+        const float magnitude = (float)PyFloat_AS_DOUBLE(a[6]);
+        at::Tensor table;
+        int rc;
+        {
+            const Unlocked unlocked;
+            table = at::empty({(int64_t)H + W, f->size(1), 2}, f->options());
+            rc = fn(f->const_data_ptr<float>(), H, W, (int)f->size(1), y0, x0, magnitude, table.mutable_data_ptr<float>(), stream);
+        }
+        if (rc) return status(rc);
+        return results({&table});
+    });
+}
+
 PyMethodDef methods[] = {
+    {"cross_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cross_fwd)), METH_FASTCALL, nullptr},
+    {"cross_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cross_bwd)), METH_FASTCALL, nullptr},
+    {"rope_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rope_fwd)), METH_FASTCALL, nullptr},
+    {"rope_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rope_bwd)), METH_FASTCALL, nullptr},
+    {"rope_table", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rope_table)), METH_FASTCALL, nullptr},
     {"fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(fwd)), METH_FASTCALL, nullptr},
     {"bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bwd)), METH_FASTCALL, nullptr},
     {"fwd_bucketed", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(fwd_bucketed)), METH_FASTCALL, nullptr},
