@@ -27,30 +27,24 @@ __device__ __forceinline__ long long stats_index(const RowStats& s, long long gr
     return (group * s.tiles + tile) * kRowTile + t * s.G + head;
 }
 
-// 64 columns of scores s and dP of a lane -> P and dS as bf16, in place.  x = s scale + neg, P = 2^x held to 1 whatever the roundings of large scores and lse make of it, dS = P (dP + d).
-// A chunk of 16 columns is loaded under the arithmetic of the one before; P and dS go where columns lie that have been read.  `stats(i)` gives (neg, neg', d, d') of
-// columns 2 i, 2 i + 1; columns from `columns` on weigh nothing, whatever they hold, and chunks that have none of them are left out.
-template <typename Stats>
+// 32 columns of scores s and dP of a lane -> P and dS as bf16, in the first 16 of them.  x = s scale + neg, P = 2^x held to 1 whatever the roundings of large scores and lse make of it, dS = P (dP + d).
+// 16 columns at a time: P and dS go where columns lie that have been read.  `stats(i)` gives (neg, neg', d, d') of columns 2 i, 2 i + 1; columns from `columns` on weigh nothing, whatever they hold, and
+// chunks that have none of them are left out.
+template <bool kStoreP, typename Stats>
 __device__ __forceinline__ void weights_in_place(uint32_t t_s, uint32_t t_dp, int columns, float2 scale2, Stats stats)
 {
-    uint32_t s[2][16], dp[2][16];
-    tmem_ld16(t_s, s[0]);
-    tmem_ld16(t_dp, dp[0]);
-    tmem_wait_ld();
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
+    for (int g = 0; g < 2; ++g) {
         if (16 * g >= columns) break;
-        if (g < 3) {
-            tmem_ld16(t_s + 16 * (g + 1), s[(g + 1) & 1]);
-            tmem_ld16(t_dp + 16 * (g + 1), dp[(g + 1) & 1]);
-        }
-        uint32_t (&a)[16] = s[g & 1], (&b)[16] = dp[g & 1];
+        uint32_t a[16], b[16], pp[8], pd[8];
+        tmem_ld16(t_s + 16 * g, a);
+        tmem_ld16(t_dp + 16 * g, b);
+        tmem_wait_ld();
         if (columns < 16 * g + 16) {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 if (16 * g + e >= columns) { a[e] = 0xff800000u; b[e] = 0u; }
         }
-        uint32_t pp[8], pd[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float4 st = stats(8 * g + i);
@@ -60,12 +54,13 @@ __device__ __forceinline__ void weights_in_place(uint32_t t_s, uint32_t t_dp, in
             pp[i] = pack_bf16x2(w.x, w.y);
             pd[i] = pack_bf16x2(z.x, z.y);
         }
-        if (g < 3) tmem_wait_ld();
-        tmem_st8(t_s + 8 * g, pp);
+        if constexpr (kStoreP) tmem_st8(t_s + 8 * g, pp);
         tmem_st8(t_dp + 8 * g, pd);
     }
     tmem_wait_st();
 }
+// where the K16 step kk of P or dS lies among its 64 columns
+__device__ __forceinline__ uint32_t weights_at(int kk) { return 32 * (kk >> 1) + 8 * (kk & 1); }
 
 // ------------------------------------------------------------------------------------------------ D, lse
 struct PrepareParams {
@@ -148,7 +143,7 @@ __global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const __grid
 // Three sets of 64 + 64 columns rotate among the steps, each with four warps of its own, so that one set's exponentials run under the others' products; dQ has two
 // accumulators, and four warps that store one while the next item is under way.
 // (The first form had four CTAs to an SM with one set of 64 columns each, S and dP one after the other: 256 x 256 tokens to 1024 states 283 us.)
-constexpr int kDqThreads = 640, kSets = 3;
+constexpr int kDqThreads = 1024, kSets = 3;
 constexpr uint32_t kTmemCols = 512, kColAcc = kSets * 128;
 
 template <int DP> struct DqCfg {
@@ -208,11 +203,11 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 
     if (threadIdx.x == 0) {
         abort_flag[0] = 0; abort_flag[1] = 0;
-        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), (i >= C::kReady && i < C::kFree) || (i >= C::kAccFree && i < C::kDrain) ? 4 : 1);
+        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i >= C::kReady && i < C::kFree ? 8 : i >= C::kAccFree && i < C::kDrain ? 4 : 1);
         fence_barrier_init();
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_do); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
     }
-    if (warp == 12) {
+    if (warp == 24) {
         tmem_alloc(base + C::kOffMisc, kTmemCols);
         tmem_relinquish();
     }
@@ -226,7 +221,7 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     bool ok = true;
     cudaGridDependencySynchronize();                      // it may have overtaken the kernel before: statistics, copies
 
-    if (warp == 12) {
+    if (warp == 24) {
         // ============================================ loads
         uint32_t step = 0, live = 0, asked = 0;            // asked: items whose rows have been asked for
         for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
@@ -264,7 +259,7 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             for (uint32_t i = step > kStages ? step - kStages : 0; i < step; ++i) mbar_wait_warp(bar(C::kKFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
             for (uint32_t i = asked > kTiles ? asked - kTiles : 0; i < asked; ++i) mbar_wait_warp(bar(C::kQFull + i % kTiles), (i / kTiles) & 1, abort_flag + 1, p.status);
         }
-    } else if (warp == 13) {
+    } else if (warp == 25) {
         // ============================================ S and dP
         uint32_t step = 0, live = 0;
         for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
@@ -297,7 +292,7 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 __syncwarp();
             }
         }
-    } else if (warp == 14) {
+    } else if (warp == 26) {
         // ============================================ dQ
         uint32_t step = 0, live = 0;
         for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
@@ -313,7 +308,7 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                     const uint64_t k = smem_desc_at(T::kDesc, base + C::kOffK + st * C::kKBytes);
                     constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
                     const int k_steps = (min(kCrossBlock, c.length - (c.first + j) * kCrossBlock) + 15) / 16;
-                    for (int kk = 0; kk < k_steps; ++kk) mma_ts(tmem + kColAcc + acc * DP, tmem + set * 128 + 64 + 8 * kk, k + T::kStepRows * kk, kIdesc, (j || kk) ? 1u : 0u);
+                    for (int kk = 0; kk < k_steps; ++kk) mma_ts(tmem + kColAcc + acc * DP, tmem + set * 128 + 64 + weights_at(kk), k + T::kStepRows * kk, kIdesc, (j || kk) ? 1u : 0u);
                     mma_commit(bar(C::kFree + set));
                     mma_commit(bar(C::kKEmpty + st));
                     if (j == c.blocks - 1) {
@@ -325,10 +320,10 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             }
             ++live;
         }
-    } else if (warp < 12) {
-        // ============================================ P and dS, a row to a thread
-        const int set = warp >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + set * 128;
+    } else if (warp < 24) {
+        // ============================================ P and dS, two threads to a row
+        const int set = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;
+        const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + set * 128 + 32 * half;
         const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
         uint32_t steps = 0;
         for (long long item = blockIdx.x + (long long)lane * gridDim.x; item < p.items; item += 32ll * gridDim.x) steps += (uint32_t)decode(p, (int)item).blocks;
@@ -343,13 +338,13 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             const float* stats = stats_entry(reinterpret_cast<float*>(base_ptr + C::kOffStats + slot * C::kStatBytes), row);
             const float neg = stats[0], d = stats[2];
             const auto of_row = [&](int) { return make_float4(neg, neg, d, d); };
-            if (keys == kCrossBlock) weights_in_place(t_s, t_s + 64, kCrossBlock, scale2, of_row);
-            else weights_in_place(t_s, t_s + 64, keys, scale2, of_row);
+            if (keys == kCrossBlock) weights_in_place<false>(t_s, t_s + 64, 32, scale2, of_row);
+            else weights_in_place<false>(t_s, t_s + 64, keys - 32 * half, scale2, of_row);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::kReady + set));
         }
-    } else if (warp >= 16) {
+    } else if (warp >= 28) {
         // ============================================ stores of dQ
         const int row = (warp & 3) * 32 + lane, within = row & (kRowTile - 1);
         int row_token, row_head;
@@ -391,15 +386,15 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             if (!none) ++live;
         }
     }
-    if (warp == 13 || warp == 14) {
+    if (warp == 25 || warp == 26) {
         // everything issued by this warp has finished before the tensor memory is released
-        if (elect_one()) mma_commit(bar(C::kDrain + warp - 13));
+        if (elect_one()) mma_commit(bar(C::kDrain + warp - 25));
         __syncwarp();
-        mbar_wait_warp(bar(C::kDrain + warp - 13), 0, abort_flag + 1, p.status);
+        mbar_wait_warp(bar(C::kDrain + warp - 25), 0, abort_flag + 1, p.status);
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 24) {
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
     }
@@ -409,7 +404,7 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 // A CTA has one tile of 128 keys of a group, K and V of it in shared memory, dV and dK in tensor memory, and walks a run of the group's tiles of 64 rows:
 //     S^T = K Q^T,  dP^T = V dO^T   (M128 N64)      P^T, dS^T over them, a key to a thread      dV += P^T dO,  dK += dS^T Q   (A from tensor memory)
 // Three sets of 64 + 64 columns rotate among the tiles, each with four warps of its own, so that one set's exponentials run under the others' products.
-constexpr int kKvThreads = 512;
+constexpr int kKvThreads = 896;
 constexpr uint32_t kColDV = kColAcc;
 
 template <int DP> struct KvCfg {
@@ -459,11 +454,11 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
 
     if (threadIdx.x == 0) {
         abort_flag[0] = 0; abort_flag[1] = 0;
-        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i >= C::kReady && i < C::kReady + kSets ? 4 : 1);
+        for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i >= C::kReady && i < C::kReady + kSets ? 8 : 1);
         fence_barrier_init();
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_do); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
     }
-    if (warp == 12) {
+    if (warp == 24) {
         tmem_alloc(base + C::kOffMisc, kTmemCols);
         tmem_relinquish();
     }
@@ -476,7 +471,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
     bool ok = true;
     cudaGridDependencySynchronize();                      // it may have overtaken the kernel before: statistics, copies
 
-    if (warp == 12) {
+    if (warp == 24) {
         // ============================================ loads
         int t = 0;
         if (tiles > 0 && elect_one()) {
@@ -501,7 +496,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             for (int i = t > kStages ? t - kStages : 0; i < t; ++i) mbar_wait_warp(bar(C::kFull + i % kStages), (i / kStages) & 1, abort_flag + 1, p.status);
             if (tiles > 0) mbar_wait_warp(bar(C::kKVFull), 0, abort_flag + 1, p.status);
         }
-    } else if (warp == 13) {
+    } else if (warp == 25) {
         // ============================================ S^T and dP^T
         if (tiles > 0) ok = mbar_wait_warp(bar(C::kKVFull), 0, abort_flag, p.status);
         for (int t = 0; t < tiles && ok; ++t) {
@@ -521,7 +516,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             }
             __syncwarp();
         }
-    } else if (warp == 14) {
+    } else if (warp == 26) {
         // ============================================ dV and dK
         for (int t = 0; t < tiles; ++t) {
             const uint32_t st = t % kStages, set = t % kSets, round = t / kSets;
@@ -531,20 +526,20 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
                 const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + st * C::kRowBytes), g = smem_desc_at(T::kDesc, base + C::kOffDO + st * C::kRowBytes);
                 constexpr uint32_t kIdesc = idesc_bf16_f32(kRows, DP, true);
 #pragma unroll
-                for (int kk = 0; kk < kRowTile / 16; ++kk) mma_ts(tmem + kColDV, tmem + set * 128 + 8 * kk, g + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
+                for (int kk = 0; kk < kRowTile / 16; ++kk) mma_ts(tmem + kColDV, tmem + set * 128 + weights_at(kk), g + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
 #pragma unroll
-                for (int kk = 0; kk < kRowTile / 16; ++kk) mma_ts(tmem + kColDV + DP, tmem + set * 128 + 64 + 8 * kk, q + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
+                for (int kk = 0; kk < kRowTile / 16; ++kk) mma_ts(tmem + kColDV + DP, tmem + set * 128 + 64 + weights_at(kk), q + T::kStepRows * kk, kIdesc, (t || kk) ? 1u : 0u);
                 mma_commit(bar(C::kFree + set));
                 mma_commit(bar(C::kEmpty + st));
                 if (t == tiles - 1) mma_commit(bar(C::kAccFull));
             }
             __syncwarp();
         }
-    } else if (warp < 12) {
-        // ============================================ P^T and dS^T, a key to a thread; then dV and dK
-        const int set = warp >> 2;
+    } else if (warp < 24) {
+        // ============================================ P^T and dS^T, two threads to a key; then dV and dK
+        const int set = warp >> 3, half = (warp >> 2) & 1;
         const int row = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + set * 128, t_dp = t_s + 64;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + set * 128 + 32 * half, t_dp = t_s + 64;
         const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
         for (int t = set; t < tiles; t += kSets) {
             const uint32_t st = t % kStages, round = t / kSets;
@@ -552,27 +547,27 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             if (!mbar_wait_warp(bar(C::kSFull + set), round & 1, abort_flag, p.status) || !mbar_wait_warp(bar(C::kFull + st), (t / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
             tc_fence_after();
             const float4* stats = reinterpret_cast<const float4*>(base_ptr + C::kOffStats + st * C::kStatBytes);
-            weights_in_place(t_s, t_dp, kRowTile, scale2, [&](int i) { return stats[i]; });
+            weights_in_place<true>(t_s, t_dp, 32, scale2, [&](int i) { return stats[16 * half + i]; });
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::kReady + set));
         }
-        if (ok && tiles > 0 && set < 2) {
+        if (ok && tiles > 0 && set == 0) {
             ok = mbar_wait_warp(bar(C::kAccFull), 0, abort_flag, p.status);
             tc_fence_after();
         }
         // four warps store dV, four dK
-        if (ok && set < 2) {
+        if (ok && set == 0) {
             const int key = key0 + row;
             const bool mine = key < p.L, zero = tiles <= 0 || key >= length;
-            const float scale = set == 0 ? 1.f : p.inv_sqrt_d;
-            __nv_bfloat16* dst = (set == 0 ? p.dv : p.dk) + (((long long)context * p.L + key) * p.kv_heads + kv) * p.d;
-            float* part = (set == 0 ? p.part_dv : p.part_dk) + (((long long)split * p.groups + group) * p.L + key) * DP;
+            const float scale = half == 0 ? 1.f : p.inv_sqrt_d;
+            __nv_bfloat16* dst = (half == 0 ? p.dv : p.dk) + (((long long)context * p.L + key) * p.kv_heads + kv) * p.d;
+            float* part = (half == 0 ? p.part_dv : p.part_dk) + (((long long)split * p.groups + group) * p.L + key) * DP;
 #pragma unroll
             for (int g = 0; g < DP / 32; ++g) {
                 uint32_t o[32];
                 float x[32];
-                if (tiles > 0) { tmem_ld32(tmem + lanes + kColDV + set * DP + 32 * g, o); tmem_wait_ld(); }
+                if (tiles > 0) { tmem_ld32(tmem + lanes + kColDV + half * DP + 32 * g, o); tmem_wait_ld(); }
 #pragma unroll
                 for (int e = 0; e < 32; ++e) x[e] = zero ? 0.f : __uint_as_float(o[e]) * scale;
                 if (mine && p.splits > 1) {
@@ -585,15 +580,15 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             }
         }
     }
-    if (warp == 13 || warp == 14) {
+    if (warp == 25 || warp == 26) {
         // everything issued by this warp has finished before the tensor memory is released
-        if (elect_one()) mma_commit(bar(C::kDrain + warp - 13));
+        if (elect_one()) mma_commit(bar(C::kDrain + warp - 25));
         __syncwarp();
-        mbar_wait_warp(bar(C::kDrain + warp - 13), 0, abort_flag + 1, p.status);
+        mbar_wait_warp(bar(C::kDrain + warp - 25), 0, abort_flag + 1, p.status);
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 24) {
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
     }
