@@ -41,6 +41,8 @@ constexpr int kCrossBlock = 64;           // keys of a block
 // Rows of a group (tokens x heads that share a head of keys) up to which the forward pass takes the plain pipes.  Plain pipes / tensor cores, us with the join: 1 row, 64 contexts of up to 4096, 6 heads
 // of 32 35 / 63; 2 rows, 64 x 4096, 6 heads of keys of 32 65 / 99, 16 x 4096, 2 of 64 25 / 26; 4 rows, 16 x 4096, 2 of 64 31 / 26; 8 rows 45 / 25.
 constexpr int kCrossFewRows = 2;
+// States up to which the forward pass takes a row's scores at once (rib_cross_short_sm100.cu has both sides); 128 columns of tensor memory for each of four tiles are all there is.
+constexpr int kCrossShort = 128;
 
 CrossPlan cross_plan(const CrossProblem& p);
 bool cross_padded(const CrossProblem& p);                                       // rows that TMA cannot address: copies filled up with zero channels
@@ -48,6 +50,8 @@ size_t cross_fwd_workspace(const CrossProblem& p);
 size_t cross_bwd_workspace(const CrossProblem& p);
 cudaError_t cross_fwd(CrossProblem p, cudaStream_t stream, int* launches);
 cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches);
+// Forward over up to kCrossShort keys (rib_cross_short_sm100.cu).
+cudaError_t cross_fwd_short(const CrossProblem& p, const CrossPlan& plan, cudaStream_t stream);
 // Forward of few rows (rib_cross_rows.cu), without the join of the splits, whose outputs are rows of `stride` floats.
 cudaError_t cross_fwd_rows(const CrossProblem& p, const CrossPlan& plan, float* part_out, float* part_lse, int stride, cudaStream_t stream);
 

@@ -12,7 +12,7 @@
 //   the reference, in nats; infinities, NaN) or whose values overflowed makes its item be noted, and
 //   Exact form (second pass of the same launch): a running maximum over both halves, which they tell each other through shared memory, and which moves, and with it O and the row's sum, when a
 //   block exceeds it by more than 2^8 in the exponentials.
-// (256 x 256 tokens to 1024 states, us: a thread to a row, blocks of 64 keys, one warp for all loads and products 170; the exact form for every item 179; the fast one 000.)
+// (256 x 256 tokens to 1024 states, us: a thread to a row, blocks of 64 keys, one warp for all loads and products 170; the exact form for every item 179; the fast one 135.)
 // Three buffers of scores rotate among the (block, tile) units, so that the scores of one tile are taken under the other's exponentials, and an item's output
 // is normalised and stored behind the exponentials of the next item's first block, when its last product is long complete.
 //
@@ -775,10 +775,15 @@ cudaError_t cross_fwd(CrossProblem p, cudaStream_t stream, int* launches)
         ++*launches;
     }
     float *part_out = reinterpret_cast<float*>(ws + l.part_out), *part_lse = reinterpret_cast<float*>(ws + l.part_lse);
-    if (cudaError_t e = plan.few_rows ? cross_fwd_rows(p, plan, part_out, part_lse, tile_width(p.d), stream) : tile_width(p.d) == 32 ? launch_fwd<32>(p, plan, part_out, part_lse, stream) : launch_fwd<64>(p, plan, part_out, part_lse, stream)) return e;
+    const int stride = tile_width(p.d);
+    cudaError_t e;
+    if (plan.few_rows) e = cross_fwd_rows(p, plan, part_out, part_lse, stride, stream);
+    else if (p.L <= kCrossShort) e = cross_fwd_short(p, plan, stream);
+    else e = stride == 32 ? launch_fwd<32>(p, plan, part_out, part_lse, stream) : launch_fwd<64>(p, plan, part_out, part_lse, stream);
+    if (e) return e;
     if (plan.splits > 1) {
         ++*launches;
-        return join(p, plan, part_out, part_lse, tile_width(p.d), stream);
+        return join(p, plan, part_out, part_lse, stride, stream);
     }
     return cudaSuccess;
 }
