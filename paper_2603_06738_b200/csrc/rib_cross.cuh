@@ -12,13 +12,13 @@ namespace rib {
 
 struct CrossProblem {
     const __nv_bfloat16 *q, *k, *v;       // rows of `width` channels
-    const __nv_bfloat16 *out, *dout;      // backward; rows of d channels (out) and `width` channels (dout)
+    const __nv_bfloat16 *out, *dout;      // backward; rows of d channels (out, but in the short form) and `width` channels
     const float* lse_in;                  // backward
     const int* lengths;                   // [contexts], or null: L
     __nv_bfloat16 *out_w, *dq, *dk, *dv;  // rows of d channels
     float* lse_w;                         // may be null
     int B, heads, kv_heads, d, L, contexts;
-    int width;                            // channels of a row in q, k, v and dout: d, or d rounded up to a multiple of 8 on padded copies
+    int width;                            // channels of a row in what is read by TMA: d, or d rounded up to a multiple of 8 on padded copies
     long long pixels, tokens;             // H W; tokens per context (pixels, or B pixels when the context is shared)
     int* status;
     bool exact_softmax;                   // forward: the exact form for every item
@@ -33,6 +33,7 @@ struct CrossPlan {
     int dq_tiles, dq_splits, dq_blocks_per_split;                      // dQ: tiles of two row tiles, and such runs of blocks of 64
     int key_tiles, row_splits, row_tiles_per_split;                    // dK and dV: tiles of 128 keys, runs of tiles of 64 rows
     int row_tiles, kv_rows_per_tile, kv_tokens_per_tile;
+    bool short_bwd;                                                    // backward in one kernel; dK and dV: a CTA has all keys, and row_tiles_per_split is even
     bool few_rows;                                                     // forward on the plain pipes; splits are then runs of a context's own keys
 };
 
@@ -52,11 +53,13 @@ cudaError_t cross_fwd(CrossProblem p, cudaStream_t stream, int* launches);
 cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches);
 // Forward over up to kCrossShort keys (rib_cross_short_sm100.cu).
 cudaError_t cross_fwd_short(const CrossProblem& p, const CrossPlan& plan, cudaStream_t stream);
+// Backward where cross_plan says short_bwd, without the sum of the splits (rib_cross_short_bwd_sm100.cu).
+cudaError_t cross_bwd_short(const CrossProblem& p, const CrossPlan& plan, float* part_dk, float* part_dv, cudaStream_t stream);
 // Forward of few rows (rib_cross_rows.cu), without the join of the splits, whose outputs are rows of `stride` floats.
 cudaError_t cross_fwd_rows(const CrossProblem& p, const CrossPlan& plan, float* part_out, float* part_lse, int stride, cudaStream_t stream);
 
-// Fills up rows of d channels with zeros to rows of `width`, up to four tensors in one launch (rib_cross_fwd_sm100.cu).
-struct CrossPad { const __nv_bfloat16* src[4]; __nv_bfloat16* dst[4]; long long rows[4]; int tensors, d, width; };
+// Fills up rows of d channels with zeros to rows of `width`, up to five tensors in one launch (rib_cross_fwd_sm100.cu).
+struct CrossPad { const __nv_bfloat16* src[5]; __nv_bfloat16* dst[5]; long long rows[5]; int tensors, d, width; };
 cudaError_t cross_pad(const CrossPad& args, cudaStream_t stream);
 
 namespace sm100 {

@@ -625,7 +625,7 @@ int tile_width(int d) { return d <= 32 ? 32 : 64; }
 
 int stat_tiles(const CrossPlan& plan) { return (plan.row_tiles + 1) / 2 * 2; }
 
-struct BwdLayout { size_t q, dout, k, v, stats, part_dq, part_dk, part_dv, bytes; };
+struct BwdLayout { size_t q, dout, k, v, out, stats, part_dq, part_dk, part_dv, bytes; };
 BwdLayout bwd_layout(const CrossProblem& p, const CrossPlan& plan)
 {
     BwdLayout l{};
@@ -634,8 +634,9 @@ BwdLayout bwd_layout(const CrossProblem& p, const CrossPlan& plan)
     if (cross_padded(p)) {
         const size_t width = (p.d + 7) / 8 * 8, queries = 2 * width * p.tokens * p.contexts * p.heads, keys = 2 * width * p.L * p.contexts * p.kv_heads;
         l.q = take(queries); l.dout = take(queries); l.k = take(keys); l.v = take(keys);
+        if (plan.short_bwd) l.out = take(queries);
     }
-    l.stats = take(sizeof(float) * 2 * kRowTile * stat_tiles(plan) * plan.groups);
+    if (!plan.short_bwd) l.stats = take(sizeof(float) * 2 * kRowTile * stat_tiles(plan) * plan.groups);
     const size_t row = sizeof(float) * tile_width(p.d);
     if (plan.dq_splits > 1) l.part_dq = take(row * plan.dq_splits * plan.groups * plan.rows);
     if (plan.row_splits > 1) {
@@ -693,30 +694,33 @@ cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches)
     RowStats stats{};
     stats.at = reinterpret_cast<float*>(ws + l.stats);
     stats.tokens_per_tile = plan.kv_tokens_per_tile; stats.tiles = stat_tiles(plan); stats.G = plan.G; stats.by_tokens = make_fast_div(plan.kv_tokens_per_tile);
-    PrepareParams a{};
-    a.out = p.out; a.dout = p.dout; a.lse = p.lse_in; a.stats = stats;
-    a.rows = (int)(p.tokens * p.contexts * p.heads); a.entries = plan.groups * stats.tiles * kRowTile; a.tokens = (int)p.tokens; a.pixels = (int)p.pixels;
-    a.d = p.d; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.vector = p.d % 8 == 0;
-    a.lane_bits = p.d <= 8 ? 0 : p.d <= 16 ? 1 : p.d <= 32 ? 2 : 3;
-    const int per_block = kPrepareRows * (256 >> a.lane_bits);
-    a.row_blocks = a.rows / per_block + (a.rows % per_block != 0);
-    a.by_heads = make_fast_div(p.heads); a.by_group = make_fast_div(plan.G); a.by_pixels = make_fast_div((int)p.pixels); a.by_tokens_of_context = make_fast_div((int)p.tokens);
-    a.by_tiles = make_fast_div(stats.tiles);
-    {
-        ProfileScope scope(RIB_KERNEL_CROSS_BWD_PREPARE, stream);
-        rib_cross_bwd_prepare_kernel<<<(unsigned)(a.row_blocks + (a.entries + 255) / 256), 256, 0, stream>>>(a);
+    if (plan.short_bwd) *launches = 1;
+    else {
+        PrepareParams a{};
+        a.out = p.out; a.dout = p.dout; a.lse = p.lse_in; a.stats = stats;
+        a.rows = (int)(p.tokens * p.contexts * p.heads); a.entries = plan.groups * stats.tiles * kRowTile; a.tokens = (int)p.tokens; a.pixels = (int)p.pixels;
+        a.d = p.d; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.vector = p.d % 8 == 0;
+        a.lane_bits = p.d <= 8 ? 0 : p.d <= 16 ? 1 : p.d <= 32 ? 2 : 3;
+        const int per_block = kPrepareRows * (256 >> a.lane_bits);
+        a.row_blocks = a.rows / per_block + (a.rows % per_block != 0);
+        a.by_heads = make_fast_div(p.heads); a.by_group = make_fast_div(plan.G); a.by_pixels = make_fast_div((int)p.pixels); a.by_tokens_of_context = make_fast_div((int)p.tokens);
+        a.by_tiles = make_fast_div(stats.tiles);
+        {
+            ProfileScope scope(RIB_KERNEL_CROSS_BWD_PREPARE, stream);
+            rib_cross_bwd_prepare_kernel<<<(unsigned)(a.row_blocks + (a.entries + 255) / 256), 256, 0, stream>>>(a);
+        }
+        if (cudaError_t e = cudaGetLastError()) return e;
     }
-    if (cudaError_t e = cudaGetLastError()) return e;
     p.width = p.d;
     if (cross_padded(p)) {
         CrossPad pad{};
-        pad.tensors = 4; pad.d = p.d; pad.width = (p.d + 7) / 8 * 8;
-        const __nv_bfloat16** src[4] = {&p.q, &p.dout, &p.k, &p.v};
-        const size_t off[4] = {l.q, l.dout, l.k, l.v};
-        for (int i = 0; i < 4; ++i) {
+        pad.tensors = plan.short_bwd ? 5 : 4; pad.d = p.d; pad.width = (p.d + 7) / 8 * 8;
+        const __nv_bfloat16** src[5] = {&p.q, &p.dout, &p.k, &p.v, &p.out};
+        const size_t off[5] = {l.q, l.dout, l.k, l.v, l.out};
+        for (int i = 0; i < pad.tensors; ++i) {
             pad.src[i] = *src[i];
             pad.dst[i] = reinterpret_cast<__nv_bfloat16*>(ws + off[i]);
-            pad.rows[i] = p.contexts * (i >= 2 ? (long long)p.L * p.kv_heads : p.tokens * p.heads);
+            pad.rows[i] = p.contexts * (i == 2 || i == 3 ? (long long)p.L * p.kv_heads : p.tokens * p.heads);
             *src[i] = pad.dst[i];
         }
         p.width = pad.width;
@@ -724,7 +728,7 @@ cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches)
         ++*launches;
     }
     float *part_dq = reinterpret_cast<float*>(ws + l.part_dq), *part_dk = reinterpret_cast<float*>(ws + l.part_dk), *part_dv = reinterpret_cast<float*>(ws + l.part_dv);
-    if (cudaError_t e = tile_width(p.d) == 32 ? launch_bwd<32>(p, plan, stats, part_dq, part_dk, part_dv, stream) : launch_bwd<64>(p, plan, stats, part_dq, part_dk, part_dv, stream)) return e;
+    if (cudaError_t e = plan.short_bwd ? cross_bwd_short(p, plan, part_dk, part_dv, stream) : tile_width(p.d) == 32 ? launch_bwd<32>(p, plan, stats, part_dq, part_dk, part_dv, stream) : launch_bwd<64>(p, plan, stats, part_dq, part_dk, part_dv, stream)) return e;
     SumParams s{};
     int tensors = 0;
     if (plan.dq_splits > 1) s.t[tensors++] = SumTensor{part_dq, p.dq, plan.groups * plan.rows, plan.dq_splits, plan.G, p.heads, plan.rows, p.tokens};

@@ -728,16 +728,20 @@ CrossPlan cross_plan(const CrossProblem& p)
     c.dq_tiles = (c.row_tiles + 1) / 2;
     split((long long)c.groups * c.dq_tiles, (p.L + kCrossBlock - 1) / kCrossBlock, &c.dq_splits, &c.dq_blocks_per_split);
     // dK and dV: a CTA to an SM; runs of row tiles such that the last round of CTAs is not a mostly empty one.  In us: 0.3 a tile, 3 for what a CTA begins and
-    // ends with, and the way of the partial sums to memory and back.
+    // ends with, and the way of the partial sums to memory and back.  Where one kernel takes all three gradients, runs of pairs of tiles: 1.2 a pair and block of keys, 4.
     c.key_tiles = (p.L + 127) / 128;
-    const long long units = (long long)c.groups * c.key_tiles;
+    c.short_bwd = p.L <= (p.d <= 32 ? 256 : 128);
+    const long long units = c.short_bwd ? c.groups : (long long)c.groups * c.key_tiles;
+    const int steps = c.short_bwd ? c.dq_tiles : c.row_tiles;
+    const double step = c.short_bwd ? 1.2 * c.key_tiles : 0.3, ends = c.short_bwd ? 4 : 3;
     double best = 0;
-    for (int s = 1; s <= c.row_tiles && s <= 64; ++s) {
-        const int per = (c.row_tiles + s - 1) / s, used = (c.row_tiles + per - 1) / per;
+    for (int s = 1; s <= steps && s <= 64; ++s) {
+        const int per = (steps + s - 1) / s, used = (steps + per - 1) / per;
         if (used != s) continue;
-        const double cost = (double)((units * s + kCrossSms - 1) / kCrossSms) * (0.3 * per + 3) + (s > 1 ? 3 + s * (double)c.groups * p.L * (p.d <= 32 ? 32 : 64) * 16 / 4e6 : 0);
-        if (s == 1 || cost < best) { best = cost; c.row_splits = s; c.row_tiles_per_split = per; }
+        const double cost = (double)((units * s + kCrossSms - 1) / kCrossSms) * (step * per + ends) + (s > 1 ? 3 + s * (double)c.groups * p.L * (p.d <= 32 ? 32 : 64) * 16 / 4e6 : 0);
+        if (s == 1 || cost < best) { best = cost; c.row_splits = s; c.row_tiles_per_split = c.short_bwd ? 2 * per : per; }
     }
+    if (c.short_bwd) c.dq_splits = 1;
     return c;
 }
 

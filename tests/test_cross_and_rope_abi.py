@@ -66,7 +66,7 @@ ROPE = ("B", "H", "W", "heads", "kv_heads", "d", "rot", "interleaved", "eps")
 
 def rope_args(backward, **over):
     a = dict(q=256, q_stride=256, k=512, k_stride=256, q_weight=768, k_weight=1024, per_head=0, table=1280, dq_out=1536, dk_out=1792, B=2, H=8, W=8, heads=4, kv_heads=2, d=32,
-             rot=32, interleaved=0, eps=1e-6, q_out=2048, k_out=2304, dq=2560, dq_stride=256, dk=2816, dk_stride=256, dq_weight=3072, dk_weight=3328, workspace=4096, bytes=1 << 40,
+             rot=32, interleaved=0, eps=1e-6, q_out=2048, k_out=2304, dq=2560, dq_stride=256, dk=2816, dk_stride=256, dq_weight=3088, dk_weight=3328, workspace=4096, bytes=1 << 40,
              stream=None)
     a.update(over)
     names = ("q", "q_stride", "k", "k_stride", "q_weight", "k_weight", "per_head", "table") + (

@@ -64,6 +64,8 @@ def refusals():
     x, y, weights, frequencies, grads = rope_inputs()
     table = rib.rib_rope_table(frequencies, 7, 9)
     short = torch.tensor([1], dtype=torch.int32, device="cuda")
+    many = make(L=300)
+    results = rib.rib_cross_attn_fwd(*many[:3])
     return [
         lambda: rib.rib_cross_attn_fwd(q.float(), k, v),
         lambda: rib.rib_cross_attn_fwd(q.transpose(1, 2), k, v),
@@ -78,7 +80,7 @@ def refusals():
         lambda: rib.rib_cross_attn_fwd(q, k, v, lengths=torch.tensor([1, 2], dtype=torch.int32)),
         lambda: rib.rib_cross_attn_bwd(q, k, v, out, lse, dout[..., :16]),
         lambda: rib.rib_cross_attn_bwd(q, k, v, out, lse[:1], dout),
-        lambda: rib.rib_cross_attn_bwd(q, k, v, out, lse, dout, workspace=torch.empty(256, dtype=torch.uint8, device="cuda")),
+        lambda: rib.rib_cross_attn_bwd(*many[:3], *results, many[3], workspace=torch.empty(256, dtype=torch.uint8, device="cuda")),
         lambda: rib.rib_rope_table(frequencies.double(), 7, 9),
         lambda: rib.rib_rope_table(frequencies, 0, 9),
         lambda: rib.rib_rope_table(torch.zeros(2, 33, device="cuda"), 7, 9),
