@@ -43,6 +43,16 @@ template <int DP> struct Cfg {
     static_assert(kColDQ + kDQs * DP <= kTmemCols, "tensor memory has 512 columns");
 };
 
+// A place in a ring of n and the parity of its round, without divisions.
+struct Place {
+    uint32_t at, round;
+    __device__ __forceinline__ void step(uint32_t by, uint32_t n)
+    {
+        at += by;
+        if (at >= n) { at -= n; round ^= 1u; }
+    }
+};
+
 struct Params {
     const int* lengths;
     const float* lse;
@@ -96,6 +106,9 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     const int length = p.lengths ? min(max(__ldg(p.lengths + context), 0), p.L) : p.L;
     const int first_pair = split * p.pairs_per_split, pairs = min(p.pairs - first_pair, p.pairs_per_split);
     const int blocks = (length + kKeys - 1) / kKeys, first = 2 * first_pair;
+    // one block of keys of 32 channels leaves the columns of the other's dV and dK to a third buffer of dP^T, which is then free with its buffer of S^T
+    const bool third = DP == 32 && blocks == 1;
+    auto column_dp = [&](uint32_t buf, int h) { return tmem + (!third ? kColDP + h * kRowTile : buf == 2 ? kColAcc + 2 * DP : kColDP + buf * kRowTile); };
     const int tiles = blocks ? 2 * pairs : 0, units = tiles * blocks;      // unit u: block (u / 2) mod blocks of keys, row tile 2 (u / 2 / blocks) + (u mod 2)
 
     if (warp == 16) {
@@ -136,12 +149,12 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 __syncwarp();
             }
         }
-        int b = 0, g = 0;
+        int b = 0;
+        Place unit{0u, 0u}, scores{0u, 1u}, pair{0u, 0u};      // scores.round: of the phase that frees a buffer; pair: the stage of the first of two row tiles
         for (int u = 0; u < units && ok; ++u) {
-            const int h = u & 1, t = 2 * g + h;
-            const uint32_t st = t % kStages, buf = u % 3;
-            if ((b == 0 && !mbar_wait_warp(bar(C::kFull + st), (t / kStages) & 1, abort_flag, p.status)) ||
-                (u >= 3 && !mbar_wait_warp(bar(C::kPFree + buf), (u / 3 - 1) & 1, abort_flag, p.status))) { ok = false; break; }
+            const int h = u & 1;
+            const uint32_t st = pair.at + h, buf = scores.at;
+            if ((b == 0 && !mbar_wait_warp(bar(C::kFull + st), pair.round, abort_flag, p.status)) || (u >= 3 && !mbar_wait_warp(bar(C::kPFree + buf), scores.round, abort_flag, p.status))) { ok = false; break; }
             tc_fence_after();
             const uint64_t k = smem_desc_at(T::kDesc, base + C::kOffK + b * C::kKeyBytes), v = smem_desc_at(T::kDesc, base + C::kOffV + b * C::kKeyBytes);
             const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + st * C::kRowBytes), go = smem_desc_at(T::kDesc, base + C::kOffDO + st * C::kRowBytes);
@@ -151,29 +164,32 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem + buf * kRowTile, k + T::kStepK * kk, q + T::kStepK * kk, kIdesc, kk ? 1u : 0u);
             }
             __syncwarp();
-            if (u >= 2 && !mbar_wait_warp(bar(C::kDPFree + h), (u / 2 - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+            if (!third && u >= 2 && !mbar_wait_warp(bar(C::kDPFree + h), (u / 2 - 1) & 1, abort_flag, p.status)) { ok = false; break; }
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < DP / 16; ++kk) mma_ss(tmem + kColDP + h * kRowTile, v + T::kStepK * kk, go + T::kStepK * kk, kIdesc, kk ? 1u : 0u);
-                mma_commit(bar(C::kSFull + u % 6));
+                for (int kk = 0; kk < DP / 16; ++kk) mma_ss(column_dp(buf, h), v + T::kStepK * kk, go + T::kStepK * kk, kIdesc, kk ? 1u : 0u);
+                mma_commit(bar(C::kSFull + unit.at));
             }
             __syncwarp();
-            if (h && ++b == blocks) { b = 0; ++g; }
+            unit.step(1, 6);
+            scores.step(1, 3);
+            if (h && ++b == blocks) { b = 0; pair.step(2, kStages); }
         }
     } else if (warp == 18) {
         // ============================================ dV and dK
-        int b = 0, g = 0;
+        int b = 0;
+        Place unit{0u, 0u}, scores{0u, 0u}, pair{0u, 0u};
         for (int u = 0; u < units; ++u) {
-            const int h = u & 1, t = 2 * g + h, w = u >> 1;
-            const uint32_t st = t % kStages, buf = u % 3;
-            if (!mbar_wait_warp(bar(C::kReady + u % 6), (u / 6) & 1, abort_flag, p.status)) { ok = false; break; }
+            const int h = u & 1, w = u >> 1;
+            const uint32_t st = pair.at + h, buf = scores.at;
+            if (!mbar_wait_warp(bar(C::kReady + unit.at), unit.round, abort_flag, p.status)) { ok = false; break; }
             tc_fence_after();
             if (elect_one()) {
                 const uint64_t q = smem_desc_at(T::kDesc, base + C::kOffQ + st * C::kRowBytes), go = smem_desc_at(T::kDesc, base + C::kOffDO + st * C::kRowBytes);
                 const uint64_t ds = smem_desc_at(smem_desc_const(16, 1024, kSwizzle128B), base + C::kOffDS + ((w & 1) * 2 + h) * C::kDSHalf);      // 128-byte lines of a key's 64 rows
                 constexpr uint32_t kIdesc = idesc_bf16_f32(kKeys, DP, true);
-                const uint32_t acc = tmem + kColAcc + 2 * DP * b, more = t > 0;
+                const uint32_t acc = tmem + kColAcc + 2 * DP * b, more = u >= 2 * blocks || h;      // (a block's first tile begins the sums)
 #pragma unroll
                 for (int kk = 0; kk < kRowTile / 16; ++kk) mma_ts(acc, tmem + buf * kRowTile + 32 * (kk >> 1) + 8 * (kk & 1), go + T::kStepRows * kk, kIdesc, more | (kk ? 1u : 0u));
                 mma_commit(bar(C::kPFree + buf));
@@ -184,14 +200,17 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 if (u == units - 1) mma_commit(bar(C::kAccFull));
             }
             __syncwarp();
-            if (h && ++b == blocks) { b = 0; ++g; }
+            unit.step(1, 6);
+            scores.step(1, 3);
+            if (h && ++b == blocks) { b = 0; pair.step(2, kStages); }
         }
     } else if (warp == 19) {
         // ============================================ dQ
         int b = 0, g = 0;
-        for (int w = 0; 2 * w < units; ++w) {
-            const int acc = g % C::kDQs, u = 2 * w;
-            if (!mbar_wait_warp(bar(C::kReady + u % 6), (u / 6) & 1, abort_flag, p.status) || !mbar_wait_warp(bar(C::kReady + (u + 1) % 6), ((u + 1) / 6) & 1, abort_flag, p.status) ||
+        Place unit{0u, 0u};
+        for (int w = 0; 2 * w < units; ++w, unit.step(2, 6)) {
+            const int acc = g % C::kDQs;
+            if (!mbar_wait_warp(bar(C::kReady + unit.at), unit.round, abort_flag, p.status) || !mbar_wait_warp(bar(C::kReady + unit.at + 1), unit.round, abort_flag, p.status) ||
                 (b == 0 && g >= C::kDQs && !mbar_wait_warp(bar(C::kDQFree + acc), (g / C::kDQs - 1) & 1, abort_flag, p.status))) { ok = false; break; }
             tc_fence_after();
             if (elect_one()) {
@@ -210,23 +229,24 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
         // ============================================ P^T and dS^T: a warp 32 keys and 32 rows
         // in four pieces of 16 x 16 (piece c: lanes 16 (c % 2) .., rows 16 (c / 2) ..), read as 16-lane fragments: a thread has 2 keys and 4 rows of a piece, and takes 16 words of statistics a unit.
         const int h = warp >> 3, part = (warp >> 2) & 1, quarter = warp & 3;
-        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, t_dp = tmem + lanes + kColDP + h * kRowTile + 32 * part;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
         const uint32_t line = base + C::kOffDS + h * C::kDSHalf + (quarter * 32 + 8 * ((lane >> 3) & 1) + (lane & 7)) * 128;
-        int b = 0, g = 0;
-        for (int u = h; u < units; u += 2) {
-            const int t = 2 * g + h, w = u >> 1, keys = length - b * kKeys - quarter * 32 - (lane >> 2);      // keys from this thread's first one on
-            const uint32_t st = t % kStages, t_s = tmem + lanes + (u % 3) * kRowTile + 32 * part, ds = line + (w & 1) * 2 * C::kDSHalf;
-            if (!mbar_wait_warp(bar(C::kSFull + u % 6), (u / 6) & 1, abort_flag, p.status) || (b == 0 && !mbar_wait_warp(bar(C::kStats + st), (t / kStages) & 1, abort_flag, p.status))) { ok = false; break; }
+        int b = 0;
+        uint32_t w = 0;
+        Place unit{(uint32_t)h, 0u}, tile{(uint32_t)h, 0u}, scores{(uint32_t)h, 0u};
+        for (int u = h; u < units; u += 2, ++w) {
+            const uint32_t t_s = tmem + lanes + scores.at * kRowTile + 32 * part, t_dp = column_dp(scores.at, h) + lanes + 32 * part, ds = line + (w & 1) * 2 * C::kDSHalf, ready = bar(C::kReady + unit.at), ds_free = bar(C::kDSFree + (w & 1)), ds_round = ((w >> 1) - 1) & 1;
+            if (!mbar_wait_warp(bar(C::kSFull + unit.at), unit.round, abort_flag, p.status) || (b == 0 && !mbar_wait_warp(bar(C::kStats + tile.at), tile.round, abort_flag, p.status))) { ok = false; break; }
             tc_fence_after();
-            const bool any = length - b * kKeys > quarter * 32, all = length - b * kKeys >= quarter * 32 + 32;      // (of the warp; where there are no keys, dS is zero for good)
-            if (any) {
+            const int here = length - b * kKeys - quarter * 32;      // of the warp's keys; where there are none, dS is zero for good
+            if (here > 0) {
                 auto load = [&](int c, uint32_t (&s)[8], uint32_t (&dp)[8]) {
                     const uint32_t at = ((uint32_t)(16 * (c & 1)) << 16) + 16 * (c >> 1);
                     tmem_ld_16x256b_x2(t_s + at, s);
                     tmem_ld_16x256b_x2(t_dp + at, dp);
                 };
-                const float4* stats = reinterpret_cast<const float4*>(base_ptr + C::kOffStats + st * C::kStatBytes) + 16 * part + (lane & 3);      // (-lse, -lse', -D, -D') of rows 8 i + 2 (lane mod 4), + 1: 4 i on
+                const float4* stats = reinterpret_cast<const float4*>(base_ptr + C::kOffStats + tile.at * C::kStatBytes) + 16 * part + (lane & 3);      // (-lse, -lse', -D, -D') of rows 8 i + 2 (lane mod 4), + 1: 4 i on
                 auto work = [&](int c, const uint32_t (&s)[8], const uint32_t (&dp)[8], const float4 (&x)[2], uint32_t (&pp)[4], uint32_t (&dd)[4]) {
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
@@ -239,10 +259,10 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                             pp[2 * q + r] = pack_bf16x2(e.x, e.y);
                             dd[2 * q + r] = pack_bf16x2(z.x, z.y);
                         }
-                    if (!all) {
+                    if (here < 32) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (keys <= 16 * (c & 1) + 8 * (i & 1)) dd[i] = 0u;
+                            if (here - (lane >> 2) <= 16 * (c & 1) + 8 * (i & 1)) dd[i] = 0u;
                     }
                 };
                 auto store = [&](int c, const uint32_t (&pp)[4], const uint32_t (&dd)[4]) {      // P over scores that this warp has read; dS: lanes 8 m .. 8 m + 7 name the rows of block m
@@ -251,12 +271,13 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 };
                 uint32_t s0[8], dp0[8], s1[8], dp1[8], pp[4], dd[4];
                 float4 xa[2], xb[2];
+                const bool free_yet = w < 2 || mbar_try_wait(ds_free, ds_round);      // (who read the dS before the last one)
                 load(0, s0, dp0);
                 load(1, s1, dp1);
                 xa[0] = stats[0]; xa[1] = stats[4];
                 tmem_wait_ld();
                 work(0, s0, dp0, xa, pp, dd);
-                if (w >= 2 && !mbar_wait_warp(bar(C::kDSFree + (w & 1)), (w / 2 - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+                if (!__all_sync(0xffffffffu, free_yet) && !mbar_wait_warp(ds_free, ds_round, abort_flag, p.status)) { ok = false; break; }
                 load(2, s0, dp0);
                 store(0, pp, dd);
                 xb[0] = stats[8]; xb[1] = stats[12];
@@ -277,8 +298,10 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
             } else if (lane == 0) mbar_arrive(bar(C::kDPFree + h));
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(C::kReady + u % 6));
-            if (++b == blocks) { b = 0; ++g; }
+            if (lane == 0) mbar_arrive(ready);
+            unit.step(2, 6);
+            scores.step(2, 3);
+            if (++b == blocks) { b = 0; tile.step(2, kStages); }
         }
         // eight warps store dV and dK
         if (ok && h == 0) {
@@ -381,20 +404,20 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
             const uint32_t st = t % kStages;
             if (!mbar_wait_warp(bar(C::kFull + st), (t / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
             const uint8_t* line = base_ptr + C::kOffDO + st * C::kRowBytes + row * C::kRow;
-            float sum = 0.f;
+            float2 sum[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = make_float2(0.f, 0.f);
 #pragma unroll
             for (int i = 0; i < DP / 8; ++i) {
                 const uint4 x = *reinterpret_cast<const uint4*>(line + (C::kOffO - C::kOffDO) + ((i ^ swizzle) << 4)), y = *reinterpret_cast<const uint4*>(line + ((i ^ swizzle) << 4));
                 const uint32_t o[4] = {x.x, x.y, x.z, x.w}, g[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sum = fmaf(__uint_as_float(o[e] << 16), __uint_as_float(g[e] << 16), sum);
-                    sum = fmaf(__uint_as_float(o[e] & 0xffff0000u), __uint_as_float(g[e] & 0xffff0000u), sum);
-                }
+                for (int e = 0; e < 4; ++e)
+                    sum[e] = __ffma2_rn(make_float2(__uint_as_float(o[e] << 16), __uint_as_float(o[e] & 0xffff0000u)), make_float2(__uint_as_float(g[e] << 16), __uint_as_float(g[e] & 0xffff0000u)), sum[e]);
             }
             float* at = reinterpret_cast<float*>(base_ptr + C::kOffStats + st * C::kStatBytes) + 4 * (row >> 1) + (row & 1);
             at[0] = -lse * kLog2e;
-            at[2] = -sum;
+            at[2] = -(((sum[0].x + sum[1].x) + (sum[2].x + sum[3].x)) + ((sum[0].y + sum[1].y) + (sum[2].y + sum[3].y)));
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::kStats + st));
             lse = next;

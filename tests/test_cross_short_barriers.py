@@ -109,6 +109,7 @@ class ShortBackward(Steps):
 
     def __init__(self, pairs, blocks, accs, seed):
         super().__init__([1], seed, 0, 0)
+        self.third = blocks == 1 and accs == 2
         self.pairs, self.blocks, self.accs, self.units = pairs, blocks, accs, 2 * pairs * blocks
 
     def where(self, u):
@@ -137,6 +138,7 @@ class ShortBackward(Steps):
             self.arrive(("stats", t % self.STAGES))
 
     def scores(self):
+        """S^T, then dP^T, of which there are three buffers as well, or two."""
         yield "wait", "kvfull", 0
         for u in range(self.units):
             t, b = self.where(u)
@@ -147,10 +149,12 @@ class ShortBackward(Steps):
                 assert ("dv", u - 3) in self.finished
             assert ("rows", t) in self.finished and ("rows", t + self.STAGES) not in self.issued
             yield "delay", self.delay("issue")
-            if u >= 2:
+            self.contract("scores", ("s", u), [])
+            if not self.third and u >= 2:
                 yield "wait", ("dpfree", u & 1), u // 2 - 1
-                assert all(("read", u - 2, w) in self.finished for w in range(WARPS))
-            self.contract("scores", ("s", u), [("sfull", u % 6)])
+            before = u - (3 if self.third else 2)
+            assert before < 0 or all(("read", before, w) in self.finished for w in range(WARPS))
+            self.contract("scores", ("dp", u), [("sfull", u % 6)])
 
     def keys(self):
         for u in range(self.units):
@@ -178,7 +182,7 @@ class ShortBackward(Steps):
             t, b = self.where(u)
             w = u >> 1
             yield "wait", ("sfull", u % 6), u // 6
-            assert ("s", u) in self.finished
+            assert ("s", u) in self.finished and ("dp", u) in self.finished
             if b == 0:
                 yield "wait", ("stats", t % self.STAGES), t // self.STAGES
             assert ("stats", t) in self.finished and ("stats", t + self.STAGES) not in self.finished
@@ -186,6 +190,7 @@ class ShortBackward(Steps):
             if w >= 2:
                 yield "wait", ("dsfree", w & 1), w // 2 - 1
                 assert ("dk", 2 * w - 3) in self.finished and ("dk", 2 * w - 4) in self.finished and ("dq", w - 2) in self.finished
+            assert ("dp", u + (3 if self.third else 2)) not in self.issued
             self.finished.add(("read", u, warp))
             self.arrive(("dpfree", h))
             yield "delay", self.delay("soft")
@@ -209,7 +214,7 @@ class ShortBackward(Steps):
             self.arrive(("dqfree", g % self.accs))
 
     def processes(self):
-        return [self.producer(), self.scores(), self.keys(), self.rows()] + [self.statistics(h) for h in range(2)] + [self.arithmetic(h, w) for h in range(2) for w in range(WARPS)] + [self.store(w) for w in range(4)]
+        return [self.producer(), self.scores(), self.keys(), self.rows(), self.statistics(0), self.statistics(1)] + [self.arithmetic(h, w) for h in range(2) for w in range(WARPS)] + [self.store(w) for w in range(4)]
 
     def complete(self):
         assert len([f for f in self.finished if f[0] == "out"]) == 4 * self.pairs and len([f for f in self.finished if f[0] == "end"]) == 2 * WARPS, "the warps wait for one another"
