@@ -607,6 +607,7 @@ __global__ void __launch_bounds__(256) rib_cross_bwd_sum_kernel(const __grid_con
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = 0.f;
+#pragma unroll 8
     for (int s = 0; s < t.splits; ++s) {
         const float4* src = reinterpret_cast<const float4*>(t.part + (s * t.rows + at) * p.stride + 8 * chunk);
         const float4 lo = src[0], hi = src[1];

@@ -727,13 +727,13 @@ CrossPlan cross_plan(const CrossProblem& p)
     }
     c.dq_tiles = (c.row_tiles + 1) / 2;
     split((long long)c.groups * c.dq_tiles, (p.L + kCrossBlock - 1) / kCrossBlock, &c.dq_splits, &c.dq_blocks_per_split);
-    // dK and dV: a CTA to an SM; runs of row tiles such that the last round of CTAs is not a mostly empty one.  In us: 0.3 a tile, 3 for what a CTA begins and
-    // ends with, and the way of the partial sums to memory and back.  Where one kernel takes all three gradients, runs of pairs of tiles: 1.2 a pair and block of keys, 4.
+    // dK and dV: a CTA to an SM; runs of row tiles such that the last round of CTAs is not a mostly empty one.  In us: 0.5 a tile, 3 for what a CTA begins and ends with, and the way of
+    // the partial sums to memory and back.  Where one kernel takes all three gradients, runs of pairs of tiles: 1.4 a pair and block of keys, 4.  (Nothing is known here of lengths.)
     c.key_tiles = (p.L + 127) / 128;
     c.short_bwd = p.L <= (p.d <= 32 ? 256 : 128);
     const long long units = c.short_bwd ? c.groups : (long long)c.groups * c.key_tiles;
     const int steps = c.short_bwd ? c.dq_tiles : c.row_tiles;
-    const double step = c.short_bwd ? 1.2 * c.key_tiles : 0.3, ends = c.short_bwd ? 4 : 3;
+    const double step = c.short_bwd ? 1.4 * c.key_tiles : 0.5, ends = c.short_bwd ? 4 : 3;
     double best = 0;
     for (int s = 1; s <= steps && s <= 64; ++s) {
         const int per = (steps + s - 1) / s, used = (steps + per - 1) / per;

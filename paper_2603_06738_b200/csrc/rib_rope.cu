@@ -19,10 +19,6 @@ namespace {
 using sm100::FastDiv;
 using sm100::make_fast_div;
 
-#ifndef RIB_ROPE_UNROLL
-#define RIB_ROPE_UNROLL (kBackward ? 2 : 4)
-#define RIB_ROPE_BLOCKS 2
-#endif
 constexpr int kThreads = 256, kMaxTurns = 2048, kMaxBlocks = 4 * 148, kUnrollMost = 4;
 
 struct RopeTensor {
@@ -97,9 +93,9 @@ __device__ __forceinline__ float2 twice(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 negated(float2 x) { return make_float2(-x.x, -x.y); }
 
 template <int V, bool kInterleaved, bool kBackward>
-__global__ void __launch_bounds__(kThreads, V == 8 ? RIB_ROPE_BLOCKS : 4) rib_qk_norm_rope_kernel(const __grid_constant__ RopeParams p)
+__global__ void __launch_bounds__(kThreads, V == 8 ? 2 : 4) rib_qk_norm_rope_kernel(const __grid_constant__ RopeParams p)
 {
-    constexpr int kUnroll = V == 8 ? RIB_ROPE_UNROLL : 4, kTwos = (V + 1) / 2;
+    constexpr int kUnroll = V == 8 && kBackward ? 2 : 4, kTwos = (V + 1) / 2;
     constexpr bool kOddPairs = kInterleaved && V == 1;           // a pair's channels are neighbours, and not in one word
     using W = typename Word<V>::type;
     extern __shared__ __align__(16) float turns[];               // [tile][pairs] cosines, then sines; backward, at the end: [threads][2 V] sums
@@ -142,15 +138,18 @@ __global__ void __launch_bounds__(kThreads, V == 8 ? RIB_ROPE_BLOCKS : 4) rib_qk
     const float* const cosines = turns + (kInterleaved && V > 1 ? V / 2 * unit : V * unit);
     const float* const sines = cosines + p.tile * p.pairs;
 
+    // (what is not there is not loaded, and stays the zero that it is here, or a token's of before, whose results are not kept)
+    W xa[kUnroll], xb[kUnroll], ga[kUnroll], gb[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) { xa[k] = W{}; xb[k] = W{}; ga[k] = W{}; gb[k] = W{}; }
+
     for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
         const int token0 = tile * p.tile, here = min(p.tile, p.tokens - token0);
-        W xa[kUnroll], xb[kUnroll], ga[kUnroll], gb[kUnroll];
         auto load = [&](int k0) {
 #pragma unroll
             for (int k = 0; k < kUnroll; ++k) {
                 const int token = k0 + k * p.tokens_at_once + at_once;
                 const bool there = token < here;
-                xa[k] = W{}; xb[k] = W{}; ga[k] = W{}; gb[k] = W{};
                 const __nv_bfloat16* src = x_at + (token0 + token) * x_stride;
                 const bool needed = !kBackward || norm;          // (the gradient of a row without a norm does not depend on it)
                 if (there && needed && has_a) xa[k] = __ldg(reinterpret_cast<const W*>(src + ca));
@@ -292,24 +291,27 @@ __global__ void __launch_bounds__(kThreads, V == 8 ? RIB_ROPE_BLOCKS : 4) rib_qk
 
 // dw of a tensor (or of one of its heads) from the blocks' sums: block (output of a chunk, or of all chunks), in a fixed order
 struct RopeSum { const float* part; float* dw[2]; int d, blocks, chunks, outputs, per_head, rows_per_chunk, heads, rows; };
-__global__ void __launch_bounds__(1024) rib_qk_norm_rope_sum_kernel(const RopeSum t)
+__global__ void __launch_bounds__(256) rib_qk_norm_rope_sum_kernel(const RopeSum t)
 {
-    __shared__ float sums[1024];
-    const int c = threadIdx.x & 63, run = threadIdx.x >> 6;
-    // per head: blockIdx.x is a row, in one chunk; else a tensor, in all of them
-    const int chunk = t.per_head ? blockIdx.x / t.rows_per_chunk : 0, output = t.per_head ? blockIdx.x % t.rows_per_chunk : blockIdx.x, chunks = t.per_head ? 1 : t.chunks;
-    const bool is_k = t.per_head ? (int)blockIdx.x >= t.heads : blockIdx.x == 1;
+    __shared__ float sums[256];
+    // a block has eight channels, 32 threads to each, of a row, whose sums are in one chunk, or of a tensor, in all of them
+    const int eights = (t.d + 7) / 8, which = blockIdx.x / eights, c = 8 * (blockIdx.x % eights) + (threadIdx.x & 7), run = threadIdx.x >> 3;
+    const int chunk = t.per_head ? which / t.rows_per_chunk : 0, output = t.per_head ? which % t.rows_per_chunk : which, chunks = t.per_head ? 1 : t.chunks;
+    const bool is_k = t.per_head ? which >= t.heads : which == 1;
     float* const dst = t.dw[is_k ? 1 : 0];
     cudaGridDependencySynchronize();                             // it may have overtaken the kernel before
     if (!dst) return;
     float total = 0.f;
-    if (c < t.d)
-        for (int i = run; i < chunks * t.blocks; i += 16) total += t.part[((long long)chunk * t.blocks + i) * t.outputs * t.d + output * t.d + c];
+    if (c < t.d) {
+#pragma unroll 8
+        for (int i = run; i < chunks * t.blocks; i += 32) total += t.part[((long long)chunk * t.blocks + i) * t.outputs * t.d + output * t.d + c];
+    }
     sums[threadIdx.x] = total;
     __syncthreads();
-    if (threadIdx.x < 64 && c < t.d) {
-        for (int i = 1; i < 16; ++i) total += sums[64 * i + c];
-        dst[(t.per_head ? (int)blockIdx.x - (is_k ? t.heads : 0) : 0) * t.d + c] = total;
+    if (threadIdx.x < 8 && c < t.d) {
+#pragma unroll
+        for (int i = 1; i < 32; ++i) total += sums[8 * i + threadIdx.x];
+        dst[(t.per_head ? which - (is_k ? t.heads : 0) : 0) * t.d + c] = total;
     }
 }
 
@@ -433,7 +435,7 @@ cudaError_t qk_norm_rope_bwd(const RopeProblem& p, float* workspace, int* launch
     const RopeSum s{workspace, {p.t[0].dw, p.t[1].dw}, p.d, plan.blocks, plan.chunks, p.per_head ? plan.rows_per_chunk : 2, p.per_head, plan.rows_per_chunk, p.heads, plan.rows};
     *launches = 2;
     ProfileScope scope(RIB_KERNEL_QK_NORM_ROPE_SUM, stream);
-    return launch_overtaking(rib_qk_norm_rope_sum_kernel, p.per_head ? plan.rows : 2, 1024, 0, stream, s);
+    return launch_overtaking(rib_qk_norm_rope_sum_kernel, (p.per_head ? plan.rows : 2) * ((p.d + 7) / 8), 256, 0, stream, s);
 }
 
 }  // namespace rib
