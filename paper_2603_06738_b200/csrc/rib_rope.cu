@@ -9,7 +9,7 @@
 // and walks tokens, kUnroll of them with their loads under way at once: a warp's accesses cover neighbouring rows of a token, whole lines, and weights and their gradients stay in registers.  The lanes
 // of a row share its sums by shuffles.  A block takes tiles of tokens and puts their cosines and sines into shared memory first, once for all heads.
 // (A thread to a token that walks the heads, table entries in registers: 32 lines touched by every access and few of them in flight, 16 x 96 x 96 tokens, 6 heads of 32, forward and backward 172 us
-// against 000.)
+// against 137 now.)
 #include "rib_common.cuh"
 #include "rib_sm100_common.cuh"
 
@@ -19,7 +19,11 @@ namespace {
 using sm100::FastDiv;
 using sm100::make_fast_div;
 
-constexpr int kThreads = 256, kMaxTurns = 2048, kMaxBlocks = 4 * 148, kUnrollMost = 4;
+constexpr int kThreads = 256, kMaxTurns = 2048, kUnrollMost = 4;
+// Blocks on an SM, which are all that are launched (592 blocks, in two rounds, 61 us forward and 84 backward where these take 56 and 81); tokens of a thread under way at once.  Forward of 8-channel words with two
+// blocks and four tokens 60; backward with three blocks, whose registers spill, 133.
+constexpr int blocks_of(int V, bool backward) { return V != 8 ? 4 : backward ? 2 : 3; }
+constexpr int unroll_of(int V) { return V == 8 ? 2 : 4; }
 
 struct RopeTensor {
     const __nv_bfloat16 *x, *g;          // x: tokens x_stride elements apart; g (backward): [tokens][heads][d]
@@ -93,9 +97,9 @@ __device__ __forceinline__ float2 twice(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 negated(float2 x) { return make_float2(-x.x, -x.y); }
 
 template <int V, bool kInterleaved, bool kBackward>
-__global__ void __launch_bounds__(kThreads, V == 8 ? 2 : 4) rib_qk_norm_rope_kernel(const __grid_constant__ RopeParams p)
+__global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm_rope_kernel(const __grid_constant__ RopeParams p)
 {
-    constexpr int kUnroll = V == 8 && kBackward ? 2 : 4, kTwos = (V + 1) / 2;
+    constexpr int kUnroll = unroll_of(V), kTwos = (V + 1) / 2, kFill = V == 8 && !kBackward ? 3 : 1;      // kFill: entries of the tile's cosines and sines that a thread has under way
     constexpr bool kOddPairs = kInterleaved && V == 1;           // a pair's channels are neighbours, and not in one word
     using W = typename Word<V>::type;
     extern __shared__ __align__(16) float turns[];               // [tile][pairs] cosines, then sines; backward, at the end: [threads][2 V] sums
@@ -164,6 +168,7 @@ __global__ void __launch_bounds__(kThreads, V == 8 ? 2 : 4) rib_qk_norm_rope_ker
         load(0);
         if (p.rot) {                                             // (under the loads)
             __syncthreads();                                     // the tile before has been used
+#pragma unroll kFill
             for (int e = threadIdx.x; e < here * p.pairs; e += kThreads) {
                 int token, i, image, pixel, y, x;
                 p.by_pairs.divmod(e, token, i);
@@ -334,7 +339,7 @@ struct Plan { int V, lanes, rows, rows_per_chunk, chunks, tokens_at_once, tile, 
 int lanes_of(int units) { int l = 1; while (l < units) l *= 2; return l; }
 
 // rows of a chunk and blocks along the tokens, for rows of `lanes` lanes
-void rope_grid(const RopeProblem& p, int lanes, Plan* plan)
+void rope_grid(const RopeProblem& p, int lanes, int blocks, Plan* plan)
 {
     plan->lanes = lanes;
     plan->rows = p.heads + p.kv_heads;
@@ -350,12 +355,12 @@ void rope_grid(const RopeProblem& p, int lanes, Plan* plan)
     tile = tile < plan->tokens_at_once ? plan->tokens_at_once : tile / plan->tokens_at_once * plan->tokens_at_once;
     plan->tile = (int)tile;
     plan->tiles = (int)((p.tokens + tile - 1) / tile);
-    const int cap = (kMaxBlocks + plan->chunks - 1) / plan->chunks;
+    const int cap = (148 * blocks + plan->chunks - 1) / plan->chunks;
     plan->blocks = plan->tiles < cap ? plan->tiles : cap;
 }
 
 // the widest words that every row allows
-Plan rope_plan(const RopeProblem& p)
+Plan rope_plan(const RopeProblem& p, bool backward)
 {
     auto fits = [&](int V) {
         if (p.d % V || p.rot % (2 * V)) return false;
@@ -367,7 +372,7 @@ Plan rope_plan(const RopeProblem& p)
     };
     Plan plan{};
     plan.V = fits(8) ? 8 : fits(2) ? 2 : 1;
-    rope_grid(p, lanes_of(p.rot / (2 * plan.V) + (p.d - p.rot + 2 * plan.V - 1) / (2 * plan.V)), &plan);
+    rope_grid(p, lanes_of(p.rot / (2 * plan.V) + (p.d - p.rot + 2 * plan.V - 1) / (2 * plan.V)), blocks_of(plan.V, backward), &plan);
     return plan;
 }
 
@@ -407,17 +412,18 @@ cudaError_t rope_table(const float* frequencies, int H, int W, int pairs, long l
     return cudaGetLastError();
 }
 
-cudaError_t qk_norm_rope_fwd(const RopeProblem& p, cudaStream_t stream) { return launch<false>(p, nullptr, rope_plan(p), stream); }
+cudaError_t qk_norm_rope_fwd(const RopeProblem& p, cudaStream_t stream) { return launch<false>(p, nullptr, rope_plan(p, false), stream); }
 
+constexpr int kMostBlocks = 4;
 // room for the sums of any alignment (a row has 1 to 32 lanes)
 size_t qk_norm_rope_bwd_workspace(const RopeProblem& p)
 {
     size_t most = 0;
     for (int lanes = 1; lanes <= 32; lanes *= 2) {
         Plan plan{};
-        rope_grid(p, lanes, &plan);
+        rope_grid(p, lanes, kMostBlocks, &plan);
         // (the tiles' size depends on `rot` too; they are no smaller than the tokens that are walked at once)
-        const long long tiles = (p.tokens + plan.tokens_at_once - 1) / plan.tokens_at_once, cap = (kMaxBlocks + plan.chunks - 1) / plan.chunks;
+        const long long tiles = (p.tokens + plan.tokens_at_once - 1) / plan.tokens_at_once, cap = (148 * kMostBlocks + plan.chunks - 1) / plan.chunks;
         plan.blocks = (int)(tiles < cap ? tiles : cap);
         const size_t bytes = sizeof(float) * part_floats(plan, p.d, p.per_head != 0);
         most = bytes > most ? bytes : most;
@@ -427,7 +433,7 @@ size_t qk_norm_rope_bwd_workspace(const RopeProblem& p)
 
 cudaError_t qk_norm_rope_bwd(const RopeProblem& p, float* workspace, int* launches, cudaStream_t stream)
 {
-    const Plan plan = rope_plan(p);
+    const Plan plan = rope_plan(p, true);
     const bool weights = p.t[0].dw || p.t[1].dw;
     *launches = 1;
     if (cudaError_t e = launch<true>(p, weights ? workspace : nullptr, plan, stream)) return e;
