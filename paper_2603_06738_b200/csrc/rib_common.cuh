@@ -274,13 +274,13 @@ struct ProfileScope {
 
 // Launch of a kernel that may start while the kernel before it on the stream still runs (it waits for that one's end by itself).
 template <typename Kernel, typename... Args>
-inline cudaError_t launch_overtaking(Kernel kernel, int grid, int threads, size_t smem, cudaStream_t stream, const Args&... args)
+inline cudaError_t launch_overtaking(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t stream, const Args&... args)
 {
     cudaLaunchAttribute overtake;
     overtake.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     overtake.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t config{};
-    config.gridDim = dim3((unsigned)grid);
+    config.gridDim = grid;
     config.blockDim = dim3((unsigned)threads);
     config.dynamicSmemBytes = smem;
     config.stream = stream;

@@ -74,6 +74,7 @@ struct PrepareParams {
 constexpr int kPrepareRows = 4;                      // of a thread, their loads under way at once
 __global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const __grid_constant__ PrepareParams p)
 {
+    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
     if ((int)blockIdx.x >= p.row_blocks) {            // entries that are no row
         const int e = (blockIdx.x - p.row_blocks) * 256 + threadIdx.x;
         if (e >= p.entries) return;
@@ -708,9 +709,8 @@ cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches)
         a.by_tiles = make_fast_div(stats.tiles);
         {
             ProfileScope scope(RIB_KERNEL_CROSS_BWD_PREPARE, stream);
-            rib_cross_bwd_prepare_kernel<<<(unsigned)(a.row_blocks + (a.entries + 255) / 256), 256, 0, stream>>>(a);
+            if (cudaError_t e = launch_overtaking(rib_cross_bwd_prepare_kernel, a.row_blocks + (a.entries + 255) / 256, 256, 0, stream, a)) return e;
         }
-        if (cudaError_t e = cudaGetLastError()) return e;
     }
     p.width = p.d;
     if (cross_padded(p)) {

@@ -126,6 +126,7 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
+    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
     uint32_t blk = 0, live = 0;                           // blocks and items (with blocks) so far
     uint32_t sb = warp == 3 || warp >= 12 ? 1u : 0u;      // score buffer of the next unit: (2 blk + tile) mod kBuffers
     uint32_t met = 0;                                     // times that the two warps of a row have met
@@ -615,6 +616,7 @@ __global__ void __launch_bounds__(128) rib_cross_join_kernel(const JoinParams p)
 
 __global__ void __launch_bounds__(256) rib_cross_pad_kernel(const CrossPad args)
 {
+    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
     const __nv_bfloat16* src = args.src[blockIdx.y];
     __nv_bfloat16* dst = args.dst[blockIdx.y];
     const long long words = args.rows[blockIdx.y] * (args.width / 8);
@@ -656,8 +658,7 @@ cudaError_t launch_fwd(const CrossProblem& p, const CrossPlan& plan, float* part
     a.by_pixels = make_fast_div((int)p.pixels); a.by_group = make_fast_div(plan.G); a.pixels = (int)p.pixels;
     const int grid = a.items < kCrossSms ? a.items : kCrossSms;
     ProfileScope scope(RIB_KERNEL_CROSS_FWD, stream);
-    rib_cross_fwd_kernel<DP><<<grid, kThreads, Cfg<DP>::kSmem, stream>>>(tm_q, tm_k, tm_v, tm_out, a);
-    return cudaGetLastError();
+    return launch_overtaking(rib_cross_fwd_kernel<DP>, grid, kThreads, Cfg<DP>::kSmem, stream, tm_q, tm_k, tm_v, tm_out, a);
 }
 
 cudaError_t join(const CrossProblem& p, const CrossPlan& plan, const float* part_out, const float* part_lse, int stride, cudaStream_t stream)
@@ -750,8 +751,7 @@ cudaError_t cross_pad(const CrossPad& args, cudaStream_t stream)
     long long most = 0;
     for (int i = 0; i < args.tensors; ++i) most = args.rows[i] > most ? args.rows[i] : most;
     const long long blocks = (most * (args.width / 8) + 255) / 256;
-    rib_cross_pad_kernel<<<dim3((unsigned)(blocks < 4 * kCrossSms ? blocks : 4 * kCrossSms), (unsigned)args.tensors), 256, 0, stream>>>(args);
-    return cudaGetLastError();
+    return launch_overtaking(rib_cross_pad_kernel, dim3((unsigned)(blocks < 4 * kCrossSms ? blocks : 4 * kCrossSms), (unsigned)args.tensors), 256, 0, stream, args);
 }
 
 size_t cross_fwd_workspace(const CrossProblem& p) { return fwd_layout(p, cross_plan(p)).bytes; }

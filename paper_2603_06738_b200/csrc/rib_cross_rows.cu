@@ -37,6 +37,7 @@ __global__ void __launch_bounds__(kThreads) rib_cross_rows_kernel(const __grid_c
     constexpr int kKeys = 32 / kLanes, kUnroll = kRows == 1 ? 8 : 4;                   // kKeys: of a warp at once
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = lane % kLanes, which = lane / kLanes;
     const int split = blockIdx.x % p.splits, group = blockIdx.x / p.splits, context = group / p.kv_heads, kv = group - context * p.kv_heads;
+    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
     const int length = p.lengths ? min(max(__ldg(p.lengths + context), 0), p.L) : p.L;
     // runs of equal length of the context's own keys
     const int run = (length + p.splits - 1) / p.splits, first = min(length, split * run), last = min(length, first + run);
@@ -152,11 +153,11 @@ __global__ void __launch_bounds__(kThreads) rib_cross_rows_kernel(const __grid_c
 }
 
 template <int kLanes>
-void launch_lanes(const RowsParams& a, unsigned blocks, cudaStream_t stream)
+cudaError_t launch_lanes(const RowsParams& a, unsigned blocks, cudaStream_t stream)
 {
     static_assert(kCrossFewRows == 2, "a kernel for every number of rows");
     const auto kernel = a.rows == 1 ? rib_cross_rows_kernel<kLanes, 1> : rib_cross_rows_kernel<kLanes, 2>;
-    kernel<<<blocks, kThreads, 0, stream>>>(a);
+    return launch_overtaking(kernel, blocks, kThreads, 0, stream, a);
 }
 
 }  // namespace
@@ -169,11 +170,7 @@ cudaError_t cross_fwd_rows(const CrossProblem& p, const CrossPlan& plan, float* 
     a.shared = p.tokens != p.pixels; a.pixels = (int)p.pixels; a.stride = stride; a.groups = plan.groups; a.scale_log2 = 1.4426950408889634f / sqrtf((float)p.d);
     const unsigned blocks = (unsigned)(plan.groups * plan.splits);
     ProfileScope scope(RIB_KERNEL_CROSS_FWD, stream);
-    if (p.width <= 8) launch_lanes<1>(a, blocks, stream);
-    else if (p.width <= 16) launch_lanes<2>(a, blocks, stream);
-    else if (p.width <= 32) launch_lanes<4>(a, blocks, stream);
-    else launch_lanes<8>(a, blocks, stream);
-    return cudaGetLastError();
+    return p.width <= 8 ? launch_lanes<1>(a, blocks, stream) : p.width <= 16 ? launch_lanes<2>(a, blocks, stream) : p.width <= 32 ? launch_lanes<4>(a, blocks, stream) : launch_lanes<8>(a, blocks, stream);
 }
 
 }  // namespace rib

@@ -100,7 +100,7 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
-    cudaGridDependencySynchronize();                      // it may have overtaken the kernel that makes copies
+    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
 
     const int split = blockIdx.x % p.splits, group = blockIdx.x / p.splits, context = group / p.kv_heads, kv = group - context * p.kv_heads;
     const int length = p.lengths ? min(max(__ldg(p.lengths + context), 0), p.L) : p.L;
@@ -461,9 +461,7 @@ cudaError_t launch(const CrossProblem& p, const CrossPlan& plan, float* part_dk,
     a.by_group = make_fast_div(plan.G); a.by_pixels = make_fast_div((int)p.pixels);
     ProfileScope scope(RIB_KERNEL_CROSS_BWD_DKV, stream);
     const int grid = plan.groups * plan.row_splits;
-    if (cross_padded(p)) return launch_overtaking(rib_cross_short_bwd_kernel<DP>, grid, kThreads, Cfg<DP>::kSmem, stream, tm_q, tm_do, tm_out, tm_k, tm_v, tm_dq, a);
-    rib_cross_short_bwd_kernel<DP><<<grid, kThreads, Cfg<DP>::kSmem, stream>>>(tm_q, tm_do, tm_out, tm_k, tm_v, tm_dq, a);
-    return cudaGetLastError();
+    return launch_overtaking(rib_cross_short_bwd_kernel<DP>, grid, kThreads, Cfg<DP>::kSmem, stream, tm_q, tm_do, tm_out, tm_k, tm_v, tm_dq, a);
 }
 
 }  // namespace

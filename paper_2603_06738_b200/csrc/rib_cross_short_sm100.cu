@@ -107,6 +107,7 @@ rib_cross_short_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
+    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
     Walk at(p);
 
     if (warp == 16) {
@@ -366,8 +367,7 @@ cudaError_t launch(const CrossProblem& p, const CrossPlan& plan, cudaStream_t st
     a.by_tiles = make_fast_div(plan.tiles); a.by_kv = make_fast_div(p.kv_heads); a.by_pixels = make_fast_div((int)p.pixels); a.by_group = make_fast_div(plan.G);
     const int grid = a.all_tiles < kCrossSms ? a.all_tiles : kCrossSms;
     ProfileScope scope(RIB_KERNEL_CROSS_FWD, stream);
-    rib_cross_short_fwd_kernel<DP><<<grid, kThreads, Cfg<DP>::kSmem, stream>>>(tm_q, tm_k, tm_v, tm_out, a);
-    return cudaGetLastError();
+    return launch_overtaking(rib_cross_short_fwd_kernel<DP>, grid, kThreads, Cfg<DP>::kSmem, stream, tm_q, tm_k, tm_v, tm_out, a);
 }
 
 }  // namespace

@@ -119,6 +119,7 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
     else { ca = p.rot + 2 * V * (unit - turned); cb = ca + V; }
     const bool has_a = works && ca < p.d, has_b = works && cb < p.d;
     const bool norm = works && t.w != nullptr;
+    cudaGridDependencySynchronize();                             // it may have overtaken the kernel before
     // place of a pair's two channels among the unit's 2 V
     auto place_a = [](int i) { return kInterleaved && V > 1 ? 2 * i : i; };
     auto place_b = [](int i) { return kInterleaved && V > 1 ? 2 * i + 1 : V + i; };
@@ -328,6 +329,7 @@ __global__ void __launch_bounds__(128) rib_rope_table_kernel(const float* __rest
     const long long row = e / pairs;
     const int i = (int)(e - row * pairs);
     const bool column = row >= H;
+    cudaGridDependencySynchronize();                             // it may have overtaken the kernel before
     double sine, cosine;
     sincos((double)(column ? x0 + row - H : y0 + row) * (double)frequencies[column ? pairs + i : i], &sine, &cosine);
     const double scale = column ? 1.0 : (double)magnitude;
@@ -398,8 +400,7 @@ cudaError_t launch(const RopeProblem& p, float* part, const Plan& plan, cudaStre
     const auto kernel = plan.V == 8 ? (p.interleaved ? rib_qk_norm_rope_kernel<8, true, kBackward> : rib_qk_norm_rope_kernel<8, false, kBackward>)
                       : plan.V == 2 ? (p.interleaved ? rib_qk_norm_rope_kernel<2, true, kBackward> : rib_qk_norm_rope_kernel<2, false, kBackward>)
                                     : (p.interleaved ? rib_qk_norm_rope_kernel<1, true, kBackward> : rib_qk_norm_rope_kernel<1, false, kBackward>);
-    kernel<<<grid, kThreads, smem, stream>>>(a);
-    return cudaGetLastError();
+    return launch_overtaking(kernel, grid, kThreads, smem, stream, a);
 }
 
 }  // namespace
@@ -408,8 +409,7 @@ cudaError_t rope_table(const float* frequencies, int H, int W, int pairs, long l
 {
     const long long entries = ((long long)H + W) * pairs;
     ProfileScope scope(RIB_KERNEL_ROPE_TABLE, stream);
-    rib_rope_table_kernel<<<(unsigned)((entries + 127) / 128), 128, 0, stream>>>(frequencies, H, W, pairs, y0, x0, magnitude, reinterpret_cast<float2*>(table));
-    return cudaGetLastError();
+    return launch_overtaking(rib_rope_table_kernel, (unsigned)((entries + 127) / 128), 128, 0, stream, frequencies, H, W, pairs, y0, x0, magnitude, reinterpret_cast<float2*>(table));
 }
 
 cudaError_t qk_norm_rope_fwd(const RopeProblem& p, cudaStream_t stream) { return launch<false>(p, nullptr, rope_plan(p, false), stream); }
