@@ -598,23 +598,33 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
 // ------------------------------------------------------------------------------------ sums of the splits
 struct SumTensor { const float* part; __nv_bfloat16* dst; long long rows; int splits, G, heads; long long rows_of_group, tokens; };      // rows of all groups; dst [contexts][tokens][heads][d], heads = groups of a context x G
 struct SumParams { SumTensor t[3]; int d, stride, chunks, vector, blocks; };      // blocks: of a tensor
+// kLanes threads have eight channels of a row; with eight of them each takes every eighth split, and they meet in a fixed order.
+template <int kLanes>
 __global__ void __launch_bounds__(256) rib_cross_bwd_sum_kernel(const __grid_constant__ SumParams p)
 {
     const SumTensor t = p.t[blockIdx.x / p.blocks];
-    const long long thread = (long long)(blockIdx.x % p.blocks) * 256 + threadIdx.x, at = thread / p.chunks;
-    const int chunk = (int)(thread - at * p.chunks);
-    if (at >= t.rows) return;
+    const long long thread = ((long long)(blockIdx.x % p.blocks) * 256 + threadIdx.x) / kLanes;
+    const int part = threadIdx.x % kLanes;
+    const bool mine = thread < t.rows * p.chunks;        // (the others go along: lanes meet in shuffles)
+    const long long at = mine ? thread / p.chunks : 0;
+    const int chunk = mine ? (int)(thread - at * p.chunks) : 0;
     cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = 0.f;
 #pragma unroll 8
-    for (int s = 0; s < t.splits; ++s) {
+    for (int s = part; s < t.splits; s += kLanes) {
         const float4* src = reinterpret_cast<const float4*>(t.part + (s * t.rows + at) * p.stride + 8 * chunk);
         const float4 lo = src[0], hi = src[1];
         x[0] += lo.x; x[1] += lo.y; x[2] += lo.z; x[3] += lo.w;
         x[4] += hi.x; x[5] += hi.y; x[6] += hi.z; x[7] += hi.w;
     }
+#pragma unroll
+    for (int o = kLanes / 2; o; o >>= 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], o);
+    }
+    if (!mine || part) return;
     const long long group = at / t.rows_of_group, r = at - group * t.rows_of_group, token = r / t.G;
     const int per_context = t.heads / t.G;
     const long long context = group / per_context;
@@ -743,8 +753,11 @@ cudaError_t cross_bwd(CrossProblem p, cudaStream_t stream, int* launches)
     for (int i = 0; i < tensors; ++i) most = s.t[i].rows > most ? s.t[i].rows : most;
     ++*launches;
     ProfileScope scope(RIB_KERNEL_CROSS_BWD_SUM, stream);
-    s.blocks = (int)((most * s.chunks + 255) / 256);
-    return launch_overtaking(rib_cross_bwd_sum_kernel, s.blocks * tensors, 256, 0, stream, s);
+    int splits = 0;
+    for (int i = 0; i < tensors; ++i) splits = s.t[i].splits > splits ? s.t[i].splits : splits;
+    const bool eight = splits > 8;
+    s.blocks = (int)((most * s.chunks * (eight ? 8 : 1) + 255) / 256);
+    return launch_overtaking(eight ? rib_cross_bwd_sum_kernel<8> : rib_cross_bwd_sum_kernel<1>, s.blocks * tensors, 256, 0, stream, s);
 }
 
 }  // namespace rib
