@@ -875,7 +875,7 @@ struct RopeCall { const void *q, *k; long long q_stride, k_stride; const float *
 int check_rope_shape(int B, int H, int W, int heads, int kv_heads, int d)
 {
     if (B <= 0 || H <= 0 || W <= 0 || heads <= 0 || kv_heads < 0 || d <= 0) return RIB_ERR_SHAPE;
-    if (d > 64 || heads > 65535 || kv_heads > 65535 - heads) return RIB_ERR_UNSUPPORTED;      // (a head to a row of the grid with weights per head)
+    if (d > 64 || heads > 65535 || kv_heads > 65535 - heads) return RIB_ERR_UNSUPPORTED;      // (chunks of heads are rows of the grid)
     return check_tokens(B, H, W, heads > kv_heads ? heads : kv_heads);
 }
 

@@ -1,11 +1,13 @@
-// Backward pass of the attention to states (rib_cross.cuh) for B200 (sm_100a), two kernels over tcgen05 products:
+// Backward pass of the attention to states (rib_cross.cuh) for B200 (sm_100a), for sequences that one CTA cannot hold (rib_cross_short_bwd_sm100.cu has the others): two kernels over tcgen05 products:
 //     P = exp(S - lse),   dS = P o (dO V^T - D),   D = rowsum(dO o O)
 //     dQ = dS K / sqrt(d)                      rows on the lanes, a CTA per tile of rows, walking the keys
 //     dV = P^T dO,  dK = dS^T Q / sqrt(d)      keys on the lanes, a CTA per tile of 128 keys, walking the rows
 // Each computes P for itself: an exponential more per score than one kernel for all three would take, and no sum of dQ over key tiles in memory, so that
 // every sum has one order and the results are the same from run to run.  Where there are too few tiles to fill the card, keys (dQ) or rows (dK, dV) are dealt
 // out to several CTAs, whose fp32 sums a last kernel adds.  A first kernel takes D and brings lse and D into the order in which tiles of rows read them.
-// P and dS enter the products as bf16 (a rounding of 2^-9 of each, as everywhere in this library); sums are fp32.
+// P and dS enter the products as bf16 (a rounding of 2^-9 of each, as everywhere in this library; dQ's share of it is as large as that of its own last rounding); sums are fp32.  dS in two parts would take
+// that away for a third product and half as many instructions again, where instructions and their latencies are what bounds both kernels:
+// a step of 128 x 64 scores takes 950 cycles in either, 512 of them exponentials.  256 x 256 tokens, 6 heads of 32, to 1024 states, us: statistics 13, dQ 160, dK and dV 157 (exponentials alone: 90 each).
 #include "rib_cross.cuh"
 
 namespace rib {
@@ -140,9 +142,9 @@ __global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const __grid
 
 // -------------------------------------------------------------------------------------------------- dQ
 // Work item = two tiles of rows of a group (128 lanes) x a run of its key blocks of 64; a persistent CTA walks items, whose key blocks are one stream of steps:
-//     S = Q K^T,  dP = dO V^T   (M128 N64)     P, dS over them, a row to a thread     dQ += dS K   (A from tensor memory)
-// Three sets of 64 + 64 columns rotate among the steps, each with four warps of its own, so that one set's exponentials run under the others' products; dQ has two
-// accumulators, and four warps that store one while the next item is under way.
+//     S = Q K^T,  dP = dO V^T   (M128 N64)     P, dS over them     dQ += dS K   (A from tensor memory)
+// Three sets of 64 + 64 columns rotate among the steps, each with eight warps of its own, two threads to a row (one: 172 against 167 us), so that one set's exponentials run under the others' products; dQ has
+// two accumulators, and four warps that store one while the next item is under way.
 // (The first form had four CTAs to an SM with one set of 64 columns each, S and dP one after the other: 256 x 256 tokens to 1024 states 283 us.)
 constexpr int kDqThreads = 1024, kSets = 3;
 constexpr uint32_t kTmemCols = 512, kColAcc = kSets * 128;
@@ -403,8 +405,8 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 
 // ----------------------------------------------------------------------------------------------- dK, dV
 // A CTA has one tile of 128 keys of a group, K and V of it in shared memory, dV and dK in tensor memory, and walks a run of the group's tiles of 64 rows:
-//     S^T = K Q^T,  dP^T = V dO^T   (M128 N64)      P^T, dS^T over them, a key to a thread      dV += P^T dO,  dK += dS^T Q   (A from tensor memory)
-// Three sets of 64 + 64 columns rotate among the tiles, each with four warps of its own, so that one set's exponentials run under the others' products.
+//     S^T = K Q^T,  dP^T = V dO^T   (M128 N64)      P^T, dS^T over them      dV += P^T dO,  dK += dS^T Q   (A from tensor memory)
+// Three sets of 64 + 64 columns rotate among the tiles, each with eight warps of its own, two threads to a key (one: 178 against 163 us), so that one set's exponentials run under the others' products.
 constexpr int kKvThreads = 896;
 constexpr uint32_t kColDV = kColAcc;
 

@@ -10,7 +10,11 @@
 // A CTA has a group of rows and keys and a run of the group's row tiles, two by two.  Unit of the pipeline is (row tile, block of 128 keys); three buffers of S^T and two of dP^T rotate among the units, and
 // two sets of arithmetic warps take the even and the odd row tiles, so that one set's exponentials run under the other's products.  D is taken here as well, by four warps of their own.
 // The sums over rows that several CTAs share are joined in a fixed order by the kernel that joins those of the long form: results are the same from run to run.
-// 000 against 000 us of the two kernels for long sequences and the one before them, ...
+// What sets the pace is the loop  scores -> arithmetic -> dV -> next scores of the buffer  (1800 cycles of issue, products and barriers, 2150 of arithmetic) over the three units in flight: 1375 cycles a
+// unit of 128 keys and 64 rows, of which exponentials take 512 and the products 300.  With statistics by two warps and S^T and dP^T issued by a warp each it was 1650, with dP^T beside dQ 1700; O in registers
+// instead of beside dO 1450; a third buffer of dP^T, where there is one block of keys, takes 2 %.
+// With the sums that follow, us: 16 x 96 x 96 tokens, 6 heads of 32, to 16 to 256 states 128 (the statistics, dQ, dK and dV, and sums of the long form, each a kernel: 222), 10 x 64 x 64 to one dictionary of 128
+// 42 (75), 180 x 320 to 77 48 (92).
 //
 // Roles (896 threads): warps 0-15 arithmetic (0-7 even, 8-15 odd row tiles; then dV and dK), 16 loads, 17 S^T and dP^T, 18 dV and dK (and owns the tensor memory), 19 dQ, 20-23 store dQ, 24-27 lse and D.
 // Every wait is bounded (tests/test_cross_short_barriers.py is a model of them).

@@ -40,7 +40,7 @@ def test_cross_attention_refuses(lib, over, code, backward):
 
 
 @pytest.mark.parametrize("over,code", [(dict(lse=None), -1), (dict(dout=None), -1), (dict(dq=None), -1), (dict(dk=None), -1), (dict(dv=None), -1), (dict(dout=1544), -4), (dict(dv=2306), -4),
-                                       (dict(workspace=None), -5), (dict(bytes=100), -5)])
+                                       (dict(workspace=None, L=777), -5), (dict(bytes=100, L=777), -5)])
 def test_cross_attention_backward_refuses(lib, over, code):
     assert lib.rib_cross_attn_bwd(*cross_args(True, **over)) == code
 
