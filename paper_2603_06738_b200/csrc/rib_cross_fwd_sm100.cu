@@ -12,7 +12,8 @@
 //   the reference, in nats; infinities, NaN) or whose values overflowed makes its item be noted, and
 //   Exact form (second pass of the same launch): a running maximum over both halves, which they tell each other through shared memory, and which moves, and with it O and the row's sum, when a
 //   block exceeds it by more than 2^8 in the exponentials.
-// (256 x 256 tokens to 1024 states, us: a thread to a row, blocks of 64 keys, one warp for all loads and products 170; the exact form for every item 179; the fast one 135.)
+// An eighth of the exponentials is taken on the FMA pipe, which has the time: 256 x 256 tokens to 1024 states 127 us, with none 132, with a quarter 127; heads of 64, 128 x 128 tokens 41 and 44.
+// (256 x 256 tokens to 1024 states, us: a thread to a row, blocks of 64 keys, one warp for all loads and products 170; the exact form for every item 179; the fast one, then without the FMA pipe, 135.)
 // Three buffers of scores rotate among the (block, tile) units, so that the scores of one tile are taken under the other's exponentials, and an item's output
 // is normalised and stored behind the exponentials of the next item's first block, when its last product is long complete.
 //
@@ -84,6 +85,28 @@ __device__ __forceinline__ Block block_of(const Item& c, int j)
     b.columns = (b.keys + 15) & ~15;
     b.half = ((b.columns >> 4) + 1) >> 1 << 4;
     return b;
+}
+
+// 2^x of a pair on the FMA pipe: 2^round(x) times a polynomial of degree 5 in what is left, which is 1 at 0 and off by 1e-7 on [-1/2, 1/2] (a fit of least largest error).  From 128 on and for NaN the result
+// is NaN, so that the row is redone; below -127, infinities among them, it is 0.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+__device__ __forceinline__ float2 exp2_pair(float2 x)
+{
+    const auto both = [](float v) { return make_float2(v, v); };
+    x = make_float2(min_nan(max_nan(x.x, -127.f), 128.5f), min_nan(max_nan(x.y, -127.f), 128.5f));
+    const float2 r = __fadd2_rn(x, both(12582912.f)), n = __fadd2_rn(r, both(-12582912.f)), f = __ffma2_rn(n, both(-1.f), x);      // (1.5 x 2^23: its last bits are the whole number)
+    float2 y = __ffma2_rn(f, both(0.00132647238f), both(0.00967151299f));
+    y = __ffma2_rn(f, y, both(0.0555073358f));
+    y = __ffma2_rn(f, y, both(0.240222424f));
+    y = __ffma2_rn(f, y, both(0.693147004f));
+    y = __ffma2_rn(f, y, both(1.f));
+    y = make_float2(__uint_as_float(__float_as_uint(y.x) + (__float_as_uint(r.x) << 23)), __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(r.y) << 23)));
+    return __ffma2_rn(x, both(0.f), y);                   // (the sum of a NaN's bits and its shifted ones is a number)
 }
 
 template <int DP>
@@ -448,35 +471,38 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         }
                     }
                 }
-                const float2 neg2 = make_float2(-m * p.scale_log2, -m * p.scale_log2);
+                // (exact form: the difference first, which is exact at the largest score however large that is; otherwise scores beyond 1e9 lose their row to the rounding of -m scale, and come here)
+                const float minus = fast ? 0.f : -m, below = fast ? -m * p.scale_log2 : 0.f;
+                const float2 minus2 = make_float2(minus, minus), neg2 = make_float2(below, below);
                 float2 sum_a = make_float2(0.f, 0.f), sum_b = make_float2(0.f, 0.f);
-                auto weights = [&](const uint32_t (&s)[16], uint32_t (&packed)[8]) {
+                auto weights = [&](const uint32_t (&s)[16], uint32_t (&packed)[8], bool any) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, neg2);
-                        const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                        const float2 score = make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+                        const float2 x = __ffma2_rn(any ? __fadd2_rn(score, minus2) : score, scale2, neg2);
+                        const float2 e = i == 7 ? exp2_pair(x) : make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         if (i & 1) sum_b = __fadd2_rn(sum_b, e); else sum_a = __fadd2_rn(sum_a, e);
                         packed[i] = pack_bf16x2(e.x, e.y);
                     }
                 };
                 // 64 keys, 16 at a time, the load of the next ones under the exponentials of these.  P goes into the second half of the columns, whose keys are therefore taken first, so that
                 // it lies where scores have been read, and not where the other half reads the reference from.
-                if (!idle && columns == 64 && keys == 64) {
+                if (!idle && fast && columns == 64 && keys == 64) {
                     uint32_t a[16], b[16], packed[8];
                     tmem_ld16(t_s + 48, a);
                     tmem_ld16(t_s + 32, b);
                     tmem_wait_ld();
-                    weights(a, packed);
+                    weights(a, packed, false);
                     tmem_st8(t_s + 56, packed);
                     tmem_ld16(t_s + 16, a);
-                    weights(b, packed);
+                    weights(b, packed, false);
                     tmem_wait_ld();
                     tmem_st8(t_s + 48, packed);
                     tmem_ld16(t_s, b);
-                    weights(a, packed);
+                    weights(a, packed, false);
                     tmem_wait_ld();
                     tmem_st8(t_s + 40, packed);
-                    weights(b, packed);
+                    weights(b, packed, false);
                     tmem_st8(t_s + 32, packed);
                 } else if (!idle) {
 #pragma unroll 1
@@ -489,7 +515,7 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             for (int e = 0; e < 16; ++e)
                                 if (g + e >= keys) s[e] = 0xff800000u;
                         }
-                        weights(s, packed);
+                        weights(s, packed, true);
                         tmem_st8(t_s + (columns + g) / 2, packed);
                     }
                 }

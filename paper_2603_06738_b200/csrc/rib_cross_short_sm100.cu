@@ -225,7 +225,7 @@ rib_cross_short_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 auto weights = [&](const auto& a, auto& packed) {
 #pragma unroll
                     for (int i = 0; i < (int)(sizeof(a) / 8); ++i) {
-                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), scale2, neg2);
+                        const float2 x = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), neg2), scale2);
                         const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         if (i & 1) sum_b = __fadd2_rn(sum_b, e); else sum_a = __fadd2_rn(sum_a, e);
                         packed[i] = pack_bf16x2(e.x, e.y);
@@ -252,7 +252,7 @@ rib_cross_short_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     maximum(a);
                 }
                 most = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
-                neg2 = make_float2(-most * p.scale_log2, -most * p.scale_log2);
+                neg2 = make_float2(-most, -most);
                 // the weights go where scores lie that have been read
 #pragma unroll 1
                 for (int g = 0; g < whole; g += 32) {

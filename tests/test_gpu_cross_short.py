@@ -99,3 +99,31 @@ def test_rows_behind_the_last_token_are_left_alone(heads, kv, d):
     (want, want_lse), (bound, bound_lse) = ref.forward(q, k, v)
     ref.check("out", out.t, want, bound)
     ref.check("lse", lse.t, want_lse, bound_lse)
+
+
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), 3e38])
+def test_every_key_of_longer_sequences_counts(d, what):
+    """A NaN or an infinity in any one key makes the rows that meet it NaN, whichever way that key's exponential is taken; a key whose logit is minus infinity weighs nothing."""
+    L = 160
+    q, k, v, _ = inputs(L, 2, 3, 1, 1, d, L, seed=d)
+    q[..., 0] = q[..., 0].abs() + 0.1
+    clean = rib.rib_cross_attn_fwd(q, k, v)[0]
+    for j in range(L):
+        k[j, j, 0, 0] = what
+    out = rib.rib_cross_attn_fwd(q, k, v)[0]
+    if what == 3e38:      # a finite logit, far above all others (or, with two channels' product beyond the type, infinite): all weight, or NaN
+        for j in range(L):
+            rows = out[j].flatten(0, 2)
+            assert (rows.isnan().any(-1) | (rows == v[j, j, 0]).all(-1)).all()
+    else:
+        assert out.isnan().all()
+    for j in range(L):
+        k[j, j, 0, 0] = -float("inf")
+    out, lse = rib.rib_cross_attn_fwd(q, k, v)
+    keep = ~torch.eye(L, dtype=torch.bool, device="cuda")
+    others = lambda x: torch.stack([x[j][keep[j]] for j in range(L)])  # noqa: E731
+    (want, want_lse), (bound, bound_lse) = ref.forward(q, others(k), others(v))
+    ref.check("out", out, want, bound)
+    ref.check("lse", lse, want_lse, bound_lse)
+    assert clean.isfinite().all()
