@@ -100,8 +100,8 @@ __global__ void __launch_bounds__(256) rib_cross_bwd_prepare_kernel(const __grid
         for (int k = 0; k < kPrepareRows; ++k) {
             const long long row = first + k * rows_at_once;
             const bool there = row < p.rows && 8 * part < p.d;
-            a[k] = there ? __ldg(reinterpret_cast<const uint4*>(p.out + row * p.d) + part) : make_uint4(0u, 0u, 0u, 0u);
-            b[k] = there ? __ldg(reinterpret_cast<const uint4*>(p.dout + row * p.d) + part) : make_uint4(0u, 0u, 0u, 0u);
+            a[k] = there ? *(reinterpret_cast<const uint4*>(p.out + row * p.d) + part) : make_uint4(0u, 0u, 0u, 0u);
+            b[k] = there ? *(reinterpret_cast<const uint4*>(p.dout + row * p.d) + part) : make_uint4(0u, 0u, 0u, 0u);
         }
 #pragma unroll
         for (int k = 0; k < kPrepareRows; ++k) {
@@ -181,7 +181,7 @@ __device__ __forceinline__ DqItem decode(const DqParams& p, int item)
     p.by_tiles.divmod(item, item, c.tile);
     p.by_splits.divmod(item, c.group, c.split);
     p.by_kv.divmod(c.group, c.context, c.kv);
-    c.length = p.lengths ? min(max(__ldg(p.lengths + c.context), 0), p.L) : p.L;
+    c.length = p.lengths ? min(max(p.lengths[c.context], 0), p.L) : p.L;
     c.first = c.split * p.blocks_per_split;
     c.blocks = max(0, min(c.first + p.blocks_per_split, (c.length + kCrossBlock - 1) / kCrossBlock) - c.first);
     return c;
@@ -448,13 +448,6 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + C::kOffMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kOffMisc + 4);      // [1] stays 0: used by the drain waits
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int rest = blockIdx.x;
-    const int split = rest % p.splits; rest /= p.splits;
-    const int key_tile = rest % p.key_tiles, group = rest / p.key_tiles, context = group / p.kv_heads, kv = group - context * p.kv_heads;
-    const int length = p.lengths ? min(max(__ldg(p.lengths + context), 0), p.L) : p.L;
-    const int first = split * p.tiles_per_split, key0 = key_tile * kRows;
-    const int tiles = key0 < length ? min(p.row_tiles - first, p.tiles_per_split) : 0;       // CTA-uniform
-
     if (threadIdx.x == 0) {
         abort_flag[0] = 0; abort_flag[1] = 0;
         for (int i = 0; i < C::kBars; ++i) mbar_init(bar(i), i >= C::kReady && i < C::kReady + kSets ? 8 : 1);
@@ -473,6 +466,12 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
     cudaGridDependencySynchronize();                      // it may have overtaken the kernel before: statistics, copies
+    int rest = blockIdx.x;
+    const int split = rest % p.splits; rest /= p.splits;
+    const int key_tile = rest % p.key_tiles, group = rest / p.key_tiles, context = group / p.kv_heads, kv = group - context * p.kv_heads;
+    const int length = p.lengths ? min(max(p.lengths[context], 0), p.L) : p.L;
+    const int first = split * p.tiles_per_split, key0 = key_tile * kRows;
+    const int tiles = key0 < length ? min(p.row_tiles - first, p.tiles_per_split) : 0;       // CTA-uniform
 
     if (warp == 24) {
         // ============================================ loads

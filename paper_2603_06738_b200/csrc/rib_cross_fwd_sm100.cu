@@ -67,7 +67,7 @@ __device__ __forceinline__ Item decode(const Params& p, int item)
     p.by_pairs.divmod(item, item, c.pair);
     p.by_splits.divmod(item, c.group, c.split);
     p.by_kv.divmod(c.group, c.context, c.kv);
-    c.length = p.lengths ? min(max(__ldg(p.lengths + c.context), 0), p.L) : p.L;
+    c.length = p.lengths ? min(max(p.lengths[c.context], 0), p.L) : p.L;
     c.first = c.split * p.blocks_per_split;
     c.blocks = max(0, min(c.first + p.blocks_per_split, (c.length + kKeys - 1) / kKeys) - c.first);
     return c;
@@ -639,7 +639,7 @@ __global__ void __launch_bounds__(128) rib_cross_join_kernel(const JoinParams p)
     if (!mine || part) return;
     const long long group = at / p.rows, r = at - group * p.rows, token = r / p.G;
     const int context = (int)(group / p.kv_heads), head = (int)(group - (long long)context * p.kv_heads) * p.G + (int)(r - token * p.G);
-    const bool none = p.lengths && __ldg(p.lengths + context) <= 0;
+    const bool none = p.lengths && p.lengths[context] <= 0;
     const float inverse = none ? 0.f : 1.f / total;
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = none ? 0.f : x[e] * inverse;

@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kThreads) rib_cross_rows_kernel(const __grid_c
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = lane % kLanes, which = lane / kLanes;
     const int split = blockIdx.x % p.splits, group = blockIdx.x / p.splits, context = group / p.kv_heads, kv = group - context * p.kv_heads;
     cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
-    const int length = p.lengths ? min(max(__ldg(p.lengths + context), 0), p.L) : p.L;
+    const int length = p.lengths ? min(max(p.lengths[context], 0), p.L) : p.L;
     // runs of equal length of the context's own keys
     const int run = (length + p.splits - 1) / p.splits, first = min(length, split * run), last = min(length, first + run);
     const bool has = 8 * part < p.width;
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kThreads) rib_cross_rows_kernel(const __grid_c
     for (int r = 0; r < kRows; ++r) {
         uint4 w = make_uint4(0u, 0u, 0u, 0u);
         const int token = r / p.G, head = kv * p.G + r % p.G;
-        if (has) w = __ldg(reinterpret_cast<const uint4*>(p.q + ((long long)(context * p.tokens + token) * p.heads + head) * p.width) + part);
+        if (has) w = *(reinterpret_cast<const uint4*>(p.q + ((long long)(context * p.tokens + token) * p.heads + head) * p.width) + part);
         unpack8(w, q[r]);
         m[r] = kCrossLowest; l[r] = 0.f;
 #pragma unroll
@@ -62,8 +62,8 @@ __global__ void __launch_bounds__(kThreads) rib_cross_rows_kernel(const __grid_c
         for (int u = 0; u < kUnroll; ++u) {
             const int j = j0 + u * kKeys + which;
             const bool there = has && j < last;
-            kw[u] = there ? __ldg(reinterpret_cast<const uint4*>(k_at + j * step)) : make_uint4(0u, 0u, 0u, 0u);
-            vw[u] = there ? __ldg(reinterpret_cast<const uint4*>(v_at + j * step)) : make_uint4(0u, 0u, 0u, 0u);
+            kw[u] = there ? *reinterpret_cast<const uint4*>(k_at + j * step) : make_uint4(0u, 0u, 0u, 0u);
+            vw[u] = there ? *reinterpret_cast<const uint4*>(v_at + j * step) : make_uint4(0u, 0u, 0u, 0u);
         }
         float s[kRows][kUnroll];
 #pragma unroll

@@ -107,7 +107,7 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
 
     const int split = blockIdx.x % p.splits, group = blockIdx.x / p.splits, context = group / p.kv_heads, kv = group - context * p.kv_heads;
-    const int length = p.lengths ? min(max(__ldg(p.lengths + context), 0), p.L) : p.L;
+    const int length = p.lengths ? min(max(p.lengths[context], 0), p.L) : p.L;
     const int first_pair = split * p.pairs_per_split, pairs = min(p.pairs - first_pair, p.pairs_per_split);
     const int blocks = (length + kKeys - 1) / kKeys, first = 2 * first_pair;
     // one block of keys of 32 channels leaves the columns of the other's dV and dK to a third buffer of dP^T, which is then free with its buffer of S^T
@@ -400,7 +400,7 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
             if (t >= tiles || row >= p.rows_per_tile || token >= p.tokens) return INFINITY;      // an entry that is no row: a weight of 0 (and rows of zeros)
             int image = context, pixel = token;
             if (p.shared) p.by_pixels.divmod(token, image, pixel);
-            return __ldg(p.lse + ((long long)image * p.heads + head) * p.pixels + pixel);
+            return p.lse[((long long)image * p.heads + head) * p.pixels + pixel];
         };
         float lse = ask(h), next = ask(h + 2);
         for (int t = h; t < tiles; t += 2) {

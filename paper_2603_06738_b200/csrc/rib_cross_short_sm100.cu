@@ -50,7 +50,7 @@ struct Walk {
     __device__ __forceinline__ void enter(const Params& p)
     {
         p.by_kv.divmod(group, context, kv);
-        length = p.lengths ? min(max(__ldg(p.lengths + context), 0), p.L) : p.L;
+        length = p.lengths ? min(max(p.lengths[context], 0), p.L) : p.L;
         if (length) ++kvs;
     }
     __device__ __forceinline__ Walk(const Params& p) : number(0), kvs(0)

@@ -8,6 +8,7 @@
 // Bound by memory: 4 bytes a channel forward, 6 backward.  A thread has a unit of 2 V channels - V pairs: two runs of V channels rot / 2 apart - of one row (a head of q or k)
 // and walks tokens, kUnroll of them with their loads under way at once: a warp's accesses cover neighbouring rows of a token, whole lines, and weights and their gradients stay in registers.  The lanes
 // of a row share its sums by shuffles.  A block takes tiles of tokens and puts their cosines and sines into shared memory first, once for all heads.
+// (Plain loads, not the read-only path: a kernel may start under the one that makes its inputs, and waits for its end.)
 // (A thread to a token that walks the heads, table entries in registers: 32 lines touched by every access and few of them in flight, 16 x 96 x 96 tokens, 6 heads of 32, forward and backward 172 us
 // against 137 now.)
 #include "rib_common.cuh"
@@ -126,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
     Pairs<V> w, dw;
     {
         const float* src = t.w + (p.per_head ? head * p.d : 0);
-        auto weight = [&](int place) { return norm && (place < V ? has_a : has_b) ? __ldg(src + (place < V ? ca + place : cb + place - V)) : 1.f; };
+        auto weight = [&](int place) { return norm && (place < V ? has_a : has_b) ? src[place < V ? ca + place : cb + place - V] : 1.f; };
 #pragma unroll
         for (int i = 0; i < kTwos; ++i) {
             w.a[i] = make_float2(weight(place_a(2 * i)), V > 1 ? weight(place_a(2 * i + 1)) : 0.f);
@@ -157,12 +158,12 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
                 const bool there = token < here;
                 const __nv_bfloat16* src = x_at + (token0 + token) * x_stride;
                 const bool needed = !kBackward || norm;          // (the gradient of a row without a norm does not depend on it)
-                if (there && needed && has_a) xa[k] = __ldg(reinterpret_cast<const W*>(src + ca));
-                if (there && needed && has_b) xb[k] = __ldg(reinterpret_cast<const W*>(src + cb));
+                if (there && needed && has_a) xa[k] = *reinterpret_cast<const W*>(src + ca);
+                if (there && needed && has_b) xb[k] = *reinterpret_cast<const W*>(src + cb);
                 if constexpr (kBackward) {
                     const __nv_bfloat16* grad = g_at + (long long)(token0 + token) * g_stride;
-                    if (there && has_a) ga[k] = __ldg(reinterpret_cast<const W*>(grad + ca));
-                    if (there && has_b) gb[k] = __ldg(reinterpret_cast<const W*>(grad + cb));
+                    if (there && has_a) ga[k] = *reinterpret_cast<const W*>(grad + ca);
+                    if (there && has_b) gb[k] = *reinterpret_cast<const W*>(grad + cb);
                 }
             }
         };
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
                 p.by_pairs.divmod(e, token, i);
                 p.by_pixels.divmod(token0 + token, image, pixel);
                 p.by_w.divmod(pixel, y, x);
-                const float2 a = __ldg(p.table + (long long)y * p.pairs + i), b = __ldg(p.table + (long long)(p.H + x) * p.pairs + i);
+                const float2 a = p.table[(long long)y * p.pairs + i], b = p.table[(long long)(p.H + x) * p.pairs + i];
                 turns[e] = a.x * b.x - a.y * b.y;
                 turns[p.tile * p.pairs + e] = a.y * b.x + a.x * b.y;
             }
