@@ -455,7 +455,7 @@ int rib_window_attn_bwd_bucketed_checkpointed(const rib_checkpoint* saved, const
  * rib_qk_norm_rope_fwd:
  *   q, k        : bf16, token t of a tensor at element t * q_stride (k_stride), its heads behind one another ([heads][d], [kv_heads][d]): slices of the output of one
  *                 projection need no copy.  Strides at least heads * d.  k may be NULL (kv_heads = 0).  Aligned to 2 bytes; the widest words that pointers,
- *                 strides, d and rot allow are used (16 bytes: all of them multiples of 16 bytes, rot a multiple of 16; else 4, else 2).
+ *                 strides, d and rot allow are used (16 bytes: all of them multiples of 16 bytes, rot a multiple of 16; 8 bytes likewise, rot a multiple of 8; else 4, else 2).
  *   q_weight, k_weight : fp32 [d], or [heads][d] and [kv_heads][d] with weight_per_head; NULL: that tensor is not normalised.
  *   table       : as above; NULL with rot = 0: no rotation.
  *   q_out, k_out: bf16 [B][H][W][heads][d], [B][H][W][kv_heads][d], overwritten.

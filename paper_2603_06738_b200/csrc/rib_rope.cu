@@ -21,10 +21,11 @@ using sm100::FastDiv;
 using sm100::make_fast_div;
 
 constexpr int kThreads = 256, kMaxTurns = 2048, kUnrollMost = 4;
-// Blocks on an SM, which are all that are launched (592 blocks, in two rounds, 61 us forward and 84 backward where these take 56 and 81); tokens of a thread under way at once.  Forward of 8-channel words with two
-// blocks and four tokens 60; backward with three blocks, whose registers spill, 133.
-constexpr int blocks_of(int V, bool backward) { return V != 8 ? 4 : backward ? 2 : 3; }
-constexpr int unroll_of(int V) { return V == 8 ? 2 : 4; }
+// Blocks on an SM, which are all that are launched, and tokens of a thread under way at once; us forward / backward on 16 x 96 x 96 tokens, 6 heads.  Words of 8 channels, heads of 32: 56 / 81 (592 blocks in two
+// rounds 61 / 84; two blocks and four tokens forward 60; three blocks backward, whose registers spill, 133).  Words of 4, heads of 24: 61 / 87 (words of 2 there 108 / 149; four tokens forward 67; three blocks and
+// two tokens backward 96).  Words of 2, heads of 20: 108 / 150 (six blocks, whose registers spill, 135 / 220; two tokens 125 / 190).
+constexpr int blocks_of(int V, bool backward) { return V == 8 ? (backward ? 2 : 3) : V == 4 && backward ? 2 : 4; }
+constexpr int unroll_of(int V, bool backward) { return V == 8 || (V == 4 && !backward) ? 2 : 4; }
 
 struct RopeTensor {
     const __nv_bfloat16 *x, *g;          // x: tokens x_stride elements apart; g (backward): [tokens][heads][d]
@@ -44,6 +45,7 @@ struct RopeParams {
 
 template <int V> struct Word;
 template <> struct Word<8> { using type = uint4; };
+template <> struct Word<4> { using type = uint2; };
 template <> struct Word<2> { using type = uint32_t; };
 template <> struct Word<1> { using type = unsigned short; };
 
@@ -100,7 +102,7 @@ __device__ __forceinline__ float2 negated(float2 x) { return make_float2(-x.x, -
 template <int V, bool kInterleaved, bool kBackward>
 __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm_rope_kernel(const __grid_constant__ RopeParams p)
 {
-    constexpr int kUnroll = unroll_of(V), kTwos = (V + 1) / 2, kFill = V == 8 && !kBackward ? 3 : 1;      // kFill: entries of the tile's cosines and sines that a thread has under way
+    constexpr int kUnroll = unroll_of(V, kBackward), kTwos = (V + 1) / 2, kFill = V == 8 && !kBackward ? 3 : 1;      // kFill: entries of the tile's cosines and sines that a thread has under way
     constexpr bool kOddPairs = kInterleaved && V == 1;           // a pair's channels are neighbours, and not in one word
     using W = typename Word<V>::type;
     extern __shared__ __align__(16) float turns[];               // [tile][pairs] cosines, then sines; backward, at the end: [threads][2 V] sums
@@ -200,6 +202,9 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
                             c[2 * i] = make_float2(u.x, u.y); c[2 * i + 1] = make_float2(u.z, u.w);
                             s[2 * i] = make_float2(v.x, v.y); s[2 * i + 1] = make_float2(v.z, v.w);
                         }
+                    } else if constexpr (V == 4) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) { c[i] = *reinterpret_cast<const float2*>(cp + i * second); s[i] = *reinterpret_cast<const float2*>(sp + i * second); }
                     } else {
                         c[0] = make_float2(cp[0], V > 1 ? cp[second] : 0.f);
                         s[0] = make_float2(sp[0], V > 1 ? sp[second] : 0.f);
@@ -374,7 +379,7 @@ Plan rope_plan(const RopeProblem& p, bool backward)
         return true;
     };
     Plan plan{};
-    plan.V = fits(8) ? 8 : fits(2) ? 2 : 1;
+    plan.V = fits(8) ? 8 : fits(4) ? 4 : fits(2) ? 2 : 1;
     rope_grid(p, lanes_of(p.rot / (2 * plan.V) + (p.d - p.rot + 2 * plan.V - 1) / (2 * plan.V)), blocks_of(plan.V, backward), &plan);
     return plan;
 }
@@ -399,6 +404,7 @@ cudaError_t launch(const RopeProblem& p, float* part, const Plan& plan, cudaStre
     if (kBackward && part && smem < sizeof(float) * kThreads * 2 * plan.V) smem = sizeof(float) * kThreads * 2 * plan.V;
     ProfileScope scope(kBackward ? RIB_KERNEL_QK_NORM_ROPE_BWD : RIB_KERNEL_QK_NORM_ROPE_FWD, stream);
     const auto kernel = plan.V == 8 ? (p.interleaved ? rib_qk_norm_rope_kernel<8, true, kBackward> : rib_qk_norm_rope_kernel<8, false, kBackward>)
+                      : plan.V == 4 ? (p.interleaved ? rib_qk_norm_rope_kernel<4, true, kBackward> : rib_qk_norm_rope_kernel<4, false, kBackward>)
                       : plan.V == 2 ? (p.interleaved ? rib_qk_norm_rope_kernel<2, true, kBackward> : rib_qk_norm_rope_kernel<2, false, kBackward>)
                                     : (p.interleaved ? rib_qk_norm_rope_kernel<1, true, kBackward> : rib_qk_norm_rope_kernel<1, false, kBackward>);
     return launch_overtaking(kernel, grid, kThreads, smem, stream, a);

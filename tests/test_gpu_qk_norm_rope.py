@@ -236,3 +236,13 @@ def test_scaled_frequencies():
     turns = 1024 * whole / (2 * math.pi)
     assert torch.allclose(parts[turns >= 32], whole[turns >= 32]) and torch.allclose(parts[turns <= 1], whole[turns <= 1] / 4)
     assert ((parts <= whole) & (parts >= whole / 4 * (1 - 1e-6))).all()
+
+
+@pytest.mark.parametrize("d,rot", [(24, 24), (40, 40), (56, 24), (32, 8), (8, 8), (20, 8), (12, 8), (44, 40), (28, 24), (60, 56), (36, 0), (4, 0), (12, 0)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("per_head", [False, True])
+def test_words_of_four_channels(d, rot, interleaved, per_head):
+    """Widths and rotated parts that are multiples of 4 and 8, not of 8 and 16."""
+    check_both(2, 13, 17, 5, 3, d, rot, interleaved=interleaved, per_head=per_head, seed=d + rot)
+    check_both(1, 64, 90, 2, 2, d, rot, interleaved=interleaved, per_head=per_head, seed=rot)
+    check_both(2, 6, 5, 3, 1, d, rot, interleaved=interleaved, per_head=per_head, normed=False, seed=d)
