@@ -4,7 +4,7 @@
 //     dV = P^T dO,  dK = dS^T Q / sqrt(d)      keys on the lanes, a CTA per tile of 128 keys, walking the rows
 // Each computes P for itself: an exponential more per score than one kernel for all three would take, and no sum of dQ over key tiles in memory, so that
 // every sum has one order and the results are the same from run to run.  Where there are too few tiles to fill the card, keys (dQ) or rows (dK, dV) are dealt
-// out to several CTAs, whose fp32 sums a last kernel adds.  A first kernel takes D and brings lse and D into the order in which tiles of rows read them.
+// out to several CTAs, whose fp32 sums a last kernel adds.  dQ runs beside dK and dV, on the SMs that those leave free.  A first kernel takes D and brings lse and D into the order in which tiles of rows read them.
 // P and dS enter the products as bf16 (a rounding of 2^-9 of each, as everywhere in this library; dQ's share of it is as large as that of its own last rounding); sums are fp32.  dS in two parts would take
 // that away for a third product and half as many instructions again, where instructions and their latencies are what bounds both kernels:
 // a step of 128 x 64 scores takes 950 cycles in either, 512 of them exponentials.  256 x 256 tokens, 6 heads of 32, to 1024 states, us: statistics 13, dQ 160, dK and dV 157 (exponentials alone: 90 each).
@@ -222,7 +222,7 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
-    cudaGridDependencySynchronize();                      // it may have overtaken the kernel before: statistics, copies
+    // (It runs beside the kernel for dK and dV, which let it start when statistics and copies were there: nothing to wait for but at the end.)
 
     if (warp == 24) {
         // ============================================ loads
@@ -401,6 +401,7 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
     }
+    if (blockIdx.x == gridDim.x - 1) cudaGridDependencySynchronize();      // what comes behind this kernel comes behind the one beside it too: its last CTA ends after that
 }
 
 // ----------------------------------------------------------------------------------------------- dK, dV
@@ -466,6 +467,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
     cudaGridDependencySynchronize();                      // it may have overtaken the kernel before: statistics, copies
+    cudaTriggerProgrammaticLaunchCompletion();            // dQ needs no more than those, and has SMs that this kernel leaves free
     int rest = blockIdx.x;
     const int split = rest % p.splits; rest /= p.splits;
     const int key_tile = rest % p.key_tiles, group = rest / p.key_tiles, context = group / p.kv_heads, kv = group - context * p.kv_heads;
@@ -680,18 +682,20 @@ cudaError_t launch_bwd(const CrossProblem& p, const CrossPlan& plan, const RowSt
     a.row_tiles = stats.tiles; a.blocks_per_split = plan.dq_blocks_per_split; a.splits = plan.dq_splits; a.items = plan.groups * plan.dq_splits * plan.dq_tiles; a.vector = p.d % 8 == 0;
     a.tokens = p.tokens; a.rows = plan.rows; a.groups = plan.groups; a.scale_log2 = scale_log2; a.inv_sqrt_d = inv_sqrt_d;
     a.by_tiles = make_fast_div(plan.dq_tiles); a.by_splits = make_fast_div(plan.dq_splits); a.by_kv = make_fast_div(p.kv_heads); a.by_group = make_fast_div(plan.G);
-    const int grid = a.items < kCrossSms ? a.items : kCrossSms;
-    {
-        ProfileScope scope(RIB_KERNEL_CROSS_BWD_DQ, stream);
-        if (cudaError_t e = launch_overtaking(rib_cross_bwd_dq_kernel<DP>, grid, kDqThreads, DqCfg<DP>::kSmem, stream, tm_q, tm_do, tm_k, tm_v, a)) return e;
-    }
     KvParams b{};
     b.lengths = p.lengths; b.stats = stats.at; b.dk = p.dk; b.dv = p.dv; b.part_dk = part_dk; b.part_dv = part_dv; b.status = p.status;
     b.d = p.d; b.L = p.L; b.kv_heads = p.kv_heads; b.G = plan.G; b.key_tiles = plan.key_tiles; b.splits = plan.row_splits; b.row_tiles = plan.row_tiles; b.stat_tiles = stats.tiles;
     b.tiles_per_split = plan.row_tiles_per_split; b.rows_per_tile = plan.kv_rows_per_tile; b.tokens_per_tile = plan.kv_tokens_per_tile; b.vector = p.d % 8 == 0;
     b.groups = plan.groups; b.scale_log2 = scale_log2; b.inv_sqrt_d = inv_sqrt_d;
-    ProfileScope scope(RIB_KERNEL_CROSS_BWD_DKV, stream);
-    return launch_overtaking(rib_cross_bwd_dkv_kernel<DP>, plan.groups * plan.key_tiles * plan.row_splits, kKvThreads, KvCfg<DP>::kSmem, stream, tm_q, tm_do, kv_k, kv_v, b);
+    {
+        ProfileScope scope(RIB_KERNEL_CROSS_BWD_DKV, stream);
+        if (cudaError_t e = launch_overtaking(rib_cross_bwd_dkv_kernel<DP>, plan.groups * plan.key_tiles * plan.row_splits, kKvThreads, KvCfg<DP>::kSmem, stream, tm_q, tm_do, kv_k, kv_v, b)) return e;
+    }
+    // It begins on SMs that the kernel before it leaves free.  Contexts of their own lengths leave it CTAs without keys, and those SMs for longer: runs of half the length then, so that they take more of them
+    // (us of both with the statistics, one run an SM / two: 4 x 48 x 48 tokens, 8 heads of 64 on 2, to 512 to 2048 states 129 / 114, 16 x 64 x 64, 4 heads of 32, to up to 512 109 / 102; full contexts of 2048 161 / 164).
+    const int most = (p.lengths ? 2 : 1) * kCrossSms, grid = a.items < most ? a.items : most;
+    ProfileScope scope(RIB_KERNEL_CROSS_BWD_DQ, stream);
+    return launch_overtaking(rib_cross_bwd_dq_kernel<DP>, grid, kDqThreads, DqCfg<DP>::kSmem, stream, tm_q, tm_do, tm_k, tm_v, a);
 }
 
 }  // namespace
