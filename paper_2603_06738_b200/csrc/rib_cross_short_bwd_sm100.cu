@@ -63,13 +63,26 @@ struct Params {
     __nv_bfloat16 *dq, *dk, *dv;
     float *part_dk, *part_dv;            // splits > 1: [splits][groups][L][DP]
     int* status;
-    int d, L, heads, kv_heads, G, splits, pairs, pairs_per_split, rows_per_tile, tokens_per_tile, vector, tma_out, tokens, pixels, shared;
+    int d, L, heads, kv_heads, G, splits, pairs, pairs_per_split, rows_per_tile, tokens_per_tile, vector, tma_out, tokens, pixels, shared, contexts;
     long long groups;
     float scale_log2, inv_sqrt_d;
     FastDiv by_group, by_pixels;
 };
 
-template <int DP>
+// The context of a rank when those of more blocks of keys come first (by a whole warp).
+__device__ __forceinline__ int context_of_rank(const Params& p, int rank, int lane)
+{
+    for (int want = 2; want >= 0; --want)
+        for (int c0 = 0; c0 < p.contexts; c0 += 32) {
+            const int c = c0 + lane, length = c < p.contexts ? min(max(p.lengths[c], 0), p.L) : -kKeys;
+            const uint32_t those = __ballot_sync(0xffffffffu, (length + kKeys - 1) / kKeys == want && c < p.contexts);
+            if (rank < __popc(those)) return c0 + __ffs(__ballot_sync(0xffffffffu, (those >> lane & 1u) && __popc(those & ((1u << lane) - 1u)) == rank)) - 1;
+            rank -= __popc(those);
+        }
+    return 0;
+}
+
+template <int DP, bool kLongFirst>
 __global__ void __launch_bounds__(kThreads, 1)
 rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ CUtensorMap tm_k,
                            const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_dq, const __grid_constant__ Params p)
@@ -106,7 +119,19 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     bool ok = true;
     cudaGridDependencySynchronize();                      // it may have overtaken the kernel before
 
-    const int split = blockIdx.x % p.splits, group = blockIdx.x / p.splits, context = group / p.kv_heads, kv = group - context * p.kv_heads;
+    const int split = blockIdx.x % p.splits;
+    int group = blockIdx.x / p.splits, context = group / p.kv_heads;
+    const int kv = group - context * p.kv_heads;
+    if constexpr (kLongFirst) {
+        volatile int* shared_context = reinterpret_cast<volatile int*>(base_ptr + C::kOffMisc + 12);
+        if (warp == 0) {
+            const int c = context_of_rank(p, context, lane);
+            if (lane == 0) *shared_context = c;
+        }
+        __syncthreads();
+        context = *shared_context;
+        group = context * p.kv_heads + kv;
+    }
     const int length = p.lengths ? min(max(p.lengths[context], 0), p.L) : p.L;
     const int first_pair = split * p.pairs_per_split, pairs = min(p.pairs - first_pair, p.pairs_per_split);
     const int blocks = (length + kKeys - 1) / kKeys, first = 2 * first_pair;
@@ -442,7 +467,7 @@ rib_cross_short_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     }
 }
 
-template <int DP>
+template <int DP, bool kLongFirst>
 cudaError_t launch(const CrossProblem& p, const CrossPlan& plan, float* part_dk, float* part_dv, cudaStream_t stream)
 {
     if (!encode_fn()) return cudaErrorNotSupported;
@@ -456,23 +481,26 @@ cudaError_t launch(const CrossProblem& p, const CrossPlan& plan, float* part_dk,
     if (tma_out && !cross_rows_map(&tm_dq, p.dq, p.contexts, p.tokens, p.heads, p.d, DP, plan.G, 32 / plan.G)) return cudaErrorInvalidValue;
     static KernelSetup setup;
     int sms = 0;
-    if (cudaError_t e = setup.prepare(rib_cross_short_bwd_kernel<DP>, Cfg<DP>::kSmem, &sms)) return e;
+    if (cudaError_t e = setup.prepare(rib_cross_short_bwd_kernel<DP, kLongFirst>, Cfg<DP>::kSmem, &sms)) return e;
     Params a{};
     a.lengths = p.lengths; a.lse = p.lse_in; a.dq = p.dq; a.dk = p.dk; a.dv = p.dv; a.part_dk = part_dk; a.part_dv = part_dv; a.status = p.status;
     a.d = p.d; a.L = p.L; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.splits = plan.row_splits; a.pairs = plan.dq_tiles; a.pairs_per_split = plan.row_tiles_per_split / 2;
     a.rows_per_tile = plan.kv_rows_per_tile; a.tokens_per_tile = plan.kv_tokens_per_tile; a.vector = p.d % 8 == 0; a.tma_out = tma_out; a.tokens = (int)p.tokens; a.pixels = (int)p.pixels;
-    a.shared = p.tokens != p.pixels; a.groups = plan.groups; a.scale_log2 = kLog2e / sqrtf((float)p.d); a.inv_sqrt_d = 1.f / sqrtf((float)p.d);
+    a.shared = p.tokens != p.pixels; a.contexts = p.contexts; a.groups = plan.groups; a.scale_log2 = kLog2e / sqrtf((float)p.d); a.inv_sqrt_d = 1.f / sqrtf((float)p.d);
     a.by_group = make_fast_div(plan.G); a.by_pixels = make_fast_div((int)p.pixels);
     ProfileScope scope(RIB_KERNEL_CROSS_BWD_DKV, stream);
     const int grid = plan.groups * plan.row_splits;
-    return launch_overtaking(rib_cross_short_bwd_kernel<DP>, grid, kThreads, Cfg<DP>::kSmem, stream, tm_q, tm_do, tm_out, tm_k, tm_v, tm_dq, a);
+    return launch_overtaking(rib_cross_short_bwd_kernel<DP, kLongFirst>, grid, kThreads, Cfg<DP>::kSmem, stream, tm_q, tm_do, tm_out, tm_k, tm_v, tm_dq, a);
 }
 
 }  // namespace
 
 cudaError_t cross_bwd_short(const CrossProblem& p, const CrossPlan& plan, float* part_dk, float* part_dv, cudaStream_t stream)
 {
-    return p.d <= 32 ? launch<32>(p, plan, part_dk, part_dv, stream) : launch<64>(p, plan, part_dk, part_dv, stream);
+    // One or two blocks of keys, as the contexts' lengths have it: CTAs of two first, so that none of them begins last (16 x 96 x 96 tokens, 6 heads of 32, to 16 to 256 states in no order 117 us, 137 as they come).
+    // With many contexts their order evens out by itself.
+    const bool long_first = p.lengths && p.L > kKeys && p.contexts > 1 && p.contexts <= 64;
+    return p.d > 32 ? launch<64, false>(p, plan, part_dk, part_dv, stream) : long_first ? launch<32, true>(p, plan, part_dk, part_dv, stream) : launch<32, false>(p, plan, part_dk, part_dv, stream);
 }
 
 }  // namespace rib

@@ -127,3 +127,14 @@ def test_every_key_of_longer_sequences_counts(d, what):
     ref.check("out", out, want, bound)
     ref.check("lse", lse, want_lse, bound_lse)
     assert clean.isfinite().all()
+
+
+@pytest.mark.parametrize("contexts", [1, 2, 5, 31, 32, 33, 63, 64, 65, 70])
+def test_contexts_of_one_and_two_blocks_of_keys(contexts):
+    """Whatever the order of the lengths: each context's gradients are its own, those without keys among them."""
+    g = torch.Generator(device="cuda").manual_seed(contexts)
+    q, k, v, dout = inputs(contexts, 5, 9, 3, 3, 32, 250, seed=contexts)
+    lengths = torch.randint(0, 251, (contexts,), dtype=torch.int32, device="cuda", generator=g)
+    lengths[torch.rand(contexts, device="cuda", generator=g) < 0.2] = 0
+    for cut in (lengths, lengths.sort().values, lengths.sort(descending=True).values, torch.full_like(lengths, 128), torch.full_like(lengths, 129), torch.zeros_like(lengths)):
+        check_all(q, k, v, dout, cut.contiguous())
