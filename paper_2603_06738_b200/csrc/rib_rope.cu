@@ -10,7 +10,7 @@
 // of a row share its sums by shuffles.  A block takes tiles of tokens and puts their cosines and sines into shared memory first, once for all heads.
 // (Plain loads, not the read-only path: a kernel may start under the one that makes its inputs, and waits for its end.)
 // (A thread to a token that walks the heads, table entries in registers: 32 lines touched by every access and few of them in flight, 16 x 96 x 96 tokens, 6 heads of 32, forward and backward 172 us
-// against 137 now.)
+// against 136 now.)
 #include "rib_common.cuh"
 #include "rib_sm100_common.cuh"
 
@@ -21,9 +21,9 @@ using sm100::FastDiv;
 using sm100::make_fast_div;
 
 constexpr int kThreads = 256, kMaxTurns = 2048, kUnrollMost = 4;
-// Blocks on an SM, which are all that are launched, and tokens of a thread under way at once; us forward / backward on 16 x 96 x 96 tokens, 6 heads.  Words of 8 channels, heads of 32: 56 / 81 (592 blocks in two
-// rounds 61 / 84; two blocks and four tokens forward 60; three blocks backward, whose registers spill, 133).  Words of 4, heads of 24: 61 / 87 (words of 2 there 108 / 149; four tokens forward 67; three blocks and
-// two tokens backward 96).  Words of 2, heads of 20: 108 / 150 (six blocks, whose registers spill, 135 / 220; two tokens 125 / 190).
+// Blocks on an SM, which are all that are launched, and tokens of a thread under way at once; us forward / backward on 16 x 96 x 96 tokens, 6 heads.  Words of 8 channels, heads of 32: 56 / 80 (592 blocks in two
+// rounds 61 / 84; two blocks and four tokens forward 60; three blocks backward, whose registers spill, 133).  Words of 4, heads of 24: 58 / 83 (words of 2 there 108 / 149; four tokens forward 67; three blocks and
+// two tokens backward 96).  Words of 2, heads of 20: 98 / 141 (six blocks, whose registers spill, 135 / 220; two tokens 125 / 190).  Words of 1, heads of 30: 184 / 280.
 constexpr int blocks_of(int V, bool backward) { return V == 8 ? (backward ? 2 : 3) : V == 4 && backward ? 2 : 4; }
 constexpr int unroll_of(int V, bool backward) { return V == 8 || (V == 4 && !backward) ? 2 : 4; }
 
@@ -109,8 +109,10 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
     // this thread: unit of a row of the chunk, and which of the tokens that are walked at once
     int at_once, slot;
     p.by_slots.divmod(threadIdx.x, at_once, slot);               // slots: rows of a chunk x lanes of a row
+    const bool spare = at_once >= p.tokens_at_once;               // (threads that are left over go along with the first token's)
+    if (spare) at_once = 0;
     const int unit = slot & (p.lanes - 1), chunk_row = slot / p.lanes, row = blockIdx.y * p.rows_per_chunk + chunk_row;
-    const bool works = at_once < p.tokens_at_once && row < p.rows;
+    const bool works = !spare && row < p.rows;
     const bool is_k = row >= p.t[0].heads;
     const RopeTensor& t = p.t[is_k ? 1 : 0];
     const int head = is_k ? row - p.t[0].heads : row;
@@ -141,10 +143,15 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
     __nv_bfloat16* y_at = t.y + head * p.d;
     const long long x_stride = t.x_stride, y_stride = t.y_stride;
     const int g_stride = t.heads * p.d;
-    // of the unit's pairs: V that follow one another, or (interleaved) V / 2 of each run
-    const int second = kInterleaved && V > 1 ? p.rot / 4 : V / 2;
-    const float* const cosines = turns + (kInterleaved && V > 1 ? V / 2 * unit : V * unit);
-    const float* const sines = cosines + p.tile * p.pairs;
+    // Where the cosines of the unit's pairs lie - V that follow one another, or (interleaved) V / 2 of each run, `second` apart -, and the sines, and how far from a token to the next one.  Units that are not turned have
+    // ones and zeros of their own, so that all threads go the same way.
+    constexpr bool kTwoRuns = kInterleaved && V > 1;
+    const int second = kTwoRuns ? p.rot / 4 : V / 2, span = kTwoRuns ? p.rot / 4 + V / 2 : V;
+    float* const unturned = turns + 2 * p.tile * p.pairs;
+    const float* const cosines = rotates ? turns + (kTwoRuns ? V / 2 * unit : V * unit) : unturned;
+    const int to_sines = rotates ? p.tile * p.pairs : span, turns_step = rotates ? p.pairs : 0;
+    for (int i = threadIdx.x; i < 2 * span; i += kThreads) unturned[i] = i < span ? 1.f : 0.f;
+    if (!p.rot) __syncthreads();                                 // (else behind the first tile's cosines and sines)
 
     // (what is not there is not loaded, and stays the zero that it is here, or a token's of before, whose results are not kept)
     W xa[kUnroll], xb[kUnroll], ga[kUnroll], gb[kUnroll];
@@ -193,25 +200,20 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
                 const int token = k0 + k * p.tokens_at_once + at_once;
                 const bool there = token < here;
                 float2 c[kTwos], s[kTwos];
-                if (rotates && there) {
-                    const float *cp = cosines + token * p.pairs, *sp = sines + token * p.pairs;
-                    if constexpr (V == 8) {
+                const float *cp = cosines + token * turns_step, *sp = cp + to_sines;
+                if constexpr (V == 8) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float4 u = *reinterpret_cast<const float4*>(cp + i * second), v = *reinterpret_cast<const float4*>(sp + i * second);
-                            c[2 * i] = make_float2(u.x, u.y); c[2 * i + 1] = make_float2(u.z, u.w);
-                            s[2 * i] = make_float2(v.x, v.y); s[2 * i + 1] = make_float2(v.z, v.w);
-                        }
-                    } else if constexpr (V == 4) {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) { c[i] = *reinterpret_cast<const float2*>(cp + i * second); s[i] = *reinterpret_cast<const float2*>(sp + i * second); }
-                    } else {
-                        c[0] = make_float2(cp[0], V > 1 ? cp[second] : 0.f);
-                        s[0] = make_float2(sp[0], V > 1 ? sp[second] : 0.f);
+                    for (int i = 0; i < 2; ++i) {
+                        const float4 u = *reinterpret_cast<const float4*>(cp + i * second), v = *reinterpret_cast<const float4*>(sp + i * second);
+                        c[2 * i] = make_float2(u.x, u.y); c[2 * i + 1] = make_float2(u.z, u.w);
+                        s[2 * i] = make_float2(v.x, v.y); s[2 * i + 1] = make_float2(v.z, v.w);
                     }
-                } else {
+                } else if constexpr (V == 4) {
 #pragma unroll
-                    for (int i = 0; i < kTwos; ++i) { c[i] = twice(1.f); s[i] = twice(0.f); }
+                    for (int i = 0; i < 2; ++i) { c[i] = *reinterpret_cast<const float2*>(cp + i * second); s[i] = *reinterpret_cast<const float2*>(sp + i * second); }
+                } else {
+                    c[0] = make_float2(cp[0], V > 1 ? cp[second] : 0.f);
+                    s[0] = make_float2(sp[0], V > 1 ? sp[second] : 0.f);
                 }
                 const Pairs<V> x = unpack<V, kInterleaved>(xa[k], xb[k]);
                 Pairs<V> z;
@@ -400,7 +402,7 @@ cudaError_t launch(const RopeProblem& p, float* part, const Plan& plan, cudaStre
     a.by_pixels = make_fast_div((int)((long long)p.H * p.W)); a.by_w = make_fast_div(p.W); a.by_pairs = make_fast_div(p.rot ? p.rot / 2 : 1);
     a.by_slots = make_fast_div(plan.rows_per_chunk * plan.lanes);
     const dim3 grid((unsigned)plan.blocks, (unsigned)plan.chunks);
-    size_t smem = sizeof(float2) * plan.tile * a.pairs;                                  // up to 16 KB, or 256 tokens of one row's pairs
+    size_t smem = sizeof(float2) * (plan.tile * a.pairs + p.rot / 4 + plan.V);           // up to 16 KB, or 256 tokens of one row's pairs
     if (kBackward && part && smem < sizeof(float) * kThreads * 2 * plan.V) smem = sizeof(float) * kThreads * 2 * plan.V;
     ProfileScope scope(kBackward ? RIB_KERNEL_QK_NORM_ROPE_BWD : RIB_KERNEL_QK_NORM_ROPE_FWD, stream);
     const auto kernel = plan.V == 8 ? (p.interleaved ? rib_qk_norm_rope_kernel<8, true, kBackward> : rib_qk_norm_rope_kernel<8, false, kBackward>)
