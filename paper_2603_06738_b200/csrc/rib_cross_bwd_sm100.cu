@@ -7,7 +7,7 @@
 // out to several CTAs, whose fp32 sums a last kernel adds.  dQ runs beside dK and dV, on the SMs that those leave free.  A first kernel takes D and brings lse and D into the order in which tiles of rows read them.
 // P and dS enter the products as bf16 (a rounding of 2^-9 of each, as everywhere in this library; dQ's share of it is as large as that of its own last rounding); sums are fp32.  dS in two parts would take
 // that away for a third product and half as many instructions again, where instructions and their latencies are what bounds both kernels:
-// a step of 128 x 64 scores takes 950 cycles in either, 512 of them exponentials.  256 x 256 tokens, 6 heads of 32, to 1024 states, us: statistics 13, dQ 160, dK and dV 157 (exponentials alone: 90 each).
+// a step of 128 x 64 scores takes 950 cycles for dQ and 890 for dK and dV, 512 of them exponentials (an eighth of which on the FMA pipe: 327 -> 340 us).  256 x 256 tokens, 6 heads of 32, to 1024 states, us: statistics 13, dQ 160, dK and dV 146 (exponentials alone: 90 each).
 #include "rib_cross.cuh"
 
 namespace rib {
@@ -29,16 +29,16 @@ __device__ __forceinline__ long long stats_index(const RowStats& s, long long gr
     return (group * s.tiles + tile) * kRowTile + t * s.G + head;
 }
 
-// 32 columns of scores s and dP of a lane -> P and dS as bf16, in the first 16 of them.  x = s scale + neg, P = 2^x held to 1 whatever the roundings of large scores and lse make of it, dS = P (dP + d).
-// 16 columns at a time: P and dS go where columns lie that have been read.  `stats(i)` gives (neg, neg', d, d') of columns 2 i, 2 i + 1; columns from `columns` on weigh nothing, whatever they hold, and
+// 32 columns of scores s and dP of a lane -> dS as bf16, in the first 16 of dP's.  x = s scale + neg, P = 2^x held to 1 whatever the roundings of large scores and lse make of it, dS = P (dP + d).
+// 16 columns at a time: dS goes where columns lie that have been read.  `stats(i)` gives (neg, neg', d, d') of columns 2 i, 2 i + 1; columns from `columns` on weigh nothing, whatever they hold, and
 // chunks that have none of them are left out.
-template <bool kStoreP, typename Stats>
+template <typename Stats>
 __device__ __forceinline__ void weights_in_place(uint32_t t_s, uint32_t t_dp, int columns, float2 scale2, Stats stats)
 {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
         if (16 * g >= columns) break;
-        uint32_t a[16], b[16], pp[8], pd[8];
+        uint32_t a[16], b[16], pd[8];
         tmem_ld16(t_s + 16 * g, a);
         tmem_ld16(t_dp + 16 * g, b);
         tmem_wait_ld();
@@ -53,12 +53,53 @@ __device__ __forceinline__ void weights_in_place(uint32_t t_s, uint32_t t_dp, in
             const float2 x = __ffma2_rn(make_float2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), scale2, make_float2(st.x, st.y));
             const float2 w = make_float2(ex2_approx(min_nan(x.x, 0.f)), ex2_approx(min_nan(x.y, 0.f)));
             const float2 z = __fmul2_rn(w, __fadd2_rn(make_float2(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])), make_float2(st.z, st.w)));
-            pp[i] = pack_bf16x2(w.x, w.y);
             pd[i] = pack_bf16x2(z.x, z.y);
         }
-        if constexpr (kStoreP) tmem_st8(t_s + 8 * g, pp);
         tmem_st8(t_dp + 8 * g, pd);
     }
+    tmem_wait_st();
+}
+// The same for keys on the lanes, 32 keys and 32 rows of a warp in four pieces of 16 x 16 (piece c: lanes 16 (c % 2) .., columns 16 (c / 2) ..), read as 16-lane fragments: a thread has 2 keys and 4 rows of a piece,
+// and takes 16 words of statistics where a key to a thread takes 64 (`stats`: at (-lse, -lse', -D, -D') of its first two rows; 163 -> 152 us on 256 x 256 tokens to 1024 states).
+__device__ __forceinline__ void weights_by_keys(uint32_t t_s, uint32_t t_dp, float2 scale2, const float4* stats)
+{
+    auto load = [&](int c, uint32_t (&a)[8], uint32_t (&b)[8]) {
+        const uint32_t at = ((uint32_t)(16 * (c & 1)) << 16) + 16 * (c >> 1);
+        tmem_ld_16x256b_x2(t_s + at, a);
+        tmem_ld_16x256b_x2(t_dp + at, b);
+    };
+    auto work = [&](int c, const uint32_t (&a)[8], const uint32_t (&b)[8], const float4 (&st)[2]) {
+        uint32_t pp[4], pd[4];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {                 // keys lane / 4 and lane / 4 + 8 of the fragment
+                const int i = 4 * q + 2 * r;
+                const float2 x = __ffma2_rn(make_float2(__uint_as_float(a[i]), __uint_as_float(a[i + 1])), scale2, make_float2(st[q].x, st[q].y));
+                const float2 w = make_float2(ex2_approx(min_nan(x.x, 0.f)), ex2_approx(min_nan(x.y, 0.f)));
+                const float2 z = __fmul2_rn(w, __fadd2_rn(make_float2(__uint_as_float(b[i]), __uint_as_float(b[i + 1])), make_float2(st[q].z, st[q].w)));
+                pp[2 * q + r] = pack_bf16x2(w.x, w.y);
+                pd[2 * q + r] = pack_bf16x2(z.x, z.y);
+            }
+        const uint32_t at = ((uint32_t)(16 * (c & 1)) << 16) + 8 * (c >> 1);
+        tmem_st_16x128b_x2(t_s + at, pp);
+        tmem_st_16x128b_x2(t_dp + at, pd);
+    };
+    uint32_t a0[8], b0[8], a1[8], b1[8];
+    float4 sa[2], sb[2];
+    load(0, a0, b0);
+    load(1, a1, b1);
+    sa[0] = stats[0]; sa[1] = stats[4];
+    tmem_wait_ld();
+    work(0, a0, b0, sa);
+    load(2, a0, b0);
+    sb[0] = stats[8]; sb[1] = stats[12];
+    work(1, a1, b1, sa);
+    tmem_wait_ld();
+    load(3, a1, b1);
+    work(2, a0, b0, sb);
+    tmem_wait_ld();
+    work(3, a1, b1, sb);
     tmem_wait_st();
 }
 // where the K16 step kk of P or dS lies among its 64 columns
@@ -341,8 +382,8 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             const float* stats = stats_entry(reinterpret_cast<float*>(base_ptr + C::kOffStats + slot * C::kStatBytes), row);
             const float neg = stats[0], d = stats[2];
             const auto of_row = [&](int) { return make_float4(neg, neg, d, d); };
-            if (keys == kCrossBlock) weights_in_place<false>(t_s, t_s + 64, 32, scale2, of_row);
-            else weights_in_place<false>(t_s, t_s + 64, keys - 32 * half, scale2, of_row);
+            if (keys == kCrossBlock) weights_in_place(t_s, t_s + 64, 32, scale2, of_row);
+            else weights_in_place(t_s, t_s + 64, keys - 32 * half, scale2, of_row);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::kReady + set));
@@ -551,7 +592,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             if (!mbar_wait_warp(bar(C::kSFull + set), round & 1, abort_flag, p.status) || !mbar_wait_warp(bar(C::kFull + st), (t / kStages) & 1, abort_flag, p.status)) { ok = false; break; }
             tc_fence_after();
             const float4* stats = reinterpret_cast<const float4*>(base_ptr + C::kOffStats + st * C::kStatBytes);
-            weights_in_place<true>(t_s, t_dp, 32, scale2, [&](int i) { return stats[16 * half + i]; });
+            weights_by_keys(t_s, t_dp, scale2, stats + 16 * half + (lane & 3));
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::kReady + set));
