@@ -521,6 +521,8 @@ void rib_tensor_map_cache_counts(long long* hits, long long* misses);
  * returns the number of entries written, or a negative RIB_ERR_* code.  Both calls create or
  * destroy CUDA events: keep them outside stream capture and outside timed regions.  One profiling
  * session per process at a time, driven from one host thread.
+ * (The backward pass of the attention to few states is one kernel for all three gradients, which counts as RIB_KERNEL_CROSS_BWD_DKV.  dQ over more of them runs beside dK and
+ * dV; between events it runs behind.)
  */
 enum { RIB_KERNEL_FWD_MAIN = 1, RIB_KERNEL_BWD_PREPARE = 2, RIB_KERNEL_BWD_MAIN = 3, RIB_KERNEL_BWD_FINISH = 4,
        RIB_KERNEL_RESERVED = 5, RIB_KERNEL_ANY_FWD = 6, RIB_KERNEL_ANY_ROWDOT = 7, RIB_KERNEL_ANY_BWD_DQ = 8,
