@@ -294,7 +294,7 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const int token = c.token0 + row_token;
             const bool mine = row < p.rows_per_tile && token < p.tokens;
             const float inverse = p.splits > 1 && l == 0.f ? 0.f : __fdividef(1.f, l);      // (a run of keys that all weigh nothing adds nothing)
-            float nothing = 0.f;                          // not 0: some output is no number or infinite
+            float2 nothing = make_float2(0.f, 0.f);       // not 0: some output is no number or infinite
             if (p.tma_out) {
                 if (lane == 0) bulk_wait_group_read<0>();      // the rows of before have left
                 __syncwarp();
@@ -309,9 +309,9 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 tmem_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[e] = inverse == 0.f ? 0.f : __uint_as_float(o[e]) * inverse;
-                if (l > 0x1p20f) {
+                if (fast) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) nothing = fmaf(__uint_as_float(o[e]), 0.f, nothing);
+                    for (int e = 0; e < 16; e += 2) nothing = __ffma2_rn(make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), make_float2(0.f, 0.f), nothing);
                 }
                 if (p.tma_out) {
                     // (stores of threads that have a row each touch 32 lines apiece and held up the load-store unit for 1500 to 2900 cycles an item)
@@ -337,8 +337,8 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 }
             }
             if (fast) {
-                // a score left the range that the fixed reference covers, or large weights times large values overflowed (with weights of up to 2^20 the exact form would overflow as well)
-                const bool bad = mine && (!(l > 0.f && l < 0x1p100f) || nothing != 0.f);
+                // a score left the range that the fixed reference covers, or weights times values overflowed, for which a weight above those of the item's first keys is enough: looked for in every row
+                const bool bad = mine && (!(l > 0.f && l < 0x1p100f) || nothing.x + nothing.y != 0.f);
                 if (__any_sync(0xffffffffu, bad) && lane == 0) {
                     const int slot = atomicAdd(redo_count, 1);
                     if (slot < kMaxRedo) redo_list[slot] = ordinal;
