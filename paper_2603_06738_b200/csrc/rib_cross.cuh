@@ -44,6 +44,8 @@ constexpr int kCrossBlock = 64;           // keys of a block
 // Rows of a group (tokens x heads that share a head of keys) up to which the forward pass takes the plain pipes.  Plain pipes / tensor cores, us with the join: 1 row, 64 contexts of up to 4096, 6 heads
 // of 32 35 / 63; 2 rows, 64 x 4096, 6 heads of keys of 32 65 / 99, 16 x 4096, 2 of 64 25 / 26; 4 rows, 16 x 4096, 2 of 64 31 / 26; 8 rows 45 / 25.
 constexpr int kCrossFewRows = 2;
+// Weights are held down by a power of two, 2^-cross_bits(their number), where they are added up with values: every sum is then one of a weighted mean and stays in range if the values do.
+inline int cross_bits(long long n) { int b = 0; while ((1ll << b) < n) ++b; return b; }
 // States up to which the forward pass takes a row's scores at once (rib_cross_short_sm100.cu has both sides); 128 columns of tensor memory for each of four tiles are all there is.
 constexpr int kCrossShort = 128;
 

@@ -11,7 +11,7 @@
 //   fp32 and bf16 carry 8 exponent bits, so weights up to 2^100 relative to the reference are as exact as those below 1.  A row whose sum says that its scores left that range (more than 69 above
 //   the reference, in nats; infinities, NaN) or whose values overflowed makes its item be noted, and
 //   Exact form (second pass of the same launch): a running maximum over both halves, which they tell each other through shared memory, and which moves, and with it O and the row's sum, when a
-//   block exceeds it by more than 2^8 in the exponentials.
+//   block exceeds it by more than 2^8 in the exponentials.  Its weights are held down by 2^8 times the number of states, so that no sum of them times values passes the largest value.
 // An eighth of the exponentials is taken on the FMA pipe, which has the time: 256 x 256 tokens to 1024 states 127 us, with none 132, with a quarter 127; heads of 64, 128 x 128 tokens 41 and 44.
 // (256 x 256 tokens to 1024 states, us: a thread to a row, blocks of 64 keys, one warp for all loads and products 170; the exact form for every item 179; the fast one, then without the FMA pipe, 135.)
 // Three buffers of scores rotate among the (block, tile) units, so that the scores of one tile are taken under the other's exponentials, and an item's output
@@ -53,7 +53,7 @@ struct Params {
     int d, L, heads, kv_heads, G, rows_per_tile, tokens_per_tile, blocks_per_split, splits, items, vector, tma_out, exact_only;      // items: pairs of tiles x splits x groups
     int tokens, shared;                  // tokens of a context; shared: one context, several maps
     long long rows, groups;
-    float scale_log2, inv_sqrt_d;
+    float scale_log2, inv_sqrt_d, bits;  // bits: the exact form's weights, up to 2^8 each, are held down by 2^bits
     FastDiv by_pairs, by_splits, by_kv, by_pixels, by_group;
     int pixels;
 };
@@ -345,7 +345,7 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 }
             }
             if (mine && half == 0) {
-                const float lse = m * p.inv_sqrt_d + __logf(l);
+                const float lse = m * p.inv_sqrt_d + (__logf(l) + (fast ? 0.f : p.bits * 0.6931471805599453f));
                 if (p.splits > 1) {
                     p.part_lse[(long long)c.group * p.rows + token * p.G + row_head] = l == 0.f ? -INFINITY : lse;
                 } else if (p.lse) {
@@ -472,7 +472,7 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     }
                 }
                 // (exact form: the difference first, which is exact at the largest score however large that is; otherwise scores beyond 1e9 lose their row to the rounding of -m scale, and come here)
-                const float minus = fast ? 0.f : -m, below = fast ? -m * p.scale_log2 : 0.f;
+                const float minus = fast ? 0.f : -m, below = fast ? -m * p.scale_log2 : -p.bits;
                 const float2 minus2 = make_float2(minus, minus), neg2 = make_float2(below, below);
                 float2 sum_a = make_float2(0.f, 0.f), sum_b = make_float2(0.f, 0.f);
                 auto weights = [&](const uint32_t (&s)[16], uint32_t (&packed)[8], bool any) {
@@ -585,6 +585,7 @@ struct JoinParams {
     __nv_bfloat16* out;
     float* lse;
     int splits, stride, d, heads, kv_heads, G, chunks, vector, pixels;
+    float down, up;                      // of the splits' weights: 2^-cross_bits(splits), and back
     long long groups, rows, tokens;
     FastDiv by_pixels;
 };
@@ -624,7 +625,7 @@ __global__ void __launch_bounds__(128) rib_cross_join_kernel(const JoinParams p)
 #pragma unroll
         for (int s = 0; s < kAtOnce; ++s) {
             if (lse[s] == -INFINITY) continue;           // (no keys, or none that weighs anything)
-            const float w = expf(lse[s] - most);
+            const float w = expf(lse[s] - most) * p.down;
             total += w;
             x[0] += w * lo[s].x; x[1] += w * lo[s].y; x[2] += w * lo[s].z; x[3] += w * lo[s].w;
             x[4] += w * hi[s].x; x[5] += w * hi[s].y; x[6] += w * hi[s].z; x[7] += w * hi[s].w;
@@ -648,7 +649,7 @@ __global__ void __launch_bounds__(128) rib_cross_join_kernel(const JoinParams p)
     if (p.lse && chunk == 0) {
         int image, pixel;
         p.by_pixels.divmod((int)pixel_of_all, image, pixel);
-        p.lse[((long long)image * p.heads + head) * p.pixels + pixel] = none ? -INFINITY : most + logf(total);
+        p.lse[((long long)image * p.heads + head) * p.pixels + pixel] = none ? -INFINITY : most + logf(total * p.up);
     }
 }
 
@@ -691,7 +692,7 @@ cudaError_t launch_fwd(const CrossProblem& p, const CrossPlan& plan, float* part
     a.blocks_per_split = plan.blocks_per_split; a.splits = plan.splits; a.items = plan.groups * plan.splits * plan.pairs;
     a.vector = p.d % 8 == 0; a.tma_out = tma_out; a.exact_only = p.exact_softmax;
     a.tokens = (int)p.tokens; a.shared = p.tokens != p.pixels; a.rows = plan.rows; a.groups = plan.groups;
-    a.scale_log2 = 1.4426950408889634f / sqrtf((float)p.d); a.inv_sqrt_d = 1.f / sqrtf((float)p.d);
+    a.scale_log2 = 1.4426950408889634f / sqrtf((float)p.d); a.inv_sqrt_d = 1.f / sqrtf((float)p.d); a.bits = 8.f + (float)cross_bits(p.L);
     a.by_pairs = make_fast_div(plan.pairs); a.by_splits = make_fast_div(plan.splits); a.by_kv = make_fast_div(p.kv_heads);
     a.by_pixels = make_fast_div((int)p.pixels); a.by_group = make_fast_div(plan.G); a.pixels = (int)p.pixels;
     const int grid = a.items < kCrossSms ? a.items : kCrossSms;
@@ -705,6 +706,7 @@ cudaError_t join(const CrossProblem& p, const CrossPlan& plan, const float* part
     j.part_out = part_out; j.part_lse = part_lse; j.lengths = p.lengths; j.out = p.out_w; j.lse = p.lse_w;
     j.splits = plan.splits; j.stride = stride; j.d = p.d; j.heads = p.heads; j.kv_heads = p.kv_heads; j.G = plan.G; j.chunks = (p.d + 7) / 8;
     j.vector = p.d % 8 == 0; j.pixels = (int)p.pixels; j.groups = plan.groups; j.rows = plan.rows; j.tokens = p.tokens; j.by_pixels = make_fast_div((int)p.pixels);
+    j.up = (float)(1 << cross_bits(plan.splits)); j.down = 1.f / j.up;
     const bool eight = plan.splits > 8;
     const long long threads = j.groups * j.rows * j.chunks * (eight ? 8 : 1);
     ProfileScope scope(RIB_KERNEL_CROSS_JOIN, stream);

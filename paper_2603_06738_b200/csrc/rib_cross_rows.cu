@@ -20,7 +20,7 @@ struct RowsParams {
     float *lse, *part_out, *part_lse;    // splits > 1: [splits][groups][rows][stride], [splits][groups][rows]
     int d, width, L, heads, kv_heads, G, tokens, rows, splits, shared, pixels, vector, stride;
     long long groups;
-    float scale_log2;
+    float scale_log2, down, bits;        // down = 2^-bits: factor of the weights
 };
 
 __device__ __forceinline__ void unpack8(const uint4& w, float (&x)[8])
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kThreads) rib_cross_rows_kernel(const __grid_c
 #pragma unroll
             for (int c = 0; c < 8; ++c) o[r][c] *= factor;
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) { s[r][u] = ex2_approx(s[r][u] - most); l[r] += s[r][u]; }
+            for (int u = 0; u < kUnroll; ++u) { s[r][u] = ex2_approx(s[r][u] - most) * p.down; l[r] += s[r][u]; }
         }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) rib_cross_rows_kernel(const __grid_c
         }
         const bool none = first == last;                 // (a run of keys that all weigh nothing adds nothing either)
         const bool empty = none || (p.splits > 1 && total == 0.f);
-        const float y = empty ? 0.f : x / total, lse = empty ? -INFINITY : (most + __log2f(total)) * 0.6931471805599453f;
+        const float y = empty ? 0.f : x / total, lse = empty ? -INFINITY : (most + (__log2f(total) + p.bits)) * 0.6931471805599453f;
         const int token = r / p.G, head = kv * p.G + r % p.G;
         if (p.splits > 1) {
             const long long at = ((long long)split * p.groups + group) * p.rows + r;
@@ -168,6 +168,8 @@ cudaError_t cross_fwd_rows(const CrossProblem& p, const CrossPlan& plan, float* 
     a.q = p.q; a.k = p.k; a.v = p.v; a.lengths = p.lengths; a.out = p.out_w; a.lse = p.lse_w; a.part_out = part_out; a.part_lse = part_lse;
     a.d = p.d; a.width = p.width; a.L = p.L; a.heads = p.heads; a.kv_heads = p.kv_heads; a.G = plan.G; a.tokens = (int)p.tokens; a.rows = (int)plan.rows; a.splits = plan.splits;
     a.shared = p.tokens != p.pixels; a.pixels = (int)p.pixels; a.stride = stride; a.groups = plan.groups; a.scale_log2 = 1.4426950408889634f / sqrtf((float)p.d);
+    const int bits = cross_bits(p.L);
+    a.bits = (float)bits; a.down = 1.f / (float)(1ll << bits);
     const unsigned blocks = (unsigned)(plan.groups * plan.splits);
     ProfileScope scope(RIB_KERNEL_CROSS_FWD, stream);
     return p.width <= 8 ? launch_lanes<1>(a, blocks, stream) : p.width <= 16 ? launch_lanes<2>(a, blocks, stream) : p.width <= 32 ? launch_lanes<4>(a, blocks, stream) : launch_lanes<8>(a, blocks, stream);

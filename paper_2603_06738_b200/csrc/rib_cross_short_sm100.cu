@@ -21,6 +21,8 @@ using namespace sm100;
 
 constexpr int kThreads = 640, kRows = 128, kSlots = 4;
 constexpr uint32_t kTmemCols = 512, kSlotCols = 128, kColO = 64;
+constexpr float kBits = 7.f;             // weights are held down by 2^7 >= kCrossShort
+static_assert(kCrossShort <= 128, "2^kBits states");
 
 template <int DP> struct Cfg {
     static constexpr uint32_t kTiles = DP == 32 ? 6 : 4;                                           // ring of row tiles
@@ -225,7 +227,7 @@ rib_cross_short_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 auto weights = [&](const auto& a, auto& packed) {
 #pragma unroll
                     for (int i = 0; i < (int)(sizeof(a) / 8); ++i) {
-                        const float2 x = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), neg2), scale2);
+                        const float2 x = __ffma2_rn(__fadd2_rn(make_float2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), neg2), scale2, make_float2(-kBits, -kBits));
                         const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         if (i & 1) sum_b = __fadd2_rn(sum_b, e); else sum_a = __fadd2_rn(sum_a, e);
                         packed[i] = pack_bf16x2(e.x, e.y);
@@ -324,7 +326,7 @@ rib_cross_short_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
             if (p.lse && mine) {
                 int image = at.context, pixel = token;
                 if (p.shared) p.by_pixels.divmod(token, image, pixel);
-                p.lse[(long long)(image * p.heads + head) * p.pixels + pixel] = most * p.inv_sqrt_d + __logf(l);
+                p.lse[(long long)(image * p.heads + head) * p.pixels + pixel] = most * p.inv_sqrt_d + (__logf(l) + kBits * 0.6931471805599453f);
             }
             __syncwarp();
         }
