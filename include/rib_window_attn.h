@@ -491,7 +491,7 @@ int rib_qk_norm_rope_bwd(const void* q, long long q_stride, const void* k, long 
  *   out and lse are the forward results.  dq, dk, dv in the layout of q, k, v, overwritten.  All sums are fp32 in a fixed order: results are the same from run to run.
  *   P and dS are rounded to bf16 for the products.  Probabilities recomputed from lse are held to 1.
  * Both calls take scratch: workspace of at least rib_cross_attn_fwd_workspace / _bwd_workspace bytes (may be 0: NULL then), 256-byte aligned, as for rib_window_attn_bwd.
- * Limits: d <= 64, heads / kv_heads <= 64, B H W heads and contexts L kv_heads below 2^31 (RIB_ERR_UNSUPPORTED), L >= 1.  d that is no multiple of 8 runs on
+ * Limits: d <= 64, heads / kv_heads <= 64, B H W heads and contexts L kv_heads below 2^31, L at most 2^31 - 4096 (RIB_ERR_UNSUPPORTED), L >= 1.  d that is no multiple of 8 runs on
  * copies in the workspace filled up with zero channels.  rib_set_path(RIB_PATH_SM100_EXACT) has the exact form of the softmax taken for every item
  * over more than 128 states (for fewer, and for one or two rows to a group, there is no other); its other settings have no effect.
  */

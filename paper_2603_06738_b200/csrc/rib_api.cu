@@ -903,7 +903,7 @@ int cross_problem(int B, int H, int W, int heads, int kv_heads, int d, int L, in
     if (d > 64 || heads / kv_heads > 64) return RIB_ERR_UNSUPPORTED;
     if (int rc = check_tokens(B, H, W, heads)) return rc;
     const __int128 states = (__int128)contexts * L * kv_heads;
-    if (states > 0x7fffffffLL || L > 0x7fffff00) return RIB_ERR_UNSUPPORTED;
+    if (states > 0x7fffffffLL || L > 0x7ffff000) return RIB_ERR_UNSUPPORTED;      // (kernels count on beyond the last state: by 1183 runs' roundings, by 1024 keys of a block under way)
     *p = rib::CrossProblem{};
     p->B = B; p->heads = heads; p->kv_heads = kv_heads; p->d = d; p->L = L; p->contexts = contexts;
     p->pixels = (long long)H * W; p->tokens = contexts == B ? p->pixels : B * p->pixels;
