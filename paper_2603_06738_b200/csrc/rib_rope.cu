@@ -98,8 +98,16 @@ template <int V, bool kInterleaved> __device__ __forceinline__ void pack(const P
 }
 __device__ __forceinline__ float2 twice(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 negated(float2 x) { return make_float2(-x.x, -x.y); }
+// x = c x + t where the unit is turned; where it is not, x stays as it is, whatever t holds: the zeros of such a unit times an infinite neighbour are NaN.  (Predicated: no instruction more.)
+template <bool kWhole> __device__ __forceinline__ void turn(float2& x, float2 c, float2 t, bool turned)
+{
+    if constexpr (kWhole) { x = __ffma2_rn(c, x, t); return; }
+    asm("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %3, 0;\n\t@p fma.rn.f32x2 %0, %1, %0, %2;\n\t}"
+        : "+l"(reinterpret_cast<unsigned long long&>(x)) : "l"(reinterpret_cast<const unsigned long long&>(c)), "l"(reinterpret_cast<const unsigned long long&>(t)), "r"((int)turned));
+}
 
-template <int V, bool kInterleaved, bool kBackward>
+// kWhole: every channel is turned (rot = d); units that are not are lanes without channels.
+template <int V, bool kInterleaved, bool kBackward, bool kWhole>
 __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm_rope_kernel(const __grid_constant__ RopeParams p)
 {
     constexpr int kUnroll = unroll_of(V, kBackward), kTwos = (V + 1) / 2, kFill = V == 8 && !kBackward ? 3 : 1;      // kFill: entries of the tile's cosines and sines that a thread has under way
@@ -224,8 +232,9 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
                     const Pairs<V> g = unpack<V, kInterleaved>(ga[k], gb[k]);
 #pragma unroll
                     for (int i = 0; i < kTwos; ++i) {            // back by the transposed rotation
-                        z.a[i] = __ffma2_rn(c[i], g.a[i], __fmul2_rn(s[i], g.b[i]));
-                        z.b[i] = __ffma2_rn(c[i], g.b[i], __fmul2_rn(negated(s[i]), g.a[i]));
+                        z.a[i] = g.a[i]; z.b[i] = g.b[i];
+                        turn<kWhole>(z.a[i], c[i], __fmul2_rn(s[i], g.b[i]), rotates);
+                        turn<kWhole>(z.b[i], c[i], __fmul2_rn(negated(s[i]), g.a[i]), rotates);
                         along = __ffma2_rn(__fmul2_rn(z.b[i], w.b[i]), x.b[i], __ffma2_rn(__fmul2_rn(z.a[i], w.a[i]), x.a[i], along));
                     }
                 }
@@ -248,14 +257,15 @@ __global__ void __launch_bounds__(kThreads, blocks_of(V, kBackward)) rib_qk_norm
                 } else {
 #pragma unroll
                     for (int i = 0; i < kTwos; ++i) {
-                        const float2 na = __fmul2_rn(__fmul2_rn(x.a[i], inverse2), w.a[i]), nb = __fmul2_rn(__fmul2_rn(x.b[i], inverse2), w.b[i]);
-                        z.a[i] = __ffma2_rn(c[i], na, __fmul2_rn(negated(s[i]), nb));
-                        z.b[i] = __ffma2_rn(c[i], nb, __fmul2_rn(s[i], na));
+                        z.a[i] = __fmul2_rn(__fmul2_rn(x.a[i], inverse2), w.a[i]); z.b[i] = __fmul2_rn(__fmul2_rn(x.b[i], inverse2), w.b[i]);
+                        const float2 ta = __fmul2_rn(negated(s[i]), z.b[i]), tb = __fmul2_rn(s[i], z.a[i]);
+                        turn<kWhole>(z.a[i], c[i], ta, rotates);
+                        turn<kWhole>(z.b[i], c[i], tb, rotates);
                     }
                 }
                 if (there) {
                     W ya, yb;
-                    if (!kBackward && !norm && !rotates) { ya = xa[k]; yb = xb[k]; }      // (as it was, NaN and all)
+                    if (!kWhole && !kBackward && !norm && !rotates) { ya = xa[k]; yb = xb[k]; }      // (as it was, NaN and all)
                     else pack<V, kInterleaved>(z, ya, yb);
                     __nv_bfloat16* dst = y_at + (token0 + token) * y_stride;
                     if (has_a) *reinterpret_cast<W*>(dst + ca) = ya;
@@ -405,10 +415,14 @@ cudaError_t launch(const RopeProblem& p, float* part, const Plan& plan, cudaStre
     size_t smem = sizeof(float2) * (plan.tile * a.pairs + p.rot / 4 + plan.V);           // up to 16 KB, or 256 tokens of one row's pairs
     if (kBackward && part && smem < sizeof(float) * kThreads * 2 * plan.V) smem = sizeof(float) * kThreads * 2 * plan.V;
     ProfileScope scope(kBackward ? RIB_KERNEL_QK_NORM_ROPE_BWD : RIB_KERNEL_QK_NORM_ROPE_FWD, stream);
-    const auto kernel = plan.V == 8 ? (p.interleaved ? rib_qk_norm_rope_kernel<8, true, kBackward> : rib_qk_norm_rope_kernel<8, false, kBackward>)
-                      : plan.V == 4 ? (p.interleaved ? rib_qk_norm_rope_kernel<4, true, kBackward> : rib_qk_norm_rope_kernel<4, false, kBackward>)
-                      : plan.V == 2 ? (p.interleaved ? rib_qk_norm_rope_kernel<2, true, kBackward> : rib_qk_norm_rope_kernel<2, false, kBackward>)
-                                    : (p.interleaved ? rib_qk_norm_rope_kernel<1, true, kBackward> : rib_qk_norm_rope_kernel<1, false, kBackward>);
+    const auto kernel_of = [&](auto whole) {
+        constexpr bool kWhole = decltype(whole)::value;
+        return plan.V == 8 ? (p.interleaved ? rib_qk_norm_rope_kernel<8, true, kBackward, kWhole> : rib_qk_norm_rope_kernel<8, false, kBackward, kWhole>)
+             : plan.V == 4 ? (p.interleaved ? rib_qk_norm_rope_kernel<4, true, kBackward, kWhole> : rib_qk_norm_rope_kernel<4, false, kBackward, kWhole>)
+             : plan.V == 2 ? (p.interleaved ? rib_qk_norm_rope_kernel<2, true, kBackward, kWhole> : rib_qk_norm_rope_kernel<2, false, kBackward, kWhole>)
+                           : (p.interleaved ? rib_qk_norm_rope_kernel<1, true, kBackward, kWhole> : rib_qk_norm_rope_kernel<1, false, kBackward, kWhole>);
+    };
+    const auto kernel = p.rot == p.d ? kernel_of(std::true_type{}) : kernel_of(std::false_type{});
     return launch_overtaking(kernel, grid, kThreads, smem, stream, a);
 }
 
