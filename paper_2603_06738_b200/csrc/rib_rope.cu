@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(256) rib_qk_norm_rope_sum_kernel(const RopeSum
 }
 
 // Angles are products of whole numbers and 32-bit frequencies, exact in 64 bits; their cosine and sine are rounded once.
-__global__ void __launch_bounds__(128) rib_rope_table_kernel(const float* __restrict__ frequencies, int H, int W, int pairs, long long y0, long long x0, float magnitude, float2* __restrict__ table)
+__global__ void __launch_bounds__(128) rib_rope_table_kernel(const float* frequencies, int H, int W, int pairs, long long y0, long long x0, float magnitude, float2* table)
 {
     const long long e = (long long)blockIdx.x * 128 + threadIdx.x;
     if (e >= ((long long)H + W) * pairs) return;
