@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(256) rib_qk_norm_rope_sum_kernel(const RopeSum
     }
 }
 
-// Angles are products of whole numbers and 32-bit frequencies, exact in 64 bits; their cosine and sine are rounded once.
+// Angles are products of whole numbers (42 bits) and 32-bit frequencies (24 bits): the product in 64 bits (53), and beyond 2^29 what it leaves, exactly; their cosine and sine are rounded once.
 __global__ void __launch_bounds__(128) rib_rope_table_kernel(const float* frequencies, int H, int W, int pairs, long long y0, long long x0, float magnitude, float2* table)
 {
     const long long e = (long long)blockIdx.x * 128 + threadIdx.x;
@@ -348,8 +348,16 @@ __global__ void __launch_bounds__(128) rib_rope_table_kernel(const float* freque
     const int i = (int)(e - row * pairs);
     const bool column = row >= H;
     cudaGridDependencySynchronize();                             // it may have overtaken the kernel before
+    const double position = (double)(column ? x0 + row - H : y0 + row), frequency = (double)frequencies[column ? pairs + i : i], angle = position * frequency;
     double sine, cosine;
-    sincos((double)(column ? x0 + row - H : y0 + row) * (double)frequencies[column ? pairs + i : i], &sine, &cosine);
+    sincos(angle, &sine, &cosine);
+    if (fabs(position) > 0x1p29) {
+        double sine_left, cosine_left;
+        sincos(fma(position, frequency, -angle), &sine_left, &cosine_left);
+        const double s = sine;
+        sine = s * cosine_left + cosine * sine_left;
+        cosine = cosine * cosine_left - s * sine_left;
+    }
     const double scale = column ? 1.0 : (double)magnitude;
     table[e] = make_float2((float)(scale * cosine), (float)(scale * sine));
 }
