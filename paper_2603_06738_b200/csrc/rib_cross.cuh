@@ -6,7 +6,7 @@
 // tokens, which is the same memory.  heads / kv_heads = G query heads share a head of keys and values; the rows of a (context, kv head) group are its
 // tokens times its G heads, token by token, and that is one TMA box {d, G heads, 128 / G tokens} per tile of up to 128 rows.
 // Every kernel may start under the one before it on the stream, waits for its end before it reads what that may have written, and reads that by plain loads: the read-only path is for what nothing writes while
-// a kernel is there.
+// a kernel is there.  The one exception is dQ over long sequences (rib_cross_bwd_sm100.cu), which runs beside the kernel before it, reads nothing of it, and relies on that one's wait.
 #pragma once
 #include "rib_sm100_common.cuh"
 

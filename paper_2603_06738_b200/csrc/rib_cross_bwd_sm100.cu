@@ -222,7 +222,7 @@ __device__ __forceinline__ DqItem decode(const DqParams& p, int item)
     p.by_tiles.divmod(item, item, c.tile);
     p.by_splits.divmod(item, c.group, c.split);
     p.by_kv.divmod(c.group, c.context, c.kv);
-    c.length = p.lengths ? min(max(p.lengths[c.context], 0), p.L) : p.L;
+    c.length = p.lengths ? min(max(__ldcg(p.lengths + c.context), 0), p.L) : p.L;      // (past L1: the kernel waits for nobody)
     c.first = c.split * p.blocks_per_split;
     c.blocks = max(0, min(c.first + p.blocks_per_split, (c.length + kCrossBlock - 1) / kCrossBlock) - c.first);
     return c;
@@ -263,7 +263,9 @@ rib_cross_bwd_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
-    // (It runs beside the kernel for dK and dV, which let it start when statistics and copies were there: nothing to wait for but at the end.)
+    // It runs beside the kernel for dK and dV, the one before it in the stream, and waits for that only at its end.  What it reads - statistics, padded copies, lengths, the caller's tensors - is of kernels before
+    // that one, which have ended and whose writes have reached L2: every CTA of dK and dV says so by starting this kernel behind its own wait for them, not before.  All reads here go to L2 (TMA, bulk copies, loads
+    // past L1).  So the trigger stays behind that wait, and no kernel comes between the two launches.
 
     if (warp == 24) {
         // ============================================ loads
@@ -508,7 +510,7 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
     cudaGridDependencySynchronize();                      // it may have overtaken the kernel before: statistics, copies
-    cudaTriggerProgrammaticLaunchCompletion();            // dQ needs no more than those, and has SMs that this kernel leaves free
+    cudaTriggerProgrammaticLaunchCompletion();            // dQ needs no more than those, and has SMs that this kernel leaves free (it does not wait for them itself: never before the line above)
     int rest = blockIdx.x;
     const int split = rest % p.splits; rest /= p.splits;
     const int key_tile = rest % p.key_tiles, group = rest / p.key_tiles, context = group / p.kv_heads, kv = group - context * p.kv_heads;
