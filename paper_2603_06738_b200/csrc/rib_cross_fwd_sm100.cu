@@ -218,9 +218,6 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 for (int t = 0; t < 2; ++t) {
                     // the scores overwrite the columns that P V of three units before, one of the other tile, reads P from: it has completed
                     const uint32_t before = blk - 2 + t;
-                    // (The tiles take turns on the special-function units if the second one begins when the first is through with its first exponentials.  In step, their warps wait for scores and
-                    // maxima all at once.)
-                    if (t == 1 && blk == 0 && c.blocks >= 4 && !mbar_wait_warp(on_block(kPReady, 0, 0), 0, abort_flag, p.status)) { ok = false; break; }
                     if (!mbar_wait_warp(on_block(kPVDone, t ^ 1, before), parity(before), abort_flag, p.status)) { ok = false; break; }
                     tc_fence_after();
                     if (elect_one()) {
