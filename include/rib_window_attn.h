@@ -446,12 +446,12 @@ int rib_window_attn_bwd_bucketed_checkpointed(const rib_checkpoint* saved, const
  *     xhat = x / sqrt(mean_c x_c^2 + eps),   z = weight o xhat,   y = R z,
  * where R turns pairs of the first `rot` channels, channels (2i, 2i + 1) if `interleaved` and (i, i + rot / 2) if not, by the angle
  *     (y0 + Y) f[0][i] + (x0 + X) f[1][i]
- * of the token at row Y, column X of its map, and leaves the other channels as they are.  One axis alone (a sequence) is a map of one column.
+ * of the token at row Y, column X of its map, and leaves the other channels as they are, whatever they hold.  One axis alone (a sequence) is a map of one column.
  *
  * rib_rope_table takes the cosines and sines of the map's rows and columns, which a program makes once for its map (Sec. 3.1 treats Pq and Pk the same way):
  *   frequencies : fp32 [2][pairs], pairs = rot / 2.   table : fp32 [H + W][pairs][2], overwritten; those of the rows times `magnitude`, a factor of y's rotated
- *                 channels (1, or the temperature that scaled frequencies go with).
- *   Angles are taken in 64 bits, so that far positions (|y0|, |x0| up to 2^40) keep their digits.
+ *                 channels (1, or the temperature that scaled frequencies go with).  The rows come first, and a table says nothing of how many they are: that of an 8 x 4 map is not that of a 4 x 8 one.
+ *   Angles are exact, so that far positions (|y0|, |x0| up to 2^40) keep their digits; their cosines and sines are rounded to 32 bits.
  * rib_qk_norm_rope_fwd:
  *   q, k        : bf16, token t of a tensor at element t * q_stride (k_stride), its heads behind one another ([heads][d], [kv_heads][d]): slices of the output of one
  *                 projection need no copy.  Strides at least heads * d.  k may be NULL (kv_heads = 0).  Aligned to 2 bytes; the widest words that pointers,
@@ -487,6 +487,7 @@ int rib_qk_norm_rope_bwd(const void* q, long long q_stride, const void* k, long 
  *   lse         : fp32 [B][heads][H][W], natural log of sum_j exp(S_ij); may be NULL.
  * A map without states (length 0) has out 0 and lse minus infinity, and passes no gradient on.  A row whose logits are all minus infinity though it has states is NaN, as
  * SoftMax has it.
+ * Sums of weights times values are held in range: results are finite for values of up to 3.3e38, whatever the weights are before they are normalised.
  * Backward, given dout: dv, dk over the rows of the heads (and, with one context, the maps) that share them; dk and dv of states behind a length are 0.
  *   out and lse are the forward results.  dq, dk, dv in the layout of q, k, v, overwritten.  All sums are fp32 in a fixed order: results are the same from run to run.
  *   P and dS are rounded to bf16 for the products.  Probabilities recomputed from lse are held to 1.

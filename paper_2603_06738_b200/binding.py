@@ -1061,8 +1061,8 @@ def rib_generate_features_bwd(w_h, b_h, w_pq, w_pk, dpq, dpk, window, stream=Non
 
 
 def rib_rope_frequencies(rot, base=100.0, sequence=False, scaling=None, scale=1.0, trained=None, device="cuda"):
-    """Frequencies fp32 [2, rot / 2] for rib_rope_table: geometric from 1 down to 1 / base, the first half of the pairs (the larger, when their number is odd) along
-    the rows and the second along the columns; with `sequence` all along the rows.  For maps larger than those a model was trained on, by a factor `scale`:
+    """Frequencies fp32 [2, rot / 2] for rib_rope_table: the i-th of the n pairs of an axis turns by base^(-i / n), from 1 down to a little above 1 / base; the
+    first half of the pairs (the larger, when their number is odd) turns along the rows and the second along the columns; with `sequence` all along the rows.  For maps larger than those a model was trained on, by a factor `scale`:
     `scaling` "linear" divides every frequency by it, "base" raises the base such that the lowest frequency is divided by it and the highest is kept, and
     "by_parts" divides those that turn less than once over `trained` positions, keeps those that turn more than 32 times, and goes over linearly in between."""
     if rot < 2 or rot % 2 or not base > 0 or not scale > 0:
@@ -1087,7 +1087,8 @@ def rib_rope_frequencies(rot, base=100.0, sequence=False, scaling=None, scale=1.
 
 def rib_rope_table(frequencies, H, W, y0=0, x0=0, magnitude=1.0, stream=None):
     """Cosines and sines of a map's rows and columns, fp32 [H + W, rot / 2, 2], from frequencies fp32 [2, rot / 2] (per row, per column); (y0, x0) is the place of the
-    map's first token, `magnitude` a factor of the rotated channels.  A sequence of L tokens is a map of L rows and one column."""
+    map's first token, `magnitude` a factor of the rotated channels.  A sequence of L tokens is a map of L rows and one column.  The first H entries are the rows, and nothing in a table's
+    shape says how many they are: it serves maps of these H and W, not of W and H."""
     if stream is not None and _elsewhere(stream):
         return _beside(stream, rib_rope_table, frequencies, H, W, y0, x0, magnitude)
     if _marshal is not None:

@@ -41,8 +41,9 @@ struct CrossPlan {
 
 constexpr int kCrossSms = 148;            // the same number everywhere, so that a call's shape decides the launch
 constexpr int kCrossBlock = 64;           // keys of a block
-// Rows of a group (tokens x heads that share a head of keys) up to which the forward pass takes the plain pipes.  Plain pipes / tensor cores, us with the join: 1 row, 64 contexts of up to 4096, 6 heads
-// of 32 35 / 63; 2 rows, 64 x 4096, 6 heads of keys of 32 65 / 99, 16 x 4096, 2 of 64 25 / 26; 4 rows, 16 x 4096, 2 of 64 31 / 26; 8 rows 45 / 25.
+// Rows of a group (tokens x heads that share a head of keys) up to which the forward pass takes the plain pipes.  Plain pipes / tensor cores, us with the join: 64 contexts of 64 to 4096 states, 6 heads
+// of keys of 32, 1 row 31 / 80, 2 rows 35 / 81; 16 contexts of 256 to 4096, 2 heads of 64, 1 row 12 / 17, 2 rows 12 / 18, 4 rows 18.5 / 17.5, 8 rows 33 / 17.
+// (Figures of whole calls here and in the kernels' files, where nothing else is said: us of a call among others, each behind a write of 256 MB, which is still on its way to memory while the call reads.)
 constexpr int kCrossFewRows = 2;
 // Weights are held down by a power of two, 2^-cross_bits(their number), where they are added up with values: every sum is then one of a weighted mean and stays in range if the values do.
 inline int cross_bits(long long n) { int b = 0; while ((1ll << b) < n) ++b; return b; }

@@ -5,7 +5,7 @@
 // Each computes P for itself: an exponential more per score than one kernel for all three would take, and no sum of dQ over key tiles in memory, so that
 // every sum has one order and the results are the same from run to run.  Where there are too few tiles to fill the card, keys (dQ) or rows (dK, dV) are dealt
 // out to several CTAs, whose fp32 sums a last kernel adds.  dQ runs beside dK and dV, on the SMs that those leave free.  A first kernel takes D and brings lse and D into the order in which tiles of rows read them.
-// P and dS enter the products as bf16 (a rounding of 2^-9 of each, as everywhere in this library; dQ's share of it is as large as that of its own last rounding); sums are fp32.  dS in two parts would take
+// P and dS enter the products as bf16 (a rounding of at most 2^-8 of each, as everywhere in this library; dQ's share of it is as large as that of its own last rounding); sums are fp32.  dS in two parts would take
 // that away for a third product and half as many instructions again, where instructions and their latencies are what bounds both kernels:
 // a step of 128 x 64 scores takes 950 cycles for dQ and 890 for dK and dV, 512 of them exponentials (an eighth of which on the FMA pipe: 327 -> 340 us).  256 x 256 tokens, 6 heads of 32, to 1024 states, us: statistics 13, dQ 160, dK and dV 146 (exponentials alone: 90 each).
 #include "rib_cross.cuh"
@@ -644,7 +644,8 @@ rib_cross_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
 // ------------------------------------------------------------------------------------ sums of the splits
 struct SumTensor { const float* part; __nv_bfloat16* dst; long long rows; int splits, G, heads; long long rows_of_group, tokens; };      // rows of all groups; dst [contexts][tokens][heads][d], heads = groups of a context x G
 struct SumParams { SumTensor t[3]; int d, stride, chunks, vector, blocks; };      // blocks: of a tensor
-// kLanes threads have eight channels of a row; with eight of them each takes every eighth split, and they meet in a fixed order.
+// kLanes threads have eight channels of a row; with eight of them each takes every eighth split, and they meet in a fixed order.  (Backward with one / eight, us of the call alone: 4 x 64 x 64 tokens, 6 heads of 32, to
+// 200 states, 6 splits, 33 / 37; 10 x 64 x 64 to one dictionary of 128, 24 splits, 40 / 38; 180 x 320 to 77, also 24, 46 / 44.)
 template <int kLanes>
 __global__ void __launch_bounds__(256) rib_cross_bwd_sum_kernel(const __grid_constant__ SumParams p)
 {

@@ -574,8 +574,9 @@ rib_cross_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     }
 }
 
-// Joins the splits of a row: out = sum_s w_s out_s / sum_s w_s, w_s = exp(lse_s - max lse).  kLanes threads have eight channels of a row; with eight of them each takes
-// every eighth split, and they meet in a fixed order (one token, 6 heads, 64 splits of 8192 states: 17 -> 9 us).
+// Joins the splits of a row: out = sum_s w_s out_s / sum_s w_s, w_s = exp(lse_s - max lse).  kLanes threads have eight channels of a row; with eight of them, from nine
+// splits on, each takes every eighth split, and they meet in a fixed order.  (The forward pass with one / eight, us of the call alone: 16 x 16 tokens, heads of 32, 4 splits 17 / 28, 8 splits 17 / 21, 12 splits 18 / 20,
+// 16 splits 18.6 / 19.2, 24 splits 19.4 / 18.8, 37 splits 23 / 18; one token, 6 heads, 64 splits of 8192 states 21 / 13.)
 struct JoinParams {
     const float *part_out, *part_lse;
     const int* lengths;
@@ -760,7 +761,9 @@ CrossPlan cross_plan(const CrossProblem& p)
     c.pairs = (c.tiles + 1) / 2;
     split((long long)c.groups * c.pairs, (p.L + kKeys - 1) / kKeys, &c.splits, &c.blocks_per_split);
     c.few_rows = c.rows <= kCrossFewRows;
-    if (c.few_rows) {      // eight blocks to an SM, of 128 keys or more
+    // Eight blocks to an SM, of 128 keys or more.  Four of them are resident, and the second four even out what lengths of their own leave idle.  Us with four / eight / sixteen: 64 contexts of 64 to 4096 states,
+    // 6 heads of 32, 37 / 31 / 33; all of 4096 45 / 49 / 49; two rows there 47 / 35 / 35; 16 contexts of 256 to 4096, 2 heads of 64, 10 / 12 / 12; 16 of 63 to 1000, 6 heads of 32, 8 / 10 / 10; 256 contexts 35 / 35 / 37.
+    if (c.few_rows) {
         const long long most = 8 * kCrossSms / c.groups, runs = (p.L + 127) / 128;
         c.splits = (int)(most < 1 ? 1 : most < runs ? most : runs);
     }

@@ -1,7 +1,7 @@
 // Forward pass of the attention to states (rib_cross.cuh) for a group of few rows - single tokens that are served, each over a long context of its own - on the plain pipes.
 //
 // With R rows to a group (tokens x heads that share a head of keys) there are 4 R d flops for the 4 d bytes of a key and its value: memory bounds it, and a tensor-core tile of 128 rows would be
-// mostly empty (a tile takes the exponentials of all its rows' warps: 64 single tokens, 6 heads of 32, up to 4096 states 63 us, these kernels 29).
+// mostly empty (a tile takes the exponentials of all its rows' warps: 64 single tokens, 6 heads of 32, to 64 to 4096 states 80 us, this kernel and the join 31).
 // A block has a run of a group's keys; a key belongs to d / 8 lanes of a warp (rounded up to a power of two), 16 bytes of K and V each, kUnroll keys of a lane under way at once.  Every group of lanes
 // keeps a running maximum, sum and output of its own for each row, all in 32 bits and P unrounded; lanes, warps and runs are joined at the end, in a fixed order.
 #include "rib_cross.cuh"

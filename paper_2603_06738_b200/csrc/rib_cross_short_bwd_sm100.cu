@@ -5,7 +5,7 @@
 //     dV += P^T dO                           (A from tensor memory)
 //     dK += dS^T Q                           (A = dS in shared memory, K-major)
 //     dQ  = dS K                             (A = the same tile, MN-major: two tiles of 64 rows are its 128 lanes; over one or two blocks of keys)
-// P and dS enter the products as bf16 (a rounding of 2^-9 of each, as everywhere in this library); statistics and sums are fp32.
+// P and dS enter the products as bf16 (a rounding of at most 2^-8 of each, as everywhere in this library); statistics and sums are fp32.
 //
 // A CTA has a group of rows and keys and a run of the group's row tiles, two by two.  Unit of the pipeline is (row tile, block of 128 keys); three buffers of S^T and two of dP^T rotate among the units, and
 // two sets of arithmetic warps take the even and the odd row tiles, so that one set's exponentials run under the other's products.  D is taken here as well, by four warps of their own.
@@ -13,8 +13,8 @@
 // What sets the pace is the loop  scores -> arithmetic -> dV -> next scores of the buffer  (1800 cycles of issue, products and barriers, 2150 of arithmetic) over the three units in flight: 1375 cycles a
 // unit of 128 keys and 64 rows, of which exponentials take 512 and the products 300.  With statistics by two warps and S^T and dP^T issued by a warp each it was 1650, with dP^T beside dQ 1700; O in registers
 // instead of beside dO 1450; a third buffer of dP^T, where there is one block of keys, takes 2 %.
-// With the sums that follow, us: 16 x 96 x 96 tokens, 6 heads of 32, to 16 to 256 states 128 (the statistics, dQ, dK and dV, and sums of the long form, each a kernel: 222), 10 x 64 x 64 to one dictionary of 128
-// 42 (75), 180 x 320 to 77 48 (92).
+// With the sums that follow, us: 16 x 96 x 96 tokens, 6 heads of 32, to 16 to 256 states 119 (the statistics, dQ, dK and dV, and sums of the long form, each a kernel: 204), 10 x 64 x 64 to one dictionary of 128
+// 31 (54), 180 x 320 to 77 37 (70), to 256 66 (103).
 //
 // Roles (896 threads): warps 0-15 arithmetic (0-7 even, 8-15 odd row tiles; then dV and dK), 16 loads, 17 S^T and dP^T, 18 dV and dK (and owns the tensor memory), 19 dQ, 20-23 store dQ, 24-27 lse and D.
 // Every wait is bounded (tests/test_cross_short_barriers.py is a model of them).
@@ -497,8 +497,9 @@ cudaError_t launch(const CrossProblem& p, const CrossPlan& plan, float* part_dk,
 
 cudaError_t cross_bwd_short(const CrossProblem& p, const CrossPlan& plan, float* part_dk, float* part_dv, cudaStream_t stream)
 {
-    // One or two blocks of keys, as the contexts' lengths have it: CTAs of two first, so that none of them begins last (16 x 96 x 96 tokens, 6 heads of 32, to 16 to 256 states in no order 117 us, 137 as they come).
-    // With many contexts their order evens out by itself.
+    // One or two blocks of keys, as the contexts' lengths have it: CTAs of two first, so that none of them begins last.  Every CTA ranks the contexts for itself, which costs more than it gives when they are many.
+    // Us of the call alone, two blocks first / as they come, lengths spread evenly up to 256 in no order: 4 contexts of 128 x 128 tokens, 6 heads of 32 78 / 77, 16 of 96 x 96 126 / 152, 32 of 48 x 48 88 / 95,
+    // 64 of 48 x 48, 4 heads, 93 / 111, 96 of 32 x 32, 6 heads, 104 / 108, 128 of 32 x 32, 4 heads, 98 / 96, 256 of 24 x 24 133 / 127, 512 of 16 x 16 190 / 152.
     const bool long_first = p.lengths && p.L > kKeys && p.contexts > 1 && p.contexts <= 64;
     return p.d > 32 ? launch<64, false>(p, plan, part_dk, part_dv, stream) : long_first ? launch<32, true>(p, plan, part_dk, part_dv, stream) : launch<32, false>(p, plan, part_dk, part_dv, stream);
 }

@@ -7,8 +7,8 @@
 // with four softmax warps of its own that have a row to a thread, take the tiles in turn; inside a slot everything runs one after the other (scores, softmax, product, output), and the
 // four fill one another's waits.  P lies in the first half of the scores' columns, O from column 64 on, where scores have been read.
 // What bounds it is the instructions of a row beside its exponentials (waits, masks, output) and the 64-byte rows of its loads and stores, not the bytes, which would take 7 us on 180 x 320 tokens, 6 heads
-// of 32, to 77 states.  That takes 22 here, and 39 in the kernel for long sequences, whose items are two tiles and whose rows have two threads that have to meet; 128 states 27 and 41, 64 x 64 x 64
-// tokens to 128 80 and 137, a small map of 16 x 16 10 and 12.
+// of 32, to 77 states.  That takes 18 here, and 34 in the kernel for long sequences, whose items are two tiles and whose rows have two threads that have to meet; 128 states 21 and 35, 64 x 64 x 64
+// tokens to 128 74 and 127, a small map of 16 x 16 4 and 6.
 //
 // Roles (640 threads): warps 4 s .. 4 s + 3 softmax and output of slot s, warp 16 loads, warp 17 issues S, warp 18 P V (and owns the tensor memory).  Every wait is bounded
 // (tests/test_cross_short_barriers.py is a model of them).

@@ -10,7 +10,7 @@
 // of a row share its sums by shuffles.  A block takes tiles of tokens and puts their cosines and sines into shared memory first, once for all heads.
 // (Plain loads, not the read-only path: a kernel may start under the one that makes its inputs, and waits for its end.)
 // (A thread to a token that walks the heads, table entries in registers: 32 lines touched by every access and few of them in flight, 16 x 96 x 96 tokens, 6 heads of 32, forward and backward 172 us
-// against 136 now.)
+// against 137 now.)
 #include "rib_common.cuh"
 #include "rib_sm100_common.cuh"
 
@@ -21,9 +21,10 @@ using sm100::FastDiv;
 using sm100::make_fast_div;
 
 constexpr int kThreads = 256, kMaxTurns = 2048, kUnrollMost = 4;
-// Blocks on an SM, which are all that are launched, and tokens of a thread under way at once; us forward / backward on 16 x 96 x 96 tokens, 6 heads.  Words of 8 channels, heads of 32: 56 / 80 (592 blocks in two
-// rounds 61 / 84; two blocks and four tokens forward 60; three blocks backward, whose registers spill, 133).  Words of 4, heads of 24: 58 / 83 (words of 2 there 108 / 149; four tokens forward 67; three blocks and
-// two tokens backward 96).  Words of 2, heads of 20: 98 / 141 (six blocks, whose registers spill, 135 / 220; two tokens 125 / 190).  Words of 1, heads of 30: 184 / 280.
+// Blocks on an SM, which are all that are launched, and tokens of a thread under way at once; us forward / backward on 16 x 96 x 96 tokens, 6 heads.  Words of 8 channels, heads of 32: 54 / 83 (592 blocks in two
+// rounds 61 / 84; two blocks and four tokens forward 60; three blocks backward, whose registers spill, 133).  Words of 4, heads of 24: 58 / 85 (words of 2 there 108 / 149; four tokens forward 67; three blocks and
+// two tokens backward 96).  Words of 2, heads of 20: 97 / 142 (six blocks, whose registers spill, 135 / 220; two tokens 125 / 190).  Words of 1, heads of 30: 181 / 282.  All of these are turned as a whole;
+// half of heads of 32 56 / 83, 16 of heads of 24 54 / 79, 12 of heads of 20 106 / 151.
 constexpr int blocks_of(int V, bool backward) { return V == 8 ? (backward ? 2 : 3) : V == 4 && backward ? 2 : 4; }
 constexpr int unroll_of(int V, bool backward) { return V == 8 || (V == 4 && !backward) ? 2 : 4; }
 
