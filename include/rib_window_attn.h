@@ -24,6 +24,8 @@
  *   lse                            : fp32  [B][heads][H][W]      natural log of sum_j exp(S_ij)
  *   dpq, dpk                       : fp32  [n][r]                summed over batch, windows, heads
  * Raw q and Pq are passed; the library applies 1/sqrt(d) and 1/sqrt(r) itself.
+ * In windows, weights of up to 2^8 are added up with values in fp32 before they are normalised: values beyond 3.4e38 / (256 n)
+ * (1.3e33 for windows of 32) may give infinities where their weighted mean is finite.
  *
  * Calls only ENQUEUE work on `stream` (a cudaStream_t passed as void*; NULL = default stream)
  * and return without synchronising.  They return RIB_OK (0) or a negative RIB_ERR_* code; on an
